@@ -290,6 +290,80 @@ int qgbdt_build_histograms_noalloc(const uint8_t *d_bins, int64_t n_rows, int32_
                                    int64_t n, qgbdt_bin *d_hist, int32_t *d_status, void *stream);
 const char *qgbdt_noalloc_last_error(void);
 
+/* ---- Operators on top of the trees ---------------------------------------------------------------
+ * The leaf a row reaches in every tree of a trained model is a list of categorical tokens (leaf l of
+ * tree k is entry k * num_leaves + l of a table).  The calls below are the training step of a softmax
+ * classifier over such tokens, for class counts far beyond what one tree per class allows: the sum of
+ * the leaves' embeddings, the softmax cross entropy over the classes, both with their gradients, and
+ * the clipping of the gradients by their global norm.  None needs a loaded bin matrix or reads the
+ * training parameters.  (The paper has no counterpart.)
+ *  - Element types are given per call (QGBDT_F32, _BF16, _F16); sums, softmax statistics and norms are
+ *    held in at least 32 bits and rounded once, when an output is written.  Equal inputs give equal
+ *    bits: no result depends on the order of atomics.
+ *  - ld_* are row strides in elements; any stride >= the row length and any alignment to the element is
+ *    accepted (16-byte aligned rows are the fast case).
+ *  - All calls are asynchronous on `stream`.  They share one work buffer of the context, which grows
+ *    with the largest call (growing synchronises); calls on different streams are ordered after one
+ *    another by an event.  A call whose buffer is large enough may be captured into a CUDA graph;
+ *    replays of that graph are not ordered against other calls, order them yourself.
+ *  - d_status: optional device word that the caller clears; set to 1 when a token was >= n_entries or a
+ *    label >= n_classes (such tokens count as missing, such rows as rows without a label). */
+#define QGBDT_F32 0
+#define QGBDT_BF16 1
+#define QGBDT_F16 2
+#define QGBDT_I32 0
+#define QGBDT_I64 1
+
+/* Embedding bag: d_out[i] = scale * sum over k < bag of d_table[d_tokens[i][k]], i < n_rows, in
+ * ascending k; a negative token is a missing one (a row of missing tokens gives zeros).  bag = 1 is the
+ * plain scaled lookup.  d_table [n_entries][ld_table] and d_out [n_rows][ld_out] of `type`, d_tokens
+ * [n_rows][ld_tokens] of `token_type`.  d_out must not overlap d_table.  rows * bag < 2^31. */
+int qgbdt_embed(qgbdt_ctx *ctx, const void *d_table, int32_t type, int64_t n_entries, int32_t dim, int64_t ld_table,
+                const void *d_tokens, int32_t token_type, int64_t n_rows, int32_t bag, int64_t ld_tokens, float scale,
+                void *d_out, int64_t ld_out, int32_t *d_status, void *stream);
+/* Its gradient: d_grad_table[v] = scale * sum of d_grad[i] over all (i, k) with d_tokens[i][k] == v.
+ * Every row of d_grad_table [n_entries][ld_grad_table] is written, zeros where no token points.  The
+ * tokens are sorted and the sums taken in an order that the tokens alone decide. */
+int qgbdt_embed_backward(qgbdt_ctx *ctx, const void *d_grad, int32_t type, int64_t ld_grad, const void *d_tokens,
+                         int32_t token_type, int64_t n_rows, int32_t bag, int64_t ld_tokens, float scale,
+                         void *d_grad_table, int64_t n_entries, int32_t dim, int64_t ld_grad_table, int32_t *d_status,
+                         void *stream);
+
+/* Softmax cross entropy of a linear classifier: z[i][v] = d_hidden[i] . d_weight[v] + d_bias[v],
+ * lse[i] = log sum exp z[i], losses[i] = lse[i] - z[i][label i], loss = the mean of losses over the rows
+ * with a label.  A negative label marks a row without one: it takes no part, its losses and lse are 0,
+ * and what its hidden row holds is never used.  Without any labelled row the loss is 0.  The logits are
+ * worked out a tile at a time and never stored.  d_hidden [n_rows][dim] and d_weight [n_classes][dim]
+ * both QGBDT_BF16 or both QGBDT_F16; d_bias [n_classes] or NULL (an entry of -infinity excludes its
+ * class); d_labels [n_rows] of `label_type`; outputs in single precision: d_loss [1], d_losses [n_rows]
+ * or NULL, d_lse [n_rows]. */
+int qgbdt_softmax_ce(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_hidden, const void *d_weight, int64_t ld_weight,
+                     int32_t type, const float *d_bias, const void *d_labels, int32_t label_type, int64_t n_rows,
+                     int64_t n_classes, int32_t dim, float *d_loss, float *d_losses, float *d_lse, int32_t *d_status,
+                     void *stream);
+/* Gradients of grad_loss * loss (d_grad_loss: one float in device memory, e.g. a loss scale; NULL: 1),
+ * with lse as the forward call gave it: g[i][v] = (exp(z[i][v] - lse[i]) - [v == label i]) * grad_loss /
+ * (rows with a label), d_grad_hidden = g d_weight, d_grad_weight = g^T d_hidden, d_grad_bias = column
+ * sums of g (or NULL).  d_grad_hidden and d_grad_weight have the inputs' type; rows without a label get
+ * zeros.  The logits are recomputed in pieces of the classes; the probabilities of a piece are held in
+ * the inputs' type in the work buffer (at most 256 MiB of them, or one piece of 256 classes). */
+int qgbdt_softmax_ce_backward(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_hidden, const void *d_weight,
+                              int64_t ld_weight, int32_t type, const float *d_bias, const void *d_labels,
+                              int32_t label_type, int64_t n_rows, int64_t n_classes, int32_t dim, const float *d_lse,
+                              const float *d_grad_loss, void *d_grad_hidden, int64_t ld_grad_hidden,
+                              void *d_grad_weight, int64_t ld_grad_weight, float *d_grad_bias, int32_t *d_status,
+                              void *stream);
+
+/* Global gradient norm and clipping: *d_norm = sqrt of the sum of the squares of all elements of all
+ * tensors (sums in double precision), then every tensor is multiplied by min(1, max_norm / norm).
+ * h_grads, h_counts, h_types [n_tensors] are HOST arrays (read before the call returns) of device
+ * pointers, element counts (0 allowed) and element types; h_out likewise: where the clipped tensors go,
+ * NULL or the same pointers for in place (a tensor must not overlap another one's output).  In place
+ * nothing is written when the norm is within max_norm.  A norm that is not finite is reported and the
+ * tensors keep their values.  max_norm may be infinite (the norm alone) and 0. */
+int qgbdt_clip_grad_norm(qgbdt_ctx *ctx, const void *const *h_grads, void *const *h_out, const int64_t *h_counts,
+                         const int32_t *h_types, int32_t n_tensors, double max_norm, float *d_norm, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -26,7 +27,14 @@ EXPORTS = [
     "qgbdt_get_leaf_rows", "qgbdt_reset_leaves", "qgbdt_refit_leaves", "qgbdt_apply_leaf_values", "qgbdt_train", "qgbdt_train_host",
     "qgbdt_set_distributed", "qgbdt_set_option", "qgbdt_get_info", "qgbdt_get_counters", "qgbdt_profile_histograms", "qgbdt_get_histogram_profile", "qgbdt_get_timings",
     "qgbdt_build_histograms_noalloc", "qgbdt_noalloc_last_error",
+    "qgbdt_embed", "qgbdt_embed_backward", "qgbdt_softmax_ce", "qgbdt_softmax_ce_backward", "qgbdt_clip_grad_norm",
 ]
+
+# element and index types of the operators on top of the trees
+F32, BF16, F16 = 0, 1, 2
+I32, I64 = 0, 1
+_ELEMENT = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_INDEX = {torch.int32: I32, torch.int64: I64}
 
 
 class QgbdtError(RuntimeError):
@@ -69,6 +77,12 @@ def load_library() -> C.CDLL:
         lib = C.CDLL(LIB_PATH)
         lib.qgbdt_last_error.restype = C.c_char_p
         lib.qgbdt_last_error.argtypes = [C.c_void_p]
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        lib.qgbdt_embed.argtypes = [p, p, i32, i64, i32, i64, p, i32, i64, i32, i64, C.c_float, p, i64, p, p]
+        lib.qgbdt_embed_backward.argtypes = [p, p, i32, i64, p, i32, i64, i32, i64, C.c_float, p, i64, i32, i64, p, p]
+        lib.qgbdt_softmax_ce.argtypes = [p, p, i64, p, i64, i32, p, p, i32, i64, i64, i32, p, p, p, p, p]
+        lib.qgbdt_softmax_ce_backward.argtypes = [p, p, i64, p, i64, i32, p, p, i32, i64, i64, i32, p, p, p, i64, p, i64, p, p, p]
+        lib.qgbdt_clip_grad_norm.argtypes = [p, p, p, p, p, i32, C.c_double, p, p]
         _lib = lib
     return _lib
 
@@ -326,6 +340,162 @@ def build_histograms_noalloc(bins: torch.Tensor, n_bins: int, gq: torch.Tensor, 
                                             _dptr(hist), _dptr(status), _stream(stream))
     if rc != OK:
         raise QgbdtError(rc, lib.qgbdt_noalloc_last_error().decode())
+
+
+class SoftmaxCE(NamedTuple):
+    """Outputs of Context.softmax_ce, float32: loss [1], losses [N], lse [N]."""
+    loss: torch.Tensor
+    losses: torch.Tensor
+    lse: torch.Tensor
+
+
+def _need(ok: bool, what: str):
+    if not ok:
+        raise QgbdtError(ERR_ARG, what)
+
+
+def _raw_stream(t: torch.Tensor, stream) -> int:
+    return torch.cuda.current_stream(t.device).cuda_stream if stream is None else stream.cuda_stream
+
+
+def _matrix(t, name: str) -> torch.Tensor:
+    """A CUDA matrix whose rows are contiguous (any row stride); a single column or row may have any stride there."""
+    _need(t.is_cuda and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "%s must be a CUDA matrix with contiguous rows" % name)
+    return t
+
+
+def _ld(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _tokens(tokens) -> tuple:
+    _need(tokens.is_cuda and tokens.dtype in _INDEX and tokens.dim() in (1, 2), "tokens must be a CUDA tensor [N] or [N, bag] of int32 or int64")
+    if tokens.dim() == 1:
+        return tokens.shape[0], 1, (tokens.stride(0) if tokens.shape[0] > 1 else 1)
+    _need(tokens.shape[1] <= 1 or tokens.stride(1) == 1, "the tokens of a row must be contiguous")
+    return tokens.shape[0], tokens.shape[1], _ld(tokens)
+
+
+def _status_ptr(status):
+    _need(status is None or (status.is_cuda and status.dtype == torch.int32 and status.numel() >= 1), "status must be a CUDA int32 tensor")
+    return None if status is None else status.data_ptr()
+
+
+def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, stream=None) -> torch.Tensor:
+    """qgbdt_embed: out[i] = scale * sum_k table[tokens[i, k]].  table [V, D] (float32, bfloat16 or float16), tokens
+    [N] or [N, bag] (int32 or int64, negative = missing); out [N, D] of the table's type is made if not given."""
+    _matrix(table, "table")
+    n, bag, ldt = _tokens(tokens)
+    _need(table.dtype in _ELEMENT, "table must be float32, bfloat16 or float16")
+    if out is None:
+        out = torch.empty((n, table.shape[1]), dtype=table.dtype, device=table.device)
+    _need(_matrix(out, "out").shape == (n, table.shape[1]) and out.dtype == table.dtype, "out must be [N, D] of the table's type")
+    _need(table.device == tokens.device == out.device, "tensors of different devices")
+    self._check(self.lib.qgbdt_embed(self.h, table.data_ptr(), _ELEMENT[table.dtype], table.shape[0], table.shape[1], _ld(table),
+                                     tokens.data_ptr(), _INDEX[tokens.dtype], n, bag, ldt, scale, out.data_ptr(), _ld(out),
+                                     _status_ptr(status), _raw_stream(table, stream)))
+    return out
+
+
+def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None, stream=None) -> torch.Tensor:
+    """qgbdt_embed_backward: the table's gradient [n_entries, D] of grad_out's type, every row of it written."""
+    _matrix(grad_out, "grad_out")
+    n, bag, ldt = _tokens(tokens)
+    _need(grad_out.dtype in _ELEMENT, "grad_out must be float32, bfloat16 or float16")
+    _need(grad_out.shape[0] == n, "grad_out and tokens differ in rows")
+    if grad_table is None:
+        grad_table = torch.empty((n_entries, grad_out.shape[1]), dtype=grad_out.dtype, device=grad_out.device)
+    _need(_matrix(grad_table, "grad_table").shape == (n_entries, grad_out.shape[1]) and grad_table.dtype == grad_out.dtype,
+          "grad_table must be [n_entries, D] of grad_out's type")
+    _need(grad_out.device == tokens.device == grad_table.device, "tensors of different devices")
+    self._check(self.lib.qgbdt_embed_backward(self.h, grad_out.data_ptr(), _ELEMENT[grad_out.dtype], _ld(grad_out), tokens.data_ptr(),
+                                              _INDEX[tokens.dtype], n, bag, ldt, scale, grad_table.data_ptr(), n_entries,
+                                              grad_out.shape[1], _ld(grad_table), _status_ptr(status), _raw_stream(grad_out, stream)))
+    return grad_table
+
+
+def _check_softmax(hidden, weight, labels, bias):
+    _matrix(hidden, "hidden")
+    _matrix(weight, "weight")
+    _need(hidden.dtype == weight.dtype and hidden.dtype in (torch.bfloat16, torch.float16), "hidden and weight must both be bfloat16 or float16")
+    _need(hidden.shape[1] == weight.shape[1], "hidden and weight differ in columns")
+    _need(labels.is_cuda and labels.dtype in _INDEX and labels.shape == (hidden.shape[0],) and labels.is_contiguous(),
+          "labels must be a contiguous CUDA tensor [N] of int32 or int64")
+    _need(bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (weight.shape[0],) and bias.is_contiguous()),
+          "bias must be a contiguous float32 CUDA tensor [V]")
+    _need(hidden.device == weight.device == labels.device and (bias is None or bias.device == hidden.device), "tensors of different devices")
+
+
+def _softmax_ce(self, hidden, weight, labels, bias=None, status=None, stream=None) -> SoftmaxCE:
+    """qgbdt_softmax_ce: softmax cross entropy of hidden [N, D] @ weight [V, D]^T + bias [V] against labels [N] (negative:
+    no label), mean over the labelled rows, without stored logits.  hidden, weight bfloat16 or float16, bias float32."""
+    _check_softmax(hidden, weight, labels, bias)
+    n = hidden.shape[0]
+    r = SoftmaxCE(*(torch.empty(k, dtype=torch.float32, device=hidden.device) for k in (1, n, n)))
+    self._check(self.lib.qgbdt_softmax_ce(self.h, hidden.data_ptr(), _ld(hidden), weight.data_ptr(), _ld(weight), _ELEMENT[hidden.dtype],
+                                          None if bias is None else bias.data_ptr(), labels.data_ptr(), _INDEX[labels.dtype], n,
+                                          weight.shape[0], hidden.shape[1], r.loss.data_ptr(), r.losses.data_ptr(), r.lse.data_ptr(),
+                                          _status_ptr(status), _raw_stream(hidden, stream)))
+    return r
+
+
+def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss=None, grad_hidden=None, grad_weight=None,
+                         status=None, stream=None) -> tuple:
+    """qgbdt_softmax_ce_backward: (grad_hidden [N, D], grad_weight [V, D], grad_bias [V] or None) of grad_loss * loss;
+    lse as softmax_ce gave it, grad_loss a float32 CUDA tensor of one element (None: 1)."""
+    _check_softmax(hidden, weight, labels, bias)
+    n, v = hidden.shape[0], weight.shape[0]
+    _need(lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (n,) and lse.is_contiguous(), "lse must be a contiguous float32 CUDA tensor [N]")
+    _need(grad_loss is None or (grad_loss.is_cuda and grad_loss.dtype == torch.float32 and grad_loss.numel() == 1),
+          "grad_loss must be a float32 CUDA tensor of one element")
+    if grad_hidden is None:
+        grad_hidden = torch.empty((n, hidden.shape[1]), dtype=hidden.dtype, device=hidden.device)
+    if grad_weight is None:
+        grad_weight = torch.empty((v, hidden.shape[1]), dtype=hidden.dtype, device=hidden.device)
+    _need(_matrix(grad_hidden, "grad_hidden").shape == hidden.shape and grad_hidden.dtype == hidden.dtype, "grad_hidden must be like hidden")
+    _need(_matrix(grad_weight, "grad_weight").shape == weight.shape and grad_weight.dtype == hidden.dtype, "grad_weight must be like weight")
+    grad_bias = None if bias is None else torch.empty(v, dtype=torch.float32, device=hidden.device)
+    self._check(self.lib.qgbdt_softmax_ce_backward(
+        self.h, hidden.data_ptr(), _ld(hidden), weight.data_ptr(), _ld(weight), _ELEMENT[hidden.dtype],
+        None if bias is None else bias.data_ptr(), labels.data_ptr(), _INDEX[labels.dtype], n, v, hidden.shape[1], lse.data_ptr(),
+        None if grad_loss is None else grad_loss.data_ptr(), grad_hidden.data_ptr(), _ld(grad_hidden), grad_weight.data_ptr(),
+        _ld(grad_weight), None if grad_bias is None else grad_bias.data_ptr(), _status_ptr(status), _raw_stream(hidden, stream)))
+    return grad_hidden, grad_weight, grad_bias
+
+
+def _pointers(tensors, what: str) -> np.ndarray:
+    _need(all(t.is_cuda and t.is_contiguous() for t in tensors), "%s must be contiguous CUDA tensors" % what)
+    return np.array([t.data_ptr() for t in tensors], np.uint64)
+
+
+def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """qgbdt_clip_grad_norm: the global norm (float32 tensor [1]) of a list of tensors, and every tensor times
+    min(1, max_norm / norm), in place or into the tensors of `out`.  float32, bfloat16 and float16 may be mixed."""
+    grads = list(grads)
+    n = len(grads)
+    types = [_ELEMENT.get(t.dtype, -1) for t in grads]
+    _need(-1 not in types, "gradients must be float32, bfloat16 or float16")
+    src = _pointers(grads, "gradients")
+    sizes = [t.numel() for t in grads]
+    dst = src
+    if out is not None:
+        out = list(out)
+        _need(len(out) == n and [t.numel() for t in out] == sizes and [t.dtype for t in out] == [t.dtype for t in grads],
+              "out must match the gradients in number, sizes and types")
+        dst = _pointers(out, "out")
+    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty(1, dtype=torch.float32, device=device)
+    counts, kinds = np.array(sizes, np.int64), np.array(types, np.int32)
+    self._check(self.lib.qgbdt_clip_grad_norm(self.h, src.ctypes.data, dst.ctypes.data, counts.ctypes.data, kinds.ctypes.data, n,
+                                              max_norm, norm.data_ptr(), _raw_stream(norm, stream)))
+    return norm
+
+
+Context.embed = _embed
+Context.embed_backward = _embed_backward
+Context.softmax_ce = _softmax_ce
+Context.softmax_ce_backward = _softmax_ce_backward
+Context.clip_grad_norm = _clip_grad_norm
 
 
 def unpack_hist(hist: torch.Tensor) -> tuple[np.ndarray, np.ndarray]:

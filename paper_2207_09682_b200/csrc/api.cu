@@ -351,6 +351,7 @@ int qgbdt_destroy(qgbdt_ctx *c) {
     dev_free(c->d_leaf_table);
     dev_free(c->d_leaf_value);
     dev_free(c->d_leaf_w);
+    qg_ops_destroy(c);
     if (c->h_pinned) cudaFreeHost(c->h_pinned);
     for (cudaEvent_t e : c->hist_events) cudaEventDestroy(e);
     delete c;

@@ -1,0 +1,258 @@
+// Global gradient norm over many tensors, and clipping.
+//
+//   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)
+//
+// Two launches: the first takes the sum of squares (one double per block), the second adds the blocks'
+// sums in a fixed order (every block for itself: 1184 doubles out of L2), and multiplies.  Bound by
+// memory traffic: every tensor is read once, and read and written once more when the norm is above
+// max_norm.  The second launch walks the chunks backwards, so that what the first one read last is
+// still in L2.
+//
+// A tensor is cut into chunks of 4096 elements counted from its first 16-byte boundary (the elements
+// before it ride with the first chunk); blocks take chunks in turn and find a chunk's tensor by a binary
+// search over the tensors' first chunk numbers, which lie with the pointers in the kernel's parameters.
+// Squares are added in double precision: single precision would overflow from |g| = 1.8e19 on and lose
+// everything below 1e-23, and the double-precision units have the throughput to spare here.
+#include "ops_internal.cuh"
+
+namespace {
+
+constexpr int CLIP_THREADS = 256;
+constexpr int CLIP_CHUNK = 4096;
+constexpr int CLIP_SMALL = 64, CLIP_LARGE = 1000;   // tensors per launch (parameters of 1.6 or 25 KB)
+
+template <int CAP>
+struct ClipTable {
+    const void *in[CAP];
+    long long count[CAP];      // elements | type << 56
+    int first[CAP];            // first chunk
+    int n, chunks;
+};
+template <int CAP>
+struct ClipOut {
+    void *out[CAP];
+};
+
+template <int CAP>
+__device__ __forceinline__ int find_tensor(const ClipTable<CAP> &t, int chunk) {
+    int lo = 0, hi = t.n;   // t.first[lo] <= chunk < t.first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.first[mid] <= chunk) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Elements of a chunk: a scalar head (first chunk only), then [begin, end) from a 16-byte boundary.
+struct ChunkRange {
+    long long begin, end;
+    int head;
+};
+
+__device__ __forceinline__ ChunkRange chunk_range(const void *p, int width, long long count, int k) {
+    ChunkRange r;
+    const int off = (int)(reinterpret_cast<uintptr_t>(p) & 15);
+    long long peel = off ? (16 - off) / width : 0;
+    if (peel > count) peel = count;
+    r.head = k == 0 ? (int)peel : 0;
+    r.begin = peel + (long long)k * CLIP_CHUNK;
+    r.end = r.begin + CLIP_CHUNK;
+    if (r.end > count) r.end = count;
+    if (r.begin > count) r.begin = count;
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ double sum_squares(const T *p, const ChunkRange &r) {
+    constexpr int V = 16 / sizeof(T);
+    double s = 0.0;
+    if ((int)threadIdx.x < r.head) {
+        const double x = (double)OpsType<T>::load(p[threadIdx.x]);
+        s = fma(x, x, s);
+    }
+    const int n = (int)(r.end - r.begin), nv = n / V;
+    const OpsVec<T, V> *q = reinterpret_cast<const OpsVec<T, V> *>(p + r.begin);
+    if (nv == CLIP_CHUNK / V) {
+        OpsVec<T, V> x[CLIP_CHUNK / V / CLIP_THREADS];
+#pragma unroll
+        for (int i = 0; i < CLIP_CHUNK / V / CLIP_THREADS; ++i) x[i] = q[threadIdx.x + i * CLIP_THREADS];
+#pragma unroll
+        for (int i = 0; i < CLIP_CHUNK / V / CLIP_THREADS; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const double y = (double)OpsType<T>::load(x[i].v[j]);
+                s = fma(y, y, s);
+            }
+    } else {
+        for (int i = threadIdx.x; i < nv; i += CLIP_THREADS) {
+            const OpsVec<T, V> x = q[i];
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const double y = (double)OpsType<T>::load(x.v[j]);
+                s = fma(y, y, s);
+            }
+        }
+        for (int i = nv * V + threadIdx.x; i < n; i += CLIP_THREADS) {
+            const double y = (double)OpsType<T>::load(p[r.begin + i]);
+            s = fma(y, y, s);
+        }
+    }
+    return s;
+}
+
+// Sum over the block, the same in every thread; a fixed tree.
+__device__ __forceinline__ double block_sum(double s) {
+    __shared__ double w[CLIP_THREADS / 32];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) w[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < CLIP_THREADS / 32; ++i) s += w[i];
+    return s;
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(CLIP_THREADS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial) {
+    double s = 0.0;
+    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        const int i = find_tensor(t, c);
+        const long long count = t.count[i] & ((1ll << 56) - 1);
+        const int type = (int)(t.count[i] >> 56), k = c - t.first[i];
+        const void *p = t.in[i];
+        const ChunkRange r = chunk_range(p, type == QGBDT_F32 ? 4 : 2, count, k);
+        if (type == QGBDT_F32) s += sum_squares(reinterpret_cast<const float *>(p), r);
+        else if (type == QGBDT_BF16) s += sum_squares(reinterpret_cast<const __nv_bfloat16 *>(p), r);
+        else s += sum_squares(reinterpret_cast<const __half *>(p), r);
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+}
+
+template <typename T>
+__device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &r, float coef) {
+    constexpr int V = 16 / sizeof(T);
+    if ((int)threadIdx.x < r.head) o[threadIdx.x] = OpsType<T>::store(OpsType<T>::load(p[threadIdx.x]) * coef);
+    const int n = (int)(r.end - r.begin);
+    const bool vec = (reinterpret_cast<uintptr_t>(o + r.begin) & 15) == 0;   // the output may be aligned differently
+    const int nv = vec ? n / V : 0;
+    const OpsVec<T, V> *q = reinterpret_cast<const OpsVec<T, V> *>(p + r.begin);
+    OpsVec<T, V> *w = reinterpret_cast<OpsVec<T, V> *>(o + r.begin);
+    if (nv == CLIP_CHUNK / V) {
+        OpsVec<T, V> x[CLIP_CHUNK / V / CLIP_THREADS];
+#pragma unroll
+        for (int i = 0; i < CLIP_CHUNK / V / CLIP_THREADS; ++i) x[i] = q[threadIdx.x + i * CLIP_THREADS];
+#pragma unroll
+        for (int i = 0; i < CLIP_CHUNK / V / CLIP_THREADS; ++i) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[i].v[j] = OpsType<T>::store(OpsType<T>::load(x[i].v[j]) * coef);
+            w[threadIdx.x + i * CLIP_THREADS] = x[i];
+        }
+    } else {
+        for (int i = threadIdx.x; i < nv; i += CLIP_THREADS) {
+            OpsVec<T, V> x = q[i];
+#pragma unroll
+            for (int j = 0; j < V; ++j) x.v[j] = OpsType<T>::store(OpsType<T>::load(x.v[j]) * coef);
+            w[i] = x;
+        }
+        for (int i = nv * V + threadIdx.x; i < n; i += CLIP_THREADS)
+            o[r.begin + i] = OpsType<T>::store(OpsType<T>::load(p[r.begin + i]) * coef);
+    }
+}
+
+template <int CAP>
+__global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
+                                                             const double *partial, int n_partial, double max_norm, bool in_place, float *d_norm) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n_partial; i += CLIP_THREADS) s += partial[i];
+    s = block_sum(s);
+    const double norm = sqrt(s);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *d_norm = (float)norm;
+    // false also for a norm that is not finite: the tensors keep their values then
+    const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
+    if (!clip && in_place) return;
+    const float coef = clip ? (float)(max_norm / norm) : 1.0f;
+    for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
+        const int i = find_tensor(t, c);
+        const long long count = t.count[i] & ((1ll << 56) - 1);
+        const int type = (int)(t.count[i] >> 56), k = c - t.first[i];
+        const void *p = t.in[i];
+        void *w = o.out[i];
+        const ChunkRange r = chunk_range(p, type == QGBDT_F32 ? 4 : 2, count, k);
+        if (type == QGBDT_F32) scale_chunk(reinterpret_cast<const float *>(p), reinterpret_cast<float *>(w), r, coef);
+        else if (type == QGBDT_BF16) scale_chunk(reinterpret_cast<const __nv_bfloat16 *>(p), reinterpret_cast<__nv_bfloat16 *>(w), r, coef);
+        else scale_chunk(reinterpret_cast<const __half *>(p), reinterpret_cast<__half *>(w), r, coef);
+    }
+}
+
+template <int CAP>
+int fill(ClipTable<CAP> &t, ClipOut<CAP> &o, const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, int32_t &at,
+         int32_t n) {
+    t.n = 0;
+    long long chunks = 0;
+    for (; at < n && t.n < CAP; ++at) {
+        if (counts[at] == 0) continue;
+        // one chunk even for a tensor that ends before its first 16-byte boundary
+        const int width = qg_type_size(types[at]), off = (int)(reinterpret_cast<uintptr_t>(in[at]) & 15);
+        const long long body = counts[at] - (off ? (16 - off) / width : 0);
+        const long long k = body > 0 ? (body + CLIP_CHUNK - 1) / CLIP_CHUNK : 1;
+        if (t.n > 0 && chunks + k > 0x40000000ll) break;
+        if (k > 0x40000000ll) return -1;
+        t.in[t.n] = in[at];
+        o.out[t.n] = out[at];
+        t.count[t.n] = counts[at] | (long long)types[at] << 56;
+        t.first[t.n] = (int)chunks;
+        chunks += k;
+        ++t.n;
+    }
+    t.chunks = (int)chunks;
+    return 0;
+}
+
+int norm_grid(const qgbdt_ctx *c, int chunks) {
+    const int full = c->sm_count * 8;
+    return chunks < full ? (chunks > 0 ? chunks : 1) : full;
+}
+
+template <int CAP>
+int clip_groups(qgbdt_ctx *c, const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, int32_t n, double max_norm,
+                float *d_norm, double *partial, cudaStream_t st) {
+    ClipTable<CAP> t;
+    ClipOut<CAP> o;
+    int n_partial = 0;
+    int32_t at = 0;
+    do {
+        if (fill(t, o, in, out, counts, types, at, n) != 0) return qg_fail(c, QGBDT_ERR_ARG, "a tensor is too large");
+        const int grid = norm_grid(c, t.chunks);
+        k_norm_partial<CAP><<<grid, CLIP_THREADS, 0, st>>>(t, partial + n_partial);
+        QG_LAUNCH_CHECK(c);
+        n_partial += grid;
+    } while (at < n);
+    bool in_place = true;
+    for (int32_t i = 0; i < n; ++i) in_place = in_place && (in[i] == out[i] || counts[i] == 0);
+    at = 0;
+    do {
+        if (t.n == n) at = n;   // a single group: still in t
+        else fill(t, o, in, out, counts, types, at, n);
+        k_clip_scale<CAP><<<norm_grid(c, t.chunks), CLIP_THREADS, 0, st>>>(t, o, partial, n_partial, max_norm, in_place, d_norm);
+        QG_LAUNCH_CHECK(c);
+    } while (at < n);
+    return QGBDT_OK;
+}
+
+}  // namespace
+
+int qg_clip_grad_norm(qgbdt_ctx *c, const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, int32_t n,
+                      double max_norm, float *d_norm, cudaStream_t st) {
+    QgWorkspace ws;
+    const size_t groups = (size_t)n / CLIP_SMALL + 2;
+    int rc = qg_ws_open(c, qg_ws_size(groups * c->sm_count * 8, sizeof(double)), st, &ws);
+    if (rc != QGBDT_OK) return rc;
+    double *partial = ws.take<double>(groups * c->sm_count * 8);
+    rc = n <= CLIP_SMALL ? clip_groups<CLIP_SMALL>(c, in, out, counts, types, n, max_norm, d_norm, partial, st)
+                         : clip_groups<CLIP_LARGE>(c, in, out, counts, types, n, max_norm, d_norm, partial, st);
+    if (rc != QGBDT_OK) return rc;
+    return qg_ws_close(c, st);
+}

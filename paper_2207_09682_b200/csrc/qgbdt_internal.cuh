@@ -276,6 +276,15 @@ struct qgbdt_ctx {
     std::vector<int> hist_event_phase;     // phase (QG_PHASE_*) of every pair
     size_t hist_events_used = 0;
     int64_t hist_prof_bytes = 0, hist_prof_launches = 0;
+    // operators on top of the trees (ops_internal.cuh): one work buffer, used by one call after the other
+    void *ops_ws = nullptr;
+    size_t ops_ws_bytes = 0;
+    cudaEvent_t ops_ws_event = nullptr;         // end of the last call's use
+    unsigned long long ops_ws_stream = 0;       // id of that call's stream
+    bool ops_ws_used = false, ops_ws_captured = false;
+    std::vector<void *> ops_ws_old;             // outgrown buffers that a captured graph may still use
+    int *ops_fault = nullptr;                   // pinned word set by an operator's kernel that gave up waiting
+    unsigned int *d_ops_counters = nullptr;     // zero between calls
     char err[512] = {0};
 };
 
@@ -362,4 +371,4 @@ int qg_grow_max_recs(const qgbdt_ctx *c);    // grow.cu: growth records / histog
 int qg_grow_max_slots(const qgbdt_ctx *c);
 int qg_hist_grow_configure(qgbdt_ctx *c);   // function attributes of the kernels it launches (before a capture)
 void qg_grow_graph_destroy(qgbdt_ctx *c);   // grow.cu: drops the captured split loop (buffers are about to change)
-
+void qg_ops_destroy(qgbdt_ctx *c);          // api_ops.cu: frees the operators' work buffers
