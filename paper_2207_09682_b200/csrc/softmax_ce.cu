@@ -30,7 +30,7 @@
 
 namespace {
 
-constexpr int CG = 1;                       // CTAs per tile
+constexpr int CG = 2;                       // CTAs per tile
 constexpr int BM = 128 * CG, BN = 256, BK = 64;
 constexpr int A_BYTES = 128 * BK * 2, B_ROWS = BN / CG, B_BYTES = B_ROWS * BK * 2;
 constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
             stop = 1;
             *a.fault = 1;
             int never = 0;
-            tc_commit<1>(drained);
+            tc_commit<CG>(drained);
             tc_bar_wait(drained, 0, &never);
         }
     } else if (warp >= 4) {
