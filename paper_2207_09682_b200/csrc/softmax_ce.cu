@@ -30,14 +30,14 @@
 
 namespace {
 
-constexpr int CG = 2;                       // CTAs per tile
+constexpr int CG = 2;                       // CTAs per tile: a pair halves what each SM loads of the second operand
 constexpr int BM = 128 * CG, BN = 256, BK = 64;
 constexpr int A_BYTES = 128 * BK * 2, B_ROWS = BN / CG, B_BYTES = B_ROWS * BK * 2;
 constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int STAGES = 196608 / STAGE_BYTES;
-constexpr int EPI_WARPS = 4, THREADS = 128 + EPI_WARPS * 32;
-constexpr int STORE_BYTES = 32 * 128;       // 32 rows of 64 columns of g, per warp; two of them
-constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * 2 * STORE_BYTES;
+constexpr int EPI_WARPS = 8, THREADS = 128 + EPI_WARPS * 32;
+constexpr int STORE_BYTES = 32 * 128;       // staging of a warp: 32 rows of 128 bytes
+constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STORE_BYTES;
 constexpr int TMEM_COLS = 512, ACC_COLS = 256;
 constexpr int GROUP_M = 16;                 // row tiles that go through all column tiles together
 constexpr float LOG2E = 1.44269504088896340736f;
@@ -48,52 +48,99 @@ struct GemmArgs {
     const int *count;           // labelled rows
     int m_tiles, n_tiles;       // tiles (LOSS, GRAD, DH: row tiles for all rows; only those with labelled rows are taken)
     int kb;                     // blocks of 64 along the products' length (DW: taken from the count)
-    int splits;                 // parts the length is cut into (DH, DW)
     int classes;                // all classes
     int v0;                     // first class of the piece
     int dim;
     int bf16;
     int *fault;
     // LOSS and GRAD
-    const float *bias;
+    const float *bias;          // aligned copy, padded to whole tiles, or NULL
     const int *label;           // [labelled rows]
-    float2 *stat;               // [row][n_tiles] maximum, sum of exp(z - maximum)
+    float2 *stat;               // [row][n_tiles * 2] maximum, sum of exp(z - maximum) over 128 columns
     float *z_label;             // [row]
     const float *lse;           // [row]
-    float *bias_part;           // [m_tiles * 4 * CG][n_tiles * 256] column sums of g over 32 rows
+    float *bias_part;           // [m_tiles * BM / 32][n_tiles * 256] column sums of g over 32 rows
     // DH and DW
-    float *part;                // [splits][part_rows][ldp]
-    long long part_rows;
-    int ldp;
-    int add;                    // DH: add to what is there
-    void *out;                  // DW without splits: the output
+    int add;                    // DH: add to the fragments of the pieces before
+    uint16_t *out;              // DW
     long long ld_out;
-    int out_vec;                // its rows are 16-byte aligned
+    int out_map;                // its rows are 16-byte aligned: tiled copies write them
     const float *grad_loss;
 };
-
-struct Tile {
-    int m, n, kb0, kb1, split;
-};
-
-template <int MODE>
-__device__ __forceinline__ Tile tile_at(const GemmArgs &a, int m_live, int kb, int t) {
-    Tile r;
-    const int per = m_live * a.n_tiles;
-    r.split = t / per;
-    t -= r.split * per;
-    const int group = t / (GROUP_M * a.n_tiles), m0 = group * GROUP_M, gm = min(GROUP_M, m_live - m0);
-    t -= group * GROUP_M * a.n_tiles;
-    r.n = t / gm;
-    r.m = m0 + t - r.n * gm;
-    r.kb0 = (int)((long long)kb * r.split / a.splits);
-    r.kb1 = (int)((long long)kb * (r.split + 1) / a.splits);
-    return r;
-}
 
 __device__ __forceinline__ float out_scale(const float *grad_loss, int count) {
     return (grad_loss ? *grad_loss : 1.0f) / (float)(count > 0 ? count : 1);
 }
+
+// Tile t in the order in which tiles are taken: groups of GROUP_M row tiles, in a group all row tiles of a
+// column tile before the next, so that CTAs that run together share both operands in L2.
+__device__ __forceinline__ void tile_place(int t, int m_live, int n_tiles, int &m, int &n) {
+    const int group = t / (GROUP_M * n_tiles), m0 = group * GROUP_M, gm = min(GROUP_M, m_live - m0);
+    t -= group * GROUP_M * n_tiles;
+    n = t / gm;
+    m = m0 + t - n * gm;
+}
+__device__ __forceinline__ int tile_number(int m, int n, int m_live, int n_tiles) {
+    const int m0 = m / GROUP_M * GROUP_M, gm = min(GROUP_M, m_live - m0);
+    return m0 * n_tiles + n * gm + m - m0;
+}
+
+// DH and DW have few tiles and long products, so whole tiles would leave SMs idle in the last round.  All blocks of
+// all tiles, tile after tile, are one line that is cut into equal runs, one per unit (pair of CTAs); a tile that a
+// cut falls into is summed from its fragments afterwards, in the order of the units.
+struct Line {
+    long long length;   // tiles * kb
+    int kb, units;      // units that get a run (each at least four blocks long)
+    __device__ Line(int tiles, int kb_, int all_units) : length((long long)tiles * kb_), kb(kb_) {
+        const long long most = length / 4;
+        units = most < 1 ? 1 : most < all_units ? (int)most : all_units;
+    }
+    __device__ __forceinline__ long long start(int u) const { return length * u / units; }
+    __device__ __forceinline__ int unit_of(long long pos) const { return (int)(((pos + 1) * units - 1) / length); }
+};
+
+// What a unit works on next.
+struct Work {
+    int m, n, kb0, kb1;
+    int fragment;        // DH, and DW where the tile is not whole: which part buffer
+    bool whole;
+};
+template <int MODE>
+struct Schedule {
+    int t, step, total, m_live, n_tiles, kb, unit;
+    long long pos, end;
+    __device__ Schedule(const GemmArgs &a, int count) : n_tiles(a.n_tiles) {
+        m_live = MODE == DW ? a.m_tiles : (count + BM - 1) / BM;
+        kb = MODE == DW ? (count + BK - 1) / BK : a.kb;
+        unit = blockIdx.x / CG;
+        step = gridDim.x / CG;
+        total = m_live * n_tiles;
+        t = unit;
+        pos = end = 0;
+        if (MODE == DH || MODE == DW) {
+            const Line line(total, kb, step);
+            if (line.length > 0 && unit < line.units) pos = line.start(unit), end = line.start(unit + 1);
+        }
+    }
+    __device__ __forceinline__ bool next(Work &w) {
+        if (MODE == LOSS || MODE == GRAD) {
+            if (t >= total) return false;
+            tile_place(t, m_live, n_tiles, w.m, w.n);
+            w.kb0 = 0, w.kb1 = kb;
+            t += step;
+            return true;
+        }
+        if (pos >= end) return false;
+        const int tile = (int)(pos / kb);
+        tile_place(tile, m_live, n_tiles, w.m, w.n);
+        w.kb0 = (int)(pos - (long long)tile * kb);
+        w.kb1 = (int)min((long long)kb, w.kb0 + end - pos);
+        w.whole = w.kb0 == 0 && w.kb1 == kb;
+        w.fragment = MODE == DH ? tile + unit : 2 * unit + (w.kb0 == 0);
+        pos += w.kb1 - w.kb0;
+        return true;
+    }
+};
 
 // x[j] summed over the warp's 32 lanes, for j = lane.
 __device__ __forceinline__ float column_sums(float (&x)[32], int lane) {
@@ -118,10 +165,179 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, bool bf16) {
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// 16 bytes of this lane's row of the staging buffer, in the 128-byte swizzle.
+__device__ __forceinline__ void stage16(uint32_t buf, int lane, int chunk, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 128 + (((uint32_t)chunk ^ (lane & 7)) << 4)), "r"(w0), "r"(w1), "r"(w2),
+                 "r"(w3)
+                 : "memory");
+}
+
+template <int MODE>
+struct Epilogue {
+    const GemmArgs &a;
+    const CUtensorMap *map_out, *map_part;
+    uint32_t buf;          // this warp's staging buffer
+    int lane, count;
+    Work c;
+    int row_in, row;       // the warp's first row, this thread's
+    int col0;              // first of the warp's 128 columns
+    bool live;
+    int label;
+    float lse, scale, m_run, l_run;
+
+    __device__ Epilogue(const GemmArgs &a_, const CUtensorMap *o, const CUtensorMap *p, uint32_t b, int l, int n)
+        : a(a_), map_out(o), map_part(p), buf(b), lane(l), count(n) {
+        if (MODE == DW) scale = out_scale(a.grad_loss, count);
+    }
+
+    __device__ __forceinline__ void begin(const Work &w, int rank, int quarter, int half) {
+        c = w;
+        row_in = w.m * BM + rank * 128 + quarter * 32;
+        row = row_in + lane;
+        col0 = w.n * BN + half * 128;
+        live = row < count;
+        if (MODE == LOSS || MODE == GRAD) label = live ? a.label[row] : -1;
+        if (MODE == GRAD) lse = live ? a.lse[row] : 0.0f;
+        if (MODE == LOSS) m_run = -INFINITY, l_run = 0.0f;
+    }
+
+    // The staging buffer may be written: the copy out of it has been read.
+    __device__ __forceinline__ void stage_open() {
+        if (lane == 0) tc_store_wait_read<0>();
+        __syncwarp();
+    }
+    // Rows of the buffer are complete: the caller's copy may start (lane 0).
+    __device__ __forceinline__ void stage_close() {
+        tc_fence_async_smem();
+        __syncwarp();
+    }
+    __device__ __forceinline__ void stage_half(const float (&x)[32], int h) {   // 32 columns as 16-bit elements, left or right half of the buffer
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            stage16(buf, lane, h * 4 + i, pack2(x[8 * i], x[8 * i + 1], a.bf16), pack2(x[8 * i + 2], x[8 * i + 3], a.bf16),
+                    pack2(x[8 * i + 4], x[8 * i + 5], a.bf16), pack2(x[8 * i + 6], x[8 * i + 7], a.bf16));
+    }
+
+    // 32 columns: chunk cc of the warp's four.
+    __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int cc) {
+        float x[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
+        const int col = col0 + cc * 32;
+        if (MODE == LOSS || MODE == GRAD) {
+            const int v = a.v0 + col;
+            if (a.bias) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float4 b = __ldg(reinterpret_cast<const float4 *>(a.bias + v) + j);
+                    x[4 * j] += b.x, x[4 * j + 1] += b.y, x[4 * j + 2] += b.z, x[4 * j + 3] += b.w;
+                }
+            }
+            if (v + 32 > a.classes) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (v + j >= a.classes) x[j] = -INFINITY;
+            }
+            const int lj = label - v;
+            const bool mine = lj >= 0 && lj < 32;
+            if (MODE == LOSS) {
+                float t0 = fmaxf(x[0], x[1]), t1 = fmaxf(x[2], x[3]);
+#pragma unroll
+                for (int j = 4; j < 32; j += 4) t0 = fmaxf(t0, fmaxf(x[j], x[j + 1])), t1 = fmaxf(t1, fmaxf(x[j + 2], x[j + 3]));
+                const float top = fmaxf(m_run, fmaxf(t0, t1)), base = top == -INFINITY ? 0.0f : top;
+                if (__any_sync(0xffffffffu, mine)) {
+                    float z = x[0];
+#pragma unroll
+                    for (int j = 1; j < 32; ++j)
+                        if (lj == j) z = x[j];
+                    if (mine) a.z_label[row] = z;
+                }
+                float s0 = l_run * tc_ex2((m_run - base) * LOG2E), s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    s0 += tc_ex2((x[j] - base) * LOG2E);
+                    s1 += tc_ex2((x[j + 1] - base) * LOG2E);
+                    s2 += tc_ex2((x[j + 2] - base) * LOG2E);
+                    s3 += tc_ex2((x[j + 3] - base) * LOG2E);
+                }
+                l_run = (s0 + s1) + (s2 + s3);
+                m_run = top;
+                return;
+            }
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = tc_ex2((x[j] - lse) * LOG2E);
+            if (__any_sync(0xffffffffu, mine)) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j)
+                    if (lj == j) x[j] -= 1.0f;
+            }
+            if (row_in + 32 > count) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[j] = live ? x[j] : 0.0f;
+            }
+            if ((cc & 1) == 0) stage_open();
+            stage_half(x, cc & 1);
+            if (cc & 1) {
+                stage_close();
+                if (lane == 0) {
+                    tc_store_2d(map_out, col - 32, row_in, buf);
+                    tc_store_commit();
+                }
+            }
+            if (a.bias_part) a.bias_part[(long long)(row_in / 32) * (a.n_tiles * BN) + col + lane] = column_sums(x, lane);
+            return;
+        }
+        if (MODE == DW && c.whole) {
+            const int v_in = a.v0 + row_in;
+            if ((cc & 1) == 0) stage_open();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] *= scale;
+            stage_half(x, cc & 1);
+            if ((cc & 1) == 0) return;
+            stage_close();
+            const int first = col - 32;   // of 64 columns
+            if (a.out_map) {
+                if (lane == 0 && first < a.dim && v_in < a.classes) {
+                    tc_store_2d(map_out, first, v_in, buf);
+                    tc_store_commit();
+                }
+            } else {   // two columns per lane, row after row
+                const int d = first + 2 * lane;
+                for (int i = 0; i < 32 && v_in + i < a.classes; ++i) {
+                    uint32_t w;
+                    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(buf + i * 128 + ((((uint32_t)lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) : "memory");
+                    uint16_t *o = a.out + (v_in + i) * a.ld_out + d;
+                    if (d < a.dim) o[0] = (uint16_t)w;
+                    if (d + 1 < a.dim) o[1] = (uint16_t)(w >> 16);
+                }
+                __syncwarp();
+            }
+            return;
+        }
+        // a fragment, single precision, to its part buffer
+        stage_open();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            stage16(buf, lane, i, __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
+        stage_close();
+        if (lane == 0) {
+            const int y = c.fragment * BM + row_in - c.m * BM, xx = col - c.n * BN;
+            if (MODE == DH && a.add) tc_add_2d(map_part, xx, y, buf);
+            else tc_store_2d(map_part, xx, y, buf);
+            tc_store_commit();
+        }
+    }
+
+    __device__ __forceinline__ void end(int half) {
+        if (MODE == LOSS && live) a.stat[((long long)row * a.n_tiles + c.n) * 2 + half] = make_float2(m_run, l_run);
+    }
+};
+
 template <int MODE>
 __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, const __grid_constant__ CUtensorMap map_a,
                                                              const __grid_constant__ CUtensorMap map_b,
-                                                             const __grid_constant__ CUtensorMap map_g) {
+                                                             const __grid_constant__ CUtensorMap map_out,
+                                                             const __grid_constant__ CUtensorMap map_part) {
     constexpr bool A_MN = MODE == DW, B_MN = MODE == DH || MODE == DW;   // operand rows run along the products' length
     extern __shared__ char smem_raw[];
     __shared__ alignas(8) unsigned long long bars[2 * STAGES + 4 + 1];
@@ -152,17 +368,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
     const uint32_t tmem = *(volatile uint32_t *)&tmem_base;
 
     const int count = *a.count;
-    const int m_live = MODE == DW ? a.m_tiles : (count + BM - 1) / BM;
-    const int kb = MODE == DW ? (count + BK - 1) / BK : a.kb;
-    const int total = m_live * a.n_tiles * a.splits;
-    const int first = blockIdx.x / CG, step = gridDim.x / CG;
+    Schedule<MODE> todo(a, count);
+    Work c;
     bool ok = true;
 
     if (warp == 0 && lane == 0) {
         // ---- copies
         int it = 0;
-        for (int t = first; t < total && ok; t += step) {
-            const Tile c = tile_at<MODE>(a, m_live, kb, t);
+        while (ok && todo.next(c)) {
             for (int k = c.kb0; k < c.kb1; ++k, ++it) {
                 const int s = it % STAGES;
                 if (!(ok = tc_bar_wait(empty(s), (it / STAGES & 1) ^ 1, &stop))) break;
@@ -195,9 +408,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
         // ---- matrix instructions
         const uint32_t idesc = tc_idesc(BM, BN, a.bf16, A_MN, B_MN);
         int it = 0, n_acc = 0;
-        for (int t = first; t < total && ok; t += step) {
-            const Tile c = tile_at<MODE>(a, m_live, kb, t);
-            if (c.kb0 == c.kb1) continue;
+        while (ok && todo.next(c)) {
             const int b = n_acc & 1;
             if (!(ok = tc_bar_wait(acc_empty(b), (n_acc / 2 & 1) ^ 1, &stop))) break;
             tc_fence_after();
@@ -226,162 +437,38 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
             tc_bar_wait(drained, 0, &never);
         }
     } else if (warp >= 4) {
-        // ---- epilogue: thread = row of the tile
-        const int q = warp & 3;
-        const uint32_t tacc = tmem + ((uint32_t)(q * 32) << 16);
-        const uint32_t store = store_at + (warp - 4) * 2 * STORE_BYTES;
-        int n_acc = 0, n_store = 0;
-        for (int t = first; t < total; t += step) {
-            const Tile c = tile_at<MODE>(a, m_live, kb, t);
-            const bool some = c.kb0 < c.kb1;   // a part of no length: zeros
+        // ---- epilogue: thread = row of the tile, half of the columns per warp
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        Epilogue<MODE> epi(a, &map_out, &map_part, store_at + (warp - 4) * STORE_BYTES, lane, count);
+        int n_acc = 0;
+        while (todo.next(c)) {
             const int b = n_acc & 1;
-            if (some) {
-                if (!(ok = __all_sync(0xffffffffu, tc_bar_wait(acc_full(b), n_acc / 2 & 1, &stop)))) break;
-                tc_fence_after();
-            }
-            const int row_in = c.m * BM + (int)rank * 128 + q * 32;   // the warp's first row
-            const int row = row_in + lane;
-            const bool live = MODE == DW || row < count;
-            float m_run = -INFINITY, l_run = 0.0f, lse = 0.0f, scale = 1.0f;
-            int label = -1;
-            if (MODE == LOSS || MODE == GRAD) label = live ? a.label[row] : -1;
-            if (MODE == GRAD) lse = live ? a.lse[row] : 0.0f;
-            if (MODE == DW && a.out) scale = out_scale(a.grad_loss, count);
-#pragma unroll 1
-            for (int cc = 0; cc < BN / 32; ++cc) {
-                const int col = c.n * BN + cc * 32;                  // in the piece (LOSS, GRAD) or in dim (DH, DW)
-                uint32_t r[32];
-                float x[32];
-                if (some) {
-                    tc_ld_32(tacc + b * ACC_COLS + cc * 32, r);
-                    if (cc == BN / 32 - 1) {   // the accumulator may be filled again
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) tc_bar_arrive_cluster(CG == 1 ? acc_empty(b) : tc_map_rank(acc_empty(b), 0));
-                    }
+            epi.begin(c, (int)rank, quarter, half);
+            if (!(ok = __all_sync(0xffffffffu, tc_bar_wait(acc_full(b), n_acc / 2 & 1, &stop)))) break;
+            tc_fence_after();
+            const uint32_t tacc = tmem + ((uint32_t)(quarter * 32) << 16) + b * ACC_COLS + half * 128;
+            uint32_t r[2][32];
+            tc_ld_32(tacc, r[0]);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) x[j] = 0.0f;
+            for (int cc = 0; cc < 4; ++cc) {
+                tc_ld_wait(r[cc & 1]);
+                if (cc < 3) {
+                    tc_ld_32(tacc + (cc + 1) * 32, r[(cc + 1) & 1]);   // read under the arithmetic of this chunk
+                } else {   // the accumulator may be filled again
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc_bar_arrive_cluster(CG == 1 ? acc_empty(b) : tc_map_rank(acc_empty(b), 0));
                 }
-                if (MODE == LOSS || MODE == GRAD) {
-                    const int v = a.v0 + col;
-                    if (a.bias) {
-                        const float bias = v + lane < a.classes ? a.bias[v + lane] : 0.0f;
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] += __shfl_sync(0xffffffffu, bias, j);
-                    }
-                    if (v + 32 > a.classes) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j)
-                            if (v + j >= a.classes) x[j] = -INFINITY;
-                    }
-                    const int lj = label - v;
-                    if (MODE == LOSS) {
-                        float top = x[0];
-#pragma unroll
-                        for (int j = 1; j < 32; ++j) top = fmaxf(top, x[j]);
-                        top = fmaxf(top, m_run);
-                        const float base = top == -INFINITY ? 0.0f : top;
-                        float s0 = l_run * tc_ex2((m_run - base) * LOG2E), s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
-#pragma unroll
-                        for (int j = 0; j < 32; j += 4) {
-                            s0 += tc_ex2((x[j] - base) * LOG2E);
-                            s1 += tc_ex2((x[j + 1] - base) * LOG2E);
-                            s2 += tc_ex2((x[j + 2] - base) * LOG2E);
-                            s3 += tc_ex2((x[j + 3] - base) * LOG2E);
-                        }
-                        l_run = (s0 + s1) + (s2 + s3);
-                        m_run = top;
-                        if (lj >= 0 && lj < 32) {
-                            float z = x[0];
-#pragma unroll
-                            for (int j = 1; j < 32; ++j)
-                                if (lj == j) z = x[j];
-                            a.z_label[row] = z;
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) x[j] = tc_ex2((x[j] - lse) * LOG2E);
-                        if (lj >= 0 && lj < 32) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (lj == j) x[j] -= 1.0f;
-                        }
-                        if (!live) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] = 0.0f;
-                        }
-                        // 32 rows by 64 columns at a time to the buffer of g
-                        const uint32_t buf = store + (n_store & 1) * STORE_BYTES;
-                        if ((cc & 1) == 0) {   // the copy that used this buffer has read it
-                            if (lane == 0) tc_store_wait_read<1>();
-                            __syncwarp();
-                        }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t w = buf + lane * 128 + (((uint32_t)((cc & 1) * 4 + i) ^ (lane & 7)) << 4);
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(w), "r"(pack2(x[8 * i], x[8 * i + 1], a.bf16)),
-                                         "r"(pack2(x[8 * i + 2], x[8 * i + 3], a.bf16)), "r"(pack2(x[8 * i + 4], x[8 * i + 5], a.bf16)),
-                                         "r"(pack2(x[8 * i + 6], x[8 * i + 7], a.bf16))
-                                         : "memory");
-                        }
-                        if (cc & 1) {
-                            tc_fence_async_smem();
-                            __syncwarp();
-                            if (lane == 0) {
-                                tc_store_2d(&map_g, col - 32, row_in, buf);
-                                tc_store_commit();
-                            }
-                            ++n_store;
-                        }
-                        if (a.bias_part) {
-                            const float s = column_sums(x, lane);
-                            a.bias_part[(long long)(row_in / 32) * (a.n_tiles * BN) + col + lane] = s;
-                        }
-                    }
-                } else if (MODE == DW && a.out) {
-                    const int v = a.v0 + row;
-                    if (v < a.classes) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t w[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) w[j] = pack2(x[8 * i + 2 * j] * scale, x[8 * i + 2 * j + 1] * scale, a.bf16);
-                            const int d = col + 8 * i;
-                            uint16_t *o = reinterpret_cast<uint16_t *>(a.out) + v * a.ld_out + d;
-                            if (a.out_vec && d + 8 <= a.dim) {
-                                *reinterpret_cast<uint4 *>(o) = make_uint4(w[0], w[1], w[2], w[3]);
-                            } else {
-#pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    if (d + j < a.dim) o[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-                            }
-                        }
-                    }
-                } else if (live) {
-                    float4 *o = reinterpret_cast<float4 *>(a.part + ((long long)c.split * a.part_rows + row) * a.ldp + col);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (col + 4 * i < a.ldp) {
-                            float4 w = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                            if (MODE == DH && a.add) {
-                                const float4 y = o[i];
-                                w.x += y.x, w.y += y.y, w.z += y.z, w.w += y.w;
-                            }
-                            o[i] = w;
-                        }
-                }
+                epi.chunk(r[cc & 1], cc);
             }
-            if (MODE == LOSS && live) a.stat[(long long)row * a.n_tiles + c.n] = make_float2(m_run, l_run);
-            if (some) ++n_acc;
+            epi.end(half);
+            ++n_acc;
         }
         if (!ok) {
             stop = 1;
             *a.fault = 1;
         }
-        if (MODE == GRAD && lane == 0) tc_store_wait();
+        if (MODE != LOSS && lane == 0) tc_store_wait();
     }
     __syncwarp();
     tc_fence_before();
@@ -410,6 +497,9 @@ struct PackArgs {
     float *lse_packed;
     uint16_t *packed;          // [n_pad][ldp]
     int ldp;
+    const float *bias;         // copied to bias_copy with the padding cleared, or NULL
+    float *bias_copy;
+    int bias_pad;
     int *status;
 };
 
@@ -440,6 +530,8 @@ __global__ void __launch_bounds__(PACK_THREADS) k_pack_count(const PackArgs a) {
 
 __global__ void __launch_bounds__(PACK_THREADS) k_pack(const PackArgs a) {
     __shared__ int place[PACK_ROWS];   // where the block's rows go, -1: no label
+    if (a.bias)
+        for (int i = blockIdx.x * PACK_THREADS + threadIdx.x; i < a.bias_pad; i += gridDim.x * PACK_THREADS) a.bias_copy[i] = i < a.classes ? a.bias[i] : 0.0f;
     const int r0 = blockIdx.x * PACK_ROWS, spans = (a.n + PACK_SPAN - 1) / PACK_SPAN, span = r0 / PACK_SPAN;
     int before = 0, all = 0;
     if (spans > 1)
@@ -581,33 +673,79 @@ __global__ void __launch_bounds__(JOIN_ROWS * 32) k_loss_join(const float2 *stat
     }
 }
 
-// ---- gradients out of single-precision parts -------------------------------------------------------------
+// ---- gradients out of single-precision fragments ---------------------------------------------------------
 
-// out[r] = scale * sum over the splits of part[split][pos_of[r]] (pos_of NULL: r itself; negative: zeros).
+// Four columns of a tile's row: the sum over its fragments.
+__device__ __forceinline__ void add4(float4 &s, const float *p) {
+    const float4 x = *reinterpret_cast<const float4 *>(p);
+    s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
+}
+
 template <typename T>
-__global__ void __launch_bounds__(256) k_grad_finish(const float *part, int splits, long long part_rows, int ldp, const int *pos_of, long long rows,
-                                                     int dim, const float *grad_loss, const int *count, T *out, long long ld_out) {
-    const float scale = out_scale(grad_loss, *count);
+__device__ __forceinline__ void write4(T *o, int left, const float4 &s, float scale) {
+    OpsVec<T, 4> y;
+    y.v[0] = OpsType<T>::store(s.x * scale), y.v[1] = OpsType<T>::store(s.y * scale);
+    y.v[2] = OpsType<T>::store(s.z * scale), y.v[3] = OpsType<T>::store(s.w * scale);
+    if (left >= 4 && reinterpret_cast<uintptr_t>(o) % sizeof(y) == 0) {
+        *reinterpret_cast<OpsVec<T, 4> *>(o) = y;
+    } else {
+        for (int j = 0; j < 4 && j < left; ++j) o[j] = y.v[j];
+    }
+}
+
+// dH: every row of the caller's, zeros where it has no label.
+template <typename T>
+__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int units, int n_tiles, int kb, const int *pos_of, long long rows, int dim,
+                                                   const float *grad_loss, const int *count, T *out, long long ld_out) {
+    const int n = *count, m_live = (n + BM - 1) / BM;
+    const float scale = out_scale(grad_loss, n);
+    const Line line(m_live * n_tiles, kb, units);
     const int quads = (dim + 3) / 4;
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * quads; i += (long long)gridDim.x * 256) {
         const long long r = i / quads;
-        const int d = (int)(i - r * quads) * 4;
-        const long long p = pos_of ? pos_of[r] : r;
+        const int d = (int)(i - r * quads) * 4, p = pos_of[r];
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (p >= 0)
-            for (int k = 0; k < splits; ++k) {
-                const float4 x = *reinterpret_cast<const float4 *>(part + (k * part_rows + p) * ldp + d);
-                s.x += x.x, s.y += x.y, s.z += x.z, s.w += x.w;
-            }
-        OpsVec<T, 4> y;
-        y.v[0] = OpsType<T>::store(s.x * scale), y.v[1] = OpsType<T>::store(s.y * scale);
-        y.v[2] = OpsType<T>::store(s.z * scale), y.v[3] = OpsType<T>::store(s.w * scale);
-        T *o = out + r * ld_out + d;
-        if (d + 4 <= dim && reinterpret_cast<uintptr_t>(o) % sizeof(y) == 0) {
-            *reinterpret_cast<OpsVec<T, 4> *>(o) = y;
-        } else {
-            for (int j = 0; j < 4 && d + j < dim; ++j) o[j] = y.v[j];
+        if (p >= 0) {
+            const int t = tile_number(p / BM, d / BN, m_live, n_tiles);
+            const int u0 = line.unit_of((long long)t * kb), u1 = line.unit_of((long long)(t + 1) * kb - 1);
+            for (int u = u0; u <= u1; ++u) add4(s, part + ((long long)(t + u) * BM + p % BM) * BN + d % BN);
         }
+        write4(out + r * ld_out + d, dim - d, s, scale);
+    }
+}
+
+// dW: the tiles that a cut falls into; block (u, y) looks at the cut in front of unit u + 1 and takes 8 rows.
+template <typename T>
+__global__ void __launch_bounds__(256) k_dw_finish(const float *part, int units, int m_tiles, int n_tiles, int rows, int dim, const float *grad_loss,
+                                                   const int *count, T *out, long long ld_out) {
+    const int n = *count, kb = (n + BK - 1) / BK;
+    if (n == 0) {   // no labelled row: nothing has been written yet
+        const int quads = (dim + 3) / 4;
+        for (long long i = (blockIdx.y * gridDim.x + blockIdx.x) * 256ll + threadIdx.x; i < (long long)rows * quads; i += gridDim.x * gridDim.y * 256ll) {
+            const long long r = i / quads;
+            const int d = (int)(i - r * quads) * 4;
+            write4(out + r * ld_out + d, dim - d, make_float4(0.0f, 0.0f, 0.0f, 0.0f), 0.0f);
+        }
+        return;
+    }
+    const Line line(m_tiles * n_tiles, kb, units);
+    const int u = blockIdx.x + 1;
+    if (u >= line.units) return;
+    const long long cut = line.start(u);
+    const int t = (int)(cut / kb);
+    if (cut == (long long)t * kb) return;
+    const int u0 = line.unit_of((long long)t * kb), u1 = line.unit_of((long long)(t + 1) * kb - 1);
+    if (u0 != u - 1) return;   // an earlier cut of the same tile
+    const float scale = out_scale(grad_loss, n);
+    int m, col;
+    tile_place(t, m_tiles, n_tiles, m, col);
+    col *= BN;
+    const int r = blockIdx.y * 8 + threadIdx.x / 32;
+    if (m * BM + r >= rows) return;
+    for (int d = (threadIdx.x & 31) * 4; d < BN && col + d < dim; d += 128) {
+        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int k = u0; k <= u1; ++k) add4(s, part + ((long long)(2 * k + (k == u0)) * BM + r) * BN + d);
+        write4(out + (long long)(m * BM + r) * ld_out + col + d, dim - col - d, s, scale);
     }
 }
 
@@ -644,28 +782,29 @@ int encoder(qgbdt_ctx *c, EncodeTiled *out) {
     return QGBDT_OK;
 }
 
-// Matrix [rows][ld] of 16-bit elements, copied in boxes of 64 columns by `box` rows, 128-byte swizzle, zeros outside.
-int matrix_map(qgbdt_ctx *c, CUtensorMap *m, const void *p, long long cols, long long rows, long long ld, int box, bool bf16) {
+// Matrix [rows][ld] copied in boxes of 128 bytes by `box` rows, 128-byte swizzle, zeros outside.
+int matrix_map(qgbdt_ctx *c, CUtensorMap *m, const void *p, long long cols, long long rows, long long ld, int box, int type) {
     EncodeTiled encode = nullptr;
     int rc = encoder(c, &encode);
     if (rc != QGBDT_OK) return rc;
-    const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
-    const cuuint32_t b[2] = {64, (cuuint32_t)box}, one[2] = {1, 1};
-    const CUresult r = encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(p), size, stride, b, one,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const int width = qg_type_size(type);
+    const cuuint64_t size[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * width};
+    const cuuint32_t b[2] = {128u / width, (cuuint32_t)box}, one[2] = {1, 1};
+    const CUtensorMapDataType t = type == QGBDT_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                  : type == QGBDT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                       : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    const CUresult r = encode(m, t, 2, const_cast<void *>(p), size, stride, b, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return qg_fail(c, QGBDT_ERR_CUDA, "cuTensorMapEncodeTiled failed (%d)", (int)r);
     return QGBDT_OK;
 }
 
 template <int MODE>
-int gemm(qgbdt_ctx *c, const GemmArgs &a, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mg, cudaStream_t st) {
+int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mo, const CUtensorMap &mp,
+         cudaStream_t st) {
     QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
-    const long long tiles = (long long)a.m_tiles * a.n_tiles * a.splits;
-    if (tiles > 0x7fffffffll) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
-    const int units = c->sm_count / CG;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(tiles < units ? (tiles > 0 ? tiles : 1) : units) * CG);
+    cfg.gridDim = dim3((unsigned)units * CG);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = SMEM_BYTES;
     cfg.stream = st;
@@ -674,31 +813,31 @@ int gemm(qgbdt_ctx *c, const GemmArgs &a, const CUtensorMap &ma, const CUtensorM
     at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    QG_CUDA(c, cudaLaunchKernelEx(&cfg, k_softmax_gemm<MODE>, a, ma, mb, mg));
+    QG_CUDA(c, cudaLaunchKernelEx(&cfg, k_softmax_gemm<MODE>, a, ma, mb, mo, mp));
     QG_LAUNCH_CHECK(c);
     return QGBDT_OK;
 }
 
 int up(int64_t x, int m) { return (int)((x + m - 1) / m * m); }
 
-// What both directions share: the packed rows and the weight with aligned rows.
+// What both directions share: the packed rows, the weight with aligned rows, the padded bias.
 struct Common {
     PackArgs pack;
     const void *weight;
     long long ld_weight;
-    uint16_t *weight_copy;
     int n_pad, ldp;
 };
 
-size_t common_bytes(const SoftmaxArgs &a, bool copy_weight) {
+// classes_pad: classes rounded up to what the tiles of the call cover.
+size_t common_bytes(const SoftmaxArgs &a, bool copy_weight, int64_t classes_pad) {
     const int n_pad = up(a.rows, 256), ldp = up(a.dim, 8);
     return qg_ws_size((size_t)n_pad * ldp, 2) + 4 * qg_ws_size((size_t)n_pad, 4) + qg_ws_size(1, 4) + qg_ws_size((size_t)a.rows / PACK_SPAN + 1, 4) +
-           (copy_weight ? qg_ws_size((size_t)a.classes * ldp, 2) : 0);
+           (copy_weight ? qg_ws_size((size_t)a.classes * ldp, 2) : 0) + (a.bias ? qg_ws_size((size_t)classes_pad, 4) : 0);
 }
 
 bool rows_aligned(const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
 
-int prepare(qgbdt_ctx *c, const SoftmaxArgs &a, QgWorkspace &ws, Common *o, cudaStream_t st) {
+int prepare(qgbdt_ctx *c, const SoftmaxArgs &a, QgWorkspace &ws, int64_t classes_pad, Common *o, cudaStream_t st) {
     PackArgs &p = o->pack;
     p = PackArgs{};
     o->n_pad = up(a.rows, 256);
@@ -711,6 +850,7 @@ int prepare(qgbdt_ctx *c, const SoftmaxArgs &a, QgWorkspace &ws, Common *o, cuda
     p.row_of = ws.take<int>(o->n_pad), p.pos_of = ws.take<int>(o->n_pad), p.label = ws.take<int>(o->n_pad), p.lse_packed = ws.take<float>(o->n_pad);
     p.count = ws.take<int>(1);
     p.span_count = ws.take<int>(a.rows / PACK_SPAN + 1);
+    if (a.bias) p.bias = a.bias, p.bias_pad = (int)classes_pad, p.bias_copy = ws.take<float>((size_t)classes_pad);
     o->weight = a.weight, o->ld_weight = a.ld_weight;
     if (!rows_aligned(a.weight, a.ld_weight)) {
         uint16_t *copy = ws.take<uint16_t>((size_t)a.classes * o->ldp);
@@ -733,28 +873,34 @@ int prepare(qgbdt_ctx *c, const SoftmaxArgs &a, QgWorkspace &ws, Common *o, cuda
 
 GemmArgs gemm_args(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o) {
     GemmArgs g{};
-    g.count = o.pack.count, g.splits = 1, g.classes = (int)a.classes, g.dim = a.dim, g.bf16 = a.type == QGBDT_BF16, g.fault = c->ops_fault;
-    g.bias = a.bias, g.label = o.pack.label, g.lse = o.pack.lse_packed, g.grad_loss = a.grad_loss;
+    g.count = o.pack.count, g.classes = (int)a.classes, g.dim = a.dim, g.bf16 = a.type == QGBDT_BF16, g.fault = c->ops_fault;
+    g.bias = o.pack.bias_copy, g.label = o.pack.label, g.lse = o.pack.lse_packed, g.grad_loss = a.grad_loss;
     g.m_tiles = o.n_pad / BM, g.kb = (a.dim + BK - 1) / BK;
     return g;
 }
 
 constexpr int64_t PIECE_ELEMENTS = 1ll << 27;   // of g: 256 MiB
 
-// Parts to cut the products' length into so that `tiles` tiles keep all SMs busy; parts hold at least four blocks.
-int split_count(int units, long long tiles, int kb) {
-    int s = (int)(units / (tiles > 0 ? tiles : 1));
-    if (s > kb / 4) s = kb / 4;
-    return s < 1 ? 1 : s;
+// Units (pairs of CTAs) for a number of tiles; -1: more tiles than a launch can number.
+int unit_count(const qgbdt_ctx *c, long long tiles) {
+    const int units = c->sm_count / CG;
+    if (tiles > 0x3fffffff) return -1;
+    return tiles < 1 ? 1 : tiles < units ? (int)tiles : units;
 }
 
 template <typename T>
-int grad_finish(qgbdt_ctx *c, const float *part, int splits, long long part_rows, int ldp, const int *pos_of, long long rows, int dim,
-                const float *grad_loss, const int *count, void *out, long long ld_out, cudaStream_t st) {
-    const long long blocks = (rows * ((dim + 3) / 4) + 255) / 256;
-    if (blocks <= 0) return QGBDT_OK;
-    k_grad_finish<T><<<(unsigned)(blocks < c->sm_count * 16 ? blocks : c->sm_count * 16), 256, 0, st>>>(
-        part, splits, part_rows, ldp, pos_of, rows, dim, grad_loss, count, reinterpret_cast<T *>(out), ld_out);
+int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, int units, int n_tiles, int kb, cudaStream_t st) {
+    const long long blocks = (a.rows * ((a.dim + 3) / 4) + 255) / 256;
+    k_dh_finish<T><<<(unsigned)(blocks < c->sm_count * 16 ? blocks : c->sm_count * 16), 256, 0, st>>>(
+        part, units, n_tiles, kb, o.pack.pos_of, a.rows, a.dim, a.grad_loss, o.pack.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden);
+    QG_LAUNCH_CHECK(c);
+    return QGBDT_OK;
+}
+
+template <typename T>
+int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, int units, const GemmArgs &g, int rows, cudaStream_t st) {
+    k_dw_finish<T><<<dim3(units, BM / 8), 256, 0, st>>>(part, units, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, o.pack.count,
+                                                       reinterpret_cast<T *>(a.d_weight) + g.v0 * a.ld_d_weight, a.ld_d_weight);
     QG_LAUNCH_CHECK(c);
     return QGBDT_OK;
 }
@@ -765,101 +911,95 @@ int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
     const bool copy = !rows_aligned(a.weight, a.ld_weight);
     const int n_tiles = up(a.classes, BN) / BN, n_pad = up(a.rows, 256);
     const int join_blocks = a.rows > 0 ? (int)((a.rows + JOIN_ROWS - 1) / JOIN_ROWS) : 1;
+    const int units = unit_count(c, (long long)(n_pad / BM) * n_tiles);
+    if (units < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
     QgWorkspace ws;
-    int rc = qg_ws_open(c, common_bytes(a, copy) + qg_ws_size((size_t)n_pad * n_tiles, 8) + qg_ws_size((size_t)n_pad, 4) + qg_ws_size(join_blocks, 8), st, &ws);
+    int rc = qg_ws_open(c, common_bytes(a, copy, (int64_t)n_tiles * BN) + qg_ws_size((size_t)n_pad * n_tiles * 2, 8) + qg_ws_size((size_t)n_pad, 4) +
+                               qg_ws_size(join_blocks, 8), st, &ws);
     if (rc != QGBDT_OK) return rc;
     Common o;
-    if ((rc = prepare(c, a, ws, &o, st)) != QGBDT_OK) return rc;
+    if ((rc = prepare(c, a, ws, (int64_t)n_tiles * BN, &o, st)) != QGBDT_OK) return rc;
     GemmArgs g = gemm_args(c, a, o);
     g.n_tiles = n_tiles;
-    g.stat = ws.take<float2>((size_t)n_pad * n_tiles);
+    g.stat = ws.take<float2>((size_t)n_pad * n_tiles * 2);
     g.z_label = ws.take<float>(n_pad);
     double *block_loss = ws.take<double>(join_blocks);
     if (a.rows > 0) {
         CUtensorMap ma, mb;
-        if ((rc = matrix_map(c, &ma, o.pack.packed, a.dim, n_pad, o.ldp, 128, g.bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &mb, o.weight, a.dim, a.classes, o.ld_weight, B_ROWS, g.bf16)) != QGBDT_OK) return rc;
-        if ((rc = gemm<LOSS>(c, g, ma, mb, ma, st)) != QGBDT_OK) return rc;
+        if ((rc = matrix_map(c, &ma, o.pack.packed, a.dim, n_pad, o.ldp, 128, a.type)) != QGBDT_OK) return rc;
+        if ((rc = matrix_map(c, &mb, o.weight, a.dim, a.classes, o.ld_weight, B_ROWS, a.type)) != QGBDT_OK) return rc;
+        if ((rc = gemm<LOSS>(c, g, units, ma, mb, ma, ma, st)) != QGBDT_OK) return rc;
     }
-    k_loss_join<<<join_blocks, JOIN_ROWS * 32, 0, st>>>(g.stat, n_tiles, g.z_label, o.pack.pos_of, (int)a.rows, o.pack.count, a.losses, a.lse, block_loss,
-                                                        c->d_ops_counters, a.loss);
+    k_loss_join<<<join_blocks, JOIN_ROWS * 32, 0, st>>>(g.stat, n_tiles * 2, g.z_label, o.pack.pos_of, (int)a.rows, o.pack.count, a.losses, a.lse,
+                                                        block_loss, c->d_ops_counters, a.loss);
     QG_LAUNCH_CHECK(c);
     return qg_ws_close(c, st);
 }
 
 int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
+    if (a.rows == 0) {
+        QG_CUDA(c, cudaMemset2DAsync(a.d_weight, a.ld_d_weight * 2, 0, (size_t)a.dim * 2, a.classes, st));
+        if (a.d_bias) QG_CUDA(c, cudaMemsetAsync(a.d_bias, 0, sizeof(float) * a.classes, st));
+        return QGBDT_OK;
+    }
     const bool copy = !rows_aligned(a.weight, a.ld_weight);
-    const int n_pad = up(a.rows > 0 ? a.rows : 1, 256), units = c->sm_count / CG;
-    // pieces of the classes
+    const int n_pad = up(a.rows, 256);
+    // pieces of the classes, all of one width (the last one's missing classes count as excluded)
     int64_t width = PIECE_ELEMENTS / n_pad / 256 * 256;
     if (width < 256) width = 256;
     const int pieces = (int)((a.classes + width - 1) / width);
     width = up((a.classes + pieces - 1) / pieces, 256);
-    const int ldf = up(a.dim, 4), d_tiles = (a.dim + BN - 1) / BN;
-    const int dh_splits = split_count(units, (long long)(n_pad / BM) * d_tiles, (int)(width / BK));
-    const int dw_splits = split_count(units, (width / BM) * d_tiles, n_pad / BK);
+    const int d_tiles = (a.dim + BN - 1) / BN, m_tiles = n_pad / BM, kb_dh = (int)(width / BK);
+    const int grad_units = unit_count(c, m_tiles * (width / BN)), dh_units = unit_count(c, (long long)m_tiles * d_tiles * kb_dh / 4);
+    const int dw_units = unit_count(c, width / BM * d_tiles * (n_pad / BK) / 4);
+    if (grad_units < 0 || dh_units < 0 || dw_units < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
+    const size_t dh_fragments = (size_t)m_tiles * d_tiles + dh_units, dw_fragments = 2 * (size_t)dw_units;
     QgWorkspace ws;
     int rc = qg_ws_open(c,
-                        common_bytes(a, copy) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size((size_t)dh_splits * n_pad * ldf, 4) +
-                            (dw_splits > 1 ? qg_ws_size((size_t)dw_splits * width * ldf, 4) : 0) +
-                            (a.d_bias ? qg_ws_size((size_t)(n_pad / 32) * width, 4) : 0) + 4096,
+                        common_bytes(a, copy, pieces * width) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size(dh_fragments * BM * BN, 4) +
+                            qg_ws_size(dw_fragments * BM * BN, 4) + (a.d_bias ? qg_ws_size((size_t)(n_pad / 32) * width, 4) : 0),
                         st, &ws);
     if (rc != QGBDT_OK) return rc;
     Common o;
-    if ((rc = prepare(c, a, ws, &o, st)) != QGBDT_OK) return rc;
+    if ((rc = prepare(c, a, ws, pieces * width, &o, st)) != QGBDT_OK) return rc;
     uint16_t *g_piece = ws.take<uint16_t>((size_t)n_pad * width);
-    float *dh_part = ws.take<float>((size_t)dh_splits * n_pad * ldf);
-    float *dw_part = dw_splits > 1 ? ws.take<float>((size_t)dw_splits * width * ldf) : nullptr;
+    float *dh_part = ws.take<float>(dh_fragments * BM * BN), *dw_part = ws.take<float>(dw_fragments * BM * BN);
     float *bias_part = a.d_bias ? ws.take<float>((size_t)(n_pad / 32) * width) : nullptr;
     const GemmArgs base = gemm_args(c, a, o);
-    const bool bf16 = base.bf16;
-    CUtensorMap h_k, h_mn, w_k, w_mn, g_k, g_mn, g_store;
-    const int hr = o.n_pad;
-    if (hr > 0) {
-        if ((rc = matrix_map(c, &h_k, o.pack.packed, a.dim, hr, o.ldp, 128, bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &h_mn, o.pack.packed, a.dim, hr, o.ldp, 64, bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &w_k, o.weight, a.dim, a.classes, o.ld_weight, B_ROWS, bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &w_mn, o.weight, a.dim, a.classes, o.ld_weight, 64, bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &g_k, g_piece, width, hr, width, 128, bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &g_mn, g_piece, width, hr, width, 64, bf16)) != QGBDT_OK) return rc;
-        if ((rc = matrix_map(c, &g_store, g_piece, width, hr, width, 32, bf16)) != QGBDT_OK) return rc;
-    }
+    const bool bf16 = base.bf16, out_map = rows_aligned(a.d_weight, a.ld_d_weight);
+    CUtensorMap h_k, h_mn, w_k, w_mn, g_k, g_mn, g_store, dh_map, dw_map, out;
+    if ((rc = matrix_map(c, &h_k, o.pack.packed, a.dim, n_pad, o.ldp, 128, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &h_mn, o.pack.packed, a.dim, n_pad, o.ldp, 64, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &w_k, o.weight, a.dim, a.classes, o.ld_weight, B_ROWS, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &w_mn, o.weight, a.dim, a.classes, o.ld_weight, 64, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &g_k, g_piece, width, n_pad, width, 128, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &g_mn, g_piece, width, n_pad, width, 64, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &g_store, g_piece, width, n_pad, width, 32, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &dh_map, dh_part, BN, (long long)dh_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &dw_map, dw_part, BN, (long long)dw_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    out = g_store;
+    if (out_map && (rc = matrix_map(c, &out, a.d_weight, a.dim, a.classes, a.ld_d_weight, 32, a.type)) != QGBDT_OK) return rc;
     for (int k = 0; k < pieces; ++k) {
         const int v0 = (int)(k * width);
-        const int nv = (int)(a.classes - v0 < width ? a.classes - v0 : width), cols = up(nv, 256);
-        if (hr > 0) {
-            GemmArgs g = base;
-            g.v0 = v0, g.n_tiles = cols / BN, g.bias_part = bias_part;
-            if ((rc = gemm<GRAD>(c, g, h_k, w_k, g_store, st)) != QGBDT_OK) return rc;
-            if (bias_part) {
-                k_bias_finish<<<cols / 32, 256, 0, st>>>(bias_part, cols, nv, a.grad_loss, base.count, a.d_bias + v0);
-                QG_LAUNCH_CHECK(c);
-            }
-            g = base;
-            g.v0 = v0, g.n_tiles = d_tiles, g.kb = (nv + BK - 1) / BK, g.splits = dh_splits, g.part = dh_part, g.part_rows = hr, g.ldp = ldf, g.add = k > 0;
-            if ((rc = gemm<DH>(c, g, g_k, w_mn, g_k, st)) != QGBDT_OK) return rc;
-        } else if (a.d_bias) {
-            QG_CUDA(c, cudaMemsetAsync(a.d_bias + v0, 0, sizeof(float) * nv, st));
-        }
+        const int nv = (int)(a.classes - v0 < width ? a.classes - v0 : width);
         GemmArgs g = base;
-        g.v0 = v0, g.m_tiles = cols / BM, g.n_tiles = d_tiles, g.splits = dw_splits, g.part = dw_part, g.part_rows = width, g.ldp = ldf;
-        if (!dw_part) g.out = a.d_weight, g.ld_out = a.ld_d_weight, g.out_vec = rows_aligned(a.d_weight, a.ld_d_weight);
-        if (hr == 0) {   // no rows: no operands, zeros out
-            QG_CUDA(c, cudaMemset2DAsync(reinterpret_cast<uint16_t *>(a.d_weight) + v0 * a.ld_d_weight, a.ld_d_weight * 2, 0, (size_t)a.dim * 2, nv, st));
-            continue;
+        g.v0 = v0, g.n_tiles = (int)(width / BN), g.bias_part = bias_part;
+        if ((rc = gemm<GRAD>(c, g, grad_units, h_k, w_k, g_store, g_store, st)) != QGBDT_OK) return rc;
+        if (bias_part) {
+            k_bias_finish<<<(nv + 31) / 32, 256, 0, st>>>(bias_part, (int)width, nv, a.grad_loss, base.count, a.d_bias + v0);
+            QG_LAUNCH_CHECK(c);
         }
-        if ((rc = gemm<DW>(c, g, g_mn, h_mn, g_mn, st)) != QGBDT_OK) return rc;
-        if (dw_part) {
-            char *out = reinterpret_cast<char *>(a.d_weight) + (size_t)v0 * a.ld_d_weight * 2;
-            rc = bf16 ? grad_finish<__nv_bfloat16>(c, dw_part, dw_splits, width, ldf, nullptr, nv, a.dim, a.grad_loss, base.count, out, a.ld_d_weight, st)
-                      : grad_finish<__half>(c, dw_part, dw_splits, width, ldf, nullptr, nv, a.dim, a.grad_loss, base.count, out, a.ld_d_weight, st);
-            if (rc != QGBDT_OK) return rc;
-        }
-    }
-    if (hr > 0) {
-        rc = bf16 ? grad_finish<__nv_bfloat16>(c, dh_part, dh_splits, hr, ldf, o.pack.pos_of, a.rows, a.dim, a.grad_loss, base.count, a.d_hidden, a.ld_d_hidden, st)
-                  : grad_finish<__half>(c, dh_part, dh_splits, hr, ldf, o.pack.pos_of, a.rows, a.dim, a.grad_loss, base.count, a.d_hidden, a.ld_d_hidden, st);
+        g = base;
+        g.v0 = v0, g.n_tiles = d_tiles, g.kb = kb_dh, g.add = k > 0;
+        if ((rc = gemm<DH>(c, g, dh_units, g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
+        g = base;
+        g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = d_tiles;
+        g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
+        if ((rc = gemm<DW>(c, g, dw_units, g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
+        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, o, dw_part, dw_units, g, nv, st) : dw_finish<__half>(c, a, o, dw_part, dw_units, g, nv, st);
         if (rc != QGBDT_OK) return rc;
     }
+    rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, o, dh_part, dh_units, d_tiles, kb_dh, st) : dh_finish<__half>(c, a, o, dh_part, dh_units, d_tiles, kb_dh, st);
+    if (rc != QGBDT_OK) return rc;
     return qg_ws_close(c, st);
 }
