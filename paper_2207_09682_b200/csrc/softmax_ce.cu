@@ -61,6 +61,7 @@ struct GemmArgs {
     const float *lse;           // [row]
     float *bias_part;           // [m_tiles * BM / 32][n_tiles * 256] column sums of g over 32 rows
     // DH and DW
+    int gang, gangs, rounds;    // units of a gang, gangs, column tiles / gang rounded up
     int add;                    // DH: add to the fragments of the pieces before
     uint16_t *out;              // DW
     long long ld_out;
@@ -80,23 +81,21 @@ __device__ __forceinline__ void tile_place(int t, int m_live, int n_tiles, int &
     n = t / gm;
     m = m0 + t - n * gm;
 }
-__device__ __forceinline__ int tile_number(int m, int n, int m_live, int n_tiles) {
-    const int m0 = m / GROUP_M * GROUP_M, gm = min(GROUP_M, m_live - m0);
-    return m0 * n_tiles + n * gm + m - m0;
-}
-
-// DH and DW have few tiles and long products, so whole tiles would leave SMs idle in the last round.  All blocks of
-// all tiles, tile after tile, are one line that is cut into equal runs, one per unit (pair of CTAs); a tile that a
-// cut falls into is summed from its fragments afterwards, in the order of the units.
+// DH and DW have few tiles and long products, so whole tiles would leave SMs idle in the last round, and their
+// first operand, g, is larger than L2.  Units (pairs of CTAs) work in gangs: the units of a gang take neighbouring
+// column tiles of the same rows and walk along the products together, so that a block of g comes out of DRAM once
+// for all of them.  All blocks of all row tiles (once per round of column tiles), one after the other, are a line
+// that is cut into equal runs, one per gang; a tile that a cut falls into is summed from its fragments afterwards,
+// in the order of the gangs.
 struct Line {
-    long long length;   // tiles * kb
-    int kb, units;      // units that get a run (each at least four blocks long)
-    __device__ Line(int tiles, int kb_, int all_units) : length((long long)tiles * kb_), kb(kb_) {
+    long long length;   // rounds * row tiles * kb
+    int kb, runs;       // gangs that get a run (each at least four blocks long)
+    __device__ Line(int lines, int kb_, int gangs) : length((long long)lines * kb_), kb(kb_) {
         const long long most = length / 4;
-        units = most < 1 ? 1 : most < all_units ? (int)most : all_units;
+        runs = most < 1 ? 1 : most < gangs ? (int)most : gangs;
     }
-    __device__ __forceinline__ long long start(int u) const { return length * u / units; }
-    __device__ __forceinline__ int unit_of(long long pos) const { return (int)(((pos + 1) * units - 1) / length); }
+    __device__ __forceinline__ long long start(int g) const { return length * g / runs; }
+    __device__ __forceinline__ int gang_of(long long pos) const { return (int)(((pos + 1) * runs - 1) / length); }
 };
 
 // What a unit works on next.
@@ -107,7 +106,7 @@ struct Work {
 };
 template <int MODE>
 struct Schedule {
-    int t, step, total, m_live, n_tiles, kb, unit;
+    int t, step, total, m_live, n_tiles, kb, unit, gang, member, size;
     long long pos, end;
     __device__ Schedule(const GemmArgs &a, int count) : n_tiles(a.n_tiles) {
         m_live = MODE == DW ? a.m_tiles : (count + BM - 1) / BM;
@@ -118,8 +117,9 @@ struct Schedule {
         t = unit;
         pos = end = 0;
         if (MODE == DH || MODE == DW) {
-            const Line line(total, kb, step);
-            if (line.length > 0 && unit < line.units) pos = line.start(unit), end = line.start(unit + 1);
+            size = a.gang, gang = unit / size, member = unit - gang * size;
+            const Line line(a.rounds * m_live, kb, a.gangs);
+            if (line.length > 0 && gang < line.runs) pos = line.start(gang), end = line.start(gang + 1);
         }
     }
     __device__ __forceinline__ bool next(Work &w) {
@@ -129,16 +129,20 @@ struct Schedule {
             w.kb0 = 0, w.kb1 = kb;
             t += step;
             return true;
+        } else {
+            while (pos < end) {
+                const int place = (int)(pos / kb), round = place / m_live;   // row tiles of round 0, of round 1, ...
+                w.m = place - round * m_live;
+                w.n = round * size + member;
+                w.kb0 = (int)(pos - (long long)place * kb);
+                w.kb1 = (int)min((long long)kb, w.kb0 + end - pos);
+                w.whole = w.kb0 == 0 && w.kb1 == kb;
+                w.fragment = MODE == DH ? (place + gang) * size + member : 2 * unit + (w.kb0 == 0);
+                pos += w.kb1 - w.kb0;
+                if (w.n < n_tiles) return true;   // the last round may have fewer column tiles than the gang units
+            }
+            return false;
         }
-        if (pos >= end) return false;
-        const int tile = (int)(pos / kb);
-        tile_place(tile, m_live, n_tiles, w.m, w.n);
-        w.kb0 = (int)(pos - (long long)tile * kb);
-        w.kb1 = (int)min((long long)kb, w.kb0 + end - pos);
-        w.whole = w.kb0 == 0 && w.kb1 == kb;
-        w.fragment = MODE == DH ? tile + unit : 2 * unit + (w.kb0 == 0);
-        pos += w.kb1 - w.kb0;
-        return true;
     }
 };
 
@@ -695,29 +699,30 @@ __device__ __forceinline__ void write4(T *o, int left, const float4 &s, float sc
 
 // dH: every row of the caller's, zeros where it has no label.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int units, int n_tiles, int kb, const int *pos_of, long long rows, int dim,
-                                                   const float *grad_loss, const int *count, T *out, long long ld_out) {
+__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, int gangs, int rounds, int kb, const int *pos_of, long long rows,
+                                                   int dim, const float *grad_loss, const int *count, T *out, long long ld_out) {
     const int n = *count, m_live = (n + BM - 1) / BM;
     const float scale = out_scale(grad_loss, n);
-    const Line line(m_live * n_tiles, kb, units);
+    const Line line(rounds * m_live, kb, gangs);
     const int quads = (dim + 3) / 4;
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * quads; i += (long long)gridDim.x * 256) {
         const long long r = i / quads;
         const int d = (int)(i - r * quads) * 4, p = pos_of[r];
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (p >= 0) {
-            const int t = tile_number(p / BM, d / BN, m_live, n_tiles);
-            const int u0 = line.unit_of((long long)t * kb), u1 = line.unit_of((long long)(t + 1) * kb - 1);
-            for (int u = u0; u <= u1; ++u) add4(s, part + ((long long)(t + u) * BM + p % BM) * BN + d % BN);
+            const int round = d / BN / gang, member = d / BN - round * gang, place = round * m_live + p / BM;
+            const int g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
+            for (int g = g0; g <= g1; ++g) add4(s, part + (((long long)(place + g) * gang + member) * BM + p % BM) * BN + d % BN);
         }
         write4(out + r * ld_out + d, dim - d, s, scale);
     }
 }
 
-// dW: the tiles that a cut falls into; block (u, y) looks at the cut in front of unit u + 1 and takes 8 rows.
+// dW: the tiles that a cut falls into; blocks x look at the cut in front of gang x / gang + 1 and the tile of member
+// x % gang, blocks y take 8 rows.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dw_finish(const float *part, int units, int m_tiles, int n_tiles, int rows, int dim, const float *grad_loss,
-                                                   const int *count, T *out, long long ld_out) {
+__global__ void __launch_bounds__(256) k_dw_finish(const float *part, int gang, int gangs, int rounds, int m_tiles, int n_tiles, int rows, int dim,
+                                                   const float *grad_loss, const int *count, T *out, long long ld_out) {
     const int n = *count, kb = (n + BK - 1) / BK;
     if (n == 0) {   // no labelled row: nothing has been written yet
         const int quads = (dim + 3) / 4;
@@ -728,23 +733,21 @@ __global__ void __launch_bounds__(256) k_dw_finish(const float *part, int units,
         }
         return;
     }
-    const Line line(m_tiles * n_tiles, kb, units);
-    const int u = blockIdx.x + 1;
-    if (u >= line.units) return;
-    const long long cut = line.start(u);
-    const int t = (int)(cut / kb);
-    if (cut == (long long)t * kb) return;
-    const int u0 = line.unit_of((long long)t * kb), u1 = line.unit_of((long long)(t + 1) * kb - 1);
-    if (u0 != u - 1) return;   // an earlier cut of the same tile
+    const Line line(rounds * m_tiles, kb, gangs);
+    const int g = blockIdx.x / gang + 1, member = blockIdx.x % gang;
+    if (g >= line.runs) return;
+    const long long cut = line.start(g);
+    const int place = (int)(cut / kb);
+    if (cut == (long long)place * kb) return;
+    const int g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
+    if (g0 != g - 1) return;   // an earlier cut of the same tile
     const float scale = out_scale(grad_loss, n);
-    int m, col;
-    tile_place(t, m_tiles, n_tiles, m, col);
-    col *= BN;
+    const int round = place / m_tiles, m = place - round * m_tiles, col = (round * gang + member) * BN;
     const int r = blockIdx.y * 8 + threadIdx.x / 32;
     if (m * BM + r >= rows) return;
     for (int d = (threadIdx.x & 31) * 4; d < BN && col + d < dim; d += 128) {
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k = u0; k <= u1; ++k) add4(s, part + ((long long)(2 * k + (k == u0)) * BM + r) * BN + d);
+        for (int k = g0; k <= g1; ++k) add4(s, part + ((long long)(2 * (k * gang + member) + (k == g0)) * BM + r) * BN + d);
         write4(out + (long long)(m * BM + r) * ld_out + col + d, dim - col - d, s, scale);
     }
 }
@@ -888,18 +891,38 @@ int unit_count(const qgbdt_ctx *c, long long tiles) {
     return tiles < 1 ? 1 : tiles < units ? (int)tiles : units;
 }
 
+// Gangs for products with `lines` row tiles of kb blocks each and n_tiles column tiles: of the sizes up to eight that
+// leave at most 6 % of the units without work the largest, or else the size that leaves the fewest.
+struct Gangs {
+    int size, gangs, rounds;
+    int units() const { return size * gangs; }
+};
+Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int n_tiles, long long kb) {
+    const int units = c->sm_count / CG;
+    Gangs best{1, units, n_tiles};
+    double best_use = 0.0;
+    for (int g = 1; g <= 8 && g <= n_tiles && g <= units; ++g) {
+        const int rounds = (n_tiles + g - 1) / g;
+        const double use = (double)(units / g * g) / units * n_tiles / (rounds * g);
+        if (use >= 0.94 || use > best_use) best = Gangs{g, units / g, rounds}, best_use = use;
+    }
+    const long long most = (best.rounds * m_tiles * kb + 3) / 4;   // runs hold at least four blocks
+    if (best.gangs > most) best.gangs = most < 1 ? 1 : (int)most;
+    return best;
+}
+
 template <typename T>
-int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, int units, int n_tiles, int kb, cudaStream_t st) {
+int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, const Gangs &g, int kb, cudaStream_t st) {
     const long long blocks = (a.rows * ((a.dim + 3) / 4) + 255) / 256;
     k_dh_finish<T><<<(unsigned)(blocks < c->sm_count * 16 ? blocks : c->sm_count * 16), 256, 0, st>>>(
-        part, units, n_tiles, kb, o.pack.pos_of, a.rows, a.dim, a.grad_loss, o.pack.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden);
+        part, g.size, g.gangs, g.rounds, kb, o.pack.pos_of, a.rows, a.dim, a.grad_loss, o.pack.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden);
     QG_LAUNCH_CHECK(c);
     return QGBDT_OK;
 }
 
 template <typename T>
-int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, int units, const GemmArgs &g, int rows, cudaStream_t st) {
-    k_dw_finish<T><<<dim3(units, BM / 8), 256, 0, st>>>(part, units, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, o.pack.count,
+int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, const GemmArgs &g, int rows, cudaStream_t st) {
+    k_dw_finish<T><<<dim3(g.gangs * g.gang, BM / 8), 256, 0, st>>>(part, g.gang, g.gangs, g.rounds, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, o.pack.count,
                                                        reinterpret_cast<T *>(a.d_weight) + g.v0 * a.ld_d_weight, a.ld_d_weight);
     QG_LAUNCH_CHECK(c);
     return QGBDT_OK;
@@ -950,10 +973,10 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     const int pieces = (int)((a.classes + width - 1) / width);
     width = up((a.classes + pieces - 1) / pieces, 256);
     const int d_tiles = (a.dim + BN - 1) / BN, m_tiles = n_pad / BM, kb_dh = (int)(width / BK);
-    const int grad_units = unit_count(c, m_tiles * (width / BN)), dh_units = unit_count(c, (long long)m_tiles * d_tiles * kb_dh / 4);
-    const int dw_units = unit_count(c, width / BM * d_tiles * (n_pad / BK) / 4);
-    if (grad_units < 0 || dh_units < 0 || dw_units < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
-    const size_t dh_fragments = (size_t)m_tiles * d_tiles + dh_units, dw_fragments = 2 * (size_t)dw_units;
+    const int grad_units = unit_count(c, m_tiles * (width / BN));
+    if (grad_units < 0 || unit_count(c, (long long)m_tiles * d_tiles) < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
+    const Gangs dh_gangs = gang_plan(c, m_tiles, d_tiles, kb_dh), dw_gangs = gang_plan(c, width / BM, d_tiles, n_pad / BK);
+    const size_t dh_fragments = ((size_t)m_tiles * dh_gangs.rounds + dh_gangs.gangs) * dh_gangs.size, dw_fragments = 2 * (size_t)dw_gangs.units();
     QgWorkspace ws;
     int rc = qg_ws_open(c,
                         common_bytes(a, copy, pieces * width) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size(dh_fragments * BM * BN, 4) +
@@ -991,15 +1014,17 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
         }
         g = base;
         g.v0 = v0, g.n_tiles = d_tiles, g.kb = kb_dh, g.add = k > 0;
-        if ((rc = gemm<DH>(c, g, dh_units, g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
+        g.gang = dh_gangs.size, g.gangs = dh_gangs.gangs, g.rounds = dh_gangs.rounds;
+        if ((rc = gemm<DH>(c, g, dh_gangs.units(), g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
         g = base;
         g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = d_tiles;
+        g.gang = dw_gangs.size, g.gangs = dw_gangs.gangs, g.rounds = dw_gangs.rounds;
         g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
-        if ((rc = gemm<DW>(c, g, dw_units, g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
-        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, o, dw_part, dw_units, g, nv, st) : dw_finish<__half>(c, a, o, dw_part, dw_units, g, nv, st);
+        if ((rc = gemm<DW>(c, g, dw_gangs.units(), g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
+        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, o, dw_part, g, nv, st) : dw_finish<__half>(c, a, o, dw_part, g, nv, st);
         if (rc != QGBDT_OK) return rc;
     }
-    rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, o, dh_part, dh_units, d_tiles, kb_dh, st) : dh_finish<__half>(c, a, o, dh_part, dh_units, d_tiles, kb_dh, st);
+    rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, o, dh_part, dh_gangs, kb_dh, st) : dh_finish<__half>(c, a, o, dh_part, dh_gangs, kb_dh, st);
     if (rc != QGBDT_OK) return rc;
     return qg_ws_close(c, st);
 }
