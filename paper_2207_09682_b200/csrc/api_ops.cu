@@ -56,6 +56,7 @@ int check_embed(qgbdt_ctx *c, const EmbedArgs &a, bool backward) {
     if (a.bag < 1 || a.bag > (1 << 20)) return qg_fail(c, QGBDT_ERR_ARG, "bag must be in [1, 2^20]");
     if (a.rows > ((1ll << 31) - 1) / a.bag) return qg_fail(c, QGBDT_ERR_ARG, "rows * bag must be below 2^31");
     if (a.ld < a.dim || a.ld_out < a.dim || a.ld_tokens < a.bag) return qg_fail(c, QGBDT_ERR_ARG, "a row stride is smaller than the row");
+    if (a.ld >= (1ll << 30) || a.ld_out >= (1ll << 30)) return qg_fail(c, QGBDT_ERR_ARG, "row strides must be below 2^30");
     if (!std::isfinite(a.scale)) return qg_fail(c, QGBDT_ERR_ARG, "scale must be finite");
     const bool none = a.rows == 0;
     if ((!none && (!a.table || !a.tokens)) || (!a.out && !(none && !backward))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");

@@ -19,8 +19,12 @@ namespace {
 constexpr int EMB_THREADS = 256;
 constexpr int EMB_UNROLL = 8;
 
-template <typename I>
-__device__ __forceinline__ long long token_at(const I *tokens, long long i) { return (long long)tokens[i]; }
+// A token as 32 bits: negative ones have the top bit, ones beyond 31 bits become 2^31 - 1 (which no table has).
+__device__ __forceinline__ unsigned token_at(const int32_t *tokens, long long i) { return (unsigned)tokens[i]; }
+__device__ __forceinline__ unsigned token_at(const int64_t *tokens, long long i) {
+    const int64_t t = tokens[i];
+    return t < 0 ? 0x80000000u : t < 0x7fffffff ? (unsigned)t : 0x7fffffffu;
+}
 
 struct EmbedPlan {
     int lg;        // log2 of the lanes per row
@@ -28,10 +32,39 @@ struct EmbedPlan {
     int col_blocks;
 };
 
+// Two single-precision sums in one instruction.
+__device__ __forceinline__ void add2(float &a, float &b, float x, float y) {
+    asm("{\n.reg .b64 s, t;\nmov.b64 s, {%0, %1};\nmov.b64 t, {%2, %3};\nadd.rn.f32x2 s, s, t;\nmov.b64 {%0, %1}, s;\n}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+
 template <typename T, int V>
 __device__ __forceinline__ void add_row(float (&acc)[V], const OpsVec<T, V> &x) {
+    if constexpr (V == 1) {
+        acc[0] += OpsType<T>::load(x.v[0]);
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) acc[j] += OpsType<T>::load(x.v[j]);
+        for (int j = 0; j < V; j += 2) add2(acc[j], acc[j + 1], x.v[j], x.v[j + 1]);
+    } else {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&x);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            const float2 y = unpack2(w[j / 2], T());
+            add2(acc[j], acc[j + 1], y.x, y.y);
+        }
+    }
+}
+
+// Row `t` of a matrix with rows of `ld_bytes` (below 2^32), or zeros: one 32 x 32 bit product per address.
+template <typename T, int V>
+__device__ __forceinline__ OpsVec<T, V> row_or_zero(const T *p, unsigned t, unsigned ld_bytes, bool on) {
+    OpsVec<T, V> x;
+#pragma unroll
+    for (int j = 0; j < V; ++j) x.v[j] = OpsType<T>::store(0.0f);
+    if (on) x = *reinterpret_cast<const OpsVec<T, V> *>(reinterpret_cast<const char *>(p) + (unsigned long long)t * ld_bytes);
+    return x;
 }
 
 // One group of lanes per (row, part of the bag, column block).  Eight rows of the table are in flight per group.
@@ -47,6 +80,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
     const bool live = row < a.rows && col < a.dim;
     const I *tok = reinterpret_cast<const I *>(a.tokens) + row * a.ld_tokens;
     const T *table = reinterpret_cast<const T *>(a.table) + col;
+    const unsigned ld_bytes = (unsigned)(a.ld * sizeof(T)), n_entries = (unsigned)a.n_entries;
     float acc[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) acc[j] = 0.0f;
@@ -54,18 +88,17 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
         const int k0 = (int)((long long)a.bag * part >> p.split), k1 = (int)((long long)a.bag * (part + 1) >> p.split);
         bool bad = false;
         for (int k = k0; k < k1; k += EMB_UNROLL) {
-            long long t[EMB_UNROLL];
+            unsigned t[EMB_UNROLL];   // 2^31 and more: missing
             Vec x[EMB_UNROLL];
 #pragma unroll
-            for (int u = 0; u < EMB_UNROLL; ++u) t[u] = k + u < k1 ? token_at(tok, k + u) : -1;
+            for (int u = 0; u < EMB_UNROLL; ++u) t[u] = k + u < k1 ? token_at(tok, k + u) : 0x80000000u;
+#pragma unroll
+            for (int u = 0; u < EMB_UNROLL; ++u) x[u] = row_or_zero<T, V>(table, t[u], ld_bytes, t[u] < n_entries);
 #pragma unroll
             for (int u = 0; u < EMB_UNROLL; ++u) {
-                if (t[u] >= a.n_entries) bad = true, t[u] = -1;
-                if (t[u] >= 0) x[u] = *reinterpret_cast<const Vec *>(table + t[u] * a.ld);
+                add_row(acc, x[u]);
+                bad |= t[u] >= n_entries && t[u] < 0x80000000u;
             }
-#pragma unroll
-            for (int u = 0; u < EMB_UNROLL; ++u)
-                if (t[u] >= 0) add_row(acc, x[u]);
         }
         if (bad && lane == 0 && a.status) *a.status = 1;
     }
@@ -91,17 +124,29 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
 struct SortArgs {
     const void *tokens;
     long long ld_tokens, n_entries, n;   // n pairs
-    int bag;
+    unsigned bag, div_mul, div_shift;    // i / bag == (i * div_mul) >> div_shift in 64 bits, for i < 2^31
     int32_t *status;
 };
 
-// Token and row of pair i; a missing or bad token becomes n_entries and sorts behind all others.
+// floor(i / d) for i < 2^31 as a product: with shift = 31 + ceil(log2 d) and mul = ceil(2^shift / d), mul < 2^32 and the
+// error i * (mul * d - 2^shift) / (d * 2^shift) stays below 1 / d.
+void set_divisor(SortArgs &a, unsigned d) {
+    unsigned l = 0;
+    while ((1ull << l) < d) ++l;
+    a.bag = d;
+    a.div_shift = 31 + l;
+    a.div_mul = (unsigned)(((1ull << a.div_shift) + d - 1) / d);
+}
+__device__ __forceinline__ unsigned div_bag(const SortArgs &a, unsigned i) { return (unsigned)(((unsigned long long)i * a.div_mul) >> a.div_shift); }
+
+// Token and row of pair i; a missing or bad token becomes n_entries and sorts behind all others.  (Bad ones are
+// reported by the caller behind its loads: a store between them would keep the loads from overlapping.)
 template <typename I>
-__device__ __forceinline__ uint2 pair_at(const SortArgs &a, long long i) {
-    const unsigned row = (unsigned)i / (unsigned)a.bag, k = (unsigned)i - row * (unsigned)a.bag;
-    const long long t = token_at(reinterpret_cast<const I *>(a.tokens), (long long)row * a.ld_tokens + k);
-    if (t >= a.n_entries && a.status) *a.status = 1;
-    return make_uint2(t >= 0 && t < a.n_entries ? (unsigned)t : (unsigned)a.n_entries, row);
+__device__ __forceinline__ uint2 pair_at(const SortArgs &a, long long i, bool &bad) {
+    const unsigned row = div_bag(a, (unsigned)i), k = (unsigned)i - row * a.bag;
+    const unsigned t = token_at(reinterpret_cast<const I *>(a.tokens), (long long)row * a.ld_tokens + k), n = (unsigned)a.n_entries;
+    bad |= t >= n && t < 0x80000000u;
+    return make_uint2(t < n ? t : n, row);
 }
 
 // Few pairs: every pair's place is the number of pairs before it, counted directly; one launch.
@@ -112,7 +157,10 @@ template <typename I>
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, uint2 *out) {
     __shared__ alignas(16) unsigned key[SORT_SMALL];
     const int n = (int)a.n, n4 = (n + 3) / 4;
-    for (int i = threadIdx.x; i < n4 * 4; i += EMB_THREADS) key[i] = i < n ? pair_at<I>(a, i).x : 0xffffffffu;
+    bool bad = false;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n4 * 4; i += EMB_THREADS) key[i] = i < n ? pair_at<I>(a, i, bad).x : 0xffffffffu;
+    if (bad && a.status) *a.status = 1;
     __syncthreads();
     const int e = (blockIdx.x * EMB_THREADS + threadIdx.x) / SORT_SMALL_LANES, lane = threadIdx.x % SORT_SMALL_LANES;
     const unsigned mine = e < n ? key[e] : 0;
@@ -124,31 +172,38 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, ui
     }
 #pragma unroll
     for (int o = SORT_SMALL_LANES / 2; o; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
-    if (e < n && lane == 0) out[before] = make_uint2(mine, (unsigned)e / (unsigned)a.bag);
+    if (e < n && lane == 0) out[before] = make_uint2(mine, div_bag(a, (unsigned)e));
 }
 
-// Many pairs: least significant digit first, up to 11 bits a pass; a pass is a count per block and digit, a
-// scan, and a stable scatter.
-constexpr int SORT_MAX_BITS = 11;
+// Many pairs: least significant digit first, up to 9 bits a pass; a pass is a count per block and digit, a
+// scan, and a stable scatter.  A block scatters tiles of 4096 pairs: every warp ranks its pairs among its own by
+// matching digits across the lanes (a ballot per bit), the tile is put in order in shared memory, and runs of equal digits leave it
+// as neighbouring words.
+constexpr int SORT_MIN_BITS = 6, SORT_MAX_BITS = 9;
 constexpr int SORT_WARPS = EMB_THREADS / 32;
-constexpr int SORT_ROUNDS = 16;                                    // pairs per lane and tile
+constexpr int SORT_ROUNDS = 8;                                    // pairs per lane and tile
 constexpr int SORT_TILE = EMB_THREADS * SORT_ROUNDS;
-
-template <typename I, bool FIRST>
-__device__ __forceinline__ uint2 sort_load(const SortArgs &a, const uint2 *in, long long i) {
-    return FIRST ? pair_at<I>(a, i) : in[i];
-}
 
 template <typename I, bool FIRST>
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const uint2 *in, int shift, int bits, long long per_block,
                                                             unsigned *counts) {
-    __shared__ unsigned cnt[1 << SORT_MAX_BITS];
+    extern __shared__ unsigned sort_smem[];
+    unsigned *cnt = sort_smem;   // [1 << bits]
     const int digits = 1 << bits;
     for (int d = threadIdx.x; d < digits; d += EMB_THREADS) cnt[d] = 0;
     __syncthreads();
     const long long i0 = per_block * blockIdx.x, i1 = i0 + per_block < a.n ? i0 + per_block : a.n;
-    for (long long i = i0 + threadIdx.x; i < i1; i += EMB_THREADS)
-        atomicAdd(&cnt[(sort_load<I, FIRST>(a, in, i).x >> shift) & (digits - 1)], 1u);
+    for (long long i = i0 + threadIdx.x; i < i1; i += EMB_THREADS * SORT_ROUNDS) {
+        unsigned key[SORT_ROUNDS];
+        bool bad = false;
+#pragma unroll
+        for (int r = 0; r < SORT_ROUNDS; ++r)
+            if (i + r * EMB_THREADS < i1) key[r] = FIRST ? pair_at<I>(a, i + r * EMB_THREADS, bad).x : in[i + r * EMB_THREADS].x;
+        if (bad && a.status) *a.status = 1;
+#pragma unroll
+        for (int r = 0; r < SORT_ROUNDS; ++r)
+            if (i + r * EMB_THREADS < i1) atomicAdd(&cnt[(key[r] >> shift) & (digits - 1)], 1u);
+    }
     __syncthreads();
     for (int d = threadIdx.x; d < digits; d += EMB_THREADS) counts[(size_t)d * gridDim.x + blockIdx.x] = cnt[d];
 }
@@ -172,28 +227,41 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_scan(unsigned *counts, uns
     if (lane == 0) totals[d] = run;
 }
 
-template <typename I, bool FIRST>
-__global__ void __launch_bounds__(EMB_THREADS) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, int bits, long long per_block,
-                                                              const unsigned *counts, const unsigned *totals, uint2 *out) {
-    __shared__ unsigned short cnt[SORT_WARPS][1 << SORT_MAX_BITS];   // per warp and digit: pairs so far in this tile, then those of earlier warps
-    __shared__ unsigned base[1 << SORT_MAX_BITS];                    // where the next pair of a digit goes
+size_t scatter_smem(int bits) { return (size_t)SORT_TILE * sizeof(uint2) + ((size_t)8 + 2 * SORT_WARPS) * ((size_t)1 << bits); }
+
+// Exclusive scan over the block of one number per thread.
+__device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    unsigned inc = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+    }
+    if (lane == 31) warp_sum[warp] = inc;
+    __syncthreads();
+    unsigned run = inc - x;
+    for (int w = 0; w < warp; ++w) run += warp_sum[w];
+    __syncthreads();
+    return run;
+}
+
+template <typename I, bool FIRST, int BITS>
+__global__ void __launch_bounds__(EMB_THREADS) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, long long per_block, const unsigned *counts,
+                                                              const unsigned *totals, uint2 *out) {
+    extern __shared__ unsigned sort_smem[];
     __shared__ unsigned warp_sum[SORT_WARPS];
-    const int digits = 1 << bits, warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    // base = pairs of smaller digits (scan of the totals) + pairs of this digit in earlier blocks
-    {
-        const int per = (digits + EMB_THREADS - 1) / EMB_THREADS, d0 = threadIdx.x * per;
+    constexpr int digits = 1 << BITS;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    uint2 *sorted = reinterpret_cast<uint2 *>(sort_smem);                       // [SORT_TILE] the tile in order
+    unsigned *base = reinterpret_cast<unsigned *>(sorted + SORT_TILE);          // [digits] where the tile's pairs of a digit go
+    unsigned *begin = base + digits;                                            // [digits] where they begin in the tile
+    unsigned short *cnt = reinterpret_cast<unsigned short *>(begin + digits);   // [SORT_WARPS][digits] pairs of a warp, then those of earlier warps
+    const int per = (digits + EMB_THREADS - 1) / EMB_THREADS, d0 = threadIdx.x * per;   // digits of this thread in the scans
+    {   // base = pairs of smaller digits (scan of the totals) + pairs of this digit in earlier blocks
         unsigned s = 0;
         for (int j = 0; j < per && d0 + j < digits; ++j) s += totals[d0 + j];
-        unsigned inc = s;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned y = __shfl_up_sync(0xffffffffu, inc, o);
-            if (lane >= o) inc += y;
-        }
-        if (lane == 31) warp_sum[warp] = inc;
-        __syncthreads();
-        unsigned run = inc - s;
-        for (int w = 0; w < warp; ++w) run += warp_sum[w];
+        unsigned run = block_scan(s, warp_sum);
         for (int j = 0; j < per && d0 + j < digits; ++j) {
             base[d0 + j] = run + counts[(size_t)(d0 + j) * gridDim.x + blockIdx.x];
             run += totals[d0 + j];
@@ -201,57 +269,72 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_scatter(const SortArgs a, 
     }
     const long long i0 = per_block * blockIdx.x, i1 = i0 + per_block < a.n ? i0 + per_block : a.n;
     for (long long tile = i0; tile < i1; tile += SORT_TILE) {
-        for (int d = threadIdx.x; d < digits * SORT_WARPS; d += EMB_THREADS) cnt[d >> bits][d & (digits - 1)] = 0;
-        __syncthreads();
         const long long w0 = tile + (long long)warp * 32 * SORT_ROUNDS;   // a warp's pairs are consecutive: its rounds keep their order
         uint2 pair[SORT_ROUNDS];
-        unsigned short place[SORT_ROUNDS];
 #pragma unroll
         for (int r = 0; r < SORT_ROUNDS; ++r) {
             const long long i = w0 + r * 32 + lane;
-            if (i < i1) pair[r] = sort_load<I, FIRST>(a, in, i);
+            bool bad;   // reported by the count
+            if (i < i1) pair[r] = FIRST ? pair_at<I>(a, i, bad) : in[i];
         }
+        for (int d = threadIdx.x; d < digits * SORT_WARPS / 2; d += EMB_THREADS) reinterpret_cast<unsigned *>(cnt)[d] = 0;
+        __syncthreads();
+        unsigned short place[SORT_ROUNDS], *mine = cnt + warp * digits;
 #pragma unroll
         for (int r = 0; r < SORT_ROUNDS; ++r) {
             const bool on = w0 + r * 32 + lane < i1;
-            const unsigned d = on ? (pair[r].x >> shift) & (digits - 1) : 0xffffffffu;
-            const unsigned same = __match_any_sync(0xffffffffu, d), below = __popc(same & ((1u << lane) - 1));
+            const unsigned d = on ? (pair[r].x >> shift) & (digits - 1) : 0u;
+            unsigned same = __ballot_sync(0xffffffffu, on);   // lanes with the same digit
+#pragma unroll
+            for (int b = 0; b < BITS; ++b) {
+                const unsigned set = __ballot_sync(0xffffffffu, d >> b & 1);
+                same &= d >> b & 1 ? set : ~set;
+            }
+            const unsigned below = __popc(same & ((1u << lane) - 1));
             unsigned short old = 0;
-            if (on) old = cnt[warp][d];
+            if (on) old = mine[d];
             __syncwarp();
-            if (on && below == 0) cnt[warp][d] = (unsigned short)(old + __popc(same));
+            if (on && below == 0) mine[d] = (unsigned short)(old + __popc(same));
             __syncwarp();
             place[r] = (unsigned short)(old + below);
         }
         __syncthreads();
-        unsigned add[(1 << SORT_MAX_BITS) / EMB_THREADS];
-#pragma unroll
-        for (int j = 0; j < (1 << SORT_MAX_BITS) / EMB_THREADS; ++j) {
-            const int d = threadIdx.x + j * EMB_THREADS;
+        unsigned sum = 0;
+        for (int j = 0; j < per && d0 + j < digits; ++j) {
             unsigned run = 0;
-            if (d < digits) {
 #pragma unroll
-                for (int w = 0; w < SORT_WARPS; ++w) {
-                    const unsigned x = cnt[w][d];
-                    cnt[w][d] = (unsigned short)run;
-                    run += x;
-                }
+            for (int w = 0; w < SORT_WARPS; ++w) {
+                const unsigned x = cnt[w * digits + d0 + j];
+                cnt[w * digits + d0 + j] = (unsigned short)run;
+                run += x;
             }
-            add[j] = run;
+            begin[d0 + j] = run;
+            sum += run;
+        }
+        unsigned run = block_scan(sum, warp_sum);
+        for (int j = 0; j < per && d0 + j < digits; ++j) {
+            const unsigned x = begin[d0 + j];
+            begin[d0 + j] = run;
+            run += x;
         }
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < SORT_ROUNDS; ++r)
             if (w0 + r * 32 + lane < i1) {
                 const unsigned d = (pair[r].x >> shift) & (digits - 1);
-                out[base[d] + cnt[warp][d] + place[r]] = pair[r];
+                sorted[begin[d] + mine[d] + place[r]] = pair[r];
             }
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < (1 << SORT_MAX_BITS) / EMB_THREADS; ++j) {
-            const int d = threadIdx.x + j * EMB_THREADS;
-            if (d < digits) base[d] += add[j];
+        const int n = (int)(i1 - tile < SORT_TILE ? i1 - tile : SORT_TILE);
+        for (int i = threadIdx.x; i < n; i += EMB_THREADS) {
+            const uint2 p = sorted[i];
+            const unsigned d = (p.x >> shift) & (digits - 1);
+            out[base[d] + i - begin[d]] = p;
         }
+        __syncthreads();
+        for (int j = 0; j < per && d0 + j < digits; ++j)   // begin of the next digit - begin = pairs of this digit in the tile
+            base[d0 + j] += (d0 + j + 1 < digits ? begin[d0 + j + 1] : (unsigned)n) - begin[d0 + j];
+        __syncthreads();
     }
 }
 
@@ -345,18 +428,30 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_sum(const SegArgs a) {
             *reinterpret_cast<Vec *>(reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col) = y;
         }
     };
+    const unsigned ld_bytes = (unsigned)(a.ld * sizeof(T));
+    // the list is padded to whole batches, which start on 64 bytes; a batch's pairs are loaded under the rows of the one before
+    OpsVec<uint2, 2> next[EMB_UNROLL / 2];
+    auto load_pairs = [&](long long i) {
+#pragma unroll
+        for (int u = 0; u < EMB_UNROLL / 2; ++u) next[u] = reinterpret_cast<const OpsVec<uint2, 2> *>(a.pair + i)[u];
+    };
+    load_pairs(i0);
     for (long long i = i0; i < i1; i += EMB_UNROLL) {
         uint2 p[EMB_UNROLL];
         Vec x[EMB_UNROLL];
-#pragma unroll
-        for (int u = 0; u < EMB_UNROLL; ++u) p[u] = i + u < i1 ? a.pair[i + u] : make_uint2(none, 0);
-#pragma unroll
-        for (int u = 0; u < EMB_UNROLL; ++u)
-            if (p[u].x != none) x[u] = *reinterpret_cast<const Vec *>(grad + (long long)p[u].y * a.ld);
+        const int left = (int)(i1 - i);
 #pragma unroll
         for (int u = 0; u < EMB_UNROLL; ++u) {
-            if (p[u].x == none) continue;   // behind the tile's end, or a missing token (these are sorted last)
+            p[u] = next[u / 2].v[u & 1];
+            if (u >= left) p[u].x = none;   // behind the tile's end; missing tokens are `none` as well, and sorted last
+        }
+#pragma unroll
+        for (int u = 0; u < EMB_UNROLL; ++u) x[u] = row_or_zero<T, V>(grad, p[u].y, ld_bytes, p[u].x != none);
+        if (left > EMB_UNROLL) load_pairs(i + EMB_UNROLL);
+#pragma unroll
+        for (int u = 0; u < EMB_UNROLL; ++u) {
             if (p[u].x != cur) {
+                if (p[u].x == none) break;
                 finish();
                 cur = p[u].x;
                 from_before = false;
@@ -370,35 +465,84 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_sum(const SegArgs a) {
     else finish();
 }
 
-// Tokens that cross tile borders: the block of the tile where such a token begins adds its partial sums
-// in tile order (cut into 256 / columns runs that are added in order as well).
-template <typename T>
+// Tokens that cross tile borders: a group of 2^lg_cols threads per tile where such a token begins adds its partial
+// sums in tile order.  A token of very many tiles is cut into runs, one per group of the block, which are added in
+// order as well (the block belongs to such a token's first tile alone then).
+constexpr int JOIN_SERIAL = 32;   // tiles that one group adds by itself
+
+template <typename T, int V>
 __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, int lg_cols) {
-    __shared__ float part_sum[EMB_THREADS];
-    const long long t = blockIdx.x;
-    const long long i0 = t * a.tile, i1 = i0 + a.tile;
-    if (i1 >= a.n) return;
-    const unsigned cur = a.pair[i1].x;
-    if (cur == (unsigned)a.n_entries || a.pair[i1 - 1].x != cur || (a.pair[i0].x == cur && i0 > 0 && a.pair[i0 - 1].x == cur)) return;
-    const long long last = first_not_below(a.pair, a.n, cur + 1) - 1;   // the token's last pair
-    const long long links = last / a.tile - t;                           // slot 0 of tiles t + 1 .. t + links
-    const int cols = 1 << lg_cols, parts = EMB_THREADS >> lg_cols, part = threadIdx.x >> lg_cols;
-    const long long l0 = links * part / parts, l1 = links * (part + 1) / parts;
-    for (int c0 = 0; c0 < a.dim; c0 += cols) {
-        const int col = c0 + (threadIdx.x & (cols - 1));
-        float s = 0.0f;
-        if (col < a.dim) {
-            if (part == 0) s = a.partial[(t * 2 + 1) * a.dim + col];
+    __shared__ float part_sum[EMB_THREADS][V];
+    const int cols = 1 << lg_cols, groups = EMB_THREADS >> lg_cols, group = threadIdx.x >> lg_cols, lane = threadIdx.x & (cols - 1);
+    const unsigned none = (unsigned)a.n_entries;
+    // does a token that goes on behind tile t begin in it, and how many more tiles has it?
+    auto begins = [&](long long t, unsigned &cur) {
+        const long long i0 = t * a.tile, i1 = i0 + a.tile;
+        if (i1 >= a.n) return false;
+        cur = a.pair[i1].x;
+        return cur != none && a.pair[i1 - 1].x == cur && !(i0 > 0 && a.pair[i0 - 1].x == cur);
+    };
+    auto links_of = [&](long long t, unsigned cur) {   // tiles t + 1 .. t + links hold the rest of it
+        long long lo = 1, hi = 2;                      // tile t + lo holds some of it; does t + hi begin with it?
+        auto inside = [&](long long l) { return (t + l) * a.tile < a.n && a.pair[(t + l) * a.tile].x == cur; };
+        while (inside(hi)) lo = hi, hi *= 2;
+        while (hi - lo > 1) {
+            const long long mid = (lo + hi) >> 1;
+            if (inside(mid)) lo = mid;
+            else hi = mid;
+        }
+        return lo;
+    };
+    auto add = [&](float (&s)[V], const float *p) {
+        const OpsVec<float, V> x = *reinterpret_cast<const OpsVec<float, V> *>(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] += x.v[j];
+    };
+    auto put = [&](unsigned cur, int col, const float (&s)[V]) {
+        OpsVec<T, V> y;
+#pragma unroll
+        for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(s[j] * a.scale);
+        *reinterpret_cast<OpsVec<T, V> *>(reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col) = y;
+    };
+    // tokens of few tiles: a group each
+    const long long t0 = (long long)blockIdx.x * groups, mine = t0 + group;
+    unsigned cur = 0;
+    long long links = 0;
+    if (begins(mine, cur)) links = links_of(mine, cur);
+    if (links > 0 && links <= JOIN_SERIAL)
+        for (int col = lane * V; col < a.dim; col += cols * V) {
+            float s[V] = {};
+            add(s, a.partial + (mine * 2 + 1) * a.dim + col);
 #pragma unroll 4
-            for (long long l = l0; l < l1; ++l) s += a.partial[((t + 1 + l) * 2) * a.dim + col];
+            for (long long l = 1; l <= links; ++l) add(s, a.partial + ((mine + l) * 2) * a.dim + col);
+            put(cur, col, s);
         }
-        part_sum[threadIdx.x] = s;
-        __syncthreads();
-        if (part == 0 && col < a.dim) {
-            for (int q = 1; q < parts; ++q) s += part_sum[threadIdx.x + (q << lg_cols)];
-            reinterpret_cast<T *>(a.out)[(long long)cur * a.ld_out + col] = OpsType<T>::store(s * a.scale);
+    if (!__syncthreads_or(links > JOIN_SERIAL)) return;
+    for (int q = 0; q < groups; ++q) {   // the whole block for each of the others
+        const long long t = t0 + q;
+        if (!begins(t, cur)) continue;
+        links = links_of(t, cur);
+        if (links <= JOIN_SERIAL) continue;
+        const long long l0 = links * group / groups, l1 = links * (group + 1) / groups;
+        for (int c0 = 0; c0 < a.dim; c0 += cols * V) {
+            const int col = c0 + lane * V;
+            float s[V] = {};
+            if (col < a.dim) {
+                if (group == 0) add(s, a.partial + (t * 2 + 1) * a.dim + col);
+#pragma unroll 4
+                for (long long l = l0; l < l1; ++l) add(s, a.partial + ((t + 1 + l) * 2) * a.dim + col);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) part_sum[threadIdx.x][j] = s[j];
+            __syncthreads();
+            if (group == 0 && col < a.dim) {
+                for (int g = 1; g < groups; ++g)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) s[j] += part_sum[threadIdx.x + (g << lg_cols)][j];
+                put(cur, col, s);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
@@ -446,9 +590,10 @@ SortPlan sort_plan(const qgbdt_ctx *c, long long n, long long n_entries) {
     s.passes = (bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS;
     if (s.passes < 1) s.passes = 1;
     s.bits = (bits + s.passes - 1) / s.passes;
-    if (s.bits < 1) s.bits = 1;
+    if (s.bits < SORT_MIN_BITS) s.bits = SORT_MIN_BITS;
     const long long tiles = (n + SORT_TILE - 1) / SORT_TILE;
-    s.blocks = (int)(tiles < 2 * c->sm_count ? tiles : 2 * c->sm_count);
+    const long long most = 4ll * c->sm_count;   // blocks that fit beside one another
+    s.blocks = (int)(tiles < most ? tiles : most);
     s.per_block = (tiles + s.blocks - 1) / s.blocks * SORT_TILE;
     return s;
 }
@@ -463,16 +608,20 @@ int sort_pairs(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, uint2 *buf0, 
         return QGBDT_OK;
     }
     const int digits = 1 << s.bits;
+    const size_t count_smem = digits * sizeof(unsigned), smem = scatter_smem(s.bits);
     uint2 *in = buf1, *out = buf0;
     for (int k = 0; k < s.passes; ++k) {
         const int shift = k * s.bits;
-        if (k == 0) k_sort_count<I, true><<<s.blocks, EMB_THREADS, 0, st>>>(a, in, shift, s.bits, s.per_block, counts);
-        else k_sort_count<I, false><<<s.blocks, EMB_THREADS, 0, st>>>(a, in, shift, s.bits, s.per_block, counts);
+        if (k == 0) k_sort_count<I, true><<<s.blocks, EMB_THREADS, count_smem, st>>>(a, in, shift, s.bits, s.per_block, counts);
+        else k_sort_count<I, false><<<s.blocks, EMB_THREADS, count_smem, st>>>(a, in, shift, s.bits, s.per_block, counts);
         QG_LAUNCH_CHECK(c);
         k_sort_scan<<<(digits + SORT_WARPS - 1) / SORT_WARPS, EMB_THREADS, 0, st>>>(counts, totals, digits, s.blocks);
         QG_LAUNCH_CHECK(c);
-        if (k == 0) k_sort_scatter<I, true><<<s.blocks, EMB_THREADS, 0, st>>>(a, in, shift, s.bits, s.per_block, counts, totals, out);
-        else k_sort_scatter<I, false><<<s.blocks, EMB_THREADS, 0, st>>>(a, in, shift, s.bits, s.per_block, counts, totals, out);
+        const auto scatter = s.bits == 6 ? (k == 0 ? k_sort_scatter<I, true, 6> : k_sort_scatter<I, false, 6>)
+                             : s.bits == 7 ? (k == 0 ? k_sort_scatter<I, true, 7> : k_sort_scatter<I, false, 7>)
+                             : s.bits == 8 ? (k == 0 ? k_sort_scatter<I, true, 8> : k_sort_scatter<I, false, 8>)
+                                           : (k == 0 ? k_sort_scatter<I, true, 9> : k_sort_scatter<I, false, 9>);
+        scatter<<<s.blocks, EMB_THREADS, smem, st>>>(a, in, shift, s.per_block, counts, totals, out);
         QG_LAUNCH_CHECK(c);
         uint2 *swap = in;
         in = out;
@@ -490,7 +639,10 @@ int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     k_segment_sum<T, V><<<(unsigned)blocks, EMB_THREADS, 0, st>>>(s);
     QG_LAUNCH_CHECK(c);
     if (s.tiles > 1) {
-        k_segment_join<T><<<(unsigned)(s.tiles - 1), EMB_THREADS, 0, st>>>(s, log2_at_least(s.dim, 8));
+        // four columns at most per thread: their partial sums are one 16-byte load
+        constexpr int JV = V < 4 ? V : 4;
+        const int lg = log2_at_least((s.dim + JV - 1) / JV, 7);
+        k_segment_join<T, JV><<<(unsigned)((s.tiles - 2) / (EMB_THREADS >> lg) + 1), EMB_THREADS, 0, st>>>(s, lg);
         QG_LAUNCH_CHECK(c);
     }
     return QGBDT_OK;
@@ -527,17 +679,18 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     const bool small = n <= SORT_SMALL;
     const SortPlan sp = small ? SortPlan{} : sort_plan(c, n, a.n_entries);
     const size_t digits = small ? 0 : (size_t)1 << sp.bits;
-    const size_t bytes = 2 * qg_ws_size((size_t)n, sizeof(uint2)) + qg_ws_size(digits * (sp.blocks + 1), sizeof(unsigned)) +
+    const size_t bytes = 2 * qg_ws_size((size_t)n + EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * (sp.blocks + 1), sizeof(unsigned)) +
                          qg_ws_size(digits, sizeof(unsigned)) + qg_ws_size((size_t)s.tiles * 2 * a.dim, sizeof(float));
     QgWorkspace ws;
     int rc = qg_ws_open(c, bytes, st, &ws);
     if (rc != QGBDT_OK) return rc;
-    uint2 *buf0 = ws.take<uint2>((size_t)n), *buf1 = ws.take<uint2>((size_t)n);
+    uint2 *buf0 = ws.take<uint2>((size_t)n + EMB_UNROLL), *buf1 = ws.take<uint2>((size_t)n + EMB_UNROLL);
     unsigned *counts = ws.take<unsigned>(digits * sp.blocks), *totals = ws.take<unsigned>(digits);
     s.partial = ws.take<float>((size_t)s.tiles * 2 * a.dim);
     s.pair = buf0;
     if (n > 0) {
-        const SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, a.bag, a.status};
+        SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, 0, 0, 0, a.status};
+        set_divisor(sa, (unsigned)a.bag);
         rc = a.token_type == QGBDT_I64 ? sort_pairs<int64_t>(c, sa, sp, buf0, buf1, counts, totals, &s.pair, st)
                                        : sort_pairs<int32_t>(c, sa, sp, buf0, buf1, counts, totals, &s.pair, st);
         if (rc != QGBDT_OK) return rc;
