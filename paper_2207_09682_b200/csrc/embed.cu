@@ -87,11 +87,12 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
     if (live) {
         const int k0 = (int)((long long)a.bag * part >> p.split), k1 = (int)((long long)a.bag * (part + 1) >> p.split);
         bool bad = false;
-        for (int k = k0; k < k1; k += EMB_UNROLL) {
+        int k = k0;
+        for (; k + EMB_UNROLL <= k1; k += EMB_UNROLL) {
             unsigned t[EMB_UNROLL];   // 2^31 and more: missing
             Vec x[EMB_UNROLL];
 #pragma unroll
-            for (int u = 0; u < EMB_UNROLL; ++u) t[u] = k + u < k1 ? token_at(tok, k + u) : 0x80000000u;
+            for (int u = 0; u < EMB_UNROLL; ++u) t[u] = token_at(tok, k + u);
 #pragma unroll
             for (int u = 0; u < EMB_UNROLL; ++u) x[u] = row_or_zero<T, V>(table, t[u], ld_bytes, t[u] < n_entries);
 #pragma unroll
@@ -99,6 +100,12 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
                 add_row(acc, x[u]);
                 bad |= t[u] >= n_entries && t[u] < 0x80000000u;
             }
+        }
+#pragma unroll 4
+        for (; k < k1; ++k) {
+            const unsigned t = token_at(tok, k);
+            add_row(acc, row_or_zero<T, V>(table, t, ld_bytes, t < n_entries));
+            bad |= t >= n_entries && t < 0x80000000u;
         }
         if (bad && lane == 0 && a.status) *a.status = 1;
     }
@@ -193,15 +200,16 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, co
     for (int d = threadIdx.x; d < digits; d += EMB_THREADS) cnt[d] = 0;
     __syncthreads();
     const long long i0 = per_block * blockIdx.x, i1 = i0 + per_block < a.n ? i0 + per_block : a.n;
-    for (long long i = i0 + threadIdx.x; i < i1; i += EMB_THREADS * SORT_ROUNDS) {
-        unsigned key[SORT_ROUNDS];
+    constexpr int LOADS = 16;
+    for (long long i = i0 + threadIdx.x; i < i1; i += EMB_THREADS * LOADS) {
+        unsigned key[LOADS];
         bool bad = false;
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r)
+        for (int r = 0; r < LOADS; ++r)
             if (i + r * EMB_THREADS < i1) key[r] = FIRST ? pair_at<I>(a, i + r * EMB_THREADS, bad).x : in[i + r * EMB_THREADS].x;
         if (bad && a.status) *a.status = 1;
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r)
+        for (int r = 0; r < LOADS; ++r)
             if (i + r * EMB_THREADS < i1) atomicAdd(&cnt[(key[r] >> shift) & (digits - 1)], 1u);
     }
     __syncthreads();
@@ -247,7 +255,7 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
 }
 
 template <typename I, bool FIRST, int BITS>
-__global__ void __launch_bounds__(EMB_THREADS) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, long long per_block, const unsigned *counts,
+__global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, long long per_block, const unsigned *counts,
                                                               const unsigned *totals, uint2 *out) {
     extern __shared__ unsigned sort_smem[];
     __shared__ unsigned warp_sum[SORT_WARPS];
@@ -393,7 +401,7 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
 }
 
 template <typename T, int V>
-__global__ void __launch_bounds__(EMB_THREADS) k_segment_sum(const SegArgs a) {
+__global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a) {
     using Vec = OpsVec<T, V>;
     if ((long long)blockIdx.x < a.zero_blocks) {
         clear_rows<T, V>(a, blockIdx.x);
@@ -429,38 +437,45 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_sum(const SegArgs a) {
         }
     };
     const unsigned ld_bytes = (unsigned)(a.ld * sizeof(T));
-    // the list is padded to whole batches, which start on 64 bytes; a batch's pairs are loaded under the rows of the one before
+    auto row_of = [&](unsigned r) { return *reinterpret_cast<const Vec *>(reinterpret_cast<const char *>(grad) + (unsigned long long)r * ld_bytes); };
+    bool more = true;
+    auto take = [&](unsigned key, const Vec &x) {
+        if (key != cur) {
+            if (key == none) {   // missing tokens are sorted last
+                more = false;
+                return;
+            }
+            finish();
+            cur = key;
+            from_before = false;
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+        }
+        add_row(acc, x);
+    };
+    // batches start on 64 bytes of the list; a batch's pairs are loaded under the rows of the one before (and, at the
+    // list's end, from its padding)
+    const long long whole = i0 + (i1 - i0) / EMB_UNROLL * EMB_UNROLL;
     OpsVec<uint2, 2> next[EMB_UNROLL / 2];
     auto load_pairs = [&](long long i) {
 #pragma unroll
         for (int u = 0; u < EMB_UNROLL / 2; ++u) next[u] = reinterpret_cast<const OpsVec<uint2, 2> *>(a.pair + i)[u];
     };
     load_pairs(i0);
-    for (long long i = i0; i < i1; i += EMB_UNROLL) {
-        uint2 p[EMB_UNROLL];
+    for (long long i = i0; i < whole && more; i += EMB_UNROLL) {
+        unsigned key[EMB_UNROLL];
         Vec x[EMB_UNROLL];
-        const int left = (int)(i1 - i);
 #pragma unroll
         for (int u = 0; u < EMB_UNROLL; ++u) {
-            p[u] = next[u / 2].v[u & 1];
-            if (u >= left) p[u].x = none;   // behind the tile's end; missing tokens are `none` as well, and sorted last
+            key[u] = next[u / 2].v[u & 1].x;
+            x[u] = row_of(next[u / 2].v[u & 1].y);   // a missing token's row is read and left out
         }
+        load_pairs(i + EMB_UNROLL);
 #pragma unroll
-        for (int u = 0; u < EMB_UNROLL; ++u) x[u] = row_or_zero<T, V>(grad, p[u].y, ld_bytes, p[u].x != none);
-        if (left > EMB_UNROLL) load_pairs(i + EMB_UNROLL);
-#pragma unroll
-        for (int u = 0; u < EMB_UNROLL; ++u) {
-            if (p[u].x != cur) {
-                if (p[u].x == none) break;
-                finish();
-                cur = p[u].x;
-                from_before = false;
-#pragma unroll
-                for (int j = 0; j < V; ++j) acc[j] = 0.0f;
-            }
-            add_row(acc, x[u]);
-        }
+        for (int u = 0; u < EMB_UNROLL; ++u)
+            if (more) take(key[u], x[u]);
     }
+    for (long long i = whole; i < i1 && more; ++i) take(a.pair[i].x, row_of(a.pair[i].y));
     if (i1 < a.n && a.pair[i1].x == cur) put_partial(from_before ? 0 : 1);
     else finish();
 }
@@ -679,12 +694,12 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     const bool small = n <= SORT_SMALL;
     const SortPlan sp = small ? SortPlan{} : sort_plan(c, n, a.n_entries);
     const size_t digits = small ? 0 : (size_t)1 << sp.bits;
-    const size_t bytes = 2 * qg_ws_size((size_t)n + EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * (sp.blocks + 1), sizeof(unsigned)) +
+    const size_t bytes = 2 * qg_ws_size((size_t)n + 2 * EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * (sp.blocks + 1), sizeof(unsigned)) +
                          qg_ws_size(digits, sizeof(unsigned)) + qg_ws_size((size_t)s.tiles * 2 * a.dim, sizeof(float));
     QgWorkspace ws;
     int rc = qg_ws_open(c, bytes, st, &ws);
     if (rc != QGBDT_OK) return rc;
-    uint2 *buf0 = ws.take<uint2>((size_t)n + EMB_UNROLL), *buf1 = ws.take<uint2>((size_t)n + EMB_UNROLL);
+    uint2 *buf0 = ws.take<uint2>((size_t)n + 2 * EMB_UNROLL), *buf1 = ws.take<uint2>((size_t)n + 2 * EMB_UNROLL);
     unsigned *counts = ws.take<unsigned>(digits * sp.blocks), *totals = ws.take<unsigned>(digits);
     s.partial = ws.take<float>((size_t)s.tiles * 2 * a.dim);
     s.pair = buf0;
