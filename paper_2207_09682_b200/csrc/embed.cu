@@ -57,14 +57,10 @@ __device__ __forceinline__ void add_row(float (&acc)[V], const OpsVec<T, V> &x) 
     }
 }
 
-// Row `t` of a matrix with rows of `ld_bytes` (below 2^32), or zeros: one 32 x 32 bit product per address.
+// Row `t` of a matrix with rows of `ld_bytes` (below 2^32): one 32 x 32 bit product per address.
 template <typename T, int V>
-__device__ __forceinline__ OpsVec<T, V> row_or_zero(const T *p, unsigned t, unsigned ld_bytes, bool on) {
-    OpsVec<T, V> x;
-#pragma unroll
-    for (int j = 0; j < V; ++j) x.v[j] = OpsType<T>::store(0.0f);
-    if (on) x = *reinterpret_cast<const OpsVec<T, V> *>(reinterpret_cast<const char *>(p) + (unsigned long long)t * ld_bytes);
-    return x;
+__device__ __forceinline__ OpsVec<T, V> row_of(const T *p, unsigned t, unsigned ld_bytes) {
+    return *reinterpret_cast<const OpsVec<T, V> *>(reinterpret_cast<const char *>(p) + (unsigned long long)t * ld_bytes);
 }
 
 // One group of lanes per (row, part of the bag, column block).  Eight rows of the table are in flight per group.
@@ -88,24 +84,33 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
         const int k0 = (int)((long long)a.bag * part >> p.split), k1 = (int)((long long)a.bag * (part + 1) >> p.split);
         bool bad = false;
         int k = k0;
+        unsigned next[EMB_UNROLL];   // tokens, 2^31 and more: missing; loaded under the rows of the batch before
+        auto load_tokens = [&](int at) {
+#pragma unroll
+            for (int u = 0; u < EMB_UNROLL; ++u) next[u] = token_at(tok, at + u);
+        };
+        if (k + EMB_UNROLL <= k1) load_tokens(k);
         for (; k + EMB_UNROLL <= k1; k += EMB_UNROLL) {
-            unsigned t[EMB_UNROLL];   // 2^31 and more: missing
+            bool on[EMB_UNROLL];
             Vec x[EMB_UNROLL];
 #pragma unroll
-            for (int u = 0; u < EMB_UNROLL; ++u) t[u] = token_at(tok, k + u);
-#pragma unroll
-            for (int u = 0; u < EMB_UNROLL; ++u) x[u] = row_or_zero<T, V>(table, t[u], ld_bytes, t[u] < n_entries);
-#pragma unroll
-            for (int u = 0; u < EMB_UNROLL; ++u) {
-                add_row(acc, x[u]);
-                bad |= t[u] >= n_entries && t[u] < 0x80000000u;
+            for (int u = 0; u < EMB_UNROLL; ++u) {   // without a predicate on the loads: for a missing token row 0 is read and left out
+                on[u] = next[u] < n_entries;
+                bad |= !on[u] && next[u] < 0x80000000u;
+                x[u] = row_of<T, V>(table, on[u] ? next[u] : 0u, ld_bytes);
             }
+            if (k + 2 * EMB_UNROLL <= k1) load_tokens(k + EMB_UNROLL);
+#pragma unroll
+            for (int u = 0; u < EMB_UNROLL; ++u)
+                if (on[u]) add_row(acc, x[u]);
         }
 #pragma unroll 4
         for (; k < k1; ++k) {
             const unsigned t = token_at(tok, k);
-            add_row(acc, row_or_zero<T, V>(table, t, ld_bytes, t < n_entries));
-            bad |= t >= n_entries && t < 0x80000000u;
+            const bool on = t < n_entries;
+            const Vec x = row_of<T, V>(table, on ? t : 0u, ld_bytes);
+            if (on) add_row(acc, x);
+            bad |= !on && t < 0x80000000u;
         }
         if (bad && lane == 0 && a.status) *a.status = 1;
     }
@@ -146,14 +151,17 @@ void set_divisor(SortArgs &a, unsigned d) {
 }
 __device__ __forceinline__ unsigned div_bag(const SortArgs &a, unsigned i) { return (unsigned)(((unsigned long long)i * a.div_mul) >> a.div_shift); }
 
-// Token and row of pair i; a missing or bad token becomes n_entries and sorts behind all others.  (Bad ones are
-// reported by the caller behind its loads: a store between them would keep the loads from overlapping.)
-template <typename I>
-__device__ __forceinline__ uint2 pair_at(const SortArgs &a, long long i, bool &bad) {
-    const unsigned row = div_bag(a, (unsigned)i), k = (unsigned)i - row * a.bag;
-    const unsigned t = token_at(reinterpret_cast<const I *>(a.tokens), (long long)row * a.ld_tokens + k), n = (unsigned)a.n_entries;
+// Where the token of pair i is, and what becomes of it: a missing or bad one is n_entries and sorts behind all
+// others.  The two steps are apart so that a thread's loads come before the first use of any of them.
+__device__ __forceinline__ long long token_index(const SortArgs &a, unsigned i) {
+    if (a.ld_tokens == a.bag) return i;
+    const unsigned row = div_bag(a, i);
+    return (long long)row * a.ld_tokens + (i - row * a.bag);
+}
+__device__ __forceinline__ unsigned token_key(const SortArgs &a, unsigned t, bool &bad) {
+    const unsigned n = (unsigned)a.n_entries;
     bad |= t >= n && t < 0x80000000u;
-    return make_uint2(t < n ? t : n, row);
+    return t < n ? t : n;
 }
 
 // Few pairs: every pair's place is the number of pairs before it, counted directly; one launch.
@@ -164,9 +172,16 @@ template <typename I>
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, uint2 *out) {
     __shared__ alignas(16) unsigned key[SORT_SMALL];
     const int n = (int)a.n, n4 = (n + 3) / 4;
+    const I *tokens = reinterpret_cast<const I *>(a.tokens);
     bool bad = false;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n4 * 4; i += EMB_THREADS) key[i] = i < n ? pair_at<I>(a, i, bad).x : 0xffffffffu;
+    for (int i = threadIdx.x; i < n4 * 4; i += EMB_THREADS * 4) {
+        unsigned t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) t[u] = token_at(tokens, token_index(a, min(i + u * EMB_THREADS, n - 1)));
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * EMB_THREADS < n4 * 4) key[i + u * EMB_THREADS] = i + u * EMB_THREADS < n ? token_key(a, t[u], bad) : 0xffffffffu;
+    }
     if (bad && a.status) *a.status = 1;
     __syncthreads();
     const int e = (blockIdx.x * EMB_THREADS + threadIdx.x) / SORT_SMALL_LANES, lane = threadIdx.x % SORT_SMALL_LANES;
@@ -203,14 +218,16 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, co
     constexpr int LOADS = 16;
     for (long long i = i0 + threadIdx.x; i < i1; i += EMB_THREADS * LOADS) {
         unsigned key[LOADS];
+#pragma unroll
+        for (int r = 0; r < LOADS; ++r) {
+            const long long at = min(i + r * EMB_THREADS, i1 - 1);
+            key[r] = FIRST ? token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, (unsigned)at)) : in[at].x;
+        }
         bool bad = false;
 #pragma unroll
         for (int r = 0; r < LOADS; ++r)
-            if (i + r * EMB_THREADS < i1) key[r] = FIRST ? pair_at<I>(a, i + r * EMB_THREADS, bad).x : in[i + r * EMB_THREADS].x;
-        if (bad && a.status) *a.status = 1;
-#pragma unroll
-        for (int r = 0; r < LOADS; ++r)
-            if (i + r * EMB_THREADS < i1) atomicAdd(&cnt[(key[r] >> shift) & (digits - 1)], 1u);
+            if (i + r * EMB_THREADS < i1) atomicAdd(&cnt[((FIRST ? token_key(a, key[r], bad) : key[r]) >> shift) & (digits - 1)], 1u);
+        if (FIRST && bad && a.status) *a.status = 1;
     }
     __syncthreads();
     for (int d = threadIdx.x; d < digits; d += EMB_THREADS) counts[(size_t)d * gridDim.x + blockIdx.x] = cnt[d];
@@ -282,8 +299,14 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
 #pragma unroll
         for (int r = 0; r < SORT_ROUNDS; ++r) {
             const long long i = w0 + r * 32 + lane;
-            bool bad;   // reported by the count
-            if (i < i1) pair[r] = FIRST ? pair_at<I>(a, i, bad) : in[i];
+            const long long at = i < i1 ? i : i1 - 1;
+            if (FIRST) pair[r] = make_uint2(token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, (unsigned)at)), div_bag(a, (unsigned)at));
+            else pair[r] = in[at];
+        }
+        if (FIRST) {
+            bool bad = false;   // reported by the count
+#pragma unroll
+            for (int r = 0; r < SORT_ROUNDS; ++r) pair[r].x = token_key(a, pair[r].x, bad);
         }
         for (int d = threadIdx.x; d < digits * SORT_WARPS / 2; d += EMB_THREADS) reinterpret_cast<unsigned *>(cnt)[d] = 0;
         __syncthreads();
@@ -437,7 +460,6 @@ __global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a)
         }
     };
     const unsigned ld_bytes = (unsigned)(a.ld * sizeof(T));
-    auto row_of = [&](unsigned r) { return *reinterpret_cast<const Vec *>(reinterpret_cast<const char *>(grad) + (unsigned long long)r * ld_bytes); };
     bool more = true;
     auto take = [&](unsigned key, const Vec &x) {
         if (key != cur) {
@@ -468,14 +490,14 @@ __global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a)
 #pragma unroll
         for (int u = 0; u < EMB_UNROLL; ++u) {
             key[u] = next[u / 2].v[u & 1].x;
-            x[u] = row_of(next[u / 2].v[u & 1].y);   // a missing token's row is read and left out
+            x[u] = row_of<T, V>(grad, next[u / 2].v[u & 1].y, ld_bytes);   // a missing token's row is read and left out
         }
         load_pairs(i + EMB_UNROLL);
 #pragma unroll
         for (int u = 0; u < EMB_UNROLL; ++u)
             if (more) take(key[u], x[u]);
     }
-    for (long long i = whole; i < i1 && more; ++i) take(a.pair[i].x, row_of(a.pair[i].y));
+    for (long long i = whole; i < i1 && more; ++i) take(a.pair[i].x, row_of<T, V>(grad, a.pair[i].y, ld_bytes));
     if (i1 < a.n && a.pair[i1].x == cur) put_partial(from_before ? 0 : 1);
     else finish();
 }
@@ -490,16 +512,18 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
     __shared__ float part_sum[EMB_THREADS][V];
     const int cols = 1 << lg_cols, groups = EMB_THREADS >> lg_cols, group = threadIdx.x >> lg_cols, lane = threadIdx.x & (cols - 1);
     const unsigned none = (unsigned)a.n_entries;
-    // does a token that goes on behind tile t begin in it, and how many more tiles has it?
-    auto begins = [&](long long t, unsigned &cur) {
+    // Tiles t + 1 .. t + links hold the rest of a token that begins in tile t; 0 where there is none.  The four words
+    // that settle nearly every tile are loaded at once.
+    auto links_of = [&](long long t, unsigned &cur) -> long long {
         const long long i0 = t * a.tile, i1 = i0 + a.tile;
-        if (i1 >= a.n) return false;
-        cur = a.pair[i1].x;
-        return cur != none && a.pair[i1 - 1].x == cur && !(i0 > 0 && a.pair[i0 - 1].x == cur);
-    };
-    auto links_of = [&](long long t, unsigned cur) {   // tiles t + 1 .. t + links hold the rest of it
-        long long lo = 1, hi = 2;                      // tile t + lo holds some of it; does t + hi begin with it?
-        auto inside = [&](long long l) { return (t + l) * a.tile < a.n && a.pair[(t + l) * a.tile].x == cur; };
+        if (i1 >= a.n) return 0;
+        auto key = [&](long long i) { return a.pair[i < a.n ? i : a.n - 1].x; };
+        const unsigned before = i0 > 0 ? key(i0 - 1) : none, last = key(i1 - 1), next = key(i1), second = key(i1 + a.tile);
+        cur = next;
+        if (cur == none || last != cur || before == cur) return 0;
+        auto inside = [&](long long l) { return (t + l) * a.tile < a.n && a.pair[(t + l) * a.tile].x == cur; };   // tile t + l begins with it
+        if (i1 + a.tile >= a.n || second != cur) return 1;
+        long long lo = 2, hi = 4;
         while (inside(hi)) lo = hi, hi *= 2;
         while (hi - lo > 1) {
             const long long mid = (lo + hi) >> 1;
@@ -522,8 +546,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
     // tokens of few tiles: a group each
     const long long t0 = (long long)blockIdx.x * groups, mine = t0 + group;
     unsigned cur = 0;
-    long long links = 0;
-    if (begins(mine, cur)) links = links_of(mine, cur);
+    long long links = links_of(mine, cur);
     if (links > 0 && links <= JOIN_SERIAL)
         for (int col = lane * V; col < a.dim; col += cols * V) {
             float s[V] = {};
@@ -535,7 +558,6 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
     if (!__syncthreads_or(links > JOIN_SERIAL)) return;
     for (int q = 0; q < groups; ++q) {   // the whole block for each of the others
         const long long t = t0 + q;
-        if (!begins(t, cur)) continue;
         links = links_of(t, cur);
         if (links <= JOIN_SERIAL) continue;
         const long long l0 = links * group / groups, l1 = links * (group + 1) / groups;
