@@ -5,6 +5,7 @@ library's kernels.  Loading fails loudly when the library has not been built.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import os
 from typing import NamedTuple
@@ -153,6 +154,7 @@ class Context:
         rc = self.lib.qgbdt_create(C.byref(self.h), C.byref(params))
         if rc != OK:
             raise QgbdtError(rc, "qgbdt_create failed")
+        self.device = torch.cuda.current_device()
         self.n_rows = self.n_features = self.n_bins = 0
 
     def close(self):
@@ -349,145 +351,178 @@ class SoftmaxCE(NamedTuple):
     lse: torch.Tensor
 
 
-def _need(ok: bool, what: str):
-    if not ok:
-        raise QgbdtError(ERR_ARG, what)
+# The calls below take a few microseconds on the GPU for small inputs, so their checks are kept short: sizes and strides
+# are fetched once per tensor, and devices compared by number.
+_raw_stream = torch._C._cuda_getCurrentRawStream   # the current stream's handle without a Stream object around it
 
 
-def _raw_stream(t: torch.Tensor, stream) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream if stream is None else stream.cuda_stream
+def _refuse(what: str):
+    raise QgbdtError(ERR_ARG, what)
 
 
-def _matrix(t, name: str) -> torch.Tensor:
-    """A CUDA matrix whose rows are contiguous (any row stride); a single column or row may have any stride there."""
-    _need(t.is_cuda and t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "%s must be a CUDA matrix with contiguous rows" % name)
-    return t
+def _rows(t, name: str, device: int) -> tuple:
+    """(rows, columns, row stride) of a matrix on the context's device whose rows are contiguous."""
+    if t.get_device() != device:
+        _refuse("%s must be a CUDA tensor on the context's device" % name)
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2:
+        _refuse("%s must be a matrix" % name)
+    n, d = shape
+    if stride[1] != 1 and d > 1:
+        _refuse("%s must have contiguous rows" % name)
+    return n, d, stride[0] if n > 1 else d or 1
 
 
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-
-
-def _tokens(tokens) -> tuple:
-    _need(tokens.is_cuda and tokens.dtype in _INDEX and tokens.dim() in (1, 2), "tokens must be a CUDA tensor [N] or [N, bag] of int32 or int64")
+def _token_rows(tokens, device: int) -> tuple:
+    """(rows, bag, row stride, index type) of tokens [N] or [N, bag]."""
+    kind = _INDEX.get(tokens.dtype, -1)
+    if kind < 0:
+        _refuse("tokens must be int32 or int64")
     if tokens.dim() == 1:
-        return tokens.shape[0], 1, (tokens.stride(0) if tokens.shape[0] > 1 else 1)
-    _need(tokens.shape[1] <= 1 or tokens.stride(1) == 1, "the tokens of a row must be contiguous")
-    return tokens.shape[0], tokens.shape[1], _ld(tokens)
+        if tokens.get_device() != device:
+            _refuse("tokens must be a CUDA tensor on the context's device")
+        n = tokens.shape[0]
+        return n, 1, tokens.stride()[0] if n > 1 else 1, kind
+    return (*_rows(tokens, "tokens", device), kind)
 
 
-def _status_ptr(status):
-    _need(status is None or (status.is_cuda and status.dtype == torch.int32 and status.numel() >= 1), "status must be a CUDA int32 tensor")
-    return None if status is None else status.data_ptr()
+def _words(t, dtype, count: int, name: str, device: int):
+    """Address of a contiguous vector of `count` elements (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous() or t.get_device() != device:
+        _refuse("%s must be a contiguous %s CUDA tensor of %d elements" % (name, str(dtype)[6:], count))
+    return t.data_ptr()
 
 
 def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, stream=None) -> torch.Tensor:
     """qgbdt_embed: out[i] = scale * sum_k table[tokens[i, k]].  table [V, D] (float32, bfloat16 or float16), tokens
     [N] or [N, bag] (int32 or int64, negative = missing); out [N, D] of the table's type is made if not given."""
-    _matrix(table, "table")
-    n, bag, ldt = _tokens(tokens)
-    _need(table.dtype in _ELEMENT, "table must be float32, bfloat16 or float16")
+    dev, dtype = self.device, table.dtype
+    kind = _ELEMENT.get(dtype, -1)
+    if kind < 0:
+        _refuse("table must be float32, bfloat16 or float16")
+    v, d, ld = _rows(table, "table", dev)
+    n, bag, ldt, index = _token_rows(tokens, dev)
     if out is None:
-        out = torch.empty((n, table.shape[1]), dtype=table.dtype, device=table.device)
-    _need(_matrix(out, "out").shape == (n, table.shape[1]) and out.dtype == table.dtype, "out must be [N, D] of the table's type")
-    _need(table.device == tokens.device == out.device, "tensors of different devices")
-    self._check(self.lib.qgbdt_embed(self.h, table.data_ptr(), _ELEMENT[table.dtype], table.shape[0], table.shape[1], _ld(table),
-                                     tokens.data_ptr(), _INDEX[tokens.dtype], n, bag, ldt, scale, out.data_ptr(), _ld(out),
-                                     _status_ptr(status), _raw_stream(table, stream)))
+        out, ldo = table.new_empty((n, d)), d
+    else:
+        no, do, ldo = _rows(out, "out", dev)
+        if no != n or do != d or out.dtype != dtype:
+            _refuse("out must be [N, D] of the table's type")
+    rc = self.lib.qgbdt_embed(self.h, table.data_ptr(), kind, v, d, ld, tokens.data_ptr(), index, n, bag, ldt, scale, out.data_ptr(), ldo,
+                              _words(status, torch.int32, 1, "status", dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc:
+        self._check(rc)
     return out
 
 
 def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None, stream=None) -> torch.Tensor:
     """qgbdt_embed_backward: the table's gradient [n_entries, D] of grad_out's type, every row of it written."""
-    _matrix(grad_out, "grad_out")
-    n, bag, ldt = _tokens(tokens)
-    _need(grad_out.dtype in _ELEMENT, "grad_out must be float32, bfloat16 or float16")
-    _need(grad_out.shape[0] == n, "grad_out and tokens differ in rows")
+    dev, dtype = self.device, grad_out.dtype
+    kind = _ELEMENT.get(dtype, -1)
+    if kind < 0:
+        _refuse("grad_out must be float32, bfloat16 or float16")
+    rows, d, ld = _rows(grad_out, "grad_out", dev)
+    n, bag, ldt, index = _token_rows(tokens, dev)
+    if rows != n:
+        _refuse("grad_out and tokens differ in rows")
     if grad_table is None:
-        grad_table = torch.empty((n_entries, grad_out.shape[1]), dtype=grad_out.dtype, device=grad_out.device)
-    _need(_matrix(grad_table, "grad_table").shape == (n_entries, grad_out.shape[1]) and grad_table.dtype == grad_out.dtype,
-          "grad_table must be [n_entries, D] of grad_out's type")
-    _need(grad_out.device == tokens.device == grad_table.device, "tensors of different devices")
-    self._check(self.lib.qgbdt_embed_backward(self.h, grad_out.data_ptr(), _ELEMENT[grad_out.dtype], _ld(grad_out), tokens.data_ptr(),
-                                              _INDEX[tokens.dtype], n, bag, ldt, scale, grad_table.data_ptr(), n_entries,
-                                              grad_out.shape[1], _ld(grad_table), _status_ptr(status), _raw_stream(grad_out, stream)))
+        grad_table, ldo = grad_out.new_empty((n_entries, d)), d
+    else:
+        no, do, ldo = _rows(grad_table, "grad_table", dev)
+        if no != n_entries or do != d or grad_table.dtype != dtype:
+            _refuse("grad_table must be [n_entries, D] of grad_out's type")
+    rc = self.lib.qgbdt_embed_backward(self.h, grad_out.data_ptr(), kind, ld, tokens.data_ptr(), index, n, bag, ldt, scale,
+                                       grad_table.data_ptr(), n_entries, d, ldo, _words(status, torch.int32, 1, "status", dev),
+                                       _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc:
+        self._check(rc)
     return grad_table
 
 
-def _check_softmax(hidden, weight, labels, bias):
-    _matrix(hidden, "hidden")
-    _matrix(weight, "weight")
-    _need(hidden.dtype == weight.dtype and hidden.dtype in (torch.bfloat16, torch.float16), "hidden and weight must both be bfloat16 or float16")
-    _need(hidden.shape[1] == weight.shape[1], "hidden and weight differ in columns")
-    _need(labels.is_cuda and labels.dtype in _INDEX and labels.shape == (hidden.shape[0],) and labels.is_contiguous(),
-          "labels must be a contiguous CUDA tensor [N] of int32 or int64")
-    _need(bias is None or (bias.is_cuda and bias.dtype == torch.float32 and bias.shape == (weight.shape[0],) and bias.is_contiguous()),
-          "bias must be a contiguous float32 CUDA tensor [V]")
-    _need(hidden.device == weight.device == labels.device and (bias is None or bias.device == hidden.device), "tensors of different devices")
+def _softmax_inputs(hidden, weight, labels, bias, dev: int) -> tuple:
+    """The arguments that both directions begin with, and the sizes."""
+    dtype = hidden.dtype
+    if dtype != weight.dtype or dtype not in (torch.bfloat16, torch.float16):
+        _refuse("hidden and weight must both be bfloat16 or float16")
+    n, d, ldh = _rows(hidden, "hidden", dev)
+    v, dw, ldw = _rows(weight, "weight", dev)
+    if d != dw:
+        _refuse("hidden and weight differ in columns")
+    index = _INDEX.get(labels.dtype, -1)
+    if index < 0 or labels.dim() != 1:
+        _refuse("labels must be [N], int32 or int64")
+    return (hidden.data_ptr(), ldh, weight.data_ptr(), ldw, _ELEMENT[dtype], _words(bias, torch.float32, v, "bias", dev),
+            _words(labels, labels.dtype, n, "labels", dev), index, n, v, d), n, v, d
 
 
 def _softmax_ce(self, hidden, weight, labels, bias=None, status=None, stream=None) -> SoftmaxCE:
     """qgbdt_softmax_ce: softmax cross entropy of hidden [N, D] @ weight [V, D]^T + bias [V] against labels [N] (negative:
     no label), mean over the labelled rows, without stored logits.  hidden, weight bfloat16 or float16, bias float32."""
-    _check_softmax(hidden, weight, labels, bias)
-    n = hidden.shape[0]
-    r = SoftmaxCE(*(torch.empty(k, dtype=torch.float32, device=hidden.device) for k in (1, n, n)))
-    self._check(self.lib.qgbdt_softmax_ce(self.h, hidden.data_ptr(), _ld(hidden), weight.data_ptr(), _ld(weight), _ELEMENT[hidden.dtype],
-                                          None if bias is None else bias.data_ptr(), labels.data_ptr(), _INDEX[labels.dtype], n,
-                                          weight.shape[0], hidden.shape[1], r.loss.data_ptr(), r.losses.data_ptr(), r.lse.data_ptr(),
-                                          _status_ptr(status), _raw_stream(hidden, stream)))
-    return r
+    dev = self.device
+    inputs, n, _, _ = _softmax_inputs(hidden, weight, labels, bias, dev)
+    losses, lse, loss = torch.empty(2 * n + 1, dtype=torch.float32, device=hidden.device).split((n, n, 1))
+    rc = self.lib.qgbdt_softmax_ce(self.h, *inputs, loss.data_ptr(), losses.data_ptr(), lse.data_ptr(),
+                                   _words(status, torch.int32, 1, "status", dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc:
+        self._check(rc)
+    return SoftmaxCE(loss, losses, lse)
 
 
 def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss=None, grad_hidden=None, grad_weight=None,
                          status=None, stream=None) -> tuple:
     """qgbdt_softmax_ce_backward: (grad_hidden [N, D], grad_weight [V, D], grad_bias [V] or None) of grad_loss * loss;
     lse as softmax_ce gave it, grad_loss a float32 CUDA tensor of one element (None: 1)."""
-    _check_softmax(hidden, weight, labels, bias)
-    n, v = hidden.shape[0], weight.shape[0]
-    _need(lse.is_cuda and lse.dtype == torch.float32 and lse.shape == (n,) and lse.is_contiguous(), "lse must be a contiguous float32 CUDA tensor [N]")
-    _need(grad_loss is None or (grad_loss.is_cuda and grad_loss.dtype == torch.float32 and grad_loss.numel() == 1),
-          "grad_loss must be a float32 CUDA tensor of one element")
-    if grad_hidden is None:
-        grad_hidden = torch.empty((n, hidden.shape[1]), dtype=hidden.dtype, device=hidden.device)
-    if grad_weight is None:
-        grad_weight = torch.empty((v, hidden.shape[1]), dtype=hidden.dtype, device=hidden.device)
-    _need(_matrix(grad_hidden, "grad_hidden").shape == hidden.shape and grad_hidden.dtype == hidden.dtype, "grad_hidden must be like hidden")
-    _need(_matrix(grad_weight, "grad_weight").shape == weight.shape and grad_weight.dtype == hidden.dtype, "grad_weight must be like weight")
+    dev, dtype = self.device, hidden.dtype
+    inputs, n, v, d = _softmax_inputs(hidden, weight, labels, bias, dev)
+
+    def made(t, rows, name):
+        if t is None:
+            return hidden.new_empty((rows, d)), d
+        no, do, ld = _rows(t, name, dev)
+        if no != rows or do != d or t.dtype != dtype:
+            _refuse("%s must be [%d, %d] of hidden's type" % (name, rows, d))
+        return t, ld
+
+    grad_hidden, ldh = made(grad_hidden, n, "grad_hidden")
+    grad_weight, ldw = made(grad_weight, v, "grad_weight")
     grad_bias = None if bias is None else torch.empty(v, dtype=torch.float32, device=hidden.device)
-    self._check(self.lib.qgbdt_softmax_ce_backward(
-        self.h, hidden.data_ptr(), _ld(hidden), weight.data_ptr(), _ld(weight), _ELEMENT[hidden.dtype],
-        None if bias is None else bias.data_ptr(), labels.data_ptr(), _INDEX[labels.dtype], n, v, hidden.shape[1], lse.data_ptr(),
-        None if grad_loss is None else grad_loss.data_ptr(), grad_hidden.data_ptr(), _ld(grad_hidden), grad_weight.data_ptr(),
-        _ld(grad_weight), None if grad_bias is None else grad_bias.data_ptr(), _status_ptr(status), _raw_stream(hidden, stream)))
+    rc = self.lib.qgbdt_softmax_ce_backward(
+        self.h, *inputs, _words(lse, torch.float32, n, "lse", dev), _words(grad_loss, torch.float32, 1, "grad_loss", dev),
+        grad_hidden.data_ptr(), ldh, grad_weight.data_ptr(), ldw, None if grad_bias is None else grad_bias.data_ptr(),
+        _words(status, torch.int32, 1, "status", dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc:
+        self._check(rc)
     return grad_hidden, grad_weight, grad_bias
-
-
-def _pointers(tensors, what: str) -> np.ndarray:
-    _need(all(t.is_cuda and t.is_contiguous() for t in tensors), "%s must be contiguous CUDA tensors" % what)
-    return np.array([t.data_ptr() for t in tensors], np.uint64)
 
 
 def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
     """qgbdt_clip_grad_norm: the global norm (float32 tensor [1]) of a list of tensors, and every tensor times
     min(1, max_norm / norm), in place or into the tensors of `out`.  float32, bfloat16 and float16 may be mixed."""
-    grads = list(grads)
-    n = len(grads)
-    types = [_ELEMENT.get(t.dtype, -1) for t in grads]
-    _need(-1 not in types, "gradients must be float32, bfloat16 or float16")
-    src = _pointers(grads, "gradients")
-    sizes = [t.numel() for t in grads]
-    dst = src
+    dev, n = self.device, len(grads)
+
+    def table(tensors, what):
+        for t in tensors:
+            if t.get_device() != dev or not t.is_contiguous():
+                _refuse("%s must be contiguous CUDA tensors on the context's device" % what)
+        return array.array("Q", [t.data_ptr() for t in tensors])
+
+    dtypes, sizes = [t.dtype for t in grads], [t.numel() for t in grads]
+    kinds = array.array("i", [_ELEMENT.get(t, -1) for t in dtypes])
+    if -1 in kinds:
+        _refuse("gradients must be float32, bfloat16 or float16")
+    src = dst = table(grads, "gradients")
     if out is not None:
-        out = list(out)
-        _need(len(out) == n and [t.numel() for t in out] == sizes and [t.dtype for t in out] == [t.dtype for t in grads],
-              "out must match the gradients in number, sizes and types")
-        dst = _pointers(out, "out")
-    device = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
-    norm = torch.empty(1, dtype=torch.float32, device=device)
-    counts, kinds = np.array(sizes, np.int64), np.array(types, np.int32)
-    self._check(self.lib.qgbdt_clip_grad_norm(self.h, src.ctypes.data, dst.ctypes.data, counts.ctypes.data, kinds.ctypes.data, n,
-                                              max_norm, norm.data_ptr(), _raw_stream(norm, stream)))
+        if [t.numel() for t in out] != sizes or [t.dtype for t in out] != dtypes:
+            _refuse("out must match the gradients in number, sizes and types")
+        dst = table(out, "out")
+    counts = array.array("q", sizes)
+    norm = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
+    rc = self.lib.qgbdt_clip_grad_norm(self.h, src.buffer_info()[0], dst.buffer_info()[0], counts.buffer_info()[0], kinds.buffer_info()[0], n,
+                                       max_norm, norm.data_ptr(), _raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc:
+        self._check(rc)
     return norm
 
 

@@ -36,6 +36,11 @@ int ops_enter(qgbdt_ctx *c) {
         *static_cast<volatile int *>(c->ops_fault) = 0;
         return qg_fail(c, QGBDT_ERR_CUDA, "a kernel of an earlier operator call gave up waiting for its copies; that call's results are not valid");
     }
+    int device = -1;
+    if (cudaGetDevice(&device) != cudaSuccess || device != c->device) {
+        cudaGetLastError();
+        return qg_fail(c, QGBDT_ERR_STATE, "the context belongs to device %d, the current one is %d", c->device, device);
+    }
     return QGBDT_OK;
 }
 

@@ -116,6 +116,7 @@ __device__ __forceinline__ double block_sum(double s) {
 
 template <int CAP>
 __global__ void __launch_bounds__(CLIP_THREADS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial) {
+    qg_after_prior();
     double s = 0.0;
     for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
         const int i = find_tensor(t, c);
@@ -165,6 +166,7 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &
 template <int CAP>
 __global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
                                                              const double *partial, int n_partial, double max_norm, bool in_place, float *d_norm) {
+    qg_after_prior();
     double s = 0.0;
     for (int i = threadIdx.x; i < n_partial; i += CLIP_THREADS) s += partial[i];
     s = block_sum(s);
@@ -226,8 +228,7 @@ int clip_groups(qgbdt_ctx *c, const void *const *in, void *const *out, const int
     do {
         if (fill(t, o, in, out, counts, types, at, n) != 0) return qg_fail(c, QGBDT_ERR_ARG, "a tensor is too large");
         const int grid = norm_grid(c, t.chunks);
-        k_norm_partial<CAP><<<grid, CLIP_THREADS, 0, st>>>(t, partial + n_partial);
-        QG_LAUNCH_CHECK(c);
+        QG_RUN(qg_launch(c, k_norm_partial<CAP>, dim3(grid), CLIP_THREADS, 0, st, t, partial + n_partial));
         n_partial += grid;
     } while (at < n);
     bool in_place = true;
@@ -236,8 +237,7 @@ int clip_groups(qgbdt_ctx *c, const void *const *in, void *const *out, const int
     do {
         if (t.n == n) at = n;   // a single group: still in t
         else fill(t, o, in, out, counts, types, at, n);
-        k_clip_scale<CAP><<<norm_grid(c, t.chunks), CLIP_THREADS, 0, st>>>(t, o, partial, n_partial, max_norm, in_place, d_norm);
-        QG_LAUNCH_CHECK(c);
+        QG_RUN(qg_launch(c, k_clip_scale<CAP>, dim3(norm_grid(c, t.chunks)), CLIP_THREADS, 0, st, t, o, partial, n_partial, max_norm, in_place, d_norm));
     } while (at < n);
     return QGBDT_OK;
 }

@@ -66,6 +66,7 @@ __device__ __forceinline__ OpsVec<T, V> row_of(const T *p, unsigned t, unsigned 
 // One group of lanes per (row, part of the bag, column block).  Eight rows of the table are in flight per group.
 template <typename T, int V, typename I>
 __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const EmbedPlan p) {
+    qg_after_prior();
     using Vec = OpsVec<T, V>;
     __shared__ float part_sum[EMB_THREADS][V];
     const int lane = threadIdx.x & ((1 << p.lg) - 1), group = threadIdx.x >> p.lg;
@@ -131,6 +132,35 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
     }
 }
 
+// The plain lookup, one token per row: a group of lanes per row, four vectors in flight per lane.
+template <typename T, int V, typename I>
+__global__ void __launch_bounds__(EMB_THREADS) k_lookup(const EmbedArgs a, int lg) {
+    qg_after_prior();
+    using Vec = OpsVec<T, V>;
+    const int lane = threadIdx.x & ((1 << lg) - 1), step = V << lg;
+    const long long row = (long long)blockIdx.x * (EMB_THREADS >> lg) + (threadIdx.x >> lg);
+    if (row >= a.rows) return;
+    const unsigned t = token_at(reinterpret_cast<const I *>(a.tokens), row * a.ld_tokens);
+    const bool on = t < (unsigned)a.n_entries;
+    if (!on && t < 0x80000000u && lane == 0 && a.status) *a.status = 1;
+    const T *in = reinterpret_cast<const T *>(a.table) + (on ? t : 0ll) * a.ld;
+    T *out = reinterpret_cast<T *>(a.out) + row * a.ld_out;
+    for (int col = lane * V; col < a.dim; col += step * 4) {
+        Vec x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (col + u * step < a.dim) x[u] = *reinterpret_cast<const Vec *>(in + col + u * step);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (col + u * step < a.dim) {
+                Vec y;
+#pragma unroll
+                for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(on ? OpsType<T>::load(x[u].v[j]) * a.scale : 0.0f);
+                *reinterpret_cast<Vec *>(out + col + u * step) = y;
+            }
+    }
+}
+
 // ---- sorting of the (token, row) pairs -----------------------------------------------------------
 
 struct SortArgs {
@@ -170,6 +200,7 @@ constexpr int SORT_SMALL_LANES = 8;   // lanes that share the count of one pair
 
 template <typename I>
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, uint2 *out) {
+    qg_after_prior();
     __shared__ alignas(16) unsigned key[SORT_SMALL];
     const int n = (int)a.n, n4 = (n + 3) / 4;
     const I *tokens = reinterpret_cast<const I *>(a.tokens);
@@ -209,6 +240,7 @@ constexpr int SORT_TILE = EMB_THREADS * SORT_ROUNDS;
 template <typename I, bool FIRST>
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const uint2 *in, int shift, int bits, long long per_block,
                                                             unsigned *counts) {
+    qg_after_prior();
     extern __shared__ unsigned sort_smem[];
     unsigned *cnt = sort_smem;   // [1 << bits]
     const int digits = 1 << bits;
@@ -235,6 +267,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, co
 
 // Per digit (one warp): exclusive scan over the blocks, and the digit's total.
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_scan(unsigned *counts, unsigned *totals, int digits, int blocks) {
+    qg_after_prior();
     const int d = blockIdx.x * SORT_WARPS + threadIdx.x / 32, lane = threadIdx.x & 31;
     if (d >= digits) return;
     unsigned *row = counts + (size_t)d * blocks, run = 0;
@@ -274,6 +307,7 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
 template <typename I, bool FIRST, int BITS>
 __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, long long per_block, const unsigned *counts,
                                                               const unsigned *totals, uint2 *out) {
+    qg_after_prior();
     extern __shared__ unsigned sort_smem[];
     __shared__ unsigned warp_sum[SORT_WARPS];
     constexpr int digits = 1 << BITS;
@@ -425,6 +459,7 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
 
 template <typename T, int V>
 __global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a) {
+    qg_after_prior();
     using Vec = OpsVec<T, V>;
     if ((long long)blockIdx.x < a.zero_blocks) {
         clear_rows<T, V>(a, blockIdx.x);
@@ -509,6 +544,7 @@ constexpr int JOIN_SERIAL = 32;   // tiles that one group adds by itself
 
 template <typename T, int V>
 __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, int lg_cols) {
+    qg_after_prior();
     __shared__ float part_sum[EMB_THREADS][V];
     const int cols = 1 << lg_cols, groups = EMB_THREADS >> lg_cols, group = threadIdx.x >> lg_cols, lane = threadIdx.x & (cols - 1);
     const unsigned none = (unsigned)a.n_entries;
@@ -602,6 +638,10 @@ int embed_typed(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     EmbedPlan p;
     p.lg = log2_at_least((a.dim + V - 1) / V, 5);
     p.col_blocks = (a.dim + (V << p.lg) - 1) / (V << p.lg);
+    if (a.bag == 1) {
+        const long long blocks = (a.rows + (EMB_THREADS >> p.lg) - 1) / (EMB_THREADS >> p.lg);
+        return qg_launch(c, a.token_type == QGBDT_I64 ? k_lookup<T, V, int64_t> : k_lookup<T, V, int32_t>, dim3((unsigned)blocks), EMB_THREADS, 0, st, a, p.lg);
+    }
     // few rows: a bag is cut into parts until every SM has 512 threads, parts hold at least two tokens
     const long long threads = a.rows * p.col_blocks << p.lg;
     p.split = 0;
@@ -609,10 +649,7 @@ int embed_typed(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     const long long rows_per_block = (EMB_THREADS >> p.lg) >> p.split;
     const long long blocks = (a.rows + rows_per_block - 1) / rows_per_block * p.col_blocks;
     if (blocks > 0x7fffffffll) return qg_fail(c, QGBDT_ERR_ARG, "rows * dim is too large for one call");
-    if (a.token_type == QGBDT_I64) k_embed<T, V, int64_t><<<(unsigned)blocks, EMB_THREADS, 0, st>>>(a, p);
-    else k_embed<T, V, int32_t><<<(unsigned)blocks, EMB_THREADS, 0, st>>>(a, p);
-    QG_LAUNCH_CHECK(c);
-    return QGBDT_OK;
+    return qg_launch(c, a.token_type == QGBDT_I64 ? k_embed<T, V, int64_t> : k_embed<T, V, int32_t>, dim3((unsigned)blocks), EMB_THREADS, 0, st, a, p);
 }
 
 // Radix passes for keys up to n_entries.
@@ -639,27 +676,22 @@ template <typename I>
 int sort_pairs(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, uint2 *buf0, uint2 *buf1, unsigned *counts, unsigned *totals,
                const uint2 **sorted, cudaStream_t st) {
     if (a.n <= SORT_SMALL) {
-        k_sort_small<I><<<(unsigned)((a.n * SORT_SMALL_LANES + EMB_THREADS - 1) / EMB_THREADS), EMB_THREADS, 0, st>>>(a, buf0);
-        QG_LAUNCH_CHECK(c);
         *sorted = buf0;
-        return QGBDT_OK;
+        return qg_launch(c, k_sort_small<I>, dim3((unsigned)((a.n * SORT_SMALL_LANES + EMB_THREADS - 1) / EMB_THREADS)), EMB_THREADS, 0, st, a, buf0);
     }
     const int digits = 1 << s.bits;
     const size_t count_smem = digits * sizeof(unsigned), smem = scatter_smem(s.bits);
     uint2 *in = buf1, *out = buf0;
     for (int k = 0; k < s.passes; ++k) {
         const int shift = k * s.bits;
-        if (k == 0) k_sort_count<I, true><<<s.blocks, EMB_THREADS, count_smem, st>>>(a, in, shift, s.bits, s.per_block, counts);
-        else k_sort_count<I, false><<<s.blocks, EMB_THREADS, count_smem, st>>>(a, in, shift, s.bits, s.per_block, counts);
-        QG_LAUNCH_CHECK(c);
-        k_sort_scan<<<(digits + SORT_WARPS - 1) / SORT_WARPS, EMB_THREADS, 0, st>>>(counts, totals, digits, s.blocks);
-        QG_LAUNCH_CHECK(c);
+        QG_RUN(qg_launch(c, k == 0 ? k_sort_count<I, true> : k_sort_count<I, false>, dim3(s.blocks), EMB_THREADS, count_smem, st, a, in, shift, s.bits,
+                         s.per_block, counts));
+        QG_RUN(qg_launch(c, k_sort_scan, dim3((digits + SORT_WARPS - 1) / SORT_WARPS), EMB_THREADS, 0, st, counts, totals, digits, s.blocks));
         const auto scatter = s.bits == 6 ? (k == 0 ? k_sort_scatter<I, true, 6> : k_sort_scatter<I, false, 6>)
                              : s.bits == 7 ? (k == 0 ? k_sort_scatter<I, true, 7> : k_sort_scatter<I, false, 7>)
                              : s.bits == 8 ? (k == 0 ? k_sort_scatter<I, true, 8> : k_sort_scatter<I, false, 8>)
                                            : (k == 0 ? k_sort_scatter<I, true, 9> : k_sort_scatter<I, false, 9>);
-        scatter<<<s.blocks, EMB_THREADS, smem, st>>>(a, in, shift, s.per_block, counts, totals, out);
-        QG_LAUNCH_CHECK(c);
+        QG_RUN(qg_launch(c, scatter, dim3(s.blocks), EMB_THREADS, smem, st, a, in, shift, s.per_block, counts, totals, out));
         uint2 *swap = in;
         in = out;
         out = swap;
@@ -673,14 +705,12 @@ int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     const long long per_block = EMB_THREADS >> s.lg;
     const long long blocks = s.zero_blocks + (s.tiles + per_block - 1) / per_block * s.col_blocks;
     if (blocks > 0x7fffffffll) return qg_fail(c, QGBDT_ERR_ARG, "rows * bag * dim is too large for one call");
-    k_segment_sum<T, V><<<(unsigned)blocks, EMB_THREADS, 0, st>>>(s);
-    QG_LAUNCH_CHECK(c);
+    QG_RUN(qg_launch(c, k_segment_sum<T, V>, dim3((unsigned)blocks), EMB_THREADS, 0, st, s));
     if (s.tiles > 1) {
         // four columns at most per thread: their partial sums are one 16-byte load
         constexpr int JV = V < 4 ? V : 4;
         const int lg = log2_at_least((s.dim + JV - 1) / JV, 7);
-        k_segment_join<T, JV><<<(unsigned)((s.tiles - 2) / (EMB_THREADS >> lg) + 1), EMB_THREADS, 0, st>>>(s, lg);
-        QG_LAUNCH_CHECK(c);
+        QG_RUN(qg_launch(c, k_segment_join<T, JV>, dim3((unsigned)((s.tiles - 2) / (EMB_THREADS >> lg) + 1)), EMB_THREADS, 0, st, s, lg));
     }
     return QGBDT_OK;
 }

@@ -42,6 +42,37 @@ static inline int qg_vec_bytes(const void *p, int64_t ld_bytes, int64_t len_byte
     return (int)(bits & (~bits + 1));
 }
 
+// ---- launches ------------------------------------------------------------------------------------
+
+// The operators' kernels are launched so that a kernel may start while the one before it on the stream ends:
+// every one of them begins with qg_after_prior(), before which it touches no memory of the device.
+__device__ __forceinline__ void qg_after_prior() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <typename... P, typename... A>
+int qg_launch(qgbdt_ctx *c, void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const A &...args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    QG_CUDA(c, cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
+    c->n_launches++;
+    return QGBDT_OK;
+}
+#define QG_RUN(expr)                        \
+    do {                                    \
+        const int rc_ = (expr);             \
+        if (rc_ != QGBDT_OK) return rc_;    \
+    } while (0)
+
 // ---- workspace -----------------------------------------------------------------------------------
 
 // A call's work memory: the context's one buffer, cut up from the front.  qg_ws_open makes the buffer

@@ -285,6 +285,7 @@ struct qgbdt_ctx {
     std::vector<void *> ops_ws_old;             // outgrown buffers that a captured graph may still use
     int *ops_fault = nullptr;                   // pinned word set by an operator's kernel that gave up waiting
     unsigned int *d_ops_counters = nullptr;     // zero between calls
+    unsigned int ops_configured = 0;            // kernels whose shared-memory limit has been raised
     char err[512] = {0};
 };
 

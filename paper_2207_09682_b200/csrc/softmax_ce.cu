@@ -371,6 +371,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
     tc_fence_after();
     const uint32_t tmem = *(volatile uint32_t *)&tmem_base;
 
+    qg_after_prior();   // what is above touches no memory of the device
     const int count = *a.count;
     Schedule<MODE> todo(a, count);
     Work c;
@@ -484,7 +485,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
 
 // ---- rows with a label, packed -----------------------------------------------------------------------
 
-constexpr int PACK_THREADS = 256, PACK_ROWS = 64, PACK_SPAN = 8192;   // labels per block, per entry of the counts
+constexpr int PACK_THREADS = 256, PACK_ROWS = 16;   // rows per block: two per warp
+constexpr int PACK_SPAN = 2048;                     // labels per entry of the counts
+constexpr int PACK_DIRECT = 8192;                   // up to here every block counts all labels itself
 
 struct PackArgs {
     const void *labels;
@@ -495,9 +498,9 @@ struct PackArgs {
     long long ld;
     int dim, vec;              // vec: rows can be read 16 bytes at a time
     const float *lse;          // or NULL
-    int *span_count;           // [spans], with more than one span
+    int *span_count;           // [spans], for more than PACK_DIRECT labels
     // results
-    int *count, *row_of, *pos_of, *label;
+    int *count, *pos_of, *label;
     float *lse_packed;
     uint16_t *packed;          // [n_pad][ldp]
     int ldp;
@@ -507,10 +510,8 @@ struct PackArgs {
     int *status;
 };
 
-__device__ __forceinline__ int label_of(const PackArgs &a, int i) {   // -1: none
-    const long long l = a.label_type == QGBDT_I64 ? reinterpret_cast<const long long *>(a.labels)[i] : (long long)reinterpret_cast<const int *>(a.labels)[i];
-    if (l >= a.classes && a.status) *a.status = 1;
-    return l >= 0 && l < a.classes ? (int)l : -1;
+__device__ __forceinline__ long long raw_label(const PackArgs &a, int i) {
+    return a.label_type == QGBDT_I64 ? reinterpret_cast<const long long *>(a.labels)[i] : (long long)reinterpret_cast<const int *>(a.labels)[i];
 }
 
 __device__ __forceinline__ int block_sum_int(int s) {
@@ -520,55 +521,70 @@ __device__ __forceinline__ int block_sum_int(int s) {
     if ((threadIdx.x & 31) == 0) w[threadIdx.x / 32] = s;
     __syncthreads();
     s = 0;
+#pragma unroll
     for (int i = 0; i < PACK_THREADS / 32; ++i) s += w[i];
     return s;
 }
 
+// Labelled rows among this thread's share of [i0, i1): in front of `mark`, and all.  Eight labels are loaded at a time.
+__device__ __forceinline__ void count_labels(const PackArgs &a, int i0, int i1, int mark, int &before, int &all) {
+    for (int i = i0 + threadIdx.x; i < i1; i += PACK_THREADS * 8) {
+        long long l[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) l[u] = raw_label(a, min(i + u * PACK_THREADS, i1 - 1));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int at = i + u * PACK_THREADS, has = at < i1 && l[u] >= 0 && l[u] < a.classes;
+            all += has;
+            before += at < mark ? has : 0;
+        }
+    }
+}
+
 __global__ void __launch_bounds__(PACK_THREADS) k_pack_count(const PackArgs a) {
-    const int i0 = blockIdx.x * PACK_SPAN, i1 = min(a.n, i0 + PACK_SPAN);
-    int s = 0;
-    for (int i = i0 + threadIdx.x; i < i1; i += PACK_THREADS) s += label_of(a, i) >= 0;
+    qg_after_prior();
+    int s = 0, none = 0;
+    count_labels(a, blockIdx.x * PACK_SPAN, min(a.n, (int)(blockIdx.x + 1) * PACK_SPAN), 0, none, s);
     s = block_sum_int(s);
     if (threadIdx.x == 0) a.span_count[blockIdx.x] = s;
 }
 
 __global__ void __launch_bounds__(PACK_THREADS) k_pack(const PackArgs a) {
+    qg_after_prior();
     __shared__ int place[PACK_ROWS];   // where the block's rows go, -1: no label
     if (a.bias)
         for (int i = blockIdx.x * PACK_THREADS + threadIdx.x; i < a.bias_pad; i += gridDim.x * PACK_THREADS) a.bias_copy[i] = i < a.classes ? a.bias[i] : 0.0f;
-    const int r0 = blockIdx.x * PACK_ROWS, spans = (a.n + PACK_SPAN - 1) / PACK_SPAN, span = r0 / PACK_SPAN;
+    const int r0 = blockIdx.x * PACK_ROWS;
     int before = 0, all = 0;
-    if (spans > 1)
+    if (a.n <= PACK_DIRECT) {
+        count_labels(a, 0, a.n, r0, before, all);
+    } else {
+        const int spans = (a.n + PACK_SPAN - 1) / PACK_SPAN, span = r0 / PACK_SPAN;
+        int rest = 0;
         for (int s = threadIdx.x; s < spans; s += PACK_THREADS) {
             const int x = a.span_count[s];
             all += x;
-            if (s < span) before += x;
+            before += s < span ? x : 0;
         }
-    {   // labels of this span in front of this block (and, with a single span, all of them)
-        const int i0 = span * PACK_SPAN, i1 = spans > 1 ? min(a.n, r0) : a.n;
-        for (int i = i0 + threadIdx.x; i < i1; i += PACK_THREADS) {
-            const int has = label_of(a, i) >= 0;
-            if (i < r0) before += has;
-            if (spans <= 1) all += has;
-        }
+        count_labels(a, span * PACK_SPAN, min(a.n, r0), r0, before, rest);
     }
     before = block_sum_int(before);
     all = block_sum_int(all);
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = all;
     if (threadIdx.x < 32) {
-        int run = before;
-        for (int h = 0; h < PACK_ROWS; h += 32) {
-            const int i = r0 + h + threadIdx.x, l = i < a.n ? label_of(a, i) : -1;
-            const unsigned has = __ballot_sync(0xffffffffu, l >= 0);
-            const int p = l >= 0 ? run + __popc(has & ((1u << threadIdx.x) - 1)) : -1;
-            place[h + threadIdx.x] = p;
+        const int i = r0 + threadIdx.x;
+        const long long l = threadIdx.x < PACK_ROWS && i < a.n ? raw_label(a, i) : -1;
+        const bool labelled = l >= 0 && l < a.classes;
+        if (l >= a.classes && a.status) *a.status = 1;
+        const unsigned has = __ballot_sync(0xffffffffu, labelled);
+        const int p = labelled ? before + __popc(has & ((1u << threadIdx.x) - 1)) : -1;
+        if (threadIdx.x < PACK_ROWS) {
+            place[threadIdx.x] = p;
             if (i < a.n) a.pos_of[i] = p;
-            if (p >= 0) {
-                a.row_of[p] = i;
-                a.label[p] = l;
-                if (a.lse) a.lse_packed[p] = a.lse[i];
-            }
-            run += __popc(has);
+        }
+        if (labelled) {
+            a.label[p] = (int)l;
+            if (a.lse) a.lse_packed[p] = a.lse[i];
         }
     }
     __syncthreads();
@@ -578,16 +594,17 @@ __global__ void __launch_bounds__(PACK_THREADS) k_pack(const PackArgs a) {
             const uint16_t *in = a.hidden + (r0 + h) * a.ld;
             uint4 *out = reinterpret_cast<uint4 *>(a.packed + (long long)place[h] * a.ldp);
             if (a.vec) {
-                for (int k = lane; k < chunks; k += 32) out[k] = reinterpret_cast<const uint4 *>(in)[k];
+                const uint4 *q = reinterpret_cast<const uint4 *>(in);
+#pragma unroll 4
+                for (int k = lane; k < chunks; k += 32) out[k] = q[k];
             } else {
                 for (int k = lane; k < chunks; k += 32) {
-                    uint32_t w[4];
+                    uint32_t w[8];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int d = 8 * k + 2 * j;
-                        w[j] = (d < a.dim ? in[d] : 0u) | (uint32_t)(d + 1 < a.dim ? in[d + 1] : 0u) << 16;
-                    }
-                    out[k] = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int j = 0; j < 8; ++j) w[j] = in[min(8 * k + j, a.dim - 1)];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) w[j] = 8 * k + j < a.dim ? w[j] : 0u;
+                    out[k] = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
                 }
             }
         }
@@ -600,15 +617,17 @@ __global__ void __launch_bounds__(PACK_THREADS) k_pack(const PackArgs a) {
 
 // Copy of a matrix whose rows do not start on 16-byte boundaries, with rows that do.
 __global__ void __launch_bounds__(256) k_realign(const uint16_t *in, long long ld, long long rows, int dim, uint16_t *out, int ldp) {
+    qg_after_prior();
     const int chunks = ldp / 8;
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * chunks; i += (long long)gridDim.x * 256) {
         const long long r = i / chunks;
         const int d = (int)(i - r * chunks) * 8;
-        uint32_t w[4];
+        uint32_t w[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = (d + 2 * j < dim ? in[r * ld + d + 2 * j] : 0u) | (uint32_t)(d + 2 * j + 1 < dim ? in[r * ld + d + 2 * j + 1] : 0u) << 16;
-        *reinterpret_cast<uint4 *>(out + r * ldp + d) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int j = 0; j < 8; ++j) w[j] = in[r * ld + min(d + j, dim - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = d + j < dim ? w[j] : 0u;
+        *reinterpret_cast<uint4 *>(out + r * ldp + d) = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
     }
 }
 
@@ -619,6 +638,7 @@ constexpr int JOIN_ROWS = 8;   // one warp per row
 __global__ void __launch_bounds__(JOIN_ROWS * 32) k_loss_join(const float2 *stat, int n_tiles, const float *z_label, const int *pos_of, int n,
                                                               const int *count, float *losses, float *lse, double *block_loss,
                                                               unsigned *arrived, float *loss) {
+    qg_after_prior();
     __shared__ double w[JOIN_ROWS];
     __shared__ bool last;
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, row = blockIdx.x * JOIN_ROWS + warp;
@@ -628,10 +648,21 @@ __global__ void __launch_bounds__(JOIN_ROWS * 32) k_loss_join(const float2 *stat
         float l_out = 0.0f;
         if (p >= 0) {
             float m = -INFINITY, l = 0.0f;
-            for (int t = lane; t < n_tiles; t += 32) {
-                const float2 s = stat[(long long)p * n_tiles + t];
-                const float top = fmaxf(m, s.x), base = top == -INFINITY ? 0.0f : top;
-                l = l * tc_ex2((m - base) * LOG2E) + s.y * tc_ex2((s.x - base) * LOG2E);
+            const float2 *q = stat + (long long)p * n_tiles;
+            for (int t = lane; t < n_tiles; t += 32 * 8) {
+                float2 s[8];
+                float top = m;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) s[u] = q[min(t + u * 32, n_tiles - 1)];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    if (t + u * 32 >= n_tiles) s[u] = make_float2(-INFINITY, 0.0f);
+                    top = fmaxf(top, s[u].x);
+                }
+                const float base = top == -INFINITY ? 0.0f : top;
+                l *= tc_ex2((m - base) * LOG2E);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) l += s[u].y * tc_ex2((s[u].x - base) * LOG2E);
                 m = top;
             }
 #pragma unroll
@@ -697,21 +728,25 @@ __device__ __forceinline__ void write4(T *o, int left, const float4 &s, float sc
     }
 }
 
-// dH: every row of the caller's, zeros where it has no label.
+// dH: every row of the caller's, zeros where it has no label.  A group of 2^lg threads per row, four columns each.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, int gangs, int rounds, int kb, const int *pos_of, long long rows,
-                                                   int dim, const float *grad_loss, const int *count, T *out, long long ld_out) {
-    const int n = *count, m_live = (n + BM - 1) / BM;
+__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, int gangs, int rounds, int kb, const int *pos_of, int rows, int dim,
+                                                   const float *grad_loss, const int *count, T *out, long long ld_out, int lg) {
+    qg_after_prior();
+    const int r = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), lane = threadIdx.x & ((1 << lg) - 1);
+    if (r >= rows) return;
+    const int n = *count, p = pos_of[r], m_live = (n + BM - 1) / BM;
     const float scale = out_scale(grad_loss, n);
     const Line line(rounds * m_live, kb, gangs);
-    const int quads = (dim + 3) / 4;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < rows * quads; i += (long long)gridDim.x * 256) {
-        const long long r = i / quads;
-        const int d = (int)(i - r * quads) * 4, p = pos_of[r];
+    int round = -1, place = 0, g0 = 0, g1 = -1;
+    for (int d = lane * 4; d < dim; d += 4 << lg) {
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (p >= 0) {
-            const int round = d / BN / gang, member = d / BN - round * gang, place = round * m_live + p / BM;
-            const int g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
+            const int now = d / BN / gang, member = d / BN - now * gang;
+            if (now != round) {
+                round = now, place = round * m_live + p / BM;
+                g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
+            }
             for (int g = g0; g <= g1; ++g) add4(s, part + (((long long)(place + g) * gang + member) * BM + p % BM) * BN + d % BN);
         }
         write4(out + r * ld_out + d, dim - d, s, scale);
@@ -723,6 +758,7 @@ __global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, 
 template <typename T>
 __global__ void __launch_bounds__(256) k_dw_finish(const float *part, int gang, int gangs, int rounds, int m_tiles, int n_tiles, int rows, int dim,
                                                    const float *grad_loss, const int *count, T *out, long long ld_out) {
+    qg_after_prior();
     const int n = *count, kb = (n + BK - 1) / BK;
     if (n == 0) {   // no labelled row: nothing has been written yet
         const int quads = (dim + 3) / 4;
@@ -754,6 +790,7 @@ __global__ void __launch_bounds__(256) k_dw_finish(const float *part, int gang, 
 
 // Bias gradient of a piece: sums over groups of 32 rows, in their order.
 __global__ void __launch_bounds__(256) k_bias_finish(const float *part, int cols, int n, const float *grad_loss, const int *count, float *out) {
+    qg_after_prior();
     __shared__ float w[8][32];
     const int v = blockIdx.x * 32 + (threadIdx.x & 31), k = threadIdx.x / 32;
     const int groups = (*count + BM - 1) / BM * (BM / 32);
@@ -805,19 +842,24 @@ int matrix_map(qgbdt_ctx *c, CUtensorMap *m, const void *p, long long cols, long
 template <int MODE>
 int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mo, const CUtensorMap &mp,
          cudaStream_t st) {
-    QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
+    if (!(c->ops_configured >> MODE & 1)) {
+        QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
+        c->ops_configured |= 1u << MODE;
+    }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)units * CG);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = SMEM_BYTES;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = CG, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     QG_CUDA(c, cudaLaunchKernelEx(&cfg, k_softmax_gemm<MODE>, a, ma, mb, mo, mp));
-    QG_LAUNCH_CHECK(c);
+    c->n_launches++;
     return QGBDT_OK;
 }
 
@@ -834,7 +876,7 @@ struct Common {
 // classes_pad: classes rounded up to what the tiles of the call cover.
 size_t common_bytes(const SoftmaxArgs &a, bool copy_weight, int64_t classes_pad) {
     const int n_pad = up(a.rows, 256), ldp = up(a.dim, 8);
-    return qg_ws_size((size_t)n_pad * ldp, 2) + 4 * qg_ws_size((size_t)n_pad, 4) + qg_ws_size(1, 4) + qg_ws_size((size_t)a.rows / PACK_SPAN + 1, 4) +
+    return qg_ws_size((size_t)n_pad * ldp, 2) + 3 * qg_ws_size((size_t)n_pad, 4) + qg_ws_size(1, 4) + qg_ws_size((size_t)a.rows / PACK_SPAN + 1, 4) +
            (copy_weight ? qg_ws_size((size_t)a.classes * ldp, 2) : 0) + (a.bias ? qg_ws_size((size_t)classes_pad, 4) : 0);
 }
 
@@ -850,7 +892,7 @@ int prepare(qgbdt_ctx *c, const SoftmaxArgs &a, QgWorkspace &ws, int64_t classes
     p.vec = rows_aligned(a.hidden, a.ld_hidden) && a.dim % 8 == 0;
     p.lse = a.lse_in, p.status = a.status, p.ldp = o->ldp;
     p.packed = ws.take<uint16_t>((size_t)o->n_pad * o->ldp);
-    p.row_of = ws.take<int>(o->n_pad), p.pos_of = ws.take<int>(o->n_pad), p.label = ws.take<int>(o->n_pad), p.lse_packed = ws.take<float>(o->n_pad);
+    p.pos_of = ws.take<int>(o->n_pad), p.label = ws.take<int>(o->n_pad), p.lse_packed = ws.take<float>(o->n_pad);
     p.count = ws.take<int>(1);
     p.span_count = ws.take<int>(a.rows / PACK_SPAN + 1);
     if (a.bias) p.bias = a.bias, p.bias_pad = (int)classes_pad, p.bias_copy = ws.take<float>((size_t)classes_pad);
@@ -859,19 +901,15 @@ int prepare(qgbdt_ctx *c, const SoftmaxArgs &a, QgWorkspace &ws, int64_t classes
         uint16_t *copy = ws.take<uint16_t>((size_t)a.classes * o->ldp);
         const long long chunks = a.classes * (o->ldp / 8);
         const long long blocks = (chunks + 255) / 256;
-        k_realign<<<(unsigned)(blocks < c->sm_count * 16 ? blocks : c->sm_count * 16), 256, 0, st>>>(
-            reinterpret_cast<const uint16_t *>(a.weight), a.ld_weight, a.classes, a.dim, copy, o->ldp);
-        QG_LAUNCH_CHECK(c);
+        QG_RUN(qg_launch(c, k_realign, dim3((unsigned)(blocks < c->sm_count * 16 ? blocks : c->sm_count * 16)), 256, 0, st, 
+            reinterpret_cast<const uint16_t *>(a.weight), a.ld_weight, a.classes, a.dim, copy, o->ldp));
         o->weight = copy, o->ld_weight = o->ldp;
     }
     const int spans = (int)((a.rows + PACK_SPAN - 1) / PACK_SPAN);
-    if (spans > 1) {
-        k_pack_count<<<spans, PACK_THREADS, 0, st>>>(p);
-        QG_LAUNCH_CHECK(c);
+    if (a.rows > PACK_DIRECT) {
+        QG_RUN(qg_launch(c, k_pack_count, dim3(spans), PACK_THREADS, 0, st, p));
     }
-    k_pack<<<o->n_pad > 0 ? o->n_pad / PACK_ROWS : 1, PACK_THREADS, 0, st>>>(p);
-    QG_LAUNCH_CHECK(c);
-    return QGBDT_OK;
+    return qg_launch(c, k_pack, dim3(o->n_pad > 0 ? o->n_pad / PACK_ROWS : 1), PACK_THREADS, 0, st, p);
 }
 
 GemmArgs gemm_args(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o) {
@@ -913,19 +951,16 @@ Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int n_tiles, long long kb
 
 template <typename T>
 int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, const Gangs &g, int kb, cudaStream_t st) {
-    const long long blocks = (a.rows * ((a.dim + 3) / 4) + 255) / 256;
-    k_dh_finish<T><<<(unsigned)(blocks < c->sm_count * 16 ? blocks : c->sm_count * 16), 256, 0, st>>>(
-        part, g.size, g.gangs, g.rounds, kb, o.pack.pos_of, a.rows, a.dim, a.grad_loss, o.pack.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden);
-    QG_LAUNCH_CHECK(c);
-    return QGBDT_OK;
+    int lg = 0;
+    while (lg < 8 && (4 << lg) < a.dim) ++lg;
+    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, part, g.size, g.gangs, g.rounds, kb,
+                     o.pack.pos_of, (int)a.rows, a.dim, a.grad_loss, o.pack.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden, lg);
 }
 
 template <typename T>
 int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, const GemmArgs &g, int rows, cudaStream_t st) {
-    k_dw_finish<T><<<dim3(g.gangs * g.gang, BM / 8), 256, 0, st>>>(part, g.gang, g.gangs, g.rounds, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, o.pack.count,
+    return qg_launch(c, k_dw_finish<T>, dim3(g.gangs * g.gang, BM / 8), 256, 0, st, part, g.gang, g.gangs, g.rounds, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, o.pack.count,
                                                        reinterpret_cast<T *>(a.d_weight) + g.v0 * a.ld_d_weight, a.ld_d_weight);
-    QG_LAUNCH_CHECK(c);
-    return QGBDT_OK;
 }
 
 }  // namespace
@@ -953,9 +988,8 @@ int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
         if ((rc = matrix_map(c, &mb, o.weight, a.dim, a.classes, o.ld_weight, B_ROWS, a.type)) != QGBDT_OK) return rc;
         if ((rc = gemm<LOSS>(c, g, units, ma, mb, ma, ma, st)) != QGBDT_OK) return rc;
     }
-    k_loss_join<<<join_blocks, JOIN_ROWS * 32, 0, st>>>(g.stat, n_tiles * 2, g.z_label, o.pack.pos_of, (int)a.rows, o.pack.count, a.losses, a.lse,
-                                                        block_loss, c->d_ops_counters, a.loss);
-    QG_LAUNCH_CHECK(c);
+    QG_RUN(qg_launch(c, k_loss_join, dim3(join_blocks), JOIN_ROWS * 32, 0, st, g.stat, n_tiles * 2, g.z_label, o.pack.pos_of, (int)a.rows, o.pack.count, a.losses, a.lse,
+                                                        block_loss, c->d_ops_counters, a.loss));
     return qg_ws_close(c, st);
 }
 
@@ -1009,8 +1043,7 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
         g.v0 = v0, g.n_tiles = (int)(width / BN), g.bias_part = bias_part;
         if ((rc = gemm<GRAD>(c, g, grad_units, h_k, w_k, g_store, g_store, st)) != QGBDT_OK) return rc;
         if (bias_part) {
-            k_bias_finish<<<(nv + 31) / 32, 256, 0, st>>>(bias_part, (int)width, nv, a.grad_loss, base.count, a.d_bias + v0);
-            QG_LAUNCH_CHECK(c);
+            QG_RUN(qg_launch(c, k_bias_finish, dim3((nv + 31) / 32), 256, 0, st, bias_part, (int)width, nv, a.grad_loss, base.count, a.d_bias + v0));
         }
         g = base;
         g.v0 = v0, g.n_tiles = d_tiles, g.kb = kb_dh, g.add = k > 0;
