@@ -3,14 +3,16 @@
 //   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)
 //
 // Two launches: the first takes the sum of squares (one double per block), the second adds the blocks'
-// sums in a fixed order (every block for itself: 1184 doubles out of L2), and multiplies.  Bound by
+// sums in a fixed order (every block for itself: 592 doubles out of L2), and multiplies.  Bound by
 // memory traffic: every tensor is read once, and read and written once more when the norm is above
-// max_norm.  The second launch walks the chunks backwards, so that what the first one read last is
+// max_norm.  The second launch walks every run backwards, so that what the first one read last is
 // still in L2.
 //
-// A tensor is cut into chunks of 4096 elements counted from its first 16-byte boundary (the elements
-// before it ride with the first chunk); blocks take chunks in turn and find a chunk's tensor by a binary
-// search over the tensors' first chunk numbers, which lie with the pointers in the kernel's parameters.
+// A tensor is cut into chunks of 8192 elements counted from its first 16-byte boundary (the elements
+// before it ride with the first chunk).  A block takes a run of neighbouring chunks: it finds the first
+// one's tensor by a binary search over the tensors' first chunk numbers, which lie with the pointers in
+// the kernel's parameters, and walks on from there (searching anew for every chunk took as long as
+// loading it).
 // Squares are added in double precision: single precision would overflow from |g| = 1.8e19 on and lose
 // everything below 1e-23, and the double-precision units have the throughput to spare here.
 #include "ops_internal.cuh"
@@ -18,7 +20,8 @@
 namespace {
 
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_CHUNK = 4096;
+constexpr int CLIP_CHUNK = 8192;
+constexpr int CLIP_BLOCKS = 4;   // per SM, all resident
 constexpr int CLIP_SMALL = 64, CLIP_LARGE = 1000;   // tensors per launch (parameters of 1.6 or 25 KB)
 
 template <int CAP>
@@ -115,11 +118,13 @@ __device__ __forceinline__ double block_sum(double s) {
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(CLIP_THREADS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial) {
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial) {
     qg_after_prior();
     double s = 0.0;
-    for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-        const int i = find_tensor(t, c);
+    const int c0 = (int)((long long)t.chunks * blockIdx.x / gridDim.x), c1 = (int)((long long)t.chunks * (blockIdx.x + 1) / gridDim.x);
+    int i = c0 < c1 ? find_tensor(t, c0) : 0;
+    for (int c = c0; c < c1; ++c) {
+        while (i + 1 < t.n && t.first[i + 1] <= c) ++i;
         const long long count = t.count[i] & ((1ll << 56) - 1);
         const int type = (int)(t.count[i] >> 56), k = c - t.first[i];
         const void *p = t.in[i];
@@ -164,7 +169,7 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
                                                              const double *partial, int n_partial, double max_norm, bool in_place, float *d_norm) {
     qg_after_prior();
     double s = 0.0;
@@ -176,8 +181,10 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_consta
     const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
     if (!clip && in_place) return;
     const float coef = clip ? (float)(max_norm / norm) : 1.0f;
-    for (int c = t.chunks - 1 - (int)blockIdx.x; c >= 0; c -= gridDim.x) {
-        const int i = find_tensor(t, c);
+    const int c0 = (int)((long long)t.chunks * blockIdx.x / gridDim.x), c1 = (int)((long long)t.chunks * (blockIdx.x + 1) / gridDim.x);
+    int i = c0 < c1 ? find_tensor(t, c1 - 1) : 0;
+    for (int c = c1 - 1; c >= c0; --c) {
+        while (t.first[i] > c) --i;
         const long long count = t.count[i] & ((1ll << 56) - 1);
         const int type = (int)(t.count[i] >> 56), k = c - t.first[i];
         const void *p = t.in[i];
@@ -214,7 +221,7 @@ int fill(ClipTable<CAP> &t, ClipOut<CAP> &o, const void *const *in, void *const 
 }
 
 int norm_grid(const qgbdt_ctx *c, int chunks) {
-    const int full = c->sm_count * 8;
+    const int full = c->sm_count * CLIP_BLOCKS;
     return chunks < full ? (chunks > 0 ? chunks : 1) : full;
 }
 
@@ -248,9 +255,9 @@ int qg_clip_grad_norm(qgbdt_ctx *c, const void *const *in, void *const *out, con
                       double max_norm, float *d_norm, cudaStream_t st) {
     QgWorkspace ws;
     const size_t groups = (size_t)n / CLIP_SMALL + 2;
-    int rc = qg_ws_open(c, qg_ws_size(groups * c->sm_count * 8, sizeof(double)), st, &ws);
+    int rc = qg_ws_open(c, qg_ws_size(groups * c->sm_count * CLIP_BLOCKS, sizeof(double)), st, &ws);
     if (rc != QGBDT_OK) return rc;
-    double *partial = ws.take<double>(groups * c->sm_count * 8);
+    double *partial = ws.take<double>(groups * c->sm_count * CLIP_BLOCKS);
     rc = n <= CLIP_SMALL ? clip_groups<CLIP_SMALL>(c, in, out, counts, types, n, max_norm, d_norm, partial, st)
                          : clip_groups<CLIP_LARGE>(c, in, out, counts, types, n, max_norm, d_norm, partial, st);
     if (rc != QGBDT_OK) return rc;
