@@ -2,17 +2,17 @@
 //
 //   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)
 //
-// Two launches: the first takes the sum of squares (one double per block), the second adds the blocks'
-// sums in a fixed order (every block for itself: 592 doubles out of L2), and multiplies.  Bound by
-// memory traffic: every tensor is read once, and read and written once more when the norm is above
-// max_norm.  The second launch walks every run backwards, so that what the first one read last is
-// still in L2.
+// Two launches: the first takes the sum of squares (one double per block; the block that ends last adds
+// the blocks' sums in their order and works out the factor), the second multiplies.  Bound by memory
+// traffic: every tensor is read once, and read and written once more when the norm is above max_norm.
 //
-// A tensor is cut into chunks of 8192 elements counted from its first 16-byte boundary (the elements
-// before it ride with the first chunk).  A block takes a run of neighbouring chunks: it finds the first
-// one's tensor by a binary search over the tensors' first chunk numbers, which lie with the pointers in
-// the kernel's parameters, and walks on from there (searching anew for every chunk took as long as
-// loading it).
+// A tensor is cut into chunks of 4096 elements counted from its first 16-byte boundary (the elements
+// before it ride with the first chunk).  A block finds its first chunk's tensor by a binary search over
+// the tensors' first chunk numbers, which lie with the pointers in the kernel's parameters, and walks on
+// from there.  The first launch has blocks that stay, each with a run of neighbouring chunks (few sums to
+// add); the second has one block per CLIP_STEP chunks, so that the memory sees one moving front of reads
+// and writes instead of hundreds.
+//
 // Squares are added in double precision: single precision would overflow from |g| = 1.8e19 on and lose
 // everything below 1e-23, and the double-precision units have the throughput to spare here.
 #include "ops_internal.cuh"
@@ -20,8 +20,9 @@
 namespace {
 
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_CHUNK = 8192;
-constexpr int CLIP_BLOCKS = 4;   // per SM, all resident
+constexpr int CLIP_CHUNK = 4096;
+constexpr int CLIP_BLOCKS = 6;   // of the first launch, per SM
+constexpr int CLIP_STEP = 2;     // chunks per block of the second launch
 constexpr int CLIP_SMALL = 64, CLIP_LARGE = 1000;   // tensors per launch (parameters of 1.6 or 25 KB)
 
 template <int CAP>
@@ -114,12 +115,23 @@ __device__ __forceinline__ double block_sum(double s) {
     s = 0.0;
 #pragma unroll
     for (int i = 0; i < CLIP_THREADS / 32; ++i) s += w[i];
+    __syncthreads();
     return s;
 }
 
+// What the second launch reads.
+struct ClipFactor {
+    float coef;
+    int scale;      // 0: the tensors keep their values
+};
+
+// n_before: sums of earlier launches of the same call; the last launch (`final`) adds them all.
 template <int CAP>
-__global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial) {
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial, int n_before,
+                                                                            bool final, double max_norm, unsigned *arrived, ClipFactor *factor,
+                                                                            float *d_norm) {
     qg_after_prior();
+    __shared__ bool last;
     double s = 0.0;
     const int c0 = (int)((long long)t.chunks * blockIdx.x / gridDim.x), c1 = (int)((long long)t.chunks * (blockIdx.x + 1) / gridDim.x);
     int i = c0 < c1 ? find_tensor(t, c0) : 0;
@@ -134,7 +146,26 @@ __global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(cons
         else s += sum_squares(reinterpret_cast<const __half *>(p), r);
     }
     s = block_sum(s);
-    if (threadIdx.x == 0) partial[blockIdx.x] = s;
+    if (threadIdx.x == 0) {
+        partial[n_before + blockIdx.x] = s;
+        __threadfence();
+        last = final && atomicAdd(arrived, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    s = 0.0;
+    for (int k = threadIdx.x; k < n_before + (int)gridDim.x; k += CLIP_THREADS) s += *(volatile double *)&partial[k];
+    s = block_sum(s);
+    if (threadIdx.x == 0) {
+        const double norm = sqrt(s);
+        // false also for a norm that is not finite: the tensors keep their values then
+        const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
+        factor->coef = clip ? (float)(max_norm / norm) : 1.0f;
+        factor->scale = clip;
+        *d_norm = (float)norm;
+        *arrived = 0;
+    }
 }
 
 template <typename T>
@@ -169,22 +200,15 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
-                                                             const double *partial, int n_partial, double max_norm, bool in_place, float *d_norm) {
+__global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
+                                                             const ClipFactor *factor, bool in_place) {
     qg_after_prior();
-    double s = 0.0;
-    for (int i = threadIdx.x; i < n_partial; i += CLIP_THREADS) s += partial[i];
-    s = block_sum(s);
-    const double norm = sqrt(s);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *d_norm = (float)norm;
-    // false also for a norm that is not finite: the tensors keep their values then
-    const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
-    if (!clip && in_place) return;
-    const float coef = clip ? (float)(max_norm / norm) : 1.0f;
-    const int c0 = (int)((long long)t.chunks * blockIdx.x / gridDim.x), c1 = (int)((long long)t.chunks * (blockIdx.x + 1) / gridDim.x);
-    int i = c0 < c1 ? find_tensor(t, c1 - 1) : 0;
-    for (int c = c1 - 1; c >= c0; --c) {
-        while (t.first[i] > c) --i;
+    const float coef = factor->coef;
+    if (!factor->scale && in_place) return;
+    const int c0 = blockIdx.x * CLIP_STEP, c1 = min(t.chunks, c0 + CLIP_STEP);
+    int i = find_tensor(t, c0);
+    for (int c = c0; c < c1; ++c) {
+        while (i + 1 < t.n && t.first[i + 1] <= c) ++i;
         const long long count = t.count[i] & ((1ll << 56) - 1);
         const int type = (int)(t.count[i] >> 56), k = c - t.first[i];
         const void *p = t.in[i];
@@ -230,21 +254,26 @@ int clip_groups(qgbdt_ctx *c, const void *const *in, void *const *out, const int
                 float *d_norm, double *partial, cudaStream_t st) {
     ClipTable<CAP> t;
     ClipOut<CAP> o;
+    ClipFactor *factor = reinterpret_cast<ClipFactor *>(partial);   // in front of the sums
+    partial += 16;
     int n_partial = 0;
     int32_t at = 0;
     do {
         if (fill(t, o, in, out, counts, types, at, n) != 0) return qg_fail(c, QGBDT_ERR_ARG, "a tensor is too large");
         const int grid = norm_grid(c, t.chunks);
-        QG_RUN(qg_launch(c, k_norm_partial<CAP>, dim3(grid), CLIP_THREADS, 0, st, t, partial + n_partial));
+        QG_RUN(qg_launch(c, k_norm_partial<CAP>, dim3(grid), CLIP_THREADS, 0, st, t, partial, n_partial, at >= n, max_norm, c->d_ops_counters + 1, factor,
+                         d_norm));
         n_partial += grid;
     } while (at < n);
     bool in_place = true;
     for (int32_t i = 0; i < n; ++i) in_place = in_place && (in[i] == out[i] || counts[i] == 0);
+    if (in_place && max_norm > 1.7976931348623157e308) return QGBDT_OK;   // the norm alone
     at = 0;
     do {
         if (t.n == n) at = n;   // a single group: still in t
         else fill(t, o, in, out, counts, types, at, n);
-        QG_RUN(qg_launch(c, k_clip_scale<CAP>, dim3(norm_grid(c, t.chunks)), CLIP_THREADS, 0, st, t, o, partial, n_partial, max_norm, in_place, d_norm));
+        if (t.chunks > 0)
+            QG_RUN(qg_launch(c, k_clip_scale<CAP>, dim3((t.chunks + CLIP_STEP - 1) / CLIP_STEP), CLIP_THREADS, 0, st, t, o, factor, in_place));
     } while (at < n);
     return QGBDT_OK;
 }
@@ -255,9 +284,9 @@ int qg_clip_grad_norm(qgbdt_ctx *c, const void *const *in, void *const *out, con
                       double max_norm, float *d_norm, cudaStream_t st) {
     QgWorkspace ws;
     const size_t groups = (size_t)n / CLIP_SMALL + 2;
-    int rc = qg_ws_open(c, qg_ws_size(groups * c->sm_count * CLIP_BLOCKS, sizeof(double)), st, &ws);
+    int rc = qg_ws_open(c, qg_ws_size(groups * c->sm_count * CLIP_BLOCKS + 16, sizeof(double)), st, &ws);
     if (rc != QGBDT_OK) return rc;
-    double *partial = ws.take<double>(groups * c->sm_count * CLIP_BLOCKS);
+    double *partial = ws.take<double>(groups * c->sm_count * CLIP_BLOCKS + 16);
     rc = n <= CLIP_SMALL ? clip_groups<CLIP_SMALL>(c, in, out, counts, types, n, max_norm, d_norm, partial, st)
                          : clip_groups<CLIP_LARGE>(c, in, out, counts, types, n, max_norm, d_norm, partial, st);
     if (rc != QGBDT_OK) return rc;
