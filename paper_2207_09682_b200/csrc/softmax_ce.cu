@@ -62,8 +62,10 @@ struct GemmArgs {
     float *bias_part;           // [m_tiles * BM / 32][n_tiles * 256] column sums of g over 32 rows
     // DH and DW
     int gang, gangs, rounds;    // units of a gang, gangs, column tiles / gang rounded up
+    bool split;                 // tiles may be cut (the same for every launch of a call)
     int add;                    // DH: add to the fragments of the pieces before
     uint16_t *out;              // DW
+    int rows;                   // its rows in this piece
     long long ld_out;
     int out_map;                // its rows are 16-byte aligned: tiled copies write them
     const float *grad_loss;
@@ -86,16 +88,21 @@ __device__ __forceinline__ void tile_place(int t, int m_live, int n_tiles, int &
 // column tiles of the same rows and walk along the products together, so that a block of g comes out of DRAM once
 // for all of them.  All blocks of all row tiles (once per round of column tiles), one after the other, are a line
 // that is cut into equal runs, one per gang; a tile that a cut falls into is summed from its fragments afterwards,
-// in the order of the gangs.
+// in the order of the gangs.  Short products (below SPLIT_KB blocks) are not cut: joining fragments costs about as
+// long as 30 blocks take, so that their runs are whole tiles.
+constexpr int SPLIT_KB = 32;
 struct Line {
     long long length;   // rounds * row tiles * kb
-    int kb, runs;       // gangs that get a run (each at least four blocks long)
-    __device__ Line(int lines, int kb_, int gangs) : length((long long)lines * kb_), kb(kb_) {
-        const long long most = length / 4;
+    int kb, runs;       // gangs that get a run (of four blocks or more)
+    bool split;
+    __device__ Line(int lines, int kb_, int gangs, bool split_) : length((long long)lines * kb_), kb(kb_), split(split_) {
+        const long long most = split ? length / 4 : lines;
         runs = most < 1 ? 1 : most < gangs ? (int)most : gangs;
     }
-    __device__ __forceinline__ long long start(int g) const { return length * g / runs; }
-    __device__ __forceinline__ int gang_of(long long pos) const { return (int)(((pos + 1) * runs - 1) / length); }
+    __device__ __forceinline__ long long start(int g) const { return split ? length * g / runs : length / kb * g / runs * kb; }
+    __device__ __forceinline__ int gang_of(long long pos) const {   // the gang whose run holds block pos
+        return split ? (int)(((pos + 1) * runs - 1) / length) : (int)(((pos / kb + 1) * runs - 1) / (length / kb));
+    }
 };
 
 // What a unit works on next.
@@ -118,7 +125,7 @@ struct Schedule {
         pos = end = 0;
         if (MODE == DH || MODE == DW) {
             size = a.gang, gang = unit / size, member = unit - gang * size;
-            const Line line(a.rounds * m_live, kb, a.gangs);
+            const Line line(a.rounds * m_live, kb, a.gangs, a.split);
             if (line.length > 0 && gang < line.runs) pos = line.start(gang), end = line.start(gang + 1);
         }
     }
@@ -222,6 +229,23 @@ struct Epilogue {
                     pack2(x[8 * i + 4], x[8 * i + 5], a.bf16), pack2(x[8 * i + 6], x[8 * i + 7], a.bf16));
     }
 
+    // x = exp(x - base), in one multiplication and addition: base * log2(e) is rounded to 24 bits, as the logits of that
+    // size are themselves.  Near the end of the range (classes masked by the type's lowest value, infinities) the
+    // product would overflow where the difference does not: the difference first.
+    __device__ __forceinline__ void exponentials(float (&x)[32], float base) {
+        if (__any_sync(0xffffffffu, !(fabsf(base) < 1e38f))) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) x[j] = tc_ex2((x[j] - base) * LOG2E);
+        } else {
+            const float shift = -base * LOG2E;
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+                tc_fma2(x[j], x[j + 1], LOG2E, shift);
+                x[j] = tc_ex2(x[j]), x[j + 1] = tc_ex2(x[j + 1]);
+            }
+        }
+    }
+
     // 32 columns: chunk cc of the warp's four.
     __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int cc) {
         float x[32];
@@ -234,7 +258,8 @@ struct Epilogue {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const float4 b = __ldg(reinterpret_cast<const float4 *>(a.bias + v) + j);
-                    x[4 * j] += b.x, x[4 * j + 1] += b.y, x[4 * j + 2] += b.z, x[4 * j + 3] += b.w;
+                    tc_add2(x[4 * j], x[4 * j + 1], b.x, b.y);
+                    tc_add2(x[4 * j + 2], x[4 * j + 3], b.z, b.w);
                 }
             }
             if (v + 32 > a.classes) {
@@ -245,10 +270,10 @@ struct Epilogue {
             const int lj = label - v;
             const bool mine = lj >= 0 && lj < 32;
             if (MODE == LOSS) {
-                float t0 = fmaxf(x[0], x[1]), t1 = fmaxf(x[2], x[3]);
+                float t0 = m_run, t1 = x[0];
 #pragma unroll
-                for (int j = 4; j < 32; j += 4) t0 = fmaxf(t0, fmaxf(x[j], x[j + 1])), t1 = fmaxf(t1, fmaxf(x[j + 2], x[j + 3]));
-                const float top = fmaxf(m_run, fmaxf(t0, t1)), base = top == -INFINITY ? 0.0f : top;
+                for (int j = 1; j < 31; j += 4) t0 = tc_max3(t0, x[j], x[j + 1]), t1 = tc_max3(t1, x[j + 2], j + 3 < 31 ? x[j + 3] : x[31]);
+                const float top = tc_max3(t0, t1, x[31]), base = top == -INFINITY ? 0.0f : top;
                 if (__any_sync(0xffffffffu, mine)) {
                     float z = x[0];
 #pragma unroll
@@ -256,20 +281,15 @@ struct Epilogue {
                         if (lj == j) z = x[j];
                     if (mine) a.z_label[row] = z;
                 }
+                exponentials(x, base);
                 float s0 = l_run * tc_ex2((m_run - base) * LOG2E), s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 32; j += 4) {
-                    s0 += tc_ex2((x[j] - base) * LOG2E);
-                    s1 += tc_ex2((x[j + 1] - base) * LOG2E);
-                    s2 += tc_ex2((x[j + 2] - base) * LOG2E);
-                    s3 += tc_ex2((x[j + 3] - base) * LOG2E);
-                }
+                for (int j = 0; j < 32; j += 4) tc_add2(s0, s1, x[j], x[j + 1]), tc_add2(s2, s3, x[j + 2], x[j + 3]);
                 l_run = (s0 + s1) + (s2 + s3);
                 m_run = top;
                 return;
             }
-#pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] = tc_ex2((x[j] - lse) * LOG2E);
+            exponentials(x, lse);
             if (__any_sync(0xffffffffu, mine)) {
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
@@ -441,6 +461,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
             tc_commit<CG>(drained);
             tc_bar_wait(drained, 0, &never);
         }
+    } else if (warp >= 4 && MODE == DW && count == 0) {
+        // no labelled row: zeros
+        for (int i = blockIdx.x * EPI_WARPS + warp - 4; i < a.rows; i += gridDim.x * EPI_WARPS)
+            for (int d = lane; d < a.dim; d += 32) a.out[(a.v0 + i) * a.ld_out + d] = 0;
     } else if (warp >= 4) {
         // ---- epilogue: thread = row of the tile, half of the columns per warp
         const int quarter = warp & 3, half = (warp - 4) >> 2;
@@ -633,58 +657,58 @@ __global__ void __launch_bounds__(256) k_realign(const uint16_t *in, long long l
 
 // ---- loss from the tiles' statistics -------------------------------------------------------------------
 
-constexpr int JOIN_ROWS = 8;   // one warp per row
+constexpr int JOIN_THREADS = 256;
 
-__global__ void __launch_bounds__(JOIN_ROWS * 32) k_loss_join(const float2 *stat, int n_tiles, const float *z_label, const int *pos_of, int n,
-                                                              const int *count, float *losses, float *lse, double *block_loss,
-                                                              unsigned *arrived, float *loss) {
+// A group of 2^lg lanes per row.
+__global__ void __launch_bounds__(JOIN_THREADS) k_loss_join(const float2 *stat, int n_tiles, const float *z_label, const int *pos_of, int n, int lg,
+                                                            const int *count, float *losses, float *lse, double *block_loss, unsigned *arrived,
+                                                            float *loss) {
     qg_after_prior();
-    __shared__ double w[JOIN_ROWS];
+    __shared__ double w[JOIN_THREADS / 32];
     __shared__ bool last;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31, row = blockIdx.x * JOIN_ROWS + warp;
-    float mine = 0.0f;
-    if (row < n) {
-        const int p = pos_of[row];
-        float l_out = 0.0f;
-        if (p >= 0) {
-            float m = -INFINITY, l = 0.0f;
-            const float2 *q = stat + (long long)p * n_tiles;
-            for (int t = lane; t < n_tiles; t += 32 * 8) {
-                float2 s[8];
-                float top = m;
+    const int lanes = 1 << lg, lane = threadIdx.x & (lanes - 1), row = blockIdx.x * (JOIN_THREADS >> lg) + (threadIdx.x >> lg);
+    const int p = row < n ? pos_of[row] : -1;
+    float mine = 0.0f, m = -INFINITY, l = 0.0f;
+    const float z = p >= 0 ? z_label[p] : 0.0f;
+    if (p >= 0) {
+        const float2 *q = stat + (long long)p * n_tiles;
+        for (int t = lane; t < n_tiles; t += lanes * 8) {
+            float2 s[8];
+            float top = m;
 #pragma unroll
-                for (int u = 0; u < 8; ++u) s[u] = q[min(t + u * 32, n_tiles - 1)];
+            for (int u = 0; u < 8; ++u) s[u] = q[min(t + u * lanes, n_tiles - 1)];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    if (t + u * 32 >= n_tiles) s[u] = make_float2(-INFINITY, 0.0f);
-                    top = fmaxf(top, s[u].x);
-                }
-                const float base = top == -INFINITY ? 0.0f : top;
-                l *= tc_ex2((m - base) * LOG2E);
-#pragma unroll
-                for (int u = 0; u < 8; ++u) l += s[u].y * tc_ex2((s[u].x - base) * LOG2E);
-                m = top;
+            for (int u = 0; u < 8; ++u) {
+                if (t + u * lanes >= n_tiles) s[u] = make_float2(-INFINITY, 0.0f);
+                top = fmaxf(top, s[u].x);
             }
+            const float base = top == -INFINITY ? 0.0f : top;
+            l *= tc_ex2((m - base) * LOG2E);
 #pragma unroll
-            for (int o = 16; o; o >>= 1) {
-                const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-                const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
-                l = l * tc_ex2((m - base) * LOG2E) + l2 * tc_ex2((m2 - base) * LOG2E);
-                m = top;
-            }
-            l_out = m + logf(l);
-            mine = l_out - z_label[p];
-        }
-        if (lane == 0) {
-            lse[row] = l_out;
-            if (losses) losses[row] = mine;
+            for (int u = 0; u < 8; ++u) l += s[u].y * tc_ex2((s[u].x - base) * LOG2E);
+            m = top;
         }
     }
-    if (lane == 0) w[warp] = (double)mine;
+    for (int o = lanes / 2; o; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+        l = l * tc_ex2((m - base) * LOG2E) + l2 * tc_ex2((m2 - base) * LOG2E);
+        m = top;
+    }
+    if (row < n && lane == 0) {
+        const float l_out = p >= 0 ? m + logf(l) : 0.0f;
+        if (p >= 0) mine = l_out - z;
+        lse[row] = l_out;
+        if (losses) losses[row] = mine;
+    }
+    double sum = (double)mine;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) w[threadIdx.x / 32] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         double s = 0.0;
-        for (int i = 0; i < JOIN_ROWS; ++i) s += w[i];
+        for (int i = 0; i < JOIN_THREADS / 32; ++i) s += w[i];
         block_loss[blockIdx.x] = s;
         __threadfence();
         last = atomicAdd(arrived, 1u) == gridDim.x - 1;
@@ -694,14 +718,14 @@ __global__ void __launch_bounds__(JOIN_ROWS * 32) k_loss_join(const float2 *stat
     // the block that comes last adds the blocks' sums, in their order
     __threadfence();
     double s = 0.0;
-    for (int i = threadIdx.x; i < (int)gridDim.x; i += JOIN_ROWS * 32) s += *(volatile double *)&block_loss[i];
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += JOIN_THREADS) s += *(volatile double *)&block_loss[i];
 #pragma unroll
     for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if (lane == 0) w[warp] = s;
+    if ((threadIdx.x & 31) == 0) w[threadIdx.x / 32] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
         s = 0.0;
-        for (int i = 0; i < JOIN_ROWS; ++i) s += w[i];
+        for (int i = 0; i < JOIN_THREADS / 32; ++i) s += w[i];
         const int c = *count;
         *loss = (float)(s / (double)(c > 0 ? c : 1));
         *arrived = 0;
@@ -730,14 +754,14 @@ __device__ __forceinline__ void write4(T *o, int left, const float4 &s, float sc
 
 // dH: every row of the caller's, zeros where it has no label.  A group of 2^lg threads per row, four columns each.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, int gangs, int rounds, int kb, const int *pos_of, int rows, int dim,
+__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, int gangs, int rounds, bool split, int kb, const int *pos_of, int rows, int dim,
                                                    const float *grad_loss, const int *count, T *out, long long ld_out, int lg) {
     qg_after_prior();
     const int r = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), lane = threadIdx.x & ((1 << lg) - 1);
     if (r >= rows) return;
     const int n = *count, p = pos_of[r], m_live = (n + BM - 1) / BM;
     const float scale = out_scale(grad_loss, n);
-    const Line line(rounds * m_live, kb, gangs);
+    const Line line(rounds * m_live, kb, gangs, split);
     int round = -1, place = 0, g0 = 0, g1 = -1;
     for (int d = lane * 4; d < dim; d += 4 << lg) {
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -760,16 +784,8 @@ __global__ void __launch_bounds__(256) k_dw_finish(const float *part, int gang, 
                                                    const float *grad_loss, const int *count, T *out, long long ld_out) {
     qg_after_prior();
     const int n = *count, kb = (n + BK - 1) / BK;
-    if (n == 0) {   // no labelled row: nothing has been written yet
-        const int quads = (dim + 3) / 4;
-        for (long long i = (blockIdx.y * gridDim.x + blockIdx.x) * 256ll + threadIdx.x; i < (long long)rows * quads; i += gridDim.x * gridDim.y * 256ll) {
-            const long long r = i / quads;
-            const int d = (int)(i - r * quads) * 4;
-            write4(out + r * ld_out + d, dim - d, make_float4(0.0f, 0.0f, 0.0f, 0.0f), 0.0f);
-        }
-        return;
-    }
-    const Line line(rounds * m_tiles, kb, gangs);
+    if (n == 0) return;
+    const Line line(rounds * m_tiles, kb, gangs, true);
     const int g = blockIdx.x / gang + 1, member = blockIdx.x % gang;
     if (g >= line.runs) return;
     const long long cut = line.start(g);
@@ -933,18 +949,20 @@ int unit_count(const qgbdt_ctx *c, long long tiles) {
 // leave at most 6 % of the units without work the largest, or else the size that leaves the fewest.
 struct Gangs {
     int size, gangs, rounds;
+    bool split;
     int units() const { return size * gangs; }
 };
 Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int n_tiles, long long kb) {
     const int units = c->sm_count / CG;
-    Gangs best{1, units, n_tiles};
+    Gangs best{1, units, n_tiles, false};
     double best_use = 0.0;
     for (int g = 1; g <= 8 && g <= n_tiles && g <= units; ++g) {
         const int rounds = (n_tiles + g - 1) / g;
         const double use = (double)(units / g * g) / units * n_tiles / (rounds * g);
-        if (use >= 0.94 || use > best_use) best = Gangs{g, units / g, rounds}, best_use = use;
+        if (use >= 0.94 || use > best_use) best = Gangs{g, units / g, rounds, false}, best_use = use;
     }
-    const long long most = (best.rounds * m_tiles * kb + 3) / 4;   // runs hold at least four blocks
+    best.split = kb >= SPLIT_KB;
+    const long long lines = best.rounds * m_tiles, most = best.split ? (lines * kb + 3) / 4 : lines;
     if (best.gangs > most) best.gangs = most < 1 ? 1 : (int)most;
     return best;
 }
@@ -953,7 +971,7 @@ template <typename T>
 int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *part, const Gangs &g, int kb, cudaStream_t st) {
     int lg = 0;
     while (lg < 8 && (4 << lg) < a.dim) ++lg;
-    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, part, g.size, g.gangs, g.rounds, kb,
+    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, part, g.size, g.gangs, g.rounds, g.split, kb,
                      o.pack.pos_of, (int)a.rows, a.dim, a.grad_loss, o.pack.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden, lg);
 }
 
@@ -968,7 +986,9 @@ int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *
 int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
     const bool copy = !rows_aligned(a.weight, a.ld_weight);
     const int n_tiles = up(a.classes, BN) / BN, n_pad = up(a.rows, 256);
-    const int join_blocks = a.rows > 0 ? (int)((a.rows + JOIN_ROWS - 1) / JOIN_ROWS) : 1;
+    int lg = 0;   // lanes per row of the join: one per two columns of a tile's statistics, at most a warp
+    while (lg < 5 && (1 << lg) < n_tiles) ++lg;
+    const int join_blocks = a.rows > 0 ? (int)((a.rows + (JOIN_THREADS >> lg) - 1) / (JOIN_THREADS >> lg)) : 1;
     const int units = unit_count(c, (long long)(n_pad / BM) * n_tiles);
     if (units < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
     QgWorkspace ws;
@@ -988,7 +1008,7 @@ int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
         if ((rc = matrix_map(c, &mb, o.weight, a.dim, a.classes, o.ld_weight, B_ROWS, a.type)) != QGBDT_OK) return rc;
         if ((rc = gemm<LOSS>(c, g, units, ma, mb, ma, ma, st)) != QGBDT_OK) return rc;
     }
-    QG_RUN(qg_launch(c, k_loss_join, dim3(join_blocks), JOIN_ROWS * 32, 0, st, g.stat, n_tiles * 2, g.z_label, o.pack.pos_of, (int)a.rows, o.pack.count, a.losses, a.lse,
+    QG_RUN(qg_launch(c, k_loss_join, dim3(join_blocks), JOIN_THREADS, 0, st, g.stat, n_tiles * 2, g.z_label, o.pack.pos_of, (int)a.rows, lg, o.pack.count, a.losses, a.lse,
                                                         block_loss, c->d_ops_counters, a.loss));
     return qg_ws_close(c, st);
 }
@@ -1010,7 +1030,7 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     const int grad_units = unit_count(c, m_tiles * (width / BN));
     if (grad_units < 0 || unit_count(c, (long long)m_tiles * d_tiles) < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
     const Gangs dh_gangs = gang_plan(c, m_tiles, d_tiles, kb_dh), dw_gangs = gang_plan(c, width / BM, d_tiles, n_pad / BK);
-    const size_t dh_fragments = ((size_t)m_tiles * dh_gangs.rounds + dh_gangs.gangs) * dh_gangs.size, dw_fragments = 2 * (size_t)dw_gangs.units();
+    const size_t dh_fragments = ((size_t)m_tiles * dh_gangs.rounds + dh_gangs.gangs) * dh_gangs.size, dw_fragments = dw_gangs.split ? 2 * (size_t)dw_gangs.units() : 0;
     QgWorkspace ws;
     int rc = qg_ws_open(c,
                         common_bytes(a, copy, pieces * width) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size(dh_fragments * BM * BN, 4) +
@@ -1033,7 +1053,8 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     if ((rc = matrix_map(c, &g_mn, g_piece, width, n_pad, width, 64, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &g_store, g_piece, width, n_pad, width, 32, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &dh_map, dh_part, BN, (long long)dh_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
-    if ((rc = matrix_map(c, &dw_map, dw_part, BN, (long long)dw_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    dw_map = dh_map;
+    if (dw_fragments && (rc = matrix_map(c, &dw_map, dw_part, BN, (long long)dw_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
     out = g_store;
     if (out_map && (rc = matrix_map(c, &out, a.d_weight, a.dim, a.classes, a.ld_d_weight, 32, a.type)) != QGBDT_OK) return rc;
     for (int k = 0; k < pieces; ++k) {
@@ -1047,13 +1068,14 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
         }
         g = base;
         g.v0 = v0, g.n_tiles = d_tiles, g.kb = kb_dh, g.add = k > 0;
-        g.gang = dh_gangs.size, g.gangs = dh_gangs.gangs, g.rounds = dh_gangs.rounds;
+        g.gang = dh_gangs.size, g.gangs = dh_gangs.gangs, g.rounds = dh_gangs.rounds, g.split = dh_gangs.split;
         if ((rc = gemm<DH>(c, g, dh_gangs.units(), g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
         g = base;
         g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = d_tiles;
-        g.gang = dw_gangs.size, g.gangs = dw_gangs.gangs, g.rounds = dw_gangs.rounds;
-        g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
+        g.gang = dw_gangs.size, g.gangs = dw_gangs.gangs, g.rounds = dw_gangs.rounds, g.split = dw_gangs.split;
+        g.rows = nv, g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
         if ((rc = gemm<DW>(c, g, dw_gangs.units(), g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
+        if (!dw_gangs.split) continue;
         rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, o, dw_part, g, nv, st) : dw_finish<__half>(c, a, o, dw_part, g, nv, st);
         if (rc != QGBDT_OK) return rc;
     }
