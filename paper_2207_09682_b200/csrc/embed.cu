@@ -195,7 +195,7 @@ __device__ __forceinline__ unsigned token_key(const SortArgs &a, unsigned t, boo
 }
 
 // Few pairs: every pair's place is the number of pairs before it, counted directly; one launch.
-constexpr int SORT_SMALL = 4096;
+constexpr int SORT_SMALL = 8192;
 constexpr int SORT_SMALL_LANES = 8;   // lanes that share the count of one pair
 
 template <typename I>
@@ -737,9 +737,10 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.lg = log2_at_least((a.dim + V - 1) / V, 5);
     s.col_blocks = (a.dim + (V << s.lg) - 1) / (V << s.lg);
     s.zero_blocks = (a.n_entries + ZERO_ROWS - 1) / ZERO_ROWS;
-    // tiles: about two rounds of resident groups, at least 16 pairs each
-    const long long target = (long long)c->sm_count * 2048 * 2 >> s.lg;
-    long long tile = (n * s.col_blocks + target - 1) / target;
+    // tiles: short lists go once over the groups that fit on the SMs together (768 threads each), long ones four times,
+    // which evens out what the SMs get; at least 16 pairs
+    const long long fit = (long long)c->sm_count * 768 >> s.lg, pairs = (n * s.col_blocks + fit - 1) / fit;
+    long long tile = pairs <= 128 ? pairs : pairs <= 512 ? 128 : pairs / 4;
     tile = tile < 16 ? 16 : (tile + EMB_UNROLL - 1) / EMB_UNROLL * EMB_UNROLL;
     s.tile = (int)(tile < (1 << 20) ? tile : 1 << 20);
     s.tiles = (n + s.tile - 1) / s.tile;

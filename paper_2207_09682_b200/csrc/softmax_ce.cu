@@ -655,6 +655,114 @@ __global__ void __launch_bounds__(256) k_realign(const uint16_t *in, long long l
     }
 }
 
+// ---- few rows -----------------------------------------------------------------------------------------
+// Scoring a handful of rows reads the weight once and does next to nothing with it: no packing, no tiles.  A warp
+// takes a few classes at a time, 16 bytes of each per lane, multiplies them with one or two rows of H and adds the
+// lanes' products in a tree that leaves every lane with one class; its statistics stay in registers until the end.
+// Bound by the weight's way out of DRAM (or L2).  From three rows on the tiles are faster: 32000 classes x 512, loss
+// from start to end, tiles against this: one row 15.9 and 10.4 us, two 15.9 and 11.7; three 16.0 and, with a four-row variant, 19.2.
+
+constexpr int FEW_ROWS = 2, FEW_CLASSES = 4, FEW_WARPS = 4, FEW_BLOCKS = 5;   // blocks per SM
+
+struct FewArgs {
+    const uint16_t *hidden, *weight;
+    long long ld_hidden, ld_weight;
+    int rows, classes, dim;        // rows of both start on 16 bytes, dim is a multiple of 8
+    const float *bias;
+    const void *labels;
+    int label_type;
+    float2 *stat;                  // [rows][gridDim.x]
+    float *z_label;
+    int *count, *pos_of;
+    int *status;
+};
+
+template <typename T, int R>
+__global__ void __launch_bounds__(FEW_WARPS * 32, FEW_BLOCKS) k_loss_few(const FewArgs a) {
+    qg_after_prior();
+    __shared__ float2 part[FEW_WARPS][R];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
+    int label[R], rows = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        long long l = -1;
+        if (r < a.rows) l = a.label_type == QGBDT_I64 ? reinterpret_cast<const long long *>(a.labels)[r] : (long long)reinterpret_cast<const int *>(a.labels)[r];
+        label[r] = l >= 0 && l < a.classes ? (int)l : -1;
+        rows += label[r] >= 0;
+        if (blockIdx.x == 0 && threadIdx.x == 0 && r < a.rows) {
+            a.pos_of[r] = label[r] >= 0 ? r : -1;
+            if (l >= a.classes && a.status) *a.status = 1;
+        }
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = rows;
+    float m[R], l[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) m[r] = -INFINITY, l[r] = 0.0f;
+    const int mine = (lane & 16 ? 2 : 0) + (lane & 8 ? 1 : 0);   // class of the four whose sum this lane gets
+    for (int v0 = (blockIdx.x * FEW_WARPS + warp) * FEW_CLASSES; v0 < a.classes; v0 += gridDim.x * FEW_WARPS * FEW_CLASSES) {
+        float acc[R][FEW_CLASSES];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < FEW_CLASSES; ++j) acc[r][j] = 0.0f;
+#pragma unroll 2
+        for (int d = lane * 8; d < a.dim; d += 256) {
+            OpsVec<T, 8> w[FEW_CLASSES], h[R];
+#pragma unroll
+            for (int j = 0; j < FEW_CLASSES; ++j)
+                w[j] = *reinterpret_cast<const OpsVec<T, 8> *>(a.weight + (long long)min(v0 + j, a.classes - 1) * a.ld_weight + d);
+#pragma unroll
+            for (int r = 0; r < R; ++r) h[r] = *reinterpret_cast<const OpsVec<T, 8> *>(a.hidden + (long long)min(r, a.rows - 1) * a.ld_hidden + d);
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int j = 0; j < FEW_CLASSES; ++j) acc[r][j] = __fmaf_rn(OpsType<T>::load(w[j].v[k]), OpsType<T>::load(h[r].v[k]), acc[r][j]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int o = 16, n = 2; o >= 8; o >>= 1, n >>= 1) {
+                const bool up = lane & o;
+#pragma unroll
+                for (int j = 0; j < n; ++j) {
+                    const float give = up ? acc[r][j] : acc[r][j + n], keep = up ? acc[r][j + n] : acc[r][j];
+                    acc[r][j] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+                }
+            }
+            float z = acc[r][0];
+#pragma unroll
+            for (int o = 4; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+            const int v = v0 + mine;
+            if (v < a.classes && (lane & 7) == 0) {
+                if (a.bias) z += a.bias[v];
+                if (v == label[r]) a.z_label[r] = z;
+                const float top = fmaxf(m[r], z), base = top == -INFINITY ? 0.0f : top;
+                l[r] = l[r] * tc_ex2((m[r] - base) * LOG2E) + tc_ex2((z - base) * LOG2E);
+                m[r] = top;
+            }
+        }
+    }
+    auto join = [](float &m, float &l, float m2, float l2) {
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+        l = l * tc_ex2((m - base) * LOG2E) + l2 * tc_ex2((m2 - base) * LOG2E);
+        m = top;
+    };
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int o = 16; o >= 8; o >>= 1) join(m[r], l[r], __shfl_xor_sync(0xffffffffu, m[r], o), __shfl_xor_sync(0xffffffffu, l[r], o));
+        if (lane == 0) part[warp][r] = make_float2(m[r], l[r]);
+    }
+    __syncthreads();
+    if (threadIdx.x < R && threadIdx.x < a.rows) {
+        float2 s = part[0][threadIdx.x];
+        for (int w = 1; w < FEW_WARPS; ++w) join(s.x, s.y, part[w][threadIdx.x].x, part[w][threadIdx.x].y);
+        a.stat[threadIdx.x * gridDim.x + blockIdx.x] = s;
+    }
+}
+
 // ---- loss from the tiles' statistics -------------------------------------------------------------------
 
 constexpr int JOIN_THREADS = 256;
@@ -983,8 +1091,31 @@ int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const Common &o, const float *
 
 }  // namespace
 
+// The loss of up to FEW_ROWS rows with aligned operands.
+static int loss_few(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
+    const long long most = c->sm_count * FEW_BLOCKS, want = (a.classes + FEW_WARPS * FEW_CLASSES - 1) / (FEW_WARPS * FEW_CLASSES);
+    const int blocks = (int)(want < most ? want : most);
+    QgWorkspace ws;
+    QG_RUN(qg_ws_open(c, qg_ws_size((size_t)FEW_ROWS * blocks, 8) + 4 * 256, st, &ws));
+    FewArgs f{};
+    f.hidden = reinterpret_cast<const uint16_t *>(a.hidden), f.weight = reinterpret_cast<const uint16_t *>(a.weight);
+    f.ld_hidden = a.ld_hidden, f.ld_weight = a.ld_weight, f.rows = (int)a.rows, f.classes = (int)a.classes, f.dim = a.dim;
+    f.bias = a.bias, f.labels = a.labels, f.label_type = a.label_type, f.status = a.status;
+    f.stat = ws.take<float2>((size_t)FEW_ROWS * blocks);
+    f.z_label = ws.take<float>(FEW_ROWS), f.count = ws.take<int>(1), f.pos_of = ws.take<int>(FEW_ROWS);
+    double *block_loss = ws.take<double>(1);
+    const bool bf16 = a.type == QGBDT_BF16;
+    const auto kernel = a.rows == 1 ? (bf16 ? k_loss_few<__nv_bfloat16, 1> : k_loss_few<__half, 1>)
+                                    : (bf16 ? k_loss_few<__nv_bfloat16, 2> : k_loss_few<__half, 2>);
+    QG_RUN(qg_launch(c, kernel, dim3(blocks), FEW_WARPS * 32, 0, st, f));
+    QG_RUN(qg_launch(c, k_loss_join, dim3(1), JOIN_THREADS, 0, st, f.stat, blocks, f.z_label, f.pos_of, f.rows, 5, f.count, a.losses, a.lse, block_loss,
+                     c->d_ops_counters, a.loss));
+    return qg_ws_close(c, st);
+}
+
 int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
     const bool copy = !rows_aligned(a.weight, a.ld_weight);
+    if (a.rows > 0 && a.rows <= FEW_ROWS && !copy && a.dim % 8 == 0 && rows_aligned(a.hidden, a.ld_hidden)) return loss_few(c, a, st);
     const int n_tiles = up(a.classes, BN) / BN, n_pad = up(a.rows, 256);
     int lg = 0;   // lanes per row of the join: one per two columns of a tile's statistics, at most a warp
     while (lg < 5 && (1 << lg) < n_tiles) ++lg;
