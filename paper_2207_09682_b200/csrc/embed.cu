@@ -195,7 +195,7 @@ __device__ __forceinline__ unsigned token_key(const SortArgs &a, unsigned t, boo
 }
 
 // Few pairs: every pair's place is the number of pairs before it, counted directly; one launch.
-constexpr int SORT_SMALL = 8192;
+constexpr int SORT_SMALL = 6144;   // 11 us at 4096 pairs and 26 us at 8000, where the passes below take 20 us
 constexpr int SORT_SMALL_LANES = 8;   // lanes that share the count of one pair
 
 template <typename I>
@@ -271,16 +271,21 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_scan(unsigned *counts, uns
     const int d = blockIdx.x * SORT_WARPS + threadIdx.x / 32, lane = threadIdx.x & 31;
     if (d >= digits) return;
     unsigned *row = counts + (size_t)d * blocks, run = 0;
-    for (int b = 0; b < blocks; b += 32) {
-        const unsigned x = b + lane < blocks ? row[b + lane] : 0;
-        unsigned s = x;
+    for (int b = 0; b < blocks; b += 32 * 8) {
+        unsigned x[8];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned y = __shfl_up_sync(0xffffffffu, s, o);
-            if (lane >= o) s += y;
+        for (int u = 0; u < 8; ++u) x[u] = b + u * 32 + lane < blocks ? row[b + u * 32 + lane] : 0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            unsigned s = x[u];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const unsigned y = __shfl_up_sync(0xffffffffu, s, o);
+                if (lane >= o) s += y;
+            }
+            if (b + u * 32 + lane < blocks) row[b + u * 32 + lane] = run + s - x[u];
+            run += __shfl_sync(0xffffffffu, s, 31);
         }
-        if (b + lane < blocks) row[b + lane] = run + s - x;
-        run += __shfl_sync(0xffffffffu, s, 31);
     }
     if (lane == 0) totals[d] = run;
 }
@@ -418,10 +423,10 @@ struct SegArgs {
     float scale;
     float *partial;         // [tiles][2][dim]: sum of a tile's first token when it began in an earlier tile;
                             // sum of its last token when it began here and goes on in the next tile
-    long long zero_blocks;  // blocks that clear the rows no token points to
+    long long sum_blocks;   // blocks that add; those behind them clear the rows no token points to
 };
 
-constexpr int ZERO_ROWS = 32;   // rows of the gradient a clearing block looks at
+constexpr int ZERO_ROWS = 128;   // rows of the gradient a clearing block looks at
 
 __device__ __forceinline__ long long first_not_below(const uint2 *pair, long long n, unsigned key) {
     long long lo = 0, hi = n;
@@ -435,9 +440,9 @@ __device__ __forceinline__ long long first_not_below(const uint2 *pair, long lon
 
 template <typename T, int V>
 __device__ void clear_rows(const SegArgs &a, long long block) {
-    __shared__ unsigned absent;
+    __shared__ unsigned absent[ZERO_ROWS / 32];
     const long long v0 = block * ZERO_ROWS;
-    if (threadIdx.x < 32) {
+    if (threadIdx.x < ZERO_ROWS) {
         const long long v = v0 + threadIdx.x;
         bool none = false;
         if (v < a.n_entries) {
@@ -445,15 +450,16 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
             none = at >= a.n || a.pair[at].x != (unsigned)v;
         }
         const unsigned m = __ballot_sync(0xffffffffu, none);
-        if (threadIdx.x == 0) absent = m;
+        if ((threadIdx.x & 31) == 0) absent[threadIdx.x / 32] = m;
     }
     __syncthreads();
     OpsVec<T, V> zero;
 #pragma unroll
     for (int j = 0; j < V; ++j) zero.v[j] = OpsType<T>::store(0.0f);
-    for (unsigned m = absent; m; m &= m - 1) {
-        T *row = reinterpret_cast<T *>(a.out) + (v0 + __ffs(m) - 1) * a.ld_out;
-        for (int col = threadIdx.x * V; col < a.dim; col += EMB_THREADS * V) *reinterpret_cast<OpsVec<T, V> *>(row + col) = zero;
+    for (int r = threadIdx.x >> a.lg; r < ZERO_ROWS; r += EMB_THREADS >> a.lg) {
+        if (!(absent[r / 32] >> (r & 31) & 1)) continue;
+        T *row = reinterpret_cast<T *>(a.out) + (v0 + r) * a.ld_out;
+        for (int col = (threadIdx.x & ((1 << a.lg) - 1)) * V; col < a.dim; col += V << a.lg) *reinterpret_cast<OpsVec<T, V> *>(row + col) = zero;
     }
 }
 
@@ -461,11 +467,11 @@ template <typename T, int V>
 __global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a) {
     qg_after_prior();
     using Vec = OpsVec<T, V>;
-    if ((long long)blockIdx.x < a.zero_blocks) {
-        clear_rows<T, V>(a, blockIdx.x);
+    const long long block = blockIdx.x;
+    if (block >= a.sum_blocks) {   // behind the others: these wait for nothing
+        clear_rows<T, V>(a, block - a.sum_blocks);
         return;
     }
-    const long long block = (long long)blockIdx.x - a.zero_blocks;
     const int lane = threadIdx.x & ((1 << a.lg) - 1), group = threadIdx.x >> a.lg;
     const long long t = block / a.col_blocks * (EMB_THREADS >> a.lg) + group;
     const int col = ((int)(block % a.col_blocks) << a.lg) * V + lane * V;
@@ -703,7 +709,8 @@ int sort_pairs(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, uint2 *buf0, 
 template <typename T, int V>
 int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     const long long per_block = EMB_THREADS >> s.lg;
-    const long long blocks = s.zero_blocks + (s.tiles + per_block - 1) / per_block * s.col_blocks;
+    s.sum_blocks = (s.tiles + per_block - 1) / per_block * s.col_blocks;
+    const long long blocks = s.sum_blocks + (s.n_entries + ZERO_ROWS - 1) / ZERO_ROWS;
     if (blocks > 0x7fffffffll) return qg_fail(c, QGBDT_ERR_ARG, "rows * bag * dim is too large for one call");
     QG_RUN(qg_launch(c, k_segment_sum<T, V>, dim3((unsigned)blocks), EMB_THREADS, 0, st, s));
     if (s.tiles > 1) {
@@ -736,7 +743,6 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.dim = a.dim, s.scale = a.scale;
     s.lg = log2_at_least((a.dim + V - 1) / V, 5);
     s.col_blocks = (a.dim + (V << s.lg) - 1) / (V << s.lg);
-    s.zero_blocks = (a.n_entries + ZERO_ROWS - 1) / ZERO_ROWS;
     // tiles: short lists go once over the groups that fit on the SMs together (768 threads each), long ones four times,
     // which evens out what the SMs get; at least 16 pairs
     const long long fit = (long long)c->sm_count * 768 >> s.lg, pairs = (n * s.col_blocks + fit - 1) / fit;
