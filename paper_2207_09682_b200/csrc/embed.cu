@@ -552,6 +552,8 @@ template <typename T, int V>
 __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, int lg_cols) {
     qg_after_prior();
     __shared__ float part_sum[EMB_THREADS][V];
+    __shared__ long long long_links[EMB_THREADS];   // per group: tiles of a token that the whole block adds, or 0
+    __shared__ unsigned long_token[EMB_THREADS];
     const int cols = 1 << lg_cols, groups = EMB_THREADS >> lg_cols, group = threadIdx.x >> lg_cols, lane = threadIdx.x & (cols - 1);
     const unsigned none = (unsigned)a.n_entries;
     // Tiles t + 1 .. t + links hold the rest of a token that begins in tile t; 0 where there is none.  The four words
@@ -597,11 +599,13 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
             for (long long l = 1; l <= links; ++l) add(s, a.partial + ((mine + l) * 2) * a.dim + col);
             put(cur, col, s);
         }
+    if (lane == 0) long_links[group] = links > JOIN_SERIAL ? links : 0, long_token[group] = cur;
     if (!__syncthreads_or(links > JOIN_SERIAL)) return;
     for (int q = 0; q < groups; ++q) {   // the whole block for each of the others
+        links = long_links[q];
+        if (links == 0) continue;
         const long long t = t0 + q;
-        links = links_of(t, cur);
-        if (links <= JOIN_SERIAL) continue;
+        cur = long_token[q];
         const long long l0 = links * group / groups, l1 = links * (group + 1) / groups;
         for (int c0 = 0; c0 < a.dim; c0 += cols * V) {
             const int col = c0 + lane * V;
