@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import array
 import ctypes as C
+import functools
 import os
 from typing import NamedTuple
 
@@ -395,7 +396,25 @@ def _words(t, dtype, count: int, name: str, device: int):
     return t.data_ptr()
 
 
-def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, stream=None) -> torch.Tensor:
+def _streamed(call):
+    """A call on another stream than the current one makes its outputs there, and tells the allocator that its inputs
+    are in use there, so that neither is handed out again too early."""
+    @functools.wraps(call)
+    def run(self, *args, stream=None, **named):
+        if stream is None:
+            return call(self, *args, **named)
+        with torch.cuda.stream(stream):
+            result = call(self, *args, **named)
+        for a in (*args, *named.values()):
+            for t in a if isinstance(a, (list, tuple)) else (a,):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+        return result
+    return run
+
+
+@_streamed
+def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None) -> torch.Tensor:
     """qgbdt_embed: out[i] = scale * sum_k table[tokens[i, k]].  table [V, D] (float32, bfloat16 or float16), tokens
     [N] or [N, bag] (int32 or int64, negative = missing); out [N, D] of the table's type is made if not given."""
     dev, dtype = self.device, table.dtype
@@ -411,13 +430,14 @@ def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, strea
         if no != n or do != d or out.dtype != dtype:
             _refuse("out must be [N, D] of the table's type")
     rc = self.lib.qgbdt_embed(self.h, table.data_ptr(), kind, v, d, ld, tokens.data_ptr(), index, n, bag, ldt, scale, out.data_ptr(), ldo,
-                              _words(status, torch.int32, 1, "status", dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
+                              _words(status, torch.int32, 1, "status", dev), _raw_stream(dev))
     if rc:
         self._check(rc)
     return out
 
 
-def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None, stream=None) -> torch.Tensor:
+@_streamed
+def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None) -> torch.Tensor:
     """qgbdt_embed_backward: the table's gradient [n_entries, D] of grad_out's type, every row of it written."""
     dev, dtype = self.device, grad_out.dtype
     kind = _ELEMENT.get(dtype, -1)
@@ -435,7 +455,7 @@ def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, 
             _refuse("grad_table must be [n_entries, D] of grad_out's type")
     rc = self.lib.qgbdt_embed_backward(self.h, grad_out.data_ptr(), kind, ld, tokens.data_ptr(), index, n, bag, ldt, scale,
                                        grad_table.data_ptr(), n_entries, d, ldo, _words(status, torch.int32, 1, "status", dev),
-                                       _raw_stream(dev) if stream is None else stream.cuda_stream)
+                                       _raw_stream(dev))
     if rc:
         self._check(rc)
     return grad_table
@@ -457,21 +477,23 @@ def _softmax_inputs(hidden, weight, labels, bias, dev: int) -> tuple:
             _words(labels, labels.dtype, n, "labels", dev), index, n, v, d), n, v, d
 
 
-def _softmax_ce(self, hidden, weight, labels, bias=None, status=None, stream=None) -> SoftmaxCE:
+@_streamed
+def _softmax_ce(self, hidden, weight, labels, bias=None, status=None) -> SoftmaxCE:
     """qgbdt_softmax_ce: softmax cross entropy of hidden [N, D] @ weight [V, D]^T + bias [V] against labels [N] (negative:
     no label), mean over the labelled rows, without stored logits.  hidden, weight bfloat16 or float16, bias float32."""
     dev = self.device
     inputs, n, _, _ = _softmax_inputs(hidden, weight, labels, bias, dev)
     losses, lse, loss = torch.empty(2 * n + 1, dtype=torch.float32, device=hidden.device).split((n, n, 1))
     rc = self.lib.qgbdt_softmax_ce(self.h, *inputs, loss.data_ptr(), losses.data_ptr(), lse.data_ptr(),
-                                   _words(status, torch.int32, 1, "status", dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
+                                   _words(status, torch.int32, 1, "status", dev), _raw_stream(dev))
     if rc:
         self._check(rc)
     return SoftmaxCE(loss, losses, lse)
 
 
+@_streamed
 def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss=None, grad_hidden=None, grad_weight=None,
-                         status=None, stream=None) -> tuple:
+                         status=None) -> tuple:
     """qgbdt_softmax_ce_backward: (grad_hidden [N, D], grad_weight [V, D], grad_bias [V] or None) of grad_loss * loss;
     lse as softmax_ce gave it, grad_loss a float32 CUDA tensor of one element (None: 1)."""
     dev, dtype = self.device, hidden.dtype
@@ -491,13 +513,14 @@ def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss
     rc = self.lib.qgbdt_softmax_ce_backward(
         self.h, *inputs, _words(lse, torch.float32, n, "lse", dev), _words(grad_loss, torch.float32, 1, "grad_loss", dev),
         grad_hidden.data_ptr(), ldh, grad_weight.data_ptr(), ldw, None if grad_bias is None else grad_bias.data_ptr(),
-        _words(status, torch.int32, 1, "status", dev), _raw_stream(dev) if stream is None else stream.cuda_stream)
+        _words(status, torch.int32, 1, "status", dev), _raw_stream(dev))
     if rc:
         self._check(rc)
     return grad_hidden, grad_weight, grad_bias
 
 
-def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+@_streamed
+def _clip_grad_norm(self, grads, max_norm: float, out=None) -> torch.Tensor:
     """qgbdt_clip_grad_norm: the global norm (float32 tensor [1]) of a list of tensors, and every tensor times
     min(1, max_norm / norm), in place or into the tensors of `out`.  float32, bfloat16 and float16 may be mixed."""
     dev, n = self.device, len(grads)
@@ -520,7 +543,7 @@ def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torc
     counts = array.array("q", sizes)
     norm = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
     rc = self.lib.qgbdt_clip_grad_norm(self.h, src.buffer_info()[0], dst.buffer_info()[0], counts.buffer_info()[0], kinds.buffer_info()[0], n,
-                                       max_norm, norm.data_ptr(), _raw_stream(dev) if stream is None else stream.cuda_stream)
+                                       max_norm, norm.data_ptr(), _raw_stream(dev))
     if rc:
         self._check(rc)
     return norm

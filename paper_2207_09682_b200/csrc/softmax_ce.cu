@@ -1174,7 +1174,7 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     float *dh_part = ws.take<float>(dh_fragments * BM * BN), *dw_part = ws.take<float>(dw_fragments * BM * BN);
     float *bias_part = a.d_bias ? ws.take<float>((size_t)(n_pad / 32) * width) : nullptr;
     const GemmArgs base = gemm_args(c, a, o);
-    const bool bf16 = base.bf16, out_map = rows_aligned(a.d_weight, a.ld_d_weight);
+    const bool bf16 = base.bf16, out_map = rows_aligned(a.d_weight, a.ld_d_weight) && a.dim % 8 == 0;   // tiled copies cut rows off at 16 bytes only
     CUtensorMap h_k, h_mn, w_k, w_mn, g_k, g_mn, g_store, dh_map, dw_map, out;
     if ((rc = matrix_map(c, &h_k, o.pack.packed, a.dim, n_pad, o.ldp, 128, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &h_mn, o.pack.packed, a.dim, n_pad, o.ldp, 64, a.type)) != QGBDT_OK) return rc;

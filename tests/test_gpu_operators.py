@@ -147,6 +147,16 @@ def test_embed_infinite_and_nan_rows_stay_where_they_are(ctx):
     assert torch.isfinite(out[[0, 2]]).all() and torch.isnan(out[1]).all()
 
 
+def test_embed_backward_never_uses_rows_without_tokens(ctx):
+    tok = torch.randint(0, 40, (3000, 3), device="cuda")
+    tok[::3] = -1
+    grad = torch.randn((3000, 24), device="cuda").half()
+    grad[::3] = math.nan
+    got = ctx.embed_backward(grad, tok, 40)
+    grad[::3] = 0.0
+    check_embed_grad(got, grad, tok, 40, 1.0)
+
+
 def test_embed_strides(ctx):
     """Rows of tokens, of the table and of the outputs that lie apart; outputs leave the gaps alone."""
     wide_table = torch.randn((50, 40), device="cuda")
@@ -283,6 +293,9 @@ SOFTMAX = [
     (1, 1, 1, False, 0.0), (1, 2, 8, True, 0.0), (1, 32000, 512, False, 0.0), (3, 257, 64, True, 0.0), (128, 256, 64, False, 0.0),
     (129, 255, 65, True, 0.3), (300, 1000, 72, False, 0.5), (777, 1003, 129, True, 0.3), (1000, 10, 200, True, 0.9), (513, 4099, 40, False, 0.1),
     (9000, 300, 16, True, 0.2), (257, 513, 1000, True, 0.0), (40, 70, 8, False, 1.0),
+    # one and two rows with and without aligned operands; more than one column tile of d; long and short products that are cut or not
+    (1, 70, 264, True, 0.0), (2, 5003, 520, True, 0.0), (2, 31, 17, False, 0.0), (2, 100, 64, True, 0.6), (3000, 40, 300, True, 0.1),
+    (300, 3000, 520, False, 0.1), (2500, 2100, 24, True, 0.2), (700, 600, 1300, False, 0.0), (100, 9000, 2050, False, 0.0),
 ]
 
 
@@ -338,6 +351,29 @@ def test_softmax_ce_strides(ctx):
     got = ctx.softmax_ce_backward(h, w, y, r.lse, bias=b, grad_hidden=dh[:, 3:53], grad_weight=dw[:, 2:52])
     check_grads(got, e, h, w, torch.bfloat16)
     assert bool((dh[:, :3] == 7).all()) and bool((dh[:, 53:] == 7).all()) and bool((dw[:, :2] == 7).all()) and bool((dw[:, 52:] == 7).all())
+
+
+def test_softmax_ce_aligned_outputs_leave_the_gaps_alone(ctx):
+    """Rows of 50 elements on 128 bytes: what lies between them is neither read nor written."""
+    h, w, b, y = softmax_case(300, 300, 50, torch.float16, True, 0.2, 11)
+    wide_h, wide_w = torch.full((300, 64), math.nan, device="cuda").half(), torch.full((300, 64), math.nan, device="cuda").half()
+    wide_h[:, :50], wide_w[:, :50] = h, w
+    h, w = wide_h[:, :50], wide_w[:, :50]
+    e = softmax_exact(h, w, b, y, 1024.0)
+    r = ctx.softmax_ce(h, w, y, bias=b)
+    dh, dw = torch.full((300, 64), 7.0, device="cuda").half(), torch.full((302, 64), 7.0, device="cuda").half()
+    got = ctx.softmax_ce_backward(h, w, y, r.lse, bias=b, grad_loss=torch.full((1,), 1024.0, device="cuda"), grad_hidden=dh[:, :50], grad_weight=dw[:300, :50])
+    check_grads(got, e, h, w, torch.float16)
+    assert bool((dh[:, 50:] == 7).all()) and bool((dw[:, 50:] == 7).all()) and bool((dw[300:] == 7).all())
+
+
+def test_softmax_ce_all_classes_at_the_lowest_value(ctx):
+    """Every class masked by the type's lowest value: a uniform distribution, up to the rounding of numbers of that size."""
+    h, w, b, y = softmax_case(20, 300, 64, torch.bfloat16, True, 0.0, 4)
+    b[:] = torch.finfo(torch.float32).min
+    r = ctx.softmax_ce(h, w, y, bias=b)
+    assert bool((r.lse == torch.finfo(torch.float32).min).all()) and bool((r.losses == 0).all())
+    assert all(bool(torch.isfinite(t).all()) for t in ctx.softmax_ce_backward(h, w, y, r.lse, bias=b))
 
 
 def test_softmax_ce_large_logits_and_excluded_classes(ctx):
