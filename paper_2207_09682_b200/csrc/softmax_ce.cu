@@ -108,14 +108,15 @@ struct Line {
 // What a unit works on next.
 struct Work {
     int m, n, kb0, kb1;
+    int cols;            // columns of the tile: 256, or 128 where no more are left (DH, DW)
     int fragment;        // DH, and DW where the tile is not whole: which part buffer
     bool whole;
 };
 template <int MODE>
 struct Schedule {
-    int t, step, total, m_live, n_tiles, kb, unit, gang, member, size;
+    int t, step, total, m_live, n_tiles, dim, kb, unit, gang, member, size;
     long long pos, end;
-    __device__ Schedule(const GemmArgs &a, int count) : n_tiles(a.n_tiles) {
+    __device__ Schedule(const GemmArgs &a, int count) : n_tiles(a.n_tiles), dim(a.dim) {
         m_live = MODE == DW ? a.m_tiles : (count + BM - 1) / BM;
         kb = MODE == DW ? (count + BK - 1) / BK : a.kb;
         unit = blockIdx.x / CG;
@@ -133,7 +134,7 @@ struct Schedule {
         if (MODE == LOSS || MODE == GRAD) {
             if (t >= total) return false;
             tile_place(t, m_live, n_tiles, w.m, w.n);
-            w.kb0 = 0, w.kb1 = kb;
+            w.kb0 = 0, w.kb1 = kb, w.cols = BN;
             t += step;
             return true;
         } else {
@@ -144,6 +145,7 @@ struct Schedule {
                 w.kb0 = (int)(pos - (long long)place * kb);
                 w.kb1 = (int)min((long long)kb, w.kb0 + end - pos);
                 w.whole = w.kb0 == 0 && w.kb1 == kb;
+                w.cols = dim - w.n * BN > BN / 2 ? BN : BN / 2;
                 w.fragment = MODE == DH ? (place + gang) * size + member : 2 * unit + (w.kb0 == 0);
                 pos += w.kb1 - w.kb0;
                 if (w.n < n_tiles) return true;   // the last round may have fewer column tiles than the gang units
@@ -194,7 +196,7 @@ struct Epilogue {
     int col0;              // first of the warp's 128 columns
     bool live;
     int label;
-    float lse, scale, m_run, l_run;
+    float lse, scale;
 
     __device__ Epilogue(const GemmArgs &a_, const CUtensorMap *o, const CUtensorMap *p, uint32_t b, int l, int n)
         : a(a_), map_out(o), map_part(p), buf(b), lane(l), count(n) {
@@ -209,7 +211,6 @@ struct Epilogue {
         live = row < count;
         if (MODE == LOSS || MODE == GRAD) label = live ? a.label[row] : -1;
         if (MODE == GRAD) lse = live ? a.lse[row] : 0.0f;
-        if (MODE == LOSS) m_run = -INFINITY, l_run = 0.0f;
     }
 
     // The staging buffer may be written: the copy out of it has been read.
@@ -229,21 +230,60 @@ struct Epilogue {
                     pack2(x[8 * i + 4], x[8 * i + 5], a.bf16), pack2(x[8 * i + 6], x[8 * i + 7], a.bf16));
     }
 
-    // x = exp(x - base), in one multiplication and addition: base * log2(e) is rounded to 24 bits, as the logits of that
-    // size are themselves.  Near the end of the range (classes masked by the type's lowest value, infinities) the
-    // product would overflow where the difference does not: the difference first.
-    __device__ __forceinline__ void exponentials(float (&x)[32], float base) {
-        if (__any_sync(0xffffffffu, !(fabsf(base) < 1e38f))) {
+    // x = exp(x - base).  The difference first: base * log2(e) would overflow for classes masked by the type's lowest value.
+    template <int N>
+    __device__ __forceinline__ void exponentials(float (&x)[N], float base) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) x[j] = tc_ex2((x[j] - base) * LOG2E);
-        } else {
-            const float shift = -base * LOG2E;
+        for (int j = 0; j < N; j += 2) {
+            tc_add2(x[j], x[j + 1], -base, -base);
+            tc_mul2(x[j], x[j + 1], LOG2E);
+            x[j] = tc_ex2(x[j]), x[j + 1] = tc_ex2(x[j + 1]);
+        }
+    }
+
+    // Bias, and minus infinity behind the last class, for N logits from class v on.
+    template <int N>
+    __device__ __forceinline__ void logits(float (&x)[N], int v) {
+        if (a.bias) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
-                tc_fma2(x[j], x[j + 1], LOG2E, shift);
-                x[j] = tc_ex2(x[j]), x[j + 1] = tc_ex2(x[j + 1]);
+            for (int j = 0; j < N / 4; ++j) {
+                const float4 b = __ldg(reinterpret_cast<const float4 *>(a.bias + v) + j);
+                tc_add2(x[4 * j], x[4 * j + 1], b.x, b.y);
+                tc_add2(x[4 * j + 2], x[4 * j + 3], b.z, b.w);
             }
         }
+        if (v + N > a.classes) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (v + j >= a.classes) x[j] = -INFINITY;
+        }
+    }
+
+    // LOSS: all 128 columns of the warp at once; no logit waits for a running maximum.
+    __device__ __forceinline__ void row_statistics(float (&x)[128], int half) {
+        const int v = a.v0 + col0, lj = label - v;
+        logits(x, v);
+        const bool mine = lj >= 0 && lj < 128;
+        if (__any_sync(0xffffffffu, mine)) {
+            float z = x[0];
+#pragma unroll
+            for (int j = 1; j < 128; ++j)
+                if (lj == j) z = x[j];
+            if (mine) a.z_label[row] = z;
+        }
+        float t[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+        for (int j = 4; j < 124; j += 8)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = tc_max3(t[k], x[j + 2 * k], x[j + 2 * k + 1]);
+        const float top = fmaxf(fmaxf(tc_max3(t[0], x[124], x[125]), tc_max3(t[1], x[126], x[127])), fmaxf(t[2], t[3])), base = top == -INFINITY ? 0.0f : top;
+        exponentials(x, base);
+        float s[8] = {};
+#pragma unroll
+        for (int j = 0; j < 128; j += 8)
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) tc_add2(s[k], s[k + 1], x[j + k], x[j + k + 1]);
+        if (live) a.stat[((long long)row * a.n_tiles + c.n) * 2 + half] = make_float2(top, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
     }
 
     // 32 columns: chunk cc of the warp's four.
@@ -252,43 +292,10 @@ struct Epilogue {
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
         const int col = col0 + cc * 32;
-        if (MODE == LOSS || MODE == GRAD) {
-            const int v = a.v0 + col;
-            if (a.bias) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float4 b = __ldg(reinterpret_cast<const float4 *>(a.bias + v) + j);
-                    tc_add2(x[4 * j], x[4 * j + 1], b.x, b.y);
-                    tc_add2(x[4 * j + 2], x[4 * j + 3], b.z, b.w);
-                }
-            }
-            if (v + 32 > a.classes) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (v + j >= a.classes) x[j] = -INFINITY;
-            }
-            const int lj = label - v;
+        if (MODE == GRAD) {
+            const int v = a.v0 + col, lj = label - v;
             const bool mine = lj >= 0 && lj < 32;
-            if (MODE == LOSS) {
-                float t0 = m_run, t1 = x[0];
-#pragma unroll
-                for (int j = 1; j < 31; j += 4) t0 = tc_max3(t0, x[j], x[j + 1]), t1 = tc_max3(t1, x[j + 2], j + 3 < 31 ? x[j + 3] : x[31]);
-                const float top = tc_max3(t0, t1, x[31]), base = top == -INFINITY ? 0.0f : top;
-                if (__any_sync(0xffffffffu, mine)) {
-                    float z = x[0];
-#pragma unroll
-                    for (int j = 1; j < 32; ++j)
-                        if (lj == j) z = x[j];
-                    if (mine) a.z_label[row] = z;
-                }
-                exponentials(x, base);
-                float s0 = l_run * tc_ex2((m_run - base) * LOG2E), s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 32; j += 4) tc_add2(s0, s1, x[j], x[j + 1]), tc_add2(s2, s3, x[j + 2], x[j + 3]);
-                l_run = (s0 + s1) + (s2 + s3);
-                m_run = top;
-                return;
-            }
+            logits(x, v);
             exponentials(x, lse);
             if (__any_sync(0xffffffffu, mine)) {
 #pragma unroll
@@ -351,10 +358,6 @@ struct Epilogue {
             tc_store_commit();
         }
     }
-
-    __device__ __forceinline__ void end(int half) {
-        if (MODE == LOSS && live) a.stat[((long long)row * a.n_tiles + c.n) * 2 + half] = make_float2(m_run, l_run);
-    }
 };
 
 template <int MODE>
@@ -405,9 +408,10 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                 const int s = it % STAGES;
                 if (!(ok = tc_bar_wait(empty(s), (it / STAGES & 1) ^ 1, &stop))) break;
                 const uint32_t bar = CG == 1 ? full(s) : tc_map_rank(full(s), 0);
-                if (rank == 0) tc_bar_expect(full(s), CG * STAGE_BYTES);
+                const int b_rows = B_MN ? c.cols / CG : B_ROWS;   // of the second operand in this CTA
+                if (rank == 0) tc_bar_expect(full(s), CG * (A_BYTES + b_rows * BK * 2));
                 const uint32_t at = tiles_at + s * STAGE_BYTES, bt = at + A_BYTES;
-                const int am = c.m * BM + rank * 128, bn = c.n * BN + rank * B_ROWS;
+                const int am = c.m * BM + rank * 128, bn = c.n * BN + rank * b_rows;
                 if (A_MN) {
                     for (int j = 0; j < 2; ++j) tc_load_2d<CG>(at + j * 8192, &map_a, am + 64 * j, k * BK, bar);
                 } else {
@@ -415,7 +419,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                 }
                 if (B_MN) {
                     const int y = (MODE == DH ? a.v0 : 0) + k * BK;
-                    for (int j = 0; j < B_ROWS / 64; ++j) tc_load_2d<CG>(bt + j * 8192, &map_b, bn + 64 * j, y, bar);
+                    for (int j = 0; j < b_rows / 64; ++j) tc_load_2d<CG>(bt + j * 8192, &map_b, bn + 64 * j, y, bar);
                 } else {
                     tc_load_2d<CG>(bt, &map_b, k * BK, a.v0 + bn, bar);
                 }
@@ -431,9 +435,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
         }
     } else if (warp == 1 && lane == 0 && rank == 0) {
         // ---- matrix instructions
-        const uint32_t idesc = tc_idesc(BM, BN, a.bf16, A_MN, B_MN);
         int it = 0, n_acc = 0;
         while (ok && todo.next(c)) {
+            const uint32_t idesc = tc_idesc(BM, MODE == DH || MODE == DW ? c.cols : BN, a.bf16, A_MN, B_MN);
             const int b = n_acc & 1;
             if (!(ok = tc_bar_wait(acc_empty(b), (n_acc / 2 & 1) ^ 1, &stop))) break;
             tc_fence_after();
@@ -476,21 +480,39 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
             if (!(ok = __all_sync(0xffffffffu, tc_bar_wait(acc_full(b), n_acc / 2 & 1, &stop)))) break;
             tc_fence_after();
             const uint32_t tacc = tmem + ((uint32_t)(quarter * 32) << 16) + b * ACC_COLS + half * 128;
-            uint32_t r[2][32];
-            tc_ld_32(tacc, r[0]);
+            auto hand_back = [&]() {   // the accumulator may be filled again
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc_bar_arrive_cluster(CG == 1 ? acc_empty(b) : tc_map_rank(acc_empty(b), 0));
+            };
+            if constexpr (MODE == LOSS) {
+                uint32_t r[4][32];
+                float x[128];
 #pragma unroll
-            for (int cc = 0; cc < 4; ++cc) {
-                tc_ld_wait(r[cc & 1]);
-                if (cc < 3) {
-                    tc_ld_32(tacc + (cc + 1) * 32, r[(cc + 1) & 1]);   // read under the arithmetic of this chunk
-                } else {   // the accumulator may be filled again
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) tc_bar_arrive_cluster(CG == 1 ? acc_empty(b) : tc_map_rank(acc_empty(b), 0));
+                for (int cc = 0; cc < 4; ++cc) tc_ld_32(tacc + cc * 32, r[cc]);
+#pragma unroll
+                for (int cc = 0; cc < 4; ++cc) {
+                    tc_ld_wait(r[cc]);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[cc * 32 + j] = __uint_as_float(r[cc][j]);
                 }
-                epi.chunk(r[cc & 1], cc);
+                hand_back();
+                epi.row_statistics(x, half);
+            } else {
+                if (half * 128 < c.cols) {   // a narrow tile has nothing for the second half
+                    uint32_t r[2][32];
+                    tc_ld_32(tacc, r[0]);
+#pragma unroll
+                    for (int cc = 0; cc < 4; ++cc) {
+                        tc_ld_wait(r[cc & 1]);
+                        if (cc < 3) tc_ld_32(tacc + (cc + 1) * 32, r[(cc + 1) & 1]);   // read under the arithmetic of this chunk
+                        else hand_back();
+                        epi.chunk(r[cc & 1], cc);
+                    }
+                } else {
+                    hand_back();
+                }
             }
-            epi.end(half);
             ++n_acc;
         }
         if (!ok) {

@@ -188,10 +188,8 @@ __device__ __forceinline__ float tc_ex2(float x) {
 __device__ __forceinline__ void tc_add2(float &a, float &b, float x, float y) {   // a += x, b += y
     asm("{\n.reg .b64 s, t;\nmov.b64 s, {%0, %1};\nmov.b64 t, {%2, %3};\nadd.rn.f32x2 s, s, t;\nmov.b64 {%0, %1}, s;\n}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
 }
-__device__ __forceinline__ void tc_fma2(float &a, float &b, float x, float y) {   // a = a * x + y, b = b * x + y
-    asm("{\n.reg .b64 s, t, u;\nmov.b64 s, {%0, %1};\nmov.b64 t, {%2, %2};\nmov.b64 u, {%3, %3};\nfma.rn.f32x2 s, s, t, u;\nmov.b64 {%0, %1}, s;\n}"
-        : "+f"(a), "+f"(b)
-        : "f"(x), "f"(y));
+__device__ __forceinline__ void tc_mul2(float &a, float &b, float x) {   // a *= x, b *= x
+    asm("{\n.reg .b64 s, t;\nmov.b64 s, {%0, %1};\nmov.b64 t, {%2, %2};\nmul.rn.f32x2 s, s, t;\nmov.b64 {%0, %1}, s;\n}" : "+f"(a), "+f"(b) : "f"(x));
 }
 __device__ __forceinline__ float tc_max3(float a, float b, float c) {
     float d;
