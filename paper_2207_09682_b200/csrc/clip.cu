@@ -2,7 +2,7 @@
 //
 //   norm = sqrt(sum over tensors and elements of g^2),   out = g * min(1, max_norm / norm)
 //
-// Two launches: the first takes the sum of squares (one double per block; the block that ends last adds
+// Two launches (one for up to 32 chunks): the first takes the sum of squares (one double per block; the block that ends last adds
 // the blocks' sums in their order and works out the factor), the second multiplies.  Bound by memory
 // traffic: every tensor is read once, and read and written once more when the norm is above max_norm.
 //
@@ -125,6 +125,15 @@ struct ClipFactor {
     int scale;      // 0: the tensors keep their values
 };
 
+// From the sum of squares; the norm goes to *d_norm (unless NULL).
+__device__ __forceinline__ ClipFactor factor_of(double s, double max_norm, float *d_norm) {
+    const double norm = sqrt(s);
+    if (d_norm) *d_norm = (float)norm;
+    // false also for a norm that is not finite: the tensors keep their values then
+    const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
+    return ClipFactor{clip ? (float)(max_norm / norm) : 1.0f, clip};
+}
+
 // n_before: sums of earlier launches of the same call; the last launch (`final`) adds them all.
 template <int CAP>
 __global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(const __grid_constant__ ClipTable<CAP> t, double *partial, int n_before,
@@ -158,12 +167,7 @@ __global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(cons
     for (int k = threadIdx.x; k < n_before + (int)gridDim.x; k += CLIP_THREADS) s += *(volatile double *)&partial[k];
     s = block_sum(s);
     if (threadIdx.x == 0) {
-        const double norm = sqrt(s);
-        // false also for a norm that is not finite: the tensors keep their values then
-        const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
-        factor->coef = clip ? (float)(max_norm / norm) : 1.0f;
-        factor->scale = clip;
-        *d_norm = (float)norm;
+        *factor = factor_of(s, max_norm, d_norm);
         *arrived = 0;
     }
 }
@@ -220,6 +224,50 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_consta
     }
 }
 
+// Few chunks: one launch.  A cluster of eight blocks, each with every eighth chunk; the blocks' sums are exchanged
+// through the cluster's shared memory.
+constexpr int CLIP_CLUSTER = 8, CLIP_FEW_CHUNKS = 32;
+
+__global__ void __cluster_dims__(CLIP_CLUSTER) __launch_bounds__(CLIP_THREADS)
+    k_clip_few(const __grid_constant__ ClipTable<CLIP_SMALL> t, const __grid_constant__ ClipOut<CLIP_SMALL> o, double max_norm, bool in_place,
+               float *d_norm) {
+    qg_after_prior();
+    __shared__ double mine;
+    double s = 0.0;
+    for (int c = blockIdx.x; c < t.chunks; c += CLIP_CLUSTER) {
+        const int i = find_tensor(t, c);
+        const long long count = t.count[i] & ((1ll << 56) - 1);
+        const int type = (int)(t.count[i] >> 56);
+        const ChunkRange r = chunk_range(t.in[i], type == QGBDT_F32 ? 4 : 2, count, c - t.first[i]);
+        if (type == QGBDT_F32) s += sum_squares(reinterpret_cast<const float *>(t.in[i]), r);
+        else if (type == QGBDT_BF16) s += sum_squares(reinterpret_cast<const __nv_bfloat16 *>(t.in[i]), r);
+        else s += sum_squares(reinterpret_cast<const __half *>(t.in[i]), r);
+    }
+    s = block_sum(s);
+    if (threadIdx.x == 0) mine = s;
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    s = 0.0;
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(&mine);
+#pragma unroll
+    for (uint32_t k = 0; k < CLIP_CLUSTER; ++k) {
+        double x;
+        asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %1, %2;\nld.shared::cluster.f64 %0, [a];\n}" : "=d"(x) : "r"(at), "r"(k) : "memory");
+        s += x;
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");   // before any block ends
+    const ClipFactor f = factor_of(s, max_norm, blockIdx.x == 0 && threadIdx.x == 0 ? d_norm : nullptr);
+    if (!f.scale && in_place) return;
+    for (int c = blockIdx.x; c < t.chunks; c += CLIP_CLUSTER) {
+        const int i = find_tensor(t, c);
+        const long long count = t.count[i] & ((1ll << 56) - 1);
+        const int type = (int)(t.count[i] >> 56);
+        const ChunkRange r = chunk_range(t.in[i], type == QGBDT_F32 ? 4 : 2, count, c - t.first[i]);
+        if (type == QGBDT_F32) scale_chunk(reinterpret_cast<const float *>(t.in[i]), reinterpret_cast<float *>(o.out[i]), r, f.coef);
+        else if (type == QGBDT_BF16) scale_chunk(reinterpret_cast<const __nv_bfloat16 *>(t.in[i]), reinterpret_cast<__nv_bfloat16 *>(o.out[i]), r, f.coef);
+        else scale_chunk(reinterpret_cast<const __half *>(t.in[i]), reinterpret_cast<__half *>(o.out[i]), r, f.coef);
+    }
+}
+
 template <int CAP>
 int fill(ClipTable<CAP> &t, ClipOut<CAP> &o, const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, int32_t &at,
          int32_t n) {
@@ -254,6 +302,13 @@ int clip_groups(qgbdt_ctx *c, const void *const *in, void *const *out, const int
                 float *d_norm, double *partial, cudaStream_t st) {
     ClipTable<CAP> t;
     ClipOut<CAP> o;
+    bool in_place = true;
+    for (int32_t i = 0; i < n; ++i) in_place = in_place && (in[i] == out[i] || counts[i] == 0);
+    if constexpr (CAP == CLIP_SMALL) {
+        int32_t at = 0;
+        if (fill(t, o, in, out, counts, types, at, n) != 0) return qg_fail(c, QGBDT_ERR_ARG, "a tensor is too large");
+        if (at >= n && t.chunks <= CLIP_FEW_CHUNKS) return qg_launch(c, k_clip_few, dim3(CLIP_CLUSTER), CLIP_THREADS, 0, st, t, o, max_norm, in_place, d_norm);
+    }
     ClipFactor *factor = reinterpret_cast<ClipFactor *>(partial);   // in front of the sums
     partial += 16;
     int n_partial = 0;
@@ -265,8 +320,6 @@ int clip_groups(qgbdt_ctx *c, const void *const *in, void *const *out, const int
                          d_norm));
         n_partial += grid;
     } while (at < n);
-    bool in_place = true;
-    for (int32_t i = 0; i < n; ++i) in_place = in_place && (in[i] == out[i] || counts[i] == 0);
     if (in_place && max_norm > 1.7976931348623157e308) return QGBDT_OK;   // the norm alone
     at = 0;
     do {

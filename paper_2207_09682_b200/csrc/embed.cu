@@ -629,6 +629,74 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
     }
 }
 
+// ---- few pairs and few entries: no sorting -----------------------------------------------------------
+// Every warp takes entries in turn, looks all tokens over for it (32 at a time), lists the rows of those it finds and
+// adds them, eight in flight, in their order.  One launch instead of three; worth it while entries * pairs stays small.
+
+constexpr int SCAN_PAIRS = 4096;
+constexpr long long SCAN_WORK = 1ll << 22;   // entries * pairs
+
+template <typename T, int V, typename I>
+__global__ void __launch_bounds__(EMB_THREADS) k_scan_sum(const SortArgs a, const SegArgs g) {
+    qg_after_prior();
+    using Vec = OpsVec<T, V>;
+    constexpr int LIST = 128;
+    __shared__ unsigned key[SCAN_PAIRS];
+    __shared__ unsigned lists[EMB_THREADS / 32][LIST];
+    unsigned *list = lists[threadIdx.x / 32];
+    const int n = (int)a.n, n32 = (n + 31) / 32 * 32, lane = threadIdx.x & 31;
+    const I *tokens = reinterpret_cast<const I *>(a.tokens);
+    bool bad = false;
+    for (int i = threadIdx.x; i < n32; i += EMB_THREADS * 4) {
+        unsigned t[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) t[u] = token_at(tokens, token_index(a, min(i + u * EMB_THREADS, n - 1)));
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (i + u * EMB_THREADS < n32) key[i + u * EMB_THREADS] = i + u * EMB_THREADS < n ? token_key(a, t[u], bad) : (unsigned)a.n_entries;
+    }
+    if (bad && a.status) *a.status = 1;
+    __syncthreads();
+    const unsigned ld_bytes = (unsigned)(g.ld * sizeof(T));
+    const int warps = gridDim.x * (EMB_THREADS / 32);
+    for (int v = blockIdx.x * (EMB_THREADS / 32) + threadIdx.x / 32; v < (int)g.n_entries; v += warps)
+        for (int c0 = 0; c0 < g.dim; c0 += 32 * V) {
+            const int col = c0 + lane * V;
+            const T *grad = reinterpret_cast<const T *>(g.grad) + (col < g.dim ? col : 0);
+            float acc[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) acc[j] = 0.0f;
+            int listed = 0;
+            auto add_listed = [&]() {
+                __syncwarp();
+                for (int k = 0; k < listed; k += EMB_UNROLL) {
+                    Vec x[EMB_UNROLL];
+#pragma unroll
+                    for (int u = 0; u < EMB_UNROLL; ++u) x[u] = row_of<T, V>(grad, list[min(k + u, listed - 1)], ld_bytes);
+#pragma unroll
+                    for (int u = 0; u < EMB_UNROLL; ++u)
+                        if (k + u < listed) add_row(acc, x[u]);
+                }
+                __syncwarp();
+                listed = 0;
+            };
+            for (int i = 0; i < n32; i += 32) {
+                const bool hit = key[i + lane] == (unsigned)v;
+                const unsigned m = __ballot_sync(0xffffffffu, hit);
+                if (hit) list[listed + __popc(m & ((1u << lane) - 1))] = div_bag(a, (unsigned)(i + lane));
+                listed += __popc(m);
+                if (listed > LIST - 32) add_listed();
+            }
+            if (listed > 0) add_listed();
+            if (col < g.dim) {
+                Vec y;
+#pragma unroll
+                for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(acc[j] * g.scale);
+                *reinterpret_cast<Vec *>(reinterpret_cast<T *>(g.out) + (long long)v * g.ld_out + col) = y;
+            }
+        }
+}
+
 // ---- launches --------------------------------------------------------------------------------------
 
 int log2_at_least(long long v, int most) {   // smallest l <= most with 2^l >= v
@@ -726,6 +794,12 @@ int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     return QGBDT_OK;
 }
 
+template <typename T, int V>
+int scan_typed(qgbdt_ctx *c, const SortArgs &a, const SegArgs &g, bool wide, cudaStream_t st) {
+    const long long want = (g.n_entries + EMB_THREADS / 32 - 1) / (EMB_THREADS / 32), most = c->sm_count * 6;
+    return qg_launch(c, wide ? k_scan_sum<T, V, int64_t> : k_scan_sum<T, V, int32_t>, dim3((unsigned)(want < most ? want : most)), EMB_THREADS, 0, st, a, g);
+}
+
 // Calls f<T, V>() for the element type and the vector width in bytes.
 #define EMBED_DISPATCH(type, vb, CALL)                                                ((type) == QGBDT_F32 ? ((vb) == 16 ? CALL(float, 4) : (vb) == 8 ? CALL(float, 2) : CALL(float, 1))                            : (type) == QGBDT_BF16                                                                                                           ? ((vb) == 16 ? CALL(__nv_bfloat16, 8) : (vb) == 8 ? CALL(__nv_bfloat16, 4) : (vb) == 4 ? CALL(__nv_bfloat16, 2) : CALL(__nv_bfloat16, 1))          : ((vb) == 16 ? CALL(__half, 8) : (vb) == 8 ? CALL(__half, 4) : (vb) == 4 ? CALL(__half, 2) : CALL(__half, 1)))
 
@@ -745,6 +819,13 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.n = n;
     s.grad = a.table, s.ld = a.ld, s.out = a.out, s.ld_out = a.ld_out, s.n_entries = a.n_entries;
     s.dim = a.dim, s.scale = a.scale;
+    SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, 0, 0, 0, a.status};
+    set_divisor(sa, (unsigned)a.bag);
+    if (n > 0 && n <= SCAN_PAIRS && n * a.n_entries <= SCAN_WORK) {
+#define CALL(T, V) scan_typed<T, V>(c, sa, s, a.token_type == QGBDT_I64, st)
+        return EMBED_DISPATCH(a.type, vb, CALL);
+#undef CALL
+    }
     s.lg = log2_at_least((a.dim + V - 1) / V, 5);
     s.col_blocks = (a.dim + (V << s.lg) - 1) / (V << s.lg);
     // tiles: short lists go once over the groups that fit on the SMs together (768 threads each), long ones four times,
@@ -767,8 +848,6 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.partial = ws.take<float>((size_t)s.tiles * 2 * a.dim);
     s.pair = buf0;
     if (n > 0) {
-        SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, 0, 0, 0, a.status};
-        set_divisor(sa, (unsigned)a.bag);
         rc = a.token_type == QGBDT_I64 ? sort_pairs<int64_t>(c, sa, sp, buf0, buf1, counts, totals, &s.pair, st)
                                        : sort_pairs<int32_t>(c, sa, sp, buf0, buf1, counts, totals, &s.pair, st);
         if (rc != QGBDT_OK) return rc;

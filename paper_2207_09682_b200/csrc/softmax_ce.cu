@@ -695,7 +695,8 @@ struct FewArgs {
     int label_type;
     float2 *stat;                  // [rows][gridDim.x]
     float *z_label;
-    int *count, *pos_of;
+    unsigned *arrived;
+    float *loss, *losses, *lse;
     int *status;
 };
 
@@ -711,12 +712,8 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, FEW_BLOCKS) k_loss_few(const F
         if (r < a.rows) l = a.label_type == QGBDT_I64 ? reinterpret_cast<const long long *>(a.labels)[r] : (long long)reinterpret_cast<const int *>(a.labels)[r];
         label[r] = l >= 0 && l < a.classes ? (int)l : -1;
         rows += label[r] >= 0;
-        if (blockIdx.x == 0 && threadIdx.x == 0 && r < a.rows) {
-            a.pos_of[r] = label[r] >= 0 ? r : -1;
-            if (l >= a.classes && a.status) *a.status = 1;
-        }
+        if (blockIdx.x == 0 && threadIdx.x == 0 && l >= a.classes && a.status) *a.status = 1;
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.count = rows;
     float m[R], l[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) m[r] = -INFINITY, l[r] = 0.0f;
@@ -782,6 +779,36 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, FEW_BLOCKS) k_loss_few(const F
         float2 s = part[0][threadIdx.x];
         for (int w = 1; w < FEW_WARPS; ++w) join(s.x, s.y, part[w][threadIdx.x].x, part[w][threadIdx.x].y);
         a.stat[threadIdx.x * gridDim.x + blockIdx.x] = s;
+    }
+    // the block that comes last joins the blocks' statistics, a warp per row
+    __shared__ bool last;
+    __shared__ float row_loss[R];
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(a.arrived, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (warp < R && warp < a.rows) {
+        float m0 = -INFINITY, l0 = 0.0f;
+        const volatile float2 *q = a.stat + warp * gridDim.x;
+        for (int t = lane; t < (int)gridDim.x; t += 32) join(m0, l0, q[t].x, q[t].y);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) join(m0, l0, __shfl_xor_sync(0xffffffffu, m0, o), __shfl_xor_sync(0xffffffffu, l0, o));
+        if (lane == 0) {
+            const bool labelled = (R == 1 || warp == 0 ? label[0] : label[R - 1]) >= 0;
+            const float lse = labelled ? m0 + logf(l0) : 0.0f, loss = labelled ? lse - *(volatile float *)&a.z_label[warp] : 0.0f;
+            a.lse[warp] = lse;
+            if (a.losses) a.losses[warp] = loss;
+            row_loss[warp] = loss;
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double sum = 0.0;
+        for (int r = 0; r < a.rows; ++r) sum += (double)row_loss[r];
+        *a.loss = (float)(sum / (double)(rows > 0 ? rows : 1));
+        *a.arrived = 0;
     }
 }
 
@@ -1118,20 +1145,17 @@ static int loss_few(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
     const long long most = c->sm_count * FEW_BLOCKS, want = (a.classes + FEW_WARPS * FEW_CLASSES - 1) / (FEW_WARPS * FEW_CLASSES);
     const int blocks = (int)(want < most ? want : most);
     QgWorkspace ws;
-    QG_RUN(qg_ws_open(c, qg_ws_size((size_t)FEW_ROWS * blocks, 8) + 4 * 256, st, &ws));
+    QG_RUN(qg_ws_open(c, qg_ws_size((size_t)FEW_ROWS * blocks, 8) + 256, st, &ws));
     FewArgs f{};
     f.hidden = reinterpret_cast<const uint16_t *>(a.hidden), f.weight = reinterpret_cast<const uint16_t *>(a.weight);
     f.ld_hidden = a.ld_hidden, f.ld_weight = a.ld_weight, f.rows = (int)a.rows, f.classes = (int)a.classes, f.dim = a.dim;
     f.bias = a.bias, f.labels = a.labels, f.label_type = a.label_type, f.status = a.status;
-    f.stat = ws.take<float2>((size_t)FEW_ROWS * blocks);
-    f.z_label = ws.take<float>(FEW_ROWS), f.count = ws.take<int>(1), f.pos_of = ws.take<int>(FEW_ROWS);
-    double *block_loss = ws.take<double>(1);
+    f.stat = ws.take<float2>((size_t)FEW_ROWS * blocks), f.z_label = ws.take<float>(FEW_ROWS);
+    f.arrived = c->d_ops_counters, f.loss = a.loss, f.losses = a.losses, f.lse = a.lse;
     const bool bf16 = a.type == QGBDT_BF16;
     const auto kernel = a.rows == 1 ? (bf16 ? k_loss_few<__nv_bfloat16, 1> : k_loss_few<__half, 1>)
                                     : (bf16 ? k_loss_few<__nv_bfloat16, 2> : k_loss_few<__half, 2>);
     QG_RUN(qg_launch(c, kernel, dim3(blocks), FEW_WARPS * 32, 0, st, f));
-    QG_RUN(qg_launch(c, k_loss_join, dim3(1), JOIN_THREADS, 0, st, f.stat, blocks, f.z_label, f.pos_of, f.rows, 5, f.count, a.losses, a.lse, block_loss,
-                     c->d_ops_counters, a.loss));
     return qg_ws_close(c, st);
 }
 
