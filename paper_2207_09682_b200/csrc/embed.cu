@@ -237,6 +237,9 @@ constexpr int SORT_WARPS = EMB_THREADS / 32;
 constexpr int SORT_ROUNDS = 8;                                    // pairs per lane and tile
 constexpr int SORT_TILE = EMB_THREADS * SORT_ROUNDS;
 
+// Counts of a digit, one per block, padded to 16 bytes.
+__host__ __device__ inline size_t count_stride(int blocks) { return ((size_t)blocks + 3) / 4 * 4; }
+
 template <typename I, bool FIRST>
 __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const uint2 *in, int shift, int bits, long long per_block,
                                                             unsigned *counts) {
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, co
         if (FIRST && bad && a.status) *a.status = 1;
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += EMB_THREADS) counts[(size_t)d * gridDim.x + blockIdx.x] = cnt[d];
+    for (int d = threadIdx.x; d < digits; d += EMB_THREADS) counts[(size_t)d * count_stride(gridDim.x) + blockIdx.x] = cnt[d];
 }
 
 // Per digit (one warp): exclusive scan over the blocks, and the digit's total.
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_scan(unsigned *counts, uns
     qg_after_prior();
     const int d = blockIdx.x * SORT_WARPS + threadIdx.x / 32, lane = threadIdx.x & 31;
     if (d >= digits) return;
-    unsigned *row = counts + (size_t)d * blocks, run = 0;
+    unsigned *row = counts + (size_t)d * count_stride(blocks), run = 0;
     for (int b = 0; b < blocks; b += 32 * 8) {
         unsigned x[8];
 #pragma unroll
@@ -309,6 +312,10 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
     return run;
 }
 
+// totals == NULL: the counts have not been scanned; with few blocks every block adds up what it needs itself, which
+// takes less time than a launch for it.
+constexpr int SORT_FEW_BLOCKS = 128;
+
 template <typename I, bool FIRST, int BITS>
 __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, long long per_block, const unsigned *counts,
                                                               const unsigned *totals, uint2 *out) {
@@ -323,12 +330,35 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
     unsigned short *cnt = reinterpret_cast<unsigned short *>(begin + digits);   // [SORT_WARPS][digits] pairs of a warp, then those of earlier warps
     const int per = (digits + EMB_THREADS - 1) / EMB_THREADS, d0 = threadIdx.x * per;   // digits of this thread in the scans
     {   // base = pairs of smaller digits (scan of the totals) + pairs of this digit in earlier blocks
+        const int blocks = gridDim.x, mine = blockIdx.x;
+        const size_t stride = count_stride(blocks);
         unsigned s = 0;
-        for (int j = 0; j < per && d0 + j < digits; ++j) s += totals[d0 + j];
+        for (int j = 0; j < per && d0 + j < digits; ++j) {
+            unsigned total = 0, before = 0;
+            if (totals) {
+                total = totals[d0 + j];
+                before = counts[(d0 + j) * stride + mine];
+            } else {
+                const uint4 *row = reinterpret_cast<const uint4 *>(counts + (d0 + j) * stride);
+#pragma unroll 8
+                for (int b = 0; b < blocks; b += 4) {
+                    const uint4 x = row[b / 4];
+                    const unsigned y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        total += b + k < blocks ? y[k] : 0;
+                        before += b + k < mine ? y[k] : 0;
+                    }
+                }
+            }
+            begin[d0 + j] = total;
+            base[d0 + j] = before;
+            s += total;
+        }
         unsigned run = block_scan(s, warp_sum);
         for (int j = 0; j < per && d0 + j < digits; ++j) {
-            base[d0 + j] = run + counts[(size_t)(d0 + j) * gridDim.x + blockIdx.x];
-            run += totals[d0 + j];
+            base[d0 + j] += run;
+            run += begin[d0 + j];
         }
     }
     const long long i0 = per_block * blockIdx.x, i1 = i0 + per_block < a.n ? i0 + per_block : a.n;
@@ -764,12 +794,13 @@ int sort_pairs(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, uint2 *buf0, 
         const int shift = k * s.bits;
         QG_RUN(qg_launch(c, k == 0 ? k_sort_count<I, true> : k_sort_count<I, false>, dim3(s.blocks), EMB_THREADS, count_smem, st, a, in, shift, s.bits,
                          s.per_block, counts));
-        QG_RUN(qg_launch(c, k_sort_scan, dim3((digits + SORT_WARPS - 1) / SORT_WARPS), EMB_THREADS, 0, st, counts, totals, digits, s.blocks));
+        const bool scan = s.blocks > SORT_FEW_BLOCKS;
+        if (scan) QG_RUN(qg_launch(c, k_sort_scan, dim3((digits + SORT_WARPS - 1) / SORT_WARPS), EMB_THREADS, 0, st, counts, totals, digits, s.blocks));
         const auto scatter = s.bits == 6 ? (k == 0 ? k_sort_scatter<I, true, 6> : k_sort_scatter<I, false, 6>)
                              : s.bits == 7 ? (k == 0 ? k_sort_scatter<I, true, 7> : k_sort_scatter<I, false, 7>)
                              : s.bits == 8 ? (k == 0 ? k_sort_scatter<I, true, 8> : k_sort_scatter<I, false, 8>)
                                            : (k == 0 ? k_sort_scatter<I, true, 9> : k_sort_scatter<I, false, 9>);
-        QG_RUN(qg_launch(c, scatter, dim3(s.blocks), EMB_THREADS, smem, st, a, in, shift, s.per_block, counts, totals, out));
+        QG_RUN(qg_launch(c, scatter, dim3(s.blocks), EMB_THREADS, smem, st, a, in, shift, s.per_block, counts, scan ? totals : nullptr, out));
         uint2 *swap = in;
         in = out;
         out = swap;
@@ -838,13 +869,13 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     const bool small = n <= SORT_SMALL;
     const SortPlan sp = small ? SortPlan{} : sort_plan(c, n, a.n_entries);
     const size_t digits = small ? 0 : (size_t)1 << sp.bits;
-    const size_t bytes = 2 * qg_ws_size((size_t)n + 2 * EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * (sp.blocks + 1), sizeof(unsigned)) +
+    const size_t bytes = 2 * qg_ws_size((size_t)n + 2 * EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * count_stride(sp.blocks), sizeof(unsigned)) +
                          qg_ws_size(digits, sizeof(unsigned)) + qg_ws_size((size_t)s.tiles * 2 * a.dim, sizeof(float));
     QgWorkspace ws;
     int rc = qg_ws_open(c, bytes, st, &ws);
     if (rc != QGBDT_OK) return rc;
     uint2 *buf0 = ws.take<uint2>((size_t)n + 2 * EMB_UNROLL), *buf1 = ws.take<uint2>((size_t)n + 2 * EMB_UNROLL);
-    unsigned *counts = ws.take<unsigned>(digits * sp.blocks), *totals = ws.take<unsigned>(digits);
+    unsigned *counts = ws.take<unsigned>(digits * count_stride(sp.blocks)), *totals = ws.take<unsigned>(digits);
     s.partial = ws.take<float>((size_t)s.tiles * 2 * a.dim);
     s.pair = buf0;
     if (n > 0) {
