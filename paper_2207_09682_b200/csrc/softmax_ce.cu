@@ -34,15 +34,21 @@ constexpr int CG = 2;                       // CTAs per tile: a pair halves what
 constexpr int BM = 128 * CG, BN = 256, BK = 64;
 constexpr int A_BYTES = 128 * BK * 2, B_ROWS = BN / CG, B_BYTES = B_ROWS * BK * 2;
 constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-constexpr int STAGES = 196608 / STAGE_BYTES;
 constexpr int EPI_WARPS = 8, THREADS = 128 + EPI_WARPS * 32;
-constexpr int STORE_BYTES = 32 * 128;       // staging of a warp: 32 rows of 128 bytes
-constexpr int SMEM_BYTES = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * STORE_BYTES;
+constexpr int STORE_BYTES = 32 * 128;       // staging buffer of a warp: 32 rows of 128 bytes
 constexpr int TMEM_COLS = 512, ACC_COLS = 256;
 constexpr int GROUP_M = 16;                 // row tiles that go through all column tiles together
 constexpr float LOG2E = 1.44269504088896340736f;
 
 enum Mode { LOSS, GRAD, DH, DW };
+
+// Shared memory: a ring of operand tiles and the warps' staging buffers.  GRAD stages every tile it makes, so it has two
+// buffers per warp and one operand tile less (8192 rows x 16384 classes x 64: 94 us with one, 82 us with two).
+template <int MODE>
+struct Layout {
+    static constexpr int BUFFERS = MODE == GRAD ? 2 : 1, STAGES = MODE == GRAD ? 5 : 6;
+    static constexpr int BYTES = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * BUFFERS * STORE_BYTES;
+};
 
 // The caller's labels.
 struct RawLabels {
@@ -305,38 +311,51 @@ struct Epilogue {
         if (live) a.stat[((long long)row * a.n_tiles + c.n) * 2 + half] = make_float2(top, ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
     }
 
-    // 32 columns: chunk cc of the warp's four.
+    // GRAD: 64 columns, left or right half of the warp's.
+    __device__ __forceinline__ void gradients(float (&x)[64], int h) {
+        const int col = col0 + h * 64, v = a.v0 + col, lj = label - v;
+        const bool mine = lj >= 0 && lj < 64;
+        logits(x, v);
+        exponentials(x, lse);
+        if (__any_sync(0xffffffffu, mine)) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j)
+                if (lj == j) x[j] -= 1.0f;
+        }
+        if (row_in + 32 > count) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) x[j] = live ? x[j] : 0.0f;
+        }
+        const uint32_t to = buf + h * STORE_BYTES;
+        if (lane == 0) tc_store_wait_read<1>();   // the copy out of this buffer has been read
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            stage16(to, lane, i, pack2(x[8 * i], x[8 * i + 1], a.bf16), pack2(x[8 * i + 2], x[8 * i + 3], a.bf16), pack2(x[8 * i + 4], x[8 * i + 5], a.bf16),
+                    pack2(x[8 * i + 6], x[8 * i + 7], a.bf16));
+        stage_close();
+        if (lane == 0) {
+            tc_store_2d(map_out, col, row_in, to);
+            tc_store_commit();
+        }
+        if (a.bias_part) {
+            float *sums = a.bias_part + (long long)(row_in / 32) * (a.n_tiles * BN) + col + lane;
+#pragma unroll
+            for (int k = 0; k < 64; k += 32) {
+                float y[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) y[j] = x[k + j];
+                sums[k] = column_sums(y, lane);
+            }
+        }
+    }
+
+    // DH and DW: 32 columns, chunk cc of the warp's four.
     __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int cc) {
         float x[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
         const int col = col0 + cc * 32;
-        if (MODE == GRAD) {
-            const int v = a.v0 + col, lj = label - v;
-            const bool mine = lj >= 0 && lj < 32;
-            logits(x, v);
-            exponentials(x, lse);
-            if (__any_sync(0xffffffffu, mine)) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (lj == j) x[j] -= 1.0f;
-            }
-            if (row_in + 32 > count) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) x[j] = live ? x[j] : 0.0f;
-            }
-            if ((cc & 1) == 0) stage_open();
-            stage_half(x, cc & 1);
-            if (cc & 1) {
-                stage_close();
-                if (lane == 0) {
-                    tc_store_2d(map_out, col - 32, row_in, buf);
-                    tc_store_commit();
-                }
-            }
-            if (a.bias_part) a.bias_part[(long long)(row_in / 32) * (a.n_tiles * BN) + col + lane] = column_sums(x, lane);
-            return;
-        }
         if (MODE == DW && c.whole) {
             const int v_in = a.v0 + row_in;
             if ((cc & 1) == 0) stage_open();
@@ -386,6 +405,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                                                              const __grid_constant__ CUtensorMap map_part) {
     constexpr bool A_MN = MODE == DW, B_MN = MODE == DH || MODE == DW;   // operand rows run along the products' length
     extern __shared__ char smem_raw[];
+    constexpr int STAGES = Layout<MODE>::STAGES;
     __shared__ alignas(8) unsigned long long bars[2 * STAGES + 4 + 1];
     __shared__ uint32_t tmem_base;
     __shared__ int stop;
@@ -491,7 +511,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
     } else if (warp >= 4) {
         // ---- epilogue: thread = row of the tile, half of the columns per warp
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        Epilogue<MODE> epi(a, &map_out, &map_part, store_at + (warp - 4) * STORE_BYTES, lane, count);
+        Epilogue<MODE> epi(a, &map_out, &map_part, store_at + (warp - 4) * Layout<MODE>::BUFFERS * STORE_BYTES, lane, count);
         int n_acc = 0;
         while (todo.next(c)) {
             const int b = n_acc & 1;
@@ -517,6 +537,25 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                 }
                 hand_back();
                 epi.row_statistics(x, half);
+            } else if constexpr (MODE == GRAD) {
+                uint32_t r[4][32];
+                tc_ld_32(tacc, r[0]);
+                tc_ld_32(tacc + 32, r[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    tc_ld_wait(r[2 * h]);
+                    tc_ld_wait(r[2 * h + 1]);
+                    if (h == 0) {   // read under the arithmetic of the first half
+                        tc_ld_32(tacc + 64, r[2]);
+                        tc_ld_32(tacc + 96, r[3]);
+                    } else {
+                        hand_back();
+                    }
+                    float x[64];
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) x[j] = __uint_as_float(r[2 * h + j / 32][j % 32]);
+                    epi.gradients(x, h);
+                }
             } else {
                 if (half * 128 < c.cols) {   // a narrow tile has nothing for the second half
                     uint32_t r[2][32];
@@ -1050,13 +1089,13 @@ template <int MODE>
 int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mo, const CUtensorMap &mp,
          cudaStream_t st) {
     if (!(c->ops_configured >> MODE & 1)) {
-        QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES));
+        QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MODE>::BYTES));
         c->ops_configured |= 1u << MODE;
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)units * CG);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.dynamicSmemBytes = Layout<MODE>::BYTES;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
