@@ -33,7 +33,6 @@ namespace {
 constexpr int CG = 2;                       // CTAs per tile: a pair halves what each SM loads of the second operand
 constexpr int BM = 128 * CG, BN = 256, BK = 64;
 constexpr int A_BYTES = 128 * BK * 2, B_ROWS = BN / CG, B_BYTES = B_ROWS * BK * 2;
-constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int EPI_WARPS = 8, THREADS = 128 + EPI_WARPS * 32;
 constexpr int STORE_BYTES = 32 * 128;       // staging buffer of a warp: 32 rows of 128 bytes
 constexpr int TMEM_COLS = 512, ACC_COLS = 256;
@@ -42,11 +41,17 @@ constexpr float LOG2E = 1.44269504088896340736f;
 
 enum Mode { LOSS, GRAD, DH, DW };
 
+// NB: accumulators of 256 columns that a tile has.  One: tensor memory holds two tiles, and a tile's epilogue runs
+// under the products of the next.  Two (DH and DW with long products): a tile of 512 columns fills tensor memory, the
+// epilogue has nothing to run under, but a quarter less comes out of L2 per product, which is what bounds the products
+// of 256 columns (32 KB per block of 64 and SM, 12 TB/s).
+//
 // Shared memory: a ring of operand tiles and the warps' staging buffers.  GRAD stages every tile it makes, so it has two
 // buffers per warp and one operand tile less (8192 rows x 16384 classes x 64: 94 us with one, 82 us with two).
-template <int MODE>
+template <int MODE, int NB>
 struct Layout {
-    static constexpr int BUFFERS = MODE == GRAD ? 2 : 1, STAGES = MODE == GRAD ? 5 : 6;
+    static constexpr int BUFFERS = MODE == GRAD ? 2 : 1, STAGES = NB == 2 ? 4 : MODE == GRAD ? 5 : 6;
+    static constexpr int STAGE_BYTES = A_BYTES + NB * B_BYTES, ACCS = NB == 2 ? 1 : 2;
     static constexpr int BYTES = 1024 + STAGES * STAGE_BYTES + EPI_WARPS * BUFFERS * STORE_BYTES;
 };
 
@@ -130,11 +135,11 @@ struct Line {
 // What a unit works on next.
 struct Work {
     int m, n, kb0, kb1;
-    int cols;            // columns of the tile: 256, or 128 where no more are left (DH, DW)
+    int cols;            // columns of the tile; the last ones of DH and DW are cut to a multiple of 128
     int fragment;        // DH, and DW where the tile is not whole: which part buffer
     bool whole;
 };
-template <int MODE>
+template <int MODE, int NB>
 struct Schedule {
     int t, step, total, m_live, n_tiles, dim, kb, unit, gang, member, size;
     long long pos, end;
@@ -167,7 +172,7 @@ struct Schedule {
                 w.kb0 = (int)(pos - (long long)place * kb);
                 w.kb1 = (int)min((long long)kb, w.kb0 + end - pos);
                 w.whole = w.kb0 == 0 && w.kb1 == kb;
-                w.cols = dim - w.n * BN > BN / 2 ? BN : BN / 2;
+                w.cols = min(BN * NB, (dim - w.n * BN * NB + 127) / 128 * 128);
                 w.fragment = MODE == DH ? (place + gang) * size + member : 2 * unit + (w.kb0 == 0);
                 pos += w.kb1 - w.kb0;
                 if (w.n < n_tiles) return true;   // the last round may have fewer column tiles than the gang units
@@ -207,7 +212,7 @@ __device__ __forceinline__ void stage16(uint32_t buf, int lane, int chunk, uint3
                  : "memory");
 }
 
-template <int MODE>
+template <int MODE, int NB>
 struct Epilogue {
     const GemmArgs &a;
     const CUtensorMap *map_out, *map_part;
@@ -215,7 +220,7 @@ struct Epilogue {
     int lane, count;
     Work c;
     int row_in, row;       // the warp's first row, this thread's
-    int col0;              // first of the warp's 128 columns
+    int col0;              // first of the warp's columns (128, with two accumulators 256)
     bool live;
     int label;
     float lse, scale;
@@ -229,7 +234,7 @@ struct Epilogue {
         c = w;
         row_in = w.m * BM + rank * 128 + quarter * 32;
         row = row_in + lane;
-        col0 = w.n * BN + half * 128;
+        col0 = w.n * BN * NB + half * (BN * NB / 2);
         live = row < count;
         if (MODE == LOSS || MODE == GRAD) label = !live ? -1 : a.label ? a.label[row] : a.labels[row];
         if (MODE == GRAD) lse = live ? a.lse[row] : 0.0f;
@@ -350,12 +355,12 @@ struct Epilogue {
         }
     }
 
-    // DH and DW: 32 columns, chunk cc of the warp's four.
-    __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int cc) {
+    // DH and DW: 32 columns, chunk cc of four from column c0 of the warp's on.
+    __device__ __forceinline__ void chunk(const uint32_t (&r)[32], int c0, int cc) {
         float x[32];
 #pragma unroll
         for (int j = 0; j < 32; ++j) x[j] = __uint_as_float(r[j]);
-        const int col = col0 + cc * 32;
+        const int col = col0 + c0 + cc * 32;
         if (MODE == DW && c.whole) {
             const int v_in = a.v0 + row_in;
             if ((cc & 1) == 0) stage_open();
@@ -390,7 +395,7 @@ struct Epilogue {
             stage16(buf, lane, i, __float_as_uint(x[4 * i]), __float_as_uint(x[4 * i + 1]), __float_as_uint(x[4 * i + 2]), __float_as_uint(x[4 * i + 3]));
         stage_close();
         if (lane == 0) {
-            const int y = c.fragment * BM + row_in - c.m * BM, xx = col - c.n * BN;
+            const int y = c.fragment * BM + row_in - c.m * BM, xx = col - c.n * BN * NB;
             if (MODE == DH && a.add) tc_add_2d(map_part, xx, y, buf);
             else tc_store_2d(map_part, xx, y, buf);
             tc_store_commit();
@@ -398,14 +403,14 @@ struct Epilogue {
     }
 };
 
-template <int MODE>
+template <int MODE, int NB>
 __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, const __grid_constant__ CUtensorMap map_a,
                                                              const __grid_constant__ CUtensorMap map_b,
                                                              const __grid_constant__ CUtensorMap map_out,
                                                              const __grid_constant__ CUtensorMap map_part) {
     constexpr bool A_MN = MODE == DW, B_MN = MODE == DH || MODE == DW;   // operand rows run along the products' length
     extern __shared__ char smem_raw[];
-    constexpr int STAGES = Layout<MODE>::STAGES;
+    constexpr int STAGES = Layout<MODE, NB>::STAGES, STAGE_BYTES = Layout<MODE, NB>::STAGE_BYTES, ACCS = Layout<MODE, NB>::ACCS;
     __shared__ alignas(8) unsigned long long bars[2 * STAGES + 4 + 1];
     __shared__ uint32_t tmem_base;
     __shared__ int stop;
@@ -435,7 +440,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
 
     qg_after_prior();   // what is above touches no memory of the device
     const int count = a.count ? *a.count : a.all_rows;
-    Schedule<MODE> todo(a, count);
+    Schedule<MODE, NB> todo(a, count);
     Work c;
     bool ok = true;
 
@@ -447,10 +452,9 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                 const int s = it % STAGES;
                 if (!(ok = tc_bar_wait(empty(s), (it / STAGES & 1) ^ 1, &stop))) break;
                 const uint32_t bar = CG == 1 ? full(s) : tc_map_rank(full(s), 0);
-                const int b_rows = B_MN ? c.cols / CG : B_ROWS;   // of the second operand in this CTA
-                if (rank == 0) tc_bar_expect(full(s), CG * (A_BYTES + b_rows * BK * 2));
+                if (rank == 0) tc_bar_expect(full(s), CG * A_BYTES + c.cols * BK * 2);
                 const uint32_t at = tiles_at + s * STAGE_BYTES, bt = at + A_BYTES;
-                const int am = c.m * BM + rank * 128, bn = c.n * BN + rank * b_rows;
+                const int am = c.m * BM + rank * 128;
                 if (A_MN) {
                     for (int j = 0; j < 2; ++j) tc_load_2d<CG>(at + j * 8192, &map_a, am + 64 * j, k * BK, bar);
                 } else {
@@ -458,9 +462,12 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                 }
                 if (B_MN) {
                     const int y = (MODE == DH ? a.v0 : 0) + k * BK;
-                    for (int j = 0; j < b_rows / 64; ++j) tc_load_2d<CG>(bt + j * 8192, &map_b, bn + 64 * j, y, bar);
+                    for (int h = 0; h < NB; ++h) {   // this CTA's part of every accumulator's columns
+                        const int part = min(BN, c.cols - h * BN) / CG, x = c.n * BN * NB + h * BN + rank * part;
+                        for (int j = 0; j < part / 64; ++j) tc_load_2d<CG>(bt + h * B_BYTES + j * 8192, &map_b, x + 64 * j, y, bar);
+                    }
                 } else {
-                    tc_load_2d<CG>(bt, &map_b, k * BK, a.v0 + bn, bar);
+                    tc_load_2d<CG>(bt, &map_b, k * BK, a.v0 + c.n * BN + rank * B_ROWS, bar);
                 }
             }
         }
@@ -476,9 +483,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
         // ---- matrix instructions
         int it = 0, n_acc = 0;
         while (ok && todo.next(c)) {
-            const uint32_t idesc = tc_idesc(BM, MODE == DH || MODE == DW ? c.cols : BN, a.bf16, A_MN, B_MN);
-            const int b = n_acc & 1;
-            if (!(ok = tc_bar_wait(acc_empty(b), (n_acc / 2 & 1) ^ 1, &stop))) break;
+            uint32_t idesc[NB];
+#pragma unroll
+            for (int h = 0; h < NB; ++h) idesc[h] = tc_idesc(BM, min(BN, max(c.cols - h * BN, 0)), a.bf16, A_MN, B_MN);
+            const int b = n_acc % ACCS;
+            if (!(ok = tc_bar_wait(acc_empty(b), (n_acc / ACCS & 1) ^ 1, &stop))) break;
             tc_fence_after();
             for (int k = c.kb0; k < c.kb1; ++k, ++it) {
                 const int s = it % STAGES;
@@ -488,8 +497,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
 #pragma unroll
                 for (int q = 0; q < BK / 16; ++q) {
                     const uint64_t da = tc_desc(at + q * (A_MN ? 2048 : 32), A_MN ? 8192 : 16);
-                    const uint64_t db = tc_desc(bt + q * (B_MN ? 2048 : 32), B_MN ? 8192 : 16);
-                    tc_mma<CG>(tmem + b * ACC_COLS, da, db, idesc, k > c.kb0 || q > 0);
+#pragma unroll
+                    for (int h = 0; h < NB; ++h) {
+                        const uint64_t db = tc_desc(bt + h * B_BYTES + q * (B_MN ? 2048 : 32), B_MN ? 8192 : 16);
+                        if (h == 0 || c.cols > h * BN) tc_mma<CG>(tmem + (b + h) * ACC_COLS, da, db, idesc[h], k > c.kb0 || q > 0);
+                    }
                 }
                 tc_commit<CG>(empty(s));
             }
@@ -511,14 +523,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
     } else if (warp >= 4) {
         // ---- epilogue: thread = row of the tile, half of the columns per warp
         const int quarter = warp & 3, half = (warp - 4) >> 2;
-        Epilogue<MODE> epi(a, &map_out, &map_part, store_at + (warp - 4) * Layout<MODE>::BUFFERS * STORE_BYTES, lane, count);
+        Epilogue<MODE, NB> epi(a, &map_out, &map_part, store_at + (warp - 4) * Layout<MODE, NB>::BUFFERS * STORE_BYTES, lane, count);
         int n_acc = 0;
         while (todo.next(c)) {
-            const int b = n_acc & 1;
+            const int b = n_acc % ACCS;
             epi.begin(c, (int)rank, quarter, half);
-            if (!(ok = __all_sync(0xffffffffu, tc_bar_wait(acc_full(b), n_acc / 2 & 1, &stop)))) break;
+            if (!(ok = __all_sync(0xffffffffu, tc_bar_wait(acc_full(b), n_acc / ACCS & 1, &stop)))) break;
             tc_fence_after();
-            const uint32_t tacc = tmem + ((uint32_t)(quarter * 32) << 16) + b * ACC_COLS + half * 128;
+            const uint32_t tacc = tmem + ((uint32_t)(quarter * 32) << 16) + b * ACC_COLS + half * (BN * NB / 2);
             auto hand_back = [&]() {   // the accumulator may be filled again
                 tc_fence_before();
                 __syncwarp();
@@ -557,18 +569,18 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                     epi.gradients(x, h);
                 }
             } else {
-                if (half * 128 < c.cols) {   // a narrow tile has nothing for the second half
+                const int mine = min(BN * NB / 2, c.cols - half * (BN * NB / 2));   // 0 or less: a narrow tile has nothing for this warp
+                if (mine <= 0) hand_back();
+                for (int c0 = 0; c0 < mine; c0 += 128) {
                     uint32_t r[2][32];
-                    tc_ld_32(tacc, r[0]);
+                    tc_ld_32(tacc + c0, r[0]);
 #pragma unroll
                     for (int cc = 0; cc < 4; ++cc) {
                         tc_ld_wait(r[cc & 1]);
-                        if (cc < 3) tc_ld_32(tacc + (cc + 1) * 32, r[(cc + 1) & 1]);   // read under the arithmetic of this chunk
-                        else hand_back();
-                        epi.chunk(r[cc & 1], cc);
+                        if (cc < 3) tc_ld_32(tacc + c0 + (cc + 1) * 32, r[(cc + 1) & 1]);   // read under the arithmetic of this chunk
+                        else if (c0 + 128 >= mine) hand_back();
+                        epi.chunk(r[cc & 1], c0, cc);
                     }
-                } else {
-                    hand_back();
                 }
             }
             ++n_acc;
@@ -984,7 +996,7 @@ __device__ __forceinline__ void write4(T *o, int left, const float4 &s, float sc
 
 // dH: every row of the caller's, zeros where it has no label.  A group of 2^lg threads per row, four columns each.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, int gangs, int rounds, bool split, int kb, const int *pos_of, int rows, int dim,
+__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int tn, int gang, int gangs, int rounds, bool split, int kb, const int *pos_of, int rows, int dim,
                                                    const float *grad_loss, const int *count, T *out, long long ld_out, int lg) {
     qg_after_prior();
     const int r = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), lane = threadIdx.x & ((1 << lg) - 1);
@@ -996,12 +1008,12 @@ __global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, 
     for (int d = lane * 4; d < dim; d += 4 << lg) {
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (p >= 0) {
-            const int now = d / BN / gang, member = d / BN - now * gang;
+            const int now = d / tn / gang, member = d / tn - now * gang;
             if (now != round) {
                 round = now, place = round * m_live + p / BM;
                 g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
             }
-            for (int g = g0; g <= g1; ++g) add4(s, part + (((long long)(place + g) * gang + member) * BM + p % BM) * BN + d % BN);
+            for (int g = g0; g <= g1; ++g) add4(s, part + (((long long)(place + g) * gang + member) * BM + p % BM) * tn + d % tn);
         }
         write4(out + r * ld_out + d, dim - d, s, scale);
     }
@@ -1010,7 +1022,7 @@ __global__ void __launch_bounds__(256) k_dh_finish(const float *part, int gang, 
 // dW: the tiles that a cut falls into; blocks x look at the cut in front of gang x / gang + 1 and the tile of member
 // x % gang, blocks y take 8 rows.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dw_finish(const float *part, int gang, int gangs, int rounds, int m_tiles, int n_tiles, int rows, int dim,
+__global__ void __launch_bounds__(256) k_dw_finish(const float *part, int tn, int gang, int gangs, int rounds, int m_tiles, int n_tiles, int rows, int dim,
                                                    const float *grad_loss, const int *count, T *out, long long ld_out) {
     qg_after_prior();
     const int n = *count, kb = (n + BK - 1) / BK;
@@ -1024,12 +1036,12 @@ __global__ void __launch_bounds__(256) k_dw_finish(const float *part, int gang, 
     const int g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
     if (g0 != g - 1) return;   // an earlier cut of the same tile
     const float scale = out_scale(grad_loss, n);
-    const int round = place / m_tiles, m = place - round * m_tiles, col = (round * gang + member) * BN;
+    const int round = place / m_tiles, m = place - round * m_tiles, col = (round * gang + member) * tn;
     const int r = blockIdx.y * 8 + threadIdx.x / 32;
     if (m * BM + r >= rows) return;
-    for (int d = (threadIdx.x & 31) * 4; d < BN && col + d < dim; d += 128) {
+    for (int d = (threadIdx.x & 31) * 4; d < tn && col + d < dim; d += 128) {
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int k = g0; k <= g1; ++k) add4(s, part + ((long long)(2 * (k * gang + member) + (k == g0)) * BM + r) * BN + d);
+        for (int k = g0; k <= g1; ++k) add4(s, part + ((long long)(2 * (k * gang + member) + (k == g0)) * BM + r) * tn + d);
         write4(out + (long long)(m * BM + r) * ld_out + col + d, dim - col - d, s, scale);
     }
 }
@@ -1085,17 +1097,17 @@ int matrix_map(qgbdt_ctx *c, CUtensorMap *m, const void *p, long long cols, long
     return QGBDT_OK;
 }
 
-template <int MODE>
+template <int MODE, int NB>
 int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mo, const CUtensorMap &mp,
          cudaStream_t st) {
-    if (!(c->ops_configured >> MODE & 1)) {
-        QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MODE>::BYTES));
-        c->ops_configured |= 1u << MODE;
+    if (!(c->ops_configured >> (MODE * 2 + NB - 1) & 1)) {
+        QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MODE, NB>::BYTES));
+        c->ops_configured |= 1u << (MODE * 2 + NB - 1);
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)units * CG);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Layout<MODE>::BYTES;
+    cfg.dynamicSmemBytes = Layout<MODE, NB>::BYTES;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -1104,7 +1116,7 @@ int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, cons
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    QG_CUDA(c, cudaLaunchKernelEx(&cfg, k_softmax_gemm<MODE>, a, ma, mb, mo, mp));
+    QG_CUDA(c, cudaLaunchKernelEx(&cfg, k_softmax_gemm<MODE, NB>, a, ma, mb, mo, mp));
     c->n_launches++;
     return QGBDT_OK;
 }
@@ -1172,20 +1184,32 @@ int unit_count(const qgbdt_ctx *c, long long tiles) {
 
 // Gangs for products with `lines` row tiles of kb blocks each and n_tiles column tiles: of the sizes up to eight that
 // leave at most 6 % of the units without work the largest, or else the size that leaves the fewest.
+// Gradients of 8192 rows x 65536 classes x 1024: 2.77 ms with one accumulator throughout, 2.69 ms with this rule; without its
+// conditions 1024 x 32000 x 768 went from 140 to 160 us, 512 x 65536 x 512 from 127 to 135, 2048 x 65536 x 1024 from 641 to 672.
+constexpr long long WIDE_RUN = 128, WIDE_OPERAND = 48ll << 20;
 struct Gangs {
     int size, gangs, rounds;
     bool split;
+    int tn, n_tiles;   // columns of a tile, tiles
     int units() const { return size * gangs; }
 };
-Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int n_tiles, long long kb) {
+Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int dim, long long kb) {
     const int units = c->sm_count / CG;
-    Gangs best{1, units, n_tiles, false};
-    double best_use = 0.0;
-    for (int g = 1; g <= 8 && g <= n_tiles && g <= units; ++g) {
-        const int rounds = (n_tiles + g - 1) / g;
-        const double use = (double)(units / g * g) / units * n_tiles / (rounds * g);
-        if (use >= 0.94 || use > best_use) best = Gangs{g, units / g, rounds, false}, best_use = use;
-    }
+    auto plan = [&](int tn) {
+        const int n_tiles = (dim + tn - 1) / tn;
+        Gangs best{1, units, n_tiles, false, tn, n_tiles};
+        double best_use = 0.0;
+        for (int g = 1; g <= 8 && g <= n_tiles && g <= units; ++g) {
+            const int rounds = (n_tiles + g - 1) / g;
+            const double use = (double)(units / g * g) / units * n_tiles / (rounds * g);
+            if (use >= 0.94 || use > best_use) best = Gangs{g, units / g, rounds, false, tn, n_tiles}, best_use = use;
+        }
+        return best;
+    };
+    // Two accumulators where the epilogue that nothing hides is a small part (long runs), the column tiles come out full,
+    // and the second operand stays in L2 (half as many units share a block of the first one).
+    Gangs best = plan(2 * BN);
+    if ((double)dim / (2 * BN * best.n_tiles) < 0.95 || best.rounds * m_tiles * kb / best.gangs < WIDE_RUN || kb * BK * dim * 2 > WIDE_OPERAND) best = plan(BN);
     best.split = kb >= SPLIT_KB;
     const long long lines = best.rounds * m_tiles, most = best.split ? (lines * kb + 3) / 4 : lines;
     if (best.gangs > most) best.gangs = most < 1 ? 1 : (int)most;
@@ -1196,13 +1220,13 @@ template <typename T>
 int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const PackArgs &p, const float *part, const Gangs &g, int kb, cudaStream_t st) {
     int lg = 0;
     while (lg < 8 && (4 << lg) < a.dim) ++lg;
-    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, part, g.size, g.gangs, g.rounds, g.split, kb,
+    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, part, g.tn, g.size, g.gangs, g.rounds, g.split, kb,
                      p.pos_of, (int)a.rows, a.dim, a.grad_loss, p.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden, lg);
 }
 
 template <typename T>
-int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const PackArgs &p, const float *part, const GemmArgs &g, int rows, cudaStream_t st) {
-    return qg_launch(c, k_dw_finish<T>, dim3(g.gangs * g.gang, BM / 8), 256, 0, st, part, g.gang, g.gangs, g.rounds, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, p.count,
+int dw_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const PackArgs &p, const float *part, int tn, const GemmArgs &g, int rows, cudaStream_t st) {
+    return qg_launch(c, k_dw_finish<T>, dim3(g.gangs * g.gang, BM / 8), 256, 0, st, part, tn, g.gang, g.gangs, g.rounds, g.m_tiles, g.n_tiles, rows, a.dim, a.grad_loss, p.count,
                                                        reinterpret_cast<T *>(a.d_weight) + g.v0 * a.ld_d_weight, a.ld_d_weight);
 }
 
@@ -1264,7 +1288,7 @@ int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
                          : matrix_map(c, &ma, p.packed, a.dim, n_pad, p.ldp, 128, a.type)) != QGBDT_OK)
             return rc;
         if ((rc = matrix_map(c, &mb, w.p, a.dim, a.classes, w.ld, B_ROWS, a.type)) != QGBDT_OK) return rc;
-        if ((rc = gemm<LOSS>(c, g, units, ma, mb, ma, ma, st)) != QGBDT_OK) return rc;
+        if ((rc = gemm<LOSS, 1>(c, g, units, ma, mb, ma, ma, st)) != QGBDT_OK) return rc;
     }
     j.stat = g.stat, j.n_tiles = n_tiles * 2, j.z_label = g.z_label, j.pos_of = p.pos_of, j.labels = g.labels, j.n = (int)a.rows;
     j.losses = a.losses, j.lse = a.lse, j.loss = a.loss, j.status = a.status, j.arrived = c->d_ops_counters;
@@ -1285,22 +1309,22 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     if (width < 256) width = 256;
     const int pieces = (int)((a.classes + width - 1) / width);
     width = up((a.classes + pieces - 1) / pieces, 256);
-    const int d_tiles = (a.dim + BN - 1) / BN, m_tiles = n_pad / BM, kb_dh = (int)(width / BK);
+    const int m_tiles = n_pad / BM, kb_dh = (int)(width / BK);
     const int grad_units = unit_count(c, m_tiles * (width / BN));
-    if (grad_units < 0 || unit_count(c, (long long)m_tiles * d_tiles) < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
-    const Gangs dh_gangs = gang_plan(c, m_tiles, d_tiles, kb_dh), dw_gangs = gang_plan(c, width / BM, d_tiles, n_pad / BK);
+    if (grad_units < 0 || unit_count(c, (long long)m_tiles * ((a.dim + BN - 1) / BN)) < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
+    const Gangs dh_gangs = gang_plan(c, m_tiles, a.dim, kb_dh), dw_gangs = gang_plan(c, width / BM, a.dim, n_pad / BK);
     const size_t dh_fragments = ((size_t)m_tiles * dh_gangs.rounds + dh_gangs.gangs) * dh_gangs.size, dw_fragments = dw_gangs.split ? 2 * (size_t)dw_gangs.units() : 0;
     QgWorkspace ws;
     int rc = qg_ws_open(c,
-                        weight_bytes(a) + pack_bytes(a) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size(dh_fragments * BM * BN, 4) +
-                            qg_ws_size(dw_fragments * BM * BN, 4) + (a.d_bias ? qg_ws_size((size_t)(n_pad / 32) * width, 4) : 0),
+                        weight_bytes(a) + pack_bytes(a) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size(dh_fragments * BM * dh_gangs.tn, 4) +
+                            qg_ws_size(dw_fragments * BM * dw_gangs.tn, 4) + (a.d_bias ? qg_ws_size((size_t)(n_pad / 32) * width, 4) : 0),
                         st, &ws);
     if (rc != QGBDT_OK) return rc;
     Weight w;
     PackArgs p;
     if ((rc = align_weight(c, a, ws, &w, st)) != QGBDT_OK || (rc = pack_rows(c, a, ws, &p, st)) != QGBDT_OK) return rc;
     uint16_t *g_piece = ws.take<uint16_t>((size_t)n_pad * width);
-    float *dh_part = ws.take<float>(dh_fragments * BM * BN), *dw_part = ws.take<float>(dw_fragments * BM * BN);
+    float *dh_part = ws.take<float>(dh_fragments * BM * dh_gangs.tn), *dw_part = ws.take<float>(dw_fragments * BM * dw_gangs.tn);
     float *bias_part = a.d_bias ? ws.take<float>((size_t)(n_pad / 32) * width) : nullptr;
     GemmArgs base = gemm_args(c, a);
     base.count = p.count, base.label = p.label, base.lse = p.lse_packed;
@@ -1313,9 +1337,9 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     if ((rc = matrix_map(c, &g_k, g_piece, width, n_pad, width, 128, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &g_mn, g_piece, width, n_pad, width, 64, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &g_store, g_piece, width, n_pad, width, 32, a.type)) != QGBDT_OK) return rc;
-    if ((rc = matrix_map(c, &dh_map, dh_part, BN, (long long)dh_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &dh_map, dh_part, dh_gangs.tn, (long long)dh_fragments * BM, dh_gangs.tn, 32, QGBDT_F32)) != QGBDT_OK) return rc;
     dw_map = dh_map;
-    if (dw_fragments && (rc = matrix_map(c, &dw_map, dw_part, BN, (long long)dw_fragments * BM, BN, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    if (dw_fragments && (rc = matrix_map(c, &dw_map, dw_part, dw_gangs.tn, (long long)dw_fragments * BM, dw_gangs.tn, 32, QGBDT_F32)) != QGBDT_OK) return rc;
     out = g_store;
     if (out_map && (rc = matrix_map(c, &out, a.d_weight, a.dim, a.classes, a.ld_d_weight, 32, a.type)) != QGBDT_OK) return rc;
     for (int k = 0; k < pieces; ++k) {
@@ -1323,21 +1347,21 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
         const int nv = (int)(a.classes - v0 < width ? a.classes - v0 : width);
         GemmArgs g = base;
         g.v0 = v0, g.n_tiles = (int)(width / BN), g.bias_part = bias_part;
-        if ((rc = gemm<GRAD>(c, g, grad_units, h_k, w_k, g_store, g_store, st)) != QGBDT_OK) return rc;
+        if ((rc = gemm<GRAD, 1>(c, g, grad_units, h_k, w_k, g_store, g_store, st)) != QGBDT_OK) return rc;
         if (bias_part) {
             QG_RUN(qg_launch(c, k_bias_finish, dim3((nv + 31) / 32), 256, 0, st, bias_part, (int)width, nv, a.grad_loss, base.count, a.d_bias + v0));
         }
         g = base;
-        g.v0 = v0, g.n_tiles = d_tiles, g.kb = kb_dh, g.add = k > 0;
+        g.v0 = v0, g.n_tiles = dh_gangs.n_tiles, g.kb = kb_dh, g.add = k > 0;
         g.gang = dh_gangs.size, g.gangs = dh_gangs.gangs, g.rounds = dh_gangs.rounds, g.split = dh_gangs.split;
-        if ((rc = gemm<DH>(c, g, dh_gangs.units(), g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
+        if ((rc = (dh_gangs.tn == BN ? gemm<DH, 1> : gemm<DH, 2>)(c, g, dh_gangs.units(), g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
         g = base;
-        g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = d_tiles;
+        g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = dw_gangs.n_tiles;
         g.gang = dw_gangs.size, g.gangs = dw_gangs.gangs, g.rounds = dw_gangs.rounds, g.split = dw_gangs.split;
         g.rows = nv, g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
-        if ((rc = gemm<DW>(c, g, dw_gangs.units(), g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
+        if ((rc = (dw_gangs.tn == BN ? gemm<DW, 1> : gemm<DW, 2>)(c, g, dw_gangs.units(), g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
         if (!dw_gangs.split) continue;
-        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, p, dw_part, g, nv, st) : dw_finish<__half>(c, a, p, dw_part, g, nv, st);
+        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, p, dw_part, dw_gangs.tn, g, nv, st) : dw_finish<__half>(c, a, p, dw_part, dw_gangs.tn, g, nv, st);
         if (rc != QGBDT_OK) return rc;
     }
     rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, p, dh_part, dh_gangs, kb_dh, st) : dh_finish<__half>(c, a, p, dh_part, dh_gangs, kb_dh, st);

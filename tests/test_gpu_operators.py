@@ -423,6 +423,15 @@ def test_softmax_ce_many_pieces(ctx):
     check_grads(ctx.softmax_ce_backward(h, w, y, r.lse, bias=b), e, h, w, torch.bfloat16)
 
 
+def test_softmax_ce_long_products(ctx):
+    """Tiles of two accumulators, cut into fragments, over more than one piece."""
+    h, w, b, y = softmax_case(5000, 30000, 1024, torch.bfloat16, True, 0.1, 3)
+    e = softmax_exact(h, w, b, y)
+    r = ctx.softmax_ce(h, w, y, bias=b)
+    check_loss(r, e, h, w)
+    check_grads(ctx.softmax_ce_backward(h, w, y, r.lse, bias=b), e, h, w, torch.bfloat16)
+
+
 def test_softmax_ce_gradient_by_differences(ctx):
     """The loss along a direction in H, W and b: central differences of the kernel's own loss."""
     h, w, b, y = softmax_case(60, 50, 24, torch.float16, True, 0.2, 8)
