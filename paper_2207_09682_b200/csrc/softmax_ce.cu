@@ -126,9 +126,15 @@ struct Line {
         const long long most = split ? length / 4 : lines;
         runs = most < 1 ? 1 : most < gangs ? (int)most : gangs;
     }
-    __device__ __forceinline__ long long start(int g) const { return split ? length * g / runs : length / kb * g / runs * kb; }
+    // a * b / c; in 32 bits where the line is short enough for that (a 64-bit division takes a hundred instructions)
+    __device__ __forceinline__ long long scaled(long long a, int b, long long c) const {
+        return length < (1 << 24) && runs < 256 ? (long long)((unsigned)a * (unsigned)b / (unsigned)c) : a * b / c;
+    }
+    __device__ __forceinline__ long long start(int g) const { return split ? scaled(length, g, runs) : scaled(length / kb, g, runs) * kb; }
     __device__ __forceinline__ int gang_of(long long pos) const {   // the gang whose run holds block pos
-        return split ? (int)(((pos + 1) * runs - 1) / length) : (int)(((pos / kb + 1) * runs - 1) / (length / kb));
+        // the last g with floor(length * g / runs) <= pos
+        const long long at = split ? pos : pos / kb, all = split ? length : length / kb;
+        return (int)(length < (1 << 24) && runs < 256 ? (((unsigned)at + 1) * (unsigned)runs - 1) / (unsigned)all : ((at + 1) * runs - 1) / all);
     }
 };
 
@@ -994,26 +1000,40 @@ __device__ __forceinline__ void write4(T *o, int left, const float4 &s, float sc
     }
 }
 
+// The fragments of the pieces of one width.
+struct DhParts {
+    const float *part;   // NULL: there is no such piece
+    int tn, gang, gangs, rounds, kb;
+    bool split;
+};
+
 // dH: every row of the caller's, zeros where it has no label.  A group of 2^lg threads per row, four columns each.
 template <typename T>
-__global__ void __launch_bounds__(256) k_dh_finish(const float *part, int tn, int gang, int gangs, int rounds, bool split, int kb, const int *pos_of, int rows, int dim,
-                                                   const float *grad_loss, const int *count, T *out, long long ld_out, int lg) {
+__global__ void __launch_bounds__(256) k_dh_finish(const DhParts full, const DhParts rest, const int *pos_of, int rows, int dim, const float *grad_loss,
+                                                   const int *count, T *out, long long ld_out, int lg) {
     qg_after_prior();
     const int r = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), lane = threadIdx.x & ((1 << lg) - 1);
     if (r >= rows) return;
     const int n = *count, p = pos_of[r], m_live = (n + BM - 1) / BM;
     const float scale = out_scale(grad_loss, n);
-    const Line line(rounds * m_live, kb, gangs, split);
-    int round = -1, place = 0, g0 = 0, g1 = -1;
+    // of one set: the gangs g0 to g1 that worked on the row's tile in a round
+    struct Span {
+        int round = -1, place, g0, g1;
+    } span[2];
+    auto add = [&](float4 &s, const DhParts &x, Span &w, int d) {
+        const int now = d / x.tn / x.gang, member = d / x.tn - now * x.gang;
+        if (now != w.round) {
+            const Line line(x.rounds * m_live, x.kb, x.gangs, x.split);
+            w.round = now, w.place = now * m_live + p / BM;
+            w.g0 = line.gang_of((long long)w.place * x.kb), w.g1 = line.gang_of((long long)(w.place + 1) * x.kb - 1);
+        }
+        for (int g = w.g0; g <= w.g1; ++g) add4(s, x.part + (((long long)(w.place + g) * x.gang + member) * BM + p % BM) * x.tn + d % x.tn);
+    };
     for (int d = lane * 4; d < dim; d += 4 << lg) {
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (p >= 0) {
-            const int now = d / tn / gang, member = d / tn - now * gang;
-            if (now != round) {
-                round = now, place = round * m_live + p / BM;
-                g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
-            }
-            for (int g = g0; g <= g1; ++g) add4(s, part + (((long long)(place + g) * gang + member) * BM + p % BM) * tn + d % tn);
+            add(s, full, span[0], d);
+            if (rest.part) add(s, rest, span[1], d);
         }
         write4(out + r * ld_out + d, dim - d, s, scale);
     }
@@ -1173,8 +1193,6 @@ GemmArgs gemm_args(qgbdt_ctx *c, const SoftmaxArgs &a) {
     return g;
 }
 
-constexpr int64_t PIECE_ELEMENTS = 1ll << 27;   // of g: 256 MiB
-
 // Units (pairs of CTAs) for a number of tiles; -1: more tiles than a launch can number.
 int unit_count(const qgbdt_ctx *c, long long tiles) {
     const int units = c->sm_count / CG;
@@ -1193,7 +1211,7 @@ struct Gangs {
     int tn, n_tiles;   // columns of a tile, tiles
     int units() const { return size * gangs; }
 };
-Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int dim, long long kb) {
+Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int dim, long long kb, int join_cost) {
     const int units = c->sm_count / CG;
     auto plan = [&](int tn) {
         const int n_tiles = (dim + tn - 1) / tn;
@@ -1210,18 +1228,64 @@ Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int dim, long long kb) {
     // and the second operand stays in L2 (half as many units share a block of the first one).
     Gangs best = plan(2 * BN);
     if ((double)dim / (2 * BN * best.n_tiles) < 0.95 || best.rounds * m_tiles * kb / best.gangs < WIDE_RUN || kb * BK * dim * 2 > WIDE_OPERAND) best = plan(BN);
-    best.split = kb >= SPLIT_KB;
-    const long long lines = best.rounds * m_tiles, most = best.split ? (lines * kb + 3) / 4 : lines;
+    // whole tiles where the last round's idle units cost less than joining fragments would
+    const long long lines = best.rounds * m_tiles;
+    best.split = kb >= SPLIT_KB && (join_cost == 0 || (lines + best.gangs - 1) / best.gangs * kb > lines * kb / best.gangs + join_cost * BN / best.tn);
+    const long long most = best.split ? (lines * kb + 3) / 4 : lines;
     if (best.gangs > most) best.gangs = most < 1 ? 1 : (int)most;
     return best;
 }
 
+// How the classes are cut into pieces.  All times in what a unit takes for a block of 256 x 256 x 64.
+constexpr int64_t PIECE_ELEMENTS = 3ll << 26;   // of g, at most: 384 MiB
+constexpr int JOIN_COST = 80;                   // of DW's fragments (DH's are joined in any case)
+constexpr int PIECE_COST = 60;                  // of the launches of a piece and of DH's additions
+
+struct Piece {
+    int width;       // classes, rounded up to 256
+    Gangs dh, dw;
+    double cost;
+};
+Piece piece_plan(const qgbdt_ctx *c, int64_t classes, int n_pad, int dim) {
+    Piece p;
+    p.width = up(classes, 256);
+    const int units = c->sm_count / CG, m_tiles = n_pad / BM, kb = (dim + BK - 1) / BK;
+    p.dh = gang_plan(c, m_tiles, dim, p.width / BK, 0);
+    p.dw = gang_plan(c, p.width / BM, dim, n_pad / BK, JOIN_COST);
+    const long long lines = (long long)p.dw.rounds * (p.width / BM), tiles = (long long)m_tiles * (p.width / BN);
+    const double dw = p.dw.split ? (double)lines / p.dw.gangs : (double)((lines + p.dw.gangs - 1) / p.dw.gangs);
+    // GRAD's epilogue takes as long as six blocks
+    p.cost = (double)((tiles + units - 1) / units) * (kb > 6 ? kb : 6) + (double)m_tiles * ((dim + BN - 1) / BN) * (p.width / BK) / units +
+             dw * (n_pad / BK) * p.dw.tn / BN + (p.dw.split ? JOIN_COST : 0) + PIECE_COST;
+    return p;
+}
+
+// Pieces of equal width and a narrower last one.  Of some widths that the memory allows (equal shares, and whole rounds of
+// DW's gangs) the one with the least cost.
+int64_t piece_width(const qgbdt_ctx *c, int64_t classes, int n_pad, int dim) {
+    int64_t most = PIECE_ELEMENTS / n_pad / 256 * 256;
+    if (most < 256) most = 256;
+    if (classes <= most) return classes;
+    const int64_t pieces = (classes + most - 1) / most, round = 256ll * piece_plan(c, most, n_pad, dim).dw.gangs;
+    int64_t best = most;
+    double best_cost = 1e300;
+    auto look = [&](int64_t width) {
+        if (width < 256 || width > most) return;
+        const int64_t rest = classes % width;
+        const double cost = (double)(classes / width) * piece_plan(c, width, n_pad, dim).cost + (rest ? piece_plan(c, rest, n_pad, dim).cost : 0.0);
+        if (cost < best_cost) best = width, best_cost = cost;
+    };
+    for (int64_t k = pieces; k < pieces + 4; ++k) look((classes + k - 1) / k + 255 & ~255ll);
+    for (int64_t k = most / round; k > 0 && k > most / round - 3; --k) look(k * round);
+    return best;
+}
+
 template <typename T>
-int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const PackArgs &p, const float *part, const Gangs &g, int kb, cudaStream_t st) {
+int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const PackArgs &p, const DhParts &full, const DhParts &rest, cudaStream_t st) {
     int lg = 0;
-    while (lg < 8 && (4 << lg) < a.dim) ++lg;
-    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, part, g.tn, g.size, g.gangs, g.rounds, g.split, kb,
-                     p.pos_of, (int)a.rows, a.dim, a.grad_loss, p.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden, lg);
+    while (lg < 6 && (4 << lg) < a.dim) ++lg;
+    return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, full, rest, p.pos_of, (int)a.rows, a.dim,
+                     a.grad_loss, p.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden, lg);
 }
 
 template <typename T>
@@ -1303,68 +1367,74 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
         if (a.d_bias) QG_CUDA(c, cudaMemsetAsync(a.d_bias, 0, sizeof(float) * a.classes, st));
         return QGBDT_OK;
     }
-    const int n_pad = up(a.rows, 256);
-    // pieces of the classes, all of one width (the last one's missing classes count as excluded)
-    int64_t width = PIECE_ELEMENTS / n_pad / 256 * 256;
-    if (width < 256) width = 256;
-    const int pieces = (int)((a.classes + width - 1) / width);
-    width = up((a.classes + pieces - 1) / pieces, 256);
-    const int m_tiles = n_pad / BM, kb_dh = (int)(width / BK);
-    const int grad_units = unit_count(c, m_tiles * (width / BN));
-    if (grad_units < 0 || unit_count(c, (long long)m_tiles * ((a.dim + BN - 1) / BN)) < 0) return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
-    const Gangs dh_gangs = gang_plan(c, m_tiles, a.dim, kb_dh), dw_gangs = gang_plan(c, width / BM, a.dim, n_pad / BK);
-    const size_t dh_fragments = ((size_t)m_tiles * dh_gangs.rounds + dh_gangs.gangs) * dh_gangs.size, dw_fragments = dw_gangs.split ? 2 * (size_t)dw_gangs.units() : 0;
+    const int n_pad = up(a.rows, 256), m_tiles = n_pad / BM;
+    // the pieces: n_full of one width, then (kind 1) what is left
+    const int64_t width = piece_width(c, a.classes, n_pad, a.dim), n_full = a.classes / width, left = a.classes - n_full * width;
+    const Piece kinds[2] = {piece_plan(c, width, n_pad, a.dim), left ? piece_plan(c, left, n_pad, a.dim) : Piece{}};
+    const int n_kinds = left ? 2 : 1, ld_g = kinds[0].width;
+    if (unit_count(c, (long long)m_tiles * (ld_g / BN)) < 0 || unit_count(c, (long long)m_tiles * ((a.dim + BN - 1) / BN)) < 0)
+        return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
+    size_t dh_rows[2] = {0, 0}, dw_floats = 0, bytes = weight_bytes(a) + pack_bytes(a) + qg_ws_size((size_t)n_pad * ld_g, 2) +
+                                                       (a.d_bias ? qg_ws_size((size_t)(n_pad / 32) * ld_g, 4) : 0);
+    size_t dw_rows[2] = {0, 0};
+    for (int i = 0; i < n_kinds; ++i) {
+        const Gangs &h = kinds[i].dh, &w = kinds[i].dw;
+        dh_rows[i] = ((size_t)m_tiles * h.rounds + h.gangs) * h.size * BM;
+        dw_rows[i] = w.split ? 2 * (size_t)w.units() * BM : 0;
+        if (dw_rows[i] * w.tn > dw_floats) dw_floats = dw_rows[i] * w.tn;
+        bytes += qg_ws_size(dh_rows[i] * h.tn, 4);
+    }
     QgWorkspace ws;
-    int rc = qg_ws_open(c,
-                        weight_bytes(a) + pack_bytes(a) + qg_ws_size((size_t)n_pad * width, 2) + qg_ws_size(dh_fragments * BM * dh_gangs.tn, 4) +
-                            qg_ws_size(dw_fragments * BM * dw_gangs.tn, 4) + (a.d_bias ? qg_ws_size((size_t)(n_pad / 32) * width, 4) : 0),
-                        st, &ws);
+    int rc = qg_ws_open(c, bytes + qg_ws_size(dw_floats, 4), st, &ws);
     if (rc != QGBDT_OK) return rc;
     Weight w;
     PackArgs p;
     if ((rc = align_weight(c, a, ws, &w, st)) != QGBDT_OK || (rc = pack_rows(c, a, ws, &p, st)) != QGBDT_OK) return rc;
-    uint16_t *g_piece = ws.take<uint16_t>((size_t)n_pad * width);
-    float *dh_part = ws.take<float>(dh_fragments * BM * dh_gangs.tn), *dw_part = ws.take<float>(dw_fragments * BM * dw_gangs.tn);
-    float *bias_part = a.d_bias ? ws.take<float>((size_t)(n_pad / 32) * width) : nullptr;
+    uint16_t *g_piece = ws.take<uint16_t>((size_t)n_pad * ld_g);
+    float *bias_part = a.d_bias ? ws.take<float>((size_t)(n_pad / 32) * ld_g) : nullptr, *dw_part = ws.take<float>(dw_floats);
     GemmArgs base = gemm_args(c, a);
     base.count = p.count, base.label = p.label, base.lse = p.lse_packed;
     const bool bf16 = base.bf16, out_map = rows_aligned(a.d_weight, a.ld_d_weight) && a.dim % 8 == 0;   // tiled copies cut rows off at 16 bytes only
-    CUtensorMap h_k, h_mn, w_k, w_mn, g_k, g_mn, g_store, dh_map, dw_map, out;
+    CUtensorMap h_k, h_mn, w_k, w_mn, g_k, g_mn, g_store, dh_map[2], dw_map[2], out;
     if ((rc = matrix_map(c, &h_k, p.packed, a.dim, n_pad, p.ldp, 128, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &h_mn, p.packed, a.dim, n_pad, p.ldp, 64, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &w_k, w.p, a.dim, a.classes, w.ld, B_ROWS, a.type)) != QGBDT_OK) return rc;
     if ((rc = matrix_map(c, &w_mn, w.p, a.dim, a.classes, w.ld, 64, a.type)) != QGBDT_OK) return rc;
-    if ((rc = matrix_map(c, &g_k, g_piece, width, n_pad, width, 128, a.type)) != QGBDT_OK) return rc;
-    if ((rc = matrix_map(c, &g_mn, g_piece, width, n_pad, width, 64, a.type)) != QGBDT_OK) return rc;
-    if ((rc = matrix_map(c, &g_store, g_piece, width, n_pad, width, 32, a.type)) != QGBDT_OK) return rc;
-    if ((rc = matrix_map(c, &dh_map, dh_part, dh_gangs.tn, (long long)dh_fragments * BM, dh_gangs.tn, 32, QGBDT_F32)) != QGBDT_OK) return rc;
-    dw_map = dh_map;
-    if (dw_fragments && (rc = matrix_map(c, &dw_map, dw_part, dw_gangs.tn, (long long)dw_fragments * BM, dw_gangs.tn, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &g_k, g_piece, ld_g, n_pad, ld_g, 128, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &g_mn, g_piece, ld_g, n_pad, ld_g, 64, a.type)) != QGBDT_OK) return rc;
+    if ((rc = matrix_map(c, &g_store, g_piece, ld_g, n_pad, ld_g, 32, a.type)) != QGBDT_OK) return rc;
+    DhParts parts[2] = {};
+    for (int i = 0; i < n_kinds; ++i) {
+        const Gangs &h = kinds[i].dh, &d = kinds[i].dw;
+        parts[i] = DhParts{ws.take<float>(dh_rows[i] * h.tn), h.tn, h.size, h.gangs, h.rounds, kinds[i].width / BK, h.split};
+        if ((rc = matrix_map(c, &dh_map[i], parts[i].part, h.tn, (long long)dh_rows[i], h.tn, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+        dw_map[i] = dh_map[i];
+        if (d.split && (rc = matrix_map(c, &dw_map[i], dw_part, d.tn, (long long)dw_rows[i], d.tn, 32, QGBDT_F32)) != QGBDT_OK) return rc;
+    }
     out = g_store;
     if (out_map && (rc = matrix_map(c, &out, a.d_weight, a.dim, a.classes, a.ld_d_weight, 32, a.type)) != QGBDT_OK) return rc;
-    for (int k = 0; k < pieces; ++k) {
-        const int v0 = (int)(k * width);
-        const int nv = (int)(a.classes - v0 < width ? a.classes - v0 : width);
+    for (int64_t k = 0; k < n_full + (left ? 1 : 0); ++k) {
+        const int kind = k < n_full ? 0 : 1, v0 = (int)(k * width), nv = (int)(kind == 0 ? width : left);
+        const Gangs &h = kinds[kind].dh, &d = kinds[kind].dw;
         GemmArgs g = base;
-        g.v0 = v0, g.n_tiles = (int)(width / BN), g.bias_part = bias_part;
-        if ((rc = gemm<GRAD, 1>(c, g, grad_units, h_k, w_k, g_store, g_store, st)) != QGBDT_OK) return rc;
-        if (bias_part) {
-            QG_RUN(qg_launch(c, k_bias_finish, dim3((nv + 31) / 32), 256, 0, st, bias_part, (int)width, nv, a.grad_loss, base.count, a.d_bias + v0));
-        }
+        g.v0 = v0, g.n_tiles = kinds[kind].width / BN, g.bias_part = bias_part;
+        if ((rc = gemm<GRAD, 1>(c, g, unit_count(c, (long long)m_tiles * g.n_tiles), h_k, w_k, g_store, g_store, st)) != QGBDT_OK) return rc;
+        if (bias_part)
+            QG_RUN(qg_launch(c, k_bias_finish, dim3((nv + 31) / 32), 256, 0, st, bias_part, kinds[kind].width, nv, a.grad_loss, base.count, a.d_bias + v0));
         g = base;
-        g.v0 = v0, g.n_tiles = dh_gangs.n_tiles, g.kb = kb_dh, g.add = k > 0;
-        g.gang = dh_gangs.size, g.gangs = dh_gangs.gangs, g.rounds = dh_gangs.rounds, g.split = dh_gangs.split;
-        if ((rc = (dh_gangs.tn == BN ? gemm<DH, 1> : gemm<DH, 2>)(c, g, dh_gangs.units(), g_k, w_mn, g_store, dh_map, st)) != QGBDT_OK) return rc;
+        g.v0 = v0, g.n_tiles = h.n_tiles, g.kb = kinds[kind].width / BK, g.add = kind == 0 && k > 0;
+        g.gang = h.size, g.gangs = h.gangs, g.rounds = h.rounds, g.split = h.split;
+        if ((rc = (h.tn == BN ? gemm<DH, 1> : gemm<DH, 2>)(c, g, h.units(), g_k, w_mn, g_store, dh_map[kind], st)) != QGBDT_OK) return rc;
         g = base;
-        g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = dw_gangs.n_tiles;
-        g.gang = dw_gangs.size, g.gangs = dw_gangs.gangs, g.rounds = dw_gangs.rounds, g.split = dw_gangs.split;
+        g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = d.n_tiles;
+        g.gang = d.size, g.gangs = d.gangs, g.rounds = d.rounds, g.split = d.split;
         g.rows = nv, g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
-        if ((rc = (dw_gangs.tn == BN ? gemm<DW, 1> : gemm<DW, 2>)(c, g, dw_gangs.units(), g_mn, h_mn, out, dw_map, st)) != QGBDT_OK) return rc;
-        if (!dw_gangs.split) continue;
-        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, p, dw_part, dw_gangs.tn, g, nv, st) : dw_finish<__half>(c, a, p, dw_part, dw_gangs.tn, g, nv, st);
+        if ((rc = (d.tn == BN ? gemm<DW, 1> : gemm<DW, 2>)(c, g, d.units(), g_mn, h_mn, out, dw_map[kind], st)) != QGBDT_OK) return rc;
+        if (!d.split) continue;
+        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, p, dw_part, d.tn, g, nv, st) : dw_finish<__half>(c, a, p, dw_part, d.tn, g, nv, st);
         if (rc != QGBDT_OK) return rc;
     }
-    rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, p, dh_part, dh_gangs, kb_dh, st) : dh_finish<__half>(c, a, p, dh_part, dh_gangs, kb_dh, st);
+    rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, p, parts[0], parts[1], st) : dh_finish<__half>(c, a, p, parts[0], parts[1], st);
     if (rc != QGBDT_OK) return rc;
     return qg_ws_close(c, st);
 }

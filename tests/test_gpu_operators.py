@@ -425,7 +425,7 @@ def test_softmax_ce_many_pieces(ctx):
 
 def test_softmax_ce_long_products(ctx):
     """Tiles of two accumulators, cut into fragments, over more than one piece."""
-    h, w, b, y = softmax_case(5000, 30000, 1024, torch.bfloat16, True, 0.1, 3)
+    h, w, b, y = softmax_case(5000, 31000, 1024, torch.bfloat16, True, 0.1, 3)
     e = softmax_exact(h, w, b, y)
     r = ctx.softmax_ce(h, w, y, bias=b)
     check_loss(r, e, h, w)
