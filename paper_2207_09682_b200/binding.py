@@ -5,9 +5,7 @@ library's kernels.  Loading fails loudly when the library has not been built.
 """
 from __future__ import annotations
 
-import array
 import ctypes as C
-import functools
 import os
 from typing import NamedTuple
 
@@ -31,12 +29,6 @@ EXPORTS = [
     "qgbdt_build_histograms_noalloc", "qgbdt_noalloc_last_error",
     "qgbdt_embed", "qgbdt_embed_backward", "qgbdt_softmax_ce", "qgbdt_softmax_ce_backward", "qgbdt_clip_grad_norm",
 ]
-
-# element and index types of the operators on top of the trees
-F32, BF16, F16 = 0, 1, 2
-I32, I64 = 0, 1
-_ELEMENT = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-_INDEX = {torch.int32: I32, torch.int64: I64}
 
 
 class QgbdtError(RuntimeError):
@@ -67,6 +59,19 @@ class Model(C.Structure):
 
 
 _lib = None
+_tensors = None
+
+
+def _load_tensors(lib):
+    """Loads the extension module that marshals tensors, and gives it the library's functions."""
+    global _tensors
+    path = os.path.join(_HERE, "_tensors.so")
+    if not os.path.exists(path):
+        raise ImportError("_tensors.so is not built: run `python -m paper_2207_09682_b200.build` (or __graft_entry__.build())")
+    from . import _tensors as module
+    module.bind(QgbdtError, *(C.cast(getattr(lib, "qgbdt_" + name), C.c_void_p).value for name in (
+        "embed", "embed_backward", "softmax_ce", "softmax_ce_backward", "clip_grad_norm", "last_error")))
+    _tensors = module
 
 
 def load_library() -> C.CDLL:
@@ -79,12 +84,7 @@ def load_library() -> C.CDLL:
         lib = C.CDLL(LIB_PATH)
         lib.qgbdt_last_error.restype = C.c_char_p
         lib.qgbdt_last_error.argtypes = [C.c_void_p]
-        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
-        lib.qgbdt_embed.argtypes = [p, p, i32, i64, i32, i64, p, i32, i64, i32, i64, C.c_float, p, i64, p, p]
-        lib.qgbdt_embed_backward.argtypes = [p, p, i32, i64, p, i32, i64, i32, i64, C.c_float, p, i64, i32, i64, p, p]
-        lib.qgbdt_softmax_ce.argtypes = [p, p, i64, p, i64, i32, p, p, i32, i64, i64, i32, p, p, p, p, p]
-        lib.qgbdt_softmax_ce_backward.argtypes = [p, p, i64, p, i64, i32, p, p, i32, i64, i64, i32, p, p, p, i64, p, i64, p, p, p]
-        lib.qgbdt_clip_grad_norm.argtypes = [p, p, p, p, p, i32, C.c_double, p, p]
+        _load_tensors(lib)
         _lib = lib
     return _lib
 
@@ -352,201 +352,59 @@ class SoftmaxCE(NamedTuple):
     lse: torch.Tensor
 
 
-# The calls below take a few microseconds on the GPU for small inputs, so their checks are kept short: sizes and strides
-# are fetched once per tensor, and devices compared by number.
-_raw_stream = torch._C._cuda_getCurrentRawStream   # the current stream's handle without a Stream object around it
+# The arguments of the calls below are taken apart by the extension module _tensors (csrc/tensors.cpp): tensors of the
+# context's device, matrices with contiguous rows of any row stride; anything else is refused with ERR_ARG.
+
+def _elsewhere(stream, call, *args):
+    """A call on another stream than the current one: its outputs are made there, and the allocator is told that its
+    inputs are in use there, so that neither is handed out again too early."""
+    with torch.cuda.stream(stream):
+        result = call(*args)
+    for a in args:
+        for t in a if isinstance(a, (list, tuple)) else (a,):
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
+    return result
 
 
-def _refuse(what: str):
-    raise QgbdtError(ERR_ARG, what)
-
-
-def _rows(t, name: str, device: int) -> tuple:
-    """(rows, columns, row stride) of a matrix on the context's device whose rows are contiguous."""
-    if t.get_device() != device:
-        _refuse("%s must be a CUDA tensor on the context's device" % name)
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2:
-        _refuse("%s must be a matrix" % name)
-    n, d = shape
-    if stride[1] != 1 and d > 1:
-        _refuse("%s must have contiguous rows" % name)
-    return n, d, stride[0] if n > 1 else d or 1
-
-
-def _token_rows(tokens, device: int) -> tuple:
-    """(rows, bag, row stride, index type) of tokens [N] or [N, bag]."""
-    kind = _INDEX.get(tokens.dtype, -1)
-    if kind < 0:
-        _refuse("tokens must be int32 or int64")
-    if tokens.dim() == 1:
-        if tokens.get_device() != device:
-            _refuse("tokens must be a CUDA tensor on the context's device")
-        n = tokens.shape[0]
-        return n, 1, tokens.stride()[0] if n > 1 else 1, kind
-    return (*_rows(tokens, "tokens", device), kind)
-
-
-def _words(t, dtype, count: int, name: str, device: int):
-    """Address of a contiguous vector of `count` elements (None: NULL)."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.numel() != count or not t.is_contiguous() or t.get_device() != device:
-        _refuse("%s must be a contiguous %s CUDA tensor of %d elements" % (name, str(dtype)[6:], count))
-    return t.data_ptr()
-
-
-def _streamed(call):
-    """A call on another stream than the current one makes its outputs there, and tells the allocator that its inputs
-    are in use there, so that neither is handed out again too early."""
-    @functools.wraps(call)
-    def run(self, *args, stream=None, **named):
-        if stream is None:
-            return call(self, *args, **named)
-        with torch.cuda.stream(stream):
-            result = call(self, *args, **named)
-        for a in (*args, *named.values()):
-            for t in a if isinstance(a, (list, tuple)) else (a,):
-                if isinstance(t, torch.Tensor):
-                    t.record_stream(stream)
-        return result
-    return run
-
-
-@_streamed
-def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None) -> torch.Tensor:
+def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, stream=None) -> torch.Tensor:
     """qgbdt_embed: out[i] = scale * sum_k table[tokens[i, k]].  table [V, D] (float32, bfloat16 or float16), tokens
     [N] or [N, bag] (int32 or int64, negative = missing); out [N, D] of the table's type is made if not given."""
-    dev, dtype = self.device, table.dtype
-    kind = _ELEMENT.get(dtype, -1)
-    if kind < 0:
-        _refuse("table must be float32, bfloat16 or float16")
-    v, d, ld = _rows(table, "table", dev)
-    n, bag, ldt, index = _token_rows(tokens, dev)
-    if out is None:
-        out, ldo = table.new_empty((n, d)), d
-    else:
-        no, do, ldo = _rows(out, "out", dev)
-        if no != n or do != d or out.dtype != dtype:
-            _refuse("out must be [N, D] of the table's type")
-    rc = self.lib.qgbdt_embed(self.h, table.data_ptr(), kind, v, d, ld, tokens.data_ptr(), index, n, bag, ldt, scale, out.data_ptr(), ldo,
-                              _words(status, torch.int32, 1, "status", dev), _raw_stream(dev))
-    if rc:
-        self._check(rc)
-    return out
+    if stream is not None:
+        return _elsewhere(stream, self.embed, table, tokens, scale, out, status)
+    return _tensors.embed(self.h.value or 0, self.device, table, tokens, scale, out, status)
 
 
-@_streamed
-def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None) -> torch.Tensor:
+def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None, stream=None) -> torch.Tensor:
     """qgbdt_embed_backward: the table's gradient [n_entries, D] of grad_out's type, every row of it written."""
-    dev, dtype = self.device, grad_out.dtype
-    kind = _ELEMENT.get(dtype, -1)
-    if kind < 0:
-        _refuse("grad_out must be float32, bfloat16 or float16")
-    rows, d, ld = _rows(grad_out, "grad_out", dev)
-    n, bag, ldt, index = _token_rows(tokens, dev)
-    if rows != n:
-        _refuse("grad_out and tokens differ in rows")
-    if grad_table is None:
-        grad_table, ldo = grad_out.new_empty((n_entries, d)), d
-    else:
-        no, do, ldo = _rows(grad_table, "grad_table", dev)
-        if no != n_entries or do != d or grad_table.dtype != dtype:
-            _refuse("grad_table must be [n_entries, D] of grad_out's type")
-    rc = self.lib.qgbdt_embed_backward(self.h, grad_out.data_ptr(), kind, ld, tokens.data_ptr(), index, n, bag, ldt, scale,
-                                       grad_table.data_ptr(), n_entries, d, ldo, _words(status, torch.int32, 1, "status", dev),
-                                       _raw_stream(dev))
-    if rc:
-        self._check(rc)
-    return grad_table
+    if stream is not None:
+        return _elsewhere(stream, self.embed_backward, grad_out, tokens, n_entries, scale, grad_table, status)
+    return _tensors.embed_backward(self.h.value or 0, self.device, grad_out, tokens, n_entries, scale, grad_table, status)
 
 
-def _softmax_inputs(hidden, weight, labels, bias, dev: int) -> tuple:
-    """The arguments that both directions begin with, and the sizes."""
-    dtype = hidden.dtype
-    if dtype != weight.dtype or dtype not in (torch.bfloat16, torch.float16):
-        _refuse("hidden and weight must both be bfloat16 or float16")
-    n, d, ldh = _rows(hidden, "hidden", dev)
-    v, dw, ldw = _rows(weight, "weight", dev)
-    if d != dw:
-        _refuse("hidden and weight differ in columns")
-    index = _INDEX.get(labels.dtype, -1)
-    if index < 0 or labels.dim() != 1:
-        _refuse("labels must be [N], int32 or int64")
-    return (hidden.data_ptr(), ldh, weight.data_ptr(), ldw, _ELEMENT[dtype], _words(bias, torch.float32, v, "bias", dev),
-            _words(labels, labels.dtype, n, "labels", dev), index, n, v, d), n, v, d
-
-
-@_streamed
-def _softmax_ce(self, hidden, weight, labels, bias=None, status=None) -> SoftmaxCE:
+def _softmax_ce(self, hidden, weight, labels, bias=None, status=None, stream=None) -> SoftmaxCE:
     """qgbdt_softmax_ce: softmax cross entropy of hidden [N, D] @ weight [V, D]^T + bias [V] against labels [N] (negative:
     no label), mean over the labelled rows, without stored logits.  hidden, weight bfloat16 or float16, bias float32."""
-    dev = self.device
-    inputs, n, _, _ = _softmax_inputs(hidden, weight, labels, bias, dev)
-    losses, lse, loss = torch.empty(2 * n + 1, dtype=torch.float32, device=hidden.device).split((n, n, 1))
-    rc = self.lib.qgbdt_softmax_ce(self.h, *inputs, loss.data_ptr(), losses.data_ptr(), lse.data_ptr(),
-                                   _words(status, torch.int32, 1, "status", dev), _raw_stream(dev))
-    if rc:
-        self._check(rc)
-    return SoftmaxCE(loss, losses, lse)
+    if stream is not None:
+        return _elsewhere(stream, self.softmax_ce, hidden, weight, labels, bias, status)
+    return SoftmaxCE(*_tensors.softmax_ce(self.h.value or 0, self.device, hidden, weight, labels, bias, status))
 
 
-@_streamed
 def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss=None, grad_hidden=None, grad_weight=None,
-                         status=None) -> tuple:
+                         status=None, stream=None) -> tuple:
     """qgbdt_softmax_ce_backward: (grad_hidden [N, D], grad_weight [V, D], grad_bias [V] or None) of grad_loss * loss;
     lse as softmax_ce gave it, grad_loss a float32 CUDA tensor of one element (None: 1)."""
-    dev, dtype = self.device, hidden.dtype
-    inputs, n, v, d = _softmax_inputs(hidden, weight, labels, bias, dev)
-
-    def made(t, rows, name):
-        if t is None:
-            return hidden.new_empty((rows, d)), d
-        no, do, ld = _rows(t, name, dev)
-        if no != rows or do != d or t.dtype != dtype:
-            _refuse("%s must be [%d, %d] of hidden's type" % (name, rows, d))
-        return t, ld
-
-    grad_hidden, ldh = made(grad_hidden, n, "grad_hidden")
-    grad_weight, ldw = made(grad_weight, v, "grad_weight")
-    grad_bias = None if bias is None else torch.empty(v, dtype=torch.float32, device=hidden.device)
-    rc = self.lib.qgbdt_softmax_ce_backward(
-        self.h, *inputs, _words(lse, torch.float32, n, "lse", dev), _words(grad_loss, torch.float32, 1, "grad_loss", dev),
-        grad_hidden.data_ptr(), ldh, grad_weight.data_ptr(), ldw, None if grad_bias is None else grad_bias.data_ptr(),
-        _words(status, torch.int32, 1, "status", dev), _raw_stream(dev))
-    if rc:
-        self._check(rc)
-    return grad_hidden, grad_weight, grad_bias
+    if stream is not None:
+        return _elsewhere(stream, self.softmax_ce_backward, hidden, weight, labels, lse, bias, grad_loss, grad_hidden, grad_weight, status)
+    return _tensors.softmax_ce_backward(self.h.value or 0, self.device, hidden, weight, labels, bias, lse, grad_loss, grad_hidden, grad_weight, status)
 
 
-@_streamed
-def _clip_grad_norm(self, grads, max_norm: float, out=None) -> torch.Tensor:
-    """qgbdt_clip_grad_norm: the global norm (float32 tensor [1]) of a list of tensors, and every tensor times
+def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """qgbdt_clip_grad_norm: the global norm (float32 tensor [1]) of a list of contiguous tensors, and every tensor times
     min(1, max_norm / norm), in place or into the tensors of `out`.  float32, bfloat16 and float16 may be mixed."""
-    dev, n = self.device, len(grads)
-
-    def table(tensors, what):
-        for t in tensors:
-            if t.get_device() != dev or not t.is_contiguous():
-                _refuse("%s must be contiguous CUDA tensors on the context's device" % what)
-        return array.array("Q", [t.data_ptr() for t in tensors])
-
-    dtypes, sizes = [t.dtype for t in grads], [t.numel() for t in grads]
-    kinds = array.array("i", [_ELEMENT.get(t, -1) for t in dtypes])
-    if -1 in kinds:
-        _refuse("gradients must be float32, bfloat16 or float16")
-    src = dst = table(grads, "gradients")
-    if out is not None:
-        if [t.numel() for t in out] != sizes or [t.dtype for t in out] != dtypes:
-            _refuse("out must match the gradients in number, sizes and types")
-        dst = table(out, "out")
-    counts = array.array("q", sizes)
-    norm = torch.empty(1, dtype=torch.float32, device=torch.device("cuda", dev))
-    rc = self.lib.qgbdt_clip_grad_norm(self.h, src.buffer_info()[0], dst.buffer_info()[0], counts.buffer_info()[0], kinds.buffer_info()[0], n,
-                                       max_norm, norm.data_ptr(), _raw_stream(dev))
-    if rc:
-        self._check(rc)
-    return norm
+    if stream is not None:
+        return _elsewhere(stream, self.clip_grad_norm, grads, max_norm, out)
+    return _tensors.clip_grad_norm(self.h.value or 0, self.device, grads, max_norm, out)
 
 
 Context.embed = _embed

@@ -1,4 +1,5 @@
-"""Builds libqgbdt.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Builds libqgbdt.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _tensors.so, the module that
+hands torch tensors to it, with the C++ compiler.
 
 Every .cu file is compiled to an object of its own (in parallel, only when it or a header is
 newer than the object), then the objects are linked into the shared library."""
@@ -15,6 +16,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqgbdt.so")
+TENSORS_SRC = os.path.join(CSRC, "tensors.cpp")
+TENSORS = os.path.join(HERE, "_tensors.so")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-fmad=false",
@@ -34,6 +37,29 @@ def _obj(src: str) -> str:
     return os.path.join(OBJ_DIR, os.path.basename(src)[:-3] + ".o")
 
 
+def tensors_stale() -> bool:
+    newest = max(os.path.getmtime(f) for f in [TENSORS_SRC, os.path.join(ROOT, "include", "qgbdt.h"), os.path.abspath(__file__)])
+    return not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < newest
+
+
+def build_tensors(force: bool = False) -> str:
+    if not force and not tensors_stale():
+        return TENSORS
+    import sysconfig
+
+    import torch
+    torch_dir = os.path.dirname(torch.__file__)
+    tmp = TENSORS + ".tmp.%d" % os.getpid()
+    subprocess.check_call(
+        [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+         "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(torch_dir, "include"),
+         "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+         "-isystem", os.path.join(os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"))), "include"),
+         TENSORS_SRC, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp])
+    os.replace(tmp, TENSORS)
+    return TENSORS
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
@@ -42,6 +68,7 @@ def is_stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_tensors(force)
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
