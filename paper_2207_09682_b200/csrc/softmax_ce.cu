@@ -854,19 +854,33 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, FEW_BLOCKS) k_loss_few(const F
     __syncthreads();
     if (!last) return;
     __threadfence();
-    if (warp < R && warp < a.rows) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {   // all threads for a row after the other; eight statistics in flight each
+        if (r >= a.rows) break;
         float m0 = -INFINITY, l0 = 0.0f;
-        const volatile float2 *q = a.stat + warp * gridDim.x;
-        for (int t = lane; t < (int)gridDim.x; t += 32) join(m0, l0, q[t].x, q[t].y);
+        const float2 *q = a.stat + r * gridDim.x;
+        for (int t = threadIdx.x; t < (int)gridDim.x; t += FEW_WARPS * 32 * 8) {
+            float2 s[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s[u] = __ldcg(q + min(t + u * FEW_WARPS * 32, (int)gridDim.x - 1));
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (t + u * FEW_WARPS * 32 < (int)gridDim.x) join(m0, l0, s[u].x, s[u].y);
+        }
 #pragma unroll
         for (int o = 16; o; o >>= 1) join(m0, l0, __shfl_xor_sync(0xffffffffu, m0, o), __shfl_xor_sync(0xffffffffu, l0, o));
-        if (lane == 0) {
-            const bool labelled = (R == 1 || warp == 0 ? label[0] : label[R - 1]) >= 0;
-            const float lse = labelled ? m0 + logf(l0) : 0.0f, loss = labelled ? lse - *(volatile float *)&a.z_label[warp] : 0.0f;
-            a.lse[warp] = lse;
-            if (a.losses) a.losses[warp] = loss;
-            row_loss[warp] = loss;
-        }
+        __syncthreads();
+        if (lane == 0) part[warp][r] = make_float2(m0, l0);
+    }
+    __syncthreads();
+    if (threadIdx.x < R && threadIdx.x < a.rows) {
+        float2 s = part[0][threadIdx.x];
+        for (int w = 1; w < FEW_WARPS; ++w) join(s.x, s.y, part[w][threadIdx.x].x, part[w][threadIdx.x].y);
+        const bool labelled = (threadIdx.x == 0 ? label[0] : label[R - 1]) >= 0;
+        const float lse = labelled ? s.x + logf(s.y) : 0.0f, loss = labelled ? lse - __ldcg(a.z_label + threadIdx.x) : 0.0f;
+        a.lse[threadIdx.x] = lse;
+        if (a.losses) a.losses[threadIdx.x] = loss;
+        row_loss[threadIdx.x] = loss;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
