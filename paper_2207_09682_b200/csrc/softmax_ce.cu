@@ -8,10 +8,10 @@
 // memory that grows with rows * classes), and the two products with g.  8 * rows * classes * dim operations
 // in all; a step that kept the logits would need 6.
 //
-// One kernel carries all four: a persistent grid whose CTAs (or pairs of CTAs) take tiles of 128 (256) rows by
-// 256 columns in turn.  One warp fills a ring of operand tiles with tiled copies, one thread issues the
-// matrix instructions, four warps empty the accumulators, of which tensor memory holds two, so that the
-// epilogue of a tile runs under the products of the next.  What the epilogues do:
+// One kernel carries all four: a persistent grid whose pairs of CTAs take tiles of 256 rows by 256 columns.  One
+// warp fills a ring of operand tiles with tiled copies, one thread issues the matrix instructions, eight warps
+// empty the accumulators, of which tensor memory holds two, so that the epilogue of a tile runs under the
+// products of the next.  What the epilogues do:
 //   LOSS  per row of the tile: maximum and sum of exponentials; the label's logit.  No logit leaves the SM.
 //   GRAD  g of a piece of the classes, rounded to the inputs' type (relative error 2^-8 in bf16, 2^-11 in f16,
 //         of each g on its own: as much as the outputs' own rounding, averaged down by the sums that follow;
@@ -19,6 +19,13 @@
 //         column sums in single precision for the bias.
 //   DH    the piece's contribution to dH, in single precision.
 //   DW    rows of dW, complete with every piece, written in the output type.
+//
+// Measured (7373 labelled rows x 65536 classes x 1024, bf16): LOSS 625 us, 1.58 PFLOP/s, the tensor cores 87 %
+// busy, bound by them and by power (1000 W: in a loop 1.25-1.3 PFLOP/s, what library products of these shapes
+// reach); GRAD 0.64 ms (77 %: its epilogue writes 1 GB of g), DH 0.60 ms, DW 0.56 ms (84-89 %, bound by what L2
+// delivers, about 12 TB/s); all of the gradient, launches and joins included, 2.5 ms.  With dim below about 400
+// the epilogues bound LOSS and GRAD: 16 exponentials per clock and SM (dim 64: 537 million logits in 222 us,
+// 120 us for the exponentials alone).
 //
 // Rows without a label are taken out first: the labelled rows are packed to the front of a copy of H (which
 // also gives the copies their alignment).  Nothing is computed for the others, and what they hold, infinities
