@@ -69,10 +69,6 @@ struct RawLabels {
     __device__ __forceinline__ long long raw(int i) const {
         return type == QGBDT_I64 ? reinterpret_cast<const long long *>(p)[i] : (long long)reinterpret_cast<const int *>(p)[i];
     }
-    __device__ __forceinline__ int operator[](int i) const {   // -1: none
-        const long long l = raw(i);
-        return l >= 0 && l < classes ? (int)l : -1;
-    }
 };
 
 struct GemmArgs {
@@ -109,14 +105,24 @@ __device__ __forceinline__ float out_scale(const float *grad_loss, int count) {
     return (grad_loss ? *grad_loss : 1.0f) / (float)(count > 0 ? count : 1);
 }
 
-// Tile t in the order in which tiles are taken: groups of GROUP_M row tiles, in a group all row tiles of a
-// column tile before the next, so that CTAs that run together share both operands in L2.
-__device__ __forceinline__ void tile_place(int t, int m_live, int n_tiles, int &m, int &n) {
-    const int group = t / (GROUP_M * n_tiles), m0 = group * GROUP_M, gm = min(GROUP_M, m_live - m0);
-    t -= group * GROUP_M * n_tiles;
-    n = t / gm;
-    m = m0 + t - n * gm;
-}
+// The tiles of LOSS and GRAD in the order in which they are taken: groups of GROUP_M row tiles, in a group all row
+// tiles of a column tile before the next, so that CTAs that run together share both operands in L2.  A unit's next tile
+// is `step` further on; kept as group and place in it, since divisions would stand in front of every tile's epilogue.
+struct TileWalk {
+    int m0, rows, place, size;   // first row tile of the group, its row tiles; place in the group, its tiles
+    int m_live, n_tiles, step;
+    __device__ TileWalk(int m_live_, int n_tiles_, int first, int step_) : m0(0), place(first), m_live(m_live_), n_tiles(n_tiles_), step(step_) { group(); }
+    __device__ __forceinline__ void group() { rows = min(GROUP_M, m_live - m0), size = rows * n_tiles; }
+    __device__ __forceinline__ bool next(int &m, int &n) {
+        while (m0 < m_live && place >= size) place -= size, m0 += GROUP_M, group();
+        if (m0 >= m_live) return false;
+        n = rows == GROUP_M ? place / GROUP_M : place / rows;
+        m = m0 + place - n * rows;
+        place += step;
+        return true;
+    }
+};
+
 // DH and DW have few tiles and long products, so whole tiles would leave SMs idle in the last round, and their
 // first operand, g, is larger than L2.  Units (pairs of CTAs) work in gangs: the units of a gang take neighbouring
 // column tiles of the same rows and walk along the products together, so that a block of g comes out of DRAM once
@@ -154,15 +160,13 @@ struct Work {
 };
 template <int MODE, int NB>
 struct Schedule {
-    int t, step, total, m_live, n_tiles, dim, kb, unit, gang, member, size;
+    int m_live, n_tiles, dim, kb, unit, gang, member, size;
+    TileWalk walk;
     long long pos, end;
-    __device__ Schedule(const GemmArgs &a, int count) : n_tiles(a.n_tiles), dim(a.dim) {
-        m_live = MODE == DW ? a.m_tiles : (count + BM - 1) / BM;
+    __device__ Schedule(const GemmArgs &a, int count)
+        : m_live(MODE == DW ? a.m_tiles : (count + BM - 1) / BM), n_tiles(a.n_tiles), dim(a.dim), walk(m_live, n_tiles, blockIdx.x / CG, gridDim.x / CG) {
         kb = MODE == DW ? (count + BK - 1) / BK : a.kb;
         unit = blockIdx.x / CG;
-        step = gridDim.x / CG;
-        total = m_live * n_tiles;
-        t = unit;
         pos = end = 0;
         if (MODE == DH || MODE == DW) {
             size = a.gang, gang = unit / size, member = unit - gang * size;
@@ -172,11 +176,8 @@ struct Schedule {
     }
     __device__ __forceinline__ bool next(Work &w) {
         if (MODE == LOSS || MODE == GRAD) {
-            if (t >= total) return false;
-            tile_place(t, m_live, n_tiles, w.m, w.n);
             w.kb0 = 0, w.kb1 = kb, w.cols = BN;
-            t += step;
-            return true;
+            return walk.next(w.m, w.n);
         } else {
             while (pos < end) {
                 const int place = (int)(pos / kb), round = place / m_live;   // row tiles of round 0, of round 1, ...
@@ -243,14 +244,57 @@ struct Epilogue {
         if (MODE == DW) scale = out_scale(a.grad_loss, count);
     }
 
+    // What the next tile's rows need from memory, loaded under this tile's work and not looked at before begin().
+    // The bias of the warp's 128 columns: four per lane, minus infinity behind the last class.
+    int label_lo, label_hi;
+    float lse_next;
+    float4 bias_next, bias_now;
+    __device__ __forceinline__ void fetch(const Work &w, int rank, int quarter, int half) {
+        if (MODE != LOSS && MODE != GRAD) return;
+        if (a.bias) {
+            const int v = a.v0 + w.n * BN + half * 128 + lane * 4;
+            if (a.bias_vec && v + 4 <= a.classes) {
+                bias_next = __ldg(reinterpret_cast<const float4 *>(a.bias + v));
+            } else {
+                bias_next.x = v < a.classes ? __ldg(a.bias + v) : -INFINITY;
+                bias_next.y = v + 1 < a.classes ? __ldg(a.bias + v + 1) : -INFINITY;
+                bias_next.z = v + 2 < a.classes ? __ldg(a.bias + v + 2) : -INFINITY;
+                bias_next.w = v + 3 < a.classes ? __ldg(a.bias + v + 3) : -INFINITY;
+            }
+        }
+        const int r = w.m * BM + rank * 128 + quarter * 32 + lane;
+        label_lo = label_hi = -1;
+        if (r >= count) return;
+        if (a.label) {
+            label_lo = a.label[r];
+        } else if (a.labels.type == QGBDT_I64) {
+            label_lo = reinterpret_cast<const int *>(a.labels.p)[2ll * r], label_hi = reinterpret_cast<const int *>(a.labels.p)[2ll * r + 1];
+        } else {
+            label_lo = reinterpret_cast<const int *>(a.labels.p)[r];
+        }
+        if (MODE == GRAD) lse_next = a.lse[r];
+    }
+
     __device__ __forceinline__ void begin(const Work &w, int rank, int quarter, int half) {
         c = w;
         row_in = w.m * BM + rank * 128 + quarter * 32;
         row = row_in + lane;
         col0 = w.n * BN * NB + half * (BN * NB / 2);
         live = row < count;
-        if (MODE == LOSS || MODE == GRAD) label = !live ? -1 : a.label ? a.label[row] : a.labels[row];
-        if (MODE == GRAD) lse = live ? a.lse[row] : 0.0f;
+        if (MODE == LOSS || MODE == GRAD) {   // a label that is none, or out of range, meets no column
+            label = live && (unsigned)label_lo < (unsigned)a.classes ? label_lo : -1;
+            if (!a.label && a.labels.type == QGBDT_I64 && label_hi != 0) label = -1;
+        }
+        if (MODE == GRAD) lse = live ? lse_next : 0.0f;
+        if ((MODE == LOSS || MODE == GRAD) && a.bias) {
+            bias_now = bias_next;
+            if (MODE == LOSS) {   // LOSS does not stage anything else: all lanes read the bias from there
+                __syncwarp();
+                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(buf + lane * 16), "f"(bias_now.x), "f"(bias_now.y), "f"(bias_now.z), "f"(bias_now.w)
+                             : "memory");
+                __syncwarp();
+            }
+        }
     }
 
     // The staging buffer may be written: the copy out of it has been read.
@@ -281,21 +325,25 @@ struct Epilogue {
         }
     }
 
-    // Bias, and minus infinity behind the last class, for N logits from class v on.
+    // Bias, or minus infinity behind the last class, for N logits from the warp's column j0 on.
     template <int N>
-    __device__ __forceinline__ void logits(float (&x)[N], int v) {
-        if (a.bias && !(a.bias_vec && v + N <= a.classes)) {
+    __device__ __forceinline__ void logits(float (&x)[N], int j0) {
+        const int v = a.v0 + col0 + j0;
+        if (a.bias) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) x[j] += __ldg(a.bias + min(v + j, a.classes - 1));
-        } else if (a.bias) {
-#pragma unroll
-            for (int j = 0; j < N / 4; ++j) {
-                const float4 b = __ldg(reinterpret_cast<const float4 *>(a.bias + v) + j);
-                tc_add2(x[4 * j], x[4 * j + 1], b.x, b.y);
-                tc_add2(x[4 * j + 2], x[4 * j + 3], b.z, b.w);
+            for (int j = 0; j < N; j += 4) {
+                float4 b;
+                if (MODE == LOSS) {
+                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b.x), "=f"(b.y), "=f"(b.z), "=f"(b.w) : "r"(buf + (j0 + j) * 4));
+                } else {
+                    const int from = (j0 + j) / 4;
+                    b.x = __shfl_sync(0xffffffffu, bias_now.x, from), b.y = __shfl_sync(0xffffffffu, bias_now.y, from);
+                    b.z = __shfl_sync(0xffffffffu, bias_now.z, from), b.w = __shfl_sync(0xffffffffu, bias_now.w, from);
+                }
+                tc_add2(x[j], x[j + 1], b.x, b.y);
+                tc_add2(x[j + 2], x[j + 3], b.z, b.w);
             }
-        }
-        if (v + N > a.classes) {
+        } else if (v + N > a.classes) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (v + j >= a.classes) x[j] = -INFINITY;
@@ -304,15 +352,18 @@ struct Epilogue {
 
     // LOSS: all 128 columns of the warp at once; no logit waits for a running maximum.
     __device__ __forceinline__ void row_statistics(float (&x)[128], int half) {
-        const int v = a.v0 + col0, lj = label - v;
-        logits(x, v);
+        const int lj = label - (a.v0 + col0);
+        logits(x, 0);
         const bool mine = lj >= 0 && lj < 128;
         if (__any_sync(0xffffffffu, mine)) {
-            float z = x[0];
+            float z[64];   // x[lj], by the bits of lj
 #pragma unroll
-            for (int j = 1; j < 128; ++j)
-                if (lj == j) z = x[j];
-            if (mine) a.z_label[row] = z;
+            for (int j = 0; j < 64; ++j) z[j] = lj & 64 ? x[j + 64] : x[j];
+#pragma unroll
+            for (int o = 32; o; o >>= 1)
+#pragma unroll
+                for (int j = 0; j < o; ++j) z[j] = lj & o ? z[j + o] : z[j];
+            if (mine) a.z_label[row] = z[0];
         }
         float t[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
@@ -331,9 +382,9 @@ struct Epilogue {
 
     // GRAD: 64 columns, left or right half of the warp's.
     __device__ __forceinline__ void gradients(float (&x)[64], int h) {
-        const int col = col0 + h * 64, v = a.v0 + col, lj = label - v;
+        const int col = col0 + h * 64, lj = label - (a.v0 + col);
         const bool mine = lj >= 0 && lj < 64;
-        logits(x, v);
+        logits(x, h * 64);
         exponentials(x, lse);
         if (__any_sync(0xffffffffu, mine)) {
 #pragma unroll
@@ -538,9 +589,14 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
         const int quarter = warp & 3, half = (warp - 4) >> 2;
         Epilogue<MODE, NB> epi(a, &map_out, &map_part, store_at + (warp - 4) * Layout<MODE, NB>::BUFFERS * STORE_BYTES, lane, count);
         int n_acc = 0;
-        while (todo.next(c)) {
+        Work following;
+        bool more = todo.next(c);
+        if (more) epi.fetch(c, (int)rank, quarter, half);
+        for (; more; c = following) {
             const int b = n_acc % ACCS;
             epi.begin(c, (int)rank, quarter, half);
+            more = todo.next(following);
+            if (more) epi.fetch(following, (int)rank, quarter, half);
             if (!(ok = __all_sync(0xffffffffu, tc_bar_wait(acc_full(b), n_acc / ACCS & 1, &stop)))) break;
             tc_fence_after();
             const uint32_t tacc = tmem + ((uint32_t)(quarter * 32) << 16) + b * ACC_COLS + half * (BN * NB / 2);
@@ -568,14 +624,11 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
                 tc_ld_32(tacc + 32, r[1]);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    if (h == 1) tc_ld_32(tacc + 96, r[3]);   // (all four at once would not fit the registers)
                     tc_ld_wait(r[2 * h]);
                     tc_ld_wait(r[2 * h + 1]);
-                    if (h == 0) {   // read under the arithmetic of the first half
-                        tc_ld_32(tacc + 64, r[2]);
-                        tc_ld_32(tacc + 96, r[3]);
-                    } else {
-                        hand_back();
-                    }
+                    if (h == 0) tc_ld_32(tacc + 64, r[2]);   // read under the arithmetic of the first half
+                    else hand_back();
                     float x[64];
 #pragma unroll
                     for (int j = 0; j < 64; ++j) x[j] = __uint_as_float(r[2 * h + j / 32][j % 32]);
