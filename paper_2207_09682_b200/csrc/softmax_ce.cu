@@ -162,16 +162,22 @@ template <int MODE, int NB>
 struct Schedule {
     int m_live, n_tiles, dim, kb, unit, gang, member, size;
     TileWalk walk;
-    long long pos, end;
+    int place, m, round, k;   // DH and DW: the tile the run has come to, its row tile and round, the block in it
+    long long left;           // blocks of the run still to come
     __device__ Schedule(const GemmArgs &a, int count)
         : m_live(MODE == DW ? a.m_tiles : (count + BM - 1) / BM), n_tiles(a.n_tiles), dim(a.dim), walk(m_live, n_tiles, blockIdx.x / CG, gridDim.x / CG) {
         kb = MODE == DW ? (count + BK - 1) / BK : a.kb;
         unit = blockIdx.x / CG;
-        pos = end = 0;
+        left = 0;
         if (MODE == DH || MODE == DW) {
             size = a.gang, gang = unit / size, member = unit - gang * size;
             const Line line(a.rounds * m_live, kb, a.gangs, a.split);
-            if (line.length > 0 && gang < line.runs) pos = line.start(gang), end = line.start(gang + 1);
+            if (line.length > 0 && gang < line.runs) {
+                const long long pos = line.start(gang);
+                left = line.start(gang + 1) - pos;
+                place = (int)(pos / kb), k = (int)(pos - (long long)place * kb);
+                round = place / m_live, m = place - round * m_live;   // row tiles of round 0, of round 1, ...
+            }
         }
     }
     __device__ __forceinline__ bool next(Work &w) {
@@ -179,16 +185,17 @@ struct Schedule {
             w.kb0 = 0, w.kb1 = kb, w.cols = BN;
             return walk.next(w.m, w.n);
         } else {
-            while (pos < end) {
-                const int place = (int)(pos / kb), round = place / m_live;   // row tiles of round 0, of round 1, ...
-                w.m = place - round * m_live;
+            while (left > 0) {
+                w.m = m;
                 w.n = round * size + member;
-                w.kb0 = (int)(pos - (long long)place * kb);
-                w.kb1 = (int)min((long long)kb, w.kb0 + end - pos);
+                w.kb0 = k;
+                w.kb1 = (int)min((long long)kb, k + left);
                 w.whole = w.kb0 == 0 && w.kb1 == kb;
                 w.cols = min(BN * NB, (dim - w.n * BN * NB + 127) / 128 * 128);
                 w.fragment = MODE == DH ? (place + gang) * size + member : 2 * unit + (w.kb0 == 0);
-                pos += w.kb1 - w.kb0;
+                left -= w.kb1 - w.kb0;
+                k = 0, ++place;
+                if (++m == m_live) m = 0, ++round;
                 if (w.n < n_tiles) return true;   // the last round may have fewer column tiles than the gang units
             }
             return false;
@@ -1357,7 +1364,7 @@ int64_t piece_width(const qgbdt_ctx *c, int64_t classes, int n_pad, int dim) {
 template <typename T>
 int dh_finish(qgbdt_ctx *c, const SoftmaxArgs &a, const PackArgs &p, const DhParts &full, const DhParts &rest, cudaStream_t st) {
     int lg = 0;
-    while (lg < 6 && (4 << lg) < a.dim) ++lg;
+    while (lg < (a.rows < 4096 ? 8 : 6) && (4 << lg) < a.dim) ++lg;   // few rows: as many threads per row as there are columns
     return qg_launch(c, k_dh_finish<T>, dim3((unsigned)((a.rows + (256 >> lg) - 1) / (256 >> lg))), 256, 0, st, full, rest, p.pos_of, (int)a.rows, a.dim,
                      a.grad_loss, p.count, reinterpret_cast<T *>(a.d_hidden), a.ld_d_hidden, lg);
 }
