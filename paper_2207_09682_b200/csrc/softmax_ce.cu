@@ -1096,7 +1096,7 @@ __global__ void __launch_bounds__(256) k_dh_finish(const DhParts full, const DhP
     const int r = blockIdx.x * (256 >> lg) + (threadIdx.x >> lg), lane = threadIdx.x & ((1 << lg) - 1);
     if (r >= rows) return;
     const int n = *count, p = pos_of[r], m_live = (n + BM - 1) / BM;
-    const float scale = out_scale(grad_loss, n);
+    const float scale = p >= 0 ? out_scale(grad_loss, n) : 0.0f;   // (an infinite grad_loss times 0 would be NaN)
     // of one set: the gangs g0 to g1 that worked on the row's tile in a round
     struct Span {
         int round = -1, place, g0, g1;
@@ -1159,7 +1159,7 @@ __global__ void __launch_bounds__(256) k_bias_finish(const float *part, int cols
     __syncthreads();
     if (k == 0 && v < n) {
         for (int j = 1; j < 8; ++j) s += w[j][threadIdx.x];
-        out[v] = s * out_scale(grad_loss, *count);
+        out[v] = *count > 0 ? s * out_scale(grad_loss, *count) : 0.0f;
     }
 }
 

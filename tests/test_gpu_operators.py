@@ -415,7 +415,7 @@ def test_softmax_ce_without_rows_or_labels(ctx):
 
 
 def test_softmax_ce_many_pieces(ctx):
-    """More classes than one piece of the probabilities holds (2^27 / rows)."""
+    """More classes than one piece of the probabilities holds (3 * 2^26 / rows)."""
     h, w, b, y = softmax_case(40000, 5000, 16, torch.bfloat16, True, 0.4, 6)
     e = softmax_exact(h, w, b, y)
     r = ctx.softmax_ce(h, w, y, bias=b)
@@ -424,12 +424,33 @@ def test_softmax_ce_many_pieces(ctx):
 
 
 def test_softmax_ce_long_products(ctx):
-    """Tiles of two accumulators, cut into fragments, over more than one piece."""
+    """Tiles of two accumulators, cut into fragments."""
     h, w, b, y = softmax_case(5000, 31000, 1024, torch.bfloat16, True, 0.1, 3)
     e = softmax_exact(h, w, b, y)
     r = ctx.softmax_ce(h, w, y, bias=b)
     check_loss(r, e, h, w)
     check_grads(ctx.softmax_ce_backward(h, w, y, r.lse, bias=b), e, h, w, torch.bfloat16)
+
+
+@pytest.mark.parametrize("rows,classes,dim,dtype", [(5000, 90000, 1024, "bf16"), (20000, 31000, 40, "f16")])
+def test_softmax_ce_several_pieces_and_a_narrow_last_one(ctx, rows, classes, dim, dtype):
+    """Fragments of the hidden rows' gradient that three pieces and more add to, whole tiles and cut ones."""
+    h, w, b, y = softmax_case(rows, classes, dim, DTYPES[dtype], True, 0.1, 4)
+    e = softmax_exact(h, w, b, y, 1024.0)
+    r = ctx.softmax_ce(h, w, y, bias=b)
+    check_loss(r, e, h, w)
+    check_grads(ctx.softmax_ce_backward(h, w, y, r.lse, bias=b, grad_loss=torch.full((1,), 1024.0, device="cuda")), e, h, w, DTYPES[dtype])
+
+
+def test_softmax_ce_infinite_grad_loss_leaves_rows_without_a_label_at_zero(ctx):
+    h, w, b, y = softmax_case(300, 70, 24, torch.float16, True, 0.4, 5)
+    inf = torch.full((1,), math.inf, device="cuda")
+    r = ctx.softmax_ce(h, w, y, bias=b)
+    dh, dw, db = ctx.softmax_ce_backward(h, w, y, r.lse, bias=b, grad_loss=inf)
+    assert not dh[y < 0].any() and not torch.isfinite(dh[y >= 0]).any()
+    y[:] = -1
+    dh, dw, db = ctx.softmax_ce_backward(h, w, y, ctx.softmax_ce(h, w, y, bias=b).lse, bias=b, grad_loss=inf)
+    assert not dh.any() and not dw.any() and not db.any()
 
 
 def test_softmax_ce_gradient_by_differences(ctx):
