@@ -12,6 +12,8 @@
 // tile adding rows until the token changes.  A token whose pairs cross a tile border leaves partial sums
 // that a second kernel adds in tile order.  Equal tile lengths keep the work even however the tokens
 // crowd, and the order of every sum depends on the tokens alone.
+#include <type_traits>
+
 #include "ops_internal.cuh"
 
 namespace {
@@ -167,7 +169,25 @@ struct SortArgs {
     const void *tokens;
     long long ld_tokens, n_entries, n;   // n pairs
     unsigned bag, div_mul, div_shift;    // i / bag == (i * div_mul) >> div_shift in 64 bits, for i < 2^31
+    int row_bits;                        // of a packed pair
     int32_t *status;
+};
+
+// A pair between two passes: token and row in one word where both fit (every usual size), or in two.  The last pass
+// writes two words in any case.
+template <bool PACKED>
+struct Pair {
+    using E = uint2;
+    static __device__ __forceinline__ E make(unsigned key, unsigned row, int) { return make_uint2(key, row); }
+    static __device__ __forceinline__ unsigned word(E p) { return p.x; }   // the digits are taken from this one
+    static __device__ __forceinline__ uint2 wide(E p, int) { return p; }
+};
+template <>
+struct Pair<true> {
+    using E = unsigned;
+    static __device__ __forceinline__ E make(unsigned key, unsigned row, int row_bits) { return key << row_bits | row; }
+    static __device__ __forceinline__ unsigned word(E p) { return p; }
+    static __device__ __forceinline__ uint2 wide(E p, int row_bits) { return make_uint2(p >> row_bits, p & ((1u << row_bits) - 1)); }
 };
 
 // floor(i / d) for i < 2^31 as a product: with shift = 31 + ceil(log2 d) and mul = ceil(2^shift / d), mul < 2^32 and the
@@ -229,9 +249,10 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, ui
 }
 
 // Many pairs: least significant digit first, up to 9 bits a pass; a pass is a count per block and digit, a
-// scan, and a stable scatter.  A block scatters tiles of 4096 pairs: every warp ranks its pairs among its own by
-// matching digits across the lanes (a ballot per bit), the tile is put in order in shared memory, and runs of equal digits leave it
-// as neighbouring words.
+// scan, and a stable scatter.  A block scatters tiles of 2048 pairs: every warp ranks its pairs among its own (each
+// lane sets its bit in a word per digit, and reads who else did), the tile is put in order in shared memory, and runs of
+// equal digits leave it as neighbouring words.  6.55 M pairs of 15 + 16 bits: 38 us per scatter, bound by instruction
+// issue and conflicts in shared memory (digits compared with a ballot per bit: 51 us); counts 11 to 14 us.
 constexpr int SORT_MIN_BITS = 6, SORT_MAX_BITS = 9;
 constexpr int SORT_WARPS = EMB_THREADS / 32;
 constexpr int SORT_ROUNDS = 8;                                    // pairs per lane and tile
@@ -240,8 +261,8 @@ constexpr int SORT_TILE = EMB_THREADS * SORT_ROUNDS;
 // Counts of a digit, one per block, padded to 16 bytes.
 __host__ __device__ inline size_t count_stride(int blocks) { return ((size_t)blocks + 3) / 4 * 4; }
 
-template <typename I, bool FIRST>
-__global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const uint2 *in, int shift, int bits, long long per_block,
+template <typename I, bool FIRST, bool PACKED>
+__global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const typename Pair<PACKED>::E *in, int shift, int bits, long long per_block,
                                                             unsigned *counts) {
     qg_after_prior();
     extern __shared__ unsigned sort_smem[];
@@ -256,7 +277,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, co
 #pragma unroll
         for (int r = 0; r < LOADS; ++r) {
             const long long at = min(i + r * EMB_THREADS, i1 - 1);
-            key[r] = FIRST ? token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, (unsigned)at)) : in[at].x;
+            key[r] = FIRST ? token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, (unsigned)at)) : Pair<PACKED>::word(in[at]);
         }
         bool bad = false;
 #pragma unroll
@@ -293,7 +314,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_scan(unsigned *counts, uns
     if (lane == 0) totals[d] = run;
 }
 
-size_t scatter_smem(int bits) { return (size_t)SORT_TILE * sizeof(uint2) + ((size_t)8 + 2 * SORT_WARPS) * ((size_t)1 << bits); }
+size_t scatter_smem(int bits, size_t pair) { return (size_t)SORT_TILE * pair + ((size_t)8 + 6 * SORT_WARPS) * ((size_t)1 << bits); }   // below 48 KB
 
 // Exclusive scan over the block of one number per thread.
 __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
@@ -316,18 +337,22 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
 // takes less time than a launch for it.
 constexpr int SORT_FEW_BLOCKS = 128;
 
-template <typename I, bool FIRST, int BITS>
-__global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const uint2 *in, int shift, long long per_block, const unsigned *counts,
-                                                              const unsigned *totals, uint2 *out) {
+template <typename I, bool FIRST, bool PACKED, bool LAST, int BITS>
+__global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const typename Pair<PACKED>::E *in, int shift, long long per_block,
+                                                                 const unsigned *counts, const unsigned *totals, void *out) {
     qg_after_prior();
+    using P = Pair<PACKED>;
+    using E = typename P::E;
     extern __shared__ unsigned sort_smem[];
     __shared__ unsigned warp_sum[SORT_WARPS];
     constexpr int digits = 1 << BITS;
     const int warp = threadIdx.x / 32, lane = threadIdx.x & 31;
-    uint2 *sorted = reinterpret_cast<uint2 *>(sort_smem);                       // [SORT_TILE] the tile in order
+    E *sorted = reinterpret_cast<E *>(sort_smem);                               // [SORT_TILE] the tile in order
     unsigned *base = reinterpret_cast<unsigned *>(sorted + SORT_TILE);          // [digits] where the tile's pairs of a digit go
     unsigned *begin = base + digits;                                            // [digits] where they begin in the tile
-    unsigned short *cnt = reinterpret_cast<unsigned short *>(begin + digits);   // [SORT_WARPS][digits] pairs of a warp, then those of earlier warps
+    unsigned *match = begin + digits;                                           // [SORT_WARPS][digits] lanes with this digit; 0 between rounds
+    unsigned short *cnt = reinterpret_cast<unsigned short *>(match + SORT_WARPS * digits);   // [SORT_WARPS][digits] pairs of a warp, then those of earlier warps
+    for (int d = threadIdx.x; d < SORT_WARPS * digits; d += EMB_THREADS) match[d] = 0;
     const int per = (digits + EMB_THREADS - 1) / EMB_THREADS, d0 = threadIdx.x * per;   // digits of this thread in the scans
     {   // base = pairs of smaller digits (scan of the totals) + pairs of this digit in earlier blocks
         const int blocks = gridDim.x, mine = blockIdx.x;
@@ -361,40 +386,48 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
             run += begin[d0 + j];
         }
     }
-    const long long i0 = per_block * blockIdx.x, i1 = i0 + per_block < a.n ? i0 + per_block : a.n;
-    for (long long tile = i0; tile < i1; tile += SORT_TILE) {
-        const long long w0 = tile + (long long)warp * 32 * SORT_ROUNDS;   // a warp's pairs are consecutive: its rounds keep their order
-        uint2 pair[SORT_ROUNDS];
+    const unsigned i0 = (unsigned)per_block * blockIdx.x, i1 = min(i0 + (unsigned)per_block, (unsigned)a.n);
+    // a tile's pairs (or tokens) are loaded under the work on the tile before; those of a warp are consecutive, so that
+    // its rounds keep their order
+    using Load = typename std::conditional<FIRST, unsigned, E>::type;
+    Load next[SORT_ROUNDS];
+    const unsigned in_tile = warp * 32 * SORT_ROUNDS + lane;
+    auto load = [&](unsigned tile) {
 #pragma unroll
         for (int r = 0; r < SORT_ROUNDS; ++r) {
-            const long long i = w0 + r * 32 + lane;
-            const long long at = i < i1 ? i : i1 - 1;
-            if (FIRST) pair[r] = make_uint2(token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, (unsigned)at)), div_bag(a, (unsigned)at));
-            else pair[r] = in[at];
+            const unsigned at = min(tile + in_tile + r * 32, i1 - 1);
+            if constexpr (FIRST) next[r] = token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, at));
+            else next[r] = in[at];
         }
-        if (FIRST) {
-            bool bad = false;   // reported by the count
+    };
+    if (i0 < i1) load(i0);
+    for (unsigned tile = i0; tile < i1; tile += SORT_TILE) {
+        const unsigned w0 = tile + in_tile;
+        E pair[SORT_ROUNDS];
 #pragma unroll
-            for (int r = 0; r < SORT_ROUNDS; ++r) pair[r].x = token_key(a, pair[r].x, bad);
+        for (int r = 0; r < SORT_ROUNDS; ++r) {
+            if constexpr (FIRST) {
+                bool bad = false;   // reported by the count
+                pair[r] = P::make(token_key(a, next[r], bad), div_bag(a, w0 + r * 32), a.row_bits);
+            } else {
+                pair[r] = next[r];
+            }
         }
+        if (tile + SORT_TILE < i1) load(tile + SORT_TILE);
         for (int d = threadIdx.x; d < digits * SORT_WARPS / 2; d += EMB_THREADS) reinterpret_cast<unsigned *>(cnt)[d] = 0;
         __syncthreads();
         unsigned short place[SORT_ROUNDS], *mine = cnt + warp * digits;
+        unsigned *lanes = match + warp * digits;
 #pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r) {
-            const bool on = w0 + r * 32 + lane < i1;
-            const unsigned d = on ? (pair[r].x >> shift) & (digits - 1) : 0u;
-            unsigned same = __ballot_sync(0xffffffffu, on);   // lanes with the same digit
-#pragma unroll
-            for (int b = 0; b < BITS; ++b) {
-                const unsigned set = __ballot_sync(0xffffffffu, d >> b & 1);
-                same &= d >> b & 1 ? set : ~set;
-            }
-            const unsigned below = __popc(same & ((1u << lane) - 1));
-            unsigned short old = 0;
-            if (on) old = mine[d];
+        for (int r = 0; r < SORT_ROUNDS; ++r) {   // every lane enters itself at its digit, and looks who else did
+            const bool on = w0 + r * 32 < i1;
+            const unsigned d = P::word(pair[r]) >> shift & (digits - 1);
+            if (on) atomicOr(&lanes[d], 1u << lane);
             __syncwarp();
-            if (on && below == 0) mine[d] = (unsigned short)(old + __popc(same));
+            const unsigned same = lanes[d], below = __popc(same & ((1u << lane) - 1));
+            const unsigned short old = mine[d];
+            __syncwarp();
+            if (on && below == 0) mine[d] = (unsigned short)(old + __popc(same)), lanes[d] = 0;
             __syncwarp();
             place[r] = (unsigned short)(old + below);
         }
@@ -420,20 +453,22 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < SORT_ROUNDS; ++r)
-            if (w0 + r * 32 + lane < i1) {
-                const unsigned d = (pair[r].x >> shift) & (digits - 1);
+            if (w0 + r * 32 < i1) {
+                const unsigned d = (P::word(pair[r]) >> shift) & (digits - 1);
                 sorted[begin[d] + mine[d] + place[r]] = pair[r];
             }
         __syncthreads();
-        const int n = (int)(i1 - tile < SORT_TILE ? i1 - tile : SORT_TILE);
-        for (int i = threadIdx.x; i < n; i += EMB_THREADS) {
-            const uint2 p = sorted[i];
-            const unsigned d = (p.x >> shift) & (digits - 1);
-            out[base[d] + i - begin[d]] = p;
+        const unsigned n = min(i1 - tile, (unsigned)SORT_TILE);
+#pragma unroll 8
+        for (unsigned i = threadIdx.x; i < n; i += EMB_THREADS) {
+            const E p = sorted[i];
+            const unsigned d = (P::word(p) >> shift) & (digits - 1), to = base[d] + i - begin[d];
+            if constexpr (LAST) reinterpret_cast<uint2 *>(out)[to] = P::wide(p, a.row_bits);
+            else reinterpret_cast<E *>(out)[to] = p;
         }
         __syncthreads();
         for (int j = 0; j < per && d0 + j < digits; ++j)   // begin of the next digit - begin = pairs of this digit in the tile
-            base[d0 + j] += (d0 + j + 1 < digits ? begin[d0 + j + 1] : (unsigned)n) - begin[d0 + j];
+            base[d0 + j] += (d0 + j + 1 < digits ? begin[d0 + j + 1] : n) - begin[d0 + j];
         __syncthreads();
     }
 }
@@ -780,33 +815,55 @@ SortPlan sort_plan(const qgbdt_ctx *c, long long n, long long n_entries) {
     return s;
 }
 
+template <typename I, bool FIRST, bool PACKED, bool LAST>
+int sort_scatter(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, const void *in, int shift, const unsigned *counts, const unsigned *totals, void *out,
+                 cudaStream_t st) {
+    using E = typename Pair<PACKED>::E;
+    const auto kernel = s.bits == 6   ? k_sort_scatter<I, FIRST, PACKED, LAST, 6>
+                        : s.bits == 7 ? k_sort_scatter<I, FIRST, PACKED, LAST, 7>
+                        : s.bits == 8 ? k_sort_scatter<I, FIRST, PACKED, LAST, 8>
+                                      : k_sort_scatter<I, FIRST, PACKED, LAST, 9>;
+    return qg_launch(c, kernel, dim3(s.blocks), EMB_THREADS, scatter_smem(s.bits, sizeof(E)), st, a, reinterpret_cast<const E *>(in), shift, s.per_block,
+                     counts, totals, out);
+}
+
+template <typename I, bool PACKED>
+int sort_passes(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, void *in, void *out, unsigned *counts, unsigned *totals, const uint2 **sorted,
+                cudaStream_t st) {
+    using E = typename Pair<PACKED>::E;
+    const int digits = 1 << s.bits;
+    const bool scan = s.blocks > SORT_FEW_BLOCKS;
+    for (int k = 0; k < s.passes; ++k) {
+        const bool first = k == 0, last = k == s.passes - 1;
+        const int shift = k * s.bits, at = PACKED ? shift + a.row_bits : shift;   // of the token; of the digit in a pair's word
+        QG_RUN(first ? qg_launch(c, k_sort_count<I, true, PACKED>, dim3(s.blocks), EMB_THREADS, digits * sizeof(unsigned), st, a,
+                                 reinterpret_cast<const E *>(in), shift, s.bits, s.per_block, counts)
+                     : qg_launch(c, k_sort_count<int32_t, false, PACKED>, dim3(s.blocks), EMB_THREADS, digits * sizeof(unsigned), st, a,
+                                 reinterpret_cast<const E *>(in), at, s.bits, s.per_block, counts));
+        if (scan) QG_RUN(qg_launch(c, k_sort_scan, dim3((digits + SORT_WARPS - 1) / SORT_WARPS), EMB_THREADS, 0, st, counts, totals, digits, s.blocks));
+        const unsigned *t = scan ? totals : nullptr;
+        QG_RUN(first ? (last ? sort_scatter<I, true, PACKED, true>(c, a, s, in, at, counts, t, out, st)
+                             : sort_scatter<I, true, PACKED, false>(c, a, s, in, at, counts, t, out, st))
+                     : (last ? sort_scatter<int32_t, false, PACKED, true>(c, a, s, in, at, counts, t, out, st)
+                             : sort_scatter<int32_t, false, PACKED, false>(c, a, s, in, at, counts, t, out, st)));
+        void *swap = in;
+        in = out;
+        out = swap;
+    }
+    *sorted = reinterpret_cast<const uint2 *>(in);
+    return QGBDT_OK;
+}
+
 template <typename I>
-int sort_pairs(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, uint2 *buf0, uint2 *buf1, unsigned *counts, unsigned *totals,
-               const uint2 **sorted, cudaStream_t st) {
+int sort_pairs(qgbdt_ctx *c, SortArgs a, const SortPlan &s, uint2 *buf0, uint2 *buf1, unsigned *counts, unsigned *totals, const uint2 **sorted,
+               cudaStream_t st) {
     if (a.n <= SORT_SMALL) {
         *sorted = buf0;
         return qg_launch(c, k_sort_small<I>, dim3((unsigned)((a.n * SORT_SMALL_LANES + EMB_THREADS - 1) / EMB_THREADS)), EMB_THREADS, 0, st, a, buf0);
     }
-    const int digits = 1 << s.bits;
-    const size_t count_smem = digits * sizeof(unsigned), smem = scatter_smem(s.bits);
-    uint2 *in = buf1, *out = buf0;
-    for (int k = 0; k < s.passes; ++k) {
-        const int shift = k * s.bits;
-        QG_RUN(qg_launch(c, k == 0 ? k_sort_count<I, true> : k_sort_count<I, false>, dim3(s.blocks), EMB_THREADS, count_smem, st, a, in, shift, s.bits,
-                         s.per_block, counts));
-        const bool scan = s.blocks > SORT_FEW_BLOCKS;
-        if (scan) QG_RUN(qg_launch(c, k_sort_scan, dim3((digits + SORT_WARPS - 1) / SORT_WARPS), EMB_THREADS, 0, st, counts, totals, digits, s.blocks));
-        const auto scatter = s.bits == 6 ? (k == 0 ? k_sort_scatter<I, true, 6> : k_sort_scatter<I, false, 6>)
-                             : s.bits == 7 ? (k == 0 ? k_sort_scatter<I, true, 7> : k_sort_scatter<I, false, 7>)
-                             : s.bits == 8 ? (k == 0 ? k_sort_scatter<I, true, 8> : k_sort_scatter<I, false, 8>)
-                                           : (k == 0 ? k_sort_scatter<I, true, 9> : k_sort_scatter<I, false, 9>);
-        QG_RUN(qg_launch(c, scatter, dim3(s.blocks), EMB_THREADS, smem, st, a, in, shift, s.per_block, counts, scan ? totals : nullptr, out));
-        uint2 *swap = in;
-        in = out;
-        out = swap;
-    }
-    *sorted = in;
-    return QGBDT_OK;
+    a.row_bits = log2_at_least(a.n / a.bag, 31);
+    return a.row_bits + log2_at_least(a.n_entries + 1, 32) <= 32 ? sort_passes<I, true>(c, a, s, buf1, buf0, counts, totals, sorted, st)
+                                                                 : sort_passes<I, false>(c, a, s, buf1, buf0, counts, totals, sorted, st);
 }
 
 template <typename T, int V>
@@ -850,7 +907,7 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.n = n;
     s.grad = a.table, s.ld = a.ld, s.out = a.out, s.ld_out = a.ld_out, s.n_entries = a.n_entries;
     s.dim = a.dim, s.scale = a.scale;
-    SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, 0, 0, 0, a.status};
+    SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, 0, 0, 0, 0, a.status};
     set_divisor(sa, (unsigned)a.bag);
     if (n > 0 && n <= SCAN_PAIRS && n * a.n_entries <= SCAN_WORK) {
 #define CALL(T, V) scan_typed<T, V>(c, sa, s, a.token_type == QGBDT_I64, st)

@@ -104,6 +104,23 @@ def test_embed_backward_long_lists(ctx, rows, bag, entries, dim):
     assert torch.equal(ctx.embed_backward(grad, tok, entries, scale=1.0), first)   # the same bits every time
 
 
+@pytest.mark.parametrize("rows,bag,entries,dim,wide", [(70000, 2, 70000, 8, False), (5000, 3, 1 << 21, 4, True), ((1 << 24) + 5, 1, 500, 2, False),
+                                                       (65536, 2, 65535, 4, True), (65537, 2, 65535, 4, False), (1, 7000, 1 << 22, 1, True)])
+def test_embed_backward_long_lists_of_one_word_pairs_and_two_word_pairs(ctx, rows, bag, entries, dim, wide):
+    """Token and row together have 32 bits, more, or just as many."""
+    table, tok = embed_case(rows, bag, entries, dim, torch.float32, 0, wide, 2)
+    grad = torch.randn((rows, dim), generator=gen(3), device="cuda")
+    check_embed_grad(ctx.embed_backward(grad, tok, entries, scale=0.5), grad, tok, entries, 0.5)
+
+
+@pytest.mark.parametrize("entries", [40, 300, 70000])
+def test_embed_backward_long_lists_of_one_token(ctx, entries):
+    """Every pair of a tile has the same digits."""
+    tok = torch.full((9000, 5), entries - 1, dtype=torch.int32, device="cuda")
+    grad = torch.randn((9000, 3), generator=gen(4), device="cuda")
+    check_embed_grad(ctx.embed_backward(grad, tok, entries), grad, tok, entries, 1.0)
+
+
 def test_embed_backward_keeps_the_order_of_rows(ctx):
     """Sums of whole numbers are exact in any order; a permutation of the rows must not change them."""
     g = gen(5)
