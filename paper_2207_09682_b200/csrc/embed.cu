@@ -171,7 +171,33 @@ struct SortArgs {
     unsigned bag, div_mul, div_shift;    // i / bag == (i * div_mul) >> div_shift in 64 bits, for i < 2^31
     int row_bits;                        // of a packed pair
     int32_t *status;
+    int blocks;                          // of a launch that sort; those behind them clear
 };
+
+// Few pairs beside the entries: nearly every row of the gradient is zero, and the sort leaves most SMs without work.  Its
+// launches clear all rows then, a share each, in blocks behind those that sort.  4099 tokens, 50021 x 768 f16: 35 us with
+// the rows no token points to cleared under the sums (as with many pairs), 29 us this way; 30000 tokens, 200000 x 512: 67 and 63 us.
+struct ClearArgs {
+    char *out;
+    long long ld_bytes, row0, row1;
+    int vectors, lg, vb;   // of a row; log2 of the lanes per row; bytes of a vector
+};
+constexpr int CLEAR_BLOCKS = 3;   // per SM, at most
+
+template <typename V>
+__device__ __forceinline__ void clear_with(const ClearArgs &z, int block, int blocks, V zero) {
+    const int rows = EMB_THREADS >> z.lg;
+    for (long long r = z.row0 + (long long)block * rows + (threadIdx.x >> z.lg); r < z.row1; r += (long long)blocks * rows) {
+        V *row = reinterpret_cast<V *>(z.out + r * z.ld_bytes);
+        for (int k = threadIdx.x & ((1 << z.lg) - 1); k < z.vectors; k += 1 << z.lg) row[k] = zero;
+    }
+}
+__device__ void clear_ahead(const ClearArgs &z, int block, int blocks) {
+    if (z.vb == 16) clear_with(z, block, blocks, make_uint4(0, 0, 0, 0));
+    else if (z.vb == 8) clear_with(z, block, blocks, make_uint2(0, 0));
+    else if (z.vb == 4) clear_with(z, block, blocks, 0u);
+    else clear_with(z, block, blocks, (unsigned short)0);
+}
 
 // A pair between two passes: token and row in one word where both fit (every usual size), or in two.  The last pass
 // writes two words in any case.
@@ -215,12 +241,20 @@ __device__ __forceinline__ unsigned token_key(const SortArgs &a, unsigned t, boo
 }
 
 // Few pairs: every pair's place is the number of pairs before it, counted directly; one launch.
-constexpr int SORT_SMALL = 6144;   // 11 us at 4096 pairs and 26 us at 8000, where the passes below take 20 us
-constexpr int SORT_SMALL_LANES = 8;   // lanes that share the count of one pair
+// A whole gradient of 4000 pairs takes 14 us with it and 20 with the passes below, of 6000 pairs 20 and 20.  Where rows are
+// cleared ahead, the several launches of the passes hide more of that, so that the limit sinks with the bytes: 50021 rows of
+// 128, 512, 1024 and 2048 bytes, 4099 pairs: 15, 19, 24, 36 us and 18, 20, 24, 34.
+constexpr int SORT_SMALL = 6144;
+constexpr long long SORT_SMALL_CLEAR = 32 << 10;   // bytes to clear that take a pair off the limit
+constexpr int SORT_SMALL_LANES = 16;   // lanes that share the count of one pair
 
 template <typename I>
-__global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, uint2 *out) {
+__global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, const ClearArgs z, uint2 *out) {
     qg_after_prior();
+    if ((int)blockIdx.x >= a.blocks) {
+        clear_ahead(z, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+        return;
+    }
     __shared__ alignas(16) unsigned key[SORT_SMALL];
     const int n = (int)a.n, n4 = (n + 3) / 4;
     const I *tokens = reinterpret_cast<const I *>(a.tokens);
@@ -238,11 +272,15 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, ui
     const int e = (blockIdx.x * EMB_THREADS + threadIdx.x) / SORT_SMALL_LANES, lane = threadIdx.x % SORT_SMALL_LANES;
     const unsigned mine = e < n ? key[e] : 0;
     unsigned before = 0;
+    const int own = e / 4;   // equal tokens in front of e count, those behind it do not
+#pragma unroll 4
     for (int q = lane; q < n4; q += SORT_SMALL_LANES) {
         const uint4 k = reinterpret_cast<const uint4 *>(key)[q];
-        before += (k.x < mine || (k.x == mine && 4 * q < e)) + (k.y < mine || (k.y == mine && 4 * q + 1 < e)) +
-                  (k.z < mine || (k.z == mine && 4 * q + 2 < e)) + (k.w < mine || (k.w == mine && 4 * q + 3 < e));
+        const unsigned limit = q < own ? mine + 1 : mine;
+        before += (k.x < limit) + (k.y < limit) + (k.z < limit) + (k.w < limit);
     }
+    if (lane == own % SORT_SMALL_LANES)
+        for (int i = 4 * own; i < e; ++i) before += key[i] == mine;
 #pragma unroll
     for (int o = SORT_SMALL_LANES / 2; o; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
     if (e < n && lane == 0) out[before] = make_uint2(mine, div_bag(a, (unsigned)e));
@@ -262,9 +300,13 @@ constexpr int SORT_TILE = EMB_THREADS * SORT_ROUNDS;
 __host__ __device__ inline size_t count_stride(int blocks) { return ((size_t)blocks + 3) / 4 * 4; }
 
 template <typename I, bool FIRST, bool PACKED>
-__global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const typename Pair<PACKED>::E *in, int shift, int bits, long long per_block,
+__global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, const ClearArgs z, const typename Pair<PACKED>::E *in, int shift, int bits, long long per_block,
                                                             unsigned *counts) {
     qg_after_prior();
+    if ((int)blockIdx.x >= a.blocks) {
+        clear_ahead(z, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+        return;
+    }
     extern __shared__ unsigned sort_smem[];
     unsigned *cnt = sort_smem;   // [1 << bits]
     const int digits = 1 << bits;
@@ -286,7 +328,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_count(const SortArgs a, co
         if (FIRST && bad && a.status) *a.status = 1;
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < digits; d += EMB_THREADS) counts[(size_t)d * count_stride(gridDim.x) + blockIdx.x] = cnt[d];
+    for (int d = threadIdx.x; d < digits; d += EMB_THREADS) counts[(size_t)d * count_stride(a.blocks) + blockIdx.x] = cnt[d];
 }
 
 // Per digit (one warp): exclusive scan over the blocks, and the digit's total.
@@ -338,9 +380,13 @@ __device__ __forceinline__ unsigned block_scan(unsigned x, unsigned *warp_sum) {
 constexpr int SORT_FEW_BLOCKS = 128;
 
 template <typename I, bool FIRST, bool PACKED, bool LAST, int BITS>
-__global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const typename Pair<PACKED>::E *in, int shift, long long per_block,
+__global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs a, const ClearArgs z, const typename Pair<PACKED>::E *in, int shift, long long per_block,
                                                                  const unsigned *counts, const unsigned *totals, void *out) {
     qg_after_prior();
+    if ((int)blockIdx.x >= a.blocks) {
+        clear_ahead(z, blockIdx.x - a.blocks, gridDim.x - a.blocks);
+        return;
+    }
     using P = Pair<PACKED>;
     using E = typename P::E;
     extern __shared__ unsigned sort_smem[];
@@ -355,7 +401,7 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
     for (int d = threadIdx.x; d < SORT_WARPS * digits; d += EMB_THREADS) match[d] = 0;
     const int per = (digits + EMB_THREADS - 1) / EMB_THREADS, d0 = threadIdx.x * per;   // digits of this thread in the scans
     {   // base = pairs of smaller digits (scan of the totals) + pairs of this digit in earlier blocks
-        const int blocks = gridDim.x, mine = blockIdx.x;
+        const int blocks = a.blocks, mine = blockIdx.x;
         const size_t stride = count_stride(blocks);
         unsigned s = 0;
         for (int j = 0; j < per && d0 + j < digits; ++j) {
@@ -488,7 +534,8 @@ struct SegArgs {
     float scale;
     float *partial;         // [tiles][2][dim]: sum of a tile's first token when it began in an earlier tile;
                             // sum of its last token when it began here and goes on in the next tile
-    long long sum_blocks;   // blocks that add; those behind them clear the rows no token points to
+    long long sum_blocks;   // blocks that add; those behind them clear the rows no token points to, unless all are
+    bool cleared;
 };
 
 constexpr int ZERO_ROWS = 128;   // rows of the gradient a clearing block looks at
@@ -815,20 +862,31 @@ SortPlan sort_plan(const qgbdt_ctx *c, long long n, long long n_entries) {
     return s;
 }
 
+// The rows to clear ahead of the sums, in equal shares for the sort's launches; blocks == 0: none.
+struct Clearing {
+    ClearArgs all;
+    int blocks, launches;
+    ClearArgs share(int k) const {
+        ClearArgs z = all;
+        z.row0 = all.row1 * k / launches, z.row1 = all.row1 * (k + 1) / launches;
+        return z;
+    }
+};
+
 template <typename I, bool FIRST, bool PACKED, bool LAST>
-int sort_scatter(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, const void *in, int shift, const unsigned *counts, const unsigned *totals, void *out,
+int sort_scatter(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, const Clearing &z, int launch, const void *in, int shift, const unsigned *counts, const unsigned *totals, void *out,
                  cudaStream_t st) {
     using E = typename Pair<PACKED>::E;
     const auto kernel = s.bits == 6   ? k_sort_scatter<I, FIRST, PACKED, LAST, 6>
                         : s.bits == 7 ? k_sort_scatter<I, FIRST, PACKED, LAST, 7>
                         : s.bits == 8 ? k_sort_scatter<I, FIRST, PACKED, LAST, 8>
                                       : k_sort_scatter<I, FIRST, PACKED, LAST, 9>;
-    return qg_launch(c, kernel, dim3(s.blocks), EMB_THREADS, scatter_smem(s.bits, sizeof(E)), st, a, reinterpret_cast<const E *>(in), shift, s.per_block,
+    return qg_launch(c, kernel, dim3(s.blocks + z.blocks), EMB_THREADS, scatter_smem(s.bits, sizeof(E)), st, a, z.share(launch), reinterpret_cast<const E *>(in), shift, s.per_block,
                      counts, totals, out);
 }
 
 template <typename I, bool PACKED>
-int sort_passes(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, void *in, void *out, unsigned *counts, unsigned *totals, const uint2 **sorted,
+int sort_passes(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, const Clearing &z, void *in, void *out, unsigned *counts, unsigned *totals, const uint2 **sorted,
                 cudaStream_t st) {
     using E = typename Pair<PACKED>::E;
     const int digits = 1 << s.bits;
@@ -836,16 +894,16 @@ int sort_passes(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, void *in, vo
     for (int k = 0; k < s.passes; ++k) {
         const bool first = k == 0, last = k == s.passes - 1;
         const int shift = k * s.bits, at = PACKED ? shift + a.row_bits : shift;   // of the token; of the digit in a pair's word
-        QG_RUN(first ? qg_launch(c, k_sort_count<I, true, PACKED>, dim3(s.blocks), EMB_THREADS, digits * sizeof(unsigned), st, a,
+        QG_RUN(first ? qg_launch(c, k_sort_count<I, true, PACKED>, dim3(s.blocks + z.blocks), EMB_THREADS, digits * sizeof(unsigned), st, a, z.share(2 * k),
                                  reinterpret_cast<const E *>(in), shift, s.bits, s.per_block, counts)
-                     : qg_launch(c, k_sort_count<int32_t, false, PACKED>, dim3(s.blocks), EMB_THREADS, digits * sizeof(unsigned), st, a,
+                     : qg_launch(c, k_sort_count<int32_t, false, PACKED>, dim3(s.blocks + z.blocks), EMB_THREADS, digits * sizeof(unsigned), st, a, z.share(2 * k),
                                  reinterpret_cast<const E *>(in), at, s.bits, s.per_block, counts));
         if (scan) QG_RUN(qg_launch(c, k_sort_scan, dim3((digits + SORT_WARPS - 1) / SORT_WARPS), EMB_THREADS, 0, st, counts, totals, digits, s.blocks));
         const unsigned *t = scan ? totals : nullptr;
-        QG_RUN(first ? (last ? sort_scatter<I, true, PACKED, true>(c, a, s, in, at, counts, t, out, st)
-                             : sort_scatter<I, true, PACKED, false>(c, a, s, in, at, counts, t, out, st))
-                     : (last ? sort_scatter<int32_t, false, PACKED, true>(c, a, s, in, at, counts, t, out, st)
-                             : sort_scatter<int32_t, false, PACKED, false>(c, a, s, in, at, counts, t, out, st)));
+        QG_RUN(first ? (last ? sort_scatter<I, true, PACKED, true>(c, a, s, z, 2 * k + 1, in, at, counts, t, out, st)
+                             : sort_scatter<I, true, PACKED, false>(c, a, s, z, 2 * k + 1, in, at, counts, t, out, st))
+                     : (last ? sort_scatter<int32_t, false, PACKED, true>(c, a, s, z, 2 * k + 1, in, at, counts, t, out, st)
+                             : sort_scatter<int32_t, false, PACKED, false>(c, a, s, z, 2 * k + 1, in, at, counts, t, out, st)));
         void *swap = in;
         in = out;
         out = swap;
@@ -855,22 +913,24 @@ int sort_passes(qgbdt_ctx *c, const SortArgs &a, const SortPlan &s, void *in, vo
 }
 
 template <typename I>
-int sort_pairs(qgbdt_ctx *c, SortArgs a, const SortPlan &s, uint2 *buf0, uint2 *buf1, unsigned *counts, unsigned *totals, const uint2 **sorted,
+int sort_pairs(qgbdt_ctx *c, SortArgs a, const SortPlan &s, Clearing z, uint2 *buf0, uint2 *buf1, unsigned *counts, unsigned *totals, const uint2 **sorted,
                cudaStream_t st) {
-    if (a.n <= SORT_SMALL) {
+    if (s.passes == 0) {
         *sorted = buf0;
-        return qg_launch(c, k_sort_small<I>, dim3((unsigned)((a.n * SORT_SMALL_LANES + EMB_THREADS - 1) / EMB_THREADS)), EMB_THREADS, 0, st, a, buf0);
+        a.blocks = (int)((a.n * SORT_SMALL_LANES + EMB_THREADS - 1) / EMB_THREADS), z.launches = 1;
+        return qg_launch(c, k_sort_small<I>, dim3(a.blocks + z.blocks), EMB_THREADS, 0, st, a, z.share(0), buf0);
     }
+    a.blocks = s.blocks, z.launches = 2 * s.passes;
     a.row_bits = log2_at_least(a.n / a.bag, 31);
-    return a.row_bits + log2_at_least(a.n_entries + 1, 32) <= 32 ? sort_passes<I, true>(c, a, s, buf1, buf0, counts, totals, sorted, st)
-                                                                 : sort_passes<I, false>(c, a, s, buf1, buf0, counts, totals, sorted, st);
+    return a.row_bits + log2_at_least(a.n_entries + 1, 32) <= 32 ? sort_passes<I, true>(c, a, s, z, buf1, buf0, counts, totals, sorted, st)
+                                                                 : sort_passes<I, false>(c, a, s, z, buf1, buf0, counts, totals, sorted, st);
 }
 
 template <typename T, int V>
 int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     const long long per_block = EMB_THREADS >> s.lg;
     s.sum_blocks = (s.tiles + per_block - 1) / per_block * s.col_blocks;
-    const long long blocks = s.sum_blocks + (s.n_entries + ZERO_ROWS - 1) / ZERO_ROWS;
+    const long long blocks = s.sum_blocks + (s.cleared ? 0 : (s.n_entries + ZERO_ROWS - 1) / ZERO_ROWS);
     if (blocks > 0x7fffffffll) return qg_fail(c, QGBDT_ERR_ARG, "rows * bag * dim is too large for one call");
     QG_RUN(qg_launch(c, k_segment_sum<T, V>, dim3((unsigned)blocks), EMB_THREADS, 0, st, s));
     if (s.tiles > 1) {
@@ -907,7 +967,8 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.n = n;
     s.grad = a.table, s.ld = a.ld, s.out = a.out, s.ld_out = a.ld_out, s.n_entries = a.n_entries;
     s.dim = a.dim, s.scale = a.scale;
-    SortArgs sa{a.tokens, a.ld_tokens, a.n_entries, n, 0, 0, 0, 0, a.status};
+    SortArgs sa{};
+    sa.tokens = a.tokens, sa.ld_tokens = a.ld_tokens, sa.n_entries = a.n_entries, sa.n = n, sa.status = a.status;
     set_divisor(sa, (unsigned)a.bag);
     if (n > 0 && n <= SCAN_PAIRS && n * a.n_entries <= SCAN_WORK) {
 #define CALL(T, V) scan_typed<T, V>(c, sa, s, a.token_type == QGBDT_I64, st)
@@ -923,7 +984,9 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     tile = tile < 16 ? 16 : (tile + EMB_UNROLL - 1) / EMB_UNROLL * EMB_UNROLL;
     s.tile = (int)(tile < (1 << 20) ? tile : 1 << 20);
     s.tiles = (n + s.tile - 1) / s.tile;
-    const bool small = n <= SORT_SMALL;
+    // few pairs beside the entries: all rows are cleared ahead (at most half as much again is written as has to be)
+    const bool ahead = n > 0 && 2 * n <= a.n_entries;
+    const bool small = n <= SORT_SMALL - (ahead ? a.n_entries * a.dim * qg_type_size(a.type) / SORT_SMALL_CLEAR : 0);
     const SortPlan sp = small ? SortPlan{} : sort_plan(c, n, a.n_entries);
     const size_t digits = small ? 0 : (size_t)1 << sp.bits;
     const size_t bytes = 2 * qg_ws_size((size_t)n + 2 * EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * count_stride(sp.blocks), sizeof(unsigned)) +
@@ -935,9 +998,17 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     unsigned *counts = ws.take<unsigned>(digits * count_stride(sp.blocks)), *totals = ws.take<unsigned>(digits);
     s.partial = ws.take<float>((size_t)s.tiles * 2 * a.dim);
     s.pair = buf0;
+    Clearing z{};
+    if (ahead) {
+        const int w = qg_type_size(a.type);
+        z.all = ClearArgs{reinterpret_cast<char *>(a.out), a.ld_out * w, 0, a.n_entries, a.dim / V, log2_at_least(a.dim / V, 8), vb};
+        const long long want = (a.n_entries * a.dim / V + EMB_THREADS * 16 - 1) / (EMB_THREADS * 16), most = (long long)c->sm_count * CLEAR_BLOCKS;
+        z.blocks = (int)(want < most ? want : most);
+        s.cleared = true;
+    }
     if (n > 0) {
-        rc = a.token_type == QGBDT_I64 ? sort_pairs<int64_t>(c, sa, sp, buf0, buf1, counts, totals, &s.pair, st)
-                                       : sort_pairs<int32_t>(c, sa, sp, buf0, buf1, counts, totals, &s.pair, st);
+        rc = a.token_type == QGBDT_I64 ? sort_pairs<int64_t>(c, sa, sp, z, buf0, buf1, counts, totals, &s.pair, st)
+                                       : sort_pairs<int32_t>(c, sa, sp, z, buf0, buf1, counts, totals, &s.pair, st);
         if (rc != QGBDT_OK) return rc;
     }
 #define CALL(T, V) segments_typed<T, V>(c, s, st)

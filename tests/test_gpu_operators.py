@@ -189,6 +189,29 @@ def test_embed_strides(ctx):
     assert bool((d[:, :1] == 7).all()) and bool((d[:, 18:] == 7).all())
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,bag,entries,dim,left,right", [(600, 7, 9001, 33, 1, 2), (3000, 4, 30000, 8, 8, 0), (40, 200, 200000, 6, 2, 4), (5, 3, 1 << 20, 300, 0, 0),
+                                                             (7, 900, 20011, 2, 0, 2), (1, 7000, 70001, 1, 1, 0)])
+def test_embed_backward_few_pairs_beside_the_entries(ctx, rows, bag, entries, dim, left, right, dtype):
+    """Nearly every row of the gradient is zero; what lies between the rows stays as it is."""
+    grad = torch.randn((rows, dim), generator=gen(6), device="cuda").to(DTYPES[dtype])
+    tok = torch.randint(-1, entries, (rows, bag), generator=gen(7), device="cuda")
+    tok[:, 0] = entries - 1
+    wide = torch.full((entries, left + dim + right), 7.0, device="cuda", dtype=DTYPES[dtype])
+    got = wide[:, left:left + dim]
+    ctx.embed_backward(grad, tok, entries, grad_table=got)
+    assert bool((wide[:, :left] == 7).all()) and bool((wide[:, left + dim:] == 7).all())
+    hit = torch.zeros(entries, dtype=torch.bool, device="cuda")
+    hit[tok[tok >= 0]] = True
+    assert not got[~hit].any()
+    index = torch.where(tok < 0, entries, tok).reshape(-1)
+    each = grad.double().unsqueeze(1).expand(-1, bag, -1).reshape(-1, dim)
+    zeros = torch.zeros((entries + 1, dim), dtype=torch.float64, device="cuda")
+    want, size = zeros.index_add(0, index, each)[:entries], zeros.index_add(0, index, each.abs())[:entries]
+    count = torch.bincount(index, minlength=entries + 1)[:entries].unsqueeze(1)
+    within(got, want, (count + 1) * 2.0 ** -24 * size + UNIT[DTYPES[dtype]] * want.abs() + TINY[DTYPES[dtype]])
+
+
 def test_embed_gradient_by_differences(ctx):
     """d sum(w * embed(table)) / d table against central differences (the function is linear: only rounding is left)."""
     g = gen(3)
