@@ -7,11 +7,14 @@
 // is added in single precision, so the time is that traffic.  A row is read by a group of 2^lg lanes, one
 // vector of up to 16 bytes per lane; wider rows are cut into column blocks of 32 vectors.
 //
+// 65536 rows of 100 tokens, 256 bf16 each: 215 us for 3.4 GB of rows, which is what L2 delivers (13 TB/s; 15 % are hits in L1).
+//
 // Gradient: the (token, row) pairs are sorted by token with a stable radix sort (pairs keep their row
 // order inside a token), the sorted list is cut into tiles of equal length, and a group of lanes walks a
 // tile adding rows until the token changes.  A token whose pairs cross a tile border leaves partial sums
-// that a second kernel adds in tile order.  Equal tile lengths keep the work even however the tokens
-// crowd, and the order of every sum depends on the tokens alone.
+// that a second kernel adds in an order that depends on the tiles alone.  Equal tile lengths keep the work even however
+// the tokens crowd, and the order of every sum depends on the tokens alone.  The same 65536 rows: 395 us, of which the sums
+// take 270 (12.7 TB/s out of L2), sorting 100, the joining 20.
 #include <type_traits>
 
 #include "ops_internal.cuh"
@@ -399,6 +402,21 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
     unsigned *match = begin + digits;                                           // [SORT_WARPS][digits] lanes with this digit; 0 between rounds
     unsigned short *cnt = reinterpret_cast<unsigned short *>(match + SORT_WARPS * digits);   // [SORT_WARPS][digits] pairs of a warp, then those of earlier warps
     for (int d = threadIdx.x; d < SORT_WARPS * digits; d += EMB_THREADS) match[d] = 0;
+    const unsigned i0 = (unsigned)per_block * blockIdx.x, i1 = min(i0 + (unsigned)per_block, (unsigned)a.n);
+    // a tile's pairs (or tokens) are loaded under the work on the tile before; those of a warp are consecutive, so that
+    // its rounds keep their order
+    using Load = typename std::conditional<FIRST, unsigned, E>::type;
+    Load next[SORT_ROUNDS];
+    const unsigned in_tile = warp * 32 * SORT_ROUNDS + lane;
+    auto load = [&](unsigned tile) {
+#pragma unroll
+        for (int r = 0; r < SORT_ROUNDS; ++r) {
+            const unsigned at = min(tile + in_tile + r * 32, i1 - 1);
+            if constexpr (FIRST) next[r] = token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, at));
+            else next[r] = in[at];
+        }
+    };
+    if (i0 < i1) load(i0);
     const int per = (digits + EMB_THREADS - 1) / EMB_THREADS, d0 = threadIdx.x * per;   // digits of this thread in the scans
     {   // base = pairs of smaller digits (scan of the totals) + pairs of this digit in earlier blocks
         const int blocks = a.blocks, mine = blockIdx.x;
@@ -432,21 +450,6 @@ __global__ void __launch_bounds__(EMB_THREADS, 4) k_sort_scatter(const SortArgs 
             run += begin[d0 + j];
         }
     }
-    const unsigned i0 = (unsigned)per_block * blockIdx.x, i1 = min(i0 + (unsigned)per_block, (unsigned)a.n);
-    // a tile's pairs (or tokens) are loaded under the work on the tile before; those of a warp are consecutive, so that
-    // its rounds keep their order
-    using Load = typename std::conditional<FIRST, unsigned, E>::type;
-    Load next[SORT_ROUNDS];
-    const unsigned in_tile = warp * 32 * SORT_ROUNDS + lane;
-    auto load = [&](unsigned tile) {
-#pragma unroll
-        for (int r = 0; r < SORT_ROUNDS; ++r) {
-            const unsigned at = min(tile + in_tile + r * 32, i1 - 1);
-            if constexpr (FIRST) next[r] = token_at(reinterpret_cast<const I *>(a.tokens), token_index(a, at));
-            else next[r] = in[at];
-        }
-    };
-    if (i0 < i1) load(i0);
     for (unsigned tile = i0; tile < i1; tile += SORT_TILE) {
         const unsigned w0 = tile + in_tile;
         E pair[SORT_ROUNDS];
@@ -575,8 +578,15 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
     }
 }
 
+// Blocks of the sums per SM, by the bytes of a vector: what the registers of eight rows in flight allow.  Narrow vectors move
+// less per load: 600000 pairs of 200 bytes in vectors of 8, the whole gradient: 53 us with three blocks, 50 with four (five
+// spill, 63).
+// Narrow vectors move less per load: 600000 pairs of 200 bytes in vectors of 8, the whole gradient: 53 us with three
+// blocks, 50 with four (five spill: 63).
+constexpr int sum_blocks_per_sm(int vector) { return vector == 16 ? 3 : 4; }
+
 template <typename T, int V>
-__global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a) {
+__global__ void __launch_bounds__(EMB_THREADS, sum_blocks_per_sm(sizeof(T) * V)) k_segment_sum(const SegArgs a) {
     qg_after_prior();
     using Vec = OpsVec<T, V>;
     const long long block = blockIdx.x;
@@ -655,18 +665,21 @@ __global__ void __launch_bounds__(EMB_THREADS, 3) k_segment_sum(const SegArgs a)
     else finish();
 }
 
-// Tokens that cross tile borders: a group of 2^lg_cols threads per tile where such a token begins adds its partial
-// sums in tile order.  A token of very many tiles is cut into runs, one per group of the block, which are added in
-// order as well (the block belongs to such a token's first tile alone then).
-constexpr int JOIN_SERIAL = 32;   // tiles that one group adds by itself
+// Tokens that cross tile borders: 2^lg_cols threads add a token's partial sums, four columns each; 2^lg_parts such rows of
+// threads, in the same warp, share those of every tile where such a token begins, and join their sums in a tree.  A token
+// of very many tiles is shared by the whole block.  The order of every sum depends on the tiles alone.
+constexpr int JOIN_PARTS = 2;    // lg_parts at most: 655360 pairs, 310 x 16 f32: 41 us with 0, 34 with 2, 36 with 3
+constexpr int JOIN_LOADS = 4;    // sums in flight per thread
+constexpr int JOIN_TILES = 32;   // tiles of a token that the block does not share
 
 template <typename T, int V>
-__global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, int lg_cols) {
+__global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, int lg_cols, int lg_parts) {
     qg_after_prior();
     __shared__ float part_sum[EMB_THREADS][V];
     __shared__ long long long_links[EMB_THREADS];   // per group: tiles of a token that the whole block adds, or 0
     __shared__ unsigned long_token[EMB_THREADS];
-    const int cols = 1 << lg_cols, groups = EMB_THREADS >> lg_cols, group = threadIdx.x >> lg_cols, lane = threadIdx.x & (cols - 1);
+    const int cols = 1 << lg_cols, row = threadIdx.x >> lg_cols, rows = EMB_THREADS >> lg_cols, lane = threadIdx.x & (cols - 1);
+    const int parts = 1 << lg_parts, part = row & (parts - 1), group = row >> lg_parts, groups = rows >> lg_parts;   // a group per tile
     const unsigned none = (unsigned)a.n_entries;
     // Tiles t + 1 .. t + links hold the rest of a token that begins in tile t; 0 where there is none.  The four words
     // that settle nearly every tile are loaded at once.
@@ -677,21 +690,30 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
         const unsigned before = i0 > 0 ? key(i0 - 1) : none, last = key(i1 - 1), next = key(i1), second = key(i1 + a.tile);
         cur = next;
         if (cur == none || last != cur || before == cur) return 0;
-        auto inside = [&](long long l) { return (t + l) * a.tile < a.n && a.pair[(t + l) * a.tile].x == cur; };   // tile t + l begins with it
         if (i1 + a.tile >= a.n || second != cur) return 1;
-        long long lo = 2, hi = 4;
-        while (inside(hi)) lo = hi, hi *= 2;
+        // the last tile that begins with it: eight places are looked at together, further and further away, then in between
+        auto inside = [&](long long l) { return a.pair[min((t + l) * a.tile, a.n - 1)].x == cur && (t + l) * a.tile < a.n; };
+        long long lo = 2, hi = 0;
+        for (long long base = 4; hi == 0; base <<= 8) {
+            bool in[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) in[u] = inside(base << u);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (hi == 0) (in[u] ? lo : hi) = base << u;
+        }
         while (hi - lo > 1) {
-            const long long mid = (lo + hi) >> 1;
-            if (inside(mid)) lo = mid;
-            else hi = mid;
+            const long long step = (hi - lo + 8) / 9, from = lo, to = hi;
+            bool in[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) in[u] = inside(min(from + step * (u + 1), to));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const long long at = from + step * (u + 1);
+                if (at < hi) (in[u] ? lo : hi) = at;
+            }
         }
         return lo;
-    };
-    auto add = [&](float (&s)[V], const float *p) {
-        const OpsVec<float, V> x = *reinterpret_cast<const OpsVec<float, V> *>(p);
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[j] += x.v[j];
     };
     auto put = [&](unsigned cur, int col, const float (&s)[V]) {
         OpsVec<T, V> y;
@@ -699,41 +721,60 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
         for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(s[j] * a.scale);
         *reinterpret_cast<OpsVec<T, V> *>(reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col) = y;
     };
-    // tokens of few tiles: a group each
+    // the token's sums 0 .. links of this row of threads: every `step`-th from `first` on
+    auto add_all = [&](float (&s)[V], long long t, long long links, int first, int step, int col) {
+        for (long long l = first; l <= links; l += JOIN_LOADS * step) {   // some loads in flight, also behind the last sum
+            OpsVec<float, V> x[JOIN_LOADS];
+#pragma unroll
+            for (int u = 0; u < JOIN_LOADS; ++u) {
+                const long long at = min(l + u * step, links);
+                x[u] = *reinterpret_cast<const OpsVec<float, V> *>(a.partial + ((t + at) * 2 + (at == 0)) * a.dim + col);
+            }
+#pragma unroll
+            for (int u = 0; u < JOIN_LOADS; ++u)
+                if (l + u * step <= links)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) s[j] += x[u].v[j];
+        }
+    };
+    auto tree = [&](float (&s)[V], int lanes) {   // over the rows of threads among `lanes` lanes
+        for (int o = lanes / 2; o >= cols; o >>= 1)
+#pragma unroll
+            for (int j = 0; j < V; ++j) s[j] += __shfl_xor_sync(0xffffffffu, s[j], o);
+    };
+    // tokens of few tiles
     const long long t0 = (long long)blockIdx.x * groups, mine = t0 + group;
     unsigned cur = 0;
     long long links = links_of(mine, cur);
-    if (links > 0 && links <= JOIN_SERIAL)
-        for (int col = lane * V; col < a.dim; col += cols * V) {
+    const bool few = links > 0 && links <= JOIN_TILES;
+    if (__any_sync(0xffffffffu, few))
+        for (int c0 = 0; c0 < a.dim; c0 += cols * V) {
+            const int col = c0 + lane * V;
             float s[V] = {};
-            add(s, a.partial + (mine * 2 + 1) * a.dim + col);
-#pragma unroll 4
-            for (long long l = 1; l <= links; ++l) add(s, a.partial + ((mine + l) * 2) * a.dim + col);
-            put(cur, col, s);
+            if (few && col < a.dim) add_all(s, mine, links, part, parts, col);
+            tree(s, cols << lg_parts);
+            if (few && col < a.dim && part == 0) put(cur, col, s);
         }
-    if (lane == 0) long_links[group] = links > JOIN_SERIAL ? links : 0, long_token[group] = cur;
-    if (!__syncthreads_or(links > JOIN_SERIAL)) return;
+    if (part == 0 && lane == 0) long_links[group] = links > JOIN_TILES ? links : 0, long_token[group] = cur;
+    if (!__syncthreads_or(links > JOIN_TILES)) return;
     for (int q = 0; q < groups; ++q) {   // the whole block for each of the others
         links = long_links[q];
         if (links == 0) continue;
         const long long t = t0 + q;
         cur = long_token[q];
-        const long long l0 = links * group / groups, l1 = links * (group + 1) / groups;
         for (int c0 = 0; c0 < a.dim; c0 += cols * V) {
             const int col = c0 + lane * V;
             float s[V] = {};
-            if (col < a.dim) {
-                if (group == 0) add(s, a.partial + (t * 2 + 1) * a.dim + col);
-#pragma unroll 4
-                for (long long l = l0; l < l1; ++l) add(s, a.partial + ((t + 1 + l) * 2) * a.dim + col);
-            }
+            if (col < a.dim) add_all(s, t, links, row, rows, col);
+            tree(s, 32);
 #pragma unroll
             for (int j = 0; j < V; ++j) part_sum[threadIdx.x][j] = s[j];
             __syncthreads();
-            if (group == 0 && col < a.dim) {
-                for (int g = 1; g < groups; ++g)
+            if (row == 0 && col < a.dim) {   // the warps, or wider rows of threads, in their order
+                const int step = cols < 32 ? 32 : cols;
+                for (int k = step; k < EMB_THREADS; k += step)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) s[j] += part_sum[threadIdx.x + (g << lg_cols)][j];
+                    for (int j = 0; j < V; ++j) s[j] += part_sum[lane + k][j];
                 put(cur, col, s);
             }
             __syncthreads();
@@ -936,8 +977,9 @@ int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     if (s.tiles > 1) {
         // four columns at most per thread: their partial sums are one 16-byte load
         constexpr int JV = V < 4 ? V : 4;
-        const int lg = log2_at_least((s.dim + JV - 1) / JV, 7);
-        QG_RUN(qg_launch(c, k_segment_join<T, JV>, dim3((unsigned)((s.tiles - 2) / (EMB_THREADS >> lg) + 1)), EMB_THREADS, 0, st, s, lg));
+        const int lg = log2_at_least((s.dim + JV - 1) / JV, 7), lg_parts = lg >= 5 ? 0 : lg >= 5 - JOIN_PARTS ? 5 - lg : JOIN_PARTS;
+        const long long groups = EMB_THREADS >> lg >> lg_parts;
+        QG_RUN(qg_launch(c, k_segment_join<T, JV>, dim3((unsigned)((s.tiles - 2) / groups + 1)), EMB_THREADS, 0, st, s, lg, lg_parts));
     }
     return QGBDT_OK;
 }
@@ -977,7 +1019,8 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     }
     s.lg = log2_at_least((a.dim + V - 1) / V, 5);
     s.col_blocks = (a.dim + (V << s.lg) - 1) / (V << s.lg);
-    // tiles: short lists go once over the groups that fit on the SMs together (768 threads each), long ones four times,
+    // tiles: short lists go once over the groups of 768 threads per SM (more and shorter ones add to the joining: 185000 pairs
+    // of 200 bytes 34 us, 39 us with 1024), long ones four times,
     // which evens out what the SMs get; at least 16 pairs
     const long long fit = (long long)c->sm_count * 768 >> s.lg, pairs = (n * s.col_blocks + fit - 1) / fit;
     long long tile = pairs <= 128 ? pairs : pairs <= 512 ? 128 : pairs / 4;
