@@ -581,8 +581,6 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
 // Blocks of the sums per SM, by the bytes of a vector: what the registers of eight rows in flight allow.  Narrow vectors move
 // less per load: 600000 pairs of 200 bytes in vectors of 8, the whole gradient: 53 us with three blocks, 50 with four (five
 // spill, 63).
-// Narrow vectors move less per load: 600000 pairs of 200 bytes in vectors of 8, the whole gradient: 53 us with three
-// blocks, 50 with four (five spill: 63).
 constexpr int sum_blocks_per_sm(int vector) { return vector == 16 ? 3 : 4; }
 
 template <typename T, int V>
