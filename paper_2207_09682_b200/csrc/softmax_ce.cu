@@ -164,10 +164,10 @@ struct Schedule {
     TileWalk walk;
     int place, m, round, k;   // DH and DW: the tile the run has come to, its row tile and round, the block in it
     long long left;           // blocks of the run still to come
-    __device__ Schedule(const GemmArgs &a, int count)
-        : m_live(MODE == DW ? a.m_tiles : (count + BM - 1) / BM), n_tiles(a.n_tiles), dim(a.dim), walk(m_live, n_tiles, blockIdx.x / CG, gridDim.x / CG) {
+    __device__ Schedule(const GemmArgs &a, int count, int cta, int ctas)
+        : m_live(MODE == DW ? a.m_tiles : (count + BM - 1) / BM), n_tiles(a.n_tiles), dim(a.dim), walk(m_live, n_tiles, cta / CG, ctas / CG) {
         kb = MODE == DW ? (count + BK - 1) / BK : a.kb;
-        unit = blockIdx.x / CG;
+        unit = cta / CG;
         left = 0;
         if (MODE == DH || MODE == DW) {
             size = a.gang, gang = unit / size, member = unit - gang * size;
@@ -474,11 +474,10 @@ struct Epilogue {
     }
 };
 
+// CTA `cta` of `ctas` that work on a product.
 template <int MODE, int NB>
-__global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, const __grid_constant__ CUtensorMap map_a,
-                                                             const __grid_constant__ CUtensorMap map_b,
-                                                             const __grid_constant__ CUtensorMap map_out,
-                                                             const __grid_constant__ CUtensorMap map_part) {
+__device__ __forceinline__ void softmax_gemm(const GemmArgs &a, const CUtensorMap &map_a, const CUtensorMap &map_b, const CUtensorMap &map_out,
+                                             const CUtensorMap &map_part, int cta, int ctas) {
     constexpr bool A_MN = MODE == DW, B_MN = MODE == DH || MODE == DW;   // operand rows run along the products' length
     extern __shared__ char smem_raw[];
     constexpr int STAGES = Layout<MODE, NB>::STAGES, STAGE_BYTES = Layout<MODE, NB>::STAGE_BYTES, ACCS = Layout<MODE, NB>::ACCS;
@@ -511,7 +510,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
 
     qg_after_prior();   // what is above touches no memory of the device
     const int count = a.count ? *a.count : a.all_rows;
-    Schedule<MODE, NB> todo(a, count);
+    Schedule<MODE, NB> todo(a, count, cta, ctas);
     Work c;
     bool ok = true;
 
@@ -589,7 +588,7 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
         }
     } else if (warp >= 4 && MODE == DW && count == 0) {
         // no labelled row: zeros
-        for (int i = blockIdx.x * EPI_WARPS + warp - 4; i < a.rows; i += gridDim.x * EPI_WARPS)
+        for (int i = cta * EPI_WARPS + warp - 4; i < a.rows; i += ctas * EPI_WARPS)
             for (int d = lane; d < a.dim; d += 32) a.out[(a.v0 + i) * a.ld_out + d] = 0;
     } else if (warp >= 4) {
         // ---- epilogue: thread = row of the tile, half of the columns per warp
@@ -670,6 +669,23 @@ __global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, c
     tc_group_sync<CG>();
     tc_fence_after();
     if (warp == 2) tc_dealloc<CG>(tmem, TMEM_COLS);
+}
+
+template <int MODE, int NB>
+__global__ void __launch_bounds__(THREADS, 1) k_softmax_gemm(const GemmArgs a, const __grid_constant__ CUtensorMap map_a,
+                                                             const __grid_constant__ CUtensorMap map_b,
+                                                             const __grid_constant__ CUtensorMap map_out,
+                                                             const __grid_constant__ CUtensorMap map_part) {
+    softmax_gemm<MODE, NB>(a, map_a, map_b, map_out, map_part, blockIdx.x, gridDim.x);
+}
+
+// DH and DW in one launch, each on a part of the units, where the products are so short that a launch counts.
+__global__ void __launch_bounds__(THREADS, 1) k_softmax_both(const GemmArgs dh, const GemmArgs dw, int dh_ctas, const __grid_constant__ CUtensorMap g_k,
+                                                             const __grid_constant__ CUtensorMap w_mn, const __grid_constant__ CUtensorMap dh_part,
+                                                             const __grid_constant__ CUtensorMap g_mn, const __grid_constant__ CUtensorMap h_mn,
+                                                             const __grid_constant__ CUtensorMap dw_out) {
+    if ((int)blockIdx.x < dh_ctas) softmax_gemm<DH, 1>(dh, g_k, w_mn, dh_part, dh_part, blockIdx.x, dh_ctas);
+    else softmax_gemm<DW, 1>(dw, g_mn, h_mn, dw_out, dw_out, blockIdx.x - dh_ctas, gridDim.x - dh_ctas);
 }
 
 // ---- rows with a label, packed -----------------------------------------------------------------------
@@ -1248,17 +1264,17 @@ int matrix_map(qgbdt_ctx *c, CUtensorMap *m, const void *p, long long cols, long
     return QGBDT_OK;
 }
 
-template <int MODE, int NB>
-int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mo, const CUtensorMap &mp,
-         cudaStream_t st) {
-    if (!(c->ops_configured >> (MODE * 2 + NB - 1) & 1)) {
-        QG_CUDA(c, cudaFuncSetAttribute(k_softmax_gemm<MODE, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<MODE, NB>::BYTES));
-        c->ops_configured |= 1u << (MODE * 2 + NB - 1);
+// Launches a kernel of `units` pairs of CTAs; `bit`: which of the context's kernels it is.
+template <typename... P, typename... A>
+int pairs(qgbdt_ctx *c, int bit, int smem, void (*kernel)(P...), int units, cudaStream_t st, const A &...args) {
+    if (!(c->ops_configured >> bit & 1)) {
+        QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        c->ops_configured |= 1u << bit;
     }
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)units * CG);
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = Layout<MODE, NB>::BYTES;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -1267,9 +1283,15 @@ int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, cons
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    QG_CUDA(c, cudaLaunchKernelEx(&cfg, k_softmax_gemm<MODE, NB>, a, ma, mb, mo, mp));
+    QG_CUDA(c, cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
     c->n_launches++;
     return QGBDT_OK;
+}
+
+template <int MODE, int NB>
+int gemm(qgbdt_ctx *c, const GemmArgs &a, int units, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &mo, const CUtensorMap &mp,
+         cudaStream_t st) {
+    return pairs(c, MODE * 2 + NB - 1, Layout<MODE, NB>::BYTES, k_softmax_gemm<MODE, NB>, units, st, a, ma, mb, mo, mp);
 }
 
 int up(int64_t x, int m) { return (int)((x + m - 1) / m * m); }
@@ -1342,8 +1364,7 @@ struct Gangs {
     int tn, n_tiles;   // columns of a tile, tiles
     int units() const { return size * gangs; }
 };
-Gangs gang_plan(const qgbdt_ctx *c, long long m_tiles, int dim, long long kb, int join_cost) {
-    const int units = c->sm_count / CG;
+Gangs gang_plan(int units, long long m_tiles, int dim, long long kb, int join_cost) {
     auto plan = [&](int tn) {
         const int n_tiles = (dim + tn - 1) / tn;
         Gangs best{1, units, n_tiles, false, tn, n_tiles};
@@ -1381,14 +1402,44 @@ Piece piece_plan(const qgbdt_ctx *c, int64_t classes, int n_pad, int dim) {
     Piece p;
     p.width = up(classes, 256);
     const int units = c->sm_count / CG, m_tiles = n_pad / BM, kb = (dim + BK - 1) / BK;
-    p.dh = gang_plan(c, m_tiles, dim, p.width / BK, 0);
-    p.dw = gang_plan(c, p.width / BM, dim, n_pad / BK, JOIN_COST);
+    p.dh = gang_plan(units, m_tiles, dim, p.width / BK, 0);
+    p.dw = gang_plan(units, p.width / BM, dim, n_pad / BK, JOIN_COST);
     const long long lines = (long long)p.dw.rounds * (p.width / BM), tiles = (long long)m_tiles * (p.width / BN);
     const double dw = p.dw.split ? (double)lines / p.dw.gangs : (double)((lines + p.dw.gangs - 1) / p.dw.gangs);
     // GRAD's epilogue takes as long as six blocks
     p.cost = (double)((tiles + units - 1) / units) * (kb > 6 ? kb : 6) + (double)m_tiles * ((dim + BN - 1) / BN) * (p.width / BK) / units +
              dw * (n_pad / BK) * p.dw.tn / BN + (p.dw.split ? JOIN_COST : 0) + PIECE_COST;
     return p;
+}
+
+// DH and DW of a piece in one launch: the units are divided so that both end together.  It is taken where that ends
+// before the two launches would, one of which costs about as long as LAUNCH_COST blocks take; long products, whose tiles have two
+// accumulators or are cut (DW), have launches of their own.
+// All gradients, two launches and one: 512 rows x 4000 classes x 256 31 and 24 us, 777 x 10007 x 129 42 and 36,
+// 3000 x 5000 x 512 69 and 56, 60 x 8000 x 40 25 and 19.
+constexpr int LAUNCH_COST = 13;
+double longest_run(const Gangs &g, long long m_tiles, long long kb) {
+    const long long lines = g.rounds * m_tiles;
+    return g.split ? (double)lines * kb / g.gangs : (double)((lines + g.gangs - 1) / g.gangs * kb);
+}
+bool both_plan(const qgbdt_ctx *c, Piece &p, int n_pad, int dim) {
+    const int units = c->sm_count / CG, m_tiles = n_pad / BM, v_tiles = p.width / BM, kb_h = p.width / BK, kb_w = n_pad / BK;
+    if (p.dh.tn != BN || p.dw.tn != BN || p.dw.split) return false;
+    double best = longest_run(p.dh, m_tiles, kb_h) + longest_run(p.dw, v_tiles, kb_w) + LAUNCH_COST;
+    bool found = false;
+    const Piece alone = p;
+    // DW's whole tiles in one round of its units, in two, ...: the others are DH's, whose products are cut anywhere
+    const int tiles = v_tiles * p.dw.n_tiles, first = tiles / units + 1;
+    for (int r = first; r < first + 5; ++r) {
+        const int u = units - (tiles + r - 1) / r;
+        if (u < 1) continue;
+        const Gangs h = gang_plan(u, m_tiles, dim, kb_h, 0), w = gang_plan(units - u, v_tiles, dim, kb_w, JOIN_COST);
+        if (h.tn != BN || w.tn != BN || w.split) continue;
+        const double a = longest_run(h, m_tiles, kb_h), b = longest_run(w, v_tiles, kb_w), cost = a > b ? a : b;
+        if (cost < best) best = cost, p.dh = h, p.dw = w, found = true;
+    }
+    if (!found) p = alone;
+    return found;
 }
 
 // Pieces of equal width and a narrower last one.  Of some widths that the memory allows (equal shares, and whole rounds of
@@ -1505,7 +1556,8 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
     const int n_pad = up(a.rows, 256), m_tiles = n_pad / BM;
     // the pieces: n_full of one width, then (kind 1) what is left
     const int64_t width = piece_width(c, a.classes, n_pad, a.dim), n_full = a.classes / width, left = a.classes - n_full * width;
-    const Piece kinds[2] = {piece_plan(c, width, n_pad, a.dim), left ? piece_plan(c, left, n_pad, a.dim) : Piece{}};
+    Piece kinds[2] = {piece_plan(c, width, n_pad, a.dim), left ? piece_plan(c, left, n_pad, a.dim) : Piece{}};
+    const bool both[2] = {both_plan(c, kinds[0], n_pad, a.dim), left && both_plan(c, kinds[1], n_pad, a.dim)};
     const int n_kinds = left ? 2 : 1, ld_g = kinds[0].width;
     if (unit_count(c, (long long)m_tiles * (ld_g / BN)) < 0 || unit_count(c, (long long)m_tiles * ((a.dim + BN - 1) / BN)) < 0)
         return qg_fail(c, QGBDT_ERR_ARG, "rows * classes is too large for one call");
@@ -1560,17 +1612,22 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) 
             bias = BiasArgs{bias_part, kinds[kind].width, nv, a.d_bias + v0, (nv + 31) / 32};
             if (v0 + nv < a.classes) QG_RUN(qg_launch(c, k_bias_finish, dim3(bias.blocks), 256, 0, st, bias, a.grad_loss, base.count));
         }
-        g = base;
-        g.v0 = v0, g.n_tiles = h.n_tiles, g.kb = kinds[kind].width / BK, g.add = kind == 0 && k > 0;
-        g.gang = h.size, g.gangs = h.gangs, g.rounds = h.rounds, g.split = h.split;
-        if ((rc = (h.tn == BN ? gemm<DH, 1> : gemm<DH, 2>)(c, g, h.units(), g_k, w_mn, g_store, dh_map[kind], st)) != QGBDT_OK) return rc;
-        g = base;
-        g.v0 = v0, g.m_tiles = (nv + BM - 1) / BM, g.n_tiles = d.n_tiles;
-        g.gang = d.size, g.gangs = d.gangs, g.rounds = d.rounds, g.split = d.split;
-        g.rows = nv, g.out = reinterpret_cast<uint16_t *>(a.d_weight), g.ld_out = a.ld_d_weight, g.out_map = out_map;
-        if ((rc = (d.tn == BN ? gemm<DW, 1> : gemm<DW, 2>)(c, g, d.units(), g_mn, h_mn, out, dw_map[kind], st)) != QGBDT_OK) return rc;
+        GemmArgs gh = base, gw = base;
+        gh.v0 = v0, gh.n_tiles = h.n_tiles, gh.kb = kinds[kind].width / BK, gh.add = kind == 0 && k > 0;
+        gh.gang = h.size, gh.gangs = h.gangs, gh.rounds = h.rounds, gh.split = h.split;
+        gw.v0 = v0, gw.m_tiles = (nv + BM - 1) / BM, gw.n_tiles = d.n_tiles;
+        gw.gang = d.size, gw.gangs = d.gangs, gw.rounds = d.rounds, gw.split = d.split;
+        gw.rows = nv, gw.out = reinterpret_cast<uint16_t *>(a.d_weight), gw.ld_out = a.ld_d_weight, gw.out_map = out_map;
+        if (both[kind]) {
+            constexpr int smem = Layout<DH, 1>::BYTES > Layout<DW, 1>::BYTES ? Layout<DH, 1>::BYTES : Layout<DW, 1>::BYTES;
+            rc = pairs(c, 8, smem, k_softmax_both, h.units() + d.units(), st, gh, gw, h.units() * CG, g_k, w_mn, dh_map[kind], g_mn, h_mn, out);
+            if (rc != QGBDT_OK) return rc;
+            continue;
+        }
+        if ((rc = (h.tn == BN ? gemm<DH, 1> : gemm<DH, 2>)(c, gh, h.units(), g_k, w_mn, g_store, dh_map[kind], st)) != QGBDT_OK) return rc;
+        if ((rc = (d.tn == BN ? gemm<DW, 1> : gemm<DW, 2>)(c, gw, d.units(), g_mn, h_mn, out, dw_map[kind], st)) != QGBDT_OK) return rc;
         if (!d.split) continue;
-        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, p, dw_part, d.tn, g, nv, st) : dw_finish<__half>(c, a, p, dw_part, d.tn, g, nv, st);
+        rc = bf16 ? dw_finish<__nv_bfloat16>(c, a, p, dw_part, d.tn, gw, nv, st) : dw_finish<__half>(c, a, p, dw_part, d.tn, gw, nv, st);
         if (rc != QGBDT_OK) return rc;
     }
     rc = bf16 ? dh_finish<__nv_bfloat16>(c, a, p, parts[0], parts[1], bias, st) : dh_finish<__half>(c, a, p, parts[0], parts[1], bias, st);
