@@ -5,7 +5,8 @@
 //
 // Both are gathers of whole rows: per (row, token) one row of `dim` elements comes out of L2 or DRAM and
 // is added in single precision, so the time is that traffic.  A row is read by a group of 2^lg lanes, one
-// vector of up to 16 bytes per lane; wider rows are cut into column blocks of 32 vectors.
+// vector of up to 16 bytes per lane; wider rows are cut into column blocks of 32 vectors.  Rows that allow only narrow
+// vectors and are read often are copied first, to where they allow wide ones.
 //
 // 65536 rows of 100 tokens, 256 bf16 each: 215 us for 3.4 GB of rows, which is what L2 delivers (13 TB/s; 15 % are hits in L1).
 //
@@ -35,6 +36,7 @@ struct EmbedPlan {
     int lg;        // log2 of the lanes per row
     int split;     // log2 of the parts a bag is cut into (forward)
     int col_blocks;
+    bool out_vec;  // the output's rows take whole vectors
 };
 
 // Two single-precision sums in one instruction.
@@ -59,6 +61,21 @@ __device__ __forceinline__ void add_row(float (&acc)[V], const OpsVec<T, V> &x) 
             const float2 y = unpack2(w[j / 2], T());
             add2(acc[j], acc[j + 1], y.x, y.y);
         }
+    }
+}
+
+// acc * scale: a whole vector, or one by one the `left` elements up to the row's end.
+template <typename T, int V>
+__device__ __forceinline__ void store_row(T *out, const float (&acc)[V], float scale, bool vec, int left) {
+    OpsVec<T, V> y;
+#pragma unroll
+    for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(acc[j] * scale);
+    if (vec) {
+        *reinterpret_cast<OpsVec<T, V> *>(out) = y;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j < left) out[j] = y.v[j];
     }
 }
 
@@ -129,12 +146,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_embed(const EmbedArgs a, const 
 #pragma unroll
                 for (int j = 0; j < V; ++j) acc[j] += part_sum[threadIdx.x + (q << p.lg)][j];
     }
-    if (live && part == 0) {
-        Vec y;
-#pragma unroll
-        for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(acc[j] * a.scale);
-        *reinterpret_cast<Vec *>(reinterpret_cast<T *>(a.out) + row * a.ld_out + col) = y;
-    }
+    if (live && part == 0) store_row(reinterpret_cast<T *>(a.out) + row * a.ld_out + col, acc, a.scale, p.out_vec, a.dim - col);
 }
 
 // The plain lookup, one token per row: a group of lanes per row, four vectors in flight per lane.
@@ -534,8 +546,10 @@ struct SegArgs {
     void *out;
     long long ld_out, n_entries;
     int dim, lg, col_blocks;
+    bool out_vec;           // the output's rows take whole vectors
+    int ld_partial;         // dim, rounded up to whole vectors
     float scale;
-    float *partial;         // [tiles][2][dim]: sum of a tile's first token when it began in an earlier tile;
+    float *partial;         // [tiles][2][ld_partial]: sum of a tile's first token when it began in an earlier tile;
                             // sum of its last token when it began here and goes on in the next tile
     long long sum_blocks;   // blocks that add; those behind them clear the rows no token points to, unless all are
     bool cleared;
@@ -553,7 +567,7 @@ __device__ __forceinline__ long long first_not_below(const uint2 *pair, long lon
     return lo;
 }
 
-template <typename T, int V>
+template <typename T, int V, bool OUT_VEC>
 __device__ void clear_rows(const SegArgs &a, long long block) {
     __shared__ unsigned absent[ZERO_ROWS / 32];
     const long long v0 = block * ZERO_ROWS;
@@ -574,7 +588,10 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
     for (int r = threadIdx.x >> a.lg; r < ZERO_ROWS; r += EMB_THREADS >> a.lg) {
         if (!(absent[r / 32] >> (r & 31) & 1)) continue;
         T *row = reinterpret_cast<T *>(a.out) + (v0 + r) * a.ld_out;
-        for (int col = (threadIdx.x & ((1 << a.lg) - 1)) * V; col < a.dim; col += V << a.lg) *reinterpret_cast<OpsVec<T, V> *>(row + col) = zero;
+        if constexpr (OUT_VEC)
+            for (int col = (threadIdx.x & ((1 << a.lg) - 1)) * V; col < a.dim; col += V << a.lg) *reinterpret_cast<OpsVec<T, V> *>(row + col) = zero;
+        else
+            for (int col = threadIdx.x & ((1 << a.lg) - 1); col < a.dim; col += 1 << a.lg) row[col] = zero.v[0];
     }
 }
 
@@ -583,13 +600,14 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
 // spill, 63).
 constexpr int sum_blocks_per_sm(int vector) { return vector == 16 ? 3 : 4; }
 
-template <typename T, int V>
+// OUT_VEC: the output's rows take whole vectors (tested at run time it costs registers: 395 and 441 us).
+template <typename T, int V, bool OUT_VEC>
 __global__ void __launch_bounds__(EMB_THREADS, sum_blocks_per_sm(sizeof(T) * V)) k_segment_sum(const SegArgs a) {
     qg_after_prior();
     using Vec = OpsVec<T, V>;
     const long long block = blockIdx.x;
     if (block >= a.sum_blocks) {   // behind the others: these wait for nothing
-        clear_rows<T, V>(a, block - a.sum_blocks);
+        clear_rows<T, V, OUT_VEC>(a, block - a.sum_blocks);
         return;
     }
     const int lane = threadIdx.x & ((1 << a.lg) - 1), group = threadIdx.x >> a.lg;
@@ -606,7 +624,7 @@ __global__ void __launch_bounds__(EMB_THREADS, sum_blocks_per_sm(sizeof(T) * V))
     if (cur == none) return;
     bool from_before = i0 > 0 && a.pair[i0 - 1].x == cur;
     auto put_partial = [&](int slot) {
-        float *w = a.partial + (t * 2 + slot) * a.dim + col;
+        float *w = a.partial + (t * 2 + slot) * a.ld_partial + col;
 #pragma unroll
         for (int j = 0; j < V; ++j) w[j] = acc[j];
     };
@@ -617,7 +635,14 @@ __global__ void __launch_bounds__(EMB_THREADS, sum_blocks_per_sm(sizeof(T) * V))
             Vec y;
 #pragma unroll
             for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(acc[j] * a.scale);
-            *reinterpret_cast<Vec *>(reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col) = y;
+            T *to = reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col;
+            if constexpr (OUT_VEC) {
+                *reinterpret_cast<Vec *>(to) = y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (col + j < a.dim) to[j] = y.v[j];
+            }
         }
     };
     const unsigned ld_bytes = (unsigned)(a.ld * sizeof(T));
@@ -670,7 +695,7 @@ constexpr int JOIN_PARTS = 2;    // lg_parts at most: 655360 pairs, 310 x 16 f32
 constexpr int JOIN_LOADS = 4;    // sums in flight per thread
 constexpr int JOIN_TILES = 32;   // tiles of a token that the block does not share
 
-template <typename T, int V>
+template <typename T, int V, bool OUT_VEC>
 __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, int lg_cols, int lg_parts) {
     qg_after_prior();
     __shared__ float part_sum[EMB_THREADS][V];
@@ -714,10 +739,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
         return lo;
     };
     auto put = [&](unsigned cur, int col, const float (&s)[V]) {
-        OpsVec<T, V> y;
-#pragma unroll
-        for (int j = 0; j < V; ++j) y.v[j] = OpsType<T>::store(s[j] * a.scale);
-        *reinterpret_cast<OpsVec<T, V> *>(reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col) = y;
+        store_row(reinterpret_cast<T *>(a.out) + (long long)cur * a.ld_out + col, s, a.scale, OUT_VEC, a.dim - col);
     };
     // the token's sums 0 .. links of this row of threads: every `step`-th from `first` on
     auto add_all = [&](float (&s)[V], long long t, long long links, int first, int step, int col) {
@@ -726,7 +748,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_segment_join(const SegArgs a, i
 #pragma unroll
             for (int u = 0; u < JOIN_LOADS; ++u) {
                 const long long at = min(l + u * step, links);
-                x[u] = *reinterpret_cast<const OpsVec<float, V> *>(a.partial + ((t + at) * 2 + (at == 0)) * a.dim + col);
+                x[u] = *reinterpret_cast<const OpsVec<float, V> *>(a.partial + ((t + at) * 2 + (at == 0)) * a.ld_partial + col);
             }
 #pragma unroll
             for (int u = 0; u < JOIN_LOADS; ++u)
@@ -850,6 +872,56 @@ __global__ void __launch_bounds__(EMB_THREADS) k_scan_sum(const SortArgs a, cons
 
 // ---- launches --------------------------------------------------------------------------------------
 
+// Copy of a matrix with rows that start on 16 bytes, zeros behind their ends.
+template <typename E>
+__global__ void __launch_bounds__(EMB_THREADS) k_align_rows(const E *in, long long ld, long long rows, int dim, E *out, int ld_out) {
+    qg_after_prior();
+    constexpr int V = 16 / sizeof(E);
+    const int vectors = ld_out / V;
+    for (long long i = blockIdx.x * (long long)EMB_THREADS + threadIdx.x; i < rows * vectors; i += (long long)gridDim.x * EMB_THREADS) {
+        const long long r = i / vectors;
+        const int d = (int)(i - r * vectors) * V;
+        OpsVec<E, V> x;
+#pragma unroll
+        for (int j = 0; j < V; ++j) x.v[j] = in[r * ld + min(d + j, dim - 1)];
+#pragma unroll
+        for (int j = 0; j < V; ++j) x.v[j] = d + j < dim ? x.v[j] : E(0);
+        *reinterpret_cast<OpsVec<E, V> *>(out + r * ld_out + d) = x;
+    }
+}
+
+// Rows that are read many times in vectors of less than 16 bytes: a copy of them with aligned rows pays for a launch and
+// a pass over them where enough is read, the sooner the narrower the vectors are.  Forward, without and with a copy, f16:
+// 20 MB in vectors of 2 bytes 12 and 9 us, of 4 bytes 8 and 9; 61 MB of 4 bytes 17 and 12, of 8 bytes 11 and 12; 504 MB of
+// 8 bytes 49 and 45, of 2 bytes 161 and 45; 2.2 GB of 2 bytes 747 and 216.  The gradient's: 725 and 315.
+constexpr int ALIGN_REUSE = 4;                // times a row is read, on average
+constexpr long long ALIGN_BYTES = 3ll << 20;  // that are read, per square of the vectors' bytes
+
+// The matrix to read from (`rows` rows), aligned where that pays for `reads` rows read in vectors of vb bytes; `below`: not
+// for vectors of this size on.
+struct AlignedRows {
+    size_t bytes = 0;   // of the copy; 0: none
+    int ld = 0;
+};
+AlignedRows align_plan(long long rows, int dim, int width, int vb, int below, long long reads) {
+    AlignedRows r;
+    if (vb >= below || reads < ALIGN_REUSE * rows || reads * dim * width < ALIGN_BYTES * vb * vb) return r;
+    r.ld = (dim * width + 15) / 16 * 16 / width;
+    r.bytes = qg_ws_size((size_t)rows * r.ld, width);
+    return r;
+}
+int align_rows(qgbdt_ctx *c, EmbedArgs &a, long long rows, const AlignedRows &r, QgWorkspace &ws, cudaStream_t st) {
+    const int w = qg_type_size(a.type);
+    const long long want = (rows * r.ld * w / 16 + EMB_THREADS - 1) / EMB_THREADS, most = c->sm_count * 16;
+    const unsigned blocks = (unsigned)(want < most ? want : most);
+    const void *in = a.table;
+    void *out = ws.take<char>(r.bytes);
+    const long long ld = a.ld;
+    a.table = out, a.ld = r.ld;
+    if (w == 4) return qg_launch(c, k_align_rows<uint32_t>, dim3(blocks), EMB_THREADS, 0, st, reinterpret_cast<const uint32_t *>(in), ld, rows, a.dim, reinterpret_cast<uint32_t *>(out), r.ld);
+    return qg_launch(c, k_align_rows<uint16_t>, dim3(blocks), EMB_THREADS, 0, st, reinterpret_cast<const uint16_t *>(in), ld, rows, a.dim, reinterpret_cast<uint16_t *>(out), r.ld);
+}
+
 int log2_at_least(long long v, int most) {   // smallest l <= most with 2^l >= v
     int l = 0;
     while (l < most && (1ll << l) < v) ++l;
@@ -863,8 +935,9 @@ int vec_bytes(const EmbedArgs &a) {
 }
 
 template <typename T, int V>
-int embed_typed(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
+int embed_typed(qgbdt_ctx *c, const EmbedArgs &a, bool out_vec, cudaStream_t st) {
     EmbedPlan p;
+    p.out_vec = out_vec;
     p.lg = log2_at_least((a.dim + V - 1) / V, 5);
     p.col_blocks = (a.dim + (V << p.lg) - 1) / (V << p.lg);
     if (a.bag == 1) {
@@ -971,13 +1044,17 @@ int segments_typed(qgbdt_ctx *c, SegArgs s, cudaStream_t st) {
     s.sum_blocks = (s.tiles + per_block - 1) / per_block * s.col_blocks;
     const long long blocks = s.sum_blocks + (s.cleared ? 0 : (s.n_entries + ZERO_ROWS - 1) / ZERO_ROWS);
     if (blocks > 0x7fffffffll) return qg_fail(c, QGBDT_ERR_ARG, "rows * bag * dim is too large for one call");
-    QG_RUN(qg_launch(c, k_segment_sum<T, V>, dim3((unsigned)blocks), EMB_THREADS, 0, st, s));
+    auto kernel = k_segment_sum<T, V, true>;
+    if constexpr (sizeof(T) * V == 16) kernel = s.out_vec ? kernel : k_segment_sum<T, V, false>;   // (of an aligned copy)
+    QG_RUN(qg_launch(c, kernel, dim3((unsigned)blocks), EMB_THREADS, 0, st, s));
     if (s.tiles > 1) {
         // four columns at most per thread: their partial sums are one 16-byte load
         constexpr int JV = V < 4 ? V : 4;
         const int lg = log2_at_least((s.dim + JV - 1) / JV, 7), lg_parts = lg >= 5 ? 0 : lg >= 5 - JOIN_PARTS ? 5 - lg : JOIN_PARTS;
         const long long groups = EMB_THREADS >> lg >> lg_parts;
-        QG_RUN(qg_launch(c, k_segment_join<T, JV>, dim3((unsigned)((s.tiles - 2) / groups + 1)), EMB_THREADS, 0, st, s, lg, lg_parts));
+        auto join = k_segment_join<T, JV, true>;
+        if constexpr (sizeof(T) * V == 16) join = s.out_vec ? join : k_segment_join<T, JV, false>;
+        QG_RUN(qg_launch(c, join, dim3((unsigned)((s.tiles - 2) / groups + 1)), EMB_THREADS, 0, st, s, lg, lg_parts));
     }
     return QGBDT_OK;
 }
@@ -993,24 +1070,39 @@ int scan_typed(qgbdt_ctx *c, const SortArgs &a, const SegArgs &g, bool wide, cud
 
 }  // namespace
 
-int qg_embed(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
-    const int vb = vec_bytes(a);
-#define CALL(T, V) embed_typed<T, V>(c, a, st)
-    return EMBED_DISPATCH(a.type, vb, CALL);
+int qg_embed(qgbdt_ctx *c, const EmbedArgs &given, cudaStream_t st) {
+    EmbedArgs a = given;
+    int vb = vec_bytes(a);
+    const AlignedRows r = align_plan(a.n_entries, a.dim, qg_type_size(a.type), vb, 16, a.bag > 1 ? a.rows * a.bag : 0);
+    QgWorkspace ws;
+    if (r.bytes) {
+        QG_RUN(qg_ws_open(c, r.bytes, st, &ws));
+        QG_RUN(align_rows(c, a, a.n_entries, r, ws, st));
+        vb = 16;
+    }
+    const bool out_vec = !r.bytes || vec_bytes(a) == 16;
+#define CALL(T, V) embed_typed<T, V>(c, a, out_vec, st)
+    QG_RUN(EMBED_DISPATCH(a.type, vb, CALL));
 #undef CALL
+    return r.bytes ? qg_ws_close(c, st) : QGBDT_OK;
 }
 
-int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
+int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &given, cudaStream_t st) {
+    EmbedArgs a = given;
     const long long n = a.rows * a.bag;
-    const int vb = vec_bytes(a), V = vb / qg_type_size(a.type);
+    const int w = qg_type_size(a.type), vb_given = vec_bytes(a);
+    const bool scan = n > 0 && n <= SCAN_PAIRS && n * a.n_entries <= SCAN_WORK;
+    const AlignedRows r = scan ? AlignedRows{} : align_plan(a.rows, a.dim, w, vb_given, 8, n);   // (504 MB in vectors of 8 bytes: 95 us, 99 with a copy)
+    const int vb = r.bytes ? 16 : vb_given, V = vb / w;
     SegArgs s{};
     s.n = n;
+    s.ld_partial = (a.dim + V - 1) / V * V, s.out_vec = !r.bytes;
     s.grad = a.table, s.ld = a.ld, s.out = a.out, s.ld_out = a.ld_out, s.n_entries = a.n_entries;
     s.dim = a.dim, s.scale = a.scale;
     SortArgs sa{};
     sa.tokens = a.tokens, sa.ld_tokens = a.ld_tokens, sa.n_entries = a.n_entries, sa.n = n, sa.status = a.status;
     set_divisor(sa, (unsigned)a.bag);
-    if (n > 0 && n <= SCAN_PAIRS && n * a.n_entries <= SCAN_WORK) {
+    if (scan) {
 #define CALL(T, V) scan_typed<T, V>(c, sa, s, a.token_type == QGBDT_I64, st)
         return EMBED_DISPATCH(a.type, vb, CALL);
 #undef CALL
@@ -1018,8 +1110,7 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     s.lg = log2_at_least((a.dim + V - 1) / V, 5);
     s.col_blocks = (a.dim + (V << s.lg) - 1) / (V << s.lg);
     // tiles: short lists go once over the groups of 768 threads per SM (more and shorter ones add to the joining: 185000 pairs
-    // of 200 bytes 34 us, 39 us with 1024), long ones four times,
-    // which evens out what the SMs get; at least 16 pairs
+    // of 200 bytes 34 us, 39 us with 1024), long ones four times, which evens out what the SMs get; at least 16 pairs
     const long long fit = (long long)c->sm_count * 768 >> s.lg, pairs = (n * s.col_blocks + fit - 1) / fit;
     long long tile = pairs <= 128 ? pairs : pairs <= 512 ? 128 : pairs / 4;
     tile = tile < 16 ? 16 : (tile + EMB_UNROLL - 1) / EMB_UNROLL * EMB_UNROLL;
@@ -1031,19 +1122,23 @@ int qg_embed_backward(qgbdt_ctx *c, const EmbedArgs &a, cudaStream_t st) {
     const SortPlan sp = small ? SortPlan{} : sort_plan(c, n, a.n_entries);
     const size_t digits = small ? 0 : (size_t)1 << sp.bits;
     const size_t bytes = 2 * qg_ws_size((size_t)n + 2 * EMB_UNROLL, sizeof(uint2)) + qg_ws_size(digits * count_stride(sp.blocks), sizeof(unsigned)) +
-                         qg_ws_size(digits, sizeof(unsigned)) + qg_ws_size((size_t)s.tiles * 2 * a.dim, sizeof(float));
+                         qg_ws_size(digits, sizeof(unsigned)) + qg_ws_size((size_t)s.tiles * 2 * s.ld_partial, sizeof(float)) + r.bytes;
     QgWorkspace ws;
     int rc = qg_ws_open(c, bytes, st, &ws);
     if (rc != QGBDT_OK) return rc;
     uint2 *buf0 = ws.take<uint2>((size_t)n + 2 * EMB_UNROLL), *buf1 = ws.take<uint2>((size_t)n + 2 * EMB_UNROLL);
     unsigned *counts = ws.take<unsigned>(digits * count_stride(sp.blocks)), *totals = ws.take<unsigned>(digits);
-    s.partial = ws.take<float>((size_t)s.tiles * 2 * a.dim);
+    s.partial = ws.take<float>((size_t)s.tiles * 2 * s.ld_partial);
+    if (r.bytes) {
+        QG_RUN(align_rows(c, a, a.rows, r, ws, st));
+        s.grad = a.table, s.ld = a.ld, s.out_vec = vec_bytes(a) == 16;
+    }
     s.pair = buf0;
     Clearing z{};
     if (ahead) {
-        const int w = qg_type_size(a.type);
-        z.all = ClearArgs{reinterpret_cast<char *>(a.out), a.ld_out * w, 0, a.n_entries, a.dim / V, log2_at_least(a.dim / V, 8), vb};
-        const long long want = (a.n_entries * a.dim / V + EMB_THREADS * 16 - 1) / (EMB_THREADS * 16), most = (long long)c->sm_count * CLEAR_BLOCKS;
+        const int W = vb_given / w;   // the output's rows take these
+        z.all = ClearArgs{reinterpret_cast<char *>(a.out), a.ld_out * w, 0, a.n_entries, a.dim / W, log2_at_least(a.dim / W, 8), vb_given};
+        const long long want = (a.n_entries * a.dim / W + EMB_THREADS * 16 - 1) / (EMB_THREADS * 16), most = (long long)c->sm_count * CLEAR_BLOCKS;
         z.blocks = (int)(want < most ? want : most);
         s.cleared = true;
     }

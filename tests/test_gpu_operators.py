@@ -212,6 +212,25 @@ def test_embed_backward_few_pairs_beside_the_entries(ctx, rows, bag, entries, di
     within(got, want, (count + 1) * 2.0 ** -24 * size + UNIT[DTYPES[dtype]] * want.abs() + TINY[DTYPES[dtype]])
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows,bag,entries,dim,left,right", [(7001, 40, 900, 51, 1, 1), (20000, 40, 640, 54, 0, 0), (20011, 50, 500, 92, 3, 1), (3000, 40, 600, 417, 0, 0),
+                                                             (900, 60, 240000, 515, 0, 0)])
+def test_embed_rows_that_are_read_often_and_start_anywhere(ctx, rows, bag, entries, dim, left, right, dtype):
+    """Enough is read of rows that do not start on 16 bytes for a copy that does; results as ever, the gaps of the outputs left alone."""
+    dtype = DTYPES[dtype]
+    table, tok = embed_case(rows, bag, entries, dim, dtype, right, False, rows)
+    wide = torch.full((rows, left + dim + right), 7.0, device="cuda", dtype=dtype)
+    out = ctx.embed(table, tok, scale=0.5, out=wide[:, left:left + dim])
+    want, size = embed_exact(table, tok, 0.5)
+    within(out, want, (bag + 1) * 2.0 ** -24 * size)
+    assert bool((wide[:, :left] == 7).all()) and bool((wide[:, left + dim:] == 7).all())
+    wide = torch.full((entries, left + dim + right), 7.0, device="cuda", dtype=dtype)
+    grad = out.clone() if left + right == 0 else torch.randn((rows, dim + right), generator=gen(rows), device="cuda").to(dtype)[:, :dim]
+    got = ctx.embed_backward(grad, tok, entries, scale=0.5, grad_table=wide[:, left:left + dim])
+    check_embed_grad(got, grad, tok, entries, 0.5)
+    assert bool((wide[:, :left] == 7).all()) and bool((wide[:, left + dim:] == 7).all())
+
+
 def test_embed_gradient_by_differences(ctx):
     """d sum(w * embed(table)) / d table against central differences (the function is linear: only rounding is left)."""
     g = gen(3)
