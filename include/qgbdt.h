@@ -317,13 +317,16 @@ const char *qgbdt_noalloc_last_error(void);
 /* Embedding bag: d_out[i] = scale * sum over k < bag of d_table[d_tokens[i][k]], i < n_rows, in
  * ascending k; a negative token is a missing one (a row of missing tokens gives zeros).  bag = 1 is the
  * plain scaled lookup.  d_table [n_entries][ld_table] and d_out [n_rows][ld_out] of `type`, d_tokens
- * [n_rows][ld_tokens] of `token_type`.  d_out must not overlap d_table.  rows * bag < 2^31. */
+ * [n_rows][ld_tokens] of `token_type`.  d_out must not overlap d_table.  rows * bag < 2^31.  A table
+ * whose rows do not start on 16 bytes and are read often is copied into the work buffer (1 GiB at
+ * most), with rows that do; the same holds for the gradient's rows. */
 int qgbdt_embed(qgbdt_ctx *ctx, const void *d_table, int32_t type, int64_t n_entries, int32_t dim, int64_t ld_table,
                 const void *d_tokens, int32_t token_type, int64_t n_rows, int32_t bag, int64_t ld_tokens, float scale,
                 void *d_out, int64_t ld_out, int32_t *d_status, void *stream);
 /* Its gradient: d_grad_table[v] = scale * sum of d_grad[i] over all (i, k) with d_tokens[i][k] == v.
  * Every row of d_grad_table [n_entries][ld_grad_table] is written, zeros where no token points.  The
- * tokens are sorted and the sums taken in an order that the tokens alone decide. */
+ * tokens are sorted and the sums taken in an order that the tokens alone decide.  d_grad_table must
+ * not overlap d_grad. */
 int qgbdt_embed_backward(qgbdt_ctx *ctx, const void *d_grad, int32_t type, int64_t ld_grad, const void *d_tokens,
                          int32_t token_type, int64_t n_rows, int32_t bag, int64_t ld_tokens, float scale,
                          void *d_grad_table, int64_t n_entries, int32_t dim, int64_t ld_grad_table, int32_t *d_status,

@@ -896,6 +896,7 @@ __global__ void __launch_bounds__(EMB_THREADS) k_align_rows(const E *in, long lo
 // 8 bytes 49 and 45, of 2 bytes 161 and 45; 2.2 GB of 2 bytes 747 and 216.  The gradient's: 725 and 315.
 constexpr int ALIGN_REUSE = 4;                // times a row is read, on average
 constexpr long long ALIGN_BYTES = 3ll << 20;  // that are read, per square of the vectors' bytes
+constexpr size_t ALIGN_MOST = 1ull << 30;     // a larger copy is not worth its memory
 
 // The matrix to read from (`rows` rows), aligned where that pays for `reads` rows read in vectors of vb bytes; `below`: not
 // for vectors of this size on.
@@ -907,7 +908,8 @@ AlignedRows align_plan(long long rows, int dim, int width, int vb, int below, lo
     AlignedRows r;
     if (vb >= below || reads < ALIGN_REUSE * rows || reads * dim * width < ALIGN_BYTES * vb * vb) return r;
     r.ld = (dim * width + 15) / 16 * 16 / width;
-    r.bytes = qg_ws_size((size_t)rows * r.ld, width);
+    const size_t bytes = qg_ws_size((size_t)rows * r.ld, width);
+    if (bytes <= ALIGN_MOST) r.bytes = bytes;
     return r;
 }
 int align_rows(qgbdt_ctx *c, EmbedArgs &a, long long rows, const AlignedRows &r, QgWorkspace &ws, cudaStream_t st) {
