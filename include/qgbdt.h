@@ -348,8 +348,10 @@ int qgbdt_softmax_ce(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_hidden, co
  * with lse as the forward call gave it: g[i][v] = (exp(z[i][v] - lse[i]) - [v == label i]) * grad_loss /
  * (rows with a label), d_grad_hidden = g d_weight, d_grad_weight = g^T d_hidden, d_grad_bias = column
  * sums of g (or NULL).  d_grad_hidden and d_grad_weight have the inputs' type; rows without a label get
- * zeros.  The logits are recomputed in pieces of the classes; the probabilities of a piece are held in
- * the inputs' type in the work buffer (at most 384 MiB of them, or one piece of 256 classes). */
+ * zeros.  The logits are recomputed in pieces of the classes; g / grad_loss * (rows with a label) of a
+ * piece is rounded to the inputs' type for the two products (half precision: as 2^15 times itself, so
+ * that small probabilities keep their bits) and held in the work buffer (at most 384 MiB of it, or one
+ * piece of 256 classes); d_grad_bias is summed before that rounding. */
 int qgbdt_softmax_ce_backward(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_hidden, const void *d_weight,
                               int64_t ld_weight, int32_t type, const float *d_bias, const void *d_labels,
                               int32_t label_type, int64_t n_rows, int64_t n_classes, int32_t dim, const float *d_lse,

@@ -13,10 +13,13 @@
 // empty the accumulators, of which tensor memory holds two, so that the epilogue of a tile runs under the
 // products of the next.  What the epilogues do:
 //   LOSS  per row of the tile: maximum and sum of exponentials; the label's logit.  No logit leaves the SM.
-//   GRAD  g of a piece of the classes, rounded to the inputs' type (relative error 2^-8 in bf16, 2^-11 in f16,
-//         of each g on its own: as much as the outputs' own rounding, averaged down by the sums that follow;
-//         the scale s is applied behind those sums, so that small g do not vanish in half precision), and its
-//         column sums in single precision for the bias.
+//   GRAD  g of a piece of the classes, rounded to the inputs' type (relative error 2^-9 in bf16, 2^-12 in f16, of
+//         each g on its own: as much as the outputs' own rounding, averaged down by the sums that follow; operands of
+//         the tensor cores have no more bits, and two of them per g would double the products), and its column sums in
+//         single precision for the bias.  Half precision holds 2^15 g: |g| <= 1 leaves it that much room, and without
+//         it classes of a probability below 2^-14 would lose bits and below 2^-25 vanish.  With it the error above
+//         holds from |g| = 2^-29 on; below it is 2^-40 at most.  The scale s, with 2^-15 in it, is applied behind the
+//         sums, to numbers in single precision.
 //   DH    the piece's contribution to dH, in single precision.
 //   DW    rows of dW, complete with every piece, written in the output type.
 //
@@ -32,6 +35,8 @@
 // included, never meets a product.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ops_internal.cuh"
 #include "tensor_core.cuh"
 
@@ -45,6 +50,7 @@ constexpr int STORE_BYTES = 32 * 128;       // staging buffer of a warp: 32 rows
 constexpr int TMEM_COLS = 512, ACC_COLS = 256;
 constexpr int GROUP_M = 16;                 // row tiles that go through all column tiles together
 constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float F16_UP = 32768.0f;          // g in half precision is held as this multiple
 
 enum Mode { LOSS, GRAD, DH, DW };
 
@@ -103,6 +109,10 @@ struct GemmArgs {
 
 __device__ __forceinline__ float out_scale(const float *grad_loss, int count) {
     return (grad_loss ? *grad_loss : 1.0f) / (float)(count > 0 ? count : 1);
+}
+// The same for sums of products with g as it is held.
+__device__ __forceinline__ float product_scale(const float *grad_loss, int count, bool bf16) {
+    return out_scale(grad_loss, count) * (bf16 ? 1.0f : 1.0f / F16_UP);
 }
 
 // The tiles of LOSS and GRAD in the order in which they are taken: groups of GROUP_M row tiles, in a group all row
@@ -248,7 +258,7 @@ struct Epilogue {
 
     __device__ Epilogue(const GemmArgs &a_, const CUtensorMap *o, const CUtensorMap *p, uint32_t b, int l, int n)
         : a(a_), map_out(o), map_part(p), buf(b), lane(l), count(n) {
-        if (MODE == DW) scale = out_scale(a.grad_loss, count);
+        if (MODE == DW) scale = product_scale(a.grad_loss, count, a.bf16);
     }
 
     // What the next tile's rows need from memory, loaded under this tile's work and not looked at before begin().
@@ -402,6 +412,10 @@ struct Epilogue {
 #pragma unroll
             for (int j = 0; j < 64; ++j) x[j] = live ? x[j] : 0.0f;
         }
+        if (!a.bf16) {
+#pragma unroll
+            for (int j = 0; j < 64; j += 2) tc_mul2(x[j], x[j + 1], F16_UP);
+        }
         const uint32_t to = buf + h * STORE_BYTES;
         if (lane == 0) tc_store_wait_read<1>();   // the copy out of this buffer has been read
         __syncwarp();
@@ -421,7 +435,7 @@ struct Epilogue {
                 float y[32];
 #pragma unroll
                 for (int j = 0; j < 32; ++j) y[j] = x[k + j];
-                sums[k] = column_sums(y, lane);
+                sums[k] = column_sums(y, lane) * (a.bf16 ? 1.0f : 1.0f / F16_UP);
             }
         }
     }
@@ -1166,7 +1180,7 @@ __global__ void __launch_bounds__(256) k_dh_finish(const DhParts full, const DhP
     const int lane = threadIdx.x & ((1 << lg) - 1), parts = 1 << lg_parts, part = threadIdx.x >> lg & (parts - 1);
     const int r = blockIdx.x * (256 >> lg >> lg_parts) + (threadIdx.x >> lg >> lg_parts);
     const int n = *count, p = r < rows ? pos_of[r] : -1, m_live = (n + BM - 1) / BM;
-    const float scale = p >= 0 ? out_scale(grad_loss, n) : 0.0f;   // (an infinite grad_loss times 0 would be NaN)
+    const float scale = p >= 0 ? product_scale(grad_loss, n, std::is_same<T, __nv_bfloat16>::value) : 0.0f;   // (an infinite grad_loss times 0 would be NaN)
     // of one set: the gangs g0 to g1 that worked on the row's tile in a round
     struct Span {
         int round = -1, place, g0, g1;
@@ -1218,7 +1232,7 @@ __global__ void __launch_bounds__(256) k_dw_finish(const float *part, int tn, in
     if (cut == (long long)place * kb) return;
     const int g0 = line.gang_of((long long)place * kb), g1 = line.gang_of((long long)(place + 1) * kb - 1);
     if (g0 != g - 1) return;   // an earlier cut of the same tile
-    const float scale = out_scale(grad_loss, n);
+    const float scale = product_scale(grad_loss, n, std::is_same<T, __nv_bfloat16>::value);
     const int round = place / m_tiles, m = place - round * m_tiles, col = (round * gang + member) * tn;
     const int r = blockIdx.y * 8 + threadIdx.x / 32;
     if (m * BM + r >= rows) return;

@@ -1,0 +1,47 @@
+"""Operators on top of the trees at the edges of their range: small probabilities in half precision, streams and captured
+graphs over the shared work buffer, extreme norms, sizes and strides, autograd's bookkeeping.  Tolerances are derived beside
+each check; u(T) = 2^-9 (bf16), 2^-12 (f16) and 2^-24 (f32) is the relative error of one rounding to nearest."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2207_09682_b200 import binding
+    c = binding.Context(binding.make_params())
+    yield c
+    c.close()
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+@pytest.mark.parametrize("rows,classes,dim", [(600, 300, 64), (777, 1003, 129), (3000, 5000, 520), (5000, 31000, 1024)])
+def test_rare_classes_keep_their_gradients_in_half_precision(ctx, rows, classes, dim):
+    """A third of the classes has probabilities near 2e-8 in every row, below the 2^-25 at which a half-precision number
+    vanishes; with the loss scale their gradients are ordinary numbers of the outputs' type.  Column 0 of the hidden rows is
+    zero, so that the rare classes' weights of 100 there change no logit and fill column 0 of the rows' gradient alone."""
+    h = 1.0 + 0.1 * torch.randn((rows, dim), generator=gen(1), device="cuda")
+    w = torch.randn((classes, dim), generator=gen(2), device="cuda") * (0.1 / math.sqrt(dim))
+    common = classes * 2 // 3
+    h[:, 0], w[:, 0], w[common:, 0] = 0.0, 0.0, 100.0
+    h, w = h.half(), w.half()
+    b = torch.zeros(classes, device="cuda")
+    b[common:] = math.log(2e-8 * common)
+    y = torch.randint(0, common, (rows,), generator=gen(3), device="cuda")
+    r = ctx.softmax_ce(h, w, y, bias=b)
+    dh, dw, db = ctx.softmax_ce_backward(h, w, y, r.lse, bias=b, grad_loss=torch.full((1,), 65536.0, device="cuda"))
+    z = h.double() @ w.double().t() + b.double()
+    p = torch.exp(z - torch.logsumexp(z, 1, keepdim=True))[:, common:] * (65536.0 / rows)
+    # all terms of these sums are positive, so that relative errors stay: p and the output are rounded to 2^-12 each; logits
+    # and lse behind p are off by dim * 2^-23 * sum |h w| <= 2^-11.5 each (1024 terms of 0.0025); the sums themselves, in chains of a
+    # few hundred, by 2^-15: below 2^-9 in all
+    for got, want in ((dw[common:], p.t() @ h.double()), (dh[:, 0], p @ w[common:, 0].double()), (db[common:], p.sum(0))):
+        assert bool(((got.double() - want).abs() <= 2.0 ** -9 * want.abs()).all())
