@@ -99,9 +99,12 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
     if (bytes > c->ops_ws_bytes) {
         if (c->ops_ws) {
             if (c->ops_ws_captured) {
-                c->ops_ws_old.push_back(c->ops_ws);   // a graph may hold its address
+                // a graph may hold its address; nothing is waited for, and a call that still runs shares the counters with
+                // this one, so that the event goes on to order them
+                c->ops_ws_old.push_back(c->ops_ws);
             } else {
                 if (c->ops_ws_used) QG_CUDA(c, cudaEventSynchronize(c->ops_ws_event));
+                c->ops_ws_used = false;
                 cudaFree(c->ops_ws);
             }
             c->ops_ws = nullptr;
@@ -114,7 +117,6 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
             return qg_fail(c, QGBDT_ERR_ALLOC, "cudaMalloc of %zu bytes of work memory failed", want);
         }
         c->ops_ws_bytes = want;
-        c->ops_ws_used = false;
     }
     if (capturing) {
         c->ops_ws_captured = true;

@@ -45,3 +45,47 @@ def test_rare_classes_keep_their_gradients_in_half_precision(ctx, rows, classes,
     # few hundred, by 2^-15: below 2^-9 in all
     for got, want in ((dw[common:], p.t() @ h.double()), (dh[:, 0], p @ w[common:, 0].double()), (db[common:], p.sum(0))):
         assert bool(((got.double() - want).abs() <= 2.0 ** -9 * want.abs()).all())
+
+
+# ---- streams, captured graphs, the shared work buffer ----------------------------------------------
+
+def loss_case(rows, classes, dim, seed):
+    h = torch.randn((rows, dim), generator=gen(seed), device="cuda").bfloat16()
+    w = (torch.randn((classes, dim), generator=gen(seed + 1), device="cuda") * 0.2).bfloat16()
+    return h, w, torch.randint(0, classes, (rows,), generator=gen(seed + 2), device="cuda")
+
+
+def captured_context(case):
+    """A context over whose work buffer a graph has been captured; the graph, its outputs, what they have to be."""
+    from paper_2207_09682_b200 import binding
+    c = binding.Context(binding.make_params())
+    want = [t.clone() for t in c.softmax_ce(*case)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = c.softmax_ce(*case)
+    return c, graph, got, want
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_a_call_that_grows_the_buffer_after_a_capture_waits_for_the_last_call(ctx):
+    """Both calls count their blocks in the same words; the graph keeps the buffer that it was captured over."""
+    cases = [loss_case(rows, classes, 64, rows) for rows, classes in ((300, 700), (8192, 30000), (8191, 60000))]
+    want = [[t.clone() for t in ctx.softmax_ce(*case)] for case in cases]
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    for k in range(3):
+        c, graph, got, _ = captured_context(cases[0])
+        torch.cuda.synchronize()
+        first = [c.softmax_ce(*cases[0], stream=a) for _ in range(50)]   # in flight when the next call grows the buffer
+        second = c.softmax_ce(*cases[1], stream=b)
+        third = c.softmax_ce(*cases[2], stream=a)
+        torch.cuda.synchronize()
+        assert all(same(r, want[0]) for r in first) and same(second, want[1]) and same(third, want[2])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(got, want[0])
+        del graph
+        c.close()
