@@ -303,9 +303,12 @@ const char *qgbdt_noalloc_last_error(void);
  *  - ld_* are row strides in elements; any stride >= the row length and any alignment to the element is
  *    accepted (16-byte aligned rows are the fast case).
  *  - All calls are asynchronous on `stream`.  They share one work buffer of the context, which grows
- *    with the largest call (growing synchronises); calls on different streams are ordered after one
- *    another by an event.  A call whose buffer is large enough may be captured into a CUDA graph;
- *    replays of that graph are not ordered against other calls, order them yourself.
+ *    with the largest call (growing synchronises, unless a graph has been captured over the buffer);
+ *    calls on different streams are ordered after one another by an event.  A call whose buffer is
+ *    large enough may be captured into a CUDA graph; calls on several streams of one capture are
+ *    ordered after one another in the graph (up to four captures may be under way side by side).
+ *    Replays of a graph are not ordered against other calls or graphs, order them yourself, and end
+ *    before the context does.
  *  - d_status: optional device word that the caller clears; set to 1 when a token was >= n_entries or a
  *    label >= n_classes (such tokens count as missing, such rows as rows without a label). */
 #define QGBDT_F32 0

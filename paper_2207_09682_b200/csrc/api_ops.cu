@@ -26,6 +26,8 @@ int ops_init(qgbdt_ctx *c) {
         QG_CUDA(c, cudaMemset(c->d_ops_counters, 0, OPS_COUNTERS * sizeof(unsigned int)));
         QG_CUDA(c, cudaDeviceSynchronize());
     }
+    for (qgbdt_ctx::OpsCapture &e : c->ops_captures)
+        if (!e.event) QG_CUDA(c, cudaEventCreateWithFlags(&e.event, cudaEventDisableTiming));
     QG_CUDA(c, cudaEventCreateWithFlags(&c->ops_ws_event, cudaEventDisableTiming));
     return QGBDT_OK;
 }
@@ -86,11 +88,19 @@ int check_softmax(qgbdt_ctx *c, const SoftmaxArgs &a) {
     return QGBDT_OK;
 }
 
+// The last call of a capture, or NULL.
+qgbdt_ctx::OpsCapture *last_of_capture(qgbdt_ctx *c, unsigned long long id) {
+    for (qgbdt_ctx::OpsCapture &e : c->ops_captures)
+        if (e.used && e.id == id) return &e;
+    return nullptr;
+}
+
 }  // namespace
 
 int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    QG_CUDA(c, cudaStreamIsCapturing(st, &cap));
+    unsigned long long capture = 0;
+    QG_CUDA(c, cudaStreamGetCaptureInfo(st, &cap, &capture));
     const bool capturing = cap != cudaStreamCaptureStatusNone;
     if (capturing && (!c->ops_ws_event || bytes > c->ops_ws_bytes))
         return qg_fail(c, QGBDT_ERR_STATE, "the work buffer has to grow: make one call of this size before the stream is captured");
@@ -120,6 +130,8 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
     }
     if (capturing) {
         c->ops_ws_captured = true;
+        const qgbdt_ctx::OpsCapture *last = last_of_capture(c, capture);
+        if (last && last->stream != st) QG_CUDA(c, cudaStreamWaitEvent(st, last->event, 0));
     } else if (c->ops_ws_used) {
         unsigned long long id = 0;
         QG_CUDA(c, cudaStreamGetId(st, &id));
@@ -132,8 +144,19 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
 
 int qg_ws_close(qgbdt_ctx *c, cudaStream_t st) {
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    QG_CUDA(c, cudaStreamIsCapturing(st, &cap));
-    if (cap != cudaStreamCaptureStatusNone) return QGBDT_OK;
+    unsigned long long capture = 0;
+    QG_CUDA(c, cudaStreamGetCaptureInfo(st, &cap, &capture));
+    if (cap != cudaStreamCaptureStatusNone) {
+        qgbdt_ctx::OpsCapture *last = last_of_capture(c, capture);
+        if (!last) {
+            last = &c->ops_captures[c->ops_capture_next];
+            c->ops_capture_next = (c->ops_capture_next + 1) % (int)(sizeof(c->ops_captures) / sizeof(*last));
+            last->used = false;
+        }
+        QG_CUDA(c, cudaEventRecord(last->event, st));
+        last->id = capture, last->stream = st, last->used = true;
+        return QGBDT_OK;
+    }
     QG_CUDA(c, cudaStreamGetId(st, &c->ops_ws_stream));
     QG_CUDA(c, cudaEventRecord(c->ops_ws_event, st));
     c->ops_ws_used = true;
@@ -147,6 +170,10 @@ void qg_ops_destroy(qgbdt_ctx *c) {
     if (c->d_ops_counters) cudaFree(c->d_ops_counters);
     if (c->ops_fault) cudaFreeHost(c->ops_fault);
     if (c->ops_ws_event) cudaEventDestroy(c->ops_ws_event);
+    for (qgbdt_ctx::OpsCapture &e : c->ops_captures) {
+        if (e.event) cudaEventDestroy(e.event);
+        e = qgbdt_ctx::OpsCapture{};
+    }
     c->ops_ws = nullptr;
     c->d_ops_counters = nullptr;
     c->ops_fault = nullptr;

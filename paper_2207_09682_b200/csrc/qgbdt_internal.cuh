@@ -282,6 +282,13 @@ struct qgbdt_ctx {
     cudaEvent_t ops_ws_event = nullptr;         // end of the last call's use
     unsigned long long ops_ws_stream = 0;       // id of that call's stream
     bool ops_ws_used = false, ops_ws_captured = false;
+    struct OpsCapture {                         // the last call inside a stream capture
+        unsigned long long id;                  // of the capture
+        cudaStream_t stream;
+        cudaEvent_t event;                      // end of the call
+        bool used;
+    } ops_captures[4] = {};                     // as many captures may be under way side by side
+    int ops_capture_next = 0;                   // the entry that the next capture takes: the oldest
     std::vector<void *> ops_ws_old;             // outgrown buffers that a captured graph may still use
     int *ops_fault = nullptr;                   // pinned word set by an operator's kernel that gave up waiting
     unsigned int *d_ops_counters = nullptr;     // zero between calls

@@ -89,3 +89,59 @@ def test_a_call_that_grows_the_buffer_after_a_capture_waits_for_the_last_call(ct
         assert same(got, want[0])
         del graph
         c.close()
+
+
+def test_calls_on_several_streams_of_one_capture_are_ordered(ctx):
+    """Forked branches of a graph that use the same work buffer: the later call waits for the earlier one's branch."""
+    a, b = loss_case(8192, 30000, 64, 1), loss_case(8000, 20000, 64, 2)
+    tok = torch.randint(0, 900, (30000, 4), generator=gen(5), device="cuda")
+    grad = torch.randn((30000, 16), generator=gen(6), device="cuda")
+    want_a, want_b, want_e = ctx.softmax_ce(*a), ctx.softmax_ce(*b), ctx.embed_backward(grad, tok, 900)
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        got_b = ctx.softmax_ce(*b, stream=side)
+        got_a = ctx.softmax_ce(*a)
+        got_e = ctx.embed_backward(grad, tok, 900, stream=side)
+        got_a2 = ctx.softmax_ce(*a)
+        main.wait_stream(side)
+    for _ in range(5):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert same(got_a, want_a) and same(got_b, want_b) and same([got_e], [want_e]) and same(got_a2, want_a)
+
+
+def test_several_captures_one_after_another_and_side_by_side(ctx):
+    """More captures than a context follows at a time; a call belongs to the capture of its own stream."""
+    case = loss_case(700, 900, 64, 7)
+    want = [t.clone() for t in ctx.softmax_ce(*case)]
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(6):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = ctx.softmax_ce(*case), ctx.softmax_ce(*case)
+        graphs.append((graph, got))
+    for graph, got in graphs:
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(got[0], want) and same(got[1], want)
+    one, two = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    s, t = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        one.capture_begin(capture_error_mode="relaxed")
+        first = ctx.softmax_ce(*case)
+    with torch.cuda.stream(t):
+        two.capture_begin(capture_error_mode="relaxed")
+        second = ctx.softmax_ce(*case)
+    with torch.cuda.stream(s):
+        third = ctx.softmax_ce(*case)
+        one.capture_end()
+    with torch.cuda.stream(t):
+        two.capture_end()
+    for graph, results in ((one, (first, third)), (two, (second,))):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(same(r, want) for r in results)
