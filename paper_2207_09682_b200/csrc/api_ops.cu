@@ -112,6 +112,7 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
                 // a graph may hold its address; nothing is waited for, and a call that still runs shares the counters with
                 // this one, so that the event goes on to order them
                 c->ops_ws_old.push_back(c->ops_ws);
+                c->ops_ws_captured = false;   // over the buffer that takes its place
             } else {
                 if (c->ops_ws_used) QG_CUDA(c, cudaEventSynchronize(c->ops_ws_event));
                 c->ops_ws_used = false;

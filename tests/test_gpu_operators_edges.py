@@ -56,7 +56,8 @@ def loss_case(rows, classes, dim, seed):
 
 
 def captured_context(case):
-    """A context over whose work buffer a graph has been captured; the graph, its outputs, what they have to be."""
+    """A context over whose work buffer a graph has been captured; the graph (which reads `case`), its outputs, what they
+    have to be."""
     from paper_2207_09682_b200 import binding
     c = binding.Context(binding.make_params())
     want = [t.clone() for t in c.softmax_ce(*case)]
@@ -145,3 +146,28 @@ def test_several_captures_one_after_another_and_side_by_side(ctx):
         graph.replay()
         torch.cuda.synchronize()
         assert all(same(r, want) for r in results)
+
+
+def test_outgrown_buffers_that_no_graph_was_captured_over_are_freed():
+    """Work buffers of 0.5 to 2 GB one after the other, in a context over whose first, small buffer a graph was captured."""
+    case = loss_case(300, 700, 64, 3)   # the graph reads it
+    c, graph, got, want = captured_context(case)
+    weight = torch.zeros((65536, 64), device="cuda").bfloat16()
+    torch.cuda.synchronize()
+    before = None
+    for rows in (1 << 16, 1 << 17, 1 << 18):   # 8 bytes per row and 128 classes
+        hidden = torch.zeros((rows, 64), device="cuda").bfloat16()
+        c.softmax_ce(hidden, weight, torch.zeros(rows, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        del hidden
+        torch.cuda.empty_cache()
+        free = torch.cuda.mem_get_info()[0]
+        if before is None:
+            before, first = free, 8 * rows * 512
+    # the last buffer holds four times the first one's bytes: 3 times more are gone, not 5 (with an eighth on top of each)
+    assert before - free < 4 * first * 1.125
+    graph.replay()
+    torch.cuda.synchronize()
+    assert same(got, want)
+    del graph
+    c.close()
