@@ -367,8 +367,10 @@ int qgbdt_softmax_ce_backward(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_h
  * h_grads, h_counts, h_types [n_tensors] are HOST arrays (read before the call returns) of device
  * pointers, element counts (0 allowed) and element types; h_out likewise: where the clipped tensors go,
  * NULL or the same pointers for in place (a tensor must not overlap another one's output).  In place
- * nothing is written when the norm is within max_norm.  A norm that is not finite is reported and the
- * tensors keep their values.  max_norm may be infinite (the norm alone) and 0. */
+ * nothing is written when the norm is within max_norm.  Where the norm is not finite because an element
+ * is not, it is reported and the tensors keep their values; a finite norm above single precision's
+ * largest number is reported as infinity, and the tensors are clipped by it.  max_norm may be infinite
+ * (the norm alone) and 0. */
 int qgbdt_clip_grad_norm(qgbdt_ctx *ctx, const void *const *h_grads, void *const *h_out, const int64_t *h_counts,
                          const int32_t *h_types, int32_t n_tensors, double max_norm, float *d_norm, void *stream);
 

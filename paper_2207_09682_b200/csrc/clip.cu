@@ -16,7 +16,9 @@
 // and writes instead of hundreds.
 //
 // Squares are added in double precision: single precision would overflow from |g| = 1.8e19 on and lose
-// everything below 1e-23, and the double-precision units have the throughput to spare here.
+// everything below 1e-23, and the double-precision units have the throughput to spare here.  The tensors are multiplied in
+// single precision, unless the factor is below its normal range (a norm above 8.5e37 times max_norm): it would lose bits
+// there, and the products are taken in double precision.
 #include "ops_internal.cuh"
 
 namespace {
@@ -25,7 +27,7 @@ constexpr int CLIP_THREADS = 256;
 constexpr int CLIP_CHUNK = 4096;
 constexpr int CLIP_BLOCKS = 6;   // of the first launch, per SM
 constexpr int CLIP_STEP = 2;     // chunks per block of the second launch
-constexpr int CLIP_SMALL = 64, CLIP_LARGE = 1000;   // tensors per launch (parameters of 1.6 or 25 KB)
+constexpr int CLIP_SMALL = 64, CLIP_LARGE = 1000;   // tensors per launch (parameters of 1.3 or 20 KB, with the outputs 1.8 or 28)
 
 template <int CAP>
 struct ClipTable {
@@ -123,8 +125,9 @@ __device__ __forceinline__ double block_sum(double s) {
 
 // What the second launch reads.
 struct ClipFactor {
-    float coef;
-    int scale;      // 0: the tensors keep their values
+    double exact;
+    float coef;     // the same in single precision
+    int scale;      // 0: the tensors keep their values; 1: times coef; 2: times exact
 };
 
 // From the sum of squares; the norm goes to *d_norm (unless NULL).
@@ -133,7 +136,8 @@ __device__ __forceinline__ ClipFactor factor_of(double s, double max_norm, float
     if (d_norm) *d_norm = (float)norm;
     // false also for a norm that is not finite: the tensors keep their values then
     const bool clip = norm > max_norm && norm <= 1.7976931348623157e308;
-    return ClipFactor{clip ? (float)(max_norm / norm) : 1.0f, clip};
+    const double exact = clip ? max_norm / norm : 1.0;
+    return ClipFactor{exact, (float)exact, !clip ? 0 : exact < 1.17549435082228751e-38 ? 2 : 1};
 }
 
 // n_before: sums of earlier launches of the same call; the last launch (`final`) adds them all.
@@ -174,10 +178,11 @@ __global__ void __launch_bounds__(CLIP_THREADS, CLIP_BLOCKS) k_norm_partial(cons
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &r, float coef) {
+template <typename T, typename F>
+__device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &r, F coef) {   // F: precision of the products
     constexpr int V = 16 / sizeof(T);
-    if ((int)threadIdx.x < r.head) o[threadIdx.x] = OpsType<T>::store(OpsType<T>::load(p[threadIdx.x]) * coef);
+    auto scaled = [coef](T x) { return OpsType<T>::store((float)((F)OpsType<T>::load(x) * coef)); };
+    if ((int)threadIdx.x < r.head) o[threadIdx.x] = scaled(p[threadIdx.x]);
     const int n = (int)(r.end - r.begin);
     const bool vec = (reinterpret_cast<uintptr_t>(o + r.begin) & 15) == 0;   // the output may be aligned differently
     const int nv = vec ? n / V : 0;
@@ -190,27 +195,33 @@ __device__ __forceinline__ void scale_chunk(const T *p, T *o, const ChunkRange &
 #pragma unroll
         for (int i = 0; i < CLIP_CHUNK / V / CLIP_THREADS; ++i) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[i].v[j] = OpsType<T>::store(OpsType<T>::load(x[i].v[j]) * coef);
+            for (int j = 0; j < V; ++j) x[i].v[j] = scaled(x[i].v[j]);
             w[threadIdx.x + i * CLIP_THREADS] = x[i];
         }
     } else {
         for (int i = threadIdx.x; i < nv; i += CLIP_THREADS) {
             OpsVec<T, V> x = q[i];
 #pragma unroll
-            for (int j = 0; j < V; ++j) x.v[j] = OpsType<T>::store(OpsType<T>::load(x.v[j]) * coef);
+            for (int j = 0; j < V; ++j) x.v[j] = scaled(x.v[j]);
             w[i] = x;
         }
         for (int i = nv * V + threadIdx.x; i < n; i += CLIP_THREADS)
-            o[r.begin + i] = OpsType<T>::store(OpsType<T>::load(p[r.begin + i]) * coef);
+            o[r.begin + i] = scaled(p[r.begin + i]);
     }
+}
+template <typename F>
+__device__ __forceinline__ void scale_any(const void *p, void *o, int type, const ChunkRange &r, F coef) {
+    if (type == QGBDT_F32) scale_chunk(reinterpret_cast<const float *>(p), reinterpret_cast<float *>(o), r, coef);
+    else if (type == QGBDT_BF16) scale_chunk(reinterpret_cast<const __nv_bfloat16 *>(p), reinterpret_cast<__nv_bfloat16 *>(o), r, coef);
+    else scale_chunk(reinterpret_cast<const __half *>(p), reinterpret_cast<__half *>(o), r, coef);
 }
 
 template <int CAP>
 __global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_constant__ ClipTable<CAP> t, const __grid_constant__ ClipOut<CAP> o,
                                                              const ClipFactor *factor, bool in_place) {
     qg_after_prior();
-    const float coef = factor->coef;
-    if (!factor->scale && in_place) return;
+    const ClipFactor f = *factor;
+    if (!f.scale && in_place) return;
     const int c0 = blockIdx.x * CLIP_STEP, c1 = min(t.chunks, c0 + CLIP_STEP);
     int i = find_tensor(t, c0);
     for (int c = c0; c < c1; ++c) {
@@ -220,9 +231,8 @@ __global__ void __launch_bounds__(CLIP_THREADS) k_clip_scale(const __grid_consta
         const void *p = t.in[i];
         void *w = o.out[i];
         const ChunkRange r = chunk_range(p, type == QGBDT_F32 ? 4 : 2, count, k);
-        if (type == QGBDT_F32) scale_chunk(reinterpret_cast<const float *>(p), reinterpret_cast<float *>(w), r, coef);
-        else if (type == QGBDT_BF16) scale_chunk(reinterpret_cast<const __nv_bfloat16 *>(p), reinterpret_cast<__nv_bfloat16 *>(w), r, coef);
-        else scale_chunk(reinterpret_cast<const __half *>(p), reinterpret_cast<__half *>(w), r, coef);
+        if (f.scale == 2) scale_any(p, w, type, r, f.exact);
+        else scale_any(p, w, type, r, f.coef);
     }
 }
 
@@ -264,9 +274,8 @@ __global__ void __cluster_dims__(CLIP_CLUSTER) __launch_bounds__(CLIP_THREADS)
         const long long count = t.count[i] & ((1ll << 56) - 1);
         const int type = (int)(t.count[i] >> 56);
         const ChunkRange r = chunk_range(t.in[i], type == QGBDT_F32 ? 4 : 2, count, c - t.first[i]);
-        if (type == QGBDT_F32) scale_chunk(reinterpret_cast<const float *>(t.in[i]), reinterpret_cast<float *>(o.out[i]), r, f.coef);
-        else if (type == QGBDT_BF16) scale_chunk(reinterpret_cast<const __nv_bfloat16 *>(t.in[i]), reinterpret_cast<__nv_bfloat16 *>(o.out[i]), r, f.coef);
-        else scale_chunk(reinterpret_cast<const __half *>(t.in[i]), reinterpret_cast<__half *>(o.out[i]), r, f.coef);
+        if (f.scale == 2) scale_any(t.in[i], o.out[i], type, r, f.exact);
+        else scale_any(t.in[i], o.out[i], type, r, f.coef);
     }
 }
 

@@ -171,3 +171,24 @@ def test_outgrown_buffers_that_no_graph_was_captured_over_are_freed():
     assert same(got, want)
     del graph
     c.close()
+
+
+# ---- clipping --------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("copies", [1, 40])
+@pytest.mark.parametrize("dtype,value", [(torch.float32, 3e38), (torch.bfloat16, 2.0 ** 127), (torch.float32, 1e36), (torch.float32, 1e30)])
+def test_clip_factors_below_single_precision(ctx, dtype, value, copies):
+    """One launch and two; norms beyond single precision, which are reported as infinity and clipped by all the same."""
+    grads = [torch.full((4096,), value, device="cuda").to(dtype)] * copies
+    x = float(grads[0][0])
+    norm, bound = math.sqrt(4096 * copies) * x, 1.5e-4
+    out = [torch.zeros_like(g) for g in grads]
+    got = float(ctx.clip_grad_norm(grads, bound, out=out))
+    assert got == math.inf if norm > 3.4028235e38 else abs(got - norm) <= 2.0 ** -23 * norm
+    want = bound * x / norm
+    # the factor in double or single precision, the product, the type: one rounding each
+    u = 2.0 ** -9 if dtype == torch.bfloat16 else 2.0 ** -24
+    assert all(bool(((o.double() - want).abs() <= (u + 2.0 ** -23) * want).all()) for o in out)
+    in_place = [grads[0].clone() for _ in range(copies)]
+    ctx.clip_grad_norm(in_place, bound)
+    assert same(in_place, out)
