@@ -62,16 +62,19 @@ _lib = None
 _tensors = None
 
 
-def _load_tensors(lib):
-    """Loads the extension module that marshals tensors, and gives it the library's functions."""
+def _load_tensors():
+    """Loads the extension module that marshals the operators' tensors, and gives it the library's functions.  Training and
+    the other calls do without it."""
     global _tensors
     path = os.path.join(_HERE, "_tensors.so")
     if not os.path.exists(path):
         raise ImportError("_tensors.so is not built: run `python -m paper_2207_09682_b200.build` (or __graft_entry__.build())")
+    lib = load_library()
     from . import _tensors as module
     module.bind(QgbdtError, *(C.cast(getattr(lib, "qgbdt_" + name), C.c_void_p).value for name in (
         "embed", "embed_backward", "softmax_ce", "softmax_ce_backward", "clip_grad_norm", "last_error")))
     _tensors = module
+    return module
 
 
 def load_library() -> C.CDLL:
@@ -84,7 +87,6 @@ def load_library() -> C.CDLL:
         lib = C.CDLL(LIB_PATH)
         lib.qgbdt_last_error.restype = C.c_char_p
         lib.qgbdt_last_error.argtypes = [C.c_void_p]
-        _load_tensors(lib)
         _lib = lib
     return _lib
 
@@ -372,14 +374,14 @@ def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, strea
     [N] or [N, bag] (int32 or int64, negative = missing); out [N, D] of the table's type is made if not given."""
     if stream is not None:
         return _elsewhere(stream, self.embed, table, tokens, scale, out, status)
-    return _tensors.embed(self.h.value or 0, self.device, table, tokens, scale, out, status)
+    return (_tensors or _load_tensors()).embed(self.h.value or 0, self.device, table, tokens, scale, out, status)
 
 
 def _embed_backward(self, grad_out, tokens, n_entries: int, scale: float = 1.0, grad_table=None, status=None, stream=None) -> torch.Tensor:
     """qgbdt_embed_backward: the table's gradient [n_entries, D] of grad_out's type, every row of it written."""
     if stream is not None:
         return _elsewhere(stream, self.embed_backward, grad_out, tokens, n_entries, scale, grad_table, status)
-    return _tensors.embed_backward(self.h.value or 0, self.device, grad_out, tokens, n_entries, scale, grad_table, status)
+    return (_tensors or _load_tensors()).embed_backward(self.h.value or 0, self.device, grad_out, tokens, n_entries, scale, grad_table, status)
 
 
 def _softmax_ce(self, hidden, weight, labels, bias=None, status=None, stream=None) -> SoftmaxCE:
@@ -387,7 +389,7 @@ def _softmax_ce(self, hidden, weight, labels, bias=None, status=None, stream=Non
     no label), mean over the labelled rows, without stored logits.  hidden, weight bfloat16 or float16, bias float32."""
     if stream is not None:
         return _elsewhere(stream, self.softmax_ce, hidden, weight, labels, bias, status)
-    return SoftmaxCE(*_tensors.softmax_ce(self.h.value or 0, self.device, hidden, weight, labels, bias, status))
+    return SoftmaxCE(*(_tensors or _load_tensors()).softmax_ce(self.h.value or 0, self.device, hidden, weight, labels, bias, status))
 
 
 def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss=None, grad_hidden=None, grad_weight=None,
@@ -396,7 +398,7 @@ def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss
     lse as softmax_ce gave it, grad_loss a float32 CUDA tensor of one element (None: 1)."""
     if stream is not None:
         return _elsewhere(stream, self.softmax_ce_backward, hidden, weight, labels, lse, bias, grad_loss, grad_hidden, grad_weight, status)
-    return _tensors.softmax_ce_backward(self.h.value or 0, self.device, hidden, weight, labels, bias, lse, grad_loss, grad_hidden, grad_weight, status)
+    return (_tensors or _load_tensors()).softmax_ce_backward(self.h.value or 0, self.device, hidden, weight, labels, bias, lse, grad_loss, grad_hidden, grad_weight, status)
 
 
 def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
@@ -404,7 +406,7 @@ def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torc
     min(1, max_norm / norm), in place or into the tensors of `out`.  float32, bfloat16 and float16 may be mixed."""
     if stream is not None:
         return _elsewhere(stream, self.clip_grad_norm, grads, max_norm, out)
-    return _tensors.clip_grad_norm(self.h.value or 0, self.device, grads, max_norm, out)
+    return (_tensors or _load_tensors()).clip_grad_norm(self.h.value or 0, self.device, grads, max_norm, out)
 
 
 Context.embed = _embed

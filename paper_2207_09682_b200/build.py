@@ -68,7 +68,12 @@ def is_stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    build_tensors(force)
+    build_library(force, verbose)
+    build_tensors(force)   # after the library, which does not need it
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
