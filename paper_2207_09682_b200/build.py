@@ -18,6 +18,7 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libqgbdt.so")
 TENSORS_SRC = os.path.join(CSRC, "tensors.cpp")
 TENSORS = os.path.join(HERE, "_tensors.so")
+TENSORS_MADE_FOR = os.path.join(OBJ_DIR, "_tensors.txt")
 
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-fmad=false",
@@ -37,7 +38,23 @@ def _obj(src: str) -> str:
     return os.path.join(OBJ_DIR, os.path.basename(src)[:-3] + ".o")
 
 
+def tensors_made_for() -> str:
+    """What the extension module's binary interface depends on, besides its source."""
+    import platform
+    import sysconfig
+
+    import torch
+    return "torch %s, C++ ABI %d, Python %s %s\n" % (torch.__version__, torch._C._GLIBCXX_USE_CXX11_ABI, platform.python_version(),
+                                                     sysconfig.get_config_var("SOABI"))
+
+
 def tensors_stale() -> bool:
+    try:
+        with open(TENSORS_MADE_FOR) as f:
+            if f.read() != tensors_made_for():
+                return True
+    except OSError:
+        return True
     newest = max(os.path.getmtime(f) for f in [TENSORS_SRC, os.path.join(ROOT, "include", "qgbdt.h"), os.path.abspath(__file__)])
     return not os.path.exists(TENSORS) or os.path.getmtime(TENSORS) < newest
 
@@ -57,6 +74,9 @@ def build_tensors(force: bool = False) -> str:
          "-isystem", os.path.join(os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"))), "include"),
          TENSORS_SRC, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp])
     os.replace(tmp, TENSORS)
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    with open(TENSORS_MADE_FOR, "w") as f:
+        f.write(tensors_made_for())
     return TENSORS
 
 

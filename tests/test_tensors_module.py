@@ -27,3 +27,21 @@ def test_the_library_loads_without_the_tensors_module(tmp_path):
             "else:\n"
             "    raise SystemExit('an operator ran without its module')\n")
     subprocess.run([sys.executable, "-c", code], cwd=tmp_path, env={**os.environ, "PYTHONPATH": str(tmp_path)}, check=True)
+
+
+def test_the_tensors_module_is_rebuilt_for_another_torch_or_python(monkeypatch):
+    import platform
+
+    import torch
+    build.build()
+    assert not build.tensors_stale()
+    with monkeypatch.context() as m:
+        m.setattr(torch, "__version__", "0.0.0")
+        assert build.tensors_stale()
+    with monkeypatch.context() as m:
+        m.setattr(platform, "python_version", lambda: "0.0.0")
+        assert build.tensors_stale()
+    with monkeypatch.context() as m:
+        m.setattr(build, "TENSORS_MADE_FOR", build.TENSORS_MADE_FOR + ".absent")
+        assert build.tensors_stale()
+    assert not build.tensors_stale()
