@@ -12,6 +12,7 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <limits>
 #include <vector>
 
 #include "qgbdt.h"
@@ -73,6 +74,12 @@ struct Call {
     bool here(const at::Tensor &t) const { return t.is_cuda() && t.get_device() == device; }
     PyObject *result(int rc) const { return rc == QGBDT_OK ? nullptr : fail(rc, lib.last_error(ctx)); }
 };
+
+// The caller's tensor has been written: its version goes up, as with torch's own in-place operations, so that autograd
+// notices where it was saved for a backward pass.
+void written(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // (those keep no version)
+}
 
 // A tensor argument; NULL and an exception if it is none.
 const at::Tensor *tensor(PyObject *o, const char *name) {
@@ -160,6 +167,7 @@ struct Output {
     }
     PyObject *give(PyObject *o) const {   // a new reference
         if (o != Py_None) {
+            written(*r.t);
             Py_INCREF(o);
             return o;
         }
@@ -279,8 +287,10 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     double max_norm;
     if (!c.take(args, nargs, 5) || !number(args[3], &max_norm)) return nullptr;
     std::vector<void *> in, out;
+    std::vector<at::Tensor> changed;   // the tensors that the call writes
     std::vector<int64_t> sizes;
     std::vector<int32_t> types;
+    const bool to_out = args[4] != Py_None, in_place = !to_out && max_norm <= std::numeric_limits<double>::max();
     auto take = [&](PyObject *list, const char *name, bool first) {
         PyObject *seq = PySequence_Fast(list, "expected a list of tensors");
         if (!seq) return false;
@@ -290,6 +300,7 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(seq, i), name);
             ok = t != nullptr;
             if (!ok) break;
+            if (first ? in_place : to_out) changed.push_back(*t);
             const int type = element(*t);
             if (!c.here(*t) || !t->is_contiguous() || type < 0) {
                 refuse(name, "must be contiguous float32, bfloat16 or float16 tensors on the context's device");
@@ -306,11 +317,13 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         Py_DECREF(seq);
         return ok;
     };
-    if (!take(args[2], "gradients", true) || (args[4] != Py_None && !take(args[4], "out", false))) return nullptr;
+    if (!take(args[2], "gradients", true) || (to_out && !take(args[4], "out", false))) return nullptr;
     const at::Tensor norm = at::empty({1}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (c10::DeviceIndex)c.device));
-    const int rc = lib.clip_grad_norm(c.ctx, in.data(), args[4] != Py_None ? out.data() : nullptr, sizes.data(), types.data(), (int32_t)in.size(), max_norm,
+    const int rc = lib.clip_grad_norm(c.ctx, in.data(), to_out ? out.data() : nullptr, sizes.data(), types.data(), (int32_t)in.size(), max_norm,
                                       norm.data_ptr<float>(), c.stream);
-    return rc == QGBDT_OK ? THPVariable_Wrap(norm) : c.result(rc);
+    if (rc != QGBDT_OK) return c.result(rc);
+    for (const at::Tensor &t : changed) written(t);
+    return THPVariable_Wrap(norm);
     END_HANDLE_TH_ERRORS
 }
 

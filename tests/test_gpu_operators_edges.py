@@ -192,3 +192,39 @@ def test_clip_factors_below_single_precision(ctx, dtype, value, copies):
     in_place = [grads[0].clone() for _ in range(copies)]
     ctx.clip_grad_norm(in_place, bound)
     assert same(in_place, out)
+
+
+# ---- autograd's bookkeeping ------------------------------------------------------------------------
+
+def test_tensors_that_a_call_writes_get_a_new_version(ctx):
+    """As with torch's own in-place operations; a tensor that was saved for a backward pass is noticed."""
+    tok = torch.zeros(3, dtype=torch.int32, device="cuda")
+    h, w, y = loss_case(20, 30, 8, 1)
+    lse = ctx.softmax_ce(h, w, y).lse
+    calls = [
+        lambda t: ctx.embed(torch.randn((8, 4), device="cuda"), tok, out=t[:3, :4]),
+        lambda t: ctx.embed_backward(torch.randn((3, 4), device="cuda"), tok, 8, grad_table=t[:8, :4]),
+        lambda t: ctx.clip_grad_norm([t], 0.5), lambda t: ctx.clip_grad_norm([torch.ones_like(t)], 0.5, out=[t]),
+        lambda t: ctx.embed(torch.randn((8, 4), device="cuda"), tok, out=t[:3, :4], stream=torch.cuda.current_stream()),
+    ]
+    for call in calls:
+        t = torch.ones((30, 8), device="cuda")
+        before = t._version
+        call(t)
+        assert t._version > before
+    gh, gw = torch.zeros_like(h), torch.zeros_like(w)
+    ctx.softmax_ce_backward(h, w, y, lse, grad_hidden=gh, grad_weight=gw)
+    assert gh._version > 0 and gw._version > 0 and h._version == 0 and w._version == 0
+    t = torch.ones(30, device="cuda")
+    ctx.clip_grad_norm([t], math.inf)                          # the norm alone
+    ctx.clip_grad_norm([t], 0.5, out=[torch.empty_like(t)])
+    assert t._version == 0
+    x, saved = torch.randn((3, 4), device="cuda", requires_grad=True), torch.randn((3, 4), device="cuda")
+    product = (x * saved).sum()
+    ctx.embed(torch.randn((8, 4), device="cuda"), tok, out=saved)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        product.backward()
+    with torch.inference_mode():
+        inside = torch.ones(30, device="cuda")
+    ctx.clip_grad_norm([inside], 0.5)
+    assert float(inside[0]) < 1.0
