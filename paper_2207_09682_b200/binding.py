@@ -355,7 +355,8 @@ class SoftmaxCE(NamedTuple):
 
 
 # The arguments of the calls below are taken apart by the extension module _tensors (csrc/tensors.cpp): tensors of the
-# context's device, matrices with contiguous rows of any row stride; anything else is refused with ERR_ARG.
+# context's device, matrices with contiguous rows of any row stride; anything else is refused with ERR_ARG.  Autograd records
+# none of them: gradients come from the *_backward calls (an input that requires one is taken with a warning).
 
 def _elsewhere(stream, call, *args):
     """A call on another stream than the current one: its outputs are made there, and the allocator is told that its

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -75,6 +76,15 @@ struct Call {
     PyObject *result(int rc) const { return rc == QGBDT_OK ? nullptr : fail(rc, lib.last_error(ctx)); }
 };
 
+// Warns where autograd would be expected to record the call; false with an exception where warnings are errors.
+bool unrecorded(const at::Tensor &t, const char *name) {
+    if (!at::GradMode::is_enabled() || !t.requires_grad()) return true;
+    char text[256];
+    snprintf(text, sizeof(text), "%s requires a gradient, but autograd does not record this call and its result has no graph; the "
+             "operators' *_backward calls give gradients (torch.no_grad() or detach() silences this)", name);
+    return PyErr_WarnEx(PyExc_UserWarning, text, 1) == 0;
+}
+
 // The caller's tensor has been written: its version goes up, as with torch's own in-place operations, so that autograd
 // notices where it was saved for a backward pass.
 void written(const at::Tensor &t) {
@@ -100,6 +110,7 @@ struct Rows {
         t = tensor(o, name);
         return t && check(c, name);
     }
+    bool take_input(const Call &c, PyObject *o, const char *name) { return take(c, o, name) && unrecorded(*t, name); }
     bool check(const Call &c, const char *name) {
         if (!c.here(*t)) return refuse(name, "must be a CUDA tensor on the context's device"), false;
         if (t->dim() != 2) return refuse(name, "must be a matrix"), false;
@@ -189,7 +200,7 @@ PyObject *py_embed(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     Output out;
     double scale;
     void *status;
-    if (!c.take(args, nargs, 7) || !table.take(c, args[2], "table") || !tok.take(c, args[3]) || !number(args[4], &scale)) return nullptr;
+    if (!c.take(args, nargs, 7) || !table.take_input(c, args[2], "table") || !tok.take(c, args[3]) || !number(args[4], &scale)) return nullptr;
     if (table.type < 0) return refuse("table must be float32, bfloat16 or float16");
     if (!out.take(c, args[5], "out", tok.n, table.d, *table.t) || !words(c, args[6], "status", at::kInt, 1, &status)) return nullptr;
     const int rc = lib.embed(c.ctx, table.p(), table.type, table.n, (int32_t)table.d, table.ld, tok.t->data_ptr(), tok.type, tok.n, (int32_t)tok.bag, tok.ld,
@@ -207,7 +218,7 @@ PyObject *py_embed_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     Output out;
     double scale;
     void *status;
-    if (!c.take(args, nargs, 8) || !grad.take(c, args[2], "grad_out") || !tok.take(c, args[3]) || !number(args[5], &scale)) return nullptr;
+    if (!c.take(args, nargs, 8) || !grad.take_input(c, args[2], "grad_out") || !tok.take(c, args[3]) || !number(args[5], &scale)) return nullptr;
     const int64_t entries = PyLong_AsLongLong(args[4]);
     if (PyErr_Occurred()) return nullptr;
     if (grad.type < 0) return refuse("grad_out must be float32, bfloat16 or float16");
@@ -226,13 +237,14 @@ struct Classifier {
     int label_type;
     void *bias, *label;
     bool take(const Call &c, PyObject *const *args) {
-        if (!hidden.take(c, args[2], "hidden") || !weight.take(c, args[3], "weight") || !(labels = tensor(args[4], "labels"))) return false;
+        if (!hidden.take_input(c, args[2], "hidden") || !weight.take_input(c, args[3], "weight") || !(labels = tensor(args[4], "labels"))) return false;
         if (hidden.type != weight.type || (hidden.type != QGBDT_BF16 && hidden.type != QGBDT_F16))
             return refuse("hidden and weight must both be bfloat16 or float16"), false;
         if (hidden.d != weight.d) return refuse("hidden and weight differ in columns"), false;
         label_type = index_type(*labels);
         if (label_type < 0 || labels->dim() != 1) return refuse("labels must be [N], int32 or int64"), false;
-        return words(c, args[4], "labels", labels->scalar_type(), hidden.n, &label) && words(c, args[5], "bias", at::kFloat, weight.n, &bias);
+        return words(c, args[4], "labels", labels->scalar_type(), hidden.n, &label) && words(c, args[5], "bias", at::kFloat, weight.n, &bias) &&
+               (args[5] == Py_None || unrecorded(THPVariable_Unpack(args[5]), "bias"));
     }
 };
 
@@ -301,6 +313,7 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             ok = t != nullptr;
             if (!ok) break;
             if (first ? in_place : to_out) changed.push_back(*t);
+            if (first && !(ok = unrecorded(*t, name))) break;
             const int type = element(*t);
             if (!c.here(*t) || !t->is_contiguous() || type < 0) {
                 refuse(name, "must be contiguous float32, bfloat16 or float16 tensors on the context's device");

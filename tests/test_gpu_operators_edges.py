@@ -2,6 +2,7 @@
 graphs over the shared work buffer, extreme norms, sizes and strides, autograd's bookkeeping.  Tolerances are derived beside
 each check; u(T) = 2^-9 (bf16), 2^-12 (f16) and 2^-24 (f32) is the relative error of one rounding to nearest."""
 import math
+import warnings
 
 import pytest
 import torch
@@ -228,3 +229,31 @@ def test_tensors_that_a_call_writes_get_a_new_version(ctx):
         inside = torch.ones(30, device="cuda")
     ctx.clip_grad_norm([inside], 0.5)
     assert float(inside[0]) < 1.0
+
+
+def test_inputs_that_require_a_gradient_are_taken_with_a_warning(ctx, recwarn):
+    tok = torch.zeros(3, dtype=torch.int32, device="cuda")
+    h, w, y = loss_case(20, 30, 8, 1)
+    r = ctx.softmax_ce(h, w, y)
+    leaf = lambda t: t.detach().clone().requires_grad_()  # noqa: E731
+    calls = [
+        ("table", lambda: ctx.embed(leaf(torch.ones((8, 4), device="cuda")), tok)),
+        ("grad_out", lambda: ctx.embed_backward(leaf(torch.ones((3, 4), device="cuda")), tok, 8)),
+        ("hidden", lambda: ctx.softmax_ce(leaf(h), w, y)), ("weight", lambda: ctx.softmax_ce(h, leaf(w), y)),
+        ("bias", lambda: ctx.softmax_ce(h, w, y, bias=leaf(torch.zeros(30, device="cuda")))),
+        ("hidden", lambda: ctx.softmax_ce_backward(leaf(h), w, y, r.lse)),
+        ("gradients", lambda: ctx.clip_grad_norm([leaf(torch.ones(4, device="cuda"))], 1.0)),
+    ]
+    for name, call in calls:
+        with pytest.warns(UserWarning, match=name + " requires a gradient, but autograd does not record"):
+            result = call()
+        first = result if isinstance(result, torch.Tensor) else result[0]
+        assert not first.requires_grad
+        with torch.no_grad():
+            call()
+    assert not recwarn.list    # neither without gradients nor under no_grad()
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        with pytest.raises(UserWarning):
+            calls[0][1]()
+    assert same(ctx.softmax_ce(h, w, y), r)
