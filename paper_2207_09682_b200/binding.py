@@ -360,14 +360,15 @@ class SoftmaxCE(NamedTuple):
 
 def _elsewhere(stream, call, *args):
     """A call on another stream than the current one: its outputs are made there, and the allocator is told that its
-    inputs are in use there, so that neither is handed out again too early."""
-    with torch.cuda.stream(stream):
-        result = call(*args)
-    for a in args:
-        for t in a if isinstance(a, (list, tuple)) else (a,):
-            if isinstance(t, torch.Tensor):
-                t.record_stream(stream)
-    return result
+    inputs are in use there, so that neither is handed out again too early (also when the call fails on its way)."""
+    try:
+        with torch.cuda.stream(stream):
+            return call(*args)
+    finally:
+        for a in args:
+            for t in a if isinstance(a, (list, tuple)) else (a,):
+                if isinstance(t, torch.Tensor) and t.is_cuda:
+                    t.record_stream(stream)
 
 
 def _embed(self, table, tokens, scale: float = 1.0, out=None, status=None, stream=None) -> torch.Tensor:
@@ -405,8 +406,8 @@ def _softmax_ce_backward(self, hidden, weight, labels, lse, bias=None, grad_loss
 def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
     """qgbdt_clip_grad_norm: the global norm (float32 tensor [1]) of a list of contiguous tensors, and every tensor times
     min(1, max_norm / norm), in place or into the tensors of `out`.  float32, bfloat16 and float16 may be mixed."""
-    if stream is not None:
-        return _elsewhere(stream, self.clip_grad_norm, grads, max_norm, out)
+    if stream is not None:   # lists, since what a generator gave would be gone when the stream is recorded
+        return _elsewhere(stream, self.clip_grad_norm, list(grads), max_norm, out if out is None else list(out))
     return (_tensors or _load_tensors()).clip_grad_norm(self.h.value or 0, self.device, grads, max_norm, out)
 
 

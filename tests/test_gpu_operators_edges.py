@@ -174,6 +174,28 @@ def test_outgrown_buffers_that_no_graph_was_captured_over_are_freed():
     c.close()
 
 
+def test_tensors_of_a_call_on_another_stream_are_recorded_there(ctx, monkeypatch):
+    """Whatever sequence they come in, and when the call is refused."""
+    from paper_2207_09682_b200 import binding
+    seen = []
+    record = torch.Tensor.record_stream
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: (seen.append(t.data_ptr()), record(t, s))[1])
+    grads, out = [[torch.ones(n, device="cuda") for n in (5, 70, 900)] for _ in range(2)]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    for of in (list, tuple, iter, lambda x: {i: t for i, t in enumerate(x)}.values(), lambda x: (t.view(-1) for t in x)):
+        seen.clear()
+        ctx.clip_grad_norm(of(grads), 2.0, out=of(out), stream=stream)
+        assert sorted(seen) == sorted(t.data_ptr() for t in grads + out)
+    torch.cuda.synchronize()
+    norm = math.sqrt(975)
+    assert all(bool(((o - 2.0 / norm).abs() <= 2.0 ** -22).all()) for o in out)
+    seen.clear()
+    with pytest.raises(binding.QgbdtError):
+        ctx.embed(grads[0].view(1, 5), torch.zeros(2, device="cuda"), stream=stream)
+    assert grads[0].data_ptr() in seen
+
+
 # ---- clipping --------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("copies", [1, 40])
