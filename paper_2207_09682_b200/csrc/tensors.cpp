@@ -115,6 +115,7 @@ struct Rows {
         if (!c.here(*t)) return refuse(name, "must be a CUDA tensor on the context's device"), false;
         if (t->dim() != 2) return refuse(name, "must be a matrix"), false;
         n = t->size(0), d = t->size(1);
+        if (d > std::numeric_limits<int32_t>::max()) return refuse(name, "has too many columns"), false;   // the calls take 32 bits
         if (d > 1 && t->stride(1) != 1) return refuse(name, "must have contiguous rows"), false;
         ld = n > 1 ? t->stride(0) : d > 0 ? d : 1;
         type = element(*t);

@@ -279,3 +279,18 @@ def test_inputs_that_require_a_gradient_are_taken_with_a_warning(ctx, recwarn):
         with pytest.raises(UserWarning):
             calls[0][1]()
     assert same(ctx.softmax_ce(h, w, y), r)
+
+
+# ---- sizes and strides -----------------------------------------------------------------------------
+
+def test_columns_beyond_32_bits_are_refused(ctx):
+    """Not taken modulo 2^32 (no memory is behind these tensors: they have no rows)."""
+    from paper_2207_09682_b200 import binding
+    table = torch.randn((8, 4), device="cuda")
+    for columns in (2 ** 32 + 1, 2 ** 31, 2 ** 33 + 4):
+        tok = torch.empty((0, columns), dtype=torch.int32, device="cuda")
+        for call in (lambda: ctx.embed(table, tok), lambda: ctx.embed_backward(table[:0], tok, 8), lambda: ctx.embed_backward(torch.empty((0, columns), device="cuda"), tok[:, :1], 8),
+                     lambda: ctx.softmax_ce(torch.empty((0, columns), device="cuda").half(), table.half(), torch.empty(0, dtype=torch.int32, device="cuda"))):
+            with pytest.raises(binding.QgbdtError) as e:
+                call()
+            assert e.value.code == binding.ERR_ARG
