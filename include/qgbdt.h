@@ -300,8 +300,9 @@ const char *qgbdt_noalloc_last_error(void);
  *  - Element types are given per call (QGBDT_F32, _BF16, _F16); sums, softmax statistics and norms are
  *    held in at least 32 bits and rounded once, when an output is written.  Equal inputs give equal
  *    bits: no result depends on the order of atomics.
- *  - ld_* are row strides in elements; any stride >= the row length and any alignment to the element is
- *    accepted (16-byte aligned rows are the fast case).
+ *  - ld_* are row strides in elements; any stride >= the row length (below 2^30 in the embedding, 2^39
+ *    in the loss; that of a single row means nothing) and any alignment to the element is accepted
+ *    (16-byte aligned rows are the fast case).
  *  - All calls are asynchronous on `stream`.  They share one work buffer of the context, which grows
  *    with the largest call (growing synchronises, unless a graph has been captured over the buffer);
  *    calls on different streams are ordered after one another by an event.  A call whose buffer is

@@ -53,7 +53,14 @@ int check_index_type(qgbdt_ctx *c, int32_t t) {
     return QGBDT_OK;
 }
 
-int check_embed(qgbdt_ctx *c, const EmbedArgs &a, bool backward) {
+// The row stride of a single row means nothing: one that suits the kernels, a multiple of `step` elements.
+void single_row(int64_t rows, int64_t width, int step, int64_t *ld) {
+    if (rows <= 1 && *ld >= width) *ld = (width + step - 1) / step * step;
+}
+
+int check_embed(qgbdt_ctx *c, EmbedArgs &a, bool backward) {
+    single_row(backward ? a.rows : a.n_entries, a.dim, 1, &a.ld);
+    single_row(backward ? a.n_entries : a.rows, a.dim, 1, &a.ld_out);
     int rc = ops_enter(c);
     if (rc != QGBDT_OK) return rc;
     if (!qg_type_ok(a.type)) return qg_fail(c, QGBDT_ERR_ARG, "element type must be QGBDT_F32, QGBDT_BF16 or QGBDT_F16");
@@ -73,7 +80,11 @@ int check_embed(qgbdt_ctx *c, const EmbedArgs &a, bool backward) {
     return QGBDT_OK;
 }
 
-int check_softmax(qgbdt_ctx *c, const SoftmaxArgs &a) {
+int check_softmax(qgbdt_ctx *c, SoftmaxArgs &a) {
+    single_row(a.rows, a.dim, 8, &a.ld_hidden);
+    single_row(a.classes, a.dim, 8, &a.ld_weight);
+    single_row(a.rows, a.dim, 8, &a.ld_d_hidden);
+    single_row(a.classes, a.dim, 8, &a.ld_d_weight);
     int rc = ops_enter(c);
     if (rc != QGBDT_OK) return rc;
     if (a.type != QGBDT_BF16 && a.type != QGBDT_F16) return qg_fail(c, QGBDT_ERR_ARG, "hidden and weight must be QGBDT_BF16 or QGBDT_F16");
@@ -82,6 +93,9 @@ int check_softmax(qgbdt_ctx *c, const SoftmaxArgs &a) {
     if (a.classes < 1 || a.classes > (1ll << 24)) return qg_fail(c, QGBDT_ERR_ARG, "classes must be in [1, 2^24]");
     if (a.dim < 1 || a.dim > (1 << 16)) return qg_fail(c, QGBDT_ERR_ARG, "dim must be in [1, 2^16]");
     if (a.ld_hidden < a.dim || a.ld_weight < a.dim) return qg_fail(c, QGBDT_ERR_ARG, "a row stride is smaller than the row");
+    const int64_t most = 1ll << 39;   // tiled copies take strides below 2^40 bytes
+    if (a.ld_hidden >= most || a.ld_weight >= most || a.ld_d_hidden >= most || a.ld_d_weight >= most)
+        return qg_fail(c, QGBDT_ERR_ARG, "row strides must be below 2^39");
     if (!a.weight || (a.rows > 0 && (!a.hidden || !a.labels))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
     if (!aligned(a.hidden, 2) || !aligned(a.weight, 2) || !aligned(a.bias, 4) || !aligned(a.labels, a.label_type == QGBDT_I64 ? 8 : 4) || !aligned(a.status, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
@@ -228,7 +242,7 @@ int qgbdt_softmax_ce_backward(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hid
     int rc = check_softmax(c, a);
     if (rc != QGBDT_OK) return rc;
     if (!d_grad_weight || (n_rows > 0 && (!d_lse || !d_grad_hidden))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
-    if ((n_rows > 0 && ld_grad_hidden < dim) || ld_grad_weight < dim) return qg_fail(c, QGBDT_ERR_ARG, "a row stride is smaller than the row");
+    if ((n_rows > 0 && a.ld_d_hidden < dim) || a.ld_d_weight < dim) return qg_fail(c, QGBDT_ERR_ARG, "a row stride is smaller than the row");
     if (!aligned(d_grad_hidden, 2) || !aligned(d_grad_weight, 2) || !aligned(d_lse, 4) || !aligned(d_grad_loss, 4) || !aligned(d_grad_bias, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
     return qg_softmax_ce_backward(c, a, (cudaStream_t)stream);

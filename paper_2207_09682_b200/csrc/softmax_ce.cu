@@ -1563,7 +1563,12 @@ int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
 
 int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
     if (a.rows == 0) {
-        QG_CUDA(c, cudaMemset2DAsync(a.d_weight, a.ld_d_weight * 2, 0, (size_t)a.dim * 2, a.classes, st));
+        if (a.ld_d_weight < 1ll << 30) {
+            QG_CUDA(c, cudaMemset2DAsync(a.d_weight, a.ld_d_weight * 2, 0, (size_t)a.dim * 2, a.classes, st));
+        } else {   // rows too far apart for one call, and so only a few
+            for (int64_t v = 0; v < a.classes; ++v)
+                QG_CUDA(c, cudaMemsetAsync(reinterpret_cast<uint16_t *>(a.d_weight) + v * a.ld_d_weight, 0, (size_t)a.dim * 2, st));
+        }
         if (a.d_bias) QG_CUDA(c, cudaMemsetAsync(a.d_bias, 0, sizeof(float) * a.classes, st));
         return QGBDT_OK;
     }

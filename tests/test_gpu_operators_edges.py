@@ -1,6 +1,7 @@
 """Operators on top of the trees at the edges of their range: small probabilities in half precision, streams and captured
 graphs over the shared work buffer, extreme norms, sizes and strides, autograd's bookkeeping.  Tolerances are derived beside
 each check; u(T) = 2^-9 (bf16), 2^-12 (f16) and 2^-24 (f32) is the relative error of one rounding to nearest."""
+import ctypes as C
 import math
 import warnings
 
@@ -294,3 +295,50 @@ def test_columns_beyond_32_bits_are_refused(ctx):
             with pytest.raises(binding.QgbdtError) as e:
                 call()
             assert e.value.code == binding.ERR_ARG
+
+
+def test_strides_of_single_rows_and_rows_far_apart(ctx):
+    """C ABI: the stride of a single row means nothing; rows of the weight's gradient more than 2^31 bytes apart; strides that
+    no copy takes are refused before anything is written."""
+    from paper_2207_09682_b200 import binding
+    p = lambda t: C.c_void_p(None if t is None else t.data_ptr())  # noqa: E731
+    i64, stream = C.c_int64, C.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+    def loss(h, ldh, w, ldw, y):
+        lse, value = torch.zeros(len(h), device="cuda"), torch.zeros(1, device="cuda")
+        rc = ctx.lib.qgbdt_softmax_ce(ctx.h, p(h), i64(ldh), p(w), i64(ldw), 2, None, p(y), 0, i64(len(h)), i64(len(w)), h.shape[1], p(value), None, p(lse), None, stream)
+        return rc, value, lse
+
+    def grads(h, ldh, w, ldw, y, lse, dh, lddh, dw, lddw):
+        return ctx.lib.qgbdt_softmax_ce_backward(ctx.h, p(h), i64(ldh), p(w), i64(ldw), 2, None, p(y), 0, i64(len(h)), i64(len(w)), w.shape[1], p(lse), None,
+                                                 p(dh), i64(lddh), p(dw), i64(lddw), None, None, stream)
+
+    far = 1 << 40
+    for rows, classes, dim in ((5, 1, 8), (1, 5, 8), (1, 1, 13), (1, 70, 13), (300, 1, 13)):
+        h = torch.randn((rows, dim), generator=gen(1), device="cuda").half()
+        w = torch.randn((classes, dim), generator=gen(2), device="cuda").half()
+        y = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        want = ctx.softmax_ce(h, w, y)
+        want_dh, want_dw, _ = ctx.softmax_ce_backward(h, w, y, want.lse)
+        ldh, ldw = far if rows == 1 else dim, far if classes == 1 else dim
+        rc, value, lse = loss(h, ldh, w, ldw, y)
+        assert rc == binding.OK and torch.equal(value, want.loss) and torch.equal(lse, want.lse)
+        dh, dw = torch.ones_like(h), torch.ones_like(w)
+        assert grads(h, ldh, w, ldw, y, lse, dh, ldh, dw, ldw) == binding.OK
+        assert torch.equal(dh, want_dh) and torch.equal(dw, want_dw)
+        none = torch.empty((0, dim), device="cuda").half()
+        assert grads(none, dim, w, ldw, y, lse, none, dim, dw, ldw) == binding.OK and not dw.any()
+    h, w, y = torch.ones((2, 8), device="cuda").half(), torch.ones((2, 8), device="cuda").half(), torch.zeros(2, dtype=torch.int32, device="cuda")
+    assert loss(h, far, w, 8, y)[0] == binding.ERR_ARG and loss(h, 8, w, far, y)[0] == binding.ERR_ARG
+    # no rows: zeros into rows 2^31 bytes apart
+    wide = torch.ones((2, 2 ** 30 + 8), dtype=torch.float16, device="cuda")
+    _, dw, _ = ctx.softmax_ce_backward(h[:0], w, y[:0], torch.empty(0, device="cuda"), grad_weight=wide[:, :8])
+    assert not dw.any() and bool((wide[:, 8:16] == 1).all())
+    # the embedding's table, output and gradients of one row
+    table, tok, out = torch.randn((1, 7), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros((1, 7), device="cuda")
+    one = C.c_float(1.0)
+    assert ctx.lib.qgbdt_embed(ctx.h, p(table), 0, i64(1), 7, i64(far), p(tok), 0, i64(1), 1, i64(far), one, p(out), i64(far), None, stream) == binding.OK
+    assert torch.equal(out, table)
+    out.zero_()
+    assert ctx.lib.qgbdt_embed_backward(ctx.h, p(table), 0, i64(far), p(tok), 0, i64(1), 1, i64(far), one, p(out), i64(1), 7, i64(far), None, stream) == binding.OK
+    assert torch.equal(out, table)
