@@ -102,6 +102,15 @@ int check_softmax(qgbdt_ctx *c, SoftmaxArgs &a) {
     return QGBDT_OK;
 }
 
+// End of a call: one that failed on its way may have launched kernels, which the next call has to wait for all the same.
+int ops_leave(qgbdt_ctx *c, int rc, void *stream) {
+    if (c->ops_ws_open) {
+        const int closed = qg_ws_close(c, (cudaStream_t)stream);
+        if (rc == QGBDT_OK) rc = closed;
+    }
+    return rc;
+}
+
 // The last call of a capture, or NULL.
 qgbdt_ctx::OpsCapture *last_of_capture(qgbdt_ctx *c, unsigned long long id) {
     for (qgbdt_ctx::OpsCapture &e : c->ops_captures)
@@ -152,12 +161,14 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
         QG_CUDA(c, cudaStreamGetId(st, &id));
         if (id != c->ops_ws_stream) QG_CUDA(c, cudaStreamWaitEvent(st, c->ops_ws_event, 0));
     }
+    c->ops_ws_open = true;
     ws->at = reinterpret_cast<char *>(c->ops_ws);
     ws->end = ws->at + c->ops_ws_bytes;
     return QGBDT_OK;
 }
 
 int qg_ws_close(qgbdt_ctx *c, cudaStream_t st) {
+    c->ops_ws_open = false;
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
     unsigned long long capture = 0;
     QG_CUDA(c, cudaStreamGetCaptureInfo(st, &cap, &capture));
@@ -203,7 +214,7 @@ int qgbdt_embed(qgbdt_ctx *c, const void *d_table, int32_t type, int64_t n_entri
     EmbedArgs a{d_table, ld_table, n_entries, dim, type, d_tokens, token_type, n_rows, ld_tokens, bag, scale, d_out, ld_out, d_status};
     int rc = check_embed(c, a, false);
     if (rc != QGBDT_OK || n_rows == 0) return rc;
-    return qg_embed(c, a, (cudaStream_t)stream);
+    return ops_leave(c, qg_embed(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_embed_backward(qgbdt_ctx *c, const void *d_grad, int32_t type, int64_t ld_grad, const void *d_tokens, int32_t token_type,
@@ -212,7 +223,7 @@ int qgbdt_embed_backward(qgbdt_ctx *c, const void *d_grad, int32_t type, int64_t
     EmbedArgs a{d_grad, ld_grad, n_entries, dim, type, d_tokens, token_type, n_rows, ld_tokens, bag, scale, d_grad_table, ld_grad_table, d_status};
     int rc = check_embed(c, a, true);
     if (rc != QGBDT_OK) return rc;
-    return qg_embed_backward(c, a, (cudaStream_t)stream);
+    return ops_leave(c, qg_embed_backward(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_softmax_ce(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hidden, const void *d_weight, int64_t ld_weight, int32_t type,
@@ -226,7 +237,7 @@ int qgbdt_softmax_ce(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hidden, cons
     if (rc != QGBDT_OK) return rc;
     if (!d_loss || (n_rows > 0 && !d_lse)) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
     if (!aligned(d_loss, 4) || !aligned(d_losses, 4) || !aligned(d_lse, 4)) return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
-    return qg_softmax_ce(c, a, (cudaStream_t)stream);
+    return ops_leave(c, qg_softmax_ce(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_softmax_ce_backward(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hidden, const void *d_weight, int64_t ld_weight,
@@ -245,7 +256,7 @@ int qgbdt_softmax_ce_backward(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hid
     if ((n_rows > 0 && a.ld_d_hidden < dim) || a.ld_d_weight < dim) return qg_fail(c, QGBDT_ERR_ARG, "a row stride is smaller than the row");
     if (!aligned(d_grad_hidden, 2) || !aligned(d_grad_weight, 2) || !aligned(d_lse, 4) || !aligned(d_grad_loss, 4) || !aligned(d_grad_bias, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
-    return qg_softmax_ce_backward(c, a, (cudaStream_t)stream);
+    return ops_leave(c, qg_softmax_ce_backward(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_clip_grad_norm(qgbdt_ctx *c, const void *const *h_grads, void *const *h_out, const int64_t *h_counts, const int32_t *h_types,
@@ -264,8 +275,8 @@ int qgbdt_clip_grad_norm(qgbdt_ctx *c, const void *const *h_grads, void *const *
         const int w = qg_type_size(h_types[i]);
         if (!aligned(h_grads[i], w) || (h_out && !aligned(h_out[i], w))) return qg_fail(c, QGBDT_ERR_ARG, "tensor %d is not aligned to its element", i);
     }
-    return qg_clip_grad_norm(c, h_grads, h_out ? h_out : const_cast<void *const *>(reinterpret_cast<const void *const *>(h_grads)), h_counts,
-                             h_types, n_tensors, max_norm, d_norm, (cudaStream_t)stream);
+    void *const *out = h_out ? h_out : const_cast<void *const *>(reinterpret_cast<const void *const *>(h_grads));
+    return ops_leave(c, qg_clip_grad_norm(c, h_grads, out, h_counts, h_types, n_tensors, max_norm, d_norm, (cudaStream_t)stream), stream);
 }
 
 }  // extern "C"

@@ -77,7 +77,7 @@ int qg_launch(qgbdt_ctx *c, void (*kernel)(P...), dim3 grid, unsigned threads, s
 
 // A call's work memory: the context's one buffer, cut up from the front.  qg_ws_open makes the buffer
 // at least `bytes` large and orders `st` after the last call that used it on another stream;
-// qg_ws_close marks the end of this call's use.
+// qg_ws_close marks the end of this call's use (the C entries do that for calls that return an error in between).
 struct QgWorkspace {
     char *at = nullptr, *end = nullptr;
     template <typename T>

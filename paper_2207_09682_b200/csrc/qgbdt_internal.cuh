@@ -282,6 +282,7 @@ struct qgbdt_ctx {
     cudaEvent_t ops_ws_event = nullptr;         // end of the last call's use
     unsigned long long ops_ws_stream = 0;       // id of that call's stream
     bool ops_ws_used = false, ops_ws_captured = false;
+    bool ops_ws_open = false;                   // a call has opened it and not closed it yet
     struct OpsCapture {                         // the last call inside a stream capture
         unsigned long long id;                  // of the capture
         cudaStream_t stream;

@@ -88,6 +88,12 @@ int main(int argc, char **argv) {
         for (const std::string &s : calls) CHECK(s.compare(0, 4, "wait") != 0 || s.compare(0, 6, "wait 3") == 0);
         for (cudaEvent_t e = (cudaEvent_t)100; (long)(intptr_t)e < next_handle; e = (cudaEvent_t)((intptr_t)e + 1))
             CHECK(!(noted("wait", C, e) && (noted("record", e, A) || noted("record", e, B))) || e == c.ops_ws_event);
+    } else if (scenario == "failure") {   // what a call that failed on its way has launched is waited for
+        embed_result = QGBDT_ERR_CUDA;
+        CHECK(embed(B) == QGBDT_ERR_CUDA);
+        CHECK(noted("record", c.ops_ws_event, B));
+        embed_result = QGBDT_OK;
+        CHECK(embed(A) == QGBDT_OK && noted("wait", A, c.ops_ws_event));
     } else {
         CHECK(!"a scenario of this name");
     }

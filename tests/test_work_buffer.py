@@ -21,3 +21,9 @@ def program(tmp_path_factory):
 def test_work_buffer(program, scenario):
     run = subprocess.run([program, scenario], capture_output=True, text=True)
     assert run.returncode == 0, run.stdout
+
+
+@pytest.mark.parametrize("scenario", ["failure"])
+def test_work_buffer_failures(program, scenario):
+    run = subprocess.run([program, scenario], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout + run.stderr
