@@ -1,5 +1,6 @@
 // C ABI of the operators on top of the trees: argument checks and the context's work buffer.
 #include <cmath>
+#include <new>
 
 #include "ops_internal.cuh"
 
@@ -134,7 +135,11 @@ int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
             if (c->ops_ws_captured) {
                 // a graph may hold its address; nothing is waited for, and a call that still runs shares the counters with
                 // this one, so that the event goes on to order them
-                c->ops_ws_old.push_back(c->ops_ws);
+                try {
+                    c->ops_ws_old.push_back(c->ops_ws);
+                } catch (const std::bad_alloc &) {
+                    return qg_fail(c, QGBDT_ERR_ALLOC, "no host memory to keep track of the work buffers");
+                }
                 c->ops_ws_captured = false;   // over the buffer that takes its place
             } else {
                 if (c->ops_ws_used) QG_CUDA(c, cudaEventSynchronize(c->ops_ws_event));

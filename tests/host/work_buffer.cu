@@ -94,6 +94,14 @@ int main(int argc, char **argv) {
         CHECK(noted("record", c.ops_ws_event, B));
         embed_result = QGBDT_OK;
         CHECK(embed(A) == QGBDT_OK && noted("wait", A, c.ops_ws_event));
+    } else if (scenario == "no host memory") {   // an error code, not an exception through the C entry
+        capture_one(SMALL);
+        no_memory = true;
+        QgWorkspace ws;
+        const int rc = qg_ws_open(&c, LARGE, A, &ws);
+        no_memory = false;
+        CHECK(rc == QGBDT_ERR_ALLOC);
+        CHECK(use(SMALL, A) == first);
     } else {
         CHECK(!"a scenario of this name");
     }

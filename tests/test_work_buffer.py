@@ -23,7 +23,7 @@ def test_work_buffer(program, scenario):
     assert run.returncode == 0, run.stdout
 
 
-@pytest.mark.parametrize("scenario", ["failure"])
+@pytest.mark.parametrize("scenario", ["failure", "no host memory"])
 def test_work_buffer_failures(program, scenario):
     run = subprocess.run([program, scenario], capture_output=True, text=True)
     assert run.returncode == 0, run.stdout + run.stderr
