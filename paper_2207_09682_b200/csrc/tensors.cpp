@@ -12,6 +12,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
 
 #include <limits>
 #include <vector>
@@ -97,7 +98,12 @@ const at::Tensor *tensor(PyObject *o, const char *name) {
         refuse(name, "must be a tensor");
         return nullptr;
     }
-    return &THPVariable_Unpack(o);
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (t.layout() != at::kStrided || t.is_neg()) {   // the memory has to hold the values themselves
+        refuse(name, "must be a dense tensor without a pending negation");
+        return nullptr;
+    }
+    return &t;
 }
 
 // A matrix on the context's device whose rows are contiguous (any row stride).
@@ -305,7 +311,8 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     std::vector<int32_t> types;
     const bool to_out = args[4] != Py_None, in_place = !to_out && max_norm <= std::numeric_limits<double>::max();
     auto take = [&](PyObject *list, const char *name, bool first) {
-        PyObject *seq = PySequence_Fast(list, "expected a list of tensors");
+        THPObjectPtr held(PySequence_Fast(list, "expected a list of tensors"));
+        PyObject *const seq = held.get();
         if (!seq) return false;
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
         bool ok = first || n == (Py_ssize_t)in.size() || (refuse("out must match the gradients in number"), false);
@@ -328,7 +335,6 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 out.push_back(t->data_ptr());
             }
         }
-        Py_DECREF(seq);
         return ok;
     };
     if (!take(args[2], "gradients", true) || (to_out && !take(args[4], "out", false))) return nullptr;

@@ -342,3 +342,18 @@ def test_strides_of_single_rows_and_rows_far_apart(ctx):
     out.zero_()
     assert ctx.lib.qgbdt_embed_backward(ctx.h, p(table), 0, i64(far), p(tok), 0, i64(1), 1, i64(far), one, p(out), i64(1), 7, i64(far), None, stream) == binding.OK
     assert torch.equal(out, table)
+
+
+def test_tensors_whose_memory_does_not_hold_their_values_are_refused(ctx):
+    """Sparse ones (as the gradients of embeddings may be) and those with a pending negation."""
+    from paper_2207_09682_b200 import binding
+    table, tok = torch.randn((8, 4), device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    negative = torch._neg_view(table)
+    for bad in (table.to_sparse(), table.to_sparse_csr(), negative):
+        for call in (lambda: ctx.clip_grad_norm([table, bad], 1.0), lambda: ctx.embed(bad, tok), lambda: ctx.embed_backward(bad[:3] if bad is negative else bad, tok, 8),
+                     lambda: ctx.embed(table, tok, out=bad)):
+            with pytest.raises(binding.QgbdtError) as e:
+                call()
+            assert e.value.code == binding.ERR_ARG
+    want = math.sqrt(float(table.double().square().sum()))
+    assert abs(float(ctx.clip_grad_norm([negative.resolve_neg()], math.inf)) - want) <= 2.0 ** -22 * want
