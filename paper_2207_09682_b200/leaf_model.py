@@ -84,10 +84,11 @@ class LeafClassifier:
         """One step of gradient descent on a batch.  A norm that is not finite (an overflow of float16) leaves the
         parameters as they are."""
         r, grads = self.gradients(tokens, labels)
+        grads = [g.float() for g in grads]   # clipped as the parameters are kept: `dtype` has rounded them once, that is enough
         norm = self.ctx.clip_grad_norm(grads, max_norm * self.loss_scale)
-        rate = torch.where(torch.isfinite(norm), lr / self.loss_scale, 0.0)
+        finite = torch.isfinite(norm)
         for p, g in zip((self.table, self.weight, self.bias), grads):
-            p.sub_(torch.where(rate > 0, g.float() * rate, 0.0))
+            p.sub_(torch.where(finite, g * (lr / self.loss_scale), 0.0))
         self._copies()
         return Step(r.loss, norm / self.loss_scale)
 

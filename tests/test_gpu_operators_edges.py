@@ -357,3 +357,22 @@ def test_tensors_whose_memory_does_not_hold_their_values_are_refused(ctx):
             assert e.value.code == binding.ERR_ARG
     want = math.sqrt(float(table.double().square().sum()))
     assert abs(float(ctx.clip_grad_norm([negative.resolve_neg()], math.inf)) - want) <= 2.0 ** -22 * want
+
+
+# ---- the classifier over leaves --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,scale", [(torch.bfloat16, 1.0), (torch.float16, 256.0)])
+def test_a_step_rounds_the_gradients_to_16_bits_once(ctx, dtype, scale):
+    """What gradients() gives is clipped and applied in single precision."""
+    from paper_2207_09682_b200.leaf_model import LeafClassifier
+    net = LeafClassifier(ctx, 6, 9, 70, 20, dtype=dtype, loss_scale=scale, seed=2)
+    tokens = torch.randint(0, 9, (300, 6), generator=gen(5), device="cuda") + 9 * torch.arange(6, device="cuda")
+    labels = torch.randint(0, 70, (300,), generator=gen(6), device="cuda")
+    _, grads = net.gradients(tokens, labels)
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in grads)) / scale
+    before = [p.double().clone() for p in (net.table, net.weight, net.bias)]
+    net.step(tokens, labels, lr=0.5, max_norm=0.3 * norm)
+    for p, q, g in zip((net.table, net.weight, net.bias), before, grads):
+        moved = 0.5 * 0.3 * g.double() / scale
+        # the factor, its product and the rate's: 2^-24 each, the norm 2^-24; the parameter itself 2^-24
+        assert bool(((p.double() - (q - moved)).abs() <= 2.0 ** -24 * (q.abs() + moved.abs()) + 2.0 ** -21 * moved.abs()).all())
