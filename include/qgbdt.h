@@ -310,6 +310,9 @@ const char *qgbdt_noalloc_last_error(void);
  *    ordered after one another in the graph (up to four captures may be under way side by side).
  *    Replays of a graph are not ordered against other calls or graphs, order them yourself, and end
  *    before the context does.
+ *  - The waits inside a kernel end after two seconds; a call whose kernel gave up has no valid results.
+ *    It has returned by then, so that the next of these calls on the context says so: it does nothing
+ *    but return QGBDT_ERR_CUDA.
  *  - d_status: optional device word that the caller clears; set to 1 when a token was >= n_entries or a
  *    label >= n_classes (such tokens count as missing, such rows as rows without a label). */
 #define QGBDT_F32 0
@@ -319,7 +322,9 @@ const char *qgbdt_noalloc_last_error(void);
 #define QGBDT_I64 1
 
 /* Embedding bag: d_out[i] = scale * sum over k < bag of d_table[d_tokens[i][k]], i < n_rows, in
- * ascending k; a negative token is a missing one (a row of missing tokens gives zeros).  bag = 1 is the
+ * ascending k, or, where a call has too few rows to occupy the GPU, in up to 256 parts of the bag that
+ * are in ascending k and added one after the other (so that the rounding of a row's sum may differ with
+ * the number of rows); a negative token is a missing one (a row of missing tokens gives zeros).  bag = 1 is the
  * plain scaled lookup.  d_table [n_entries][ld_table] and d_out [n_rows][ld_out] of `type`, d_tokens
  * [n_rows][ld_tokens] of `token_type`.  d_out must not overlap d_table.  rows * bag < 2^31.  A table
  * whose rows do not start on 16 bytes and are read often is copied into the work buffer (1 GiB at
@@ -352,10 +357,11 @@ int qgbdt_softmax_ce(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_hidden, co
  * with lse as the forward call gave it: g[i][v] = (exp(z[i][v] - lse[i]) - [v == label i]) * grad_loss /
  * (rows with a label), d_grad_hidden = g d_weight, d_grad_weight = g^T d_hidden, d_grad_bias = column
  * sums of g (or NULL).  d_grad_hidden and d_grad_weight have the inputs' type; rows without a label get
- * zeros.  The logits are recomputed in pieces of the classes; g / grad_loss * (rows with a label) of a
- * piece is rounded to the inputs' type for the two products (half precision: as 2^15 times itself, so
- * that small probabilities keep their bits) and held in the work buffer (at most 384 MiB of it, or one
- * piece of 256 classes); d_grad_bias is summed before that rounding. */
+ * zeros.  The logits are recomputed in pieces of the classes; a piece's exp(z - lse) - [v == label]
+ * are rounded to the inputs' type for the two products (half precision: as 2^15 times themselves, so
+ * that small probabilities keep their bits; |exp(z - lse) - [...]| has to stay below 1.99, as it does
+ * with the forward call's lse) and held in the work buffer (at most 384 MiB of it, or one piece of 256
+ * classes); d_grad_bias is summed before that rounding. */
 int qgbdt_softmax_ce_backward(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_hidden, const void *d_weight,
                               int64_t ld_weight, int32_t type, const float *d_bias, const void *d_labels,
                               int32_t label_type, int64_t n_rows, int64_t n_classes, int32_t dim, const float *d_lse,

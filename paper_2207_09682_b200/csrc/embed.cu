@@ -304,8 +304,9 @@ __global__ void __launch_bounds__(EMB_THREADS) k_sort_small(const SortArgs a, co
 // Many pairs: least significant digit first, up to 9 bits a pass; a pass is a count per block and digit, a
 // scan, and a stable scatter.  A block scatters tiles of 2048 pairs: every warp ranks its pairs among its own (each
 // lane sets its bit in a word per digit, and reads who else did), the tile is put in order in shared memory, and runs of
-// equal digits leave it as neighbouring words.  6.55 M pairs of 15 + 16 bits: 38 us per scatter, bound by instruction
-// issue and conflicts in shared memory (digits compared with a ballot per bit: 51 us); counts 11 to 14 us.
+// equal digits leave it as neighbouring words.  6.55 M pairs of 15 + 16 bits: 38 us per scatter, bound by shared
+// memory: its data pipe is busy 55 % of the time (l1tex as a whole 81 % of its active cycles), warps wait for it most, a
+// third of the issue slots is used (digits compared with a ballot per bit: 51 us); counts 11 to 15 us.
 constexpr int SORT_MIN_BITS = 6, SORT_MAX_BITS = 9;
 constexpr int SORT_WARPS = EMB_THREADS / 32;
 constexpr int SORT_ROUNDS = 8;                                    // pairs per lane and tile
@@ -597,7 +598,7 @@ __device__ void clear_rows(const SegArgs &a, long long block) {
 
 // Blocks of the sums per SM, by the bytes of a vector: what the registers of eight rows in flight allow.  Narrow vectors move
 // less per load: 600000 pairs of 200 bytes in vectors of 8, the whole gradient: 53 us with three blocks, 50 with four (five
-// spill, 63).
+// spill more, 63).  The widest vectors spill a few bytes (4 to 8 stored) at these settings too.
 constexpr int sum_blocks_per_sm(int vector) { return vector == 16 ? 3 : 4; }
 
 // OUT_VEC: the output's rows take whole vectors (tested at run time it costs registers: 395 and 441 us).

@@ -4,9 +4,11 @@
 //   g_iv = exp(z_iv - lse_i) - [v == label i],   dH = s g W,   dW = s g^T H,   db = s sum_i g_i
 //
 // with s = grad_loss / (rows with a label).  Four matrix products on the tensor cores: z once for the loss,
-// z again for the gradients (cheaper than 2 bytes per logit out of and into DRAM at these widths, and no
-// memory that grows with rows * classes), and the two products with g.  8 * rows * classes * dim operations
-// in all; a step that kept the logits would need 6.
+// z again for the gradients, and the two products with g.  8 * rows * classes * dim operations in all; a step that
+// kept the logits would need 6.  Keeping them would cost 4 bytes per logit out of and into DRAM (z has more bits than
+// the inputs' type: half that would round it), which at dim 1024 takes as long as working them out again (0.65 ms for
+// 537 million), at smaller dim longer, and memory for all of them (2 GB there); what is kept instead is a maximum and
+// a sum per row and 128 classes, 8 bytes.
 //
 // One kernel carries all four: a persistent grid whose pairs of CTAs take tiles of 256 rows by 256 columns.  One
 // warp fills a ring of operand tiles with tiled copies, one thread issues the matrix instructions, eight warps
@@ -23,16 +25,17 @@
 //   DH    the piece's contribution to dH, in single precision.
 //   DW    rows of dW, complete with every piece, written in the output type.
 //
-// Measured (7373 labelled rows x 65536 classes x 1024, bf16): LOSS 625 us, 1.58 PFLOP/s, the tensor cores 87 %
-// busy, bound by them and by power (1000 W: in a loop 1.25-1.3 PFLOP/s, what library products of these shapes
-// reach); GRAD 0.64 ms (77 %: its epilogue writes 1 GB of g), DH 0.60 ms, DW 0.56 ms (84-89 %, bound by what L2
-// delivers, about 12 TB/s); all of the gradient, launches and joins included, 2.5 ms.  With dim below about 400
-// the epilogues bound LOSS and GRAD: 16 exponentials per clock and SM (dim 64: 537 million logits in 222 us,
-// 120 us for the exponentials alone).
+// Measured (7373 labelled rows x 65536 classes x 1024, bf16, single launches from cold caches): LOSS 671 us, 1.48
+// PFLOP/s; GRAD 0.70 ms (its epilogue writes 1 GB of g), DH 0.67 ms, DW 0.64 ms; the whole step in a stream 3.15 ms.
+// The tensor cores are busy 75 to 83 % of a launch's time; they and power bound LOSS (1000 W: in a loop 1.25-1.3 PFLOP/s,
+// what library products of these shapes reach), what L2 delivers (about 12 TB/s) DH and DW.  With dim below about 400 the
+// epilogues bound LOSS and GRAD (dim 64: 537 million logits in 222 us, of which 120 us are what the exponentials alone
+// need at 16 per clock and SM; the rest is the latency of an epilogue's steps).
 //
-// Rows without a label are taken out first: the labelled rows are packed to the front of a copy of H (which
-// also gives the copies their alignment).  Nothing is computed for the others, and what they hold, infinities
-// included, never meets a product.
+// Rows without a label are taken out first, but for the loss at small sizes (DIRECT_PRODUCTS): the labelled rows are
+// packed to the front of a copy of H (which also gives the copies their alignment), and nothing is computed for the
+// others.  Where the rows are taken as they are, a row's products meet its own statistics alone, and nobody reads those of
+// a row without a label: what it holds, infinities included, reaches no result either way.
 #include <math.h>
 
 #include <type_traits>
@@ -1515,7 +1518,9 @@ static int loss_few(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
 }
 
 // Up to here (rows * classes * dim) all rows go through the products, labelled or not: packing takes two launches and a copy
-// of H, more than the products it could save.  20000 rows x 1000 classes x 256, all labelled: 36 us packed, 29 us not; none labelled, the worst case: 13 and 19 us.
+// of H, more than the products it could save.  20000 rows x 1000 classes x 256, all labelled: 36 us packed, 29 us not; none
+// labelled, the worst case: 13 and 19 us.  The rule counts products; with dim below about 400 a tile takes as long as its
+// epilogue, whatever dim is, so that many classes of small dim with few labelled rows would be better off packed.
 constexpr double DIRECT_PRODUCTS = 1e10;
 
 int qg_softmax_ce(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st) {
