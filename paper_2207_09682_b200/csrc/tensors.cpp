@@ -306,22 +306,22 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     double max_norm;
     if (!c.take(args, nargs, 5) || !number(args[3], &max_norm)) return nullptr;
     std::vector<void *> in, out;
-    std::vector<at::Tensor> changed;   // the tensors that the call writes
     std::vector<int64_t> sizes;
     std::vector<int32_t> types;
     const bool to_out = args[4] != Py_None, in_place = !to_out && max_norm <= std::numeric_limits<double>::max();
+    THPObjectPtr held[2];   // the tensors stay alive until the call has been made
     auto take = [&](PyObject *list, const char *name, bool first) {
-        THPObjectPtr held(PySequence_Fast(list, "expected a list of tensors"));
-        PyObject *const seq = held.get();
+        PyObject *const seq = PySequence_Fast(list, "expected a list of tensors");
         if (!seq) return false;
+        held[!first] = THPObjectPtr(seq);
+        const at::Tensor *recorded = nullptr;
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
         bool ok = first || n == (Py_ssize_t)in.size() || (refuse("out must match the gradients in number"), false);
         for (Py_ssize_t i = 0; ok && i < n; ++i) {
             const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(seq, i), name);
             ok = t != nullptr;
             if (!ok) break;
-            if (first ? in_place : to_out) changed.push_back(*t);
-            if (first && !(ok = unrecorded(*t, name))) break;
+            if (first && t->requires_grad()) recorded = t;
             const int type = element(*t);
             if (!c.here(*t) || !t->is_contiguous() || type < 0) {
                 refuse(name, "must be contiguous float32, bfloat16 or float16 tensors on the context's device");
@@ -335,14 +335,20 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 out.push_back(t->data_ptr());
             }
         }
-        return ok;
+        return ok && (!recorded || unrecorded(*recorded, name));
     };
     if (!take(args[2], "gradients", true) || (to_out && !take(args[4], "out", false))) return nullptr;
     const at::Tensor norm = at::empty({1}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (c10::DeviceIndex)c.device));
     const int rc = lib.clip_grad_norm(c.ctx, in.data(), to_out ? out.data() : nullptr, sizes.data(), types.data(), (int32_t)in.size(), max_norm,
                                       norm.data_ptr<float>(), c.stream);
     if (rc != QGBDT_OK) return c.result(rc);
-    for (const at::Tensor &t : changed) written(t);
+    if (in_place || to_out) {
+        PyObject *const seq = held[to_out].get();
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(seq); ++i) {
+            PyObject *const o = PySequence_Fast_GET_ITEM(seq, i);
+            if (THPVariable_Check(o)) written(THPVariable_Unpack(o));   // (a warning's handler may have changed the list)
+        }
+    }
     return THPVariable_Wrap(norm);
     END_HANDLE_TH_ERRORS
 }
