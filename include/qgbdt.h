@@ -294,14 +294,14 @@ const char *qgbdt_noalloc_last_error(void);
  * The leaf a row reaches in every tree of a trained model is a list of categorical tokens (leaf l of
  * tree k is entry k * num_leaves + l of a table).  The calls below are the training step of a softmax
  * classifier over such tokens, for class counts far beyond what one tree per class allows: the sum of
- * the leaves' embeddings, the softmax cross entropy over the classes, both with their gradients, and
- * the clipping of the gradients by their global norm.  None needs a loaded bin matrix or reads the
- * training parameters.  (The paper has no counterpart.)
+ * the leaves' embeddings, layer norm, the softmax cross entropy over the classes, all with their
+ * gradients, the clipping of the gradients by their global norm, and an AdamW step.  None needs a loaded
+ * bin matrix or reads the training parameters.  (The paper has no counterpart.)
  *  - Element types are given per call (QGBDT_F32, _BF16, _F16); sums, softmax statistics and norms are
  *    held in at least 32 bits and rounded once, when an output is written.  Equal inputs give equal
  *    bits: no result depends on the order of atomics.
  *  - ld_* are row strides in elements; any stride >= the row length (below 2^30 in the embedding, 2^39
- *    in the loss; that of a single row means nothing) and any alignment to the element is accepted
+ *    in the loss and the layer norm; that of a single row means nothing) and any alignment to the element is accepted
  *    (16-byte aligned rows are the fast case).
  *  - All calls are asynchronous on `stream`.  They share one work buffer of the context, which grows
  *    with the largest call (growing synchronises, unless a graph has been captured over the buffer);
@@ -380,6 +380,80 @@ int qgbdt_softmax_ce_backward(qgbdt_ctx *ctx, const void *d_hidden, int64_t ld_h
  * (the norm alone) and 0. */
 int qgbdt_clip_grad_norm(qgbdt_ctx *ctx, const void *const *h_grads, void *const *h_out, const int64_t *h_counts,
                          const int32_t *h_types, int32_t n_tensors, double max_norm, float *d_norm, void *stream);
+
+/* Layer norm of every row: mean = sum x / dim, var = sum (x - mean)^2 / dim, rstd = 1 / sqrt(var + eps),
+ * d_out = (x - mean) * rstd * d_weight + d_bias.  d_x [n_rows][dim] and d_out of `type`; d_weight and
+ * d_bias [dim], both of `weight_type` (QGBDT_F32, or `type`), each may be NULL (1 and 0); d_mean and
+ * d_rstd [n_rows] in single precision, each may be NULL.  eps >= 0; where var + eps is 0 (equal values
+ * and no eps) rstd is infinite and the row NaN, as the formula has it.  The order of a row's sums goes by
+ * dim and by the vectors that addresses and strides allow.  d_out may be d_x itself with the
+ * same stride; it must not overlap d_x otherwise.  dim in [1, 2^20]. */
+int qgbdt_layer_norm(qgbdt_ctx *ctx, const void *d_x, int64_t ld_x, int32_t type, const void *d_weight, const void *d_bias,
+                     int32_t weight_type, int64_t n_rows, int32_t dim, double eps, void *d_out, int64_t ld_out,
+                     float *d_mean, float *d_rstd, void *stream);
+/* Its gradients, with mean and rstd as the forward call gave them: xh = (x - mean) * rstd,
+ * d_grad_x = rstd * (w g - mean of w g - xh * mean of w g xh) with the means over the row,
+ * d_grad_weight = sum over the rows of g xh, d_grad_bias = sum over the rows of g, for g = d_grad and
+ * w = d_weight (NULL: 1).  d_grad, d_x and d_grad_x [n_rows][dim] of `type`; d_weight, d_grad_weight and
+ * d_grad_bias [dim] of `weight_type`; the latter two may be NULL, and are zeros without rows.  The sums
+ * over the rows are taken in parts whose number goes by the sizes and the GPU, and joined in their order.
+ * d_grad_x may be d_grad or d_x itself with the same stride; it must not overlap them otherwise. */
+int qgbdt_layer_norm_backward(qgbdt_ctx *ctx, const void *d_grad, int64_t ld_grad, const void *d_x, int64_t ld_x, int32_t type,
+                              const float *d_mean, const float *d_rstd, const void *d_weight, int32_t weight_type,
+                              int64_t n_rows, int32_t dim, void *d_grad_x, int64_t ld_grad_x, void *d_grad_weight,
+                              void *d_grad_bias, void *stream);
+
+/* One AdamW step over many tensors:
+ *   g = grad * min(1, max_norm * loss_scale / norm) / loss_scale
+ *   exp_avg    = beta1 * exp_avg + (1 - beta1) * g
+ *   exp_avg_sq = beta2 * exp_avg_sq + (1 - beta2) * g^2
+ *   param = param * (1 - lr * weight_decay)
+ *           - lr / (1 - beta1^step) * exp_avg / (sqrt(exp_avg_sq / (1 - beta2^step)) + eps)
+ *   copy  = param, rounded to the copy's type
+ * in single precision (the factors that are the same for all elements in double).  The first step is 1.
+ * d_norm: the gradients' norm as qgbdt_clip_grad_norm reports it for these gradients (NULL: no clipping);
+ * where it is not finite nothing at all is written.  loss_scale: what the loss was multiplied with.
+ * d_lr, d_step: one number in device memory in place of lr or step (NULL: those), for a captured call.
+ * Tensors are contiguous; count may be 0.  A tensor of parameters may be listed once only; exp_avg,
+ * exp_avg_sq, exponents and copy are written and must not overlap anything else.  No work buffer is used.
+ *
+ * state_bits 32: exp_avg and exp_avg_sq [count] are floats.
+ * state_bits 8: they are bytes, zeros before the first step, with `exponents` [ceil(count / 256)][2], also
+ * zeros then.  256 neighbouring elements, counted from the tensor's start, share the exponents E (of
+ * exp_avg, of exp_avg_sq): 2^(E - 127) <= the largest magnitude < 2^(E - 126) (E = 0: all below 2^-126).  A code
+ * c > 0 stands for the float with bits (c + 897) << 20 (exp_avg, bit 7 is the sign) or (c + 769) << 20
+ * (exp_avg_sq), times 2^(E - 127); 0 is zero: four significant bits over 16 or 32 powers of two.  The update
+ * works with the new values in single precision; they are then rounded to one of the two codes around them,
+ * up with the probability that keeps the mean (rounding to nearest would hold exp_avg_sq where it is for as
+ * long as its changes are below half a step), except that an exp_avg_sq above zero never becomes zero.  The
+ * probability is held against a hash of seed, step, the number of the block of 256 (counted through the
+ * tensors of the call) and the element's place in it: the same call gives the same bits.  A block with a
+ * value that is not finite gets E = 255 and reads as NaN. */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *exp_avg, *exp_avg_sq;
+    uint8_t *exponents;          /* state_bits 8 only */
+    void *copy;                  /* or NULL */
+    int64_t count;
+    int32_t param_type, grad_type, copy_type;
+} qgbdt_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay, max_norm, loss_scale;
+    int64_t step;
+    uint64_t seed;
+    const float *d_lr;
+    const int64_t *d_step;
+    const float *d_norm;
+    int32_t state_bits;
+} qgbdt_adamw_options;
+int qgbdt_adamw(qgbdt_ctx *ctx, const qgbdt_adamw_tensor *h_tensors, int32_t n_tensors, const qgbdt_adamw_options *h_options,
+                void *stream);
+/* What states of 8 bits stand for: d_m and d_v [count] of `type` (QGBDT_F32 or QGBDT_BF16; both hold the values
+ * exactly down to their smallest number).  The h_* are host arrays of n_tensors entries. */
+int qgbdt_adamw_values(qgbdt_ctx *ctx, const uint8_t *const *h_exp_avg, const uint8_t *const *h_exp_avg_sq,
+                       const uint8_t *const *h_exponents, void *const *h_m, void *const *h_v, const int64_t *h_counts,
+                       int32_t n_tensors, int32_t type, void *stream);
 
 #ifdef __cplusplus
 }

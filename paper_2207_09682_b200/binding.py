@@ -28,6 +28,7 @@ EXPORTS = [
     "qgbdt_set_distributed", "qgbdt_set_option", "qgbdt_get_info", "qgbdt_get_counters", "qgbdt_profile_histograms", "qgbdt_get_histogram_profile", "qgbdt_get_timings",
     "qgbdt_build_histograms_noalloc", "qgbdt_noalloc_last_error",
     "qgbdt_embed", "qgbdt_embed_backward", "qgbdt_softmax_ce", "qgbdt_softmax_ce_backward", "qgbdt_clip_grad_norm",
+    "qgbdt_layer_norm", "qgbdt_layer_norm_backward", "qgbdt_adamw", "qgbdt_adamw_values",
 ]
 
 
@@ -72,7 +73,8 @@ def _load_tensors():
     lib = load_library()
     from . import _tensors as module
     module.bind(QgbdtError, *(C.cast(getattr(lib, "qgbdt_" + name), C.c_void_p).value for name in (
-        "embed", "embed_backward", "softmax_ce", "softmax_ce_backward", "clip_grad_norm", "last_error")))
+        "embed", "embed_backward", "softmax_ce", "softmax_ce_backward", "clip_grad_norm", "layer_norm", "layer_norm_backward", "adamw", "adamw_values",
+        "last_error")))
     _tensors = module
     return module
 
@@ -354,6 +356,13 @@ class SoftmaxCE(NamedTuple):
     lse: torch.Tensor
 
 
+class LayerNorm(NamedTuple):
+    """Outputs of Context.layer_norm: out [N, D] of the rows' type, mean [N] and rstd [N] float32."""
+    out: torch.Tensor
+    mean: torch.Tensor
+    rstd: torch.Tensor
+
+
 # The arguments of the calls below are taken apart by the extension module _tensors (csrc/tensors.cpp): tensors of the
 # context's device, matrices with contiguous rows of any row stride; anything else is refused with ERR_ARG.  Autograd records
 # none of them: gradients come from the *_backward calls (an input that requires one is taken with a warning).
@@ -411,11 +420,65 @@ def _clip_grad_norm(self, grads, max_norm: float, out=None, stream=None) -> torc
     return (_tensors or _load_tensors()).clip_grad_norm(self.h.value or 0, self.device, grads, max_norm, out)
 
 
+def _layer_norm(self, x, weight=None, bias=None, eps: float = 1e-5, out=None, stream=None) -> LayerNorm:
+    """qgbdt_layer_norm: (x - mean) * rstd * weight + bias for every row of x [N, D] (float32, bfloat16 or float16); weight, bias
+    [D] float32 or of x's type (None: 1, 0).  `out` may be x itself."""
+    if stream is not None:
+        return _elsewhere(stream, self.layer_norm, x, weight, bias, eps, out)
+    return LayerNorm(*(_tensors or _load_tensors()).layer_norm(self.h.value or 0, self.device, x, weight, bias, eps, out))
+
+
+def _layer_norm_backward(self, grad_out, x, mean, rstd, weight=None, grad_x=None, stream=None) -> tuple:
+    """qgbdt_layer_norm_backward: (grad_x [N, D], grad_weight [D], grad_bias [D]), mean and rstd as layer_norm gave them; the latter
+    two are of the weight's type, None without a weight.  `grad_x` may be grad_out or x itself."""
+    if stream is not None:
+        return _elsewhere(stream, self.layer_norm_backward, grad_out, x, mean, rstd, weight, grad_x)
+    return (_tensors or _load_tensors()).layer_norm_backward(self.h.value or 0, self.device, grad_out, x, mean, rstd, weight, grad_x)
+
+
+def adamw_states(params, bits: int = 32) -> tuple:
+    """States of Context.adamw before the first step: (exp_avgs, exp_avg_sqs, exponents), one tensor per parameter;
+    float32 and no exponents (None), or, with 8 bits, uint8 and exponents [ceil(elements / 256), 2]."""
+    if bits not in (8, 32):
+        raise QgbdtError(ERR_ARG, "states have 8 or 32 bits")
+    params = list(params)
+    dtype = torch.uint8 if bits == 8 else torch.float32
+    m, v = ([torch.zeros(p.shape, dtype=dtype, device=p.device) for p in params] for _ in range(2))
+    return m, v, [torch.zeros((-(-p.numel() // 256), 2), dtype=torch.uint8, device=p.device) for p in params] if bits == 8 else None
+
+
+def _adamw(self, params, grads, exp_avgs, exp_avg_sqs, step, lr, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01, exponents=None, copies=None,
+           norm=None, max_norm: float = float("inf"), loss_scale: float = 1.0, seed: int = 0, stream=None) -> None:
+    """qgbdt_adamw: an AdamW step over lists of contiguous tensors, in place; states as adamw_states makes them (8 bits where
+    `exponents` is given).  step: the number of this step, from 1 (or an int64 CUDA tensor of one element); lr a number or a float32
+    CUDA tensor of one element.  norm: what clip_grad_norm gave for these gradients; they are then clipped to max_norm (of the gradients
+    divided by loss_scale), and nothing is done where the norm is not finite.  copies: tensors that receive the new parameters."""
+    if stream is not None:
+        lists = [None if a is None else list(a) for a in (params, grads, exp_avgs, exp_avg_sqs, exponents, copies)]
+        return _elsewhere(stream, self.adamw, *lists[:4], step, lr, betas, eps, weight_decay, *lists[4:], norm, max_norm, loss_scale, seed)
+    beta1, beta2 = betas
+    (_tensors or _load_tensors()).adamw(self.h.value or 0, self.device, params, grads, exp_avgs, exp_avg_sqs, exponents, copies, step, lr, beta1, beta2, eps,
+                                        weight_decay, norm, max_norm, loss_scale, seed)
+
+
+def _adamw_values(self, exp_avgs, exp_avg_sqs, exponents, dtype=torch.float32, stream=None) -> tuple:
+    """qgbdt_adamw_values: what states of 8 bits stand for, as two lists of new tensors (float32 or bfloat16)."""
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise QgbdtError(ERR_ARG, "the values' type must be float32 or bfloat16")
+    if stream is not None:
+        return _elsewhere(stream, self.adamw_values, list(exp_avgs), list(exp_avg_sqs), list(exponents), dtype)
+    return (_tensors or _load_tensors()).adamw_values(self.h.value or 0, self.device, exp_avgs, exp_avg_sqs, exponents, dtype == torch.bfloat16)
+
+
 Context.embed = _embed
 Context.embed_backward = _embed_backward
 Context.softmax_ce = _softmax_ce
 Context.softmax_ce_backward = _softmax_ce_backward
 Context.clip_grad_norm = _clip_grad_norm
+Context.layer_norm = _layer_norm
+Context.layer_norm_backward = _layer_norm_backward
+Context.adamw = _adamw
+Context.adamw_values = _adamw_values
 
 
 def unpack_hist(hist: torch.Tensor) -> tuple[np.ndarray, np.ndarray]:

@@ -33,36 +33,15 @@ int ops_init(qgbdt_ctx *c) {
     return QGBDT_OK;
 }
 
-int ops_enter(qgbdt_ctx *c) {
-    if (!c) return QGBDT_ERR_ARG;
-    if (c->ops_fault && *static_cast<volatile int *>(c->ops_fault)) {
-        *static_cast<volatile int *>(c->ops_fault) = 0;
-        return qg_fail(c, QGBDT_ERR_CUDA, "a kernel of an earlier operator call gave up waiting for its copies; that call's results are not valid");
-    }
-    int device = -1;
-    if (cudaGetDevice(&device) != cudaSuccess || device != c->device) {
-        cudaGetLastError();
-        return qg_fail(c, QGBDT_ERR_STATE, "the context belongs to device %d, the current one is %d", c->device, device);
-    }
-    return QGBDT_OK;
-}
-
-bool aligned(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)size == 0; }
-
 int check_index_type(qgbdt_ctx *c, int32_t t) {
     if (t != QGBDT_I32 && t != QGBDT_I64) return qg_fail(c, QGBDT_ERR_ARG, "index type must be QGBDT_I32 or QGBDT_I64");
     return QGBDT_OK;
 }
 
-// The row stride of a single row means nothing: one that suits the kernels, a multiple of `step` elements.
-void single_row(int64_t rows, int64_t width, int step, int64_t *ld) {
-    if (rows <= 1 && *ld >= width) *ld = (width + step - 1) / step * step;
-}
-
 int check_embed(qgbdt_ctx *c, EmbedArgs &a, bool backward) {
-    single_row(backward ? a.rows : a.n_entries, a.dim, 1, &a.ld);
-    single_row(backward ? a.n_entries : a.rows, a.dim, 1, &a.ld_out);
-    int rc = ops_enter(c);
+    qg_single_row(backward ? a.rows : a.n_entries, a.dim, 1, &a.ld);
+    qg_single_row(backward ? a.n_entries : a.rows, a.dim, 1, &a.ld_out);
+    int rc = qg_ops_enter(c);
     if (rc != QGBDT_OK) return rc;
     if (!qg_type_ok(a.type)) return qg_fail(c, QGBDT_ERR_ARG, "element type must be QGBDT_F32, QGBDT_BF16 or QGBDT_F16");
     if ((rc = check_index_type(c, a.token_type)) != QGBDT_OK) return rc;
@@ -76,17 +55,17 @@ int check_embed(qgbdt_ctx *c, EmbedArgs &a, bool backward) {
     const bool none = a.rows == 0;
     if ((!none && (!a.table || !a.tokens)) || (!a.out && !(none && !backward))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
     const int w = qg_type_size(a.type);
-    if (!aligned(a.table, w) || !aligned(a.out, w) || !aligned(a.tokens, a.token_type == QGBDT_I64 ? 8 : 4) || !aligned(a.status, 4))
+    if (!qg_aligned(a.table, w) || !qg_aligned(a.out, w) || !qg_aligned(a.tokens, a.token_type == QGBDT_I64 ? 8 : 4) || !qg_aligned(a.status, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
     return QGBDT_OK;
 }
 
 int check_softmax(qgbdt_ctx *c, SoftmaxArgs &a) {
-    single_row(a.rows, a.dim, 8, &a.ld_hidden);
-    single_row(a.classes, a.dim, 8, &a.ld_weight);
-    single_row(a.rows, a.dim, 8, &a.ld_d_hidden);
-    single_row(a.classes, a.dim, 8, &a.ld_d_weight);
-    int rc = ops_enter(c);
+    qg_single_row(a.rows, a.dim, 8, &a.ld_hidden);
+    qg_single_row(a.classes, a.dim, 8, &a.ld_weight);
+    qg_single_row(a.rows, a.dim, 8, &a.ld_d_hidden);
+    qg_single_row(a.classes, a.dim, 8, &a.ld_d_weight);
+    int rc = qg_ops_enter(c);
     if (rc != QGBDT_OK) return rc;
     if (a.type != QGBDT_BF16 && a.type != QGBDT_F16) return qg_fail(c, QGBDT_ERR_ARG, "hidden and weight must be QGBDT_BF16 or QGBDT_F16");
     if ((rc = check_index_type(c, a.label_type)) != QGBDT_OK) return rc;
@@ -98,18 +77,9 @@ int check_softmax(qgbdt_ctx *c, SoftmaxArgs &a) {
     if (a.ld_hidden >= most || a.ld_weight >= most || a.ld_d_hidden >= most || a.ld_d_weight >= most)
         return qg_fail(c, QGBDT_ERR_ARG, "row strides must be below 2^39");
     if (!a.weight || (a.rows > 0 && (!a.hidden || !a.labels))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
-    if (!aligned(a.hidden, 2) || !aligned(a.weight, 2) || !aligned(a.bias, 4) || !aligned(a.labels, a.label_type == QGBDT_I64 ? 8 : 4) || !aligned(a.status, 4))
+    if (!qg_aligned(a.hidden, 2) || !qg_aligned(a.weight, 2) || !qg_aligned(a.bias, 4) || !qg_aligned(a.labels, a.label_type == QGBDT_I64 ? 8 : 4) || !qg_aligned(a.status, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
     return QGBDT_OK;
-}
-
-// End of a call: one that failed on its way may have launched kernels, which the next call has to wait for all the same.
-int ops_leave(qgbdt_ctx *c, int rc, void *stream) {
-    if (c->ops_ws_open) {
-        const int closed = qg_ws_close(c, (cudaStream_t)stream);
-        if (rc == QGBDT_OK) rc = closed;
-    }
-    return rc;
 }
 
 // The last call of a capture, or NULL.
@@ -120,6 +90,29 @@ qgbdt_ctx::OpsCapture *last_of_capture(qgbdt_ctx *c, unsigned long long id) {
 }
 
 }  // namespace
+
+int qg_ops_enter(qgbdt_ctx *c) {
+    if (!c) return QGBDT_ERR_ARG;
+    if (c->ops_fault && *static_cast<volatile int *>(c->ops_fault)) {
+        *static_cast<volatile int *>(c->ops_fault) = 0;
+        return qg_fail(c, QGBDT_ERR_CUDA, "a kernel of an earlier operator call gave up waiting for its copies; that call's results are not valid");
+    }
+    int device = -1;
+    if (cudaGetDevice(&device) != cudaSuccess || device != c->device) {
+        cudaGetLastError();
+        return qg_fail(c, QGBDT_ERR_STATE, "the context belongs to device %d, the current one is %d", c->device, device);
+    }
+    return QGBDT_OK;
+}
+
+// End of a call: one that failed on its way may have launched kernels, which the next call has to wait for all the same.
+int qg_ops_leave(qgbdt_ctx *c, int rc, void *stream) {
+    if (c->ops_ws_open) {
+        const int closed = qg_ws_close(c, (cudaStream_t)stream);
+        if (rc == QGBDT_OK) rc = closed;
+    }
+    return rc;
+}
 
 int qg_ws_open(qgbdt_ctx *c, size_t bytes, cudaStream_t st, QgWorkspace *ws) {
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
@@ -219,7 +212,7 @@ int qgbdt_embed(qgbdt_ctx *c, const void *d_table, int32_t type, int64_t n_entri
     EmbedArgs a{d_table, ld_table, n_entries, dim, type, d_tokens, token_type, n_rows, ld_tokens, bag, scale, d_out, ld_out, d_status};
     int rc = check_embed(c, a, false);
     if (rc != QGBDT_OK || n_rows == 0) return rc;
-    return ops_leave(c, qg_embed(c, a, (cudaStream_t)stream), stream);
+    return qg_ops_leave(c, qg_embed(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_embed_backward(qgbdt_ctx *c, const void *d_grad, int32_t type, int64_t ld_grad, const void *d_tokens, int32_t token_type,
@@ -228,7 +221,7 @@ int qgbdt_embed_backward(qgbdt_ctx *c, const void *d_grad, int32_t type, int64_t
     EmbedArgs a{d_grad, ld_grad, n_entries, dim, type, d_tokens, token_type, n_rows, ld_tokens, bag, scale, d_grad_table, ld_grad_table, d_status};
     int rc = check_embed(c, a, true);
     if (rc != QGBDT_OK) return rc;
-    return ops_leave(c, qg_embed_backward(c, a, (cudaStream_t)stream), stream);
+    return qg_ops_leave(c, qg_embed_backward(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_softmax_ce(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hidden, const void *d_weight, int64_t ld_weight, int32_t type,
@@ -241,8 +234,8 @@ int qgbdt_softmax_ce(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hidden, cons
     int rc = check_softmax(c, a);
     if (rc != QGBDT_OK) return rc;
     if (!d_loss || (n_rows > 0 && !d_lse)) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
-    if (!aligned(d_loss, 4) || !aligned(d_losses, 4) || !aligned(d_lse, 4)) return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
-    return ops_leave(c, qg_softmax_ce(c, a, (cudaStream_t)stream), stream);
+    if (!qg_aligned(d_loss, 4) || !qg_aligned(d_losses, 4) || !qg_aligned(d_lse, 4)) return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
+    return qg_ops_leave(c, qg_softmax_ce(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_softmax_ce_backward(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hidden, const void *d_weight, int64_t ld_weight,
@@ -259,29 +252,29 @@ int qgbdt_softmax_ce_backward(qgbdt_ctx *c, const void *d_hidden, int64_t ld_hid
     if (rc != QGBDT_OK) return rc;
     if (!d_grad_weight || (n_rows > 0 && (!d_lse || !d_grad_hidden))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
     if ((n_rows > 0 && a.ld_d_hidden < dim) || a.ld_d_weight < dim) return qg_fail(c, QGBDT_ERR_ARG, "a row stride is smaller than the row");
-    if (!aligned(d_grad_hidden, 2) || !aligned(d_grad_weight, 2) || !aligned(d_lse, 4) || !aligned(d_grad_loss, 4) || !aligned(d_grad_bias, 4))
+    if (!qg_aligned(d_grad_hidden, 2) || !qg_aligned(d_grad_weight, 2) || !qg_aligned(d_lse, 4) || !qg_aligned(d_grad_loss, 4) || !qg_aligned(d_grad_bias, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
-    return ops_leave(c, qg_softmax_ce_backward(c, a, (cudaStream_t)stream), stream);
+    return qg_ops_leave(c, qg_softmax_ce_backward(c, a, (cudaStream_t)stream), stream);
 }
 
 int qgbdt_clip_grad_norm(qgbdt_ctx *c, const void *const *h_grads, void *const *h_out, const int64_t *h_counts, const int32_t *h_types,
                          int32_t n_tensors, double max_norm, float *d_norm, void *stream) {
-    int rc = ops_enter(c);
+    int rc = qg_ops_enter(c);
     if (rc != QGBDT_OK) return rc;
     if (n_tensors < 0 || n_tensors > (1 << 20)) return qg_fail(c, QGBDT_ERR_ARG, "n_tensors must be in [0, 2^20]");
     if (!d_norm || (n_tensors > 0 && (!h_grads || !h_counts || !h_types))) return qg_fail(c, QGBDT_ERR_ARG, "null pointer");
     if (!(max_norm >= 0.0)) return qg_fail(c, QGBDT_ERR_ARG, "max_norm must be >= 0 (infinity: the norm alone)");
-    if (!aligned(d_norm, 4)) return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
+    if (!qg_aligned(d_norm, 4)) return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
     for (int32_t i = 0; i < n_tensors; ++i) {
         if (h_counts[i] < 0) return qg_fail(c, QGBDT_ERR_ARG, "tensor %d has a negative size", i);
         if (!qg_type_ok(h_types[i])) return qg_fail(c, QGBDT_ERR_ARG, "tensor %d: element type must be QGBDT_F32, QGBDT_BF16 or QGBDT_F16", i);
         if (h_counts[i] == 0) continue;
         if (!h_grads[i] || (h_out && !h_out[i])) return qg_fail(c, QGBDT_ERR_ARG, "tensor %d is NULL", i);
         const int w = qg_type_size(h_types[i]);
-        if (!aligned(h_grads[i], w) || (h_out && !aligned(h_out[i], w))) return qg_fail(c, QGBDT_ERR_ARG, "tensor %d is not aligned to its element", i);
+        if (!qg_aligned(h_grads[i], w) || (h_out && !qg_aligned(h_out[i], w))) return qg_fail(c, QGBDT_ERR_ARG, "tensor %d is not aligned to its element", i);
     }
     void *const *out = h_out ? h_out : const_cast<void *const *>(reinterpret_cast<const void *const *>(h_grads));
-    return ops_leave(c, qg_clip_grad_norm(c, h_grads, out, h_counts, h_types, n_tensors, max_norm, d_norm, (cudaStream_t)stream), stream);
+    return qg_ops_leave(c, qg_clip_grad_norm(c, h_grads, out, h_counts, h_types, n_tensors, max_norm, d_norm, (cudaStream_t)stream), stream);
 }
 
 }  // extern "C"

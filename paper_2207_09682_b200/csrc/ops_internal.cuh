@@ -1,5 +1,5 @@
-// Shared by the operators that sit on top of the trees (embedding of leaf numbers, softmax cross
-// entropy, clipping by the gradient norm): element types, vector loads, the context's workspace.
+// Shared by the operators that sit on top of the trees (embedding of leaf numbers, layer norm, softmax
+// cross entropy, clipping by the gradient norm, AdamW): element types, vector loads, the context's workspace.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -41,6 +41,19 @@ static inline int qg_vec_bytes(const void *p, int64_t ld_bytes, int64_t len_byte
     const uintptr_t bits = reinterpret_cast<uintptr_t>(p) | (uintptr_t)ld_bytes | (uintptr_t)len_bytes | 16u;
     return (int)(bits & (~bits + 1));
 }
+
+// ---- argument checks ------------------------------------------------------------------------------
+
+static inline bool qg_aligned(const void *p, int size) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)size == 0; }
+
+// The row stride of a single row means nothing: one that suits the kernels, a multiple of `step` elements.
+static inline void qg_single_row(int64_t rows, int64_t width, int step, int64_t *ld) {
+    if (rows <= 1 && *ld >= width) *ld = (width + step - 1) / step * step;
+}
+
+// At the start and the end of a C entry: what an earlier kernel reported and the current device; the work buffer's use.
+int qg_ops_enter(qgbdt_ctx *c);
+int qg_ops_leave(qgbdt_ctx *c, int rc, void *stream);
 
 // ---- launches ------------------------------------------------------------------------------------
 
@@ -132,3 +145,23 @@ int qg_softmax_ce_backward(qgbdt_ctx *c, const SoftmaxArgs &a, cudaStream_t st);
 
 int qg_clip_grad_norm(qgbdt_ctx *c, const void *const *in, void *const *out, const int64_t *counts, const int32_t *types,
                       int32_t n, double max_norm, float *d_norm, cudaStream_t st);
+
+struct LayerNormArgs {
+    const void *x, *grad;                   // grad: backward only
+    int64_t ld_x, ld_grad;
+    int32_t type, weight_type;
+    const void *weight, *bias;              // NULL: 1, 0
+    int64_t rows;
+    int32_t dim;
+    float eps;
+    void *out;                              // backward: the gradient of x
+    int64_t ld_out;
+    float *mean, *rstd;                     // forward: NULL where not wanted; backward: read
+    void *d_weight, *d_bias;
+};
+int qg_layer_norm(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st);
+int qg_layer_norm_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st);
+
+int qg_adamw(qgbdt_ctx *c, const qgbdt_adamw_tensor *t, int32_t n, const qgbdt_adamw_options &o, cudaStream_t st);
+int qg_adamw_values(qgbdt_ctx *c, const uint8_t *const *m, const uint8_t *const *v, const uint8_t *const *exponents, void *const *out_m,
+                    void *const *out_v, const int64_t *counts, int32_t n, int32_t type, cudaStream_t st);

@@ -28,6 +28,10 @@ struct Bound {
     decltype(&qgbdt_softmax_ce) softmax_ce;
     decltype(&qgbdt_softmax_ce_backward) softmax_ce_backward;
     decltype(&qgbdt_clip_grad_norm) clip_grad_norm;
+    decltype(&qgbdt_layer_norm) layer_norm;
+    decltype(&qgbdt_layer_norm_backward) layer_norm_backward;
+    decltype(&qgbdt_adamw) adamw;
+    decltype(&qgbdt_adamw_values) adamw_values;
     decltype(&qgbdt_last_error) last_error;
     PyObject *error;
 } lib = {};
@@ -353,21 +357,233 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     END_HANDLE_TH_ERRORS
 }
 
-// bind(error class, addresses of embed, embed_backward, softmax_ce, softmax_ce_backward, clip_grad_norm, last_error)
+// Weight and bias of a layer norm: vectors of float32 or of the rows' type, or None.
+struct Affine {
+    int type = QGBDT_F32;
+    at::ScalarType scalar = at::kFloat;
+    void *weight = nullptr, *bias = nullptr;
+    bool take(const Call &c, const Rows &x, PyObject *w, PyObject *b) {
+        for (PyObject *o : {w, b}) {
+            if (o == Py_None) continue;
+            const at::Tensor *t = tensor(o, o == w ? "weight" : "bias");
+            if (!t) return false;
+            if ((o == w || w == Py_None)) scalar = t->scalar_type();
+            else if (t->scalar_type() != scalar) return refuse("weight and bias must have the same type"), false;
+            if (!unrecorded(*t, o == w ? "weight" : "bias")) return false;
+        }
+        if (scalar != at::kFloat && scalar != x.t->scalar_type()) return refuse("weight and bias must be float32 or of the rows' type"), false;
+        type = scalar == at::kFloat ? QGBDT_F32 : x.type;
+        return words(c, w, "weight", scalar, x.d, &weight) && words(c, b, "bias", scalar, x.d, &bias);
+    }
+};
+
+// layer_norm(ctx, device, x, weight, bias, eps, out) -> (out, mean, rstd)
+PyObject *py_layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Call c;
+    Rows x;
+    Affine w;
+    Output out;
+    double eps;
+    if (!c.take(args, nargs, 7) || !x.take_input(c, args[2], "x")) return nullptr;
+    if (x.type < 0) return refuse("x must be float32, bfloat16 or float16");
+    if (!w.take(c, x, args[3], args[4]) || !number(args[5], &eps) || !out.take(c, args[6], "out", x.n, x.d, *x.t)) return nullptr;
+    const at::Tensor both = at::empty({2 * x.n}, x.t->options().dtype(at::kFloat).requires_grad(false));
+    float *p = both.data_ptr<float>();   // mean, rstd
+    const int rc = lib.layer_norm(c.ctx, x.p(), x.ld, x.type, w.weight, w.bias, w.type, x.n, (int32_t)x.d, eps, out.r.p(), out.r.ld, p, p + x.n, c.stream);
+    if (rc != QGBDT_OK) return c.result(rc);
+    PyObject *const mean = THPVariable_Wrap(both.slice(0, 0, x.n)), *const rstd = THPVariable_Wrap(both.slice(0, x.n, 2 * x.n));
+    return Py_BuildValue("(NNN)", out.give(args[6]), mean, rstd);
+    END_HANDLE_TH_ERRORS
+}
+
+// layer_norm_backward(ctx, device, grad_out, x, mean, rstd, weight, grad_x) -> (grad_x, grad_weight or None, grad_bias or None)
+PyObject *py_layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Call c;
+    Rows grad, x;
+    Affine w;
+    Output gx;
+    void *mean, *rstd;
+    if (!c.take(args, nargs, 8) || !grad.take_input(c, args[2], "grad_out") || !x.take_input(c, args[3], "x")) return nullptr;
+    if (x.type < 0) return refuse("x must be float32, bfloat16 or float16");
+    if (grad.type != x.type || grad.n != x.n || grad.d != x.d) return refuse("grad_out and x differ in size or type");
+    if (args[4] == Py_None || args[5] == Py_None) return refuse("mean and rstd are those of the forward call");
+    if (!words(c, args[4], "mean", at::kFloat, x.n, &mean) || !words(c, args[5], "rstd", at::kFloat, x.n, &rstd) ||
+        !w.take(c, x, args[6], Py_None) || !gx.take(c, args[7], "grad_x", x.n, x.d, *x.t))
+        return nullptr;
+    at::Tensor gw, gb;
+    if (w.weight || args[6] != Py_None) {
+        const auto options = x.t->options().dtype(w.scalar).requires_grad(false);
+        gw = at::empty({x.d}, options), gb = at::empty({x.d}, options);
+    }
+    const int rc = lib.layer_norm_backward(c.ctx, grad.p(), grad.ld, x.p(), x.ld, x.type, (const float *)mean, (const float *)rstd, w.weight, w.type, x.n,
+                                           (int32_t)x.d, gx.r.p(), gx.r.ld, gw.defined() ? gw.data_ptr() : nullptr, gb.defined() ? gb.data_ptr() : nullptr,
+                                           c.stream);
+    if (rc != QGBDT_OK) return c.result(rc);
+    PyObject *const x_grad = gx.give(args[7]);
+    if (!gw.defined()) return Py_BuildValue("(NOO)", x_grad, Py_None, Py_None);
+    PyObject *const weight_grad = THPVariable_Wrap(gw), *const bias_grad = THPVariable_Wrap(gb);
+    return Py_BuildValue("(NNN)", x_grad, weight_grad, bias_grad);
+    END_HANDLE_TH_ERRORS
+}
+
+// A list of contiguous tensors on the context's device.
+struct List {
+    THPObjectPtr held;   // the tensors stay alive until the call has been made
+    Py_ssize_t n = 0;
+    const char *name = "";
+    bool take(PyObject *o, const char *what, Py_ssize_t want) {
+        name = what;
+        held = THPObjectPtr(PySequence_Fast(o, "expected a list of tensors"));
+        if (!held.get()) return false;
+        n = PySequence_Fast_GET_SIZE(held.get());
+        return want < 0 || n == want || (refuse(name, "must match the parameters in number"), false);
+    }
+    const at::Tensor *get(const Call &c, Py_ssize_t i) const {
+        if (i >= PySequence_Fast_GET_SIZE(held.get())) return refuse(name, "changed during the call"), nullptr;
+        const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(held.get(), i), name);
+        if (t && (!c.here(*t) || !t->is_contiguous())) return refuse(name, "must be contiguous tensors on the context's device"), nullptr;
+        return t;
+    }
+    void written_all() const {
+        for (Py_ssize_t i = 0; held.get() && i < PySequence_Fast_GET_SIZE(held.get()); ++i) {
+            PyObject *const o = PySequence_Fast_GET_ITEM(held.get(), i);
+            if (THPVariable_Check(o)) written(THPVariable_Unpack(o));
+        }
+    }
+};
+
+// A number, or one in device memory: a CUDA tensor of one element of type `type`.
+bool number_or_tensor(const Call &c, PyObject *o, const char *name, at::ScalarType type, void **at) {
+    *at = nullptr;
+    return !THPVariable_Check(o) || words(c, o, name, type, 1, at);
+}
+
+// adamw(ctx, device, params, grads, exp_avgs, exp_avg_sqs, exponents, copies, step, lr, beta1, beta2, eps, weight_decay, norm, max_norm, loss_scale, seed)
+PyObject *py_adamw(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Call c;
+    List params, grads, ms, vs, exponents, copies;
+    qgbdt_adamw_options o{};
+    void *d_step, *d_lr, *d_norm;
+    if (!c.take(args, nargs, 18) || !params.take(args[2], "params", -1) || !grads.take(args[3], "grads", params.n) || !ms.take(args[4], "exp_avgs", params.n) ||
+        !vs.take(args[5], "exp_avg_sqs", params.n))
+        return nullptr;
+    const bool packed = args[6] != Py_None, copied = args[7] != Py_None;
+    if ((packed && !exponents.take(args[6], "exponents", params.n)) || (copied && !copies.take(args[7], "copies", params.n))) return nullptr;
+    if (!number_or_tensor(c, args[8], "step", at::kLong, &d_step) || !number_or_tensor(c, args[9], "lr", at::kFloat, &d_lr) ||
+        !words(c, args[14], "norm", at::kFloat, 1, &d_norm))
+        return nullptr;
+    if (!d_step) o.step = PyLong_AsLongLong(args[8]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!d_lr && !number(args[9], &o.lr)) return nullptr;
+    if (!number(args[10], &o.beta1) || !number(args[11], &o.beta2) || !number(args[12], &o.eps) || !number(args[13], &o.weight_decay) ||
+        !number(args[15], &o.max_norm) || !number(args[16], &o.loss_scale))
+        return nullptr;
+    o.seed = PyLong_AsUnsignedLongLongMask(args[17]);
+    if (PyErr_Occurred()) return nullptr;
+    o.d_step = (const int64_t *)d_step, o.d_lr = (const float *)d_lr, o.d_norm = (const float *)d_norm, o.state_bits = packed ? 8 : 32;
+    std::vector<qgbdt_adamw_tensor> list((size_t)params.n);
+    const at::Tensor *recorded = nullptr;
+    for (Py_ssize_t i = 0; i < params.n; ++i) {
+        const at::Tensor *p = params.get(c, i), *g = p ? grads.get(c, i) : nullptr, *m = g ? ms.get(c, i) : nullptr, *v = m ? vs.get(c, i) : nullptr;
+        if (!v) return nullptr;
+        qgbdt_adamw_tensor &t = list[(size_t)i];
+        t.count = p->numel();
+        t.param_type = element(*p), t.grad_type = element(*g);
+        if (t.param_type < 0 || t.grad_type < 0) return refuse("params and grads must be float32, bfloat16 or float16");
+        if (g->numel() != t.count || m->numel() != t.count || v->numel() != t.count) return refuse("grads and states must match the parameters in sizes");
+        const at::ScalarType state = packed ? at::kByte : at::kFloat;
+        if (m->scalar_type() != state || v->scalar_type() != state)
+            return refuse(packed ? "states with exponents must be uint8" : "states must be float32 (or uint8, with exponents)");
+        if (g->requires_grad()) recorded = g;
+        t.param = p->data_ptr(), t.grad = g->data_ptr(), t.exp_avg = m->data_ptr(), t.exp_avg_sq = v->data_ptr();
+        if (packed) {
+            const at::Tensor *e = exponents.get(c, i);
+            if (!e) return nullptr;
+            if (e->scalar_type() != at::kByte || e->dim() != 2 || e->size(0) != (t.count + 255) / 256 || e->size(1) != 2)
+                return refuse("exponents must be uint8 [ceil(elements / 256), 2]");
+            t.exponents = (uint8_t *)e->data_ptr();
+        }
+        if (copied) {
+            const at::Tensor *k = copies.get(c, i);
+            if (!k) return nullptr;
+            t.copy_type = element(*k);
+            if (t.copy_type < 0 || k->numel() != t.count) return refuse("copies must match the parameters in sizes and be float32, bfloat16 or float16");
+            t.copy = k->data_ptr();
+        }
+    }
+    if (recorded && !unrecorded(*recorded, "grads")) return nullptr;
+    const int rc = lib.adamw(c.ctx, list.data(), (int32_t)params.n, &o, c.stream);
+    if (rc != QGBDT_OK) return c.result(rc);
+    for (const List *l : {&params, &ms, &vs, &exponents, &copies}) l->written_all();
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// adamw_values(ctx, device, exp_avgs, exp_avg_sqs, exponents, bfloat16) -> (list of m, list of v)
+PyObject *py_adamw_values(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    HANDLE_TH_ERRORS
+    Call c;
+    List ms, vs, exponents;
+    if (!c.take(args, nargs, 6) || !ms.take(args[2], "exp_avgs", -1) || !vs.take(args[3], "exp_avg_sqs", ms.n) || !exponents.take(args[4], "exponents", ms.n))
+        return nullptr;
+    const int half = PyObject_IsTrue(args[5]);
+    if (half < 0) return nullptr;
+    std::vector<const uint8_t *> m, v, e;
+    std::vector<at::Tensor> made[2];
+    std::vector<void *> out[2];
+    std::vector<int64_t> counts;
+    for (Py_ssize_t i = 0; i < ms.n; ++i) {
+        const at::Tensor *a = ms.get(c, i), *b = a ? vs.get(c, i) : nullptr, *x = b ? exponents.get(c, i) : nullptr;
+        if (!x) return nullptr;
+        const int64_t n = a->numel();
+        if (a->scalar_type() != at::kByte || b->scalar_type() != at::kByte || b->numel() != n) return refuse("states must be uint8 and match in sizes");
+        if (x->scalar_type() != at::kByte || x->dim() != 2 || x->size(0) != (n + 255) / 256 || x->size(1) != 2)
+            return refuse("exponents must be uint8 [ceil(elements / 256), 2]");
+        m.push_back((const uint8_t *)a->data_ptr()), v.push_back((const uint8_t *)b->data_ptr()), e.push_back((const uint8_t *)x->data_ptr());
+        counts.push_back(n);
+        for (int k = 0; k < 2; ++k) {
+            made[k].push_back(at::empty(a->sizes(), a->options().dtype(half ? at::kBFloat16 : at::kFloat)));
+            out[k].push_back(made[k].back().data_ptr());
+        }
+    }
+    const int rc = lib.adamw_values(c.ctx, m.data(), v.data(), e.data(), out[0].data(), out[1].data(), counts.data(), (int32_t)ms.n,
+                                    half ? QGBDT_BF16 : QGBDT_F32, c.stream);
+    if (rc != QGBDT_OK) return c.result(rc);
+    PyObject *lists[2];
+    for (int k = 0; k < 2; ++k) {
+        lists[k] = PyList_New(ms.n);
+        if (!lists[k]) {
+            if (k) Py_DECREF(lists[0]);
+            return nullptr;
+        }
+        for (Py_ssize_t i = 0; i < ms.n; ++i) PyList_SET_ITEM(lists[k], i, THPVariable_Wrap(made[k][(size_t)i]));
+    }
+    return Py_BuildValue("(NN)", lists[0], lists[1]);
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(error class, addresses of embed, embed_backward, softmax_ce, softmax_ce_backward, clip_grad_norm, layer_norm, layer_norm_backward, adamw,
+// adamw_values, last_error)
 PyObject *py_bind(PyObject *, PyObject *args) {
     PyObject *error;
-    unsigned long long p[6];
-    if (!PyArg_ParseTuple(args, "OKKKKKK", &error, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5])) return nullptr;
+    unsigned long long p[10];
+    if (!PyArg_ParseTuple(args, "OKKKKKKKKKK", &error, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9])) return nullptr;
     Py_INCREF(error);
     Py_XDECREF(lib.error);
     lib = Bound{reinterpret_cast<decltype(lib.embed)>(p[0]),          reinterpret_cast<decltype(lib.embed_backward)>(p[1]),
                 reinterpret_cast<decltype(lib.softmax_ce)>(p[2]),     reinterpret_cast<decltype(lib.softmax_ce_backward)>(p[3]),
-                reinterpret_cast<decltype(lib.clip_grad_norm)>(p[4]), reinterpret_cast<decltype(lib.last_error)>(p[5]), error};
+                reinterpret_cast<decltype(lib.clip_grad_norm)>(p[4]), reinterpret_cast<decltype(lib.layer_norm)>(p[5]),
+                reinterpret_cast<decltype(lib.layer_norm_backward)>(p[6]), reinterpret_cast<decltype(lib.adamw)>(p[7]),
+                reinterpret_cast<decltype(lib.adamw_values)>(p[8]),   reinterpret_cast<decltype(lib.last_error)>(p[9]), error};
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(embed), FAST(embed_backward), FAST(softmax_ce), FAST(softmax_ce_backward), FAST(clip_grad_norm),
+                         FAST(layer_norm), FAST(layer_norm_backward), FAST(adamw), FAST(adamw_values),
                          {"bind", py_bind, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", "Argument marshalling of the operators on top of the trees.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
