@@ -4,6 +4,7 @@ Trains trees on a synthetic binary task, sends the rows through them, and trains
 their leaves to tell one of --classes classes that depend on the same features.
 
     python examples/leaf_classifier.py [--rows 50000] [--classes 500] [--dim 64] [--epochs 5]
+                                       [--layer-norm] [--optimizer adamw [--state-bits 8]]
 """
 import argparse
 import os
@@ -32,20 +33,24 @@ def main(argv=None) -> tuple:
     ap.add_argument("--dim", type=int, default=64)
     ap.add_argument("--epochs", type=int, default=5)
     ap.add_argument("--batch", type=int, default=1024)
-    ap.add_argument("--lr", type=float, default=4.0)
+    ap.add_argument("--lr", type=float, default=None, help="4 for sgd, 0.01 for adamw")
+    ap.add_argument("--layer-norm", action="store_true", help="normalise the sums of embeddings")
+    ap.add_argument("--optimizer", choices=["sgd", "adamw"], default="sgd")
+    ap.add_argument("--state-bits", type=int, choices=[8, 32], default=32, help="of AdamW's states")
     a = ap.parse_args(argv)
+    lr = a.lr if a.lr is not None else 4.0 if a.optimizer == "sgd" else 0.01
     wl = synth.tiny(device="cuda", rows=a.rows)
     ctx = binding.Context(binding.make_params(**wl.params))
     ctx.load_binned(wl.bins, wl.n_bins)
     trees = wl.params["num_trees"]
     model = ctx.train(wl.labels, torch.zeros(a.rows, device="cuda"), 0, trees)
     tokens, labels = leaf_tokens(ctx, model), classes_of(wl.bins, wl.n_bins, a.classes)
-    net = LeafClassifier(ctx, trees, model.L, a.classes, a.dim)
+    net = LeafClassifier(ctx, trees, model.L, a.classes, a.dim, layer_norm=a.layer_norm, optimizer=a.optimizer, state_bits=a.state_bits)
     losses = []
     for epoch in range(a.epochs):
         order = torch.randperm(a.rows, device="cuda")
         for at in order.split(a.batch):
-            step = net.step(tokens[at], labels[at], a.lr, max_norm=1.0)
+            step = net.step(tokens[at], labels[at], lr, max_norm=1.0)
         losses.append(float(net.loss(tokens, labels).loss))
         print("epoch %d: loss %.4f, gradient norm of the last batch %.3f" % (epoch, losses[-1], float(step.norm)))
     right = float((net.predict(tokens) == labels).float().mean())

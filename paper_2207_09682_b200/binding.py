@@ -452,7 +452,7 @@ def _adamw(self, params, grads, exp_avgs, exp_avg_sqs, step, lr, betas=(0.9, 0.9
     """qgbdt_adamw: an AdamW step over lists of contiguous tensors, in place; states as adamw_states makes them (8 bits where
     `exponents` is given).  step: the number of this step, from 1 (or an int64 CUDA tensor of one element); lr a number or a float32
     CUDA tensor of one element.  norm: what clip_grad_norm gave for these gradients; they are then clipped to max_norm (of the gradients
-    divided by loss_scale), and nothing is done where the norm is not finite.  copies: tensors that receive the new parameters."""
+    divided by loss_scale), and nothing is done where the norm is not finite.  copies: tensors that receive the new parameters (None where there is none)."""
     if stream is not None:
         lists = [None if a is None else list(a) for a in (params, grads, exp_avgs, exp_avg_sqs, exponents, copies)]
         return _elsewhere(stream, self.adamw, *lists[:4], step, lr, betas, eps, weight_decay, *lists[4:], norm, max_norm, loss_scale, seed)

@@ -413,7 +413,7 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n
         !w.take(c, x, args[6], Py_None) || !gx.take(c, args[7], "grad_x", x.n, x.d, *x.t))
         return nullptr;
     at::Tensor gw, gb;
-    if (w.weight || args[6] != Py_None) {
+    if (args[6] != Py_None) {
         const auto options = x.t->options().dtype(w.scalar).requires_grad(false);
         gw = at::empty({x.d}, options), gb = at::empty({x.d}, options);
     }
@@ -440,6 +440,7 @@ struct List {
         n = PySequence_Fast_GET_SIZE(held.get());
         return want < 0 || n == want || (refuse(name, "must match the parameters in number"), false);
     }
+    bool none(Py_ssize_t i) const { return i < PySequence_Fast_GET_SIZE(held.get()) && PySequence_Fast_GET_ITEM(held.get(), i) == Py_None; }
     const at::Tensor *get(const Call &c, Py_ssize_t i) const {
         if (i >= PySequence_Fast_GET_SIZE(held.get())) return refuse(name, "changed during the call"), nullptr;
         const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(held.get(), i), name);
@@ -506,7 +507,7 @@ PyObject *py_adamw(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
                 return refuse("exponents must be uint8 [ceil(elements / 256), 2]");
             t.exponents = (uint8_t *)e->data_ptr();
         }
-        if (copied) {
+        if (copied && !copies.none(i)) {
             const at::Tensor *k = copies.get(c, i);
             if (!k) return nullptr;
             t.copy_type = element(*k);
