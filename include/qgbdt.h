@@ -410,7 +410,9 @@ int qgbdt_layer_norm_backward(qgbdt_ctx *ctx, const void *d_grad, int64_t ld_gra
  *   param = param * (1 - lr * weight_decay)
  *           - lr / (1 - beta1^step) * exp_avg / (sqrt(exp_avg_sq / (1 - beta2^step)) + eps)
  *   copy  = param, rounded to the copy's type
- * in single precision (the factors that are the same for all elements in double).  The first step is 1.
+ * in single precision (the factors that are the same for all elements in double; root and quotient by
+ * approximations, 2^-22 of the change off, for which an exp_avg_sq below 2^-126 counts as that).  The
+ * first step is 1.
  * d_norm: the gradients' norm as qgbdt_clip_grad_norm reports it for these gradients (NULL: no clipping);
  * where it is not finite nothing at all is written.  loss_scale: what the loss was multiplied with.
  * d_lr, d_step: one number in device memory in place of lr or step (NULL: those), for a captured call.

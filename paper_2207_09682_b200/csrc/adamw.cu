@@ -11,11 +11,15 @@
 
 namespace {
 
-constexpr int AW_THREADS = 256;
+// Threads and resident blocks of an SM, of the update with packed and with plain states: the former waits more for its own
+// instructions than for the memory and has 20 warps of 96 registers (16 of 128: 2 % slower), the latter 16 (20: 1 % slower).
+template <bool PACKED>
+constexpr int AW_THREADS = PACKED ? 128 : 256;
+template <bool PACKED>
+constexpr int AW_RESIDENT = PACKED ? 5 : 2;
 constexpr int AW_BLOCK = 256;                    // elements that share exponents: 8 per lane
-constexpr int AW_WARPS = AW_THREADS / 32;
-constexpr int AW_SMALL = 32, AW_LARGE = 400;     // tensors per launch (parameters of 2.3 or 28 KB)
-constexpr int AW_CODES_M = 897, AW_CODES_V = 769;
+constexpr int AW_SMALL = 16, AW_MEDIUM = 64, AW_LARGE = 400;     // tensors per launch (parameters of 1.1, 4 or 25 KB)
+constexpr unsigned AW_CODES_M = 897, AW_CODES_V = 769;
 
 // Types in `what`: bits 0-1 parameter, 2-3 gradient, 4-5 copy; bit 6: vectors.
 template <int CAP>
@@ -33,14 +37,14 @@ struct AdamwTable {
 };
 
 struct AdamwScalars {
-    float coef, b1, c1, b2, c2, eps, keep, size, root;   // p = p * keep - size * m / (sqrt(v) * root + eps)
+    float coef, b1, c1, b2, c2, keep, root, eps;   // p = p * keep - m / (sqrt(v) * root + eps)
     unsigned key;
 };
 
 // The same for all elements: worked out on the host, but for what depends on numbers in device memory.
 struct AdamwFactors {
     AdamwScalars s;
-    double lr, beta1, beta2, decay, max_norm, loss_scale;   // max_norm: times loss_scale
+    double lr, beta1, beta2, eps, decay, max_norm, loss_scale;   // max_norm: times loss_scale
     long long step;
     unsigned seed;             // hashed
     const float *d_lr;
@@ -57,9 +61,11 @@ __host__ __device__ __forceinline__ unsigned aw_mix(unsigned x) {
 }
 
 __host__ __device__ inline void aw_of_step(AdamwScalars &s, const AdamwFactors &f, double lr, long long step) {
+    const double size = lr / (1.0 - pow(f.beta1, (double)step));
     s.keep = (float)(1.0 - lr * f.decay);
-    s.size = (float)(lr / (1.0 - pow(f.beta1, (double)step)));
-    s.root = (float)(1.0 / sqrt(1.0 - pow(f.beta2, (double)step)));
+    // both infinite without a rate
+    s.root = (float)(1.0 / (size * sqrt(1.0 - pow(f.beta2, (double)step))));
+    s.eps = size > 0.0 ? (float)(f.eps / size) : s.root;
     s.key = aw_mix(f.seed ^ (unsigned)step);
 }
 
@@ -91,19 +97,71 @@ __device__ __forceinline__ void aw_store(void *p, int type, int64_t i, float x) 
 // 2^(E - 127); NaN for E = 255.
 __device__ __forceinline__ float aw_power(unsigned e) { return __uint_as_float(e == 255 ? 0x7fc00000u : e ? e << 23 : 0x00400000u); }
 
-__device__ __forceinline__ float aw_decode(unsigned code, unsigned offset, float power) {   // code without its sign
-    return (code ? __uint_as_float((code + offset) << 20) : 0.f) * power;
+// 2^(127 - E) for E < 255.
+__device__ __forceinline__ float aw_inverse(unsigned e) { return __uint_as_float(e == 254 ? 0x00400000u : (254 - e) << 23); }
+
+// What eight codes stand for, times 2^(127 - E).  Two at once, as halves of a word that hold the upper 16 bits of the values: bits (code + offset) << 4, or 0
+// for code 0.  (Integer instructions have half the rate of the others; sums and shifts are products where they can be.)
+template <unsigned OFFSET, bool SIGNED>
+__device__ __forceinline__ void aw_values_of(const uint2 &codes, float (&x)[8]) {
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+        const unsigned word = k < 4 ? codes.x : codes.y, code = SIGNED ? word & 0x7f7f7f7fu : word;
+        const unsigned two = __byte_perm(code, 0, k & 2 ? 0x4342 : 0x4140);
+        unsigned bits = two * 16u;
+        if (SIGNED) bits += __byte_perm(word & 0x80808080u, 0, k & 2 ? 0x3424 : 0x1404);
+        bits += __vminu2(two, 0x00010001u) * (OFFSET * 16u);
+        x[k] = __uint_as_float(bits << 16);
+        x[k + 1] = __uint_as_float(bits & 0xffff0000u);
+    }
 }
 
-// The code of y >= 0, below 2; r: 16 random bits.  From the smallest code's value on the bits below the code's are cut off
-// after the random ones have been added to them; below it, it is the smallest code or zero.
-template <bool KEEP>
-__device__ __forceinline__ unsigned aw_encode(float y, unsigned offset, unsigned r) {
-    const float least = __uint_as_float((offset + 1) << 20);
-    r = (r << 4) + 8;
-    const unsigned code = ((__float_as_uint(y) + r) >> 20) - offset;
-    const bool one = KEEP ? y > 0.f : (float)r * (least * 0x1p-20f) < y;
-    return y < least ? (one ? 1u : 0u) : code;
+// Code of y (2 > y >= the smallest code's value, or the value at the place of code 0 for zero) in the uppermost byte: the bits below a
+// code's, and 8 below those, are rounded by the carry of 16 random bits r << 8.  (What is above the code falls off at the top.)
+template <unsigned OFFSET>
+__device__ __forceinline__ unsigned aw_encode(unsigned y, unsigned r) { return y * 16u + (128u - (OFFSET << 24)) + r; }
+
+// The uppermost bytes of four words.
+__device__ __forceinline__ unsigned aw_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// The code, 0 or 1, of a y below the smallest code's value; r: 16 random bits.
+__device__ __forceinline__ unsigned aw_code(float y, unsigned offset, unsigned r) {
+    return (float)((r << 4) + 8) * (__uint_as_float((offset + 1) << 20) * 0x1p-20f) < y ? 1u : 0u;
+}
+
+// Eight elements' states to codes; `hash`: that of the first one's place, before it is mixed; the places are 2^APART apart.
+template <int APART>
+__device__ __forceinline__ void aw_round(const float (&m)[8], const float (&v)[8], float inverse_m, float inverse_v, unsigned hash, uint2 (&codes)[2]) {
+    constexpr unsigned zero_m = AW_CODES_M << 20, zero_v = AW_CODES_V << 20, least_m = (AW_CODES_M + 1) << 20;
+    const unsigned mixed = hash ^ hash >> 16;      // aw_mix's first step, for all eight: their places differ in three bits
+    unsigned cm[8], cv[8], ym[8], smallest = ~0u;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        unsigned x = (mixed ^ k << APART) * 0x9E3779B9u;
+        x ^= x >> 15;
+        x *= 0xBB67AE85u;
+        const unsigned upper = __byte_perm(x, 0, 0x4324);    // the upper half, << 8 (the last step leaves it)
+        ym[k] = __float_as_uint(fabsf(m[k]) * inverse_m);
+        if (k & 1) smallest = __vimin3_u32(smallest, ym[k - 1] - 1, ym[k] - 1);
+        cm[k] = aw_encode<AW_CODES_M>(max(ym[k], zero_m), upper);
+        // v: above zero it is the smallest code at least
+        const unsigned yv = __float_as_uint(v[k] * inverse_v);
+        cv[k] = aw_encode<AW_CODES_V>(max(yv, min(yv, 1u) * (1u << 20) + zero_v), __byte_perm(x, 0, 0x4104) ^ upper);
+    }
+    if (smallest < least_m - 1) {   // rare: an m between zero and the smallest code is one of the two
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float y = fabsf(m[k]) * inverse_m;
+            if (y > 0.f && y < __uint_as_float(least_m)) cm[k] = aw_code(y, AW_CODES_M, aw_mix(hash ^ k << APART) >> 16) << 24;
+        }
+    }
+    codes[1].x = aw_bytes(cv[0], cv[1], cv[2], cv[3]);
+    codes[1].y = aw_bytes(cv[4], cv[5], cv[6], cv[7]);
+    auto bits = [&](int k) { return __float_as_uint(m[k]); };
+    codes[0].x = aw_bytes(cm[0], cm[1], cm[2], cm[3]) | (aw_bytes(bits(0), bits(1), bits(2), bits(3)) & 0x80808080u);
+    codes[0].y = aw_bytes(cm[4], cm[5], cm[6], cm[7]) | (aw_bytes(bits(4), bits(5), bits(6), bits(7)) & 0x80808080u);
 }
 
 template <int CAP>
@@ -117,22 +175,19 @@ __device__ __forceinline__ int aw_find(const AdamwTable<CAP> &t, unsigned block)
     return lo;
 }
 
-// One element: m, v and p are replaced.  m and v in operations that are rounded one by one (what is rounded to 8 bits
-// afterwards then has the bits of the formula written out); the root and the quotient by the approximations of the
-// special function unit, 2^-22 of the change off at most: with the exact ones the update has half as many instructions again.
-__device__ __forceinline__ void aw_element(const AdamwScalars &s, float g, float &m, float &v, float &p) {
+// One element: m, v and p are replaced.  b1 and b2 come with the power of two that m and v are to be multiplied with (which
+// changes no rounding).  m and v in operations that are rounded one by one (what is rounded to 8 bits afterwards then has the
+// bits of the formula written out); the root and the quotient by the approximations of the special function unit, 2^-22 of the
+// change off at most: exact ones would be half as many instructions again.  Below 2^-126 they take v for that.
+__device__ __forceinline__ void aw_element(const AdamwScalars &s, float b1, float b2, float g, float &m, float &v, float &p) {
     g = g * s.coef;
-    m = m * s.b1 + g * s.c1;
-    v = v * s.b2 + (g * s.c2) * g;
-    float root;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(root) : "f"(v));
-    p = fmaf(p, s.keep, -s.size * __fdividef(m, fmaf(root, s.root, s.eps)));
+    m = m * b1 + g * s.c1;
+    v = v * b2 + (g * s.c2) * g;
+    float root, one;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v + 1.17549435e-38f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(one) : "f"(fmaf(root, s.root, s.eps)));
+    p = fmaf(p, s.keep, -(m * one));
 }
-
-// The exponent of a block's largest magnitude (E; NaN and infinity give 255), from the lanes' largest bits.
-__device__ __forceinline__ unsigned aw_exponent(unsigned bits) { return __reduce_max_sync(0xffffffffu, bits) >> 23; }
-// 2^(127 - E) for E < 255.
-__device__ __forceinline__ float aw_inverse(unsigned e) { return __uint_as_float(e == 254 ? 0x00400000u : (254 - e) << 23); }
 
 // Eight neighbouring elements of a lane: 32 bytes in one access where they have 4 each, 16 or 8 else.
 constexpr int AW_EACH = AW_BLOCK / 32;
@@ -150,19 +205,21 @@ __device__ __forceinline__ void aw_write32(void *p, const AwRaw &r) {
                  "r"(r.x[5]), "r"(r.x[6]), "r"(r.x[7]), "l"(p)
                  : "memory");
 }
-__device__ __forceinline__ void aw_read(AwRaw &r, const void *p, int type, int64_t at) {
-    if (type == QGBDT_F32) {
+template <bool WIDE>
+__device__ __forceinline__ void aw_read(AwRaw &r, const void *p, int64_t at) {
+    if constexpr (WIDE) {
         aw_read32(r, reinterpret_cast<const float *>(p) + at);
     } else {
         const uint4 q = *reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(p) + at);
         r.x[0] = q.x, r.x[1] = q.y, r.x[2] = q.z, r.x[3] = q.w;
     }
 }
-__device__ __forceinline__ void aw_unpack(float (&f)[8], const AwRaw &r, int type) {
-    if (type == QGBDT_F32) {
+template <bool WIDE>
+__device__ __forceinline__ void aw_unpack(float (&f)[8], const AwRaw &r, bool bf16) {
+    if constexpr (WIDE) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) f[k] = __uint_as_float(r.x[k]);
-    } else if (type == QGBDT_BF16) {
+    } else if (bf16) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) f[2 * k] = __uint_as_float(r.x[k] << 16), f[2 * k + 1] = __uint_as_float(r.x[k] & 0xffff0000u);
     } else {
@@ -173,186 +230,276 @@ __device__ __forceinline__ void aw_unpack(float (&f)[8], const AwRaw &r, int typ
         }
     }
 }
-__device__ __forceinline__ void aw_write(void *p, int type, int64_t at, const float (&f)[8]) {
+template <bool WIDE>
+__device__ __forceinline__ void aw_write(void *p, int64_t at, const float (&f)[8], bool bf16) {
     AwRaw r;
-    if (type == QGBDT_F32) {
+    if constexpr (WIDE) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) r.x[k] = __float_as_uint(f[k]);
         aw_write32(reinterpret_cast<float *>(p) + at, r);
-        return;
-    }
+    } else {
+        if (bf16) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (type == QGBDT_BF16) *reinterpret_cast<__nv_bfloat162 *>(&r.x[k]) = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
-        else *reinterpret_cast<__half2 *>(&r.x[k]) = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<__nv_bfloat162 *>(&r.x[k]) = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<__half2 *>(&r.x[k]) = __floats2half2_rn(f[2 * k], f[2 * k + 1]);
+        }
+        *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(p) + at) = make_uint4(r.x[0], r.x[1], r.x[2], r.x[3]);
     }
-    *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(p) + at) = make_uint4(r.x[0], r.x[1], r.x[2], r.x[3]);
 }
 
-// A warp takes `per` neighbouring blocks of 256 at a time.  Where addresses allow it and the block is whole, a lane has eight
-// neighbouring elements, else every 32nd.
+// The larger of a and two magnitudes; NaN if one is NaN.
+__device__ __forceinline__ float aw_largest(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+// Exponent E of the largest of the lanes' values (NaN and infinity: 255).
+__device__ __forceinline__ unsigned aw_exponent(float largest) { return __reduce_max_sync(0xffffffffu, __float_as_uint(largest)) >> 23; }
+
+// What a tensor's blocks have in common.
+struct AwTensor {
+    void *param, *copy, *m, *v;
+    const void *grad;
+    int param_type, grad_type, copy_type;
+};
+
+// A lane's eight neighbouring elements, as they are read.
+template <bool PACKED, bool WIDE_P, bool WIDE_G>
+struct AwInput {
+    AwRaw p, g, m, v;    // 16-bit p and g: four words; packed m and v: two
+    __device__ __forceinline__ void read(const AwTensor &t, int64_t at) {
+        if constexpr (PACKED) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(t.m) + at);
+            const uint2 b = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(t.v) + at);
+            m.x[0] = a.x, m.x[1] = a.y, v.x[0] = b.x, v.x[1] = b.y;
+        } else {
+            aw_read32(m, reinterpret_cast<const float *>(t.m) + at);
+            aw_read32(v, reinterpret_cast<const float *>(t.v) + at);
+        }
+        aw_read<WIDE_P>(p, t.param, at);
+        aw_read<WIDE_G>(g, t.grad, at);
+    }
+};
+
+// Eight elements of a lane, whose places are 2^APART apart, m and v without the powers of two of the exponents e.  Packed: m and
+// v are rounded to codes, e is replaced.
+template <bool PACKED, int APART>
+__device__ __forceinline__ void aw_eight(const AdamwScalars &s, float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8], unsigned hash, unsigned (&e)[2],
+                                         uint2 (&codes)[2]) {
+    const float b1 = PACKED ? s.b1 * aw_power(e[0]) : s.b1, b2 = PACKED ? s.b2 * aw_power(e[1]) : s.b2;
+    float top[2] = {0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < AW_EACH; ++k) {
+        aw_element(s, b1, b2, g[k], m[k], v[k], p[k]);
+        if (PACKED && (k & 1)) top[0] = aw_largest(top[0], m[k - 1], m[k]), top[1] = aw_largest(top[1], v[k - 1], v[k]);
+    }
+    if constexpr (PACKED) {
+        e[0] = aw_exponent(top[0]), e[1] = aw_exponent(top[1]);
+        aw_round<APART>(m, v, aw_inverse(e[0]), aw_inverse(e[1]), hash, codes);
+        if (e[0] == 255) codes[0] = make_uint2(0, 0);
+        if (e[1] == 255) codes[1] = make_uint2(0, 0);
+    }
+}
+
+// A whole block whose addresses allow eight neighbouring elements per lane.
+template <bool PACKED, bool WIDE_P, bool WIDE_G>
+__device__ __forceinline__ void aw_whole_block(const AwTensor &t, const AdamwScalars &s, const AwInput<PACKED, WIDE_P, WIDE_G> &in, int64_t at, unsigned hash,
+                                               unsigned (&e)[2]) {
+    float p[8], g[8], m[8], v[8];
+    uint2 codes[2];
+    if constexpr (PACKED) {
+        aw_values_of<AW_CODES_M, true>(make_uint2(in.m.x[0], in.m.x[1]), m);
+        aw_values_of<AW_CODES_V, false>(make_uint2(in.v.x[0], in.v.x[1]), v);
+    } else {
+        aw_unpack<true>(m, in.m, false);
+        aw_unpack<true>(v, in.v, false);
+    }
+    aw_unpack<WIDE_P>(p, in.p, t.param_type == QGBDT_BF16);
+    aw_unpack<WIDE_G>(g, in.g, t.grad_type == QGBDT_BF16);
+    aw_eight<PACKED, 0>(s, p, g, m, v, hash, e, codes);
+    aw_write<WIDE_P>(t.param, at, p, t.param_type == QGBDT_BF16);
+    if (t.copy) {
+        if (t.copy_type == QGBDT_F32) aw_write<true>(t.copy, at, p, false);
+        else aw_write<false>(t.copy, at, p, t.copy_type == QGBDT_BF16);
+    }
+    if constexpr (PACKED) {
+        *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(t.m) + at) = codes[0];
+        *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(t.v) + at) = codes[1];
+    } else {
+        aw_write<true>(t.m, at, m, false);
+        aw_write<true>(t.v, at, v, false);
+    }
+}
+
+// Any other block, of n elements: a lane has every 32nd, from its own on.
+template <bool PACKED>
+__device__ __forceinline__ void aw_ragged_block(const AwTensor &t, const AdamwScalars &s, int64_t at, int n, unsigned hash, unsigned (&e)[2]) {
+    float p[8], g[8], m[8], v[8];
+    uint2 codes[2] = {};
+#pragma unroll
+    for (int k = 0; k < AW_EACH; ++k) {
+        p[k] = g[k] = m[k] = v[k] = 0.f;
+        if (32 * k >= n) continue;
+        const int64_t i = at + 32 * k;
+        p[k] = aw_load(t.param, t.param_type, i);
+        g[k] = aw_load(t.grad, t.grad_type, i);
+        if constexpr (PACKED) {
+            (k < 4 ? codes[0].x : codes[0].y) |= (unsigned)reinterpret_cast<const uint8_t *>(t.m)[i] << (k & 3) * 8;
+            (k < 4 ? codes[1].x : codes[1].y) |= (unsigned)reinterpret_cast<const uint8_t *>(t.v)[i] << (k & 3) * 8;
+        } else {
+            m[k] = reinterpret_cast<const float *>(t.m)[i], v[k] = reinterpret_cast<const float *>(t.v)[i];
+        }
+    }
+    if constexpr (PACKED) {
+        aw_values_of<AW_CODES_M, true>(codes[0], m);
+        aw_values_of<AW_CODES_V, false>(codes[1], v);
+    }
+    aw_eight<PACKED, 5>(s, p, g, m, v, hash, e, codes);
+#pragma unroll
+    for (int k = 0; k < AW_EACH; ++k) {
+        if (32 * k >= n) continue;
+        const int64_t i = at + 32 * k;
+        aw_store(t.param, t.param_type, i, p[k]);
+        if (t.copy) aw_store(t.copy, t.copy_type, i, p[k]);
+        if constexpr (PACKED) {
+            reinterpret_cast<uint8_t *>(t.m)[i] = (uint8_t)((k < 4 ? codes[0].x : codes[0].y) >> (k & 3) * 8);
+            reinterpret_cast<uint8_t *>(t.v)[i] = (uint8_t)((k < 4 ? codes[1].x : codes[1].y) >> (k & 3) * 8);
+        } else {
+            reinterpret_cast<float *>(t.m)[i] = m[k], reinterpret_cast<float *>(t.v)[i] = v[k];
+        }
+    }
+}
+
+// The first blocks of a run, the whole ones; `held`: the run's exponents, a byte per lane (replaced); `number`: of the first block.
+template <bool PACKED, bool WIDE_P, bool WIDE_G>
+__device__ __forceinline__ void aw_whole_blocks(const AwTensor &t, const AdamwScalars &s, int64_t at, int whole, unsigned number, int lane, unsigned &held) {
+    at += lane * AW_EACH;
+    AwInput<PACKED, WIDE_P, WIDE_G> next;
+    if (PACKED) next.read(t, at);
+#pragma unroll 1
+    for (int k = 0; k < whole; ++k, at += AW_BLOCK) {
+        unsigned e[2] = {};
+        if constexpr (PACKED) {
+            const unsigned key = aw_mix(s.key ^ (number + k));
+            e[0] = __shfl_sync(0xffffffffu, held, 2 * k), e[1] = __shfl_sync(0xffffffffu, held, 2 * k + 1);
+            const AwInput<PACKED, WIDE_P, WIDE_G> now = next;
+            if (k + 1 < whole) next.read(t, at + AW_BLOCK);   // under this block's work
+            aw_whole_block<PACKED, WIDE_P, WIDE_G>(t, s, now, at, key ^ (lane * AW_EACH), e);
+            held = lane == 2 * k ? e[0] : lane == 2 * k + 1 ? e[1] : held;
+        } else {
+            next.read(t, at);   // four times the bytes in flight as it is
+            aw_whole_block<PACKED, WIDE_P, WIDE_G>(t, s, next, at, 0, e);
+        }
+    }
+}
+
+// A warp takes `per` (AW_RUN at most) neighbouring blocks of 256 at a time.  Their exponents are read together and written
+// together, a byte per lane: single ones would have warps wait for one another's sectors.
+constexpr int AW_RUN = 16;
+
 template <int CAP, bool PACKED>
-__global__ void __launch_bounds__(AW_THREADS) k_adamw(const __grid_constant__ AdamwTable<CAP> t, const __grid_constant__ AdamwFactors f, int per) {
+__global__ void __launch_bounds__(AW_THREADS<PACKED>, AW_RESIDENT<PACKED>) k_adamw(const __grid_constant__ AdamwTable<CAP> t, const __grid_constant__ AdamwFactors f, int per) {
     qg_after_prior();
     __shared__ AdamwScalars scalars;
     __shared__ bool fine;
-    if (f.d_norm || f.d_lr || f.d_step) {
-        if (threadIdx.x == 0) scalars = f.s, fine = aw_scalars(f, scalars);
-        __syncthreads();
-        if (!fine) return;
-    } else {
-        if (threadIdx.x == 0) scalars = f.s;
-        __syncthreads();
+    if (threadIdx.x == 0) {
+        scalars = f.s;
+        fine = !(f.d_norm || f.d_lr || f.d_step) || aw_scalars(f, scalars);
     }
+    __syncthreads();
+    if (!fine) return;
     const AdamwScalars s = scalars;
-    const int lane = threadIdx.x & 31;
-    for (unsigned unit = blockIdx.x * AW_WARPS + (threadIdx.x >> 5); unit * (unsigned)per < t.blocks; unit += gridDim.x * AW_WARPS) {
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);   // (so that the compiler sees one for all lanes)
+    constexpr int warps = AW_THREADS<PACKED> / 32;
+    for (unsigned unit = blockIdx.x * warps + warp; unit * (unsigned)per < t.blocks; unit += gridDim.x * warps) {
         unsigned block = unit * per;
         const unsigned end = min(t.blocks, block + per);
-        int i = aw_find(t, block);
-        for (; block < end; ++block) {
-            while (i + 1 < t.n && t.first[i + 1] <= block) ++i;
-            const int what = (int)(t.count[i] >> 48), param_type = what & 3, grad_type = what >> 2 & 3, copy_type = what >> 4 & 3;
-            const int64_t base = (int64_t)(block - t.first[i]) * AW_BLOCK, left = (t.count[i] & ((1ll << 48) - 1)) - base;
-            const int n = left < AW_BLOCK ? (int)left : AW_BLOCK;
-            const bool vectors = (what & 64) && n == AW_BLOCK;
-            const int64_t at = base + (vectors ? lane * AW_EACH : lane);
-            void *const param = t.param[i], *const copy = t.copy[i], *const pm = t.m[i], *const pv = t.v[i];
-            uint8_t *const exponents = t.exponents[i] + base / AW_BLOCK * 2;
-            float p[AW_EACH], g[AW_EACH], m[AW_EACH], v[AW_EACH];
-            uint2 codes[2] = {};
-            float power[2] = {};
-            if constexpr (PACKED) power[0] = aw_power(exponents[0]), power[1] = aw_power(exponents[1]);
-            if (vectors) {
-                AwRaw rp, rg, rm, rv;
-                aw_read(rp, param, param_type, at);
-                aw_read(rg, t.grad[i], grad_type, at);
-                if constexpr (PACKED) {
-                    codes[0] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(pm) + at);
-                    codes[1] = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(pv) + at);
+        for (int i = aw_find(t, block); block < end; ++i) {
+            const int run = (int)((i + 1 < t.n ? min(end, t.first[i + 1]) : end) - block);   // of this tensor's blocks
+            const int what = (int)(t.count[i] >> 48);
+            const AwTensor one{t.param[i], t.copy[i], t.m[i], t.v[i], t.grad[i], what & 3, what >> 2 & 3, what >> 4 & 3};
+            const int64_t at = (int64_t)(block - t.first[i]) * AW_BLOCK, count = (t.count[i] & ((1ll << 48) - 1)) - at;
+            const int whole = !(what & 64) ? 0 : count >= (int64_t)run * AW_BLOCK ? run : (int)(count / AW_BLOCK);
+            uint8_t *const exponents = t.exponents[i] + at / AW_BLOCK * 2 + lane;
+            unsigned held = PACKED && lane < 2 * run ? *exponents : 0;
+            const unsigned number = t.number + block;
+            if (whole > 0) {
+                if (one.param_type == QGBDT_F32) {
+                    if (one.grad_type == QGBDT_F32) aw_whole_blocks<PACKED, true, true>(one, s, at, whole, number, lane, held);
+                    else aw_whole_blocks<PACKED, true, false>(one, s, at, whole, number, lane, held);
                 } else {
-                    aw_read32(rm, reinterpret_cast<const float *>(pm) + at);
-                    aw_read32(rv, reinterpret_cast<const float *>(pv) + at);
-                    aw_unpack(m, rm, QGBDT_F32);
-                    aw_unpack(v, rv, QGBDT_F32);
-                }
-                aw_unpack(p, rp, param_type);
-                aw_unpack(g, rg, grad_type);
-            } else {
-#pragma unroll
-                for (int k = 0; k < AW_EACH; ++k) {
-                    p[k] = g[k] = m[k] = v[k] = 0.f;
-                    if (lane + 32 * k >= n) continue;
-                    p[k] = aw_load(param, param_type, at + 32 * k);
-                    g[k] = aw_load(t.grad[i], grad_type, at + 32 * k);
-                    if constexpr (PACKED) {
-                        (k < 4 ? codes[0].x : codes[0].y) |= (unsigned)reinterpret_cast<const uint8_t *>(pm)[at + 32 * k] << (k & 3) * 8;
-                        (k < 4 ? codes[1].x : codes[1].y) |= (unsigned)reinterpret_cast<const uint8_t *>(pv)[at + 32 * k] << (k & 3) * 8;
-                    } else {
-                        m[k] = reinterpret_cast<const float *>(pm)[at + 32 * k];
-                        v[k] = reinterpret_cast<const float *>(pv)[at + 32 * k];
-                    }
+                    if (one.grad_type == QGBDT_F32) aw_whole_blocks<PACKED, false, true>(one, s, at, whole, number, lane, held);
+                    else aw_whole_blocks<PACKED, false, false>(one, s, at, whole, number, lane, held);
                 }
             }
-            unsigned top[2] = {0, 0};
-#pragma unroll
-            for (int k = 0; k < AW_EACH; ++k) {
-                if constexpr (PACKED) {
-                    const unsigned cm = (k < 4 ? codes[0].x : codes[0].y) >> (k & 3) * 8, cv = (k < 4 ? codes[1].x : codes[1].y) >> (k & 3) * 8 & 255;
-                    m[k] = aw_decode(cm & 127, AW_CODES_M, power[0]);
-                    m[k] = __uint_as_float(__float_as_uint(m[k]) | (cm & 128) << 24);
-                    v[k] = aw_decode(cv, AW_CODES_V, power[1]);
-                }
-                aw_element(s, g[k], m[k], v[k], p[k]);
-                if constexpr (PACKED) {
-                    top[0] = max(top[0], __float_as_uint(fabsf(m[k])));
-                    top[1] = max(top[1], __float_as_uint(fabsf(v[k])));
-                }
+#pragma unroll 1
+            for (int k = whole; k < run; ++k) {
+                unsigned e[2] = {};
+                if constexpr (PACKED) e[0] = __shfl_sync(0xffffffffu, held, 2 * k), e[1] = __shfl_sync(0xffffffffu, held, 2 * k + 1);
+                const int64_t left = count - (int64_t)k * AW_BLOCK;
+                aw_ragged_block<PACKED>(one, s, at + (int64_t)k * AW_BLOCK + lane, (left < AW_BLOCK ? (int)left : AW_BLOCK) - lane, aw_mix(s.key ^ (number + k)) ^ lane, e);
+                if constexpr (PACKED) held = lane == 2 * k ? e[0] : lane == 2 * k + 1 ? e[1] : held;
             }
-            if constexpr (PACKED) {
-                const unsigned key = aw_mix(s.key ^ (t.number + block));
-                const unsigned e[2] = {aw_exponent(top[0]), aw_exponent(top[1])};
-                const float inverse[2] = {aw_inverse(e[0]), aw_inverse(e[1])};
-                codes[0] = codes[1] = make_uint2(0, 0);
-#pragma unroll
-                for (int k = 0; k < AW_EACH; ++k) {
-                    const unsigned r = aw_mix(key ^ (unsigned)(vectors ? lane * AW_EACH + k : lane + 32 * k));
-                    unsigned cm = aw_encode<false>(fabsf(m[k]) * inverse[0], AW_CODES_M, r >> 16);
-                    if (cm && m[k] < 0.f) cm |= 128;
-                    const unsigned cv = aw_encode<true>(v[k] * inverse[1], AW_CODES_V, r & 0xffffu);
-                    (k < 4 ? codes[0].x : codes[0].y) |= cm << (k & 3) * 8;
-                    (k < 4 ? codes[1].x : codes[1].y) |= cv << (k & 3) * 8;
-                }
-                if (e[0] == 255) codes[0] = make_uint2(0, 0);
-                if (e[1] == 255) codes[1] = make_uint2(0, 0);
-                if (lane == 0) exponents[0] = (uint8_t)e[0], exponents[1] = (uint8_t)e[1];
-            }
-            if (vectors) {
-                aw_write(param, param_type, at, p);
-                if (copy) aw_write(copy, copy_type, at, p);
-                if constexpr (PACKED) {
-                    *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(pm) + at) = codes[0];
-                    *reinterpret_cast<uint2 *>(reinterpret_cast<uint8_t *>(pv) + at) = codes[1];
-                } else {
-                    aw_write(pm, QGBDT_F32, at, m);
-                    aw_write(pv, QGBDT_F32, at, v);
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < AW_EACH; ++k) {
-                    if (lane + 32 * k >= n) continue;
-                    aw_store(param, param_type, at + 32 * k, p[k]);
-                    if (copy) aw_store(copy, copy_type, at + 32 * k, p[k]);
-                    if constexpr (PACKED) {
-                        reinterpret_cast<uint8_t *>(pm)[at + 32 * k] = (uint8_t)((k < 4 ? codes[0].x : codes[0].y) >> (k & 3) * 8);
-                        reinterpret_cast<uint8_t *>(pv)[at + 32 * k] = (uint8_t)((k < 4 ? codes[1].x : codes[1].y) >> (k & 3) * 8);
-                    } else {
-                        reinterpret_cast<float *>(pm)[at + 32 * k] = m[k];
-                        reinterpret_cast<float *>(pv)[at + 32 * k] = v[k];
-                    }
-                }
-            }
+            if (PACKED && lane < 2 * run) *exponents = (uint8_t)held;
+            block += run;
         }
     }
 }
 
 // What packed states stand for.  Of the table: m, v and exponents as above, param and copy for the values of m and v.
 template <int CAP>
-__global__ void __launch_bounds__(AW_THREADS) k_adamw_values(const __grid_constant__ AdamwTable<CAP> t, int per) {
+__global__ void __launch_bounds__(AW_THREADS<false>) k_adamw_values(const __grid_constant__ AdamwTable<CAP> t, int per) {
     qg_after_prior();
     const int lane = threadIdx.x & 31;
-    for (unsigned unit = blockIdx.x * AW_WARPS + (threadIdx.x >> 5); unit * (unsigned)per < t.blocks; unit += gridDim.x * AW_WARPS) {
+    constexpr int warps = AW_THREADS<false> / 32;
+    for (unsigned unit = blockIdx.x * warps + __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0); unit * (unsigned)per < t.blocks; unit += gridDim.x * warps) {
         unsigned block = unit * per;
         const unsigned end = min(t.blocks, block + per);
-        int i = aw_find(t, block);
-        for (; block < end; ++block) {
-            while (i + 1 < t.n && t.first[i + 1] <= block) ++i;
+        for (int i = aw_find(t, block); block < end; ++i) {
+            const int run = (int)((i + 1 < t.n ? min(end, t.first[i + 1]) : end) - block);
             const int what = (int)(t.count[i] >> 48), type = what & 3;
-            const int64_t base = (int64_t)(block - t.first[i]) * AW_BLOCK, left = (t.count[i] & ((1ll << 48) - 1)) - base;
-            const int n = left < AW_BLOCK ? (int)left : AW_BLOCK;
             const uint8_t *const pm = reinterpret_cast<const uint8_t *>(t.m[i]), *const pv = reinterpret_cast<const uint8_t *>(t.v[i]);
-            const float power[2] = {aw_power(t.exponents[i][base / AW_BLOCK * 2]), aw_power(t.exponents[i][base / AW_BLOCK * 2 + 1])};
-            if ((what & 64) && n == AW_BLOCK) {
-                const int64_t at = base + lane * AW_EACH;
-                const uint2 cm = *reinterpret_cast<const uint2 *>(pm + at), cv = *reinterpret_cast<const uint2 *>(pv + at);
+            int64_t at = (int64_t)(block - t.first[i]) * AW_BLOCK;
+            const int64_t count = (t.count[i] & ((1ll << 48) - 1)) - at;
+            const unsigned held = lane < 2 * run ? t.exponents[i][at / AW_BLOCK * 2 + lane] : 0;
+#pragma unroll 2
+            for (int k = 0; k < run; ++k, at += AW_BLOCK) {
+                const int64_t left = count - (int64_t)k * AW_BLOCK;
+                const int n = left < AW_BLOCK ? (int)left : AW_BLOCK;
+                const bool vectors = (what & 64) && n == AW_BLOCK;
+                const int64_t mine = at + (vectors ? lane * AW_EACH : lane);
+                uint2 codes[2] = {};
                 float m[AW_EACH], v[AW_EACH];
+                if (vectors) {
+                    codes[0] = *reinterpret_cast<const uint2 *>(pm + mine), codes[1] = *reinterpret_cast<const uint2 *>(pv + mine);
+                } else {
 #pragma unroll
-                for (int k = 0; k < AW_EACH; ++k) {
-                    const unsigned one = (k < 4 ? cm.x : cm.y) >> (k & 3) * 8;
-                    m[k] = aw_decode(one & 127, AW_CODES_M, power[0]);
-                    m[k] = __uint_as_float(__float_as_uint(m[k]) | (one & 128) << 24);
-                    v[k] = aw_decode((k < 4 ? cv.x : cv.y) >> (k & 3) * 8 & 255, AW_CODES_V, power[1]);
+                    for (int j = 0; j < AW_EACH; ++j) {
+                        if (lane + 32 * j >= n) continue;
+                        (j < 4 ? codes[0].x : codes[0].y) |= (unsigned)pm[mine + 32 * j] << (j & 3) * 8;
+                        (j < 4 ? codes[1].x : codes[1].y) |= (unsigned)pv[mine + 32 * j] << (j & 3) * 8;
+                    }
                 }
-                aw_write(t.param[i], type, at, m);
-                aw_write(t.copy[i], type, at, v);
-            } else {
-                for (int j = lane; j < n; j += 32) {
-                    const unsigned one = pm[base + j];
-                    const float m = aw_decode(one & 127, AW_CODES_M, power[0]);
-                    aw_store(t.param[i], type, base + j, __uint_as_float(__float_as_uint(m) | (one & 128) << 24));
-                    aw_store(t.copy[i], type, base + j, aw_decode(pv[base + j], AW_CODES_V, power[1]));
+                aw_values_of<AW_CODES_M, true>(codes[0], m);
+                aw_values_of<AW_CODES_V, false>(codes[1], v);
+                const float power[2] = {aw_power(__shfl_sync(0xffffffffu, held, 2 * k)), aw_power(__shfl_sync(0xffffffffu, held, 2 * k + 1))};
+#pragma unroll
+                for (int j = 0; j < AW_EACH; ++j) m[j] *= power[0], v[j] *= power[1];
+                if (vectors) {
+                    if (type == QGBDT_F32) aw_write<true>(t.param[i], mine, m, false), aw_write<true>(t.copy[i], mine, v, false);
+                    else aw_write<false>(t.param[i], mine, m, true), aw_write<false>(t.copy[i], mine, v, true);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < AW_EACH; ++j) {
+                        if (lane + 32 * j >= n) continue;
+                        aw_store(t.param[i], type, mine + 32 * j, m[j]);
+                        aw_store(t.copy[i], type, mine + 32 * j, v[j]);
+                    }
                 }
             }
+            block += run;
         }
     }
 }
@@ -381,18 +528,19 @@ void aw_fill(AdamwTable<CAP> &t, int32_t &at, int64_t &done, int32_t n, unsigned
 // Whether lanes may read and write eight neighbouring elements of `width` bytes at once.
 bool aw_whole(const void *p, int64_t width) { return qg_aligned(p, (int)(8 * width)); }
 
-// Blocks of 256 that a warp takes at a time (it looks for its tensor once for all of them): four where every warp of the GPU has
-// that many, one else.  And the grid: what fits on the GPU at once, so that the work in front of the first block is done once.
+// The grid is what fits on the GPU at once, so that the work in front of the first block is done once.  A warp takes up to AW_RUN
+// neighbouring blocks of 256 at a time, as many as let all warps end with the same number of turns.
 template <typename K>
-int aw_grid(qgbdt_ctx *c, K kernel, unsigned blocks, int *per, unsigned *grid) {
+int aw_grid(qgbdt_ctx *c, K kernel, int threads, unsigned blocks, int *per, unsigned *grid) {
+    const unsigned each = threads / 32;   // warps
     *per = 1;
-    *grid = (blocks + AW_WARPS - 1) / AW_WARPS;
+    *grid = (blocks + each - 1) / each;
     if (*grid <= (unsigned)c->sm_count) return QGBDT_OK;
-    int each = 0;
-    QG_CUDA(c, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, AW_THREADS, 0));
-    const unsigned most = (unsigned)(each * c->sm_count);
-    *per = blocks >= most * AW_WARPS * 4 ? 4 : 1;
-    const unsigned want = (blocks + AW_WARPS * *per - 1) / (AW_WARPS * *per);
+    int resident = 0;
+    QG_CUDA(c, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&resident, kernel, threads, 0));
+    const unsigned most = (unsigned)(resident * c->sm_count), warps = most * each, turns = (blocks + warps * AW_RUN - 1) / (warps * AW_RUN);
+    *per = (int)((blocks + warps * turns - 1) / (warps * turns));
+    const unsigned want = (blocks + each * *per - 1) / (each * *per);
     *grid = want < most ? want : most;
     return QGBDT_OK;
 }
@@ -421,8 +569,8 @@ int aw_run(qgbdt_ctx *c, const qgbdt_adamw_tensor *in, int32_t n, const AdamwFac
         if (t.blocks == 0) continue;
         int per;
         unsigned grid;
-        QG_RUN(aw_grid(c, k_adamw<CAP, PACKED>, t.blocks, &per, &grid));
-        QG_RUN(qg_launch(c, k_adamw<CAP, PACKED>, dim3(grid), AW_THREADS, 0, st, t, f, per));
+        QG_RUN(aw_grid(c, k_adamw<CAP, PACKED>, AW_THREADS<PACKED>, t.blocks, &per, &grid));
+        QG_RUN(qg_launch(c, k_adamw<CAP, PACKED>, dim3(grid), AW_THREADS<PACKED>, 0, st, t, f, per));
     }
     return QGBDT_OK;
 }
@@ -447,8 +595,8 @@ int aw_values(qgbdt_ctx *c, const uint8_t *const *m, const uint8_t *const *v, co
         if (t.blocks == 0) continue;
         int per;
         unsigned grid;
-        QG_RUN(aw_grid(c, k_adamw_values<CAP>, t.blocks, &per, &grid));
-        QG_RUN(qg_launch(c, k_adamw_values<CAP>, dim3(grid), AW_THREADS, 0, st, t, per));
+        QG_RUN(aw_grid(c, k_adamw_values<CAP>, AW_THREADS<false>, t.blocks, &per, &grid));
+        QG_RUN(qg_launch(c, k_adamw_values<CAP>, dim3(grid), AW_THREADS<false>, 0, st, t, per));
     }
     return QGBDT_OK;
 }
@@ -457,15 +605,17 @@ int aw_values(qgbdt_ctx *c, const uint8_t *const *m, const uint8_t *const *v, co
 
 int qg_adamw(qgbdt_ctx *c, const qgbdt_adamw_tensor *t, int32_t n, const qgbdt_adamw_options &o, cudaStream_t st) {
     AdamwFactors f;
-    f.lr = o.lr, f.beta1 = o.beta1, f.beta2 = o.beta2, f.decay = o.weight_decay, f.max_norm = o.max_norm * o.loss_scale;
+    f.lr = o.lr, f.beta1 = o.beta1, f.beta2 = o.beta2, f.eps = o.eps, f.decay = o.weight_decay, f.max_norm = o.max_norm * o.loss_scale;
     f.loss_scale = o.loss_scale, f.step = o.step;
     f.seed = aw_mix(aw_mix((unsigned)o.seed) ^ (unsigned)(o.seed >> 32));
     f.d_lr = o.d_lr, f.d_step = reinterpret_cast<const long long *>(o.d_step), f.d_norm = o.d_norm;
-    f.s.coef = (float)(1.0 / o.loss_scale), f.s.eps = (float)o.eps;
+    f.s.coef = (float)(1.0 / o.loss_scale);
     f.s.b1 = (float)o.beta1, f.s.c1 = (float)(1.0 - o.beta1), f.s.b2 = (float)o.beta2, f.s.c2 = (float)(1.0 - o.beta2);
     aw_of_step(f.s, f, o.d_lr ? 0.0 : o.lr, o.d_step ? 1 : o.step);
-    if (o.state_bits == 8) return n <= AW_SMALL ? aw_run<AW_SMALL, true>(c, t, n, f, st) : aw_run<AW_LARGE, true>(c, t, n, f, st);
-    return n <= AW_SMALL ? aw_run<AW_SMALL, false>(c, t, n, f, st) : aw_run<AW_LARGE, false>(c, t, n, f, st);
+    const bool packed = o.state_bits == 8;
+    if (n <= AW_SMALL) return packed ? aw_run<AW_SMALL, true>(c, t, n, f, st) : aw_run<AW_SMALL, false>(c, t, n, f, st);
+    if (n <= AW_MEDIUM) return packed ? aw_run<AW_MEDIUM, true>(c, t, n, f, st) : aw_run<AW_MEDIUM, false>(c, t, n, f, st);
+    return packed ? aw_run<AW_LARGE, true>(c, t, n, f, st) : aw_run<AW_LARGE, false>(c, t, n, f, st);
 }
 
 int qg_adamw_values(qgbdt_ctx *c, const uint8_t *const *m, const uint8_t *const *v, const uint8_t *const *exponents, void *const *out_m,
