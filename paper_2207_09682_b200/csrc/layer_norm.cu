@@ -170,6 +170,194 @@ __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a,
     }
 }
 
+// ---- rows that fit in registers ---------------------------------------------------------------------
+// `lanes` threads have a row: a power of two up to 32, or whole warps; thread g has the vectors g, g + lanes, ... of V
+// elements, N of them.  What belongs to the columns stays in registers over all rows of the group, and the next row is
+// loaded under this one's work.
+
+// Elements of a row per thread and threads of a row, at most; single elements take more registers each.
+template <int V>
+constexpr int LN_EACH = V == 1 ? 8 : 16;
+template <int V>
+constexpr int LN_MOST = V == 1 ? 1024 : 512;
+constexpr int LN_ROW = 8192;     // the product of the two
+
+// Sum over the threads of a row, the same in all of them, in a fixed order.  More than a warp: through shared memory, `at`
+// alternating between two places, so that one barrier per sum is enough; `barrier` is the group's own.
+template <bool MULTI, typename F>
+__device__ __forceinline__ F ln_row_sum(F s, int lanes, F (*part)[32], int &at, int barrier) {
+    constexpr int words = sizeof(F) / 4;
+    float *v = reinterpret_cast<float *>(&s);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        if (MULTI || o < lanes) {
+#pragma unroll
+            for (int k = 0; k < words; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        }
+    }
+    if constexpr (MULTI) {
+        const int first = threadIdx.x / lanes * (lanes / 32);    // warp of the block
+        if ((threadIdx.x & 31) == 0) part[at][threadIdx.x / 32] = s;
+        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(lanes) : "memory");
+        s = F{};
+        for (int i = 0; i < lanes / 32; ++i) {
+            const F p = part[at][first + i];
+            const float *q = reinterpret_cast<const float *>(&p);
+#pragma unroll
+            for (int k = 0; k < words; ++k) v[k] += q[k];
+        }
+        at ^= 1;
+    }
+    return s;
+}
+
+template <typename T, int V, int N>
+struct LnRow {
+    OpsVec<T, V> v[N];
+    __device__ __forceinline__ void load(const void *p, int64_t at, int dim, int g, int lanes) {
+        const T *q = reinterpret_cast<const T *>(p) + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = (g + i * lanes) * V;
+            if (c < dim) v[i] = *reinterpret_cast<const OpsVec<T, V> *>(q + c);
+        }
+    }
+    __device__ __forceinline__ void store(void *p, int64_t at, int dim, int g, int lanes) const {
+        T *q = reinterpret_cast<T *>(p) + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = (g + i * lanes) * V;
+            if (c < dim) *reinterpret_cast<OpsVec<T, V> *>(q + c) = v[i];
+        }
+    }
+    __device__ __forceinline__ float get(int i) const { return OpsType<T>::load(v[i / V].v[i % V]); }
+    __device__ __forceinline__ void set(int i, float x) { v[i / V].v[i % V] = OpsType<T>::store(x); }
+};
+
+template <typename T, int V, int N, bool MULTI>
+__global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const LayerNormArgs a, int lanes) {
+    qg_after_prior();
+    __shared__ float part[2][32];
+    constexpr int E = N * V;
+    const int groups = MULTI ? 1 : blockDim.x / lanes, group = MULTI ? 0 : threadIdx.x / lanes, g = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1);
+    const int64_t stride = (int64_t)gridDim.x * groups;
+    const float per = 1.f / (float)a.dim;
+    const bool f32 = a.weight_type == QGBDT_F32;
+    int at = 0;
+    int64_t row = (int64_t)blockIdx.x * groups + group;
+    LnRow<T, V, N> x;
+    if (row < a.rows) x.load(a.x, row * a.ld_x, a.dim, g, lanes);
+    float w[E], b[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int c = (g + i / V * lanes) * V + i % V;
+        w[i] = c < a.dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
+        b[i] = c < a.dim ? ln_weight<T>(a.bias, f32, c, 0.f) : 0.f;
+    }
+    for (int64_t base = row - group; base < a.rows; base += stride, row += stride) {
+        float y[E], s = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            y[i] = (g + i / V * lanes) * V < a.dim ? x.get(i) : 0.f;
+            s += y[i];
+        }
+        if (row + stride < a.rows) x.load(a.x, (row + stride) * a.ld_x, a.dim, g, lanes);
+        const float mean = ln_row_sum<MULTI>(s, lanes, part, at, 1) * per;
+        s = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            y[i] = (g + i / V * lanes) * V < a.dim ? y[i] - mean : 0.f;
+            s = fmaf(y[i], y[i], s);
+        }
+        const float rstd = __frsqrt_rn(fmaf(ln_row_sum<MULTI>(s, lanes, part, at, 1), per, a.eps));
+        if (row >= a.rows) continue;
+        LnRow<T, V, N> out;
+#pragma unroll
+        for (int i = 0; i < E; ++i) out.set(i, fmaf(y[i] * rstd, w[i], b[i]));
+        out.store(a.out, row * a.ld_out, a.dim, g, lanes);
+        if (g == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+    }
+}
+
+// The gradients; the sums over the rows are gathered by column in registers, joined in shared memory over the block's groups and
+// written as the block's part of partial [blocks][2][dim], or, from a single block, as they are.
+template <typename T, int V, int N, bool MULTI>
+__global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
+    qg_after_prior();
+    extern __shared__ float shared[];
+    float *const weight = shared, *const joined = shared + (a.dim + 3) / 4 * 4;   // [dim], [N * V][threads]
+    __shared__ float2 part[2][32];
+    constexpr int E = N * V;
+    const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes;
+    const int64_t stride = (int64_t)gridDim.x * groups;
+    const float per = 1.f / (float)a.dim;
+    const bool f32 = a.weight_type == QGBDT_F32;
+    int at = 0;
+    int64_t row = (int64_t)blockIdx.x * groups + group;
+    LnRow<T, V, N> x, u;
+    float mean = 0.f, rstd = 0.f;
+    auto load = [&](int64_t r) {
+        x.load(a.x, r * a.ld_x, a.dim, g, lanes);
+        u.load(a.grad, r * a.ld_grad, a.dim, g, lanes);
+        mean = a.mean[r], rstd = a.rstd[r];
+    };
+    if (row < a.rows) load(row);
+    for (int c = threadIdx.x; c < a.dim; c += blockDim.x) weight[c] = ln_weight<T>(a.weight, f32, c, 1.f);
+    __syncthreads();
+    float dw[E] = {}, db[E] = {};
+    for (int64_t base = row - group; base < a.rows; base += stride, row += stride) {
+        float xh[E], y[E];
+        float2 s = make_float2(0.f, 0.f);
+        const float r = rstd;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int c = (g + k * lanes) * V;
+            const bool in = c < a.dim && row < a.rows;
+            OpsVec<float, V> w = {};
+            if (in) w = *reinterpret_cast<const OpsVec<float, V> *>(weight + c);
+#pragma unroll
+            for (int i = k * V; i < (k + 1) * V; ++i) {
+                xh[i] = in ? (x.get(i) - mean) * r : 0.f;
+                const float v = in ? u.get(i) : 0.f;
+                db[i] += v;
+                dw[i] = fmaf(v, xh[i], dw[i]);
+                y[i] = v * w.v[i % V];
+                s.x += y[i];
+                s.y = fmaf(y[i], xh[i], s.y);
+            }
+        }
+        if (row + stride < a.rows) load(row + stride);
+        s = ln_row_sum<MULTI>(s, lanes, part, at, 1 + group);
+        if (row >= a.rows) continue;
+        const float c1 = s.x * per, c2 = s.y * per;
+        LnRow<T, V, N> out;
+#pragma unroll
+        for (int i = 0; i < E; ++i) out.set(i, (y[i] - c1 - xh[i] * c2) * r);
+        out.store(a.out, row * a.ld_out, a.dim, g, lanes);
+    }
+    if (!a.d_weight && !a.d_bias) return;
+    for (int which = 0; which < 2; ++which) {
+        void *const final = which ? a.d_bias : a.d_weight;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < E; ++i) joined[i * blockDim.x + threadIdx.x] = which ? db[i] : dw[i];
+        __syncthreads();
+        // column c of a group: vector c / V, element c % V
+        for (int c = threadIdx.x; c < a.dim; c += blockDim.x) {
+            const int v = c / V, i = v / lanes * V + c % V;
+            float s = 0.f;
+            for (int k = 0; k < groups; ++k) s += joined[i * blockDim.x + k * lanes + v % lanes];
+            if (gridDim.x > 1) partial[((int64_t)blockIdx.x * 2 + which) * a.dim + c] = s;
+            else if (!final) continue;
+            else if (f32) reinterpret_cast<float *>(final)[c] = s;
+            else reinterpret_cast<T *>(final)[c] = OpsType<T>::store(s);
+        }
+    }
+}
+
 // ---- launches --------------------------------------------------------------------------------------
 
 // Whether rows allow vectors of 16 bytes throughout.
@@ -178,18 +366,100 @@ bool wide(const void *p, int64_t ld, const LayerNormArgs &a) {
     return !p || qg_vec_bytes(p, ld * w, (int64_t)a.dim * w) == 16;
 }
 
+// Threads of a row: one vector each up to a warp's worth, then as many vectors each as there may be, then more warps.
+template <int V>
+int ln_lanes(int dim) {
+    const int vectors = (dim + V - 1) / V;
+    if (vectors > 32) return (vectors + 32 * (LN_EACH<V> / V) - 1) / (32 * (LN_EACH<V> / V)) * 32;
+    int lanes = 1;
+    while (lanes < vectors) lanes *= 2;
+    return lanes;
+}
+
+// Blocks of `threads` that the GPU holds at once.
+template <typename K>
+int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *blocks) {
+    int each = 0;
+    QG_CUDA(c, cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, threads, smem));
+    *blocks = (int64_t)each * c->sm_count;
+    return QGBDT_OK;
+}
+
+template <typename T, int V, int N, bool MULTI>
+int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
+    const int threads = MULTI ? lanes : 128, groups = threads / lanes;
+    const int64_t want = (a.rows + groups - 1) / groups;
+    int64_t grid = want;
+    if (want > c->sm_count) {
+        QG_RUN(ln_resident(c, k_ln_rows<T, V, N, MULTI>, threads, 0, &grid));
+        if (want < grid) grid = want;
+    }
+    return qg_launch(c, k_ln_rows<T, V, N, MULTI>, dim3((unsigned)grid), threads, 0, st, a, lanes);
+}
+
+template <typename T, int V>
+int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
+    const int lanes = ln_lanes<V>(a.dim);
+    const int each = (a.dim + lanes * V - 1) / (lanes * V);
+    constexpr int most = LN_EACH<V> / V;
+    if (lanes > 32) return rows_forward<T, V, most, true>(c, a, lanes, st);
+    if (each == 1) return rows_forward<T, V, 1, false>(c, a, lanes, st);
+    if constexpr (most > 4) {
+        if (each <= 4) return rows_forward<T, V, 4, false>(c, a, lanes, st);
+    }
+    return rows_forward<T, V, most, false>(c, a, lanes, st);
+}
+
 template <typename T>
 int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
+    const bool vectors = wide(a.x, a.ld_x, a) && wide(a.out, a.ld_out, a);
+    if (a.dim <= LN_ROW) return vectors ? rows_forward<T, V>(c, a, st) : rows_forward<T, 1>(c, a, st);
     const int64_t most = (int64_t)c->sm_count * 4;
     const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
-    if (wide(a.x, a.ld_x, a) && wide(a.out, a.ld_out, a)) return qg_launch(c, k_ln_long<T, V>, grid, LN_THREADS, 0, st, a);
+    if (vectors) return qg_launch(c, k_ln_long<T, V>, grid, LN_THREADS, 0, st, a);
     return qg_launch(c, k_ln_long<T, 1>, grid, LN_THREADS, 0, st, a);
+}
+
+template <typename T, int V, int N, bool MULTI>
+int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
+    const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
+    const size_t smem = ((size_t)(a.dim + 3) / 4 * 4 + (size_t)threads * N * V) * sizeof(float);
+    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(k_ln_rows_backward<T, V, N, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    int64_t grid = 0;
+    QG_RUN(ln_resident(c, k_ln_rows_backward<T, V, N, MULTI>, threads, smem, &grid));
+    // four rows per group at least: the partial sums are as large as one and a half
+    const int64_t want = (a.rows + groups * 4 - 1) / (groups * 4);
+    if (want < grid) grid = want;
+    if (grid < 1) grid = 1;
+    const bool sums = a.d_weight || a.d_bias;
+    if (!sums || grid == 1) return qg_launch(c, k_ln_rows_backward<T, V, N, MULTI>, dim3((unsigned)grid), threads, smem, st, a, (float *)nullptr, lanes);
+    QgWorkspace ws;
+    QG_RUN(qg_ws_open(c, qg_ws_size((size_t)grid * 2 * a.dim, sizeof(float)), st, &ws));
+    float *partial = ws.take<float>((size_t)grid * 2 * a.dim);
+    QG_RUN(qg_launch(c, k_ln_rows_backward<T, V, N, MULTI>, dim3((unsigned)grid), threads, smem, st, a, partial, lanes));
+    QG_RUN(qg_launch(c, k_ln_join<T>, dim3((a.dim + 31) / 32, 2), 32 * LN_JOIN, 0, st, a, partial, (int)grid));
+    return qg_ws_close(c, st);
+}
+
+template <typename T, int V>
+int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
+    const int lanes = ln_lanes<V>(a.dim);
+    const int each = (a.dim + lanes * V - 1) / (lanes * V);
+    constexpr int most = LN_EACH<V> / V;
+    if (lanes > 32) return rows_backward<T, V, most, true>(c, a, lanes, st);
+    if (each == 1) return rows_backward<T, V, 1, false>(c, a, lanes, st);
+    if constexpr (most > 4) {
+        if (each <= 4) return rows_backward<T, V, 4, false>(c, a, lanes, st);
+    }
+    return rows_backward<T, V, most, false>(c, a, lanes, st);
 }
 
 template <typename T>
 int backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
+    const bool vectors = wide(a.x, a.ld_x, a) && wide(a.grad, a.ld_grad, a) && wide(a.out, a.ld_out, a);
+    if (a.dim <= LN_ROW) return vectors ? rows_backward<T, V>(c, a, st) : rows_backward<T, 1>(c, a, st);
     if (a.d_weight || a.d_bias) {
         // before the rows' gradients, which may take the place of an input
         const int tiles = (a.dim + 31) / 32;
@@ -207,7 +477,7 @@ int backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     if (a.rows == 0) return QGBDT_OK;
     const int64_t most = (int64_t)c->sm_count * 4;
     const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
-    if (wide(a.x, a.ld_x, a) && wide(a.grad, a.ld_grad, a) && wide(a.out, a.ld_out, a)) return qg_launch(c, k_ln_long_dx<T, V>, grid, LN_THREADS, 0, st, a);
+    if (vectors) return qg_launch(c, k_ln_long_dx<T, V>, grid, LN_THREADS, 0, st, a);
     return qg_launch(c, k_ln_long_dx<T, 1>, grid, LN_THREADS, 0, st, a);
 }
 
