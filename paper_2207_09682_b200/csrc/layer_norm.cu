@@ -175,78 +175,117 @@ __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a,
 // elements, N of them.  What belongs to the columns stays in registers over all rows of the group, and the next row is
 // loaded under this one's work.
 
-// Elements of a row per thread and threads of a row, at most; single elements take more registers each.
+// Elements of a row per thread and threads of a row, at most; narrow vectors take more registers each.
 template <int V>
-constexpr int LN_EACH = V == 1 ? 8 : 16;
+constexpr int LN_EACH = V <= 2 ? 8 : 16;
 template <int V>
-constexpr int LN_MOST = V == 1 ? 1024 : 512;
+constexpr int LN_MOST = V <= 2 ? 1024 : 512;
 constexpr int LN_ROW = 8192;     // the product of the two
 
-// Sum over the threads of a row, the same in all of them, in a fixed order.  More than a warp: through shared memory, `at`
-// alternating between two places, so that one barrier per sum is enough; `barrier` is the group's own.
-template <bool MULTI, typename F>
-__device__ __forceinline__ F ln_row_sum(F s, int lanes, F (*part)[32], int &at, int barrier) {
-    constexpr int words = sizeof(F) / 4;
-    float *v = reinterpret_cast<float *>(&s);
+__device__ __forceinline__ float ln_lanes_sum(float s, int lanes) {   // a power of two of neighbouring lanes
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        if (MULTI || o < lanes) {
-#pragma unroll
-            for (int k = 0; k < words; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        }
-    }
-    if constexpr (MULTI) {
-        const int first = threadIdx.x / lanes * (lanes / 32);    // warp of the block
-        if ((threadIdx.x & 31) == 0) part[at][threadIdx.x / 32] = s;
-        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(lanes) : "memory");
-        s = F{};
-        for (int i = 0; i < lanes / 32; ++i) {
-            const F p = part[at][first + i];
-            const float *q = reinterpret_cast<const float *>(&p);
-#pragma unroll
-            for (int k = 0; k < words; ++k) v[k] += q[k];
-        }
-        at ^= 1;
-    }
+    for (int o = 16; o; o >>= 1)
+        if (o < lanes) s += __shfl_xor_sync(0xffffffffu, s, o);
     return s;
 }
 
-template <typename T, int V, int N>
-struct LnRow {
-    OpsVec<T, V> v[N];
-    __device__ __forceinline__ void load(const void *p, int64_t at, int dim, int g, int lanes) {
+// What each warp of a row (lanes / 32 of them) has to give, handed round: lane i gets warp i's.  `at` alternates between two places
+// of the shared memory, so that one barrier is enough; `barrier` is the row's own.
+__device__ __forceinline__ float2 ln_exchange(float2 mine, int lanes, float2 (&part)[2][32], int &at, int barrier) {
+    const int first = threadIdx.x / lanes * (lanes / 32), lane = threadIdx.x & 31;
+    if (lane == 0) part[at][threadIdx.x / 32] = mine;
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(lanes) : "memory");
+    const float2 other = lane < lanes / 32 ? part[at][first + lane] : make_float2(0.f, 0.f);
+    at ^= 1;
+    return other;
+}
+
+// Lanes that `warps` warps' sums are in, as a power of two.
+__device__ __forceinline__ int ln_power(int warps) { return warps <= 1 ? 1 : 2 << (31 - __clz(warps - 1)); }
+
+// A thread's vectors of the coming rows: copied asynchronously to places of the shared memory that are the thread's own, DEPTH rows
+// ahead (so that nobody waits for another thread's copies; 64 KB and more on their way per SM, which is what the memory's latency under
+// load takes).  Vectors of 2 bytes, which such copies do not come in, are kept in registers, one row ahead.
+template <typename T, int V, int N, int DEPTH>
+struct LnRows {
+    static constexpr bool RING = sizeof(T) * V >= 4;
+    using Vec = OpsVec<T, V>;
+    static constexpr size_t bytes(int threads) { return RING ? sizeof(Vec) * N * DEPTH * threads : 0; }
+    Vec v[N];      // the row's
+    Vec next[RING ? 1 : N];
+    __device__ __forceinline__ void fetch(Vec *ring, int slot, const void *p, int64_t at, int dim, int g, int lanes) {
         const T *q = reinterpret_cast<const T *>(p) + at;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = (g + i * lanes) * V;
-            if (c < dim) v[i] = *reinterpret_cast<const OpsVec<T, V> *>(q + c);
+            if (c >= dim) continue;
+            if constexpr (RING) {
+                const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + (slot * N + i) * blockDim.x + threadIdx.x);
+                if constexpr (sizeof(Vec) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(q + c) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(q + c), "n"(sizeof(Vec)) : "memory");
+            } else {
+                next[i] = *reinterpret_cast<const Vec *>(q + c);
+            }
         }
     }
+    __device__ __forceinline__ void take(const Vec *ring, int slot) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (RING) v[i] = ring[(slot * N + i) * blockDim.x + threadIdx.x];
+            else v[i] = next[i];
+        }
+    }
+    __device__ __forceinline__ float get(int i) const { return OpsType<T>::load(v[i / V].v[i % V]); }
+    __device__ __forceinline__ void set(int i, float x) { v[i / V].v[i % V] = OpsType<T>::store(x); }
     __device__ __forceinline__ void store(void *p, int64_t at, int dim, int g, int lanes) const {
         T *q = reinterpret_cast<T *>(p) + at;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int c = (g + i * lanes) * V;
-            if (c < dim) *reinterpret_cast<OpsVec<T, V> *>(q + c) = v[i];
+            if (c < dim) *reinterpret_cast<Vec *>(q + c) = v[i];
         }
     }
-    __device__ __forceinline__ float get(int i) const { return OpsType<T>::load(v[i / V].v[i % V]); }
-    __device__ __forceinline__ void set(int i, float x) { v[i / V].v[i % V] = OpsType<T>::store(x); }
 };
+__device__ __forceinline__ void ln_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void ln_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }   // all but the last LEFT
 
+constexpr int LN_AHEAD = 4, LN_AHEAD_BACKWARD = 3;   // rows
+
+// Mean and sum of squared differences from it: over a warp in two passes; the warps' are joined by
+//   sum over warps of M2 + count (mean of the warp - mean)^2,
+// which takes one exchange and loses nothing where the mean is large beside the differences.
 template <typename T, int V, int N, bool MULTI>
 __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
-    __shared__ float part[2][32];
+    extern __shared__ __align__(16) unsigned char shared_bytes[];
+    using Rows = LnRows<T, V, N, LN_AHEAD>;
+    constexpr int AHEAD = Rows::RING ? LN_AHEAD : 1;
+    typename Rows::Vec *const ring = reinterpret_cast<typename Rows::Vec *>(shared_bytes);
+    __shared__ float2 part[2][32];
     constexpr int E = N * V;
     const int groups = MULTI ? 1 : blockDim.x / lanes, group = MULTI ? 0 : threadIdx.x / lanes, g = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1);
     const int64_t stride = (int64_t)gridDim.x * groups;
     const float per = 1.f / (float)a.dim;
     const bool f32 = a.weight_type == QGBDT_F32;
+    // elements of a row that a warp has: this one, and the one with this lane's number
+    auto elements = [&](int warp) {
+        int n = 0;
+        for (int i = 0; i < N; ++i) n += max(0, min(32, a.dim / V - warp * 32 - i * lanes)) * V;
+        return (float)n;
+    };
+    const float count = MULTI && (int)(threadIdx.x & 31) < lanes / 32 ? elements(threadIdx.x & 31) : 0.f, warp_count = MULTI ? elements(threadIdx.x / 32) : (float)a.dim;
+    const float warp_per = warp_count > 0.f ? 1.f / warp_count : 0.f;
+    const int warps = ln_power(lanes / 32);
     int at = 0;
     int64_t row = (int64_t)blockIdx.x * groups + group;
-    LnRow<T, V, N> x;
-    if (row < a.rows) x.load(a.x, row * a.ld_x, a.dim, g, lanes);
+    Rows x;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+        if (row + k * stride < a.rows) x.fetch(ring, k, a.x, (row + k * stride) * a.ld_x, a.dim, g, lanes);
+        ln_commit();
+    }
+    int slot = 0;
     float w[E], b[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) {
@@ -255,25 +294,37 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const Laye
         b[i] = c < a.dim ? ln_weight<T>(a.bias, f32, c, 0.f) : 0.f;
     }
     for (int64_t base = row - group; base < a.rows; base += stride, row += stride) {
+        ln_arrived<AHEAD - 1>();
+        x.take(ring, slot);
         float y[E], s = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
             y[i] = (g + i / V * lanes) * V < a.dim ? x.get(i) : 0.f;
             s += y[i];
         }
-        if (row + stride < a.rows) x.load(a.x, (row + stride) * a.ld_x, a.dim, g, lanes);
-        const float mean = ln_row_sum<MULTI>(s, lanes, part, at, 1) * per;
+        if (row + AHEAD * stride < a.rows) x.fetch(ring, slot, a.x, (row + AHEAD * stride) * a.ld_x, a.dim, g, lanes);
+        ln_commit();
+        slot = slot + 1 < AHEAD ? slot + 1 : 0;
+        float mean = ln_lanes_sum(s, MULTI ? 32 : lanes) * warp_per;
         s = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            y[i] = (g + i / V * lanes) * V < a.dim ? y[i] - mean : 0.f;
-            s = fmaf(y[i], y[i], s);
+            const float z = (g + i / V * lanes) * V < a.dim ? y[i] - mean : 0.f;
+            s = fmaf(z, z, s);
         }
-        const float rstd = __frsqrt_rn(fmaf(ln_row_sum<MULTI>(s, lanes, part, at, 1), per, a.eps));
+        s = ln_lanes_sum(s, MULTI ? 32 : lanes);
+        if constexpr (MULTI) {
+            const float2 other = ln_exchange(make_float2(mean, s), lanes, part, at, 1);
+            mean = ln_lanes_sum(other.x * count, warps) * per;
+            const float z = other.x - mean;
+            s = ln_lanes_sum(fmaf(z * count, z, other.y), warps);
+            if (warps < 32) mean = __shfl_sync(0xffffffffu, mean, 0), s = __shfl_sync(0xffffffffu, s, 0);
+        }
+        const float rstd = __frsqrt_rn(fmaf(s, per, a.eps));
         if (row >= a.rows) continue;
-        LnRow<T, V, N> out;
+        Rows out;
 #pragma unroll
-        for (int i = 0; i < E; ++i) out.set(i, fmaf(y[i] * rstd, w[i], b[i]));
+        for (int i = 0; i < E; ++i) out.set(i, fmaf((y[i] - mean) * rstd, w[i], b[i]));
         out.store(a.out, row * a.ld_out, a.dim, g, lanes);
         if (g == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -287,31 +338,49 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const Laye
 template <typename T, int V, int N, bool MULTI>
 __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
     qg_after_prior();
-    extern __shared__ float shared[];
-    float *const weight = shared, *const joined = shared + (a.dim + 3) / 4 * 4;   // [dim], [N * V][threads]
+    extern __shared__ __align__(16) unsigned char shared_bytes[];
+    using Rows = LnRows<T, V, N, LN_AHEAD_BACKWARD>;
+    constexpr int AHEAD = Rows::RING ? LN_AHEAD_BACKWARD : 1;
+    // weight [dim]; the coming rows of x and of the gradient, afterwards the columns' sums [N * V][threads]
+    float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + (a.dim + 3) / 4 * 4;
+    typename Rows::Vec *const ring_x = reinterpret_cast<typename Rows::Vec *>(joined), *const ring_u = ring_x + N * AHEAD * blockDim.x;
     __shared__ float2 part[2][32];
     constexpr int E = N * V;
     const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes;
     const int64_t stride = (int64_t)gridDim.x * groups;
     const float per = 1.f / (float)a.dim;
     const bool f32 = a.weight_type == QGBDT_F32;
-    int at = 0;
+    const int warps = ln_power(lanes / 32);
+    int at = 0, slot = 0;
     int64_t row = (int64_t)blockIdx.x * groups + group;
-    LnRow<T, V, N> x, u;
-    float mean = 0.f, rstd = 0.f;
-    auto load = [&](int64_t r) {
-        x.load(a.x, r * a.ld_x, a.dim, g, lanes);
-        u.load(a.grad, r * a.ld_grad, a.dim, g, lanes);
-        mean = a.mean[r], rstd = a.rstd[r];
+    Rows x, u;
+    auto fetch = [&](int to, int64_t r) {
+        if (r < a.rows) {
+            x.fetch(ring_x, to, a.x, r * a.ld_x, a.dim, g, lanes);
+            u.fetch(ring_u, to, a.grad, r * a.ld_grad, a.dim, g, lanes);
+        }
+        ln_commit();
     };
-    if (row < a.rows) load(row);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) fetch(k, row + k * stride);
+    // mean and rstd: a lane has those of one of the group's next `turns` rows, and of as many after those
+    const int turns = lanes < 32 ? lanes : 32, mine = threadIdx.x & (turns - 1);
+    float2 stats, later = make_float2(0.f, 0.f);
+    auto statistics = [&](int64_t r) { return r < a.rows ? make_float2(a.mean[r], a.rstd[r]) : make_float2(0.f, 0.f); };
+    stats = statistics(row + mine * stride);
+    int turn = 0;
     for (int c = threadIdx.x; c < a.dim; c += blockDim.x) weight[c] = ln_weight<T>(a.weight, f32, c, 1.f);
     __syncthreads();
     float dw[E] = {}, db[E] = {};
     for (int64_t base = row - group; base < a.rows; base += stride, row += stride) {
+        if (turn == 0) later = statistics(row + (mine + turns) * stride);
+        const float mean = __shfl_sync(0xffffffffu, stats.x, turn, turns), r = __shfl_sync(0xffffffffu, stats.y, turn, turns);
+        if (++turn == turns) turn = 0, stats = later;
+        ln_arrived<AHEAD - 1>();
+        x.take(ring_x, slot);
+        u.take(ring_u, slot);
         float xh[E], y[E];
         float2 s = make_float2(0.f, 0.f);
-        const float r = rstd;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
             const int c = (g + k * lanes) * V;
@@ -329,16 +398,22 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
                 s.y = fmaf(y[i], xh[i], s.y);
             }
         }
-        if (row + stride < a.rows) load(row + stride);
-        s = ln_row_sum<MULTI>(s, lanes, part, at, 1 + group);
+        fetch(slot, row + AHEAD * stride);
+        slot = slot + 1 < AHEAD ? slot + 1 : 0;
+        s.x = ln_lanes_sum(s.x, MULTI ? 32 : lanes), s.y = ln_lanes_sum(s.y, MULTI ? 32 : lanes);
+        if constexpr (MULTI) {
+            s = ln_exchange(s, lanes, part, at, 1 + group);
+            s.x = __shfl_sync(0xffffffffu, ln_lanes_sum(s.x, warps), 0), s.y = __shfl_sync(0xffffffffu, ln_lanes_sum(s.y, warps), 0);
+        }
         if (row >= a.rows) continue;
         const float c1 = s.x * per, c2 = s.y * per;
-        LnRow<T, V, N> out;
+        Rows out;
 #pragma unroll
         for (int i = 0; i < E; ++i) out.set(i, (y[i] - c1 - xh[i] * c2) * r);
         out.store(a.out, row * a.ld_out, a.dim, g, lanes);
     }
     if (!a.d_weight && !a.d_bias) return;
+    ln_arrived<0>();
     for (int which = 0; which < 2; ++which) {
         void *const final = which ? a.d_bias : a.d_weight;
         __syncthreads();
@@ -360,10 +435,17 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
 
 // ---- launches --------------------------------------------------------------------------------------
 
-// Whether rows allow vectors of 16 bytes throughout.
-bool wide(const void *p, int64_t ld, const LayerNormArgs &a) {
+// Widest vector (bytes) that the rows allow throughout.
+int common(const LayerNormArgs &a) {
     const int w = qg_type_size(a.type);
-    return !p || qg_vec_bytes(p, ld * w, (int64_t)a.dim * w) == 16;
+    int bytes = qg_vec_bytes(a.x, a.ld_x * w, (int64_t)a.dim * w);
+    const int out = qg_vec_bytes(a.out, a.ld_out * w, (int64_t)a.dim * w);
+    if (out < bytes) bytes = out;
+    if (a.grad) {
+        const int grad = qg_vec_bytes(a.grad, a.ld_grad * w, (int64_t)a.dim * w);
+        if (grad < bytes) bytes = grad;
+    }
+    return bytes;
 }
 
 // Threads of a row: one vector each up to a warp's worth, then as many vectors each as there may be, then more warps.
@@ -389,12 +471,14 @@ template <typename T, int V, int N, bool MULTI>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
     const int64_t want = (a.rows + groups - 1) / groups;
+    const size_t smem = LnRows<T, V, N, LN_AHEAD>::bytes(threads);
+    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(k_ln_rows<T, V, N, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = want;
     if (want > c->sm_count) {
-        QG_RUN(ln_resident(c, k_ln_rows<T, V, N, MULTI>, threads, 0, &grid));
+        QG_RUN(ln_resident(c, k_ln_rows<T, V, N, MULTI>, threads, smem, &grid));
         if (want < grid) grid = want;
     }
-    return qg_launch(c, k_ln_rows<T, V, N, MULTI>, dim3((unsigned)grid), threads, 0, st, a, lanes);
+    return qg_launch(c, k_ln_rows<T, V, N, MULTI>, dim3((unsigned)grid), threads, smem, st, a, lanes);
 }
 
 template <typename T, int V>
@@ -413,8 +497,15 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
 template <typename T>
 int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
-    const bool vectors = wide(a.x, a.ld_x, a) && wide(a.out, a.ld_out, a);
-    if (a.dim <= LN_ROW) return vectors ? rows_forward<T, V>(c, a, st) : rows_forward<T, 1>(c, a, st);
+    const int bytes = common(a);
+    const bool vectors = bytes == 16;
+    if (a.dim <= LN_ROW) {
+        if (vectors) return rows_forward<T, V>(c, a, st);
+        if constexpr (sizeof(T) == 2) {
+            if (bytes >= 4) return rows_forward<T, 2>(c, a, st);
+        }
+        return rows_forward<T, 1>(c, a, st);
+    }
     const int64_t most = (int64_t)c->sm_count * 4;
     const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
     if (vectors) return qg_launch(c, k_ln_long<T, V>, grid, LN_THREADS, 0, st, a);
@@ -424,7 +515,8 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
 template <typename T, int V, int N, bool MULTI>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
-    const size_t smem = ((size_t)(a.dim + 3) / 4 * 4 + (size_t)threads * N * V) * sizeof(float);
+    const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnRows<T, V, N, LN_AHEAD_BACKWARD>::bytes(threads);
+    const size_t smem = (size_t)(a.dim + 3) / 4 * 4 * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(k_ln_rows_backward<T, V, N, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = 0;
     QG_RUN(ln_resident(c, k_ln_rows_backward<T, V, N, MULTI>, threads, smem, &grid));
@@ -458,8 +550,15 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
 template <typename T>
 int backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
-    const bool vectors = wide(a.x, a.ld_x, a) && wide(a.grad, a.ld_grad, a) && wide(a.out, a.ld_out, a);
-    if (a.dim <= LN_ROW) return vectors ? rows_backward<T, V>(c, a, st) : rows_backward<T, 1>(c, a, st);
+    const int bytes = common(a);
+    const bool vectors = bytes == 16;
+    if (a.dim <= LN_ROW) {
+        if (vectors) return rows_backward<T, V>(c, a, st);
+        if constexpr (sizeof(T) == 2) {
+            if (bytes >= 4) return rows_backward<T, 2>(c, a, st);
+        }
+        return rows_backward<T, 1>(c, a, st);
+    }
     if (a.d_weight || a.d_bias) {
         // before the rows' gradients, which may take the place of an input
         const int tiles = (a.dim + 31) / 32;
