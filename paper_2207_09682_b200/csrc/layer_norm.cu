@@ -4,6 +4,8 @@
 //   xh = (x - mean) rstd,  dx = rstd (w g - sum (w g) / d - xh sum (w g xh) / d),  dw = sum over rows of g xh,  db = sum over rows of g
 //
 // Sums and statistics are held in single precision; an output is rounded once, when it is written.
+#include <type_traits>
+
 #include "ops_internal.cuh"
 
 namespace {
@@ -172,8 +174,9 @@ __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a,
 
 // ---- rows that fit in registers ---------------------------------------------------------------------
 // `lanes` threads have a row: a power of two up to 32, or whole warps; thread g has the vectors g, g + lanes, ... of V
-// elements, N of them.  What belongs to the columns stays in registers over all rows of the group, and the next row is
-// loaded under this one's work.
+// elements, N of them (EXACT: all of them inside the row).  What belongs to the columns stays in registers over all rows.
+// Instructions bound these kernels as soon as the memory does not: sums and products are taken of two elements at once,
+// and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
 
 // Elements of a row per thread and threads of a row, at most; narrow vectors take more registers each.
 template <int V>
@@ -181,12 +184,54 @@ constexpr int LN_EACH = V <= 2 ? 8 : 16;
 template <int V>
 constexpr int LN_MOST = V <= 2 ? 1024 : 512;
 constexpr int LN_ROW = 8192;     // the product of the two
+template <int E, bool MULTI>
+constexpr int LN_PAIR = !MULTI && E <= 8 ? 2 : 1;    // rows at a time
 
-__device__ __forceinline__ float ln_lanes_sum(float s, int lanes) {   // a power of two of neighbouring lanes
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<uint64_t *>(&r)) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(*reinterpret_cast<uint64_t *>(&r)) : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(*reinterpret_cast<uint64_t *>(&r))
+        : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+    return r;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Sums of K values over a power of two of neighbouring lanes, the same in all of them, in a fixed order.  Two values cost little
+// more than one: each half of the lanes takes one of them from the other half and goes on with that; then they are handed back.
+template <int K>
+__device__ __forceinline__ void ln_sum(float (&v)[K], int lanes) {
+    if constexpr (K == 1) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-        if (o < lanes) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return s;
+        for (int o = 16; o; o >>= 1)
+            if (o < lanes) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    } else {
+        if (lanes < 2) return;
+        const int half = lanes / 2;
+        const bool upper = threadIdx.x & half;
+        float w[K / 2];
+#pragma unroll
+        for (int k = 0; k < K / 2; ++k) {
+            const float give = upper ? v[k] : v[k + K / 2];
+            w[k] = (upper ? v[k + K / 2] : v[k]) + __shfl_xor_sync(0xffffffffu, give, half);
+        }
+        ln_sum<K / 2>(w, half);
+#pragma unroll
+        for (int k = 0; k < K / 2; ++k) {
+            const float other = __shfl_xor_sync(0xffffffffu, w[k], half);
+            v[k] = upper ? other : w[k];
+            v[k + K / 2] = upper ? w[k] : other;
+        }
+    }
 }
 
 // What each warp of a row (lanes / 32 of them) has to give, handed round: lane i gets warp i's.  `at` alternates between two places
@@ -203,46 +248,99 @@ __device__ __forceinline__ float2 ln_exchange(float2 mine, int lanes, float2 (&p
 // Lanes that `warps` warps' sums are in, as a power of two.
 __device__ __forceinline__ int ln_power(int warps) { return warps <= 1 ? 1 : 2 << (31 - __clz(warps - 1)); }
 
-// A thread's vectors of the coming rows: copied asynchronously to places of the shared memory that are the thread's own, DEPTH rows
-// ahead (so that nobody waits for another thread's copies; 64 KB and more on their way per SM, which is what the memory's latency under
-// load takes).  Vectors of 2 bytes, which such copies do not come in, are kept in registers, one row ahead.
-template <typename T, int V, int N, int DEPTH>
-struct LnRows {
-    static constexpr bool RING = sizeof(T) * V >= 4;
+// A thread's vectors of a row.
+template <typename T, int V, int N, bool EXACT>
+struct LnRow {
     using Vec = OpsVec<T, V>;
-    static constexpr size_t bytes(int threads) { return RING ? sizeof(Vec) * N * DEPTH * threads : 0; }
-    Vec v[N];      // the row's
-    Vec next[RING ? 1 : N];
-    __device__ __forceinline__ void fetch(Vec *ring, int slot, const void *p, int64_t at, int dim, int g, int lanes) {
-        const T *q = reinterpret_cast<const T *>(p) + at;
+    static constexpr int E = N * V, PAIRS = (E + 1) / 2;
+    Vec v[N];
+    __device__ __forceinline__ static bool in(int i, int dim, int g, int lanes) { return EXACT || (g + i * lanes) * V < dim; }   // vector i
+    __device__ __forceinline__ void load(const T *p, int dim, int g, int lanes) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = (g + i * lanes) * V;
-            if (c >= dim) continue;
+        for (int i = 0; i < N; ++i)
+            if (in(i, dim, g, lanes)) v[i] = *reinterpret_cast<const Vec *>(p + (g + i * lanes) * V);
+    }
+    __device__ __forceinline__ void store(T *p, int dim, int g, int lanes) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (in(i, dim, g, lanes)) *reinterpret_cast<Vec *>(p + (g + i * lanes) * V) = v[i];
+    }
+    __device__ __forceinline__ float one(int e) const { return OpsType<T>::load(v[e / V].v[e % V]); }
+    // elements 2 p and 2 p + 1, zero outside the row
+    __device__ __forceinline__ float2 get(int p, int dim, int g, int lanes) const {
+        float2 r = make_float2(0.f, 0.f);
+        if (in(2 * p / V, dim, g, lanes)) {
+            if constexpr (V > 1 && sizeof(T) == 2) r = two(v[2 * p / V], 2 * p % V);
+            else r.x = one(2 * p);
+        }
+        if constexpr (!(V > 1 && sizeof(T) == 2)) {
+            if (2 * p + 1 < E && in((2 * p + 1) / V, dim, g, lanes)) r.y = one(2 * p + 1);
+        }
+        return r;
+    }
+    __device__ __forceinline__ void set(int p, float2 x) {
+        if constexpr (V > 1 && sizeof(T) == 2) {
+            if constexpr (sizeof(T) == 2) pack(v[2 * p / V], 2 * p % V, x);
+        } else {
+            v[2 * p / V].v[2 * p % V] = OpsType<T>::store(x.x);
+            if (2 * p + 1 < E) v[(2 * p + 1) / V].v[(2 * p + 1) % V] = OpsType<T>::store(x.y);
+        }
+    }
+
+private:
+    __device__ __forceinline__ static float2 two(const Vec &q, int k) {
+        const unsigned w = *reinterpret_cast<const unsigned *>(&q.v[k]);
+        if constexpr (sizeof(T) == 2 && OpsType<T>::BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        else return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    }
+    __device__ __forceinline__ static void pack(Vec &q, int k, float2 x) {
+        if constexpr (OpsType<T>::BF16) *reinterpret_cast<__nv_bfloat162 *>(&q.v[k]) = __float22bfloat162_rn(x);
+        else *reinterpret_cast<__half2 *>(&q.v[k]) = __float22half2_rn(x);
+    }
+};
+
+// The coming rows of an input: copied asynchronously to places of the shared memory that are the thread's own (so that nobody waits for
+// another thread's copies), DEPTH steps of ROWS rows ahead: the memory's latency under load takes 64 KB on their way per SM.  Vectors
+// of 2 bytes, which such copies do not come in, are kept in registers, one step ahead.
+template <typename T, int V, int N, bool EXACT, int ROWS, int DEPTH>
+struct LnAhead {
+    static constexpr bool RING = sizeof(T) * V >= 4;
+    static constexpr int STEPS = RING ? DEPTH : 1;
+    using Row = LnRow<T, V, N, EXACT>;
+    using Vec = typename Row::Vec;
+    __host__ __device__ static constexpr size_t bytes(int threads) { return RING ? sizeof(Vec) * N * ROWS * DEPTH * threads : 0; }
+    const T *from;            // of the next row to be fetched
+    int64_t ld, step;         // elements
+    Vec *ring;                // the thread's first
+    Row next[RING ? 1 : ROWS];
+    __device__ __forceinline__ LnAhead(const void *p, int64_t ld_, unsigned unit, unsigned stride, void *shared)
+        : from(reinterpret_cast<const T *>(p) + (int64_t)unit * ROWS * ld_), ld(ld_), step((int64_t)stride * ROWS * ld_),
+          ring(reinterpret_cast<Vec *>(shared) + threadIdx.x) {}
+    __device__ __forceinline__ void fetch(int slot, unsigned row, unsigned rows, int dim, int g, int lanes) {
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (row + r >= rows) continue;
+            const T *const q = from + r * ld;
             if constexpr (RING) {
-                const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + (slot * N + i) * blockDim.x + threadIdx.x);
-                if constexpr (sizeof(Vec) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(q + c) : "memory");
-                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(q + c), "n"(sizeof(Vec)) : "memory");
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if (!Row::in(i, dim, g, lanes)) continue;
+                    const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + ((slot * ROWS + r) * N + i) * blockDim.x);
+                    if constexpr (sizeof(Vec) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(q + (g + i * lanes) * V) : "memory");
+                    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(q + (g + i * lanes) * V), "n"(sizeof(Vec)) : "memory");
+                }
             } else {
-                next[i] = *reinterpret_cast<const Vec *>(q + c);
+                next[r].load(q, dim, g, lanes);
             }
         }
+        from += step;
     }
-    __device__ __forceinline__ void take(const Vec *ring, int slot) {
+    __device__ __forceinline__ void take(Row &x, int slot, int r) const {
+        if constexpr (RING) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if constexpr (RING) v[i] = ring[(slot * N + i) * blockDim.x + threadIdx.x];
-            else v[i] = next[i];
-        }
-    }
-    __device__ __forceinline__ float get(int i) const { return OpsType<T>::load(v[i / V].v[i % V]); }
-    __device__ __forceinline__ void set(int i, float x) { v[i / V].v[i % V] = OpsType<T>::store(x); }
-    __device__ __forceinline__ void store(void *p, int64_t at, int dim, int g, int lanes) const {
-        T *q = reinterpret_cast<T *>(p) + at;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = (g + i * lanes) * V;
-            if (c < dim) *reinterpret_cast<Vec *>(q + c) = v[i];
+            for (int i = 0; i < N; ++i) x.v[i] = ring[((slot * ROWS + r) * N + i) * blockDim.x];
+        } else {
+            x = next[r];
         }
     }
 };
@@ -250,167 +348,218 @@ __device__ __forceinline__ void ln_commit() { asm volatile("cp.async.commit_grou
 template <int LEFT>
 __device__ __forceinline__ void ln_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }   // all but the last LEFT
 
-constexpr int LN_AHEAD = 4, LN_AHEAD_BACKWARD = 3;   // rows
+template <int ROWS>
+constexpr int LN_AHEAD = ROWS == 1 ? 4 : 2;             // steps
+template <int ROWS>
+constexpr int LN_AHEAD_BACKWARD = ROWS == 1 ? 3 : 2;
 
 // Mean and sum of squared differences from it: over a warp in two passes; the warps' are joined by
 //   sum over warps of M2 + count (mean of the warp - mean)^2,
 // which takes one exchange and loses nothing where the mean is large beside the differences.
-template <typename T, int V, int N, bool MULTI>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
-    using Rows = LnRows<T, V, N, LN_AHEAD>;
-    constexpr int AHEAD = Rows::RING ? LN_AHEAD : 1;
-    typename Rows::Vec *const ring = reinterpret_cast<typename Rows::Vec *>(shared_bytes);
     __shared__ float2 part[2][32];
-    constexpr int E = N * V;
-    const int groups = MULTI ? 1 : blockDim.x / lanes, group = MULTI ? 0 : threadIdx.x / lanes, g = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1);
-    const int64_t stride = (int64_t)gridDim.x * groups;
-    const float per = 1.f / (float)a.dim;
-    const bool f32 = a.weight_type == QGBDT_F32;
+    constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD<R>;
+    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    using Row = typename Ahead::Row;
+    constexpr int P = Row::PAIRS;
+    const int groups = MULTI ? 1 : blockDim.x / lanes, group = MULTI ? 0 : threadIdx.x / lanes, g = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1), dim = a.dim;
+    const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
+    const float per = 1.f / (float)dim;
+    unsigned unit = blockIdx.x * groups + group;
+    Ahead in(a.x, a.ld_x, unit, stride, shared_bytes);
+#pragma unroll
+    for (int k = 0; k < Ahead::STEPS; ++k) {
+        in.fetch(k, (unit + k * stride) * R, rows, dim, g, lanes);
+        ln_commit();
+    }
     // elements of a row that a warp has: this one, and the one with this lane's number
     auto elements = [&](int warp) {
         int n = 0;
-        for (int i = 0; i < N; ++i) n += max(0, min(32, a.dim / V - warp * 32 - i * lanes)) * V;
+        for (int i = 0; i < N; ++i) n += max(0, min(32, dim / V - warp * 32 - i * lanes)) * V;
         return (float)n;
     };
-    const float count = MULTI && (int)(threadIdx.x & 31) < lanes / 32 ? elements(threadIdx.x & 31) : 0.f, warp_count = MULTI ? elements(threadIdx.x / 32) : (float)a.dim;
+    const float count = MULTI && (int)(threadIdx.x & 31) < lanes / 32 ? elements(threadIdx.x & 31) : 0.f, warp_count = MULTI ? elements(threadIdx.x / 32) : (float)dim;
     const float warp_per = warp_count > 0.f ? 1.f / warp_count : 0.f;
     const int warps = ln_power(lanes / 32);
-    int at = 0;
-    int64_t row = (int64_t)blockIdx.x * groups + group;
-    Rows x;
+    const bool f32 = a.weight_type == QGBDT_F32;
+    float2 w[P], b[P];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-        if (row + k * stride < a.rows) x.fetch(ring, k, a.x, (row + k * stride) * a.ld_x, a.dim, g, lanes);
-        ln_commit();
-    }
-    int slot = 0;
-    float w[E], b[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const int c = (g + i / V * lanes) * V + i % V;
-        w[i] = c < a.dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
-        b[i] = c < a.dim ? ln_weight<T>(a.bias, f32, c, 0.f) : 0.f;
-    }
-    for (int64_t base = row - group; base < a.rows; base += stride, row += stride) {
-        ln_arrived<AHEAD - 1>();
-        x.take(ring, slot);
-        float y[E], s = 0.f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            y[i] = (g + i / V * lanes) * V < a.dim ? x.get(i) : 0.f;
-            s += y[i];
+    for (int p = 0; p < P; ++p) {
+        float *const q[2] = {&w[p].x, &b[p].x};
+        for (int k = 0; k < 2; ++k) {
+            const int e = 2 * p + k, c = (g + e / V * lanes) * V + e % V;
+            const bool is = e < E && c < dim;
+            q[0][k] = is ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
+            q[1][k] = is ? ln_weight<T>(a.bias, f32, c, 0.f) : 0.f;
         }
-        if (row + AHEAD * stride < a.rows) x.fetch(ring, slot, a.x, (row + AHEAD * stride) * a.ld_x, a.dim, g, lanes);
-        ln_commit();
-        slot = slot + 1 < AHEAD ? slot + 1 : 0;
-        float mean = ln_lanes_sum(s, MULTI ? 32 : lanes) * warp_per;
-        s = 0.f;
+    }
+    T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
+    const int64_t out_step = (int64_t)stride * R * a.ld_out;
+    int at = 0, slot = 0;
+    for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
+        ln_arrived<Ahead::STEPS - 1>();
+        float2 y[R][P];
+        float s[R], mean[R];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float z = (g + i / V * lanes) * V < a.dim ? y[i] - mean : 0.f;
-            s = fmaf(z, z, s);
+        for (int r = 0; r < R; ++r) {
+            Row x;
+            in.take(x, slot, r);
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int p = 0; p < P; ++p) y[r][p] = x.get(p, dim, g, lanes), sum = add2(sum, y[r][p]);
+            s[r] = sum.x + sum.y;
         }
-        s = ln_lanes_sum(s, MULTI ? 32 : lanes);
+        in.fetch(slot, (unit + Ahead::STEPS * stride) * R, rows, dim, g, lanes);
+        ln_commit();
+        slot = slot + 1 < Ahead::STEPS ? slot + 1 : 0;
+        ln_sum<R>(s, MULTI ? 32 : lanes);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            mean[r] = s[r] * warp_per;
+            float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                float2 z = add2(y[r][p], both(-mean[r]));
+                if (!Row::in(2 * p / V, dim, g, lanes)) z.x = 0.f;
+                if (2 * p + 1 >= E || !Row::in((2 * p + 1) / V, dim, g, lanes)) z.y = 0.f;
+                sum = fma2(z, z, sum);
+                if (!MULTI) y[r][p] = z;
+            }
+            s[r] = sum.x + sum.y;
+        }
+        ln_sum<R>(s, MULTI ? 32 : lanes);
         if constexpr (MULTI) {
-            const float2 other = ln_exchange(make_float2(mean, s), lanes, part, at, 1);
-            mean = ln_lanes_sum(other.x * count, warps) * per;
-            const float z = other.x - mean;
-            s = ln_lanes_sum(fmaf(z * count, z, other.y), warps);
-            if (warps < 32) mean = __shfl_sync(0xffffffffu, mean, 0), s = __shfl_sync(0xffffffffu, s, 0);
+            const float2 other = ln_exchange(make_float2(mean[0], s[0]), lanes, part, at, 1);
+            float m[1] = {other.x * count};
+            ln_sum<1>(m, warps);
+            mean[0] = m[0] * per;
+            const float z = other.x - mean[0];
+            m[0] = fmaf(z * count, z, other.y);
+            ln_sum<1>(m, warps);
+            mean[0] = __shfl_sync(0xffffffffu, mean[0], 0), s[0] = __shfl_sync(0xffffffffu, m[0], 0);
         }
-        const float rstd = __frsqrt_rn(fmaf(s, per, a.eps));
-        if (row >= a.rows) continue;
-        Rows out;
 #pragma unroll
-        for (int i = 0; i < E; ++i) out.set(i, fmaf((y[i] - mean) * rstd, w[i], b[i]));
-        out.store(a.out, row * a.ld_out, a.dim, g, lanes);
-        if (g == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
+        for (int r = 0; r < R; ++r) {
+            const unsigned row = unit * R + r;
+            if (row >= rows) continue;
+            const float rstd = __frsqrt_rn(fmaf(s[r], per, a.eps));
+            Row x;
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                const float2 z = MULTI ? add2(y[r][p], both(-mean[r])) : y[r][p];
+                x.set(p, fma2(mul2(z, both(rstd)), w[p], b[p]));
+            }
+            x.store(out + r * a.ld_out, dim, g, lanes);
+            if (g == 0) {
+                if (a.mean) a.mean[row] = mean[r];
+                if (a.rstd) a.rstd[row] = rstd;
+            }
         }
     }
 }
 
 // The gradients; the sums over the rows are gathered by column in registers, joined in shared memory over the block's groups and
 // written as the block's part of partial [blocks][2][dim], or, from a single block, as they are.
-template <typename T, int V, int N, bool MULTI>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
-    using Rows = LnRows<T, V, N, LN_AHEAD_BACKWARD>;
-    constexpr int AHEAD = Rows::RING ? LN_AHEAD_BACKWARD : 1;
-    // weight [dim]; the coming rows of x and of the gradient, afterwards the columns' sums [N * V][threads]
-    float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + (a.dim + 3) / 4 * 4;
-    typename Rows::Vec *const ring_x = reinterpret_cast<typename Rows::Vec *>(joined), *const ring_u = ring_x + N * AHEAD * blockDim.x;
     __shared__ float2 part[2][32];
-    constexpr int E = N * V;
-    const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes;
-    const int64_t stride = (int64_t)gridDim.x * groups;
-    const float per = 1.f / (float)a.dim;
-    const bool f32 = a.weight_type == QGBDT_F32;
-    const int warps = ln_power(lanes / 32);
-    int at = 0, slot = 0;
-    int64_t row = (int64_t)blockIdx.x * groups + group;
-    Rows x, u;
-    auto fetch = [&](int to, int64_t r) {
-        if (r < a.rows) {
-            x.fetch(ring_x, to, a.x, r * a.ld_x, a.dim, g, lanes);
-            u.fetch(ring_u, to, a.grad, r * a.ld_grad, a.dim, g, lanes);
-        }
+    constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD_BACKWARD<R>;
+    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    using Row = typename Ahead::Row;
+    constexpr int P = Row::PAIRS;
+    const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes, dim = a.dim;
+    const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
+    const float per = 1.f / (float)dim;
+    // weight [dim]; the coming rows of x and of the gradient, afterwards the columns' sums [2 P][threads]
+    float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + (dim + 3) / 4 * 4;
+    unsigned unit = blockIdx.x * groups + group;
+    Ahead in_x(a.x, a.ld_x, unit, stride, joined), in_u(a.grad, a.ld_grad, unit, stride, reinterpret_cast<unsigned char *>(joined) + Ahead::bytes(blockDim.x));
+    auto fetch = [&](int slot, unsigned row) {
+        in_x.fetch(slot, row, rows, dim, g, lanes);
+        in_u.fetch(slot, row, rows, dim, g, lanes);
         ln_commit();
     };
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) fetch(k, row + k * stride);
-    // mean and rstd: a lane has those of one of the group's next `turns` rows, and of as many after those
+    for (int k = 0; k < Ahead::STEPS; ++k) fetch(k, (unit + k * stride) * R);
+    // mean and rstd: a lane has those of one of the group's next `turns` steps, and of as many after those
     const int turns = lanes < 32 ? lanes : 32, mine = threadIdx.x & (turns - 1);
-    float2 stats, later = make_float2(0.f, 0.f);
-    auto statistics = [&](int64_t r) { return r < a.rows ? make_float2(a.mean[r], a.rstd[r]) : make_float2(0.f, 0.f); };
-    stats = statistics(row + mine * stride);
-    int turn = 0;
-    for (int c = threadIdx.x; c < a.dim; c += blockDim.x) weight[c] = ln_weight<T>(a.weight, f32, c, 1.f);
+    float2 stats[R], later[R];
+    auto statistics = [&](float2 (&to)[R], unsigned of) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) to[r] = of * R + r < rows ? make_float2(a.mean[of * R + r], a.rstd[of * R + r]) : make_float2(0.f, 0.f);
+    };
+    statistics(stats, unit + mine * stride);
+    const bool f32 = a.weight_type == QGBDT_F32;
+    for (int c = threadIdx.x; c < dim; c += blockDim.x) weight[c] = ln_weight<T>(a.weight, f32, c, 1.f);
     __syncthreads();
-    float dw[E] = {}, db[E] = {};
-    for (int64_t base = row - group; base < a.rows; base += stride, row += stride) {
-        if (turn == 0) later = statistics(row + (mine + turns) * stride);
-        const float mean = __shfl_sync(0xffffffffu, stats.x, turn, turns), r = __shfl_sync(0xffffffffu, stats.y, turn, turns);
-        if (++turn == turns) turn = 0, stats = later;
-        ln_arrived<AHEAD - 1>();
-        x.take(ring_x, slot);
-        u.take(ring_u, slot);
-        float xh[E], y[E];
-        float2 s = make_float2(0.f, 0.f);
+    float2 dw[P] = {}, db[P] = {};
+    T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
+    const int64_t out_step = (int64_t)stride * R * a.ld_out;
+    const int warps = ln_power(lanes / 32);
+    int at = 0, slot = 0, turn = 0;
+    for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
+        if (turn == 0) statistics(later, unit + (mine + turns) * stride);
+        float2 xh[R][P], y[R][P];
+        float s[2 * R], rstd[R];
+        ln_arrived<Ahead::STEPS - 1>();
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            const int c = (g + k * lanes) * V;
-            const bool in = c < a.dim && row < a.rows;
-            OpsVec<float, V> w = {};
-            if (in) w = *reinterpret_cast<const OpsVec<float, V> *>(weight + c);
+        for (int r = 0; r < R; ++r) {
+            const float mean = __shfl_sync(0xffffffffu, stats[r].x, turn, turns);
+            rstd[r] = __shfl_sync(0xffffffffu, stats[r].y, turn, turns);
+            Row x, u;
+            in_x.take(x, slot, r);
+            in_u.take(u, slot, r);
+            const bool is = unit * R + r < rows;
+            float2 sum = make_float2(0.f, 0.f), along = sum;
 #pragma unroll
-            for (int i = k * V; i < (k + 1) * V; ++i) {
-                xh[i] = in ? (x.get(i) - mean) * r : 0.f;
-                const float v = in ? u.get(i) : 0.f;
-                db[i] += v;
-                dw[i] = fmaf(v, xh[i], dw[i]);
-                y[i] = v * w.v[i % V];
-                s.x += y[i];
-                s.y = fmaf(y[i], xh[i], s.y);
+            for (int p = 0; p < P; ++p) {
+                float2 v = u.get(p, dim, g, lanes), h = mul2(add2(x.get(p, dim, g, lanes), both(-mean)), both(rstd[r]));
+                if (!is || !Row::in(2 * p / V, dim, g, lanes)) v.x = h.x = 0.f;
+                if (!is || 2 * p + 1 >= E || !Row::in((2 * p + 1) / V, dim, g, lanes)) v.y = h.y = 0.f;
+                db[p] = add2(db[p], v);
+                dw[p] = fma2(v, h, dw[p]);
+                float2 w = make_float2(0.f, 0.f);
+                if constexpr (V > 1) {
+                    if (Row::in(2 * p / V, dim, g, lanes)) w = *reinterpret_cast<const float2 *>(weight + (g + 2 * p / V * lanes) * V + 2 * p % V);
+                } else {
+                    if (Row::in(2 * p, dim, g, lanes)) w.x = weight[g + 2 * p * lanes];
+                    if (2 * p + 1 < E && Row::in(2 * p + 1, dim, g, lanes)) w.y = weight[g + (2 * p + 1) * lanes];
+                }
+                xh[r][p] = h;
+                y[r][p] = mul2(v, w);
+                sum = add2(sum, y[r][p]);
+                along = fma2(y[r][p], h, along);
             }
+            s[2 * r] = sum.x + sum.y, s[2 * r + 1] = along.x + along.y;
         }
-        fetch(slot, row + AHEAD * stride);
-        slot = slot + 1 < AHEAD ? slot + 1 : 0;
-        s.x = ln_lanes_sum(s.x, MULTI ? 32 : lanes), s.y = ln_lanes_sum(s.y, MULTI ? 32 : lanes);
-        if constexpr (MULTI) {
-            s = ln_exchange(s, lanes, part, at, 1 + group);
-            s.x = __shfl_sync(0xffffffffu, ln_lanes_sum(s.x, warps), 0), s.y = __shfl_sync(0xffffffffu, ln_lanes_sum(s.y, warps), 0);
-        }
-        if (row >= a.rows) continue;
-        const float c1 = s.x * per, c2 = s.y * per;
-        Rows out;
+        if (++turn == turns) {
+            turn = 0;
 #pragma unroll
-        for (int i = 0; i < E; ++i) out.set(i, (y[i] - c1 - xh[i] * c2) * r);
-        out.store(a.out, row * a.ld_out, a.dim, g, lanes);
+            for (int r = 0; r < R; ++r) stats[r] = later[r];
+        }
+        fetch(slot, (unit + Ahead::STEPS * stride) * R);
+        slot = slot + 1 < Ahead::STEPS ? slot + 1 : 0;
+        ln_sum<2 * R>(s, MULTI ? 32 : lanes);
+        if constexpr (MULTI) {
+            const float2 other = ln_exchange(make_float2(s[0], s[1]), lanes, part, at, 1 + group);
+            s[0] = other.x, s[1] = other.y;
+            ln_sum<2>(s, warps);
+            s[0] = __shfl_sync(0xffffffffu, s[0], 0), s[1] = __shfl_sync(0xffffffffu, s[1], 0);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (unit * R + r >= rows) continue;
+            const float2 c1 = both(-s[2 * r] * per), c2 = both(-s[2 * r + 1] * per);
+            Row x;
+#pragma unroll
+            for (int p = 0; p < P; ++p) x.set(p, mul2(fma2(xh[r][p], c2, add2(y[r][p], c1)), both(rstd[r])));
+            x.store(out + r * a.ld_out, dim, g, lanes);
+        }
     }
     if (!a.d_weight && !a.d_bias) return;
     ln_arrived<0>();
@@ -418,14 +567,18 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
         void *const final = which ? a.d_bias : a.d_weight;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < E; ++i) joined[i * blockDim.x + threadIdx.x] = which ? db[i] : dw[i];
+        for (int p = 0; p < P; ++p) {
+            const float2 v = which ? db[p] : dw[p];
+            joined[2 * p * blockDim.x + threadIdx.x] = v.x;
+            joined[(2 * p + 1) * blockDim.x + threadIdx.x] = v.y;
+        }
         __syncthreads();
         // column c of a group: vector c / V, element c % V
-        for (int c = threadIdx.x; c < a.dim; c += blockDim.x) {
+        for (int c = threadIdx.x; c < dim; c += blockDim.x) {
             const int v = c / V, i = v / lanes * V + c % V;
             float s = 0.f;
             for (int k = 0; k < groups; ++k) s += joined[i * blockDim.x + k * lanes + v % lanes];
-            if (gridDim.x > 1) partial[((int64_t)blockIdx.x * 2 + which) * a.dim + c] = s;
+            if (gridDim.x > 1) partial[((int64_t)blockIdx.x * 2 + which) * dim + c] = s;
             else if (!final) continue;
             else if (f32) reinterpret_cast<float *>(final)[c] = s;
             else reinterpret_cast<T *>(final)[c] = OpsType<T>::store(s);
@@ -467,31 +620,42 @@ int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *block
     return QGBDT_OK;
 }
 
-template <typename T, int V, int N, bool MULTI>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
+    constexpr int R = LN_PAIR<N * V, MULTI>;
+    constexpr auto kernel = k_ln_rows<T, V, N, MULTI, EXACT>;
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
-    const int64_t want = (a.rows + groups - 1) / groups;
-    const size_t smem = LnRows<T, V, N, LN_AHEAD>::bytes(threads);
-    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(k_ln_rows<T, V, N, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const int64_t want = (a.rows + groups * R - 1) / (groups * R);
+    const size_t smem = LnAhead<T, V, N, EXACT, R, LN_AHEAD<R>>::bytes(threads);
+    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = want;
     if (want > c->sm_count) {
-        QG_RUN(ln_resident(c, k_ln_rows<T, V, N, MULTI>, threads, smem, &grid));
+        QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
         if (want < grid) grid = want;
     }
-    return qg_launch(c, k_ln_rows<T, V, N, MULTI>, dim3((unsigned)grid), threads, smem, st, a, lanes);
+    return qg_launch(c, kernel, dim3((unsigned)grid), threads, smem, st, a, lanes);
+}
+
+// How a row is cut up: calls `with` with N, MULTI and EXACT.
+template <int V, typename F>
+int rows_cut(int dim, F with) {
+    constexpr int most = LN_EACH<V> / V;
+    const int lanes = ln_lanes<V>(dim), each = (dim + lanes * V - 1) / (lanes * V);
+    auto exact = [&](auto n, auto multi) {
+        if (dim == lanes * n.value * V) return with(n, multi, std::true_type{}, lanes);
+        return with(n, multi, std::false_type{}, lanes);
+    };
+    if (lanes > 32) return exact(std::integral_constant<int, most>{}, std::true_type{});
+    if (each == 1) return exact(std::integral_constant<int, 1>{}, std::false_type{});
+    if constexpr (most > 4) {
+        if (each <= 4) return exact(std::integral_constant<int, 4>{}, std::false_type{});
+    }
+    return exact(std::integral_constant<int, most>{}, std::false_type{});
 }
 
 template <typename T, int V>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    const int lanes = ln_lanes<V>(a.dim);
-    const int each = (a.dim + lanes * V - 1) / (lanes * V);
-    constexpr int most = LN_EACH<V> / V;
-    if (lanes > 32) return rows_forward<T, V, most, true>(c, a, lanes, st);
-    if (each == 1) return rows_forward<T, V, 1, false>(c, a, lanes, st);
-    if constexpr (most > 4) {
-        if (each <= 4) return rows_forward<T, V, 4, false>(c, a, lanes, st);
-    }
-    return rows_forward<T, V, most, false>(c, a, lanes, st);
+    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
 }
 
 template <typename T>
@@ -512,39 +676,33 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     return qg_launch(c, k_ln_long<T, 1>, grid, LN_THREADS, 0, st, a);
 }
 
-template <typename T, int V, int N, bool MULTI>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
+    constexpr int R = LN_PAIR<N * V, MULTI>;
+    constexpr auto kernel = k_ln_rows_backward<T, V, N, MULTI, EXACT>;
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
-    const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnRows<T, V, N, LN_AHEAD_BACKWARD>::bytes(threads);
+    const size_t sums_bytes = (size_t)threads * ((N * V + 1) / 2 * 2) * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, R, LN_AHEAD_BACKWARD<R>>::bytes(threads);
     const size_t smem = (size_t)(a.dim + 3) / 4 * 4 * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
-    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(k_ln_rows_backward<T, V, N, MULTI>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = 0;
-    QG_RUN(ln_resident(c, k_ln_rows_backward<T, V, N, MULTI>, threads, smem, &grid));
+    QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
     // four rows per group at least: the partial sums are as large as one and a half
     const int64_t want = (a.rows + groups * 4 - 1) / (groups * 4);
     if (want < grid) grid = want;
     if (grid < 1) grid = 1;
     const bool sums = a.d_weight || a.d_bias;
-    if (!sums || grid == 1) return qg_launch(c, k_ln_rows_backward<T, V, N, MULTI>, dim3((unsigned)grid), threads, smem, st, a, (float *)nullptr, lanes);
+    if (!sums || grid == 1) return qg_launch(c, kernel, dim3((unsigned)grid), threads, smem, st, a, (float *)nullptr, lanes);
     QgWorkspace ws;
     QG_RUN(qg_ws_open(c, qg_ws_size((size_t)grid * 2 * a.dim, sizeof(float)), st, &ws));
     float *partial = ws.take<float>((size_t)grid * 2 * a.dim);
-    QG_RUN(qg_launch(c, k_ln_rows_backward<T, V, N, MULTI>, dim3((unsigned)grid), threads, smem, st, a, partial, lanes));
+    QG_RUN(qg_launch(c, kernel, dim3((unsigned)grid), threads, smem, st, a, partial, lanes));
     QG_RUN(qg_launch(c, k_ln_join<T>, dim3((a.dim + 31) / 32, 2), 32 * LN_JOIN, 0, st, a, partial, (int)grid));
     return qg_ws_close(c, st);
 }
 
 template <typename T, int V>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    const int lanes = ln_lanes<V>(a.dim);
-    const int each = (a.dim + lanes * V - 1) / (lanes * V);
-    constexpr int most = LN_EACH<V> / V;
-    if (lanes > 32) return rows_backward<T, V, most, true>(c, a, lanes, st);
-    if (each == 1) return rows_backward<T, V, 1, false>(c, a, lanes, st);
-    if constexpr (most > 4) {
-        if (each <= 4) return rows_backward<T, V, 4, false>(c, a, lanes, st);
-    }
-    return rows_backward<T, V, most, false>(c, a, lanes, st);
+    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
 }
 
 template <typename T>

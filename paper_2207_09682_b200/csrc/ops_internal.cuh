@@ -18,11 +18,13 @@ struct OpsType<float> {
 };
 template <>
 struct OpsType<__nv_bfloat16> {
+    static constexpr bool BF16 = true;
     static __device__ __forceinline__ float load(__nv_bfloat16 x) { return __bfloat162float(x); }
     static __device__ __forceinline__ __nv_bfloat16 store(float x) { return __float2bfloat16_rn(x); }
 };
 template <>
 struct OpsType<__half> {
+    static constexpr bool BF16 = false;
     static __device__ __forceinline__ float load(__half x) { return __half2float(x); }
     static __device__ __forceinline__ __half store(float x) { return __float2half_rn(x); }
 };
