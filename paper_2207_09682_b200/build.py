@@ -72,7 +72,7 @@ def build_tensors(force: bool = False) -> str:
          "-I", os.path.join(ROOT, "include"), "-isystem", os.path.join(torch_dir, "include"),
          "-isystem", os.path.join(torch_dir, "include", "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
          "-isystem", os.path.join(os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"))), "include"),
-         TENSORS_SRC, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp])
+         TENSORS_SRC, "-L", os.path.join(torch_dir, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-ltorch_cuda", "-o", tmp])
     os.replace(tmp, TENSORS)
     os.makedirs(OBJ_DIR, exist_ok=True)
     with open(TENSORS_MADE_FOR, "w") as f:

@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(32 * LN_COLUMN_ROWS) k_ln_columns(const LayerN
 }
 
 // The partial sums joined in their order: 32 columns per block, LN_JOIN parts of the slices side by side.
-constexpr int LN_JOIN = 32;
+constexpr int LN_JOIN = 32;      // (a warp's lanes)
 
 template <typename T>
 __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a, const float *partial, int slices) {
@@ -165,10 +165,13 @@ __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a,
     }
     w[part][lane] = s;
     __syncthreads();
-    if (part == 0 && c < a.dim) {
-        for (int i = 1; i < LN_JOIN; ++i) s += w[i][lane];
-        if (a.weight_type == QGBDT_F32) reinterpret_cast<float *>(out)[c] = s;
-        else reinterpret_cast<T *>(out)[c] = OpsType<T>::store(s);
+    const int64_t column = (int64_t)blockIdx.x * 32 + part;       // a warp per column
+    s = w[lane][part];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (lane == 0 && column < a.dim) {
+        if (a.weight_type == QGBDT_F32) reinterpret_cast<float *>(out)[column] = s;
+        else reinterpret_cast<T *>(out)[column] = OpsType<T>::store(s);
     }
 }
 
@@ -248,39 +251,44 @@ __device__ __forceinline__ float2 ln_exchange(float2 mine, int lanes, float2 (&p
 // Lanes that `warps` warps' sums are in, as a power of two.
 __device__ __forceinline__ int ln_power(int warps) { return warps <= 1 ? 1 : 2 << (31 - __clz(warps - 1)); }
 
-// A thread's vectors of a row.
-template <typename T, int V, int N, bool EXACT>
+// A thread's vectors of a row.  LOOSE: rows of 16-bit elements that start anywhere; vectors of two elements, the last of which may
+// lie outside the row.
+template <typename T, int V, int N, bool EXACT, bool LOOSE>
 struct LnRow {
     using Vec = OpsVec<T, V>;
     static constexpr int E = N * V, PAIRS = (E + 1) / 2;
+    static constexpr bool HALVES = V > 1 && sizeof(T) == 2;    // pairs are words
     Vec v[N];
     __device__ __forceinline__ static bool in(int i, int dim, int g, int lanes) { return EXACT || (g + i * lanes) * V < dim; }   // vector i
-    __device__ __forceinline__ void load(const T *p, int dim, int g, int lanes) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (in(i, dim, g, lanes)) v[i] = *reinterpret_cast<const Vec *>(p + (g + i * lanes) * V);
+    __device__ __forceinline__ static bool has(int e, int dim, int g, int lanes) {                                              // element e
+        return e < E && (LOOSE ? (g + e / V * lanes) * V + e % V < dim : in(e / V, dim, g, lanes));
     }
     __device__ __forceinline__ void store(T *p, int dim, int g, int lanes) const {
+        if constexpr (LOOSE) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (in(i, dim, g, lanes)) *reinterpret_cast<Vec *>(p + (g + i * lanes) * V) = v[i];
+            for (int e = 0; e < E; ++e)
+                if (has(e, dim, g, lanes)) p[(g + e / V * lanes) * V + e % V] = v[e / V].v[e % V];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (in(i, dim, g, lanes)) *reinterpret_cast<Vec *>(p + (g + i * lanes) * V) = v[i];
+        }
     }
-    __device__ __forceinline__ float one(int e) const { return OpsType<T>::load(v[e / V].v[e % V]); }
     // elements 2 p and 2 p + 1, zero outside the row
     __device__ __forceinline__ float2 get(int p, int dim, int g, int lanes) const {
         float2 r = make_float2(0.f, 0.f);
-        if (in(2 * p / V, dim, g, lanes)) {
-            if constexpr (V > 1 && sizeof(T) == 2) r = two(v[2 * p / V], 2 * p % V);
-            else r.x = one(2 * p);
-        }
-        if constexpr (!(V > 1 && sizeof(T) == 2)) {
-            if (2 * p + 1 < E && in((2 * p + 1) / V, dim, g, lanes)) r.y = one(2 * p + 1);
+        if constexpr (HALVES) {
+            if (in(2 * p / V, dim, g, lanes)) r = two(v[2 * p / V], 2 * p % V);
+            if (LOOSE && !has(2 * p + 1, dim, g, lanes)) r.y = 0.f;
+        } else {
+            if (has(2 * p, dim, g, lanes)) r.x = OpsType<T>::load(v[2 * p / V].v[2 * p % V]);
+            if (has(2 * p + 1, dim, g, lanes)) r.y = OpsType<T>::load(v[(2 * p + 1) / V].v[(2 * p + 1) % V]);
         }
         return r;
     }
     __device__ __forceinline__ void set(int p, float2 x) {
-        if constexpr (V > 1 && sizeof(T) == 2) {
-            if constexpr (sizeof(T) == 2) pack(v[2 * p / V], 2 * p % V, x);
+        if constexpr (HALVES) {
+            pack(v[2 * p / V], 2 * p % V, x);
         } else {
             v[2 * p / V].v[2 * p % V] = OpsType<T>::store(x.x);
             if (2 * p + 1 < E) v[(2 * p + 1) / V].v[(2 * p + 1) % V] = OpsType<T>::store(x.y);
@@ -290,7 +298,7 @@ struct LnRow {
 private:
     __device__ __forceinline__ static float2 two(const Vec &q, int k) {
         const unsigned w = *reinterpret_cast<const unsigned *>(&q.v[k]);
-        if constexpr (sizeof(T) == 2 && OpsType<T>::BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+        if constexpr (OpsType<T>::BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
         else return __half22float2(*reinterpret_cast<const __half2 *>(&w));
     }
     __device__ __forceinline__ static void pack(Vec &q, int k, float2 x) {
@@ -299,54 +307,89 @@ private:
     }
 };
 
-// The coming rows of an input: copied asynchronously to places of the shared memory that are the thread's own (so that nobody waits for
-// another thread's copies), DEPTH steps of ROWS rows ahead: the memory's latency under load takes 64 KB on their way per SM.  Vectors
-// of 2 bytes, which such copies do not come in, are kept in registers, one step ahead.
-template <typename T, int V, int N, bool EXACT, int ROWS, int DEPTH>
+// The coming rows of an input, copied asynchronously to the shared memory, DEPTH steps of ROWS rows ahead: the memory's latency under
+// load takes 64 KB on their way per SM.  A thread's vectors go to places of its own, so that nobody waits for another thread's copies.
+// LOOSE: such copies come in aligned words, so a row is copied as the words that hold it, by all its threads for one another, and a
+// thread's pairs are cut from two neighbouring words each.  (The word in which a row starts may hold an element of the row before it;
+// in front of the first row nothing is read, and the last word is copied as far as the row goes.)
+template <typename T, int V, int N, bool EXACT, bool LOOSE, int ROWS, int DEPTH>
 struct LnAhead {
-    static constexpr bool RING = sizeof(T) * V >= 4;
-    static constexpr int STEPS = RING ? DEPTH : 1;
-    using Row = LnRow<T, V, N, EXACT>;
+    using Row = LnRow<T, V, N, EXACT, LOOSE>;
     using Vec = typename Row::Vec;
-    __host__ __device__ static constexpr size_t bytes(int threads) { return RING ? sizeof(Vec) * N * ROWS * DEPTH * threads : 0; }
+    static constexpr int WORD = LOOSE ? 4 : (int)sizeof(Vec);
+    static_assert(WORD >= 4, "asynchronous copies have 4, 8 or 16 bytes");
+    // words of a row in a slot
+    __host__ __device__ static constexpr int words(int lanes) { return lanes * N + (LOOSE ? 1 : 0); }
+    __host__ __device__ static constexpr size_t bytes(int threads, int lanes) { return (size_t)WORD * words(lanes) * (threads / lanes) * ROWS * DEPTH; }
     const T *from;            // of the next row to be fetched
     int64_t ld, step;         // elements
-    Vec *ring;                // the thread's first
-    Row next[RING ? 1 : ROWS];
-    __device__ __forceinline__ LnAhead(const void *p, int64_t ld_, unsigned unit, unsigned stride, void *shared)
-        : from(reinterpret_cast<const T *>(p) + (int64_t)unit * ROWS * ld_), ld(ld_), step((int64_t)stride * ROWS * ld_),
-          ring(reinterpret_cast<Vec *>(shared) + threadIdx.x) {}
+    const unsigned char *shared;
+    uint32_t ring;            // shared address of the first word of the group's row, or of the thread's vector
+    unsigned odd, odd_step;   // LOOSE: whether the rows of the first step to be taken start in the upper half of a word; of later steps
+    int slot_words;
+    __device__ __forceinline__ LnAhead(const void *p, int64_t ld_, unsigned unit, unsigned stride, int lanes, int group, void *shared_)
+        : from(reinterpret_cast<const T *>(p) + (int64_t)unit * ROWS * ld_), ld(ld_), step((int64_t)stride * ROWS * ld_), shared(reinterpret_cast<unsigned char *>(shared_)) {
+        slot_words = words(lanes) * (blockDim.x / lanes);
+        ring = (uint32_t)__cvta_generic_to_shared(shared) + (LOOSE ? group * words(lanes) : (int)threadIdx.x) * WORD;
+        odd = (unsigned)(reinterpret_cast<uintptr_t>(from) >> 1) & 1, odd_step = (unsigned)step & 1;
+    }
     __device__ __forceinline__ void fetch(int slot, unsigned row, unsigned rows, int dim, int g, int lanes) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row + r >= rows) continue;
             const T *const q = from + r * ld;
-            if constexpr (RING) {
+            const uint32_t to = ring + (slot * ROWS + r) * slot_words * WORD;
+            if constexpr (LOOSE) {
+                const unsigned upper = (unsigned)(reinterpret_cast<uintptr_t>(q) >> 1) & 1;
+                const char *const w = reinterpret_cast<const char *>(q) - 2 * upper;
+                const int all = dim + (int)upper, count = (all + 1) / 2;      // halves and words
+                auto copy = [&](int j) {
+                    if (j >= count) return;
+                    if (j == 0 && upper && row + r == 0) {
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + 2), "h"(*reinterpret_cast<const unsigned short *>(q)) : "memory");
+                    } else {
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to + 4 * j), "l"(w + 4 * j), "r"(2 * j + 1 < all ? 4 : 2) : "memory");
+                    }
+                };
+#pragma unroll
+                for (int i = 0; i < N; ++i) copy(g + i * lanes);
+                if (g == 0) copy(lanes * N);
+            } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     if (!Row::in(i, dim, g, lanes)) continue;
-                    const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring + ((slot * ROWS + r) * N + i) * blockDim.x);
-                    if constexpr (sizeof(Vec) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(q + (g + i * lanes) * V) : "memory");
-                    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(q + (g + i * lanes) * V), "n"(sizeof(Vec)) : "memory");
+                    if constexpr (WORD == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * blockDim.x * WORD), "l"(q + (g + i * lanes) * V) : "memory");
+                    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + i * blockDim.x * WORD), "l"(q + (g + i * lanes) * V), "n"(WORD) : "memory");
                 }
-            } else {
-                next[r].load(q, dim, g, lanes);
             }
         }
         from += step;
     }
-    __device__ __forceinline__ void take(Row &x, int slot, int r) const {
-        if constexpr (RING) {
+    __device__ __forceinline__ void take(Row &x, int slot, int r, int g, int lanes) const {
+        const uint32_t at = ring + (slot * ROWS + r) * slot_words * WORD;
 #pragma unroll
-            for (int i = 0; i < N; ++i) x.v[i] = ring[((slot * ROWS + r) * N + i) * blockDim.x];
-        } else {
-            x = next[r];
+        for (int i = 0; i < N; ++i) {
+            if constexpr (LOOSE) {
+                unsigned a, b;
+                asm volatile("ld.shared.u32 %0, [%2];\nld.shared.u32 %1, [%2 + 4];" : "=r"(a), "=r"(b) : "r"(at + (g + i * lanes) * 4) : "memory");
+                *reinterpret_cast<unsigned *>(&x.v[i]) = __funnelshift_r(a, b, 16 * ((odd + r * (unsigned)ld) & 1));
+            } else {
+                x.v[i] = reinterpret_cast<const Vec *>(shared)[(slot * ROWS + r) * slot_words + i * blockDim.x + threadIdx.x];
+            }
         }
     }
+    __device__ __forceinline__ void taken() { odd = (odd + odd_step) & 1; }   // a step
 };
 __device__ __forceinline__ void ln_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
 __device__ __forceinline__ void ln_arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }   // all but the last LEFT
+// The same for the copies of all threads of a row.
+template <int LEFT, bool LOOSE, bool MULTI>
+__device__ __forceinline__ void ln_row_arrived(int lanes, int barrier) {
+    ln_arrived<LEFT>();
+    if constexpr (LOOSE && MULTI) asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(lanes) : "memory");
+    else if constexpr (LOOSE) __syncwarp();
+}
 
 template <int ROWS>
 constexpr int LN_AHEAD = ROWS == 1 ? 4 : 2;             // steps
@@ -356,29 +399,29 @@ constexpr int LN_AHEAD_BACKWARD = ROWS == 1 ? 3 : 2;
 // Mean and sum of squared differences from it: over a warp in two passes; the warps' are joined by
 //   sum over warps of M2 + count (mean of the warp - mean)^2,
 // which takes one exchange and loses nothing where the mean is large beside the differences.
-template <typename T, int V, int N, bool MULTI, bool EXACT>
+template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
 __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD<R>;
-    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    using Ahead = LnAhead<T, V, N, EXACT, LOOSE, R, AHEAD>;
     using Row = typename Ahead::Row;
     constexpr int P = Row::PAIRS;
     const int groups = MULTI ? 1 : blockDim.x / lanes, group = MULTI ? 0 : threadIdx.x / lanes, g = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1), dim = a.dim;
     const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
     const float per = 1.f / (float)dim;
     unsigned unit = blockIdx.x * groups + group;
-    Ahead in(a.x, a.ld_x, unit, stride, shared_bytes);
+    Ahead in(a.x, a.ld_x, unit, stride, lanes, group, shared_bytes);
 #pragma unroll
-    for (int k = 0; k < Ahead::STEPS; ++k) {
+    for (int k = 0; k < AHEAD; ++k) {
         in.fetch(k, (unit + k * stride) * R, rows, dim, g, lanes);
         ln_commit();
     }
     // elements of a row that a warp has: this one, and the one with this lane's number
     auto elements = [&](int warp) {
         int n = 0;
-        for (int i = 0; i < N; ++i) n += max(0, min(32, dim / V - warp * 32 - i * lanes)) * V;
+        for (int i = 0; i < N; ++i) n += max(0, min(32 * V, dim - (warp * 32 + i * lanes) * V));
         return (float)n;
     };
     const float count = MULTI && (int)(threadIdx.x & 31) < lanes / 32 ? elements(threadIdx.x & 31) : 0.f, warp_count = MULTI ? elements(threadIdx.x / 32) : (float)dim;
@@ -400,22 +443,27 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const Laye
     const int64_t out_step = (int64_t)stride * R * a.ld_out;
     int at = 0, slot = 0;
     for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
-        ln_arrived<Ahead::STEPS - 1>();
+        ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1);
         float2 y[R][P];
         float s[R], mean[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             Row x;
-            in.take(x, slot, r);
+            in.take(x, slot, r, g, lanes);
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
             for (int p = 0; p < P; ++p) y[r][p] = x.get(p, dim, g, lanes), sum = add2(sum, y[r][p]);
             s[r] = sum.x + sum.y;
         }
-        in.fetch(slot, (unit + Ahead::STEPS * stride) * R, rows, dim, g, lanes);
-        ln_commit();
-        slot = slot + 1 < Ahead::STEPS ? slot + 1 : 0;
+        auto fetch = [&] {
+            in.taken();
+            in.fetch(slot, (unit + AHEAD * stride) * R, rows, dim, g, lanes);
+            ln_commit();
+            slot = slot + 1 < AHEAD ? slot + 1 : 0;
+        };
+        if (!LOOSE) fetch();
         ln_sum<R>(s, MULTI ? 32 : lanes);
+        if (LOOSE && !MULTI) fetch();      // when all threads have taken theirs
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             mean[r] = s[r] * warp_per;
@@ -423,8 +471,8 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const Laye
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 float2 z = add2(y[r][p], both(-mean[r]));
-                if (!Row::in(2 * p / V, dim, g, lanes)) z.x = 0.f;
-                if (2 * p + 1 >= E || !Row::in((2 * p + 1) / V, dim, g, lanes)) z.y = 0.f;
+                if (!Row::has(2 * p, dim, g, lanes)) z.x = 0.f;
+                if (!Row::has(2 * p + 1, dim, g, lanes)) z.y = 0.f;
                 sum = fma2(z, z, sum);
                 if (!MULTI) y[r][p] = z;
             }
@@ -433,6 +481,7 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const Laye
         ln_sum<R>(s, MULTI ? 32 : lanes);
         if constexpr (MULTI) {
             const float2 other = ln_exchange(make_float2(mean[0], s[0]), lanes, part, at, 1);
+            if (LOOSE) fetch();
             float m[1] = {other.x * count};
             ln_sum<1>(m, warps);
             mean[0] = m[0] * per;
@@ -463,13 +512,13 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 128) k_ln_rows(const Laye
 
 // The gradients; the sums over the rows are gathered by column in registers, joined in shared memory over the block's groups and
 // written as the block's part of partial [blocks][2][dim], or, from a single block, as they are.
-template <typename T, int V, int N, bool MULTI, bool EXACT>
+template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
 __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD_BACKWARD<R>;
-    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    using Ahead = LnAhead<T, V, N, EXACT, LOOSE, R, AHEAD>;
     using Row = typename Ahead::Row;
     constexpr int P = Row::PAIRS;
     const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes, dim = a.dim;
@@ -478,14 +527,15 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
     // weight [dim]; the coming rows of x and of the gradient, afterwards the columns' sums [2 P][threads]
     float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + (dim + 3) / 4 * 4;
     unsigned unit = blockIdx.x * groups + group;
-    Ahead in_x(a.x, a.ld_x, unit, stride, joined), in_u(a.grad, a.ld_grad, unit, stride, reinterpret_cast<unsigned char *>(joined) + Ahead::bytes(blockDim.x));
+    Ahead in_x(a.x, a.ld_x, unit, stride, lanes, group, joined),
+        in_u(a.grad, a.ld_grad, unit, stride, lanes, group, reinterpret_cast<unsigned char *>(joined) + Ahead::bytes(blockDim.x, lanes));
     auto fetch = [&](int slot, unsigned row) {
         in_x.fetch(slot, row, rows, dim, g, lanes);
         in_u.fetch(slot, row, rows, dim, g, lanes);
         ln_commit();
     };
 #pragma unroll
-    for (int k = 0; k < Ahead::STEPS; ++k) fetch(k, (unit + k * stride) * R);
+    for (int k = 0; k < AHEAD; ++k) fetch(k, (unit + k * stride) * R);
     // mean and rstd: a lane has those of one of the group's next `turns` steps, and of as many after those
     const int turns = lanes < 32 ? lanes : 32, mine = threadIdx.x & (turns - 1);
     float2 stats[R], later[R];
@@ -495,7 +545,7 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
     };
     statistics(stats, unit + mine * stride);
     const bool f32 = a.weight_type == QGBDT_F32;
-    for (int c = threadIdx.x; c < dim; c += blockDim.x) weight[c] = ln_weight<T>(a.weight, f32, c, 1.f);
+    for (int c = threadIdx.x; c < (dim + 3) / 4 * 4; c += blockDim.x) weight[c] = c < dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
     __syncthreads();
     float2 dw[P] = {}, db[P] = {};
     T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
@@ -506,29 +556,29 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
         if (turn == 0) statistics(later, unit + (mine + turns) * stride);
         float2 xh[R][P], y[R][P];
         float s[2 * R], rstd[R];
-        ln_arrived<Ahead::STEPS - 1>();
+        ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1 + group);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const float mean = __shfl_sync(0xffffffffu, stats[r].x, turn, turns);
             rstd[r] = __shfl_sync(0xffffffffu, stats[r].y, turn, turns);
             Row x, u;
-            in_x.take(x, slot, r);
-            in_u.take(u, slot, r);
+            in_x.take(x, slot, r, g, lanes);
+            in_u.take(u, slot, r, g, lanes);
             const bool is = unit * R + r < rows;
             float2 sum = make_float2(0.f, 0.f), along = sum;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 float2 v = u.get(p, dim, g, lanes), h = mul2(add2(x.get(p, dim, g, lanes), both(-mean)), both(rstd[r]));
-                if (!is || !Row::in(2 * p / V, dim, g, lanes)) v.x = h.x = 0.f;
-                if (!is || 2 * p + 1 >= E || !Row::in((2 * p + 1) / V, dim, g, lanes)) v.y = h.y = 0.f;
+                if (!is || !Row::has(2 * p, dim, g, lanes)) v.x = h.x = 0.f;
+                if (!is || !Row::has(2 * p + 1, dim, g, lanes)) v.y = h.y = 0.f;
                 db[p] = add2(db[p], v);
                 dw[p] = fma2(v, h, dw[p]);
                 float2 w = make_float2(0.f, 0.f);
                 if constexpr (V > 1) {
                     if (Row::in(2 * p / V, dim, g, lanes)) w = *reinterpret_cast<const float2 *>(weight + (g + 2 * p / V * lanes) * V + 2 * p % V);
                 } else {
-                    if (Row::in(2 * p, dim, g, lanes)) w.x = weight[g + 2 * p * lanes];
-                    if (2 * p + 1 < E && Row::in(2 * p + 1, dim, g, lanes)) w.y = weight[g + (2 * p + 1) * lanes];
+                    if (Row::has(2 * p, dim, g, lanes)) w.x = weight[g + 2 * p * lanes];
+                    if (Row::has(2 * p + 1, dim, g, lanes)) w.y = weight[g + (2 * p + 1) * lanes];
                 }
                 xh[r][p] = h;
                 y[r][p] = mul2(v, w);
@@ -542,11 +592,17 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST<V> : 256) k_ln_rows_backward(c
 #pragma unroll
             for (int r = 0; r < R; ++r) stats[r] = later[r];
         }
-        fetch(slot, (unit + Ahead::STEPS * stride) * R);
-        slot = slot + 1 < Ahead::STEPS ? slot + 1 : 0;
+        auto next = [&] {
+            in_x.taken(), in_u.taken();
+            fetch(slot, (unit + AHEAD * stride) * R);
+            slot = slot + 1 < AHEAD ? slot + 1 : 0;
+        };
+        if (!LOOSE) next();
         ln_sum<2 * R>(s, MULTI ? 32 : lanes);
+        if (LOOSE && !MULTI) next();       // when all threads have taken theirs
         if constexpr (MULTI) {
             const float2 other = ln_exchange(make_float2(s[0], s[1]), lanes, part, at, 1 + group);
+            if (LOOSE) next();
             s[0] = other.x, s[1] = other.y;
             ln_sum<2>(s, warps);
             s[0] = __shfl_sync(0xffffffffu, s[0], 0), s[1] = __shfl_sync(0xffffffffu, s[1], 0);
@@ -620,13 +676,13 @@ int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *block
     return QGBDT_OK;
 }
 
-template <typename T, int V, int N, bool MULTI, bool EXACT>
+template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     constexpr int R = LN_PAIR<N * V, MULTI>;
-    constexpr auto kernel = k_ln_rows<T, V, N, MULTI, EXACT>;
+    constexpr auto kernel = k_ln_rows<T, V, N, MULTI, EXACT, LOOSE>;
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
     const int64_t want = (a.rows + groups * R - 1) / (groups * R);
-    const size_t smem = LnAhead<T, V, N, EXACT, R, LN_AHEAD<R>>::bytes(threads);
+    const size_t smem = LnAhead<T, V, N, EXACT, LOOSE, R, LN_AHEAD<R>>::bytes(threads, lanes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = want;
     if (want > c->sm_count) {
@@ -637,12 +693,14 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
 }
 
 // How a row is cut up: calls `with` with N, MULTI and EXACT.
-template <int V, typename F>
+template <int V, bool LOOSE, typename F>
 int rows_cut(int dim, F with) {
     constexpr int most = LN_EACH<V> / V;
     const int lanes = ln_lanes<V>(dim), each = (dim + lanes * V - 1) / (lanes * V);
     auto exact = [&](auto n, auto multi) {
-        if (dim == lanes * n.value * V) return with(n, multi, std::true_type{}, lanes);
+        if constexpr (!LOOSE) {
+            if (dim == lanes * n.value * V) return with(n, multi, std::true_type{}, lanes);
+        }
         return with(n, multi, std::false_type{}, lanes);
     };
     if (lanes > 32) return exact(std::integral_constant<int, most>{}, std::true_type{});
@@ -653,9 +711,9 @@ int rows_cut(int dim, F with) {
     return exact(std::integral_constant<int, most>{}, std::false_type{});
 }
 
-template <typename T, int V>
+template <typename T, int V, bool LOOSE = false>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
+    return rows_cut<V, LOOSE>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value, LOOSE>(c, a, lanes, st); });
 }
 
 template <typename T>
@@ -665,10 +723,9 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     const bool vectors = bytes == 16;
     if (a.dim <= LN_ROW) {
         if (vectors) return rows_forward<T, V>(c, a, st);
-        if constexpr (sizeof(T) == 2) {
-            if (bytes >= 4) return rows_forward<T, 2>(c, a, st);
-        }
-        return rows_forward<T, 1>(c, a, st);
+        if (bytes == 8) return rows_forward<T, V / 2>(c, a, st);
+        if (bytes == 4) return rows_forward<T, V / 4>(c, a, st);
+        if constexpr (sizeof(T) == 2) return rows_forward<T, 2, true>(c, a, st);
     }
     const int64_t most = (int64_t)c->sm_count * 4;
     const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
@@ -676,12 +733,12 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     return qg_launch(c, k_ln_long<T, 1>, grid, LN_THREADS, 0, st, a);
 }
 
-template <typename T, int V, int N, bool MULTI, bool EXACT>
+template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     constexpr int R = LN_PAIR<N * V, MULTI>;
-    constexpr auto kernel = k_ln_rows_backward<T, V, N, MULTI, EXACT>;
+    constexpr auto kernel = k_ln_rows_backward<T, V, N, MULTI, EXACT, LOOSE>;
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
-    const size_t sums_bytes = (size_t)threads * ((N * V + 1) / 2 * 2) * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, R, LN_AHEAD_BACKWARD<R>>::bytes(threads);
+    const size_t sums_bytes = (size_t)threads * ((N * V + 1) / 2 * 2) * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, LOOSE, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
     const size_t smem = (size_t)(a.dim + 3) / 4 * 4 * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = 0;
@@ -700,9 +757,9 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     return qg_ws_close(c, st);
 }
 
-template <typename T, int V>
+template <typename T, int V, bool LOOSE = false>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
+    return rows_cut<V, LOOSE>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value, LOOSE>(c, a, lanes, st); });
 }
 
 template <typename T>
@@ -712,10 +769,9 @@ int backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     const bool vectors = bytes == 16;
     if (a.dim <= LN_ROW) {
         if (vectors) return rows_backward<T, V>(c, a, st);
-        if constexpr (sizeof(T) == 2) {
-            if (bytes >= 4) return rows_backward<T, 2>(c, a, st);
-        }
-        return rows_backward<T, 1>(c, a, st);
+        if (bytes == 8) return rows_backward<T, V / 2>(c, a, st);
+        if (bytes == 4) return rows_backward<T, V / 4>(c, a, st);
+        if constexpr (sizeof(T) == 2) return rows_backward<T, 2, true>(c, a, st);
     }
     if (a.d_weight || a.d_bias) {
         // before the rows' gradients, which may take the place of an input

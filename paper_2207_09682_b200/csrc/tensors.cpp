@@ -8,6 +8,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -172,6 +173,17 @@ bool words(const Call &c, PyObject *o, const char *name, at::ScalarType type, in
     return true;
 }
 
+// New tensors without the dispatcher, which takes as long as a small call's kernel: contiguous, and parts [at, at + n) of a vector.
+at::Tensor fresh(at::IntArrayRef sizes, at::ScalarType type, const Call &c) {
+    return at::detail::empty_cuda(sizes, type, at::Device(at::kCUDA, (c10::DeviceIndex)c.device), std::nullopt);
+}
+at::Tensor part(const at::Tensor &all, int64_t at, int64_t n) {
+    at::Tensor t = at::detail::make_tensor<c10::TensorImpl>(c10::TensorImpl::VIEW, c10::Storage(all.storage()), all.key_set(), all.dtype());
+    t.unsafeGetTensorImpl()->set_storage_offset(all.storage_offset() + at);
+    t.unsafeGetTensorImpl()->set_sizes_contiguous({n});
+    return t;
+}
+
 // An output [n, d] of `like`'s type: the caller's, or a new one if None.
 struct Output {
     at::Tensor made;
@@ -185,6 +197,13 @@ struct Output {
         }
         if (!r.take(c, o, name)) return false;
         if (r.n != n || r.d != d || r.t->scalar_type() != like.scalar_type()) return refuse(name, "has the wrong size or type"), false;
+        return true;
+    }
+    // as large as `x`
+    bool take_or_make(const Call &c, PyObject *o, const char *name, const Rows &x) {
+        if (o != Py_None) return take(c, o, name, x.n, x.d, *x.t);
+        made = fresh({x.n, x.d}, x.t->scalar_type(), c);
+        r.t = &made, r.n = x.n, r.d = x.d, r.ld = x.d > 0 ? x.d : 1;
         return true;
     }
     PyObject *give(PyObject *o) const {   // a new reference
@@ -387,12 +406,12 @@ PyObject *py_layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     double eps;
     if (!c.take(args, nargs, 7) || !x.take_input(c, args[2], "x")) return nullptr;
     if (x.type < 0) return refuse("x must be float32, bfloat16 or float16");
-    if (!w.take(c, x, args[3], args[4]) || !number(args[5], &eps) || !out.take(c, args[6], "out", x.n, x.d, *x.t)) return nullptr;
-    const at::Tensor both = at::empty({2 * x.n}, x.t->options().dtype(at::kFloat).requires_grad(false));
+    if (!w.take(c, x, args[3], args[4]) || !number(args[5], &eps) || !out.take_or_make(c, args[6], "out", x)) return nullptr;
+    const at::Tensor both = fresh({2 * x.n}, at::kFloat, c);
     float *p = both.data_ptr<float>();   // mean, rstd
     const int rc = lib.layer_norm(c.ctx, x.p(), x.ld, x.type, w.weight, w.bias, w.type, x.n, (int32_t)x.d, eps, out.r.p(), out.r.ld, p, p + x.n, c.stream);
     if (rc != QGBDT_OK) return c.result(rc);
-    PyObject *const mean = THPVariable_Wrap(both.slice(0, 0, x.n)), *const rstd = THPVariable_Wrap(both.slice(0, x.n, 2 * x.n));
+    PyObject *const mean = THPVariable_Wrap(part(both, 0, x.n)), *const rstd = THPVariable_Wrap(part(both, x.n, x.n));
     return Py_BuildValue("(NNN)", out.give(args[6]), mean, rstd);
     END_HANDLE_TH_ERRORS
 }
@@ -410,12 +429,11 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n
     if (grad.type != x.type || grad.n != x.n || grad.d != x.d) return refuse("grad_out and x differ in size or type");
     if (args[4] == Py_None || args[5] == Py_None) return refuse("mean and rstd are those of the forward call");
     if (!words(c, args[4], "mean", at::kFloat, x.n, &mean) || !words(c, args[5], "rstd", at::kFloat, x.n, &rstd) ||
-        !w.take(c, x, args[6], Py_None) || !gx.take(c, args[7], "grad_x", x.n, x.d, *x.t))
+        !w.take(c, x, args[6], Py_None) || !gx.take_or_make(c, args[7], "grad_x", x))
         return nullptr;
     at::Tensor gw, gb;
     if (args[6] != Py_None) {
-        const auto options = x.t->options().dtype(w.scalar).requires_grad(false);
-        gw = at::empty({x.d}, options), gb = at::empty({x.d}, options);
+        gw = fresh({x.d}, w.scalar, c), gb = fresh({x.d}, w.scalar, c);
     }
     const int rc = lib.layer_norm_backward(c.ctx, grad.p(), grad.ld, x.p(), x.ld, x.type, (const float *)mean, (const float *)rstd, w.weight, w.type, x.n,
                                            (int32_t)x.d, gx.r.p(), gx.r.ld, gw.defined() ? gw.data_ptr() : nullptr, gb.defined() ? gb.data_ptr() : nullptr,
@@ -546,7 +564,7 @@ PyObject *py_adamw_values(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
         m.push_back((const uint8_t *)a->data_ptr()), v.push_back((const uint8_t *)b->data_ptr()), e.push_back((const uint8_t *)x->data_ptr());
         counts.push_back(n);
         for (int k = 0; k < 2; ++k) {
-            made[k].push_back(at::empty(a->sizes(), a->options().dtype(half ? at::kBFloat16 : at::kFloat)));
+            made[k].push_back(fresh(a->sizes(), half ? at::kBFloat16 : at::kFloat, c));
             out[k].push_back(made[k].back().data_ptr());
         }
     }
