@@ -248,119 +248,86 @@ __device__ __forceinline__ float2 ln_exchange(float2 mine, int lanes, float2 (&p
 // Lanes that `warps` warps' sums are in, as a power of two.
 __device__ __forceinline__ int ln_power(int warps) { return warps <= 1 ? 1 : 2 << (31 - __clz(warps - 1)); }
 
-// Eight words from `first` bytes (0 to 16) of two neighbouring vectors on: the four that start there.
-template <bool HALVES>   // first may be a multiple of 2, not only of 4
-__device__ __forceinline__ uint4 ln_cut(const uint4 &a, const uint4 &b, unsigned first) {
-    unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    if (first & 16) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = w[k + 4];
-    }
-    if (first & 8) {
-#pragma unroll
-        for (int k = 0; k < 6; ++k) w[k] = w[k + 2];
-    }
-    if (first & 4) {
-#pragma unroll
-        for (int k = 0; k < 5; ++k) w[k] = w[k + 1];
-    }
-    if (HALVES && (first & 2)) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], 16);
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// A thread's vectors of a row.  LOOSE: the last vector may be partly outside the row (its elements are zeros there).
-template <typename T, int V, int N, bool EXACT, bool LOOSE>
+// A thread's vectors of a row.  V = 1: single elements, of rows that start anywhere.
+template <typename T, int V, int N, bool EXACT>
 struct LnRow {
     using Vec = OpsVec<T, V>;
     static constexpr int E = N * V, PAIRS = E / 2;
     Vec v[N];
-    // elements of vector i inside the row
-    __device__ __forceinline__ static int inside(int i, int dim, int g, int lanes) { return EXACT ? V : max(0, min(V, dim - (g + i * lanes) * V)); }
-    __device__ __forceinline__ static bool in(int i, int dim, int g, int lanes) { return EXACT || (g + i * lanes) * V < dim; }
+    __device__ __forceinline__ static bool in(int i, int dim, int g, int lanes) { return EXACT || (g + i * lanes) * V < dim; }   // vector i
     __device__ __forceinline__ void store(T *p, int dim, int g, int lanes) const {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (in(i, dim, g, lanes)) *reinterpret_cast<Vec *>(p + (g + i * lanes) * V) = v[i];
     }
     __device__ __forceinline__ float2 get(int p) const {   // elements 2 p and 2 p + 1
-        const Vec &q = v[2 * p / V];
-        if constexpr (sizeof(T) == 4) {
-            return make_float2(q.v[2 * p % V], q.v[2 * p % V + 1]);
+        if constexpr (V == 1 || sizeof(T) == 4) {
+            return make_float2(OpsType<T>::load(v[2 * p / V].v[2 * p % V]), OpsType<T>::load(v[(2 * p + 1) / V].v[(2 * p + 1) % V]));
         } else {
-            const unsigned w = *reinterpret_cast<const unsigned *>(&q.v[2 * p % V]);
+            const unsigned w = *reinterpret_cast<const unsigned *>(&v[2 * p / V].v[2 * p % V]);
             if constexpr (OpsType<T>::BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
             else return __half22float2(*reinterpret_cast<const __half2 *>(&w));
         }
     }
     __device__ __forceinline__ void set(int p, float2 x) {
-        Vec &q = v[2 * p / V];
-        if constexpr (sizeof(T) == 4) q.v[2 * p % V] = x.x, q.v[2 * p % V + 1] = x.y;
-        else if constexpr (OpsType<T>::BF16) *reinterpret_cast<__nv_bfloat162 *>(&q.v[2 * p % V]) = __float22bfloat162_rn(x);
-        else *reinterpret_cast<__half2 *>(&q.v[2 * p % V]) = __float22half2_rn(x);
+        if constexpr (V == 1 || sizeof(T) == 4) {
+            v[2 * p / V].v[2 * p % V] = OpsType<T>::store(x.x), v[(2 * p + 1) / V].v[(2 * p + 1) % V] = OpsType<T>::store(x.y);
+        } else {
+            T *const q = &v[2 * p / V].v[2 * p % V];
+            if constexpr (OpsType<T>::BF16) *reinterpret_cast<__nv_bfloat162 *>(q) = __float22bfloat162_rn(x);
+            else *reinterpret_cast<__half2 *>(q) = __float22half2_rn(x);
+        }
     }
 };
 
 // The coming rows of an input, copied asynchronously to the shared memory, DEPTH steps of ROWS rows ahead: the memory's latency under
 // load takes 64 KB on their way per SM.  A thread's vectors go to places of its own, so that nobody waits for another thread's copies.
-// LOOSE: rows that start anywhere.  Such copies come in aligned vectors, so a row is copied as the aligned vectors that hold it, by all
-// its threads for one another, and a thread's vectors are cut from two neighbouring ones each.  (Where a row starts inside a vector, the
-// elements in front of it come along; what is in front of the first row is not read.  The last vector is copied as far as the row goes.)
-template <typename T, int V, int N, bool EXACT, bool LOOSE, int ROWS, int DEPTH>
+// Rows that start anywhere (V = 1): such copies come in aligned vectors, so a row is copied as the aligned vectors that hold it, by all its
+// threads for one another.  (Where a row starts inside a vector, the elements in front of it come along; what is in front of the
+// first row is not read.  The last vector is copied as far as the row goes, and zeros follow up to the threads' last elements.)
+template <typename T, int V, int N, bool EXACT, int ROWS, int DEPTH>
 struct LnAhead {
-    using Row = LnRow<T, V, N, EXACT, LOOSE>;
+    static constexpr bool LOOSE = V == 1;
+    using Row = LnRow<T, V, N, EXACT>;
     using Vec = typename Row::Vec;
-    // vectors of a row in a slot
-    __host__ __device__ static constexpr int vectors(int lanes) { return lanes * N + (LOOSE ? 1 : 0); }
+    // vectors of 16 bytes of a row in a slot
+    __host__ __device__ static constexpr int vectors(int lanes) { return LOOSE ? (lanes * N * (int)sizeof(T) + 15) / 16 + 1 : lanes * N; }
     __host__ __device__ static constexpr size_t bytes(int threads, int lanes) { return (size_t)16 * vectors(lanes) * (threads / lanes) * ROWS * DEPTH; }
     const T *from, *first;    // the next row to be fetched; the first of all
     int64_t ld, step;         // elements
-    const uint4 *ring;        // the group's first row, or the thread's first vector
+    const unsigned char *ring;   // the group's first row, or the thread's first vector
     uint32_t ring_at;         // its shared address
-    int slot_vectors;
-    unsigned offset, offset_step, offset_row;   // LOOSE: bytes of the first row to be taken within a vector; what a step and a row add
-    uint4 mask[LOOSE ? N : 1];                  // LOOSE: the bits of the thread's vectors that are inside the row
-    __device__ __forceinline__ LnAhead(const void *p, int64_t ld_, unsigned unit, unsigned stride, int dim, int lanes, int group, int g, void *shared)
+    int slot_bytes;
+    unsigned before, before_step, before_row;   // LOOSE: bytes of a vector in front of the first row to be taken; what a step and a row add
+    __device__ __forceinline__ LnAhead(const void *p, int64_t ld_, unsigned unit, unsigned stride, int lanes, int group, void *shared)
         : from(reinterpret_cast<const T *>(p) + (int64_t)unit * ROWS * ld_), first(reinterpret_cast<const T *>(p)), ld(ld_), step((int64_t)stride * ROWS * ld_) {
-        slot_vectors = vectors(lanes) * (blockDim.x / lanes);
-        ring = reinterpret_cast<const uint4 *>(shared) + (LOOSE ? group * vectors(lanes) : (int)threadIdx.x);
+        slot_bytes = 16 * vectors(lanes) * (blockDim.x / lanes);
+        ring = reinterpret_cast<const unsigned char *>(shared) + (LOOSE ? group * vectors(lanes) : (int)threadIdx.x) * 16;
         ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-        if constexpr (LOOSE) {
-            offset = (unsigned)reinterpret_cast<uintptr_t>(from) & 15, offset_step = (unsigned)step * sizeof(T) & 15, offset_row = (unsigned)ld * sizeof(T) & 15;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int n = Row::inside(i, dim, g, lanes) * (int)sizeof(T);   // bytes
-                auto bits = [n](int k) { return n >= 4 * k + 4 ? ~0u : n <= 4 * k ? 0u : 0xffffu; };
-                mask[i] = make_uint4(bits(0), bits(1), bits(2), bits(3));
-            }
-        }
+        before = (unsigned)reinterpret_cast<uintptr_t>(from) & 15, before_step = (unsigned)step * sizeof(T) & 15, before_row = (unsigned)ld * sizeof(T) & 15;
     }
     __device__ __forceinline__ void fetch(int slot, unsigned row, unsigned rows, int dim, int g, int lanes) {
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row + r >= rows) continue;
             const T *const q = from + r * ld;
-            const uint32_t to = ring_at + (slot * ROWS + r) * slot_vectors * 16;
+            const uint32_t to = ring_at + (slot * ROWS + r) * slot_bytes;
             if constexpr (LOOSE) {
-                const int before = (int)(reinterpret_cast<uintptr_t>(q) & 15), all = before + dim * (int)sizeof(T);   // bytes
-                const char *const w = reinterpret_cast<const char *>(q) - before;
-                auto copy = [&](int j) {
-                    const int left = all - 16 * j;
-                    if (left <= 0) return;
-                    if (j == 0 && w < reinterpret_cast<const char *>(first)) {
-                        for (int e = 0; e < (min(16, left) - before) / (int)sizeof(T); ++e) {
-                            if constexpr (sizeof(T) == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + before + 4 * e), "f"(q[e]) : "memory");
-                            else asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + before + 2 * e), "h"(reinterpret_cast<const unsigned short *>(q)[e]) : "memory");
-                        }
-                    } else {
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 16 * j), "l"(w + 16 * j), "r"(min(16, left)) : "memory");
+                const int front = (int)(reinterpret_cast<uintptr_t>(q) & 15), all = front + dim * (int)sizeof(T);   // bytes
+                const char *const w = reinterpret_cast<const char *>(q) - front;
+                int j = g;
+                if (g == 0 && w < reinterpret_cast<const char *>(first)) {
+                    for (int e = 0; e < (16 - front) / (int)sizeof(T); ++e) {
+                        const bool is = e < dim;
+                        if constexpr (sizeof(T) == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + front + 4 * e), "f"(is ? q[e] : 0.f) : "memory");
+                        else asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + front + 2 * e), "h"(is ? reinterpret_cast<const unsigned short *>(q)[e] : (unsigned short)0) : "memory");
                     }
-                };
-#pragma unroll
-                for (int i = 0; i < N; ++i) copy(g + i * lanes);
-                if (g == 0) copy(lanes * N);
+                    j += lanes;
+                }
+                for (; j < vectors(lanes); j += lanes) {
+                    const int left = max(0, min(16, all - 16 * j));
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 16 * j), "l"(left ? w + 16 * j : reinterpret_cast<const char *>(first)), "r"(left) : "memory");
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
@@ -370,51 +337,24 @@ struct LnAhead {
         }
         from += step;
     }
-    // Vectors outside the row (and, LOOSE, their parts) are zeros.
+    // Zeros outside the row.
     __device__ __forceinline__ void take(Row &x, int slot, int r, int dim, int g, int lanes) const {
-        const uint4 *const at = ring + (slot * ROWS + r) * slot_vectors;
+        const unsigned char *const at = ring + (slot * ROWS + r) * slot_bytes;
+        if constexpr (LOOSE) {
+            const T *const q = reinterpret_cast<const T *>(at + ((before + r * before_row) & 15)) + g;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            uint4 q = make_uint4(0, 0, 0, 0);
-            if constexpr (LOOSE) {
-                q = ln_cut<sizeof(T) == 2>(at[g + i * lanes], at[g + i * lanes + 1], (offset + r * offset_row) & 15);
-                q.x &= mask[i].x, q.y &= mask[i].y, q.z &= mask[i].z, q.w &= mask[i].w;
-            } else {
-                if (Row::in(i, dim, g, lanes)) q = at[i * blockDim.x];
+            for (int i = 0; i < N; ++i) x.v[i].v[0] = q[i * lanes];
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint4 q = make_uint4(0, 0, 0, 0);
+                if (Row::in(i, dim, g, lanes)) q = reinterpret_cast<const uint4 *>(at)[i * blockDim.x];
+                *reinterpret_cast<uint4 *>(&x.v[i]) = q;
             }
-            *reinterpret_cast<uint4 *>(&x.v[i]) = q;
         }
     }
-    __device__ __forceinline__ void taken() {   // a step
-        if constexpr (LOOSE) offset = (offset + offset_step) & 15;
-    }
+    __device__ __forceinline__ void taken() { before = (before + before_step) & 15; }   // a step
 };
-
-// Writes a row.  LOOSE: a row that does not start on a vector is handed round through the shared memory (`own`: the group's place for
-// it, in turn one of two) and written as the aligned vectors that it fills, its ends by element.
-template <typename T, int V, int N, bool EXACT, bool LOOSE, bool MULTI>
-__device__ __forceinline__ void ln_write(const LnRow<T, V, N, EXACT, LOOSE> &x, T *p, int dim, int g, int lanes, uint4 *own, int barrier, bool is) {
-    if constexpr (!LOOSE) {
-        if (is) x.store(p, dim, g, lanes);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) own[g + i * lanes] = *reinterpret_cast<const uint4 *>(&x.v[i]);
-        if constexpr (MULTI) asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(lanes) : "memory");
-        else __syncwarp();
-        if (!is) return;
-        const int before = (int)(reinterpret_cast<uintptr_t>(p) & 15) / (int)sizeof(T), head = before ? min(V - before, dim) : 0;   // elements
-        const int full = (dim - head) / V, tail = head + full * V;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int j = g + i * lanes;      // of the vectors that the row fills; before > 0: behind its j-th own one
-            if (j < full) *reinterpret_cast<uint4 *>(p + head + j * V) = head ? ln_cut<sizeof(T) == 2>(own[j], own[j + 1 < lanes * N ? j + 1 : j], head * (unsigned)sizeof(T)) : own[j];
-        }
-        for (int e = g; e < 2 * V; e += lanes) {   // the ends: an element per thread
-            const int c = e < V ? e : tail + e - V;
-            if (c < (e < V ? head : dim)) p[c] = reinterpret_cast<const T *>(own)[c];
-        }
-    }
-}
 
 __device__ __forceinline__ void ln_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
@@ -429,27 +369,27 @@ __device__ __forceinline__ void ln_row_arrived(int lanes, int barrier) {
 
 template <int ROWS>
 constexpr int LN_AHEAD = ROWS == 1 ? 4 : 2;             // steps
-template <typename T, int ROWS, bool LOOSE>
-constexpr int LN_AHEAD_BACKWARD = ROWS > 1 || (LOOSE && sizeof(T) == 4) ? 2 : 3;      // (two, where three longest rows do not fit)
+template <int ROWS>
+constexpr int LN_AHEAD_BACKWARD = ROWS == 1 ? 3 : 2;
 
 // Mean and sum of squared differences from it: over a warp in two passes; the warps' are joined by
 //   sum over warps of M2 + count (mean of the warp - mean)^2,
 // which takes one exchange and loses nothing where the mean is large beside the differences.
-template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
-__global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && !LOOSE ? 2 : 1) k_ln_rows(const LayerNormArgs a, int lanes) {
+template <typename T, int V, int N, bool MULTI, bool EXACT>
+__global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && V > 1 ? 2 : 1) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD<R>;
-    using Ahead = LnAhead<T, V, N, EXACT, LOOSE, R, AHEAD>;
+    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    constexpr bool LOOSE = Ahead::LOOSE;
     using Row = typename Ahead::Row;
-    constexpr int P = Row::PAIRS, PV = V / 2;      // pairs, and of a vector
+    constexpr int P = Row::PAIRS;
     const int groups = MULTI ? 1 : blockDim.x / lanes, group = MULTI ? 0 : threadIdx.x / lanes, g = MULTI ? threadIdx.x : threadIdx.x & (lanes - 1), dim = a.dim;
     const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
     const float per = 1.f / (float)dim;
     unsigned unit = blockIdx.x * groups + group;
-    Ahead in(a.x, a.ld_x, unit, stride, dim, lanes, group, g, shared_bytes);
-    uint4 *const own = reinterpret_cast<uint4 *>(shared_bytes + Ahead::bytes(blockDim.x, lanes)) + group * lanes * N;   // LOOSE, [2][groups][lanes * N]
+    Ahead in(a.x, a.ld_x, unit, stride, lanes, group, shared_bytes);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
         in.fetch(k, (unit + k * stride) * R, rows, dim, g, lanes);
@@ -478,7 +418,7 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && !LOOSE ? 2 : 1
     }
     T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
     const int64_t out_step = (int64_t)stride * R * a.ld_out;
-    int at = 0, slot = 0, turn = 0;
+    int at = 0, slot = 0;
     for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
         ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1);
         float2 y[R][P];
@@ -506,23 +446,12 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && !LOOSE ? 2 : 1
             mean[r] = s[r] * warp_per;
             float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (!Row::in(i, dim, g, lanes)) continue;
-                float2 z[PV];
-#pragma unroll
-                for (int p = 0; p < PV; ++p) z[p] = add2(y[r][i * PV + p], both(-mean[r]));
-                if (LOOSE && Row::inside(i, dim, g, lanes) < V) {
-#pragma unroll
-                    for (int p = 0; p < PV; ++p) {
-                        if (2 * p >= Row::inside(i, dim, g, lanes)) z[p].x = 0.f;
-                        if (2 * p + 1 >= Row::inside(i, dim, g, lanes)) z[p].y = 0.f;
-                    }
-                }
-#pragma unroll
-                for (int p = 0; p < PV; ++p) {
-                    sum = fma2(z[p], z[p], sum);
-                    if (!MULTI) y[r][i * PV + p] = z[p];
-                }
+            for (int p = 0; p < P; ++p) {
+                float2 z = add2(y[r][p], both(-mean[r]));
+                if (!Row::in(2 * p / V, dim, g, lanes)) z.x = 0.f;
+                if (!Row::in((2 * p + 1) / V, dim, g, lanes)) z.y = 0.f;
+                sum = fma2(z, z, sum);
+                if (!MULTI) y[r][p] = z;
             }
             s[r] = sum.x + sum.y;
         }
@@ -541,16 +470,16 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && !LOOSE ? 2 : 1
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const unsigned row = unit * R + r;
-            if (!LOOSE && row >= rows) continue;
-            const float rstd = __frsqrt_rn(fmaf(s[r], per, a.eps));
+            if (row >= rows) continue;
+            const float rstd = rsqrtf(fmaf(s[r], per, a.eps));      // (two units in the last place)
             Row x;
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 const float2 z = MULTI ? add2(y[r][p], both(-mean[r])) : y[r][p];
                 x.set(p, fma2(mul2(z, both(rstd)), w[p], b[p]));
             }
-            ln_write<T, V, N, EXACT, LOOSE, MULTI>(x, out + r * a.ld_out, dim, g, lanes, own + (turn ^= 1) * blockDim.x * N, 1, row < rows);
-            if (g == 0 && row < rows) {
+            x.store(out + r * a.ld_out, dim, g, lanes);
+            if (g == 0) {
                 if (a.mean) a.mean[row] = mean[r];
                 if (a.rstd) a.rstd[row] = rstd;
             }
@@ -560,25 +489,25 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && !LOOSE ? 2 : 1
 
 // The gradients; the sums over the rows are gathered by column in registers, joined in shared memory over the block's groups and
 // written as the block's part of partial [blocks][2][dim], or, from a single block, as they are.
-template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 __global__ void __launch_bounds__(MULTI ? LN_MOST : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
-    constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD_BACKWARD<T, R, LOOSE>;
-    using Ahead = LnAhead<T, V, N, EXACT, LOOSE, R, AHEAD>;
+    constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD_BACKWARD<R>;
+    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    constexpr bool LOOSE = Ahead::LOOSE;
     using Row = typename Ahead::Row;
     constexpr int P = Row::PAIRS;
     const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes, dim = a.dim;
     const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
     const float per = 1.f / (float)dim;
-    // weight [dim]; the coming rows of x and of the gradient, afterwards the columns' sums [2 P][threads]
-    float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + (dim + V - 1) / V * V;
+    // weight (zeros outside the row); the coming rows of x and of the gradient, afterwards the columns' sums [2 P][threads]
+    float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + lanes * E;
     unsigned unit = blockIdx.x * groups + group;
     unsigned char *const rings = reinterpret_cast<unsigned char *>(joined);
     const size_t ring = Ahead::bytes(blockDim.x, lanes);
-    Ahead in_x(a.x, a.ld_x, unit, stride, dim, lanes, group, g, rings), in_u(a.grad, a.ld_grad, unit, stride, dim, lanes, group, g, rings + ring);
-    uint4 *const own = reinterpret_cast<uint4 *>(rings + 2 * ring) + group * lanes * N;   // LOOSE, [2][groups][lanes * N]
+    Ahead in_x(a.x, a.ld_x, unit, stride, lanes, group, rings), in_u(a.grad, a.ld_grad, unit, stride, lanes, group, rings + ring);
     auto fetch = [&](int slot, unsigned row) {
         in_x.fetch(slot, row, rows, dim, g, lanes);
         in_u.fetch(slot, row, rows, dim, g, lanes);
@@ -595,13 +524,13 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 256) k_ln_rows_backward(cons
     };
     statistics(stats, unit + mine * stride);
     const bool f32 = a.weight_type == QGBDT_F32;
-    for (int c = threadIdx.x; c < (dim + V - 1) / V * V; c += blockDim.x) weight[c] = c < dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
+    for (int c = threadIdx.x; c < lanes * E; c += blockDim.x) weight[c] = c < dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
     __syncthreads();
     float2 dw[P] = {}, db[P] = {};
     T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
     const int64_t out_step = (int64_t)stride * R * a.ld_out;
     const int warps = ln_power(lanes / 32);
-    int at = 0, slot = 0, turn = 0, which = 0;
+    int at = 0, slot = 0, turn = 0;
     for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
         if (turn == 0) statistics(later, unit + (mine + turns) * stride);
         float2 xh[R][P], y[R][P];
@@ -617,7 +546,7 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 256) k_ln_rows_backward(cons
             float2 sum = make_float2(0.f, 0.f), along = sum;
             if (unit * R + r >= rows) {        // (what its slot holds may be anything)
 #pragma unroll
-                for (int i = 0; i < N; ++i) *reinterpret_cast<uint4 *>(&x.v[i]) = *reinterpret_cast<uint4 *>(&u.v[i]) = make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < N; ++i) x.v[i] = u.v[i] = typename Row::Vec{};
             }
 #pragma unroll
             for (int p = 0; p < P; ++p) {
@@ -625,8 +554,9 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 256) k_ln_rows_backward(cons
                 const float2 v = u.get(p), h = mul2(add2(x.get(p), both(-mean)), both(rstd[r]));     // v is zero outside the row
                 db[p] = add2(db[p], v);
                 dw[p] = fma2(v, h, dw[p]);
-                float2 w = make_float2(0.f, 0.f);
-                if (Row::in(i, dim, g, lanes)) w = *reinterpret_cast<const float2 *>(weight + (g + i * lanes) * V + 2 * p % V);
+                float2 w;
+                if constexpr (LOOSE) w = make_float2(weight[g + i * lanes], weight[g + (i + 1) * lanes]);
+                else w = *reinterpret_cast<const float2 *>(weight + (g + i * lanes) * V + 2 * p % V);
                 xh[r][p] = h;
                 y[r][p] = mul2(v, w);
                 sum = add2(sum, y[r][p]);
@@ -656,17 +586,17 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 256) k_ln_rows_backward(cons
         }
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            if (!LOOSE && unit * R + r >= rows) continue;
+            if (unit * R + r >= rows) continue;
             const float2 c1 = both(-s[2 * r] * per), c2 = both(-s[2 * r + 1] * per);
             Row x;
 #pragma unroll
             for (int p = 0; p < P; ++p) x.set(p, mul2(fma2(xh[r][p], c2, add2(y[r][p], c1)), both(rstd[r])));
-            ln_write<T, V, N, EXACT, LOOSE, MULTI>(x, out + r * a.ld_out, dim, g, lanes, own + (which ^= 1) * blockDim.x * N, 1 + group, unit * R + r < rows);
+            x.store(out + r * a.ld_out, dim, g, lanes);
         }
     }
     if (!a.d_weight && !a.d_bias) return;
     ln_arrived<0>();
-    for (which = 0; which < 2; ++which) {
+    for (int which = 0; which < 2; ++which) {
         void *const final = which ? a.d_bias : a.d_weight;
         __syncthreads();
 #pragma unroll
@@ -698,16 +628,6 @@ bool aligned(const LayerNormArgs &a) {
            (!a.grad || qg_vec_bytes(a.grad, a.ld_grad * w, (int64_t)a.dim * w) == 16);
 }
 
-// Threads of a row: one vector each up to a warp's worth, then as many vectors each as there may be, then more warps.
-template <int V>
-int ln_lanes(int dim) {
-    const int vectors = (dim + V - 1) / V;
-    if (vectors > 32) return (vectors + 32 * (LN_EACH / V) - 1) / (32 * (LN_EACH / V)) * 32;
-    int lanes = 1;
-    while (lanes < vectors) lanes *= 2;
-    return lanes;
-}
-
 // Blocks of `threads` that the GPU holds at once.
 template <typename K>
 int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *blocks) {
@@ -717,13 +637,13 @@ int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *block
     return QGBDT_OK;
 }
 
-template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     constexpr int R = LN_PAIR<N * V, MULTI>;
-    constexpr auto kernel = k_ln_rows<T, V, N, MULTI, EXACT, LOOSE>;
+    constexpr auto kernel = k_ln_rows<T, V, N, MULTI, EXACT>;
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
     const int64_t want = (a.rows + groups * R - 1) / (groups * R);
-    const size_t smem = LnAhead<T, V, N, EXACT, LOOSE, R, LN_AHEAD<R>>::bytes(threads, lanes) + (LOOSE ? 2 * 16 * N * threads : 0);
+    const size_t smem = LnAhead<T, V, N, EXACT, R, LN_AHEAD<R>>::bytes(threads, lanes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = want;
     if (want > c->sm_count) {
@@ -733,25 +653,37 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
     return qg_launch(c, kernel, dim3((unsigned)grid), threads, smem, st, a, lanes);
 }
 
-// How a row is cut up: calls `with` with N, MULTI and EXACT.
-template <int V, bool LOOSE, typename F>
+// How a row is cut up: calls `with` with N, MULTI, EXACT and the threads of a row.  Vectors: one per thread up to a warp's worth, then
+// LN_EACH elements; single elements: four, eight or LN_EACH; then more warps.
+template <int V, typename F>
 int rows_cut(int dim, F with) {
     constexpr int most = LN_EACH / V;
-    const int lanes = ln_lanes<V>(dim), each = (dim + lanes * V - 1) / (lanes * V);
-    auto exact = [&](auto n, auto multi) {
-        if constexpr (!LOOSE) {
-            if (dim == lanes * n.value * V) return with(n, multi, std::true_type{}, lanes);
+    const int vectors = (dim + V - 1) / V;
+    auto few = [&](auto n) {      // of a warp's lanes
+        int lanes = 1;
+        while (lanes * n.value < vectors) lanes *= 2;
+        if constexpr (V > 1) {
+            if (dim == lanes * n.value * V) return with(n, std::false_type{}, std::true_type{}, lanes);
         }
-        return with(n, multi, std::false_type{}, lanes);
+        return with(n, std::false_type{}, std::false_type{}, lanes);
     };
-    if (lanes > 32) return exact(std::integral_constant<int, most>{}, std::true_type{});
-    if (each == 1) return exact(std::integral_constant<int, 1>{}, std::false_type{});
-    return exact(std::integral_constant<int, most>{}, std::false_type{});
+    if constexpr (V > 1) {
+        if (vectors <= 32) return few(std::integral_constant<int, 1>{});
+    } else {
+        if (vectors <= 32 * 4) return few(std::integral_constant<int, 4>{});
+        if (vectors <= 32 * 8) return few(std::integral_constant<int, 8>{});
+    }
+    if (vectors <= 32 * most) return few(std::integral_constant<int, most>{});
+    const int lanes = (vectors + 32 * most - 1) / (32 * most) * 32;
+    if constexpr (V > 1) {
+        if (dim == lanes * LN_EACH) return with(std::integral_constant<int, most>{}, std::true_type{}, std::true_type{}, lanes);
+    }
+    return with(std::integral_constant<int, most>{}, std::true_type{}, std::false_type{}, lanes);
 }
 
-template <typename T, int V, bool LOOSE>
+template <typename T, int V>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    return rows_cut<V, LOOSE>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value, LOOSE>(c, a, lanes, st); });
+    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
 }
 
 template <typename T>
@@ -759,8 +691,7 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
     const bool vectors = aligned(a);
     if (a.dim <= LN_ROW) {
-        if (vectors) return rows_forward<T, V, false>(c, a, st);
-        return rows_forward<T, V, true>(c, a, st);
+        return vectors ? rows_forward<T, V>(c, a, st) : rows_forward<T, 1>(c, a, st);
     }
     const int64_t most = (int64_t)c->sm_count * 4;
     const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
@@ -768,13 +699,13 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     return qg_launch(c, k_ln_long<T, 1>, grid, LN_THREADS, 0, st, a);
 }
 
-template <typename T, int V, int N, bool MULTI, bool EXACT, bool LOOSE>
+template <typename T, int V, int N, bool MULTI, bool EXACT>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     constexpr int R = LN_PAIR<N * V, MULTI>;
-    constexpr auto kernel = k_ln_rows_backward<T, V, N, MULTI, EXACT, LOOSE>;
+    constexpr auto kernel = k_ln_rows_backward<T, V, N, MULTI, EXACT>;
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
-    const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, LOOSE, R, LN_AHEAD_BACKWARD<T, R, LOOSE>>::bytes(threads, lanes) + (LOOSE ? 2 * 16 * N * threads : 0);
-    const size_t smem = (size_t)(a.dim + V - 1) / V * V * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
+    const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
+    const size_t smem = (size_t)lanes * N * V * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = 0;
     QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
@@ -792,9 +723,9 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     return qg_ws_close(c, st);
 }
 
-template <typename T, int V, bool LOOSE>
+template <typename T, int V>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    return rows_cut<V, LOOSE>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value, LOOSE>(c, a, lanes, st); });
+    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
 }
 
 template <typename T>
@@ -802,8 +733,7 @@ int backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
     const bool vectors = aligned(a);
     if (a.dim <= LN_ROW) {
-        if (vectors) return rows_backward<T, V, false>(c, a, st);
-        return rows_backward<T, V, true>(c, a, st);
+        return vectors ? rows_backward<T, V>(c, a, st) : rows_backward<T, 1>(c, a, st);
     }
     if (a.d_weight || a.d_bias) {
         // before the rows' gradients, which may take the place of an input
