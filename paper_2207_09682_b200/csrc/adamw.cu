@@ -18,18 +18,22 @@ constexpr int AW_THREADS = PACKED ? 128 : 256;
 template <bool PACKED>
 constexpr int AW_RESIDENT = PACKED ? 5 : 2;
 constexpr int AW_BLOCK = 256;                    // elements that share exponents: 8 per lane
-constexpr int AW_SMALL = 16, AW_MEDIUM = 64, AW_LARGE = 400;     // tensors per launch (parameters of 1.1, 4 or 25 KB)
+constexpr int AW_SMALL = 16, AW_MEDIUM = 56, AW_LARGE = 400;     // tensors per launch (parameters of 1.2, 3.9 or 27 KB)
 constexpr unsigned AW_CODES_M = 897, AW_CODES_V = 769;
 
-// Types in `what`: bits 0-1 parameter, 2-3 gradient, 4-5 copy; bit 6: vectors.
+// A tensor.  Types in the upper bits of `count`: bits 48-49 parameter, 50-51 gradient, 52-53 copy; bit 54: vectors.  (What a warp reads
+// of a tensor is neighbouring in the kernel's parameters: it comes from memory, with as many misses as there are lines.)
+struct alignas(64) AdamwEntry {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    uint8_t *exponents;
+    void *copy;
+    long long count;
+};
 template <int CAP>
 struct AdamwTable {
-    void *param[CAP];
-    const void *grad[CAP];
-    void *m[CAP], *v[CAP];
-    uint8_t *exponents[CAP];
-    void *copy[CAP];
-    long long count[CAP];     // elements | what << 48
+    AdamwEntry entry[CAP];
     unsigned first[CAP];      // first block of 256 of this launch
     int n;
     unsigned blocks;
@@ -418,11 +422,11 @@ __global__ void __launch_bounds__(AW_THREADS<PACKED>, AW_RESIDENT<PACKED>) k_ada
         const unsigned end = min(t.blocks, block + per);
         for (int i = aw_find(t, block); block < end; ++i) {
             const int run = (int)((i + 1 < t.n ? min(end, t.first[i + 1]) : end) - block);   // of this tensor's blocks
-            const int what = (int)(t.count[i] >> 48);
-            const AwTensor one{t.param[i], t.copy[i], t.m[i], t.v[i], t.grad[i], what & 3, what >> 2 & 3, what >> 4 & 3};
-            const int64_t at = (int64_t)(block - t.first[i]) * AW_BLOCK, count = (t.count[i] & ((1ll << 48) - 1)) - at;
+            const int what = (int)(t.entry[i].count >> 48);
+            const AwTensor one{t.entry[i].param, t.entry[i].copy, t.entry[i].m, t.entry[i].v, t.entry[i].grad, what & 3, what >> 2 & 3, what >> 4 & 3};
+            const int64_t at = (int64_t)(block - t.first[i]) * AW_BLOCK, count = (t.entry[i].count & ((1ll << 48) - 1)) - at;
             const int whole = !(what & 64) ? 0 : count >= (int64_t)run * AW_BLOCK ? run : (int)(count / AW_BLOCK);
-            uint8_t *const exponents = t.exponents[i] + at / AW_BLOCK * 2 + lane;
+            uint8_t *const exponents = t.entry[i].exponents + at / AW_BLOCK * 2 + lane;
             unsigned held = PACKED && lane < 2 * run ? *exponents : 0;
             const unsigned number = t.number + block;
             if (whole > 0) {
@@ -459,11 +463,11 @@ __global__ void __launch_bounds__(AW_THREADS<false>) k_adamw_values(const __grid
         const unsigned end = min(t.blocks, block + per);
         for (int i = aw_find(t, block); block < end; ++i) {
             const int run = (int)((i + 1 < t.n ? min(end, t.first[i + 1]) : end) - block);
-            const int what = (int)(t.count[i] >> 48), type = what & 3;
-            const uint8_t *const pm = reinterpret_cast<const uint8_t *>(t.m[i]), *const pv = reinterpret_cast<const uint8_t *>(t.v[i]);
+            const int what = (int)(t.entry[i].count >> 48), type = what & 3;
+            const uint8_t *const pm = reinterpret_cast<const uint8_t *>(t.entry[i].m), *const pv = reinterpret_cast<const uint8_t *>(t.entry[i].v);
             int64_t at = (int64_t)(block - t.first[i]) * AW_BLOCK;
-            const int64_t count = (t.count[i] & ((1ll << 48) - 1)) - at;
-            const unsigned held = lane < 2 * run ? t.exponents[i][at / AW_BLOCK * 2 + lane] : 0;
+            const int64_t count = (t.entry[i].count & ((1ll << 48) - 1)) - at;
+            const unsigned held = lane < 2 * run ? t.entry[i].exponents[at / AW_BLOCK * 2 + lane] : 0;
 #pragma unroll 2
             for (int k = 0; k < run; ++k, at += AW_BLOCK) {
                 const int64_t left = count - (int64_t)k * AW_BLOCK;
@@ -488,14 +492,14 @@ __global__ void __launch_bounds__(AW_THREADS<false>) k_adamw_values(const __grid
 #pragma unroll
                 for (int j = 0; j < AW_EACH; ++j) m[j] *= power[0], v[j] *= power[1];
                 if (vectors) {
-                    if (type == QGBDT_F32) aw_write<true>(t.param[i], mine, m, false), aw_write<true>(t.copy[i], mine, v, false);
-                    else aw_write<false>(t.param[i], mine, m, true), aw_write<false>(t.copy[i], mine, v, true);
+                    if (type == QGBDT_F32) aw_write<true>(t.entry[i].param, mine, m, false), aw_write<true>(t.entry[i].copy, mine, v, false);
+                    else aw_write<false>(t.entry[i].param, mine, m, true), aw_write<false>(t.entry[i].copy, mine, v, true);
                 } else {
 #pragma unroll
                     for (int j = 0; j < AW_EACH; ++j) {
                         if (lane + 32 * j >= n) continue;
-                        aw_store(t.param[i], type, mine + 32 * j, m[j]);
-                        aw_store(t.copy[i], type, mine + 32 * j, v[j]);
+                        aw_store(t.entry[i].param, type, mine + 32 * j, m[j]);
+                        aw_store(t.entry[i].copy, type, mine + 32 * j, v[j]);
                     }
                 }
             }
@@ -514,7 +518,7 @@ void aw_fill(AdamwTable<CAP> &t, int32_t &at, int64_t &done, int32_t n, unsigned
         const int64_t count = fill(t, t.n, at, done);
         if (count > 0) {
             const int64_t blocks = (count + AW_BLOCK - 1) / AW_BLOCK, room = most - t.blocks, here = blocks < room ? blocks : room;
-            t.count[t.n] |= here < blocks ? here * AW_BLOCK : count;
+            t.entry[t.n].count |= here < blocks ? here * AW_BLOCK : count;
             t.first[t.n++] = t.blocks;
             t.blocks += (unsigned)here;
             done += here * AW_BLOCK;
@@ -556,14 +560,14 @@ int aw_run(qgbdt_ctx *c, const qgbdt_adamw_tensor *in, int32_t n, const AdamwFac
             const qgbdt_adamw_tensor &a = in[i];
             const int64_t state = PACKED ? 1 : 4;
             auto moved = [from](const void *p, int64_t width) { return const_cast<char *>(reinterpret_cast<const char *>(p)) + from * width; };
-            t.param[k] = moved(a.param, qg_type_size(a.param_type));
-            t.grad[k] = moved(a.grad, qg_type_size(a.grad_type));
-            t.m[k] = moved(a.exp_avg, state), t.v[k] = moved(a.exp_avg_sq, state);
-            t.exponents[k] = PACKED ? a.exponents + from / AW_BLOCK * 2 : nullptr;
-            t.copy[k] = a.copy ? moved(a.copy, qg_type_size(a.copy_type)) : nullptr;
-            const bool vectors = aw_whole(t.param[k], qg_type_size(a.param_type)) && aw_whole(t.grad[k], qg_type_size(a.grad_type)) && aw_whole(t.m[k], state) &&
-                                 aw_whole(t.v[k], state) && (!a.copy || aw_whole(t.copy[k], qg_type_size(a.copy_type)));
-            t.count[k] = (long long)(a.param_type | a.grad_type << 2 | (a.copy ? a.copy_type : 0) << 4 | (vectors ? 64 : 0)) << 48;
+            t.entry[k].param = moved(a.param, qg_type_size(a.param_type));
+            t.entry[k].grad = moved(a.grad, qg_type_size(a.grad_type));
+            t.entry[k].m = moved(a.exp_avg, state), t.entry[k].v = moved(a.exp_avg_sq, state);
+            t.entry[k].exponents = PACKED ? a.exponents + from / AW_BLOCK * 2 : nullptr;
+            t.entry[k].copy = a.copy ? moved(a.copy, qg_type_size(a.copy_type)) : nullptr;
+            const bool vectors = aw_whole(t.entry[k].param, qg_type_size(a.param_type)) && aw_whole(t.entry[k].grad, qg_type_size(a.grad_type)) && aw_whole(t.entry[k].m, state) &&
+                                 aw_whole(t.entry[k].v, state) && (!a.copy || aw_whole(t.entry[k].copy, qg_type_size(a.copy_type)));
+            t.entry[k].count = (long long)(a.param_type | a.grad_type << 2 | (a.copy ? a.copy_type : 0) << 4 | (vectors ? 64 : 0)) << 48;
             return a.count - from;
         });
         if (t.blocks == 0) continue;
@@ -585,11 +589,11 @@ int aw_values(qgbdt_ctx *c, const uint8_t *const *m, const uint8_t *const *v, co
     while (at < n) {
         aw_fill(t, at, done, n, number, [&](AdamwTable<CAP> &t, int k, int32_t i, int64_t from) -> int64_t {
             const int w = qg_type_size(type);
-            t.m[k] = const_cast<uint8_t *>(m[i]) + from, t.v[k] = const_cast<uint8_t *>(v[i]) + from;
-            t.exponents[k] = const_cast<uint8_t *>(exponents[i]) + from / AW_BLOCK * 2;
-            t.param[k] = reinterpret_cast<char *>(out_m[i]) + from * w, t.copy[k] = reinterpret_cast<char *>(out_v[i]) + from * w;
-            const bool vectors = aw_whole(t.param[k], w) && aw_whole(t.copy[k], w) && aw_whole(t.m[k], 1) && aw_whole(t.v[k], 1);
-            t.count[k] = (long long)(type | (vectors ? 64 : 0)) << 48;
+            t.entry[k].m = const_cast<uint8_t *>(m[i]) + from, t.entry[k].v = const_cast<uint8_t *>(v[i]) + from;
+            t.entry[k].exponents = const_cast<uint8_t *>(exponents[i]) + from / AW_BLOCK * 2;
+            t.entry[k].param = reinterpret_cast<char *>(out_m[i]) + from * w, t.entry[k].copy = reinterpret_cast<char *>(out_v[i]) + from * w;
+            const bool vectors = aw_whole(t.entry[k].param, w) && aw_whole(t.entry[k].copy, w) && aw_whole(t.entry[k].m, 1) && aw_whole(t.entry[k].v, 1);
+            t.entry[k].count = (long long)(type | (vectors ? 64 : 0)) << 48;
             return counts[i] - from;
         });
         if (t.blocks == 0) continue;
