@@ -181,9 +181,18 @@ __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a,
 // Instructions bound these kernels as soon as the memory does not: sums and products are taken of two elements at once,
 // and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
 
-constexpr int LN_EACH = 16;      // elements of a row per thread, at most
-constexpr int LN_MOST = 512;     // threads of a row, at most
-constexpr int LN_ROW = LN_EACH * LN_MOST;
+constexpr int LN_ROW = 8192;     // elements of a row, at most
+constexpr int LN_EACH = 16;      // per thread of a warp that has rows of its own, at most
+// Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32 (two thirds of the instructions of 16 go
+// into elements at 8192 columns, the rest into sums and loops: 92 instead of 100 us for 16384 rows; f32: no difference).  Backward: 16, and
+// 8 of rows above 2048 columns, whose threads then come to 32 instead of 16 warps of an SM (7324 x 4096 bf16: 48 instead of 54 us;
+// 14648 x 2048: 48 instead of 44).
+template <typename T, int V>
+constexpr int LN_MANY = V > 1 && sizeof(T) == 2 ? 32 : 16;
+constexpr int LN_WIDE = 2048;
+// Threads that the registers of a row's threads leave room for, single elements forward: two rows of up to 5120 columns on an SM
+// (5998 x 5001 bf16: 44 us; with registers for 512 threads 72 us at 4097 columns, here 51).
+constexpr int LN_LOOSE = 640;
 template <int E, bool MULTI>
 constexpr int LN_PAIR = !MULTI && E <= 8 ? 2 : 1;    // rows at a time
 
@@ -376,7 +385,7 @@ constexpr int LN_AHEAD_BACKWARD = ROWS == 1 ? 3 : 2;
 //   sum over warps of M2 + count (mean of the warp - mean)^2,
 // which takes one exchange and loses nothing where the mean is large beside the differences.
 template <typename T, int V, int N, bool MULTI, bool EXACT>
-__global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && V > 1 ? 2 : 1) k_ln_rows(const LayerNormArgs a, int lanes) {
+__global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_ROW / (N * V) : LN_LOOSE) : 128, MULTI && V > 1 ? 2 : 1) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
@@ -490,7 +499,7 @@ __global__ void __launch_bounds__(MULTI ? LN_MOST : 128, MULTI && V > 1 ? 2 : 1)
 // The gradients; the sums over the rows are gathered by column in registers, joined in shared memory over the block's groups and
 // written as the block's part of partial [blocks][2][dim], or, from a single block, as they are.
 template <typename T, int V, int N, bool MULTI, bool EXACT>
-__global__ void __launch_bounds__(MULTI ? LN_MOST : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
+__global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
@@ -655,7 +664,7 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
 
 // How a row is cut up: calls `with` with N, MULTI, EXACT and the threads of a row.  Vectors: one per thread up to a warp's worth, then
 // LN_EACH elements; single elements: four, eight or LN_EACH; then more warps.
-template <int V, typename F>
+template <int V, int MANY, typename F>
 int rows_cut(int dim, F with) {
     constexpr int most = LN_EACH / V;
     const int vectors = (dim + V - 1) / V;
@@ -674,16 +683,17 @@ int rows_cut(int dim, F with) {
         if (vectors <= 32 * 8) return few(std::integral_constant<int, 8>{});
     }
     if (vectors <= 32 * most) return few(std::integral_constant<int, most>{});
-    const int lanes = (vectors + 32 * most - 1) / (32 * most) * 32;
+    constexpr int many = MANY / V;
+    const int lanes = (vectors + 32 * many - 1) / (32 * many) * 32;
     if constexpr (V > 1) {
-        if (dim == lanes * LN_EACH) return with(std::integral_constant<int, most>{}, std::true_type{}, std::true_type{}, lanes);
+        if (dim == lanes * MANY) return with(std::integral_constant<int, many>{}, std::true_type{}, std::true_type{}, lanes);
     }
-    return with(std::integral_constant<int, most>{}, std::true_type{}, std::false_type{}, lanes);
+    return with(std::integral_constant<int, many>{}, std::true_type{}, std::false_type{}, lanes);
 }
 
 template <typename T, int V>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
+    return rows_cut<V, LN_MANY<T, V>>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_forward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
 }
 
 template <typename T>
@@ -725,7 +735,11 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
 
 template <typename T, int V>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
-    return rows_cut<V>(a.dim, [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); });
+    auto cut = [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); };
+    if constexpr (V > 1) {
+        if (a.dim > LN_WIDE) return rows_cut<V, 8>(a.dim, cut);
+    }
+    return rows_cut<V, 16>(a.dim, cut);
 }
 
 template <typename T>
