@@ -717,12 +717,17 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
     const size_t smem = (size_t)lanes * N * V * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    int64_t grid = 0;
-    QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
-    // four rows per group at least: the partial sums are as large as one and a half
-    const int64_t want = (a.rows + groups * 4 - 1) / (groups * 4);
-    if (want < grid) grid = want;
-    if (grid < 1) grid = 1;
+    // Few steps: one block, which needs no other launch to join anything.  As many blocks as there are steps up to one per
+    // SM; beyond that four rows per group at least, since the partial sums are as large as one and a half.
+    const int64_t steps = (a.rows + groups * R - 1) / (groups * R), fours = (a.rows + groups * 4 - 1) / (groups * 4);
+    int64_t want = steps < c->sm_count ? steps : c->sm_count;
+    if (want < fours) want = fours;
+    if (steps <= (V > 1 ? 4 : 2)) want = 1;
+    int64_t grid = want;
+    if (want > c->sm_count) {
+        QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
+        if (want < grid) grid = want;
+    }
     const bool sums = a.d_weight || a.d_bias;
     if (!sums || grid == 1) return qg_launch(c, kernel, dim3((unsigned)grid), threads, smem, st, a, (float *)nullptr, lanes);
     QgWorkspace ws;
