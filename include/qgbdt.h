@@ -416,8 +416,9 @@ int qgbdt_layer_norm_backward(qgbdt_ctx *ctx, const void *d_grad, int64_t ld_gra
  * d_norm: the gradients' norm as qgbdt_clip_grad_norm reports it for these gradients (NULL: no clipping);
  * where it is not finite nothing at all is written.  loss_scale: what the loss was multiplied with.
  * d_lr, d_step: one number in device memory in place of lr or step (NULL: those), for a captured call.
- * Tensors are contiguous; count may be 0.  A tensor of parameters may be listed once only; exp_avg,
- * exp_avg_sq, exponents and copy are written and must not overlap anything else.  No work buffer is used.
+ * Tensors are contiguous; count may be 0.  A tensor of parameters may be listed once only, and what
+ * belongs to one tensor must not overlap (both are refused); nor may what is written of it (param, exp_avg,
+ * exp_avg_sq, exponents, copy) overlap another one's (not checked).  No work buffer is used.
  *
  * state_bits 32: exp_avg and exp_avg_sq [count] are floats.
  * state_bits 8: they are bytes, zeros before the first step, with `exponents` [ceil(count / 256)][2], also

@@ -83,6 +83,15 @@ int check_adamw(qgbdt_ctx *c, const qgbdt_adamw_tensor *t, int32_t n, const qgbd
         if (!qg_aligned(a.param, qg_type_size(a.param_type)) || !qg_aligned(a.grad, qg_type_size(a.grad_type)) || !qg_aligned(a.exp_avg, state) ||
             !qg_aligned(a.exp_avg_sq, state) || (a.copy && !qg_aligned(a.copy, qg_type_size(a.copy_type))))
             return qg_fail(c, QGBDT_ERR_ARG, "tensor %d is not aligned to its element", i);
+        // what the step writes of this tensor, and the gradient that it reads
+        const void *const at[] = {a.param, a.exp_avg, a.exp_avg_sq, a.copy, packed ? a.exponents : nullptr, a.grad};
+        const int64_t bytes[] = {a.count * qg_type_size(a.param_type), a.count * state, a.count * state, a.count * qg_type_size(a.copy_type), (a.count + 255) / 256 * 2,
+                                 a.count * qg_type_size(a.grad_type)};
+        for (int j = 0; j < 6; ++j)
+            for (int k = 0; k < j; ++k)
+                if (at[j] && at[k] && reinterpret_cast<uintptr_t>(at[j]) < reinterpret_cast<uintptr_t>(at[k]) + (uintptr_t)bytes[k] &&
+                    reinterpret_cast<uintptr_t>(at[k]) < reinterpret_cast<uintptr_t>(at[j]) + (uintptr_t)bytes[j])
+                    return qg_fail(c, QGBDT_ERR_ARG, "tensor %d: parameters, gradient, states and copy overlap", i);
         blocks += (a.count + 255) / 256;
         if (blocks >= (1ll << 32)) return qg_fail(c, QGBDT_ERR_ARG, "the tensors have 2^40 elements or more together");
     }

@@ -76,7 +76,7 @@ struct Step {
         o.lr = 0.1, o.beta1 = 0.9, o.beta2 = 0.999, o.eps = 1e-8, o.max_norm = 1.0, o.loss_scale = 1.0, o.step = 1, o.state_bits = 32;
         for (int i = 0; i < 3; ++i) {
             qgbdt_adamw_tensor a{};
-            a.param = P + 4096 * i, a.grad = P, a.exp_avg = P, a.exp_avg_sq = P, a.count = 1000, a.param_type = QGBDT_F32, a.grad_type = QGBDT_BF16;
+            a.param = P + 4096 * i, a.grad = P + 0x20000, a.exp_avg = P + 0x30000, a.exp_avg_sq = P + 0x40000, a.count = 1000, a.param_type = QGBDT_F32, a.grad_type = QGBDT_BF16;
             a.copy_type = 77;   // of no meaning without a copy
             t.push_back(a);
         }
@@ -156,7 +156,7 @@ int main() {
         e = s;
         e.o.state_bits = 8;
         REFUSED(e.run());   // without exponents
-        for (qgbdt_adamw_tensor &a : e.t) a.exponents = reinterpret_cast<uint8_t *>(P + 1), a.exp_avg = P + 1, a.exp_avg_sq = P + 3;
+        for (qgbdt_adamw_tensor &a : e.t) a.exponents = reinterpret_cast<uint8_t *>(P + 0x50001), a.exp_avg = P + 0x30001, a.exp_avg_sq = P + 0x40003;
         TAKEN(e.run());
         e = s;
         std::swap(e.t[0].param, e.t[2].param);   // in any order
@@ -171,8 +171,11 @@ int main() {
         expect(e.run() == QGBDT_ERR_ALLOC, __LINE__, "no host memory is an error code");
         no_memory = false;
         e = s;
-        for (qgbdt_adamw_tensor &a : e.t) a.count = 1ll << 39;   // too many together
-        e.t[1].param = P + (1ll << 43), e.t[2].param = P + (1ll << 44);
+        for (int i = 0; i < 3; ++i) {   // too many together
+            qgbdt_adamw_tensor &a = e.t[(size_t)i];
+            char *const at = P + ((int64_t)(i + 1) << 46);
+            a.count = 1ll << 39, a.param = at, a.grad = at + (1ll << 43), a.exp_avg = at + (2ll << 43), a.exp_avg_sq = at + (3ll << 43);
+        }
         REFUSED(e.run());
         e.t.pop_back();
         REFUSED(e.run());   // 2^40 elements
@@ -207,8 +210,15 @@ int main() {
     for (int32_t v : {-1, 3}) {
         REFUSED(s.with(&qgbdt_adamw_tensor::param_type, v).run());
         REFUSED(s.with(&qgbdt_adamw_tensor::grad_type, v).run());
-        REFUSED(s.with(&qgbdt_adamw_tensor::copy, P).with(&qgbdt_adamw_tensor::copy_type, v).run());
+        REFUSED(s.with(&qgbdt_adamw_tensor::copy, P + 0x60000).with(&qgbdt_adamw_tensor::copy_type, v).run());
     }
+    // what belongs to one tensor overlaps: the first and the last byte
+    for (char *at : {P + 0x30000, P + 0x30000 + 3996, P + 0x30000 - 3996, P + 4096, P + 0x20000}) REFUSED(s.with(&qgbdt_adamw_tensor::exp_avg_sq, at).run());
+    TAKEN(s.with(&qgbdt_adamw_tensor::exp_avg_sq, P + 0x30000 + 4000).run());
+    TAKEN(s.with(&qgbdt_adamw_tensor::exp_avg_sq, P + 0x30000 - 4000).run());
+    REFUSED(s.with(&qgbdt_adamw_tensor::copy, P + 4096).with(&qgbdt_adamw_tensor::copy_type, QGBDT_F32).run());
+    REFUSED(s.with(&qgbdt_adamw_tensor::copy, P + 4096 - 1998).with(&qgbdt_adamw_tensor::copy_type, QGBDT_BF16).run());
+    TAKEN(s.with(&qgbdt_adamw_tensor::copy, P + 0x60000).with(&qgbdt_adamw_tensor::copy_type, QGBDT_BF16).run());
     REFUSED(s.with(&qgbdt_adamw_tensor::count, -1).run());
     REFUSED(s.with(&qgbdt_adamw_tensor::param, nullptr).run());
     REFUSED(s.with(&qgbdt_adamw_tensor::grad, nullptr).run());

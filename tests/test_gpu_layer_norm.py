@@ -304,6 +304,16 @@ def test_bookkeeping(ctx):
     assert out._version == 1 and x._version == 0
     ctx.layer_norm_backward(g, x, r.mean, r.rstd, w, grad_x=out)
     assert out._version == 2 and g._version == 0
+    # mean and rstd lie in one buffer, but are tensors of their own
+    assert r.mean._version == r.rstd._version == 0 and not r.mean.requires_grad and r.mean.is_contiguous() and r.rstd.is_contiguous()
+    was = r.rstd.clone()
+    r.mean.add_(0.0)
+    assert r.mean._version == 1 and r.rstd._version == 0 and torch.equal(r.rstd, was)
+    scale = torch.ones(5, device="cuda", requires_grad=True)
+    (r.mean * scale).sum().backward()
+    assert torch.equal(scale.grad, r.mean)
+    with torch.inference_mode():
+        assert torch.equal(ctx.layer_norm(x, w, b).out, r.out)
     leaf = w.clone().requires_grad_()
     with pytest.warns(UserWarning, match="weight requires a gradient"):
         assert not ctx.layer_norm(x, leaf, b).out.requires_grad
