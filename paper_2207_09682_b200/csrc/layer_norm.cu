@@ -10,11 +10,14 @@
 
 namespace {
 
-// ---- rows of any length ----------------------------------------------------------------------------
-// A block per row, which goes over the row once for each of its sums and once more to write (the later
-// times from L1 or L2).
+// ---- rows longer than a block's registers -----------------------------------------------------------
+// A row is cut into segments of LN_SEGMENT elements, so that few long rows occupy the GPU too.  A first launch takes every
+// segment's share of the row's sums (forward: mean and sum of squared differences from it, backward: sums of w g and w g xh), a second one
+// joins the shares of the row in their order, in every block that needs them, and writes.  Inputs are read twice, the
+// second time from L2 where they fit: 1.5 times the bytes forward, 1.67 backward.
 
-constexpr int LN_THREADS = 512;
+constexpr int LN_THREADS = 256, LN_PIECE = 16;      // elements per thread
+constexpr int LN_SEGMENT = LN_THREADS * LN_PIECE;
 
 // Sums of a and b over the block, the same in every thread, in a fixed order.  `at` alternates between two
 // places of the shared memory, so that one barrier per sum is enough.
@@ -38,111 +41,151 @@ __device__ __forceinline__ float ln_weight(const void *w, bool f32, int col, flo
     return f32 ? reinterpret_cast<const float *>(w)[col] : OpsType<T>::load(reinterpret_cast<const T *>(w)[col]);
 }
 
+// A thread's elements of a segment: vectors tid, tid + LN_THREADS, ...; zeros outside the row.  V = 1: rows that start anywhere.
 template <typename T, int V>
-__global__ void __launch_bounds__(LN_THREADS) k_ln_long(const LayerNormArgs a) {
+struct LnPiece {
+    static constexpr int N = LN_PIECE / V;
+    OpsVec<T, V> v[N];
+    __device__ __forceinline__ static int column(int i) { return (i * LN_THREADS + (int)threadIdx.x) * V; }
+    __device__ __forceinline__ void load(const void *p, int64_t at, int n) {      // n: elements of the segment
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            v[i] = OpsVec<T, V>{};
+            if (column(i) < n) v[i] = *reinterpret_cast<const OpsVec<T, V> *>(reinterpret_cast<const T *>(p) + at + column(i));
+        }
+    }
+    __device__ __forceinline__ void store(void *p, int64_t at, int n) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (column(i) < n) *reinterpret_cast<OpsVec<T, V> *>(reinterpret_cast<T *>(p) + at + column(i)) = v[i];
+    }
+    __device__ __forceinline__ float get(int e) const { return OpsType<T>::load(v[e / V].v[e % V]); }
+    __device__ __forceinline__ void set(int e, float x) { v[e / V].v[e % V] = OpsType<T>::store(x); }
+    __device__ __forceinline__ static int place(int e) { return column(e / V) + e % V; }
+};
+
+// Elements of segment i of a row.
+__device__ __forceinline__ int ln_segment(int dim, int i) { return min(LN_SEGMENT, dim - i * LN_SEGMENT); }
+
+// The columns' weights of a thread's elements of a segment, of n elements from column `first` on; zeros outside the row.
+template <typename T, int V>
+__device__ __forceinline__ void ln_weights(float (&w)[LN_PIECE], const void *weight, bool f32, int first, int n, float none) {
+#pragma unroll
+    for (int e = 0; e < LN_PIECE; ++e) w[e] = LnPiece<T, V>::place(e) < n ? ln_weight<T>(weight, f32, first + LnPiece<T, V>::place(e), none) : 0.f;
+}
+
+// A block has a segment (blockIdx.x) of every gridDim.y-th row, so that the columns' weights stay in registers.
+template <typename T, int V, bool BACKWARD>
+__global__ void __launch_bounds__(LN_THREADS) k_ln_shares(const LayerNormArgs a, float2 *shares, int segments) {
     qg_after_prior();
-    __shared__ float2 w[2][32];
+    __shared__ float2 part[2][32];
     int at = 0;
-    const bool f32 = a.weight_type == QGBDT_F32;
-    const float per = 1.f / (float)a.dim;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T *x = reinterpret_cast<const T *>(a.x) + row * a.ld_x;
-        T *out = reinterpret_cast<T *>(a.out) + row * a.ld_out;
+    const int segment = blockIdx.x, n = ln_segment(a.dim, segment), first = segment * LN_SEGMENT;
+    float w[LN_PIECE];
+    if (BACKWARD) ln_weights<T, V>(w, a.weight, a.weight_type == QGBDT_F32, first, n, 1.f);
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        LnPiece<T, V> x;
+        x.load(a.x, row * a.ld_x + first, n);
         float2 s = make_float2(0.f, 0.f);
-        for (int c = threadIdx.x * V; c < a.dim; c += LN_THREADS * V) {
-            const OpsVec<T, V> v = *reinterpret_cast<const OpsVec<T, V> *>(x + c);
+        if constexpr (!BACKWARD) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) s.x += OpsType<T>::load(v.v[j]);
-        }
-        const float mean = ln_block_sum(s, w, at).x * per;
-        s = make_float2(0.f, 0.f);
-        for (int c = threadIdx.x * V; c < a.dim; c += LN_THREADS * V) {
-            const OpsVec<T, V> v = *reinterpret_cast<const OpsVec<T, V> *>(x + c);
+            for (int e = 0; e < LN_PIECE; ++e) s.x += x.get(e);
+            const float mean = ln_block_sum(s, part, at).x / (float)n;
+            s.x = 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float y = OpsType<T>::load(v.v[j]) - mean;
-                s.x = fmaf(y, y, s.x);
+            for (int e = 0; e < LN_PIECE; ++e) {
+                const float y = x.get(e) - mean;
+                if (x.place(e) < n) s.x = fmaf(y, y, s.x);
             }
-        }
-        const float rstd = __frsqrt_rn(fmaf(ln_block_sum(s, w, at).x, per, a.eps));
-        for (int c = threadIdx.x * V; c < a.dim; c += LN_THREADS * V) {
-            OpsVec<T, V> v = *reinterpret_cast<const OpsVec<T, V> *>(x + c);
+            s = ln_block_sum(s, part, at);
+            if (threadIdx.x == 0) shares[row * segments + segment] = make_float2(mean, s.x);
+        } else {
+            const float mean = a.mean[row], rstd = a.rstd[row];
+            LnPiece<T, V> u;
+            u.load(a.grad, row * a.ld_grad + first, n);
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                v.v[j] = OpsType<T>::store(fmaf((OpsType<T>::load(v.v[j]) - mean) * rstd, ln_weight<T>(a.weight, f32, c + j, 1.f), ln_weight<T>(a.bias, f32, c + j, 0.f)));
-            *reinterpret_cast<OpsVec<T, V> *>(out + c) = v;
+            for (int e = 0; e < LN_PIECE; ++e) {
+                const float y = u.get(e) * w[e];      // zero outside the row
+                s.x += y;
+                s.y = fmaf(y, (x.get(e) - mean) * rstd, s.y);
+            }
+            s = ln_block_sum(s, part, at);
+            if (threadIdx.x == 0) shares[row * segments + segment] = s;
         }
-        if (threadIdx.x == 0) {
+    }
+}
+
+__device__ __forceinline__ float ln_warp_sum(float s) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    return s;
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(LN_THREADS) k_ln_segments(const LayerNormArgs a, const float2 *shares, int segments) {
+    qg_after_prior();
+    const bool f32 = a.weight_type == QGBDT_F32;
+    const int lane = threadIdx.x & 31, segment = blockIdx.x, n = ln_segment(a.dim, segment), first = segment * LN_SEGMENT;
+    const float per = 1.f / (float)a.dim;
+    float w[LN_PIECE], b[LN_PIECE];
+    ln_weights<T, V>(w, a.weight, f32, first, n, 1.f);
+    ln_weights<T, V>(b, a.bias, f32, first, n, 0.f);
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        LnPiece<T, V> x;
+        x.load(a.x, row * a.ld_x + first, n);
+        const float2 *const of = shares + row * segments;
+        float s = 0.f;
+        for (int i = lane; i < segments; i += 32) s = fmaf(of[i].x, (float)ln_segment(a.dim, i), s);
+        const float mean = ln_warp_sum(s) * per;
+        s = 0.f;
+        for (int i = lane; i < segments; i += 32) {
+            const float z = of[i].x - mean;
+            s += fmaf(z * (float)ln_segment(a.dim, i), z, of[i].y);
+        }
+        const float rstd = rsqrtf(fmaf(ln_warp_sum(s), per, a.eps));
+#pragma unroll
+        for (int e = 0; e < LN_PIECE; ++e) x.set(e, fmaf((x.get(e) - mean) * rstd, w[e], b[e]));
+        x.store(a.out, row * a.ld_out + first, n);
+        if (segment == 0 && threadIdx.x == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
     }
 }
 
+// A block has a segment of a slice of the rows, and the sums over those rows: partial [slices][2][dim] (of the weight's gradient, of
+// the bias's).
 template <typename T, int V>
-__global__ void __launch_bounds__(LN_THREADS) k_ln_long_dx(const LayerNormArgs a) {
+__global__ void __launch_bounds__(LN_THREADS, 2) k_ln_segments_backward(const LayerNormArgs a, const float2 *shares, float *partial, int segments) {
     qg_after_prior();
-    __shared__ float2 w[2][32];
-    int at = 0;
-    const bool f32 = a.weight_type == QGBDT_F32;
+    const int lane = threadIdx.x & 31, segment = blockIdx.x, n = ln_segment(a.dim, segment), first = segment * LN_SEGMENT;
+    const int64_t r0 = a.rows * blockIdx.y / gridDim.y, r1 = a.rows * (blockIdx.y + 1) / gridDim.y;
     const float per = 1.f / (float)a.dim;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const T *x = reinterpret_cast<const T *>(a.x) + row * a.ld_x, *g = reinterpret_cast<const T *>(a.grad) + row * a.ld_grad;
-        T *out = reinterpret_cast<T *>(a.out) + row * a.ld_out;
+    float w[LN_PIECE], dw[LN_PIECE] = {}, db[LN_PIECE] = {};
+    ln_weights<T, V>(w, a.weight, a.weight_type == QGBDT_F32, first, n, 1.f);
+    for (int64_t row = r0; row < r1; ++row) {
+        LnPiece<T, V> x, u;
+        x.load(a.x, row * a.ld_x + first, n);
+        u.load(a.grad, row * a.ld_grad + first, n);
         const float mean = a.mean[row], rstd = a.rstd[row];
         float2 s = make_float2(0.f, 0.f);
-        for (int c = threadIdx.x * V; c < a.dim; c += LN_THREADS * V) {
-            const OpsVec<T, V> v = *reinterpret_cast<const OpsVec<T, V> *>(x + c), u = *reinterpret_cast<const OpsVec<T, V> *>(g + c);
+        for (int i = lane; i < segments; i += 32) s.x += shares[row * segments + i].x, s.y += shares[row * segments + i].y;
+        const float c1 = ln_warp_sum(s.x) * per, c2 = ln_warp_sum(s.y) * per;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float y = OpsType<T>::load(u.v[j]) * ln_weight<T>(a.weight, f32, c + j, 1.f);
-                s.x += y;
-                s.y = fmaf(y, (OpsType<T>::load(v.v[j]) - mean) * rstd, s.y);
-            }
+        for (int e = 0; e < LN_PIECE; ++e) {
+            const float g = u.get(e), xh = (x.get(e) - mean) * rstd;
+            dw[e] = fmaf(g, xh, dw[e]);      // (outside the row: never read)
+            db[e] += g;
+            u.set(e, (g * w[e] - c1 - xh * c2) * rstd);
         }
-        s = ln_block_sum(s, w, at);
-        const float c1 = s.x * per, c2 = s.y * per;
-        for (int c = threadIdx.x * V; c < a.dim; c += LN_THREADS * V) {
-            const OpsVec<T, V> v = *reinterpret_cast<const OpsVec<T, V> *>(x + c);
-            OpsVec<T, V> u = *reinterpret_cast<const OpsVec<T, V> *>(g + c);
+        u.store(a.out, row * a.ld_out + first, n);
+    }
+    if (!partial) return;
+    float *const to = partial + (int64_t)blockIdx.y * 2 * a.dim + first;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float y = OpsType<T>::load(u.v[j]) * ln_weight<T>(a.weight, f32, c + j, 1.f), xh = (OpsType<T>::load(v.v[j]) - mean) * rstd;
-                u.v[j] = OpsType<T>::store((y - c1 - xh * c2) * rstd);
-            }
-            *reinterpret_cast<OpsVec<T, V> *>(out + c) = u;
-        }
-    }
-}
-
-// Sums over a slice of the rows, 32 columns per block: partial [slices][2][dim] (of the weight's gradient, of the bias's).
-constexpr int LN_COLUMN_ROWS = 16;   // rows side by side
-
-template <typename T>
-__global__ void __launch_bounds__(32 * LN_COLUMN_ROWS) k_ln_columns(const LayerNormArgs a, float *partial) {
-    qg_after_prior();
-    __shared__ float2 w[LN_COLUMN_ROWS][32];
-    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
-    const int64_t r0 = a.rows * blockIdx.y / gridDim.y, r1 = a.rows * (blockIdx.y + 1) / gridDim.y;
-    float2 s = make_float2(0.f, 0.f);
-    if (c < a.dim) {
-#pragma unroll 4
-        for (int64_t r = r0 + part; r < r1; r += LN_COLUMN_ROWS) {
-            const float g = OpsType<T>::load(reinterpret_cast<const T *>(a.grad)[r * a.ld_grad + c]);
-            const float x = OpsType<T>::load(reinterpret_cast<const T *>(a.x)[r * a.ld_x + c]);
-            s.x = fmaf(g, (x - a.mean[r]) * a.rstd[r], s.x);
-            s.y += g;
-        }
-    }
-    w[part][lane] = s;
-    __syncthreads();
-    if (part == 0 && c < a.dim) {
-        s = w[0][lane];
-        for (int i = 1; i < LN_COLUMN_ROWS; ++i) s.x += w[i][lane].x, s.y += w[i][lane].y;
-        float *p = partial + (int64_t)blockIdx.y * 2 * a.dim + c;
-        p[0] = s.x;
-        p[a.dim] = s.y;
+    for (int e = 0; e < LN_PIECE; ++e) {
+        const int c = LnPiece<T, V>::place(e);
+        if (c < n) to[c] = dw[e], to[a.dim + c] = db[e];
     }
 }
 
@@ -173,6 +216,28 @@ __global__ void __launch_bounds__(32 * LN_JOIN) k_ln_join(const LayerNormArgs a,
         if (a.weight_type == QGBDT_F32) reinterpret_cast<float *>(out)[column] = s;
         else reinterpret_cast<T *>(out)[column] = OpsType<T>::store(s);
     }
+}
+
+// Few slices: a thread per column, of the weight's gradient and then of the bias's.
+constexpr int LN_FEW = 16;
+
+template <typename T>
+__global__ void __launch_bounds__(LN_THREADS) k_ln_join_few(const LayerNormArgs a, const float *partial, int slices) {
+    qg_after_prior();
+    const int64_t i = (int64_t)blockIdx.x * LN_THREADS + threadIdx.x, c = i < a.dim ? i : i - a.dim;
+    void *const out = i < a.dim ? a.d_weight : a.d_bias;
+    if (i >= 2 * (int64_t)a.dim || !out) return;
+    float s = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < slices; ++k) s += partial[(int64_t)k * 2 * a.dim + i];
+    if (a.weight_type == QGBDT_F32) reinterpret_cast<float *>(out)[c] = s;
+    else reinterpret_cast<T *>(out)[c] = OpsType<T>::store(s);
+}
+
+template <typename T>
+int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slices, cudaStream_t st) {
+    if (slices <= LN_FEW) return qg_launch(c, k_ln_join_few<T>, dim3((unsigned)((2 * (int64_t)a.dim + LN_THREADS - 1) / LN_THREADS)), LN_THREADS, 0, st, a, partial, slices);
+    return qg_launch(c, k_ln_join<T>, dim3((a.dim + 31) / 32, 2), 32 * LN_JOIN, 0, st, a, partial, slices);
 }
 
 // ---- rows that fit in registers ---------------------------------------------------------------------
@@ -637,6 +702,12 @@ bool aligned(const LayerNormArgs &a) {
            (!a.grad || qg_vec_bytes(a.grad, a.ld_grad * w, (int64_t)a.dim * w) == 16);
 }
 
+// Of the launches over segments: eight blocks per SM, or one for every segment of every row.
+dim3 ln_segments_grid(const qgbdt_ctx *c, int64_t rows, int segments) {
+    const int64_t most = ((int64_t)c->sm_count * 8 + segments - 1) / segments;
+    return dim3((unsigned)segments, (unsigned)(rows < 1 ? 1 : rows < most ? rows : most));
+}
+
 // Blocks of `threads` that the GPU holds at once.
 template <typename K>
 int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *blocks) {
@@ -703,10 +774,19 @@ int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     if (a.dim <= LN_ROW) {
         return vectors ? rows_forward<T, V>(c, a, st) : rows_forward<T, 1>(c, a, st);
     }
-    const int64_t most = (int64_t)c->sm_count * 4;
-    const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
-    if (vectors) return qg_launch(c, k_ln_long<T, V>, grid, LN_THREADS, 0, st, a);
-    return qg_launch(c, k_ln_long<T, 1>, grid, LN_THREADS, 0, st, a);
+    const int segments = (a.dim + LN_SEGMENT - 1) / LN_SEGMENT;
+    QgWorkspace ws;
+    QG_RUN(qg_ws_open(c, qg_ws_size((size_t)a.rows * segments, sizeof(float2)), st, &ws));
+    float2 *shares = ws.take<float2>((size_t)a.rows * segments);
+    const dim3 grid = ln_segments_grid(c, a.rows, segments);
+    if (vectors) {
+        QG_RUN(qg_launch(c, k_ln_shares<T, V, false>, grid, LN_THREADS, 0, st, a, shares, segments));
+        QG_RUN(qg_launch(c, k_ln_segments<T, V>, grid, LN_THREADS, 0, st, a, (const float2 *)shares, segments));
+    } else {
+        QG_RUN(qg_launch(c, k_ln_shares<T, 1, false>, grid, LN_THREADS, 0, st, a, shares, segments));
+        QG_RUN(qg_launch(c, k_ln_segments<T, 1>, grid, LN_THREADS, 0, st, a, (const float2 *)shares, segments));
+    }
+    return qg_ws_close(c, st);
 }
 
 template <typename T, int V, int N, bool MULTI, bool EXACT>
@@ -734,7 +814,7 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     QG_RUN(qg_ws_open(c, qg_ws_size((size_t)grid * 2 * a.dim, sizeof(float)), st, &ws));
     float *partial = ws.take<float>((size_t)grid * 2 * a.dim);
     QG_RUN(qg_launch(c, kernel, dim3((unsigned)grid), threads, smem, st, a, partial, lanes));
-    QG_RUN(qg_launch(c, k_ln_join<T>, dim3((a.dim + 31) / 32, 2), 32 * LN_JOIN, 0, st, a, partial, (int)grid));
+    QG_RUN(ln_join<T>(c, a, partial, (int)grid, st));
     return qg_ws_close(c, st);
 }
 
@@ -754,25 +834,25 @@ int backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     if (a.dim <= LN_ROW) {
         return vectors ? rows_backward<T, V>(c, a, st) : rows_backward<T, 1>(c, a, st);
     }
-    if (a.d_weight || a.d_bias) {
-        // before the rows' gradients, which may take the place of an input
-        const int tiles = (a.dim + 31) / 32;
-        int64_t slices = (a.rows + LN_COLUMN_ROWS * 8 - 1) / (LN_COLUMN_ROWS * 8);
-        const int64_t most = ((int64_t)c->sm_count * 8 + tiles - 1) / tiles;
-        if (slices > most) slices = most;
-        if (slices < 1) slices = 1;
-        QgWorkspace ws;
-        QG_RUN(qg_ws_open(c, qg_ws_size((size_t)slices * 2 * a.dim, sizeof(float)), st, &ws));
-        float *partial = ws.take<float>((size_t)slices * 2 * a.dim);
-        QG_RUN(qg_launch(c, k_ln_columns<T>, dim3(tiles, (unsigned)slices), 32 * LN_COLUMN_ROWS, 0, st, a, partial));
-        QG_RUN(qg_launch(c, k_ln_join<T>, dim3(tiles, 2), 32 * LN_JOIN, 0, st, a, partial, (int)slices));
-        QG_RUN(qg_ws_close(c, st));
+    const int segments = (a.dim + LN_SEGMENT - 1) / LN_SEGMENT;
+    const bool sums = a.d_weight || a.d_bias;
+    // two blocks per SM, of four rows each at least
+    int64_t slices = ((int64_t)c->sm_count * 2 + segments - 1) / segments, fours = (a.rows + 3) / 4;
+    if (slices > fours) slices = fours;
+    if (slices < 1) slices = 1;
+    QgWorkspace ws;
+    QG_RUN(qg_ws_open(c, qg_ws_size((size_t)a.rows * segments, sizeof(float2)) + qg_ws_size((size_t)slices * 2 * a.dim, sizeof(float)), st, &ws));
+    float2 *shares = ws.take<float2>((size_t)a.rows * segments);
+    float *partial = ws.take<float>((size_t)slices * 2 * a.dim);
+    const dim3 grid = ln_segments_grid(c, a.rows, segments), blocks((unsigned)segments, (unsigned)slices);
+    if (a.rows > 0) {
+        if (vectors) QG_RUN(qg_launch(c, k_ln_shares<T, V, true>, grid, LN_THREADS, 0, st, a, shares, segments));
+        else QG_RUN(qg_launch(c, k_ln_shares<T, 1, true>, grid, LN_THREADS, 0, st, a, shares, segments));
     }
-    if (a.rows == 0) return QGBDT_OK;
-    const int64_t most = (int64_t)c->sm_count * 4;
-    const dim3 grid((unsigned)(a.rows < most ? a.rows : most));
-    if (vectors) return qg_launch(c, k_ln_long_dx<T, V>, grid, LN_THREADS, 0, st, a);
-    return qg_launch(c, k_ln_long_dx<T, 1>, grid, LN_THREADS, 0, st, a);
+    if (vectors) QG_RUN(qg_launch(c, k_ln_segments_backward<T, V>, blocks, LN_THREADS, 0, st, a, (const float2 *)shares, sums ? partial : (float *)nullptr, segments));
+    else QG_RUN(qg_launch(c, k_ln_segments_backward<T, 1>, blocks, LN_THREADS, 0, st, a, (const float2 *)shares, sums ? partial : (float *)nullptr, segments));
+    if (sums) QG_RUN(ln_join<T>(c, a, partial, (int)slices, st));
+    return qg_ws_close(c, st);
 }
 
 }  // namespace

@@ -96,7 +96,7 @@ SIZES = [
     (1, 1, 0), (3, 2, 0), (2, 3, 1), (1, 8, 0), (5, 7, 0), (64, 16, 0), (33, 24, 8), (17, 31, 0), (9, 32, 0), (40, 33, 5), (1000, 64, 0), (7, 100, 0), (300, 129, 0),
     (1, 256, 0), (4099, 256, 0), (7, 257, 0), (129, 511, 1), (65, 512, 0), (31, 520, 0), (513, 770, 30), (150, 1000, 24), (600, 1023, 0), (700, 1024, 0), (1, 1025, 0),
     (20, 1032, 0), (37, 2047, 0), (300, 2048, 0), (3, 2050, 6), (10, 4095, 2), (150, 4096, 0), (5, 5000, 0), (149, 8192, 0), (9, 8191, 0), (2, 8193, 0), (6, 8200, 0),
-    (160, 12288, 0), (4, 16384, 0), (3, 16385, 0), (2, 40000, 0), (1, 100003, 0),
+    (160, 12288, 0), (4, 16384, 0), (3, 16385, 0), (2, 40000, 0), (1, 100003, 0), (1, 1 << 20, 0), (3, 300001, 3), (70, 12289, 0), (1200, 8200, 0),
 ]
 
 
