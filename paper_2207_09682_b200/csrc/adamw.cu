@@ -4,7 +4,12 @@
 //   p = p (1 - lr decay) - lr / (1 - b1^t) * m / (sqrt(v / (1 - b2^t)) + eps)
 //
 // A tensor is cut into blocks of 256 elements from its start, which is what shares exponents where states have 8
-// bits; a warp works on one of them at a time.
+// bits; a warp works on one of them at a time.  One launch for up to 400 tensors.
+//
+// With states in 32 bits it is bound by memory traffic: 200 M elements with 32-bit gradients and a 16-bit copy, 6.0 GB, take
+// 0.957 ms (6.3 TB/s; 19 instructions per element).  With states in 8 bits half the bytes are left and three times the
+// instructions (63, 27 of them on the integer pipe): 73.7 M elements with 16-bit gradients and copies, 1.18 GB, take 0.21 ms (5.6 TB/s,
+// 69 % of the issue slots); parameters in 16 bits alone, 10 bytes an element, are bound by instructions (30 M: 85 us, 3.5 TB/s).
 #include <cmath>
 
 #include "ops_internal.cuh"
@@ -104,8 +109,9 @@ __device__ __forceinline__ float aw_power(unsigned e) { return __uint_as_float(e
 // 2^(127 - E) for E < 255.
 __device__ __forceinline__ float aw_inverse(unsigned e) { return __uint_as_float(e == 254 ? 0x00400000u : (254 - e) << 23); }
 
-// What eight codes stand for, times 2^(127 - E).  Two at once, as halves of a word that hold the upper 16 bits of the values: bits (code + offset) << 4, or 0
-// for code 0.  (Integer instructions have half the rate of the others; sums and shifts are products where they can be.)
+// What eight codes stand for, times 2^(127 - E).  Two at once, as halves of a word that hold the upper 16 bits of the values: bits
+// (code + offset) << 4, or 0 for code 0.  (Integer instructions have half the rate of the others; sums and shifts are products where
+// they can be.)
 template <unsigned OFFSET, bool SIGNED>
 __device__ __forceinline__ void aw_values_of(const uint2 &codes, float (&x)[8]) {
 #pragma unroll

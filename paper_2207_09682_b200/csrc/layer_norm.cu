@@ -4,6 +4,12 @@
 //   xh = (x - mean) rstd,  dx = rstd (w g - sum (w g) / d - xh sum (w g xh) / d),  dw = sum over rows of g xh,  db = sum over rows of g
 //
 // Sums and statistics are held in single precision; an output is rounded once, when it is written.
+//
+// Rows of up to 8192 columns are held in registers and read once: bound by memory traffic where a row's threads have many
+// elements (16384 x 8192 bf16: 91 us, 5.9 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have few
+// (65536 x 256 bf16: 12 us, 5.7 TB/s; 13 instructions per element, of which the elements' own are 5) and where rows start anywhere
+// (60000 x 1001 bf16: 78 us, 3.1 TB/s; 31 instructions).  Small calls are bound by the launch, and, where the sums over the rows come from
+// several blocks, by a second one (3.5 us).  Longer rows are cut into segments and read twice.
 #include <type_traits>
 
 #include "ops_internal.cuh"
@@ -14,7 +20,8 @@ namespace {
 // A row is cut into segments of LN_SEGMENT elements, so that few long rows occupy the GPU too.  A first launch takes every
 // segment's share of the row's sums (forward: mean and sum of squared differences from it, backward: sums of w g and w g xh), a second one
 // joins the shares of the row in their order, in every block that needs them, and writes.  Inputs are read twice, the
-// second time from L2 where they fit: 1.5 times the bytes forward, 1.67 backward.
+// second time from L2 where they fit: 1.5 times the bytes forward, 1.67 backward.  One row of 2^20 columns in bf16 takes 8.6 us (by
+// a single block: 354), 4096 x 16384 138 us, its gradients 165 us.
 
 constexpr int LN_THREADS = 256, LN_PIECE = 16;      // elements per thread
 constexpr int LN_SEGMENT = LN_THREADS * LN_PIECE;
@@ -248,10 +255,9 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 
 constexpr int LN_ROW = 8192;     // elements of a row, at most
 constexpr int LN_EACH = 16;      // per thread of a warp that has rows of its own, at most
-// Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32 (two thirds of the instructions of 16 go
-// into elements at 8192 columns, the rest into sums and loops: 92 instead of 100 us for 16384 rows; f32: no difference).  Backward: 16, and
-// 8 of rows above 2048 columns, whose threads then come to 32 instead of 16 warps of an SM (7324 x 4096 bf16: 48 instead of 54 us;
-// 14648 x 2048: 48 instead of 44).
+// Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32, so that the sums and loops are for more of
+// them (16384 x 8192 bf16: 92 instead of 100 us; f32: no difference, 16).  Backward: 16, and 8 in rows above 2048 columns, whose
+// threads then come to 32 instead of 16 warps of an SM (7324 x 4096 bf16: 48 instead of 54 us; 14648 x 2048: 48 instead of 44).
 template <typename T, int V>
 constexpr int LN_MANY = V > 1 && sizeof(T) == 2 ? 32 : 16;
 constexpr int LN_WIDE = 2048;

@@ -48,8 +48,8 @@ class Step(NamedTuple):
 
 class LeafClassifier:
     """Embedding table [trees * num_leaves, dim], weight [classes, dim], bias [classes], and with `layer_norm` the norm's weight and
-    bias [dim]; trained by gradient descent ("sgd") or by AdamW ("adamw", states in 32 or 8 bits) with the gradients clipped to a
-    global norm.  Parameters are kept in float32; the embedding and the products run on copies of type `dtype` (bfloat16 or
+    bias [dim]; trained by gradient descent ("sgd") or by AdamW ("adamw", states in 32 or 8 bits, the same decay for all
+    parameters) with the gradients clipped to a global norm.  Parameters are kept in float32; the embedding and the products run on copies of type `dtype` (bfloat16 or
     float16, the latter with a loss scale)."""
 
     def __init__(self, ctx: binding.Context, n_trees: int, num_leaves: int, n_classes: int, dim: int, dtype=torch.bfloat16,
