@@ -248,8 +248,11 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 }
 
 // ---- rows that fit in registers ---------------------------------------------------------------------
-// `lanes` threads have a row: a power of two up to 32, or whole warps; thread g has the vectors g, g + lanes, ... of 16 bytes
-// (V elements), N of them (EXACT: all of them inside the row).  What belongs to the columns stays in registers over all rows.
+// `lanes` threads have a row: a power of two up to 32, or whole warps.  A warp has N * 32 neighbouring vectors of 16 bytes (V elements),
+// each of its threads every 32nd of them (fewer threads: every lanes-th).  What belongs to the columns stays in registers over all
+// rows.  EXACT: every vector is inside the row.  Single elements: so are those of all warps but the last, which take a loop without
+// checks (60000 x 1000 bf16 that starts anywhere 78 -> 64 us; 16-byte vectors have one loop, whose registers decide there:
+// 7000 x 8192 gradients 84 us, 104 with two).
 // Instructions bound these kernels as soon as the memory does not: sums and products are taken of two elements at once,
 // and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
 
@@ -328,17 +331,36 @@ __device__ __forceinline__ float2 ln_exchange(float2 mine, int lanes, float2 (&p
 // Lanes that `warps` warps' sums are in, as a power of two.
 __device__ __forceinline__ int ln_power(int warps) { return warps <= 1 ? 1 : 2 << (31 - __clz(warps - 1)); }
 
+// Which vectors of a row a thread has: from `home` on every APART-th (0: every lanes-th).
+template <int V, int N, int APART>
+struct LnPlace {
+    int dim, lanes, home;
+    __device__ __forceinline__ LnPlace(int dim_, int lanes_, int g) : dim(dim_), lanes(lanes_), home(APART ? (g & ~31) * N + (g & 31) : g) {}
+    __device__ __forceinline__ int apart() const { return APART ? APART : lanes; }
+    __device__ __forceinline__ int column(int i) const { return (home + i * apart()) * V; }
+    template <bool WHOLE>
+    __device__ __forceinline__ bool in(int i) const {
+        return WHOLE || column(i) < dim;
+    }
+    // whether all vectors of the warp are inside the row
+    __device__ __forceinline__ bool whole() const { return (APART ? (home / (32 * N) + 1) * 32 : lanes) * N * V <= dim; }
+};
+// Known to the compiler where a row always has a warp or more: rows_cut() takes the first N that is enough for a warp, so the
+// next one, if at most twice that, has all 32.
+template <int V, int N, bool MULTI>
+constexpr int LN_APART = MULTI || N == (V > 1 ? 2 : 8) || (V == 1 && N == 16) ? 32 : 0;
+
 // A thread's vectors of a row.  V = 1: single elements, of rows that start anywhere.
-template <typename T, int V, int N, bool EXACT>
+template <typename T, int V, int N>
 struct LnRow {
     using Vec = OpsVec<T, V>;
     static constexpr int E = N * V, PAIRS = E / 2;
     Vec v[N];
-    __device__ __forceinline__ static bool in(int i, int dim, int g, int lanes) { return EXACT || (g + i * lanes) * V < dim; }   // vector i
-    __device__ __forceinline__ void store(T *p, int dim, int g, int lanes) const {
+    template <bool WHOLE, typename PLACE>
+    __device__ __forceinline__ void store(T *p, const PLACE &place) const {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (in(i, dim, g, lanes)) *reinterpret_cast<Vec *>(p + (g + i * lanes) * V) = v[i];
+            if (place.template in<WHOLE>(i)) *reinterpret_cast<Vec *>(p + place.column(i)) = v[i];
     }
     __device__ __forceinline__ float2 get(int p) const {   // elements 2 p and 2 p + 1
         if constexpr (V == 1 || sizeof(T) == 4) {
@@ -365,10 +387,10 @@ struct LnRow {
 // Rows that start anywhere (V = 1): such copies come in aligned vectors, so a row is copied as the aligned vectors that hold it, by all its
 // threads for one another.  (Where a row starts inside a vector, the elements in front of it come along; what is in front of the
 // first row is not read.  The last vector is copied as far as the row goes, and zeros follow up to the threads' last elements.)
-template <typename T, int V, int N, bool EXACT, int ROWS, int DEPTH>
+template <typename T, int V, int N, int ROWS, int DEPTH>
 struct LnAhead {
     static constexpr bool LOOSE = V == 1;
-    using Row = LnRow<T, V, N, EXACT>;
+    using Row = LnRow<T, V, N>;
     using Vec = typename Row::Vec;
     // vectors of 16 bytes of a row in a slot
     __host__ __device__ static constexpr int vectors(int lanes) { return LOOSE ? (lanes * N * (int)sizeof(T) + 15) / 16 + 1 : lanes * N; }
@@ -386,7 +408,9 @@ struct LnAhead {
         ring_at = (uint32_t)__cvta_generic_to_shared(ring);
         before = (unsigned)reinterpret_cast<uintptr_t>(from) & 15, before_step = (unsigned)step * sizeof(T) & 15, before_row = (unsigned)ld * sizeof(T) & 15;
     }
-    __device__ __forceinline__ void fetch(int slot, unsigned row, unsigned rows, int dim, int g, int lanes) {
+    template <bool WHOLE, typename PLACE>
+    __device__ __forceinline__ void fetch(int slot, unsigned row, unsigned rows, const PLACE &place, int g) {
+        const int dim = place.dim, lanes = place.lanes;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             if (row + r >= rows) continue;
@@ -411,24 +435,25 @@ struct LnAhead {
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i)
-                    if (Row::in(i, dim, g, lanes))
-                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * blockDim.x * 16), "l"(q + (g + i * lanes) * V) : "memory");
+                    if (place.template in<WHOLE>(i))
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * blockDim.x * 16), "l"(q + place.column(i)) : "memory");
             }
         }
         from += step;
     }
     // Zeros outside the row.
-    __device__ __forceinline__ void take(Row &x, int slot, int r, int dim, int g, int lanes) const {
+    template <bool WHOLE, typename PLACE>
+    __device__ __forceinline__ void take(Row &x, int slot, int r, const PLACE &place) const {
         const unsigned char *const at = ring + (slot * ROWS + r) * slot_bytes;
         if constexpr (LOOSE) {
-            const T *const q = reinterpret_cast<const T *>(at + ((before + r * before_row) & 15)) + g;
+            const T *const q = reinterpret_cast<const T *>(at + ((before + r * before_row) & 15)) + place.home;
 #pragma unroll
-            for (int i = 0; i < N; ++i) x.v[i].v[0] = q[i * lanes];
+            for (int i = 0; i < N; ++i) x.v[i].v[0] = q[i * place.apart()];
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 uint4 q = make_uint4(0, 0, 0, 0);
-                if (Row::in(i, dim, g, lanes)) q = reinterpret_cast<const uint4 *>(at)[i * blockDim.x];
+                if (place.template in<WHOLE>(i)) q = reinterpret_cast<const uint4 *>(at)[i * blockDim.x];
                 *reinterpret_cast<uint4 *>(&x.v[i]) = q;
             }
         }
@@ -461,7 +486,7 @@ __global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_ROW / (N * V) : LN_LOOSE) 
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD<R>;
-    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    using Ahead = LnAhead<T, V, N, R, AHEAD>;
     constexpr bool LOOSE = Ahead::LOOSE;
     using Row = typename Ahead::Row;
     constexpr int P = Row::PAIRS;
@@ -469,18 +494,15 @@ __global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_ROW / (N * V) : LN_LOOSE) 
     const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
     const float per = 1.f / (float)dim;
     unsigned unit = blockIdx.x * groups + group;
+    const LnPlace<V, N, LN_APART<V, N, MULTI>> place(dim, lanes, g);
     Ahead in(a.x, a.ld_x, unit, stride, lanes, group, shared_bytes);
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-        in.fetch(k, (unit + k * stride) * R, rows, dim, g, lanes);
+        in.template fetch<EXACT>(k, (unit + k * stride) * R, rows, place, g);
         ln_commit();
     }
     // elements of a row that a warp has: this one, and the one with this lane's number
-    auto elements = [&](int warp) {
-        int n = 0;
-        for (int i = 0; i < N; ++i) n += max(0, min(32 * V, dim - (warp * 32 + i * lanes) * V));
-        return (float)n;
-    };
+    auto elements = [&](int warp) { return (float)max(0, min(32 * E, dim - warp * 32 * E)); };
     const float count = MULTI && (int)(threadIdx.x & 31) < lanes / 32 ? elements(threadIdx.x & 31) : 0.f, warp_count = MULTI ? elements(threadIdx.x / 32) : (float)dim;
     const float warp_per = warp_count > 0.f ? 1.f / warp_count : 0.f;
     const int warps = ln_power(lanes / 32);
@@ -490,8 +512,8 @@ __global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_ROW / (N * V) : LN_LOOSE) 
     for (int p = 0; p < P; ++p) {
         float *const q[2] = {&w[p].x, &b[p].x};
         for (int k = 0; k < 2; ++k) {
-            const int e = 2 * p + k, c = (g + e / V * lanes) * V + e % V;
-            const bool is = e < E && c < dim;
+            const int e = 2 * p + k, c = place.column(e / V) + e % V;
+            const bool is = c < dim;
             q[0][k] = is ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
             q[1][k] = is ? ln_weight<T>(a.bias, f32, c, 0.f) : 0.f;
         }
@@ -499,72 +521,77 @@ __global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_ROW / (N * V) : LN_LOOSE) 
     T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
     const int64_t out_step = (int64_t)stride * R * a.ld_out;
     int at = 0, slot = 0;
-    for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
-        ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1);
-        float2 y[R][P];
-        float s[R], mean[R];
+    auto work = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
+            ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1);
+            float2 y[R][P];
+            float s[R], mean[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            Row x;
-            in.take(x, slot, r, dim, g, lanes);
-            float2 sum = make_float2(0.f, 0.f);
+            for (int r = 0; r < R; ++r) {
+                Row x;
+                in.template take<WHOLE>(x, slot, r, place);
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int p = 0; p < P; ++p) y[r][p] = x.get(p), sum = add2(sum, y[r][p]);
-            s[r] = sum.x + sum.y;
-        }
-        auto fetch = [&] {
-            in.taken();
-            in.fetch(slot, (unit + AHEAD * stride) * R, rows, dim, g, lanes);
-            ln_commit();
-            slot = slot + 1 < AHEAD ? slot + 1 : 0;
-        };
-        if (!LOOSE) fetch();
-        ln_sum<R>(s, MULTI ? 32 : lanes);
-        if (LOOSE && !MULTI) fetch();      // when all threads have taken theirs
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            mean[r] = s[r] * warp_per;
-            float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int p = 0; p < P; ++p) {
-                float2 z = add2(y[r][p], both(-mean[r]));
-                if (!Row::in(2 * p / V, dim, g, lanes)) z.x = 0.f;
-                if (!Row::in((2 * p + 1) / V, dim, g, lanes)) z.y = 0.f;
-                sum = fma2(z, z, sum);
-                if (!MULTI) y[r][p] = z;
+                for (int p = 0; p < P; ++p) y[r][p] = x.get(p), sum = add2(sum, y[r][p]);
+                s[r] = sum.x + sum.y;
             }
-            s[r] = sum.x + sum.y;
-        }
-        ln_sum<R>(s, MULTI ? 32 : lanes);
-        if constexpr (MULTI) {
-            const float2 other = ln_exchange(make_float2(mean[0], s[0]), lanes, part, at, 1);
-            if (LOOSE) fetch();
-            float m[1] = {other.x * count};
-            ln_sum<1>(m, warps);
-            mean[0] = m[0] * per;
-            const float z = other.x - mean[0];
-            m[0] = fmaf(z * count, z, other.y);
-            ln_sum<1>(m, warps);
-            mean[0] = __shfl_sync(0xffffffffu, mean[0], 0), s[0] = __shfl_sync(0xffffffffu, m[0], 0);
-        }
+            auto fetch = [&] {
+                in.taken();
+                in.template fetch<WHOLE>(slot, (unit + AHEAD * stride) * R, rows, place, g);
+                ln_commit();
+                slot = slot + 1 < AHEAD ? slot + 1 : 0;
+            };
+            if (!LOOSE) fetch();
+            ln_sum<R>(s, MULTI ? 32 : lanes);
+            if (LOOSE && !MULTI) fetch();      // when all threads have taken theirs
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const unsigned row = unit * R + r;
-            if (row >= rows) continue;
-            const float rstd = rsqrtf(fmaf(s[r], per, a.eps));      // (two units in the last place)
-            Row x;
+            for (int r = 0; r < R; ++r) {
+                mean[r] = s[r] * warp_per;
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const float2 z = MULTI ? add2(y[r][p], both(-mean[r])) : y[r][p];
-                x.set(p, fma2(mul2(z, both(rstd)), w[p], b[p]));
+                for (int p = 0; p < P; ++p) {
+                    float2 z = add2(y[r][p], both(-mean[r]));
+                    if (!place.template in<WHOLE>(2 * p / V)) z.x = 0.f;
+                    if (!place.template in<WHOLE>((2 * p + 1) / V)) z.y = 0.f;
+                    sum = fma2(z, z, sum);
+                    if (!MULTI) y[r][p] = z;
+                }
+                s[r] = sum.x + sum.y;
             }
-            x.store(out + r * a.ld_out, dim, g, lanes);
-            if (g == 0) {
-                if (a.mean) a.mean[row] = mean[r];
-                if (a.rstd) a.rstd[row] = rstd;
+            ln_sum<R>(s, MULTI ? 32 : lanes);
+            if constexpr (MULTI) {
+                const float2 other = ln_exchange(make_float2(mean[0], s[0]), lanes, part, at, 1);
+                if (LOOSE) fetch();
+                float m[1] = {other.x * count};
+                ln_sum<1>(m, warps);
+                mean[0] = m[0] * per;
+                const float z = other.x - mean[0];
+                m[0] = fmaf(z * count, z, other.y);
+                ln_sum<1>(m, warps);
+                mean[0] = __shfl_sync(0xffffffffu, mean[0], 0), s[0] = __shfl_sync(0xffffffffu, m[0], 0);
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const unsigned row = unit * R + r;
+                if (row >= rows) continue;
+                const float rstd = rsqrtf(fmaf(s[r], per, a.eps));      // (two units in the last place)
+                Row x;
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const float2 z = MULTI ? add2(y[r][p], both(-mean[r])) : y[r][p];
+                    x.set(p, fma2(mul2(z, both(rstd)), w[p], b[p]));
+                }
+                x.template store<WHOLE>(out + r * a.ld_out, place);
+                if (g == 0) {
+                    if (a.mean) a.mean[row] = mean[r];
+                    if (a.rstd) a.rstd[row] = rstd;
+                }
             }
         }
-    }
+    };
+    if (EXACT || (LOOSE && place.whole())) work(std::true_type{});
+    else work(std::false_type{});
 }
 
 // The gradients; the sums over the rows are gathered by column in registers, joined in shared memory over the block's groups and
@@ -575,7 +602,7 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD_BACKWARD<R>;
-    using Ahead = LnAhead<T, V, N, EXACT, R, AHEAD>;
+    using Ahead = LnAhead<T, V, N, R, AHEAD>;
     constexpr bool LOOSE = Ahead::LOOSE;
     using Row = typename Ahead::Row;
     constexpr int P = Row::PAIRS;
@@ -588,13 +615,14 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
     unsigned char *const rings = reinterpret_cast<unsigned char *>(joined);
     const size_t ring = Ahead::bytes(blockDim.x, lanes);
     Ahead in_x(a.x, a.ld_x, unit, stride, lanes, group, rings), in_u(a.grad, a.ld_grad, unit, stride, lanes, group, rings + ring);
-    auto fetch = [&](int slot, unsigned row) {
-        in_x.fetch(slot, row, rows, dim, g, lanes);
-        in_u.fetch(slot, row, rows, dim, g, lanes);
+    const LnPlace<V, N, LN_APART<V, N, MULTI>> place(dim, lanes, g);
+    auto fetch = [&](auto whole, int slot, unsigned row) {
+        in_x.template fetch<decltype(whole)::value>(slot, row, rows, place, g);
+        in_u.template fetch<decltype(whole)::value>(slot, row, rows, place, g);
         ln_commit();
     };
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) fetch(k, (unit + k * stride) * R);
+    for (int k = 0; k < AHEAD; ++k) fetch(std::bool_constant<EXACT>{}, k, (unit + k * stride) * R);
     // mean and rstd: a lane has those of one of the group's next `turns` steps, and of as many after those
     const int turns = lanes < 32 ? lanes : 32, mine = threadIdx.x & (turns - 1);
     float2 stats[R], later[R];
@@ -611,69 +639,73 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
     const int64_t out_step = (int64_t)stride * R * a.ld_out;
     const int warps = ln_power(lanes / 32);
     int at = 0, slot = 0, turn = 0;
-    for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
-        if (turn == 0) statistics(later, unit + (mine + turns) * stride);
-        float2 xh[R][P], y[R][P];
-        float s[2 * R], rstd[R];
-        ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1 + group);
+    auto work = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        for (unsigned base = unit - group; base < units; base += stride, unit += stride, out += out_step) {
+            if (turn == 0) statistics(later, unit + (mine + turns) * stride);
+            float2 xh[R][P], y[R][P];
+            float s[2 * R], rstd[R];
+            ln_row_arrived<AHEAD - 1, LOOSE, MULTI>(lanes, 1 + group);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float mean = __shfl_sync(0xffffffffu, stats[r].x, turn, turns);
-            rstd[r] = __shfl_sync(0xffffffffu, stats[r].y, turn, turns);
-            Row x, u;
-            in_x.take(x, slot, r, dim, g, lanes);
-            in_u.take(u, slot, r, dim, g, lanes);
-            float2 sum = make_float2(0.f, 0.f), along = sum;
-            if (unit * R + r >= rows) {        // (what its slot holds may be anything)
+            for (int r = 0; r < R; ++r) {
+                const float mean = __shfl_sync(0xffffffffu, stats[r].x, turn, turns);
+                rstd[r] = __shfl_sync(0xffffffffu, stats[r].y, turn, turns);
+                Row x, u;
+                in_x.template take<WHOLE>(x, slot, r, place);
+                in_u.template take<WHOLE>(u, slot, r, place);
+                float2 sum = make_float2(0.f, 0.f), along = sum;
+                if (unit * R + r >= rows) {        // (what its slot holds may be anything)
 #pragma unroll
-                for (int i = 0; i < N; ++i) x.v[i] = u.v[i] = typename Row::Vec{};
+                    for (int i = 0; i < N; ++i) x.v[i] = u.v[i] = typename Row::Vec{};
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    const float2 v = u.get(p), h = mul2(add2(x.get(p), both(-mean)), both(rstd[r]));     // v is zero outside the row
+                    db[p] = add2(db[p], v);
+                    dw[p] = fma2(v, h, dw[p]);
+                    float2 w;
+                    if constexpr (LOOSE) w = make_float2(weight[place.column(2 * p)], weight[place.column(2 * p + 1)]);
+                    else w = *reinterpret_cast<const float2 *>(weight + place.column(2 * p / V) + 2 * p % V);
+                    xh[r][p] = h;
+                    y[r][p] = mul2(v, w);
+                    sum = add2(sum, y[r][p]);
+                    along = fma2(y[r][p], h, along);
+                }
+                s[2 * r] = sum.x + sum.y, s[2 * r + 1] = along.x + along.y;
+            }
+            if (++turn == turns) {
+                turn = 0;
+#pragma unroll
+                for (int r = 0; r < R; ++r) stats[r] = later[r];
+            }
+            auto next = [&] {
+                in_x.taken(), in_u.taken();
+                fetch(whole, slot, (unit + AHEAD * stride) * R);
+                slot = slot + 1 < AHEAD ? slot + 1 : 0;
+            };
+            if (!LOOSE) next();
+            ln_sum<2 * R>(s, MULTI ? 32 : lanes);
+            if (LOOSE && !MULTI) next();       // when all threads have taken theirs
+            if constexpr (MULTI) {
+                const float2 other = ln_exchange(make_float2(s[0], s[1]), lanes, part, at, 1 + group);
+                if (LOOSE) next();
+                s[0] = other.x, s[1] = other.y;
+                ln_sum<2>(s, warps);
+                s[0] = __shfl_sync(0xffffffffu, s[0], 0), s[1] = __shfl_sync(0xffffffffu, s[1], 0);
             }
 #pragma unroll
-            for (int p = 0; p < P; ++p) {
-                const int i = 2 * p / V;
-                const float2 v = u.get(p), h = mul2(add2(x.get(p), both(-mean)), both(rstd[r]));     // v is zero outside the row
-                db[p] = add2(db[p], v);
-                dw[p] = fma2(v, h, dw[p]);
-                float2 w;
-                if constexpr (LOOSE) w = make_float2(weight[g + i * lanes], weight[g + (i + 1) * lanes]);
-                else w = *reinterpret_cast<const float2 *>(weight + (g + i * lanes) * V + 2 * p % V);
-                xh[r][p] = h;
-                y[r][p] = mul2(v, w);
-                sum = add2(sum, y[r][p]);
-                along = fma2(y[r][p], h, along);
+            for (int r = 0; r < R; ++r) {
+                if (unit * R + r >= rows) continue;
+                const float2 c1 = both(-s[2 * r] * per), c2 = both(-s[2 * r + 1] * per);
+                Row x;
+#pragma unroll
+                for (int p = 0; p < P; ++p) x.set(p, mul2(fma2(xh[r][p], c2, add2(y[r][p], c1)), both(rstd[r])));
+                x.template store<WHOLE>(out + r * a.ld_out, place);
             }
-            s[2 * r] = sum.x + sum.y, s[2 * r + 1] = along.x + along.y;
         }
-        if (++turn == turns) {
-            turn = 0;
-#pragma unroll
-            for (int r = 0; r < R; ++r) stats[r] = later[r];
-        }
-        auto next = [&] {
-            in_x.taken(), in_u.taken();
-            fetch(slot, (unit + AHEAD * stride) * R);
-            slot = slot + 1 < AHEAD ? slot + 1 : 0;
-        };
-        if (!LOOSE) next();
-        ln_sum<2 * R>(s, MULTI ? 32 : lanes);
-        if (LOOSE && !MULTI) next();       // when all threads have taken theirs
-        if constexpr (MULTI) {
-            const float2 other = ln_exchange(make_float2(s[0], s[1]), lanes, part, at, 1 + group);
-            if (LOOSE) next();
-            s[0] = other.x, s[1] = other.y;
-            ln_sum<2>(s, warps);
-            s[0] = __shfl_sync(0xffffffffu, s[0], 0), s[1] = __shfl_sync(0xffffffffu, s[1], 0);
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            if (unit * R + r >= rows) continue;
-            const float2 c1 = both(-s[2 * r] * per), c2 = both(-s[2 * r + 1] * per);
-            Row x;
-#pragma unroll
-            for (int p = 0; p < P; ++p) x.set(p, mul2(fma2(xh[r][p], c2, add2(y[r][p], c1)), both(rstd[r])));
-            x.store(out + r * a.ld_out, dim, g, lanes);
-        }
-    }
+    };
+    if (EXACT || (LOOSE && place.whole())) work(std::true_type{});
+    else work(std::false_type{});
     if (!a.d_weight && !a.d_bias) return;
     ln_arrived<0>();
     for (int which = 0; which < 2; ++which) {
@@ -686,11 +718,12 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
             joined[(2 * p + 1) * blockDim.x + threadIdx.x] = v.y;
         }
         __syncthreads();
-        // column c of a group: vector c / V, element c % V
+        // column c of a group: vector c / V, of a warp's (or of the fewer threads') its `in`-th, of a thread its in / apart-th
         for (int c = threadIdx.x; c < dim; c += blockDim.x) {
-            const int v = c / V, i = v / lanes * V + c % V;
+            const int apart = place.apart(), warp = c / (apart * N * V), in = c / V - warp * apart * N, i = in / apart;
+            const float *const of = joined + (i * V + c % V) * blockDim.x + warp * apart + (in - i * apart);
             float s = 0.f;
-            for (int k = 0; k < groups; ++k) s += joined[i * blockDim.x + k * lanes + v % lanes];
+            for (int k = 0; k < groups; ++k) s += of[k * lanes];
             if (gridDim.x > 1) partial[((int64_t)blockIdx.x * 2 + which) * dim + c] = s;
             else if (!final) continue;
             else if (f32) reinterpret_cast<float *>(final)[c] = s;
@@ -729,7 +762,7 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
     constexpr auto kernel = k_ln_rows<T, V, N, MULTI, EXACT>;
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
     const int64_t want = (a.rows + groups * R - 1) / (groups * R);
-    const size_t smem = LnAhead<T, V, N, EXACT, R, LN_AHEAD<R>>::bytes(threads, lanes);
+    const size_t smem = LnAhead<T, V, N, R, LN_AHEAD<R>>::bytes(threads, lanes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = want;
     if (want > c->sm_count) {
@@ -743,15 +776,17 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
 // LN_EACH elements; single elements: four, eight or LN_EACH; then more warps.
 template <int V, int MANY, typename F>
 int rows_cut(int dim, F with) {
-    constexpr int most = LN_EACH / V;
+    constexpr int most = LN_EACH / V, many = MANY / V;
     const int vectors = (dim + V - 1) / V;
+    auto choose = [&](auto n, auto multi, int lanes) {
+        if constexpr (V > 1)
+            if (lanes * n.value * V == dim) return with(n, multi, std::true_type{}, lanes);
+        return with(n, multi, std::false_type{}, lanes);
+    };
     auto few = [&](auto n) {      // of a warp's lanes
         int lanes = 1;
         while (lanes * n.value < vectors) lanes *= 2;
-        if constexpr (V > 1) {
-            if (dim == lanes * n.value * V) return with(n, std::false_type{}, std::true_type{}, lanes);
-        }
-        return with(n, std::false_type{}, std::false_type{}, lanes);
+        return choose(n, std::false_type{}, lanes);
     };
     if constexpr (V > 1) {
         if (vectors <= 32) return few(std::integral_constant<int, 1>{});
@@ -760,12 +795,7 @@ int rows_cut(int dim, F with) {
         if (vectors <= 32 * 8) return few(std::integral_constant<int, 8>{});
     }
     if (vectors <= 32 * most) return few(std::integral_constant<int, most>{});
-    constexpr int many = MANY / V;
-    const int lanes = (vectors + 32 * many - 1) / (32 * many) * 32;
-    if constexpr (V > 1) {
-        if (dim == lanes * MANY) return with(std::integral_constant<int, many>{}, std::true_type{}, std::true_type{}, lanes);
-    }
-    return with(std::integral_constant<int, many>{}, std::true_type{}, std::false_type{}, lanes);
+    return choose(std::integral_constant<int, many>{}, std::true_type{}, (vectors + 32 * many - 1) / (32 * many) * 32);
 }
 
 template <typename T, int V>
@@ -800,7 +830,7 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     constexpr int R = LN_PAIR<N * V, MULTI>;
     constexpr auto kernel = k_ln_rows_backward<T, V, N, MULTI, EXACT>;
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
-    const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, EXACT, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
+    const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
     const size_t smem = (size_t)lanes * N * V * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
     if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     // Few steps: one block, which needs no other launch to join anything.  As many blocks as there are steps up to one per
