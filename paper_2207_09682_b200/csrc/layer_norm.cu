@@ -336,7 +336,8 @@ template <int V, int N, int APART>
 struct LnPlace {
     int dim, lanes, home;
     __device__ __forceinline__ LnPlace(int dim_, int lanes_, int g) : dim(dim_), lanes(lanes_), home(APART ? (g & ~31) * N + (g & 31) : g) {}
-    __device__ __forceinline__ int apart() const { return APART ? APART : lanes; }
+    __device__ __forceinline__ static int apart_of(int lanes) { return APART ? APART : lanes; }
+    __device__ __forceinline__ int apart() const { return apart_of(lanes); }
     __device__ __forceinline__ int column(int i) const { return (home + i * apart()) * V; }
     template <bool WHOLE>
     __device__ __forceinline__ bool in(int i) const {
@@ -384,8 +385,8 @@ struct LnRow {
 
 // The coming rows of an input, copied asynchronously to the shared memory, DEPTH steps of ROWS rows ahead: the memory's latency under
 // load takes 64 KB on their way per SM.  A thread's vectors go to places of its own, so that nobody waits for another thread's copies.
-// Rows that start anywhere (V = 1): such copies come in aligned vectors, so a row is copied as the aligned vectors that hold it, by all its
-// threads for one another.  (Where a row starts inside a vector, the elements in front of it come along; what is in front of the
+// Rows that start anywhere (V = 1): such copies come in aligned vectors, so a row is copied as the aligned vectors that hold it, by its threads
+// for one another.  (Where a row starts inside a vector, the elements in front of it come along; what is in front of the
 // first row is not read.  The last vector is copied as far as the row goes, and zeros follow up to the threads' last elements.)
 template <typename T, int V, int N, int ROWS, int DEPTH>
 struct LnAhead {
@@ -419,18 +420,29 @@ struct LnAhead {
             if constexpr (LOOSE) {
                 const int front = (int)(reinterpret_cast<uintptr_t>(q) & 15), all = front + dim * (int)sizeof(T);   // bytes
                 const char *const w = reinterpret_cast<const char *>(q) - front;
-                int j = g;
-                if (g == 0 && w < reinterpret_cast<const char *>(first)) {
+                const bool begins = g == 0 && w < reinterpret_cast<const char *>(first);
+                if (begins)
                     for (int e = 0; e < (16 - front) / (int)sizeof(T); ++e) {
                         const bool is = e < dim;
                         if constexpr (sizeof(T) == 4) asm volatile("st.shared.b32 [%0], %1;" ::"r"(to + front + 4 * e), "f"(is ? q[e] : 0.f) : "memory");
                         else asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + front + 2 * e), "h"(is ? reinterpret_cast<const unsigned short *>(q)[e] : (unsigned short)0) : "memory");
                     }
-                    j += lanes;
-                }
-                for (; j < vectors(lanes); j += lanes) {
+                auto upto_end = [&](int j) {
                     const int left = max(0, min(16, all - 16 * j));
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 16 * j), "l"(left ? w + 16 * j : reinterpret_cast<const char *>(first)), "r"(left) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 16 * j), "l"(w + 16 * min(j, (all - 1) / 16)), "r"(left) : "memory");
+                };
+                if constexpr (N * sizeof(T) >= 16) {     // each warp the vectors of its elements, the first thread the one more
+                    constexpr int K = N * (int)sizeof(T) / 16;
+                    const int own = PLACE::apart_of(lanes), j = own == lanes ? g : (g & ~31) * K + (g & 31);
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        if (k == 0 && begins) continue;
+                        if (WHOLE) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 16 * (j + k * own)), "l"(w + 16 * (j + k * own)) : "memory");
+                        else upto_end(j + k * own);
+                    }
+                    if (g == 0) upto_end(vectors(lanes) - 1);
+                } else {
+                    for (int j = begins ? lanes : g; j < vectors(lanes); j += lanes) upto_end(j);
                 }
             } else {
 #pragma unroll
