@@ -8,7 +8,7 @@
 // Rows of up to 8192 columns are held in registers and read once: bound by memory traffic where a row's threads have many
 // elements (16384 x 8192 bf16: 91 us, 5.9 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have few
 // (65536 x 256 bf16: 12 us, 5.7 TB/s; 13 instructions per element, of which the elements' own are 5) and where rows start anywhere
-// (60000 x 1001 bf16: 78 us, 3.1 TB/s; 31 instructions).  Small calls are bound by the launch, and, where the sums over the rows come from
+// (60000 x 1001 bf16: 67 us, 3.6 TB/s; 25 instructions).  Small calls are bound by the launch, and, where the sums over the rows come from
 // several blocks, by a second one (3.5 us).  Longer rows are cut into segments and read twice.
 #include <type_traits>
 
@@ -251,7 +251,7 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 // `lanes` threads have a row: a power of two up to 32, or whole warps.  A warp has N * 32 neighbouring vectors of 16 bytes (V elements),
 // each of its threads every 32nd of them (fewer threads: every lanes-th).  What belongs to the columns stays in registers over all
 // rows.  EXACT: every vector is inside the row.  Single elements: so are those of all warps but the last, which take a loop without
-// checks (60000 x 1000 bf16 that starts anywhere 78 -> 64 us; 16-byte vectors have one loop, whose registers decide there:
+// checks (60000 x 1000 bf16 that starts anywhere: 64 instead of 78 us when it came; 16-byte vectors have one loop, whose registers decide there:
 // 7000 x 8192 gradients 84 us, 104 with two).
 // Instructions bound these kernels as soon as the memory does not: sums and products are taken of two elements at once,
 // and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
@@ -265,7 +265,8 @@ template <typename T, int V>
 constexpr int LN_MANY = V > 1 && sizeof(T) == 2 ? 32 : 16;
 constexpr int LN_WIDE = 2048;
 // Threads that the registers of a row's threads leave room for, single elements forward: two rows of up to 5120 columns on an SM
-// (5998 x 5001 bf16: 44 us; with registers for 512 threads 72 us at 4097 columns, here 51).
+// (10000 x 4097 f32: 62 us, with registers for 512 threads 84; for 768 threads 15000 x 4096 bf16 takes 59 instead of 69 us, but
+// 60000 x 1000 78 instead of 67).
 constexpr int LN_LOOSE = 640;
 template <int E, bool MULTI>
 constexpr int LN_PAIR = !MULTI && E <= 8 ? 2 : 1;    // rows at a time
