@@ -123,7 +123,9 @@ def test_many_rows(ctx, rows, dim):
 
 
 @pytest.mark.parametrize("dtype", list(DTYPES))
-@pytest.mark.parametrize("rows,dim,pad,shift", [(50, 64, 7, 1), (50, 64, 12, 4), (9, 1024, 1, 3), (3, 9000, 3, 5), (50, 64, 8, 8)])
+@pytest.mark.parametrize("rows,dim,pad,shift", [(50, 64, 7, 1), (50, 64, 12, 4), (9, 1024, 1, 3), (3, 9000, 3, 5), (50, 64, 8, 8),
+                                                 (3000, 128, 1, 1), (3000, 256, 1, 7), (2000, 512, 3, 1), (1500, 1024, 1, 5), (700, 1536, 1, 2),
+                                                 (700, 4096, 1, 3), (400, 8192, 5, 7)])
 def test_rows_that_start_anywhere(ctx, rows, dim, pad, shift, dtype):
     """Inputs and outputs inside wider matrices; what is around the outputs stays as it was."""
     x, g, w, b = make(rows, dim, DTYPES[dtype], DTYPES[dtype], pad, 5, shift)
