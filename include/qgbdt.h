@@ -386,8 +386,8 @@ int qgbdt_clip_grad_norm(qgbdt_ctx *ctx, const void *const *h_grads, void *const
  * d_bias [dim], both of `weight_type` (QGBDT_F32, or `type`), each may be NULL (1 and 0); d_mean and
  * d_rstd [n_rows] in single precision, each may be NULL.  eps >= 0; where var + eps is 0 (equal values
  * and no eps) rstd is infinite and the row NaN, as the formula has it.  The order of a row's sums goes by
- * dim and by the vectors that addresses and strides allow.  Rows of more than 8192 columns use the work
- * buffer (8 bytes per 4096 elements).  d_out may be d_x itself with the
+ * dim and by the vectors that addresses and strides allow.  Rows of more than 8192 columns may use the
+ * work buffer (8 bytes per 4096 elements).  d_out may be d_x itself with the
  * same stride; it must not overlap d_x otherwise.  dim in [1, 2^20]. */
 int qgbdt_layer_norm(qgbdt_ctx *ctx, const void *d_x, int64_t ld_x, int32_t type, const void *d_weight, const void *d_bias,
                      int32_t weight_type, int64_t n_rows, int32_t dim, double eps, void *d_out, int64_t ld_out,

@@ -5,7 +5,7 @@
 //
 // Sums and statistics are held in single precision; an output is rounded once, when it is written.
 //
-// Rows of up to 8192 columns are held in registers and read once: bound by memory traffic where a row's threads have many
+// Rows of up to 8192 columns (forward mostly 16384) are held in registers and read once: bound by memory traffic where a row's threads have many
 // elements (16384 x 8192 bf16: 91 us, 5.9 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have few
 // (65536 x 256 bf16: 12 us, 5.7 TB/s; 13 instructions per element, of which the elements' own are 5) and where rows start anywhere
 // (60000 x 1001 bf16: 67 us, 3.6 TB/s; 25 instructions).  Small calls are bound by the launch, and, where the sums over the rows come from
@@ -257,10 +257,12 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 // and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
 
 constexpr int LN_ROW = 8192;     // elements of a row, at most
+constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 51 us, in segments 136)
+constexpr int LN_SHARED = 224 * 1024;   // bytes of shared memory that a block can have for them
 constexpr int LN_EACH = 16;      // per thread of a warp that has rows of its own, at most
 // Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32, so that the sums and loops are for more of
-// them (16384 x 8192 bf16: 92 instead of 100 us; f32: no difference, 16).  Backward: 16, and 8 in rows above 2048 columns, whose
-// threads then come to 32 instead of 16 warps of an SM (7324 x 4096 bf16: 48 instead of 54 us; 14648 x 2048: 48 instead of 44).
+// them (16384 x 8192 bf16: 92 instead of 100 us; f32: no difference, 16).  Backward: 16, and 8 in rows of f32 above 2048 columns, whose
+// threads then come to 32 instead of 16 warps of an SM (7324 x 4096: 73 instead of 76 us; bf16: 47 instead of 45).
 template <typename T, int V>
 constexpr int LN_MANY = V > 1 && sizeof(T) == 2 ? 32 : 16;
 constexpr int LN_WIDE = 2048;
@@ -494,7 +496,7 @@ constexpr int LN_AHEAD_BACKWARD = ROWS == 1 ? 3 : 2;
 //   sum over warps of M2 + count (mean of the warp - mean)^2,
 // which takes one exchange and loses nothing where the mean is large beside the differences.
 template <typename T, int V, int N, bool MULTI, bool EXACT>
-__global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_ROW / (N * V) : LN_LOOSE) : 128, MULTI && V > 1 ? 2 : 1) k_ln_rows(const LayerNormArgs a, int lanes) {
+__global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_LONG / (N * V) : LN_LOOSE) : 128) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
@@ -820,7 +822,8 @@ template <typename T>
 int forward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     constexpr int V = 16 / sizeof(T);
     const bool vectors = aligned(a);
-    if (a.dim <= LN_ROW) {
+    constexpr int most = LN_SHARED / (LN_AHEAD<1> * (int)sizeof(T)) < LN_LONG ? LN_SHARED / (LN_AHEAD<1> * (int)sizeof(T)) / 512 * 512 : LN_LONG;
+    if (a.dim <= (vectors ? most : LN_ROW)) {
         return vectors ? rows_forward<T, V>(c, a, st) : rows_forward<T, 1>(c, a, st);
     }
     const int segments = (a.dim + LN_SEGMENT - 1) / LN_SEGMENT;
@@ -870,7 +873,7 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
 template <typename T, int V>
 int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, cudaStream_t st) {
     auto cut = [&](auto n, auto multi, auto exact, int lanes) { return rows_backward<T, V, n.value, multi.value, exact.value>(c, a, lanes, st); };
-    if constexpr (V > 1) {
+    if constexpr (V == 4) {
         if (a.dim > LN_WIDE) return rows_cut<V, 8>(a.dim, cut);
     }
     return rows_cut<V, 16>(a.dim, cut);
