@@ -624,7 +624,8 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
     const int groups = blockDim.x / lanes, group = threadIdx.x / lanes, g = threadIdx.x - group * lanes, dim = a.dim;
     const unsigned rows = (unsigned)a.rows, stride = gridDim.x * groups, units = (rows + R - 1) / R;
     const float per = 1.f / (float)dim;
-    // weight (zeros outside the row); the coming rows of x and of the gradient, afterwards the columns' sums [2 P][threads]
+    // weight (zeros outside the row; of a warp's vectors of 8 the first halves, then the second ones, so that its threads read from all
+    // banks); the coming rows of x and of the gradient, afterwards the columns' sums [2 P][threads]
     float *const weight = reinterpret_cast<float *>(shared_bytes), *const joined = weight + lanes * E;
     unsigned unit = blockIdx.x * groups + group;
     unsigned char *const rings = reinterpret_cast<unsigned char *>(joined);
@@ -647,7 +648,12 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
     };
     statistics(stats, unit + mine * stride);
     const bool f32 = a.weight_type == QGBDT_F32;
-    for (int c = threadIdx.x; c < lanes * E; c += blockDim.x) weight[c] = c < dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
+    const int plane = place.apart() * N;      // a warp's vectors
+    const float4 *const weights = reinterpret_cast<const float4 *>(weight) + (MULTI ? (g & ~31) * N * (V / 4) + (g & 31) : g);
+    for (int c = threadIdx.x; c < lanes * E; c += blockDim.x) {
+        const int to = LOOSE ? c : (c / (V * plane) * (V / 4) * plane + c / 4 % (V / 4) * plane + c / V % plane) * 4 + c % 4;
+        weight[to] = c < dim ? ln_weight<T>(a.weight, f32, c, 1.f) : 0.f;
+    }
     __syncthreads();
     float2 dw[P] = {}, db[P] = {};
     T *out = reinterpret_cast<T *>(a.out) + (int64_t)unit * R * a.ld_out;
@@ -680,7 +686,7 @@ __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_back
                     dw[p] = fma2(v, h, dw[p]);
                     float2 w;
                     if constexpr (LOOSE) w = make_float2(weight[place.column(2 * p)], weight[place.column(2 * p + 1)]);
-                    else w = *reinterpret_cast<const float2 *>(weight + place.column(2 * p / V) + 2 * p % V);
+                    else w = reinterpret_cast<const float2 *>(weights + 2 * p % V / 4 * plane + 2 * p / V * place.apart())[p % 2];
                     xh[r][p] = h;
                     y[r][p] = mul2(v, w);
                     sum = add2(sum, y[r][p]);
