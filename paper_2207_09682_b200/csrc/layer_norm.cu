@@ -257,7 +257,7 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 // and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
 
 constexpr int LN_ROW = 8192;     // elements of a row, at most
-constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 51 us, in segments 136)
+constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 49 us, in segments 136)
 constexpr int LN_SHARED = 224 * 1024;   // bytes of shared memory that a block can have for them
 constexpr int LN_EACH = 16;      // per thread of a warp that has rows of its own, at most
 // Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32, so that the sums and loops are for more of
@@ -496,7 +496,7 @@ constexpr int LN_AHEAD_BACKWARD = ROWS == 1 ? 3 : 2;
 //   sum over warps of M2 + count (mean of the warp - mean)^2,
 // which takes one exchange and loses nothing where the mean is large beside the differences.
 template <typename T, int V, int N, bool MULTI, bool EXACT>
-__global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_LONG / (N * V) : LN_LOOSE) : 128) k_ln_rows(const LayerNormArgs a, int lanes) {
+__global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_LONG / (N * V) : LN_LOOSE) : 128, 1) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     __shared__ float2 part[2][32];
