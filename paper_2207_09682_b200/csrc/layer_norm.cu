@@ -6,7 +6,7 @@
 // Sums and statistics are held in single precision; an output is rounded once, when it is written.
 //
 // Rows of up to 8192 columns (forward mostly 16384) are held in registers and read once: bound by memory traffic where a row's threads have many
-// elements (16384 x 8192 bf16: 91 us, 5.9 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have few
+// elements (16384 x 8192 bf16: 90 us, 6.0 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have few
 // (65536 x 256 bf16: 12 us, 5.7 TB/s; 13 instructions per element, of which the elements' own are 5) and where rows start anywhere
 // (60000 x 1001 bf16: 67 us, 3.6 TB/s; 25 instructions).  Small calls are bound by the launch, and, where the sums over the rows come from
 // several blocks, by a second one (3.5 us).  Longer rows are cut into segments and read twice.
@@ -21,7 +21,7 @@ namespace {
 // segment's share of the row's sums (forward: mean and sum of squared differences from it, backward: sums of w g and w g xh), a second one
 // joins the shares of the row in their order, in every block that needs them, and writes.  Inputs are read twice, the
 // second time from L2 where they fit: 1.5 times the bytes forward, 1.67 backward.  One row of 2^20 columns in bf16 takes 8.6 us (by
-// a single block: 354), 4096 x 16384 138 us, its gradients 165 us.
+// a single block: 354), 2048 x 32768 136 us, gradients of 4096 x 16384 165 us.
 
 constexpr int LN_THREADS = 256, LN_PIECE = 16;      // elements per thread
 constexpr int LN_SEGMENT = LN_THREADS * LN_PIECE;
