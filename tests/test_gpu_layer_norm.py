@@ -97,6 +97,7 @@ SIZES = [
     (1, 256, 0), (4099, 256, 0), (7, 257, 0), (129, 511, 1), (65, 512, 0), (31, 520, 0), (513, 770, 30), (150, 1000, 24), (600, 1023, 0), (700, 1024, 0), (1, 1025, 0),
     (20, 1032, 0), (37, 2047, 0), (300, 2048, 0), (3, 2050, 6), (10, 4095, 2), (150, 4096, 0), (5, 5000, 0), (149, 8192, 0), (9, 8191, 0), (2, 8193, 0), (6, 8200, 0),
     (160, 12288, 0), (4, 16384, 0), (3, 16385, 0), (2, 40000, 0), (1, 100003, 0), (1, 1 << 20, 0), (3, 300001, 3), (70, 12289, 0), (1200, 8200, 0),
+    (300, 14336, 0), (300, 14340, 0), (1000, 16384, 0), (20, 9000, 24), (160, 16376, 0),
 ]
 
 
@@ -146,7 +147,7 @@ def test_rows_that_start_anywhere(ctx, rows, dim, pad, shift, dtype):
         assert bool((around == 7.0).all())
 
 
-@pytest.mark.parametrize("rows,dim", [(70, 64), (70, 129), (300, 1024), (200, 2048), (5, 8192), (3, 20000), (3, 20001)])
+@pytest.mark.parametrize("rows,dim", [(70, 64), (70, 129), (300, 1024), (200, 2048), (5, 8192), (500, 16384), (3, 20000), (3, 20001)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_in_place(ctx, rows, dim, dtype):
     x, g, w, b = make(rows, dim, DTYPES[dtype], torch.float32, 0, 6)
