@@ -259,6 +259,9 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 constexpr int LN_ROW = 8192;     // elements of a row, at most
 constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 49 us, in segments 136)
 constexpr int LN_SHARED = 224 * 1024;   // bytes of shared memory that a block can have for them
+// What a launch may give a block without leave for more: 48 KB, less what the kernels hold themselves.
+using LnParts = float2[2][32];
+constexpr size_t LN_LEAVE = 48 * 1024 - sizeof(LnParts);
 constexpr int LN_EACH = 16;      // per thread of a warp that has rows of its own, at most
 // Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32, so that the sums and loops are for more of
 // them (16384 x 8192 bf16: 92 instead of 100 us; f32: no difference, 16).  Backward: 16, and 8 in rows of f32 above 2048 columns, whose
@@ -499,7 +502,7 @@ template <typename T, int V, int N, bool MULTI, bool EXACT>
 __global__ void __launch_bounds__(MULTI ? (V > 1 ? LN_LONG / (N * V) : LN_LOOSE) : 128, 1) k_ln_rows(const LayerNormArgs a, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
-    __shared__ float2 part[2][32];
+    __shared__ LnParts part;
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD<R>;
     using Ahead = LnAhead<T, V, N, R, AHEAD>;
     constexpr bool LOOSE = Ahead::LOOSE;
@@ -615,7 +618,7 @@ template <typename T, int V, int N, bool MULTI, bool EXACT>
 __global__ void __launch_bounds__(MULTI ? LN_ROW / (N * V) : 256) k_ln_rows_backward(const LayerNormArgs a, float *partial, int lanes) {
     qg_after_prior();
     extern __shared__ __align__(16) unsigned char shared_bytes[];
-    __shared__ float2 part[2][32];
+    __shared__ LnParts part;
     constexpr int E = N * V, R = LN_PAIR<E, MULTI>, AHEAD = LN_AHEAD_BACKWARD<R>;
     using Ahead = LnAhead<T, V, N, R, AHEAD>;
     constexpr bool LOOSE = Ahead::LOOSE;
@@ -784,7 +787,7 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
     const int64_t want = (a.rows + groups * R - 1) / (groups * R);
     const size_t smem = LnAhead<T, V, N, R, LN_AHEAD<R>>::bytes(threads, lanes);
-    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (smem > LN_LEAVE) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     int64_t grid = want;
     if (want > c->sm_count) {
         QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
@@ -854,7 +857,7 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
     const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
     const size_t smem = (size_t)lanes * N * V * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
-    if (smem > 48 * 1024) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    if (smem > LN_LEAVE) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     // Few steps: one block, which needs no other launch to join anything.  As many blocks as there are steps up to one per
     // SM; beyond that four rows per group at least, since the partial sums are as large as one and a half.
     const int64_t steps = (a.rows + groups * R - 1) / (groups * R), fours = (a.rows + groups * 4 - 1) / (groups * 4);
