@@ -259,9 +259,10 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 constexpr int LN_ROW = 8192;     // elements of a row, at most
 constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 49 us, in segments 136)
 constexpr int LN_SHARED = 224 * 1024;   // bytes of shared memory that a block can have for them
-// What a launch may give a block without leave for more: 48 KB, less what the kernels hold themselves.
+// What a launch may give a block without leave for more, and with it: 48 and 227 KB, less what the kernels hold themselves.
 using LnParts = float2[2][32];
 constexpr size_t LN_LEAVE = 48 * 1024 - sizeof(LnParts);
+constexpr int LN_MOST = 227 * 1024 - (int)sizeof(LnParts);
 constexpr int LN_EACH = 16;      // per thread of a warp that has rows of its own, at most
 // Elements per thread where a row has several warps.  Forward, vectors of 16-bit elements: 32, so that the sums and loops are for more of
 // them (16384 x 8192 bf16: 92 instead of 100 us; f32: no difference, 16).  Backward: 16, and 8 in rows of f32 above 2048 columns, whose
@@ -780,6 +781,14 @@ int ln_resident(qgbdt_ctx *c, K kernel, int threads, size_t smem, int64_t *block
     return QGBDT_OK;
 }
 
+// Leave for a launch that gives a block `smem` bytes.  It is the kernel's, for rows of all widths and for all contexts of the process, so that
+// every call asks for the same: a call's own size would take from another thread what it has asked for and not yet launched with.
+template <typename K>
+int ln_leave(qgbdt_ctx *c, K kernel, size_t smem) {
+    if (smem > LN_LEAVE) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, LN_MOST));
+    return QGBDT_OK;
+}
+
 template <typename T, int V, int N, bool MULTI, bool EXACT>
 int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t st) {
     constexpr int R = LN_PAIR<N * V, MULTI>;
@@ -787,7 +796,7 @@ int rows_forward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t s
     const int threads = MULTI ? lanes : 128, groups = threads / lanes;
     const int64_t want = (a.rows + groups * R - 1) / (groups * R);
     const size_t smem = LnAhead<T, V, N, R, LN_AHEAD<R>>::bytes(threads, lanes);
-    if (smem > LN_LEAVE) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    QG_RUN(ln_leave(c, kernel, smem));
     int64_t grid = want;
     if (want > c->sm_count) {
         QG_RUN(ln_resident(c, kernel, threads, smem, &grid));
@@ -857,7 +866,7 @@ int rows_backward(qgbdt_ctx *c, const LayerNormArgs &a, int lanes, cudaStream_t 
     const int threads = lanes >= 256 ? lanes : 256 / lanes * lanes, groups = threads / lanes;
     const size_t sums_bytes = (size_t)threads * N * V * sizeof(float), ring = 2 * LnAhead<T, V, N, R, LN_AHEAD_BACKWARD<R>>::bytes(threads, lanes);
     const size_t smem = (size_t)lanes * N * V * sizeof(float) + (ring > sums_bytes ? ring : sums_bytes);
-    if (smem > LN_LEAVE) QG_CUDA(c, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    QG_RUN(ln_leave(c, kernel, smem));
     // Few steps: one block, which needs no other launch to join anything.  As many blocks as there are steps up to one per
     // SM; beyond that four rows per group at least, since the partial sums are as large as one and a half.
     const int64_t steps = (a.rows + groups * R - 1) / (groups * R), fours = (a.rows + groups * 4 - 1) / (groups * 4);

@@ -13,7 +13,7 @@
 constexpr int DEFAULT = 48 * 1024, OWN = 512, MOST = 227 * 1024;
 
 static std::map<const void *, int> leave;      // bytes a launch may give a kernel, where that was set
-static int launches = 0, failures = 0;
+static int launches = 0, failures = 0, lowered = 0;
 static char what[160];
 
 static void fail(const char *why, long a, long b) {
@@ -24,6 +24,7 @@ static int may(const void *f) { return leave.count(f) ? leave[f] : DEFAULT - OWN
 extern "C" {
 cudaError_t cudaFuncSetAttribute(const void *f, cudaFuncAttribute, int value) {
     if (value > MOST - OWN) fail("more shared memory than a block can have", value, 0);
+    if (leave.count(f) && leave[f] > value) ++lowered;
     return leave[f] = value, cudaSuccess;
 }
 cudaError_t cudaOccupancyMaxActiveBlocksPerMultiprocessorWithFlags(int *n, const void *f, int, size_t smem, unsigned) {
@@ -90,6 +91,8 @@ static void all(F before) {
 int main(int, char **argv) {
     c.sm_count = 148;
     if (!strcmp(argv[1], "first")) all([] { leave.clear(); });      // every call is the first one of its process
-    return failures ? 1 : 0;
+    else all([] {});                                                // one after the other
+    if (lowered) printf("a kernel's leave for shared memory was lowered %d times\n", lowered);
+    return failures || lowered ? 1 : 0;
 }
 #endif

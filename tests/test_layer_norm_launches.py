@@ -18,8 +18,9 @@ def program(tmp_path_factory):
     return out
 
 
-@pytest.mark.parametrize("calls", ["first"])
+@pytest.mark.parametrize("calls", ["first", "one after the other"])
 def test_shared_memory_of_the_launches(program, calls):
-    """first: a launch gets the shared memory that it asks for without an earlier call of other sizes."""
+    """first: a launch gets the shared memory that it asks for without an earlier call of other sizes.  One after the other: no
+    call takes from a kernel what another call, of another thread perhaps, has asked for."""
     run = subprocess.run([program, calls], capture_output=True, text=True)
     assert run.returncode == 0, run.stdout[-4000:]
