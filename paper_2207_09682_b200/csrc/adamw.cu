@@ -188,13 +188,18 @@ __device__ __forceinline__ int aw_find(const AdamwTable<CAP> &t, unsigned block)
 // One element: m, v and p are replaced.  b1 and b2 come with the power of two that m and v are to be multiplied with (which
 // changes no rounding).  m and v in operations that are rounded one by one (what is rounded to 8 bits afterwards then has the
 // bits of the formula written out); the root and the quotient by the approximations of the special function unit, 2^-22 of the
-// change off at most: exact ones would be half as many instructions again.  Below 2^-126 they take v for that.
+// change off at most: exact ones would be half as many instructions again.  Below 2^-126 they take v for that: by a maximum where eps
+// is too small to cover the difference (BARE), else by a sum, which goes to a pipe that has room (30 M bf16, 8 bits, with the values read
+// back: 114 instead of 117 us).
+template <bool BARE>
 __device__ __forceinline__ void aw_element(const AdamwScalars &s, float b1, float b2, float g, float &m, float &v, float &p) {
     g = g * s.coef;
     m = m * b1 + g * s.c1;
     v = v * b2 + (g * s.c2) * g;
     float root, one;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(v + 1.17549435e-38f));
+    float x = v + 1.17549435e-38f;
+    if (BARE) asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(v), "f"(1.17549435e-38f));
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(root) : "f"(x));
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(one) : "f"(fmaf(root, s.root, s.eps)));
     p = fmaf(p, s.keep, -(m * one));
 }
@@ -295,14 +300,14 @@ struct AwInput {
 
 // Eight elements of a lane, whose places are 2^APART apart, m and v without the powers of two of the exponents e.  Packed: m and
 // v are rounded to codes, e is replaced.
-template <bool PACKED, int APART>
+template <bool PACKED, bool BARE, int APART>
 __device__ __forceinline__ void aw_eight(const AdamwScalars &s, float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8], unsigned hash, unsigned (&e)[2],
                                          uint2 (&codes)[2]) {
     const float b1 = PACKED ? s.b1 * aw_power(e[0]) : s.b1, b2 = PACKED ? s.b2 * aw_power(e[1]) : s.b2;
     float top[2] = {0.f, 0.f};
 #pragma unroll
     for (int k = 0; k < AW_EACH; ++k) {
-        aw_element(s, b1, b2, g[k], m[k], v[k], p[k]);
+        aw_element<BARE>(s, b1, b2, g[k], m[k], v[k], p[k]);
         if (PACKED && (k & 1)) top[0] = aw_largest(top[0], m[k - 1], m[k]), top[1] = aw_largest(top[1], v[k - 1], v[k]);
     }
     if constexpr (PACKED) {
@@ -314,7 +319,7 @@ __device__ __forceinline__ void aw_eight(const AdamwScalars &s, float (&p)[8], c
 }
 
 // A whole block whose addresses allow eight neighbouring elements per lane.
-template <bool PACKED, bool WIDE_P, bool WIDE_G>
+template <bool PACKED, bool BARE, bool WIDE_P, bool WIDE_G>
 __device__ __forceinline__ void aw_whole_block(const AwTensor &t, const AdamwScalars &s, const AwInput<PACKED, WIDE_P, WIDE_G> &in, int64_t at, unsigned hash,
                                                unsigned (&e)[2]) {
     float p[8], g[8], m[8], v[8];
@@ -328,7 +333,7 @@ __device__ __forceinline__ void aw_whole_block(const AwTensor &t, const AdamwSca
     }
     aw_unpack<WIDE_P>(p, in.p, t.param_type == QGBDT_BF16);
     aw_unpack<WIDE_G>(g, in.g, t.grad_type == QGBDT_BF16);
-    aw_eight<PACKED, 0>(s, p, g, m, v, hash, e, codes);
+    aw_eight<PACKED, BARE, 0>(s, p, g, m, v, hash, e, codes);
     aw_write<WIDE_P>(t.param, at, p, t.param_type == QGBDT_BF16);
     if (t.copy) {
         if (t.copy_type == QGBDT_F32) aw_write<true>(t.copy, at, p, false);
@@ -344,7 +349,7 @@ __device__ __forceinline__ void aw_whole_block(const AwTensor &t, const AdamwSca
 }
 
 // Any other block, of n elements: a lane has every 32nd, from its own on.
-template <bool PACKED>
+template <bool PACKED, bool BARE>
 __device__ __forceinline__ void aw_ragged_block(const AwTensor &t, const AdamwScalars &s, int64_t at, int n, unsigned hash, unsigned (&e)[2]) {
     float p[8], g[8], m[8], v[8];
     uint2 codes[2] = {};
@@ -366,7 +371,7 @@ __device__ __forceinline__ void aw_ragged_block(const AwTensor &t, const AdamwSc
         aw_values_of<AW_CODES_M, true>(codes[0], m);
         aw_values_of<AW_CODES_V, false>(codes[1], v);
     }
-    aw_eight<PACKED, 5>(s, p, g, m, v, hash, e, codes);
+    aw_eight<PACKED, BARE, 5>(s, p, g, m, v, hash, e, codes);
 #pragma unroll
     for (int k = 0; k < AW_EACH; ++k) {
         if (32 * k >= n) continue;
@@ -383,7 +388,7 @@ __device__ __forceinline__ void aw_ragged_block(const AwTensor &t, const AdamwSc
 }
 
 // The first blocks of a run, the whole ones; `held`: the run's exponents, a byte per lane (replaced); `number`: of the first block.
-template <bool PACKED, bool WIDE_P, bool WIDE_G>
+template <bool PACKED, bool BARE, bool WIDE_P, bool WIDE_G>
 __device__ __forceinline__ void aw_whole_blocks(const AwTensor &t, const AdamwScalars &s, int64_t at, int whole, unsigned number, int lane, unsigned &held) {
     at += lane * AW_EACH;
     AwInput<PACKED, WIDE_P, WIDE_G> next;
@@ -396,11 +401,11 @@ __device__ __forceinline__ void aw_whole_blocks(const AwTensor &t, const AdamwSc
             e[0] = __shfl_sync(0xffffffffu, held, 2 * k), e[1] = __shfl_sync(0xffffffffu, held, 2 * k + 1);
             const AwInput<PACKED, WIDE_P, WIDE_G> now = next;
             if (k + 1 < whole) next.read(t, at + AW_BLOCK);   // under this block's work
-            aw_whole_block<PACKED, WIDE_P, WIDE_G>(t, s, now, at, key ^ (lane * AW_EACH), e);
+            aw_whole_block<PACKED, BARE, WIDE_P, WIDE_G>(t, s, now, at, key ^ (lane * AW_EACH), e);
             held = lane == 2 * k ? e[0] : lane == 2 * k + 1 ? e[1] : held;
         } else {
             next.read(t, at);   // four times the bytes in flight as it is
-            aw_whole_block<PACKED, WIDE_P, WIDE_G>(t, s, next, at, 0, e);
+            aw_whole_block<PACKED, BARE, WIDE_P, WIDE_G>(t, s, next, at, 0, e);
         }
     }
 }
@@ -409,7 +414,7 @@ __device__ __forceinline__ void aw_whole_blocks(const AwTensor &t, const AdamwSc
 // together, a byte per lane: single ones would have warps wait for one another's sectors.
 constexpr int AW_RUN = 16;
 
-template <int CAP, bool PACKED>
+template <int CAP, bool PACKED, bool BARE>
 __global__ void __launch_bounds__(AW_THREADS<PACKED>, AW_RESIDENT<PACKED>) k_adamw(const __grid_constant__ AdamwTable<CAP> t, const __grid_constant__ AdamwFactors f, int per) {
     qg_after_prior();
     __shared__ AdamwScalars scalars;
@@ -437,11 +442,11 @@ __global__ void __launch_bounds__(AW_THREADS<PACKED>, AW_RESIDENT<PACKED>) k_ada
             const unsigned number = t.number + block;
             if (whole > 0) {
                 if (one.param_type == QGBDT_F32) {
-                    if (one.grad_type == QGBDT_F32) aw_whole_blocks<PACKED, true, true>(one, s, at, whole, number, lane, held);
-                    else aw_whole_blocks<PACKED, true, false>(one, s, at, whole, number, lane, held);
+                    if (one.grad_type == QGBDT_F32) aw_whole_blocks<PACKED, BARE, true, true>(one, s, at, whole, number, lane, held);
+                    else aw_whole_blocks<PACKED, BARE, true, false>(one, s, at, whole, number, lane, held);
                 } else {
-                    if (one.grad_type == QGBDT_F32) aw_whole_blocks<PACKED, false, true>(one, s, at, whole, number, lane, held);
-                    else aw_whole_blocks<PACKED, false, false>(one, s, at, whole, number, lane, held);
+                    if (one.grad_type == QGBDT_F32) aw_whole_blocks<PACKED, BARE, false, true>(one, s, at, whole, number, lane, held);
+                    else aw_whole_blocks<PACKED, BARE, false, false>(one, s, at, whole, number, lane, held);
                 }
             }
 #pragma unroll 1
@@ -449,7 +454,7 @@ __global__ void __launch_bounds__(AW_THREADS<PACKED>, AW_RESIDENT<PACKED>) k_ada
                 unsigned e[2] = {};
                 if constexpr (PACKED) e[0] = __shfl_sync(0xffffffffu, held, 2 * k), e[1] = __shfl_sync(0xffffffffu, held, 2 * k + 1);
                 const int64_t left = count - (int64_t)k * AW_BLOCK;
-                aw_ragged_block<PACKED>(one, s, at + (int64_t)k * AW_BLOCK + lane, (left < AW_BLOCK ? (int)left : AW_BLOCK) - lane, aw_mix(s.key ^ (number + k)) ^ lane, e);
+                aw_ragged_block<PACKED, BARE>(one, s, at + (int64_t)k * AW_BLOCK + lane, (left < AW_BLOCK ? (int)left : AW_BLOCK) - lane, aw_mix(s.key ^ (number + k)) ^ lane, e);
                 if constexpr (PACKED) held = lane == 2 * k ? e[0] : lane == 2 * k + 1 ? e[1] : held;
             }
             if (PACKED && lane < 2 * run) *exponents = (uint8_t)held;
@@ -555,7 +560,7 @@ int aw_grid(qgbdt_ctx *c, K kernel, int threads, unsigned blocks, int *per, unsi
     return QGBDT_OK;
 }
 
-template <int CAP, bool PACKED>
+template <int CAP, bool PACKED, bool BARE>
 int aw_run(qgbdt_ctx *c, const qgbdt_adamw_tensor *in, int32_t n, const AdamwFactors &f, cudaStream_t st) {
     AdamwTable<CAP> t;
     int32_t at = 0;
@@ -579,8 +584,8 @@ int aw_run(qgbdt_ctx *c, const qgbdt_adamw_tensor *in, int32_t n, const AdamwFac
         if (t.blocks == 0) continue;
         int per;
         unsigned grid;
-        QG_RUN(aw_grid(c, k_adamw<CAP, PACKED>, AW_THREADS<PACKED>, t.blocks, &per, &grid));
-        QG_RUN(qg_launch(c, k_adamw<CAP, PACKED>, dim3(grid), AW_THREADS<PACKED>, 0, st, t, f, per));
+        QG_RUN(aw_grid(c, k_adamw<CAP, PACKED, BARE>, AW_THREADS<PACKED>, t.blocks, &per, &grid));
+        QG_RUN(qg_launch(c, k_adamw<CAP, PACKED, BARE>, dim3(grid), AW_THREADS<PACKED>, 0, st, t, f, per));
     }
     return QGBDT_OK;
 }
@@ -623,9 +628,12 @@ int qg_adamw(qgbdt_ctx *c, const qgbdt_adamw_tensor *t, int32_t n, const qgbdt_a
     f.s.b1 = (float)o.beta1, f.s.c1 = (float)(1.0 - o.beta1), f.s.b2 = (float)o.beta2, f.s.c2 = (float)(1.0 - o.beta2);
     aw_of_step(f.s, f, o.d_lr ? 0.0 : o.lr, o.d_step ? 1 : o.step);
     const bool packed = o.state_bits == 8;
-    if (n <= AW_SMALL) return packed ? aw_run<AW_SMALL, true>(c, t, n, f, st) : aw_run<AW_SMALL, false>(c, t, n, f, st);
-    if (n <= AW_MEDIUM) return packed ? aw_run<AW_MEDIUM, true>(c, t, n, f, st) : aw_run<AW_MEDIUM, false>(c, t, n, f, st);
-    return packed ? aw_run<AW_LARGE, true>(c, t, n, f, st) : aw_run<AW_LARGE, false>(c, t, n, f, st);
+    // An eps that is 2^23 times the root of 2^-126 or more in the first step already covers what a sum adds to the moments.  Smaller ones
+    // (rare) are not worth a kernel of their own for few tensors.
+    if (o.eps * sqrt(1.0 - o.beta2) < 0x1p-40) return packed ? aw_run<AW_LARGE, true, true>(c, t, n, f, st) : aw_run<AW_LARGE, false, true>(c, t, n, f, st);
+    if (n <= AW_SMALL) return packed ? aw_run<AW_SMALL, true, false>(c, t, n, f, st) : aw_run<AW_SMALL, false, false>(c, t, n, f, st);
+    if (n <= AW_MEDIUM) return packed ? aw_run<AW_MEDIUM, true, false>(c, t, n, f, st) : aw_run<AW_MEDIUM, false, false>(c, t, n, f, st);
+    return packed ? aw_run<AW_LARGE, true, false>(c, t, n, f, st) : aw_run<AW_LARGE, false, false>(c, t, n, f, st);
 }
 
 int qg_adamw_values(qgbdt_ctx *c, const uint8_t *const *m, const uint8_t *const *v, const uint8_t *const *exponents, void *const *out_m,

@@ -261,6 +261,32 @@ def test_extreme_gradients_and_moments(ctx):
     assert abs(float(was[8] - case.p[0][8])) <= 0.01 * 1e-9
 
 
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-18, 1e-14, 1e-11, 3e-11, 1e-8])
+def test_small_moments_and_small_eps(ctx, eps):
+    """An exp_avg_sq from 2^-126 to 2^-100 counts as what it is, a smaller one (zero too) as 2^-126; NaN stays NaN."""
+    n = 27 * 64
+    case = Case([n + 3], bits=32)
+    case.g[0].zero_()
+    case.p[0].zero_()
+    v = power_of_two(torch.arange(-126, -99, device="cuda")).repeat_interleave(64) * (1.01 + torch.rand(n, dtype=torch.float64, generator=gen(3), device="cuda"))
+    case.v[0][:n] = v.float()
+    case.v[0][n:] = torch.tensor([0.0, 2.0 ** -149, math.nan], device="cuda")
+    case.m[0][:n] = (v.sqrt() * torch.rand(n, dtype=torch.float64, generator=gen(4), device="cuda")).float()
+    case.m[0][n:] = 2.0 ** -64
+    was = before(case, ctx)
+    case.step(ctx, 3, 0.01, eps=eps, weight_decay=0.0)
+    assert torch.isnan(case.p[0][-1])
+    for t in (case.p, case.m, case.v, *was):
+        t[0] = t[0][:n]
+    case.g[0], case.sizes = case.g[0][:n], [n]
+    least = -0.01 / (1 - 0.9 ** 3) * 0.9 * 2.0 ** -64 / (math.sqrt(2.0 ** -126 / (1 - 0.999 ** 3)) + eps)
+    flat = case.around[0][0]
+    assert bool(((flat[n:n + 2].double() - least).abs() <= 40 * U * abs(least)).all())
+    m, v, p, m_size, slack = formula(case.g[0], was[1][0], was[2][0], was[0][0], 3, 0.01, eps=eps, weight_decay=0.0)
+    assert bool((v >= 2.0 ** -126).all())
+    within(case.p[0], p, slack)
+
+
 # ---- states of 8 bits ----------------------------------------------------------------------------------
 
 def mix(x):
