@@ -156,9 +156,9 @@ __device__ __forceinline__ void aw_round(const float (&m)[8], const float (&v)[8
         ym[k] = __float_as_uint(fabsf(m[k]) * inverse_m);
         if (k & 1) smallest = __vimin3_u32(smallest, ym[k - 1] - 1, ym[k] - 1);
         cm[k] = aw_encode<AW_CODES_M>(max(ym[k], zero_m), upper);
-        // v: above zero it is the smallest code at least
+        // v: above zero it is the smallest code at least, also where the product is zero
         const unsigned yv = __float_as_uint(v[k] * inverse_v);
-        cv[k] = aw_encode<AW_CODES_V>(max(yv, min(yv, 1u) * (1u << 20) + zero_v), __byte_perm(x, 0, 0x4104) ^ upper);
+        cv[k] = aw_encode<AW_CODES_V>(max(yv, min(__float_as_uint(v[k]), 1u) * (1u << 20) + zero_v), __byte_perm(x, 0, 0x4104) ^ upper);
     }
     if (smallest < least_m - 1) {   // rare: an m between zero and the smallest code is one of the two
 #pragma unroll

@@ -381,6 +381,22 @@ def test_sizes_of_states(ctx, scale):
         assert bool((case.v[0][held] > 0).all())
 
 
+@pytest.mark.parametrize("small", [1e-3, 1e-6, 1e-10, 1e-18])
+@pytest.mark.parametrize("n", [1024, 777])
+def test_moments_far_below_their_neighbours(ctx, n, small):
+    """An exp_avg_sq above zero never becomes zero, not even where its block's largest is 2^200 times it."""
+    case = Case([n], bits=8)
+    for t in (*case.m, *case.v, *case.e):
+        t.zero_()
+    case.g[0].fill_(small)
+    case.g[0][::100] = 1e19
+    case.g[0][1::100] = 0.0
+    was = before(case, ctx)
+    case.step(ctx, 1, 0.01, seed=4)
+    check_codes(case, was, 1, 4)
+    assert torch.equal(case.v[0] > 0, case.g[0] != 0)
+
+
 def test_rounding_keeps_the_mean(ctx):
     """400 000 elements with the same history under different seeds and places: the means of m and v follow the formula to six
     standard deviations of the mean; v follows gradients that became ten times smaller."""
