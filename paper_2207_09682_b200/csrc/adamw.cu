@@ -78,6 +78,16 @@ __host__ __device__ inline void aw_of_step(AdamwScalars &s, const AdamwFactors &
     s.key = aw_mix(f.seed ^ (unsigned)step);
 }
 
+// The gradients' factor x.  Below single precision's normal range it would lose bits that the gradients (of norms near the other end of that
+// range) have: they are then taken times 2^k, which the factors behind theirs take back.
+__host__ __device__ inline void aw_of_gradients(AdamwScalars &s, const AdamwFactors &f, double x) {
+    s.coef = (float)x;
+    if (!(x > 0.0 && x < 0x1p-126)) return;
+    const int k = x < 0x1p-190 ? 64 : -126 - ilogb(x);
+    s.coef = (float)ldexp(x, k);
+    s.c1 = (float)ldexp(1.0 - f.beta1, -k), s.c2 = (float)ldexp(1.0 - f.beta2, -2 * k);
+}
+
 // One thread's work, for the block; false: the gradients' norm is not finite.
 __device__ __noinline__ bool aw_scalars(const AdamwFactors &f, AdamwScalars &s) {
     bool fine = true;
@@ -86,7 +96,7 @@ __device__ __noinline__ bool aw_scalars(const AdamwFactors &f, AdamwScalars &s) 
         fine = norm <= 3.402823466e38f;
         double coef = f.max_norm / (double)norm;
         if (!(coef < 1.0)) coef = 1.0;             // 0 / 0 too: nothing to clip
-        s.coef = (float)(coef / f.loss_scale);
+        aw_of_gradients(s, f, coef / f.loss_scale);
     }
     if (f.d_lr || f.d_step) aw_of_step(s, f, f.d_lr ? (double)*f.d_lr : f.lr, f.d_step ? *f.d_step : f.step);
     return fine;
@@ -624,8 +634,8 @@ int qg_adamw(qgbdt_ctx *c, const qgbdt_adamw_tensor *t, int32_t n, const qgbdt_a
     f.loss_scale = o.loss_scale, f.step = o.step;
     f.seed = aw_mix(aw_mix((unsigned)o.seed) ^ (unsigned)(o.seed >> 32));
     f.d_lr = o.d_lr, f.d_step = reinterpret_cast<const long long *>(o.d_step), f.d_norm = o.d_norm;
-    f.s.coef = (float)(1.0 / o.loss_scale);
     f.s.b1 = (float)o.beta1, f.s.c1 = (float)(1.0 - o.beta1), f.s.b2 = (float)o.beta2, f.s.c2 = (float)(1.0 - o.beta2);
+    if (!o.d_norm) aw_of_gradients(f.s, f, 1.0 / o.loss_scale);
     aw_of_step(f.s, f, o.d_lr ? 0.0 : o.lr, o.d_step ? 1 : o.step);
     const bool packed = o.state_bits == 8;
     // An eps that is 2^23 times the root of 2^-126 or more in the first step already covers what a sum adds to the moments.  Smaller ones

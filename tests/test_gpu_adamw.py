@@ -199,6 +199,28 @@ def test_clipping_factor(ctx, fraction, scale, bits):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("norm,max_norm,scale", [(3e38, 1e-2, 1.0), (2e38, 1e-6, 4.0), (1e38, 1.0, 2.0 ** 20), (1e30, math.inf, 1e39), (3e38, 1e-40, 1.0), (1e38, 0.0, 1.0)])
+@pytest.mark.parametrize("eps", [1e-12, 1e-8])
+def test_clipping_factors_below_single_precision(ctx, eps, norm, max_norm, scale, bits):
+    """Factors below 2^-126 are as exact as others: gradients near the upper end of the range come out as the formula has them."""
+    case = Case([3000, 17, 5001], "f32", "f32", None, bits, 8, scale=1e33)
+    for t in (case.m + case.v + (case.e or [])):
+        t.zero_()
+    norm = torch.full((1,), norm, device="cuda")
+    coef = min(1.0, max_norm * scale / float(norm)) / scale
+    assert coef < 2.0 ** -126
+    was = before(case, ctx)
+    case.step(ctx, 5, 0.01, norm=norm, max_norm=max_norm, loss_scale=scale, eps=eps)
+    check_32(case, was, ctx, 5, 0.01, coef=coef, eps=eps)
+    if not math.isfinite(max_norm):      # the same without a norm
+        again = Case([3000, 17, 5001], "f32", "f32", None, bits, 8, scale=1e33)
+        for t in (again.m + again.v + (again.e or [])):
+            t.zero_()
+        again.step(ctx, 5, 0.01, loss_scale=scale, eps=eps)
+        assert all(torch.equal(a, b) for a, b in zip(again.all(), case.all()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("bad", [math.inf, math.nan, -math.inf])
 def test_a_norm_that_is_not_finite_leaves_everything(ctx, bad, bits):
     case = Case([3000, 17], "f32", "f32", "bf16", bits)
