@@ -415,7 +415,7 @@ int qgbdt_layer_norm_backward(qgbdt_ctx *ctx, const void *d_grad, int64_t ld_gra
  * approximations, 2^-22 of the change off, for which an exp_avg_sq below 2^-126 counts as that).  The
  * first step is 1.
  * d_norm: the gradients' norm as qgbdt_clip_grad_norm reports it for these gradients (NULL: no clipping);
- * where it is not finite nothing at all is written.  loss_scale: what the loss was multiplied with.
+ * where it is not finite nothing at all is written.  loss_scale: what the loss was multiplied with, 2^-127 at least.
  * d_lr, d_step: one number in device memory in place of lr or step (NULL: those), for a captured call.
  * Tensors are contiguous; count may be 0.  A tensor of parameters may be listed once only, and what
  * belongs to one tensor must not overlap (both are refused); nor may what is written of it (param, exp_avg,

@@ -68,7 +68,7 @@ int check_adamw(qgbdt_ctx *c, const qgbdt_adamw_tensor *t, int32_t n, const qgbd
     if (!o->d_lr && (!(o->lr >= 0.0) || !std::isfinite(o->lr))) return qg_fail(c, QGBDT_ERR_ARG, "lr must be finite and >= 0");
     if (!o->d_step && o->step < 1) return qg_fail(c, QGBDT_ERR_ARG, "step must be >= 1");
     if (o->d_norm && !(o->max_norm >= 0.0)) return qg_fail(c, QGBDT_ERR_ARG, "max_norm must be >= 0 (infinity: no clipping)");
-    if (!(o->loss_scale > 0.0) || !std::isfinite(o->loss_scale)) return qg_fail(c, QGBDT_ERR_ARG, "loss_scale must be finite and > 0");
+    if (!(o->loss_scale >= 0x1p-127) || !std::isfinite(o->loss_scale)) return qg_fail(c, QGBDT_ERR_ARG, "loss_scale must be finite and >= 2^-127");
     if (!qg_aligned(o->d_lr, 4) || !qg_aligned(o->d_step, 8) || !qg_aligned(o->d_norm, 4)) return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
     const bool packed = o->state_bits == 8;
     int64_t blocks = 0;

@@ -240,5 +240,9 @@ int main() {
     REFUSED(qgbdt_adamw_values(&c, in, in, in, out, out, both, 2, QGBDT_F32, nullptr));
     REFUSED(qgbdt_adamw_values(&c, in, nullptr, in, out, out, counts, 2, QGBDT_F32, nullptr));
     REFUSED(qgbdt_adamw_values(&c, in, in, in, out, out, counts, -1, QGBDT_F32, nullptr));
+
+    // a loss scale whose inverse single precision does not hold would make NaN of gradients that are zero
+    for (double v : {1e-300, 1e-39, 0x1p-128}) REFUSED(s.with(&qgbdt_adamw_options::loss_scale, v).run());
+    for (double v : {0x1p-127, 1e-38, 1e300}) TAKEN(s.with(&qgbdt_adamw_options::loss_scale, v).run());
     return failures ? 1 : 0;
 }
