@@ -387,8 +387,8 @@ int qgbdt_clip_grad_norm(qgbdt_ctx *ctx, const void *const *h_grads, void *const
  * d_rstd [n_rows] in single precision, each may be NULL.  eps >= 0; where var + eps is 0 (equal values
  * and no eps) rstd is infinite and the row NaN, as the formula has it.  The order of a row's sums goes by
  * dim and by the vectors that addresses and strides allow.  Rows of more than 8192 columns may use the
- * work buffer (8 bytes per 4096 elements).  d_out may be d_x itself with the
- * same stride; it must not overlap d_x otherwise.  dim in [1, 2^20]. */
+ * work buffer (8 bytes per 4096 elements).  d_out may be d_x itself with the same stride; rows of it that
+ * overlap d_x otherwise, the weight, the bias, mean or rstd are refused.  dim in [1, 2^20]. */
 int qgbdt_layer_norm(qgbdt_ctx *ctx, const void *d_x, int64_t ld_x, int32_t type, const void *d_weight, const void *d_bias,
                      int32_t weight_type, int64_t n_rows, int32_t dim, double eps, void *d_out, int64_t ld_out,
                      float *d_mean, float *d_rstd, void *stream);
@@ -398,7 +398,8 @@ int qgbdt_layer_norm(qgbdt_ctx *ctx, const void *d_x, int64_t ld_x, int32_t type
  * w = d_weight (NULL: 1).  d_grad, d_x and d_grad_x [n_rows][dim] of `type`; d_weight, d_grad_weight and
  * d_grad_bias [dim] of `weight_type`; the latter two may be NULL, and are zeros without rows.  The sums
  * over the rows are taken in parts whose number goes by the sizes and the GPU, and joined in their order.
- * d_grad_x may be d_grad or d_x itself with the same stride; it must not overlap them otherwise. */
+ * d_grad_x may be d_grad or d_x itself with the same stride; rows of it that overlap them otherwise, the
+ * weight, mean or rstd are refused. */
 int qgbdt_layer_norm_backward(qgbdt_ctx *ctx, const void *d_grad, int64_t ld_grad, const void *d_x, int64_t ld_x, int32_t type,
                               const float *d_mean, const float *d_rstd, const void *d_weight, int32_t weight_type,
                               int64_t n_rows, int32_t dim, void *d_grad_x, int64_t ld_grad_x, void *d_grad_weight,

@@ -9,6 +9,42 @@
 
 namespace {
 
+using wide = __int128;   // rows times their stride: up to 2^72 bytes
+
+// Rows of `width` bytes, `step` apart.
+struct Rows {
+    const void *p;
+    wide n, step, width;
+    wide at() const { return (wide) reinterpret_cast<uintptr_t>(p); }
+    wide end() const { return at() + (n - 1) * step + width; }
+};
+
+// The smallest x >= 0 with low <= a x mod m <= high, -1 if there is none; a < m, 0 <= low <= high < m.
+// No multiple of a in [low, high]: a x - m y is in there for the smallest y whose m y mod a is in [-high, -low] mod a.
+wide first_between(wide a, wide m, wide low, wide high) {
+    if (low == 0) return 0;
+    if (a == 0) return -1;
+    const wide x = (low + a - 1) / a;
+    if (x * a <= high) return x;
+    const wide y = first_between(m % a, a, (a - high % a) % a, (a - low % a) % a);
+    return y < 0 ? -1 : (low + m * y + a - 1) / a;
+}
+
+// Whether a row of a and a row of b have a byte in common.  Rows of one matrix may lie between another one's.
+bool meet(const Rows &a, const Rows &b) {
+    if (!a.p || !b.p || a.n < 1 || b.n < 1 || a.end() <= b.at() || b.end() <= a.at()) return false;
+    if (a.n > 1 && b.n == 1) return meet(b, a);
+    // row i of a begins t = from + i a.step behind b's first row; among b's rows from its first to its last
+    const wide from = a.at() - b.at(), last = (b.n - 1) * b.step + b.width - 1, begin = -a.width + 1;
+    const wide i0 = a.n == 1 || from >= begin ? 0 : (begin - from + a.step - 1) / a.step, i1 = a.n == 1 ? 0 : std::min(a.n - 1, (last - from) / a.step);
+    if (i0 > i1 || b.n == 1) return i0 <= i1;
+    // it meets one of them where (t - begin) mod b.step is `room` at most
+    const wide room = a.width + b.width - 2, m = b.step, t = (from + i0 * a.step - begin) % m;
+    if (t <= room || room >= m) return true;
+    const wide i = first_between(a.step % m, m, m - t, m - t + room);
+    return i >= 0 && i0 + i <= i1;
+}
+
 int check_layer_norm(qgbdt_ctx *c, LayerNormArgs &a, bool backward) {
     const int step = 16 / (a.type == QGBDT_F32 ? 4 : 2);
     qg_single_row(a.rows, a.dim, step, &a.ld_x);
@@ -29,6 +65,12 @@ int check_layer_norm(qgbdt_ctx *c, LayerNormArgs &a, bool backward) {
     if (!qg_aligned(a.x, w) || !qg_aligned(a.out, w) || !qg_aligned(a.grad, w) || !qg_aligned(a.weight, ww) || !qg_aligned(a.bias, ww) || !qg_aligned(a.d_weight, ww) ||
         !qg_aligned(a.d_bias, ww) || !qg_aligned(a.mean, 4) || !qg_aligned(a.rstd, 4))
         return qg_fail(c, QGBDT_ERR_ARG, "a pointer is not aligned to its element");
+    // the output is one of the inputs, or apart from them all
+    const Rows out{a.out, a.rows, (wide)a.ld_out * w, (wide)a.dim * w}, x{a.x, a.rows, (wide)a.ld_x * w, (wide)a.dim * w}, grad{a.grad, a.rows, (wide)a.ld_grad * w, (wide)a.dim * w};
+    auto apart = [&](const Rows &in) { return (out.p == in.p && (out.n <= 1 || out.step == in.step)) || !meet(out, in); };
+    if (!apart(x) || !apart(grad)) return qg_fail(c, QGBDT_ERR_ARG, "the output's rows overlap an input's and are not the same");
+    for (const Rows &in : {Rows{a.weight, 1, 0, (wide)a.dim * ww}, Rows{a.bias, 1, 0, (wide)a.dim * ww}, Rows{a.mean, 1, 0, (wide)a.rows * 4}, Rows{a.rstd, 1, 0, (wide)a.rows * 4}})
+        if (meet(out, in)) return qg_fail(c, QGBDT_ERR_ARG, "the output's rows overlap the weight, the bias, mean or rstd");
     return QGBDT_OK;
 }
 

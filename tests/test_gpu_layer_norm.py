@@ -338,3 +338,30 @@ def test_bookkeeping(ctx):
             call()
         assert e.value.code == binding.ERR_ARG
     assert torch.equal(ctx.layer_norm(x, w, b).out, r.out)
+
+
+def test_outputs_over_inputs(ctx):
+    """An output that overlaps an input without being it is refused; one whose rows lie between the input's is not."""
+    from paper_2207_09682_b200 import binding
+    _, _, w, b = make(1, 40, torch.float32, torch.float32)
+    wide = torch.randn((60, 100), generator=gen(2), device="cuda")
+    x, was = wide[:, :40], wide.clone()
+    for out in (wide[:, 1:41], wide[:, 39:79], wide[1:, :40], wide.view(-1)[:60 * 50].view(60, 50)[:, :40], w.expand(1, 40), b.view(1, 40)):
+        k = min(len(out), 59)
+        with pytest.raises(binding.QgbdtError) as e:
+            ctx.layer_norm(x[:k], w, b, out=out[:k])
+        assert e.value.code == binding.ERR_ARG
+    stats = torch.zeros(59, device="cuda")
+    for g, y in ((x, wide[:, 60:]), (wide[:, 60:], x)):
+        with pytest.raises(binding.QgbdtError):
+            ctx.layer_norm_backward(g[:59], y[:59], stats, stats, w, grad_x=wide[1:, 20:60] if g is x else wide[:59, 30:70])
+    with pytest.raises(binding.QgbdtError):
+        ctx.layer_norm_backward(x[:1], wide[:1, 60:], stats[:1], stats[:1], w, grad_x=w.view(1, 40))
+    assert torch.equal(wide, was)
+    r = ctx.layer_norm(x, w, b, out=wide[:, 40:80])
+    check_forward(r, was[:, :40], w, b)
+    assert torch.equal(wide[:, :40], was[:, :40]) and torch.equal(wide[:, 80:], was[:, 80:])
+    normed = r.out.clone()
+    got = ctx.layer_norm_backward(x, r.out, r.mean, r.rstd, w, grad_x=r.out)
+    check_backward(got, was[:, :40], normed, r.mean, r.rstd, w)
+    assert torch.equal(wide[:, :40], was[:, :40]) and torch.equal(wide[:, 80:], was[:, 80:])
