@@ -428,12 +428,13 @@ def _layer_norm(self, x, weight=None, bias=None, eps: float = 1e-5, out=None, st
     return LayerNorm(*(_tensors or _load_tensors()).layer_norm(self.h.value or 0, self.device, x, weight, bias, eps, out))
 
 
-def _layer_norm_backward(self, grad_out, x, mean, rstd, weight=None, grad_x=None, stream=None) -> tuple:
+def _layer_norm_backward(self, grad_out, x, mean, rstd, weight=None, grad_x=None, stream=None, bias=None) -> tuple:
     """qgbdt_layer_norm_backward: (grad_x [N, D], grad_weight [D], grad_bias [D]), mean and rstd as layer_norm gave them; the latter
-    two are of the weight's type, None without a weight.  `grad_x` may be grad_out or x itself."""
+    two are of the weight's type, None without a weight.  `bias` (its values are not read) gives grad_bias of its type without a
+    weight too.  `grad_x` may be grad_out or x itself."""
     if stream is not None:
-        return _elsewhere(stream, self.layer_norm_backward, grad_out, x, mean, rstd, weight, grad_x)
-    return (_tensors or _load_tensors()).layer_norm_backward(self.h.value or 0, self.device, grad_out, x, mean, rstd, weight, grad_x)
+        return _elsewhere(stream, self.layer_norm_backward, grad_out, x, mean, rstd, weight, grad_x, None, bias)
+    return (_tensors or _load_tensors()).layer_norm_backward(self.h.value or 0, self.device, grad_out, x, mean, rstd, weight, grad_x, bias)
 
 
 def adamw_states(params, bits: int = 32) -> tuple:

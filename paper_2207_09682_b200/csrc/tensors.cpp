@@ -416,7 +416,7 @@ PyObject *py_layer_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     END_HANDLE_TH_ERRORS
 }
 
-// layer_norm_backward(ctx, device, grad_out, x, mean, rstd, weight, grad_x) -> (grad_x, grad_weight or None, grad_bias or None)
+// layer_norm_backward(ctx, device, grad_out, x, mean, rstd, weight, grad_x, bias) -> (grad_x, grad_weight or None, grad_bias or None)
 PyObject *py_layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     HANDLE_TH_ERRORS
     Call c;
@@ -424,24 +424,23 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n
     Affine w;
     Output gx;
     void *mean, *rstd;
-    if (!c.take(args, nargs, 8) || !grad.take_input(c, args[2], "grad_out") || !x.take_input(c, args[3], "x")) return nullptr;
+    if (!c.take(args, nargs, 9) || !grad.take_input(c, args[2], "grad_out") || !x.take_input(c, args[3], "x")) return nullptr;
     if (x.type < 0) return refuse("x must be float32, bfloat16 or float16");
     if (grad.type != x.type || grad.n != x.n || grad.d != x.d) return refuse("grad_out and x differ in size or type");
     if (args[4] == Py_None || args[5] == Py_None) return refuse("mean and rstd are those of the forward call");
     if (!words(c, args[4], "mean", at::kFloat, x.n, &mean) || !words(c, args[5], "rstd", at::kFloat, x.n, &rstd) ||
-        !w.take(c, x, args[6], Py_None) || !gx.take_or_make(c, args[7], "grad_x", x))
+        !w.take(c, x, args[6], args[8]) || !gx.take_or_make(c, args[7], "grad_x", x))
         return nullptr;
-    at::Tensor gw, gb;
-    if (args[6] != Py_None) {
-        gw = fresh({x.d}, w.scalar, c), gb = fresh({x.d}, w.scalar, c);
-    }
+    at::Tensor gw, gb;     // a weight's call has always given both
+    if (args[6] != Py_None) gw = fresh({x.d}, w.scalar, c);
+    if (args[6] != Py_None || args[8] != Py_None) gb = fresh({x.d}, w.scalar, c);
     const int rc = lib.layer_norm_backward(c.ctx, grad.p(), grad.ld, x.p(), x.ld, x.type, (const float *)mean, (const float *)rstd, w.weight, w.type, x.n,
                                            (int32_t)x.d, gx.r.p(), gx.r.ld, gw.defined() ? gw.data_ptr() : nullptr, gb.defined() ? gb.data_ptr() : nullptr,
                                            c.stream);
     if (rc != QGBDT_OK) return c.result(rc);
     PyObject *const x_grad = gx.give(args[7]);
-    if (!gw.defined()) return Py_BuildValue("(NOO)", x_grad, Py_None, Py_None);
-    PyObject *const weight_grad = THPVariable_Wrap(gw), *const bias_grad = THPVariable_Wrap(gb);
+    auto give = [](const at::Tensor &t) { return t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None); };
+    PyObject *const weight_grad = give(gw), *const bias_grad = give(gb);
     return Py_BuildValue("(NNN)", x_grad, weight_grad, bias_grad);
     END_HANDLE_TH_ERRORS
 }

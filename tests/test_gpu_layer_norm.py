@@ -365,3 +365,22 @@ def test_outputs_over_inputs(ctx):
     got = ctx.layer_norm_backward(x, r.out, r.mean, r.rstd, w, grad_x=r.out)
     check_backward(got, was[:, :40], normed, r.mean, r.rstd, w)
     assert torch.equal(wide[:, :40], was[:, :40]) and torch.equal(wide[:, 80:], was[:, 80:])
+
+
+@pytest.mark.parametrize("rows,dim", [(70, 64), (70, 129), (3000, 40), (200, 2048), (3, 20000), (0, 16)])
+def test_bias_without_a_weight_has_a_gradient(ctx, rows, dim):
+    from paper_2207_09682_b200 import binding
+    for dtype, btype in ((torch.float16, torch.float32), (torch.bfloat16, torch.bfloat16)):
+        x, g, w, b = make(rows, dim, dtype, btype, 0, 7)
+        r = ctx.layer_norm(x, None, b)
+        gx, gw, gb = ctx.layer_norm_backward(g, x, r.mean, r.rstd, bias=b)
+        assert gw is None and gb.dtype == btype
+        within(gb, g.double().sum(0), (rows / 16 + 204) * U * g.double().abs().sum(0), "grad_bias")
+        plain = ctx.layer_norm_backward(g, x, r.mean, r.rstd)
+        assert torch.equal(gx, plain[0]) and plain[1] is None and plain[2] is None
+        both = ctx.layer_norm_backward(g, x, r.mean, r.rstd, w, bias=b, stream=torch.cuda.current_stream())
+        want = ctx.layer_norm_backward(g, x, r.mean, r.rstd, w)
+        assert all(torch.equal(p, q) for p, q in zip(both, want))
+        for bad in (b[1:], b.double(), b.cpu()):
+            with pytest.raises(binding.QgbdtError):
+                ctx.layer_norm_backward(g, x, r.mean, r.rstd, bias=bad)
