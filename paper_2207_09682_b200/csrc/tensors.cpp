@@ -82,12 +82,21 @@ struct Call {
     PyObject *result(int rc) const { return rc == QGBDT_OK ? nullptr : fail(rc, lib.last_error(ctx)); }
 };
 
-// Warns where autograd would be expected to record the call; false with an exception where warnings are errors.
+// Whether autograd would have to know what is done with the tensor: it requires a gradient, or has a tangent (of forward mode).
+bool followed(const at::Tensor &t) { return t.requires_grad() || t._fw_grad(0).defined(); }
+
+// Warns where autograd would be expected to record the call or to carry a tangent on; false with an exception where warnings are errors.
 bool unrecorded(const at::Tensor &t, const char *name) {
-    if (!at::GradMode::is_enabled() || !t.requires_grad()) return true;
+    if (!followed(t)) return true;
     char text[256];
-    snprintf(text, sizeof(text), "%s requires a gradient, but autograd does not record this call and its result has no graph; the "
-             "operators' *_backward calls give gradients (torch.no_grad() or detach() silences this)", name);
+    if (at::GradMode::is_enabled() && t.requires_grad()) {
+        snprintf(text, sizeof(text), "%s requires a gradient, but autograd does not record this call and its result has no graph; the "
+                 "operators' *_backward calls give gradients (torch.no_grad() or detach() silences this)", name);
+        if (PyErr_WarnEx(PyExc_UserWarning, text, 1)) return false;
+    }
+    if (!t._fw_grad(0).defined()) return true;
+    snprintf(text, sizeof(text), "%s has a tangent, but this call does not carry it on and its result has none (torch.autograd.forward_ad.unpack_dual() "
+             "gives the tensor without one)", name);
     return PyErr_WarnEx(PyExc_UserWarning, text, 1) == 0;
 }
 
@@ -344,7 +353,7 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(seq, i), name);
             ok = t != nullptr;
             if (!ok) break;
-            if (first && t->requires_grad()) recorded = t;
+            if (first && followed(*t)) recorded = t;
             const int type = element(*t);
             if (!c.here(*t) || !t->is_contiguous() || type < 0) {
                 refuse(name, "must be contiguous float32, bfloat16 or float16 tensors on the context's device");
@@ -515,7 +524,7 @@ PyObject *py_adamw(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
         const at::ScalarType state = packed ? at::kByte : at::kFloat;
         if (m->scalar_type() != state || v->scalar_type() != state)
             return refuse(packed ? "states with exponents must be uint8" : "states must be float32 (or uint8, with exponents)");
-        if (g->requires_grad()) recorded = g;
+        if (followed(*g)) recorded = g;
         t.param = p->data_ptr(), t.grad = g->data_ptr(), t.exp_avg = m->data_ptr(), t.exp_avg_sq = v->data_ptr();
         if (packed) {
             const at::Tensor *e = exponents.get(c, i);
