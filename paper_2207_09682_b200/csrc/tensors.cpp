@@ -88,13 +88,14 @@ bool followed(const at::Tensor &t) { return t.requires_grad() || t._fw_grad(0).d
 // Warns where autograd would be expected to record the call or to carry a tangent on; false with an exception where warnings are errors.
 bool unrecorded(const at::Tensor &t, const char *name) {
     if (!followed(t)) return true;
+    const bool tangent = t._fw_grad(0).defined();     // (t may be gone after a warning)
     char text[256];
     if (at::GradMode::is_enabled() && t.requires_grad()) {
         snprintf(text, sizeof(text), "%s requires a gradient, but autograd does not record this call and its result has no graph; the "
                  "operators' *_backward calls give gradients (torch.no_grad() or detach() silences this)", name);
         if (PyErr_WarnEx(PyExc_UserWarning, text, 1)) return false;
     }
-    if (!t._fw_grad(0).defined()) return true;
+    if (!tangent) return true;
     snprintf(text, sizeof(text), "%s has a tangent, but this call does not carry it on and its result has none (torch.autograd.forward_ad.unpack_dual() "
              "gives the tensor without one)", name);
     return PyErr_WarnEx(PyExc_UserWarning, text, 1) == 0;
@@ -342,18 +343,18 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     std::vector<int32_t> types;
     const bool to_out = args[4] != Py_None, in_place = !to_out && max_norm <= std::numeric_limits<double>::max();
     THPObjectPtr held[2];   // the tensors stay alive until the call has been made
+    at::Tensor recorded;
     auto take = [&](PyObject *list, const char *name, bool first) {
         PyObject *const seq = PySequence_Fast(list, "expected a list of tensors");
         if (!seq) return false;
         held[!first] = THPObjectPtr(seq);
-        const at::Tensor *recorded = nullptr;
         const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
         bool ok = first || n == (Py_ssize_t)in.size() || (refuse("out must match the gradients in number"), false);
         for (Py_ssize_t i = 0; ok && i < n; ++i) {
             const at::Tensor *t = tensor(PySequence_Fast_GET_ITEM(seq, i), name);
             ok = t != nullptr;
             if (!ok) break;
-            if (first && followed(*t)) recorded = t;
+            if (first && followed(*t)) recorded = *t;
             const int type = element(*t);
             if (!c.here(*t) || !t->is_contiguous() || type < 0) {
                 refuse(name, "must be contiguous float32, bfloat16 or float16 tensors on the context's device");
@@ -367,9 +368,17 @@ PyObject *py_clip_grad_norm(PyObject *, PyObject *const *args, Py_ssize_t nargs)
                 out.push_back(t->data_ptr());
             }
         }
-        return ok && (!recorded || unrecorded(*recorded, name));
+        return ok;
     };
-    if (!take(args[2], "gradients", true) || (to_out && !take(args[4], "out", false))) return nullptr;
+    auto collect = [&] {
+        auto once = [&](int k, PyObject *o) { return held[k].get() ? held[k].get() : o; };     // what a generator gave
+        return take(once(0, args[2]), "gradients", true) && (!to_out || take(once(1, args[4]), "out", false));
+    };
+    if (!collect()) return nullptr;
+    if (recorded.defined()) {     // a warning's handler may have changed the lists, and with them what holds the tensors
+        in.clear(), out.clear(), sizes.clear(), types.clear();
+        if (!unrecorded(recorded, "gradients") || !collect()) return nullptr;
+    }
     const at::Tensor norm = at::empty({1}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, (c10::DeviceIndex)c.device));
     const int rc = lib.clip_grad_norm(c.ctx, in.data(), to_out ? out.data() : nullptr, sizes.data(), types.data(), (int32_t)in.size(), max_norm,
                                       norm.data_ptr<float>(), c.stream);
@@ -512,36 +521,41 @@ PyObject *py_adamw(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     if (PyErr_Occurred()) return nullptr;
     o.d_step = (const int64_t *)d_step, o.d_lr = (const float *)d_lr, o.d_norm = (const float *)d_norm, o.state_bits = packed ? 8 : 32;
     std::vector<qgbdt_adamw_tensor> list((size_t)params.n);
-    const at::Tensor *recorded = nullptr;
-    for (Py_ssize_t i = 0; i < params.n; ++i) {
-        const at::Tensor *p = params.get(c, i), *g = p ? grads.get(c, i) : nullptr, *m = g ? ms.get(c, i) : nullptr, *v = m ? vs.get(c, i) : nullptr;
-        if (!v) return nullptr;
-        qgbdt_adamw_tensor &t = list[(size_t)i];
-        t.count = p->numel();
-        t.param_type = element(*p), t.grad_type = element(*g);
-        if (t.param_type < 0 || t.grad_type < 0) return refuse("params and grads must be float32, bfloat16 or float16");
-        if (g->numel() != t.count || m->numel() != t.count || v->numel() != t.count) return refuse("grads and states must match the parameters in sizes");
-        const at::ScalarType state = packed ? at::kByte : at::kFloat;
-        if (m->scalar_type() != state || v->scalar_type() != state)
-            return refuse(packed ? "states with exponents must be uint8" : "states must be float32 (or uint8, with exponents)");
-        if (followed(*g)) recorded = g;
-        t.param = p->data_ptr(), t.grad = g->data_ptr(), t.exp_avg = m->data_ptr(), t.exp_avg_sq = v->data_ptr();
-        if (packed) {
-            const at::Tensor *e = exponents.get(c, i);
-            if (!e) return nullptr;
-            if (e->scalar_type() != at::kByte || e->dim() != 2 || e->size(0) != (t.count + 255) / 256 || e->size(1) != 2)
-                return refuse("exponents must be uint8 [ceil(elements / 256), 2]");
-            t.exponents = (uint8_t *)e->data_ptr();
+    at::Tensor recorded;
+    auto collect = [&] {
+        for (Py_ssize_t i = 0; i < params.n; ++i) {
+            const at::Tensor *p = params.get(c, i), *g = p ? grads.get(c, i) : nullptr, *m = g ? ms.get(c, i) : nullptr, *v = m ? vs.get(c, i) : nullptr;
+            if (!v) return false;
+            qgbdt_adamw_tensor &t = list[(size_t)i] = {};
+            t.count = p->numel();
+            t.param_type = element(*p), t.grad_type = element(*g);
+            if (t.param_type < 0 || t.grad_type < 0) return refuse("params and grads must be float32, bfloat16 or float16"), false;
+            if (g->numel() != t.count || m->numel() != t.count || v->numel() != t.count) return refuse("grads and states must match the parameters in sizes"), false;
+            const at::ScalarType state = packed ? at::kByte : at::kFloat;
+            if (m->scalar_type() != state || v->scalar_type() != state)
+                return refuse(packed ? "states with exponents must be uint8" : "states must be float32 (or uint8, with exponents)"), false;
+            if (followed(*g)) recorded = *g;
+            t.param = p->data_ptr(), t.grad = g->data_ptr(), t.exp_avg = m->data_ptr(), t.exp_avg_sq = v->data_ptr();
+            if (packed) {
+                const at::Tensor *e = exponents.get(c, i);
+                if (!e) return false;
+                if (e->scalar_type() != at::kByte || e->dim() != 2 || e->size(0) != (t.count + 255) / 256 || e->size(1) != 2)
+                    return refuse("exponents must be uint8 [ceil(elements / 256), 2]"), false;
+                t.exponents = (uint8_t *)e->data_ptr();
+            }
+            if (copied && !copies.none(i)) {
+                const at::Tensor *k = copies.get(c, i);
+                if (!k) return false;
+                t.copy_type = element(*k);
+                if (t.copy_type < 0 || k->numel() != t.count) return refuse("copies must match the parameters in sizes and be float32, bfloat16 or float16"), false;
+                t.copy = k->data_ptr();
+            }
         }
-        if (copied && !copies.none(i)) {
-            const at::Tensor *k = copies.get(c, i);
-            if (!k) return nullptr;
-            t.copy_type = element(*k);
-            if (t.copy_type < 0 || k->numel() != t.count) return refuse("copies must match the parameters in sizes and be float32, bfloat16 or float16");
-            t.copy = k->data_ptr();
-        }
-    }
-    if (recorded && !unrecorded(*recorded, "grads")) return nullptr;
+        return true;
+    };
+    if (!collect()) return nullptr;
+    // a warning's handler may have changed the lists, and with them what holds the tensors
+    if (recorded.defined() && !(unrecorded(recorded, "grads") && collect())) return nullptr;
     const int rc = lib.adamw(c.ctx, list.data(), (int32_t)params.n, &o, c.stream);
     if (rc != QGBDT_OK) return c.result(rc);
     for (const List *l : {&params, &ms, &vs, &exponents, &copies}) l->written_all();
