@@ -536,3 +536,33 @@ def test_bookkeeping(ctx):
         ctx.adamw(iter([p]), iter([g]), iter([m]), iter([v]), step, torch.ones(1, device="cuda"), copies=iter([c]), stream=stream)
     torch.cuda.synchronize()
     assert torch.equal(c, p.detach())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("tensors", [15, 16, 17, 55, 56, 57, 400, 401, 801])
+def test_where_the_tables_of_tensors_change(ctx, tensors, bits):
+    """Up to 16, 56 and 400 tensors per launch, and more launches; the values of 8-bit states through all of them."""
+    sizes = [(53 * i + 300) % 900 for i in range(tensors)]
+    case = Case(sizes, "f32", "bf16", "bf16", bits, tensors)
+    was = before(case, ctx)
+    case.step(ctx, 3, 0.02, seed=11)
+    check_32(case, was, ctx, 3, 0.02)
+    if bits == 8:
+        check_codes(case, was, 3, 11)
+        for dtype in (torch.float32, torch.bfloat16):
+            m, v = ctx.adamw_values(case.m, case.v, case.e, dtype=dtype)
+            for i, n in enumerate(sizes):
+                assert m[i].shape == v[i].shape == (n,) and m[i].dtype == v[i].dtype == dtype
+                assert torch.equal(m[i].double(), decode(case.m[i], case.e[i][:, 0], 897, True)) and torch.equal(v[i].double(), decode(case.v[i], case.e[i][:, 1], 769, False))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("tensors", [3, 30, 500])
+def test_small_eps_in_many_tensors(ctx, tensors, bits):
+    """An eps that needs the maximum goes through the large tables whatever the number of tensors."""
+    case = Case([(71 * i + 1) % 700 for i in range(tensors)], "f32", "f16", None, bits, tensors)
+    was = before(case, ctx)
+    case.step(ctx, 3, 0.02, eps=0.0, seed=12)
+    check_32(case, was, ctx, 3, 0.02, eps=0.0)
+    if bits == 8:
+        check_codes(case, was, 3, 12)
