@@ -83,7 +83,7 @@ struct Call {
 };
 
 // Whether autograd would have to know what is done with the tensor: it requires a gradient, or has a tangent (of forward mode).
-bool followed(const at::Tensor &t) { return t.requires_grad() || t._fw_grad(0).defined(); }
+bool followed(const at::Tensor &t) { return t.unsafeGetTensorImpl()->autograd_meta() && (t.requires_grad() || t._fw_grad(0).defined()); }   // (mostly not even asked)
 
 // Warns where autograd would be expected to record the call or to carry a tangent on; false with an exception where warnings are errors.
 bool unrecorded(const at::Tensor &t, const char *name) {
