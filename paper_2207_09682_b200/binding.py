@@ -357,7 +357,8 @@ class SoftmaxCE(NamedTuple):
 
 
 class LayerNorm(NamedTuple):
-    """Outputs of Context.layer_norm: out [N, D] of the rows' type, mean [N] and rstd [N] float32."""
+    """Outputs of Context.layer_norm: out [N, D] of the rows' type, mean [N] and rstd [N] float32 (tensors of their own in one storage:
+    either one saved to a file brings the other along)."""
     out: torch.Tensor
     mean: torch.Tensor
     rstd: torch.Tensor
@@ -365,7 +366,7 @@ class LayerNorm(NamedTuple):
 
 # The arguments of the calls below are taken apart by the extension module _tensors (csrc/tensors.cpp): tensors of the
 # context's device, matrices with contiguous rows of any row stride; anything else is refused with ERR_ARG.  Autograd records
-# none of them: gradients come from the *_backward calls (an input that requires one is taken with a warning).
+# none of them: gradients come from the *_backward calls (an input that requires one, or has a tangent, is taken with a warning).
 
 def _elsewhere(stream, call, *args):
     """A call on another stream than the current one: its outputs are made there, and the allocator is told that its

@@ -7,9 +7,10 @@
 // bits; a warp works on one of them at a time.  One launch for up to 400 tensors.
 //
 // With states in 32 bits it is bound by memory traffic: 200 M elements with 32-bit gradients and a 16-bit copy, 6.0 GB, take
-// 0.957 ms (6.3 TB/s; 19 instructions per element).  With states in 8 bits half the bytes are left and three times the
-// instructions (63, 27 of them on the integer pipe): 73.7 M elements with 16-bit gradients and copies, 1.18 GB, take 0.21 ms (5.6 TB/s,
-// 69 % of the issue slots); parameters in 16 bits alone, 10 bytes an element, are bound by instructions (30 M: 85 us, 3.5 TB/s).
+// 0.96 ms (6.2 TB/s; 19 instructions per element).  With states in 8 bits half the bytes are left and three times the
+// instructions (63, 27 of them on the integer pipe): 73.7 M elements with 16-bit gradients and copies, 1.18 GB, take 0.20 ms (5.9 TB/s,
+// 69 % of the issue slots); parameters in 16 bits alone, 10 bytes an element, are bound by instructions (30 M: 84 us, 3.6 TB/s; in few
+// tensors 80 % of the issue slots and 67 % of the integer pipe, which warps wait for most).
 #include <cmath>
 
 #include "ops_internal.cuh"

@@ -6,8 +6,8 @@
 // Sums and statistics are held in single precision; an output is rounded once, when it is written.
 //
 // Rows of up to 8192 columns (forward mostly 16384) are held in registers and read once: bound by memory traffic where a row's threads have many
-// elements (16384 x 8192 bf16: 90 us, 6.0 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have few
-// (65536 x 256 bf16: 12 us, 5.7 TB/s; 13 instructions per element, of which the elements' own are 5) and where rows start anywhere
+// elements (16384 x 8192 bf16: 90 to 99 us, 5.4 to 6.0 TB/s; gradients of 65536 x 1024 bf16: 73 us, 5.5 TB/s), by instructions where they have
+// few (65536 x 256 bf16: 13 us, 5.1 TB/s; 13 instructions per element, of which the elements' own are 5) and where rows start anywhere
 // (60000 x 1001 bf16: 67 us, 3.6 TB/s; 25 instructions).  Small calls are bound by the launch, and, where the sums over the rows come from
 // several blocks, by a second one (3.5 us).  Longer rows are cut into segments and read twice.
 #include <type_traits>
@@ -21,7 +21,9 @@ namespace {
 // segment's share of the row's sums (forward: mean and sum of squared differences from it, backward: sums of w g and w g xh), a second one
 // joins the shares of the row in their order, in every block that needs them, and writes.  Inputs are read twice, the
 // second time from L2 where they fit: 1.5 times the bytes forward, 1.67 backward.  One row of 2^20 columns in bf16 takes 8.6 us (by
-// a single block: 354), 2048 x 32768 136 us, gradients of 4096 x 16384 165 us.
+// a single block: 354), 2048 x 32768 136 us, gradients of 4096 x 16384 164 us.  That is 2.2 and 1.6 times what those bytes take: the shares are
+// bound by instructions (18 per element, 69 % of the issue slots), the writers by latency (a row is asked for when the one before it is
+// done: 45 % of the issue slots, 4 to 5 warps waiting for memory per instruction).
 
 constexpr int LN_THREADS = 256, LN_PIECE = 16;      // elements per thread
 constexpr int LN_SEGMENT = LN_THREADS * LN_PIECE;
@@ -257,7 +259,7 @@ int ln_join(qgbdt_ctx *c, const LayerNormArgs &a, const float *partial, int slic
 // and rows whose threads have few elements are worked on two at a time, which share the exchanges of their sums.
 
 constexpr int LN_ROW = 8192;     // elements of a row, at most
-constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 49 us, in segments 136)
+constexpr int LN_LONG = 16384;   // forward, vectors, where the copies ahead fit (4096 x 16384 bf16: 50 us, in segments 136)
 constexpr int LN_SHARED = 224 * 1024;   // bytes of shared memory that a block can have for them
 // What a launch may give a block without leave for more, and with it: 48 and 227 KB, less what the kernels hold themselves.
 using LnParts = float2[2][32];
