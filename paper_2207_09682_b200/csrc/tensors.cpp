@@ -449,7 +449,7 @@ PyObject *py_layer_norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n
     if (!words(c, args[4], "mean", at::kFloat, x.n, &mean) || !words(c, args[5], "rstd", at::kFloat, x.n, &rstd) ||
         !w.take(c, x, args[6], args[8]) || !gx.take_or_make(c, args[7], "grad_x", x))
         return nullptr;
-    at::Tensor gw, gb;     // a weight's call has always given both
+    at::Tensor gw, gb;     // a weight alone gives both
     if (args[6] != Py_None) gw = fresh({x.d}, w.scalar, c);
     if (args[6] != Py_None || args[8] != Py_None) gb = fresh({x.d}, w.scalar, c);
     const int rc = lib.layer_norm_backward(c.ctx, grad.p(), grad.ld, x.p(), x.ld, x.type, (const float *)mean, (const float *)rstd, w.weight, w.type, x.n,
